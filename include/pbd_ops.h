@@ -100,13 +100,93 @@ size_t pbd_op_lm_head_workspace_bytes(int32_t M, int32_t H, int32_t V);
 pbd_status pbd_op_lm_head_argmax(int32_t M, int32_t H, int32_t V, const void *d_x, const void *d_embed,
                                  int32_t *d_ids, float *d_logits_opt, void *d_ws, size_t ws_bytes, void *d_stream);
 
-/* Device status of the last pbd_op_linear or pbd_op_lm_head_argmax call that used the
- * workspace d_ws (the 1024-byte-aligned pointer that call was given): waits for d_stream, then
- * reads the status word at the start of d_ws.  PBD_OK when no kernel latched an error;
- * PBD_ERR_DEVICE with the latched code in *h_device_code (may be NULL) otherwise, and that call's
- * outputs are invalid; PBD_ERR_INVALID_ARG for a null or misaligned d_ws; PBD_ERR_CUDA if the
- * stream failed.  A device wait bounded at one second that runs out is the only way these kernels
- * latch an error (the kernels' bounds on their inputs are checked on the host). */
+/* Types of values that the calls below take. */
+typedef enum { PBD_BF16 = 0, PBD_FP16 = 1, PBD_FP32 = 2 } pbd_dtype;
+
+/* A paged key-value cache that the caller owns: one layer's K and V for `batch` sequences.
+ * Slot j of sequence b is slot j % page_size of page d_page_table[b * max_pages + j / page_size]; its K (and likewise V)
+ * of one head starts at d_k + page * stride_page + head * stride_head + (j % page_size) * stride_slot, strides in
+ * values, head_dim values in a row.  [page][head][slot][d] and [page][slot][head][d] are both expressed so.
+ * Requirements: head_dim 64, 128 or 256; d_k and d_v 16-byte aligned and every stride a multiple of 8; batch <= 1024.
+ * Pages of a sequence's slots [0, d_lens[b]) are read; table entries behind them are not.  Sequences may share pages that
+ * a call only reads.  Which token a slot holds is up to the caller: attention does not depend on the order. */
+typedef struct {
+    void *d_k, *d_v;
+    int32_t dtype;                    /* PBD_BF16 or PBD_FP16 */
+    int32_t n_pages, page_size, n_kv_heads, head_dim, batch, max_pages;
+    int64_t stride_page, stride_head, stride_slot;
+    const int32_t *d_page_table;      /* [batch, max_pages] */
+    const int32_t *d_lens;            /* [batch] cached tokens, 0 to max_pages * page_size */
+    float *d_weights;                 /* [batch, n_kv_heads, max_pages * page_size] accumulated attention weight, or NULL */
+    int32_t *d_positions;             /* the same shape: position of the token in each slot, or NULL */
+} pbd_kv_pages;
+
+/* Workspace bytes pbd_op_decode_attention needs (0 if unsupported); only the cache's sizes, strides and type are read. */
+size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n_q_heads, int32_t accumulate);
+
+/* Attention of one new token per sequence over a paged cache (the attention step of a plain decoding pass, on the
+ * caller's own cache): query head h reads KV head h / (n_q_heads / n_kv_heads),
+ *     s_j = q . k_j,  p = softmax(scale * s),  out = sum_j p_j v_j,  lse = ln sum_j exp(scale * s_j).
+ * d_q: batch rows q_stride values apart of [n_q_heads, head_dim]; d_out [batch, n_q_heads, head_dim]; both of the cache's
+ * type.  d_lse_opt [batch, n_q_heads] fp32 or NULL.  A sequence without a slot gets zeros and -inf.
+ * d_k_new, d_v_new (both or neither): the new token's own K and V, batch rows new_stride values apart of [n_kv_heads,
+ * head_dim].  They are stored into slot d_lens[b] (whose page the table must name) and attended to as well; its position
+ * goes to d_positions from d_new_positions [batch] when both are there.  d_lens is not changed: a layer's call leaves it
+ * to the caller, who raises it once all layers are through.
+ * accumulate: adds to d_weights[b, kv head, j] the p_j of all query heads of the group; the slot of a new token starts
+ * from 0.  The sums run in an order fixed by the sizes and lengths: repeated calls give the same bits.
+ * Score, softmax and output sums are fp32; p is split into two 16-bit parts for the tensor cores, so that the output's
+ * error is that of its one rounding.
+ * Requirements: n_q_heads a multiple of n_kv_heads; scale > 0; d_q, d_out, d_k_new and d_v_new 16-byte aligned, row strides
+ * multiples of 8; d_out lies over nothing that is read.  The workspace (1024-byte aligned) is scratch; its first word
+ * is the status word for pbd_op_status: a length outside [0, max_pages * page_size] (with a new token: one less) or a
+ * page outside [0, n_pages) is reported there, read as nothing, and makes the outputs invalid. */
+pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, float scale, const void *d_q, int64_t q_stride,
+                                   const void *d_k_new, const void *d_v_new, int64_t new_stride,
+                                   const int32_t *d_new_positions, int32_t accumulate, void *d_out, float *d_lse_opt,
+                                   void *d_ws, size_t ws_bytes, void *d_stream);
+
+/* Workspace bytes pbd_op_evict needs (0 if unsupported); only the cache's sizes, strides and type are read. */
+size_t pbd_op_evict_workspace_bytes(const pbd_kv_pages *kv, int32_t n_keep);
+
+/* Eviction from a paged cache by accumulated attention weight.  Of the d_lens[b] slots of each sequence and KV head the
+ * min(d_lens[b], n_keep) that rank first stay: slots whose position is below n_sink or at least d_next_positions[b] -
+ * n_recent, then by d_weights (NaN last), equal ones by the lower slot.  Kept slots at or behind n_keep move (K, V, weight,
+ * position) into the places in front that came free, the i-th into the i-th; all others stay where they are, so the
+ * kept ones are slots [0, n_keep) afterwards, in no order of their tokens.  Sequences of at most n_keep slots keep all.
+ * K and V move in place.  Weights and positions of the kept slots go to d_out_weights and d_out_positions, shaped like
+ * d_weights and d_positions: those arrays themselves, or others apart from them; slots behind the kept ones are not
+ * written.  d_lens is not changed: the caller lowers it to at most n_keep once all layers are through.
+ * Requirements: n_recent + n_sink <= n_keep; no two sequences share a page.  The workspace (1024-byte aligned) is scratch;
+ * its first word is the status word for pbd_op_status, as for pbd_op_decode_attention. */
+pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent, int32_t n_sink,
+                        const int32_t *d_next_positions, float *d_out_weights, int32_t *d_out_positions, void *d_ws,
+                        size_t ws_bytes, void *d_stream);
+
+/* Workspace bytes pbd_op_token_logprobs needs (0 if unsupported). */
+size_t pbd_op_token_logprobs_workspace_bytes(int32_t M, int32_t V, int32_t k);
+
+/* Log probabilities of given tokens, entropy and top alternatives of M rows of V logits (those of pbd_op_lm_head_argmax,
+ * pbd_verify_block or pbd_decode_step, or the caller's), in one pass over them:
+ *     p = softmax(x / temperature),  logprob = ln p[token],  entropy = -sum p ln p,
+ *     top_ids / top_logprobs: the k likeliest, by logit, equal ones by the lower id.
+ * d_logits: rows ld values apart, of type dtype (pbd_dtype).  d_tokens_opt [M] with d_logprob_opt [M] fp32, both or
+ * neither: a negative token asks for nothing (its log probability is 0), one at or above V is reported by
+ * pbd_op_status (DEV_BAD_TOKEN) and gives NaN.  d_entropy_opt [M] fp32 or NULL.  d_top_ids [M, k] int32 and
+ * d_top_logprobs [M, k] fp32, not read for k = 0.  Logits of -inf are masked; a row with nothing else has log
+ * probabilities of -inf and entropy 0.  A row that holds NaN or +inf gives NaN (and ids that say nothing).
+ * Requirements: 1 <= V <= 2^30, ld >= V, 0 <= k <= min(32, V); temperature > 0.  Sums are fp32.  The workspace (1024-byte
+ * aligned) is scratch; its first word is the status word for pbd_op_status. */
+pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void *d_logits, int64_t ld, float temperature,
+                                 const int32_t *d_tokens_opt, int32_t k, float *d_logprob_opt, float *d_entropy_opt,
+                                 int32_t *d_top_ids, float *d_top_logprobs, void *d_ws, size_t ws_bytes, void *d_stream);
+
+/* Device status of the last call of an entry point above that used the workspace d_ws (the 1024-byte-aligned
+ * pointer that call was given): waits for d_stream, then reads the status word at the start of d_ws.  PBD_OK when no
+ * kernel latched an error; PBD_ERR_DEVICE with the latched code in *h_device_code (may be NULL) otherwise, and that
+ * call's outputs are invalid; PBD_ERR_INVALID_ARG for a null or misaligned d_ws; PBD_ERR_CUDA if the stream failed.
+ * What kernels latch: a device wait bounded at one second that runs out (linear, lm_head), and lengths, pages (7) and
+ * tokens (4) in device memory that lie outside their range (5: a length), which the host cannot check. */
 pbd_status pbd_op_status(const void *d_ws, void *d_stream, int32_t *h_device_code);
 
 /* Message of the last failed pbd_op_* call on this thread ("" if none). */

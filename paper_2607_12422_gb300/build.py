@@ -17,8 +17,9 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libpbd.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-SOURCES = ["lm_head.cu", "gemm.cu", "linear_op.cu", "rows.cu", "steps.cu", "pass_kernel.cu", "ops.cu", "ops_api.cu", "op_linear_static.cu", "pbd.cu"]
-HEADERS = ["attn.cuh", "common.cuh", "pbd_internal.h"]
+SOURCES = ["lm_head.cu", "gemm.cu", "linear_op.cu", "rows.cu", "steps.cu", "pass_kernel.cu", "ops.cu", "ops_api.cu", "op_linear_static.cu",
+           "kv_api.cu", "kv_attn.cu", "kv_evict.cu", "logprobs.cu", "pbd.cu"]
+HEADERS = ["attn.cuh", "common.cuh", "kv_ops.h", "pbd_internal.h"]
 
 
 def nvcc() -> str:

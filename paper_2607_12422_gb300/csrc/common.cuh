@@ -24,6 +24,7 @@ enum : int {
     DEV_BAD_TOKEN = 4,      // token id outside [0, V)
     DEV_BAD_POSITION = 5,   // position beyond the reserved pages
     DEV_TIMEOUT_DEP = 6,    // a work item's inputs never completed
+    DEV_BAD_PAGE = 7,       // page index outside the cache
 };
 
 constexpr unsigned long long WAIT_LIMIT_NS = 1000000000ull;  // 1 s

@@ -1,0 +1,226 @@
+// kv_api.cu -- C entry points (include/pbd_ops.h) of the operators on a caller's paged cache and on logits: argument
+// checks, workspace plans and launches.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+
+#include "../../include/pbd_ops.h"
+#include "kv_ops.h"
+
+using namespace pbd;
+
+namespace {
+
+pbd_status fail(pbd_status s, const char *who, const char *what, cudaError_t e = cudaSuccess) {
+    char b[256];
+    snprintf(b, sizeof b, "%s: %s%s%s", who, what, e != cudaSuccess ? ": " : "", e != cudaSuccess ? cudaGetErrorString(e) : "");
+    op_record_error(b);
+    return s;
+}
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+bool overlap(const void *a, long long na, const void *b, long long nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
+}
+
+// What is wrong with a cache's sizes and strides, or null.  Pointers are looked at by the entry points: workspace sizes
+// are asked for before there are any.
+const char *bad_sizes(const pbd_kv_pages *kv) {
+    if (!kv) return "null cache";
+    if (kv->dtype != PBD_BF16 && kv->dtype != PBD_FP16) return "the cache's type must be PBD_BF16 or PBD_FP16";
+    if (kv->batch < 1 || kv->batch > KV_MAX_BATCH) return "batch must be 1 to 1024";
+    if (kv->n_kv_heads < 1 || kv->n_kv_heads > 256) return "n_kv_heads must be 1 to 256";
+    if (kv->head_dim != 64 && kv->head_dim != 128 && kv->head_dim != 256) return "head_dim must be 64, 128 or 256";
+    if (kv->n_pages < 1 || kv->page_size < 1 || kv->max_pages < 1) return "n_pages, page_size and max_pages must be positive";
+    if ((long long)kv->max_pages * kv->page_size > (1ll << 30)) return "a sequence holds at most 2^30 slots";
+    if (kv->stride_page < 0 || kv->stride_head < 0 || kv->stride_slot < 0 || kv->stride_page % 8 || kv->stride_head % 8 ||
+        kv->stride_slot % 8)
+        return "strides must be multiples of 8 values and not negative";
+    return nullptr;
+}
+
+const char *bad_cache(const pbd_kv_pages *kv) {
+    if (const char *w = bad_sizes(kv)) return w;
+    if (!kv->d_k || !kv->d_v || !kv->d_page_table || !kv->d_lens) return "null pointer in the cache";
+    if (!aligned(kv->d_k, 16) || !aligned(kv->d_v, 16)) return "K and V must be 16-byte aligned";
+    if (!aligned(kv->d_page_table, 4) || !aligned(kv->d_lens, 4) || !aligned(kv->d_weights, 4) || !aligned(kv->d_positions, 4))
+        return "the cache's 32-bit arrays must be 4-byte aligned";
+    return nullptr;
+}
+
+KvView view(const pbd_kv_pages &kv) {
+    KvView v{};
+    v.k = static_cast<const uint16_t *>(kv.d_k);
+    v.v = static_cast<const uint16_t *>(kv.d_v);
+    v.stride_page = kv.stride_page;
+    v.stride_head = kv.stride_head;
+    v.stride_slot = kv.stride_slot;
+    v.table = kv.d_page_table;
+    v.lens = kv.d_lens;
+    v.weights = kv.d_weights;
+    v.positions = kv.d_positions;
+    v.cap = (long long)kv.max_pages * kv.page_size;
+    v.n_pages = kv.n_pages;
+    v.page_size = kv.page_size;
+    v.hkv = kv.n_kv_heads;
+    v.d = kv.head_dim;
+    v.B = kv.batch;
+    v.max_pages = kv.max_pages;
+    return v;
+}
+
+const char *bad_heads(const pbd_kv_pages *kv, int hq) {
+    if (hq < kv->n_kv_heads || hq % kv->n_kv_heads || hq > 4096) return "n_q_heads must be a multiple of n_kv_heads, at most 4096";
+    return nullptr;
+}
+
+const char *bad_workspace(const void *ws, size_t have, size_t need) {
+    return !ws || !aligned(ws, 1024) || have < need ? "workspace missing, misaligned or too small" : nullptr;
+}
+
+size_t evict_bytes(const KvView &v, int n_keep) {
+    const long long most = std::max(0ll, std::min((long long)n_keep, v.cap - n_keep));
+    return 1024 + ((size_t)v.B * v.hkv * 2 * most * sizeof(int) + 1023) / 1024 * 1024;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n_q_heads, int32_t accumulate) {
+    DecodePlan p;
+    if (bad_sizes(kv) || bad_heads(kv, n_q_heads) || !decode_plan(view(*kv), n_q_heads, accumulate != 0, &p)) return 0;
+    return p.total;
+}
+
+pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, float scale, const void *d_q, int64_t q_stride,
+                                   const void *d_k_new, const void *d_v_new, int64_t new_stride,
+                                   const int32_t *d_new_positions, int32_t accumulate, void *d_out, float *d_lse_opt,
+                                   void *d_ws, size_t ws_bytes, void *d_stream) {
+    const char *who = "pbd_op_decode_attention";
+    if (const char *w = bad_cache(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
+    if (const char *w = bad_heads(kv, n_q_heads)) return fail(PBD_ERR_INVALID_ARG, who, w);
+    if (!(scale > 0.f) || std::isinf(scale)) return fail(PBD_ERR_INVALID_ARG, who, "scale must be positive and finite");
+    if (!d_q || !d_out) return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
+    if (!d_k_new != !d_v_new) return fail(PBD_ERR_INVALID_ARG, who, "d_k_new and d_v_new come together");
+    if (!aligned(d_q, 16) || !aligned(d_out, 16) || !aligned(d_k_new, 16) || !aligned(d_v_new, 16))
+        return fail(PBD_ERR_INVALID_ARG, who, "q, out, k_new and v_new must be 16-byte aligned");
+    const int D = kv->head_dim;
+    if (q_stride < (int64_t)n_q_heads * D || q_stride % 8 || (d_k_new && (new_stride < (int64_t)kv->n_kv_heads * D || new_stride % 8)))
+        return fail(PBD_ERR_INVALID_ARG, who, "row strides must be multiples of 8 values and hold a row");
+    if (accumulate && !kv->d_weights) return fail(PBD_ERR_INVALID_ARG, who, "accumulate needs the cache's d_weights");
+    DecodePlan p;
+    const KvView v = view(*kv);
+    if (!decode_plan(v, n_q_heads, accumulate != 0, &p))
+        return fail(PBD_ERR_CAPACITY, who, "more than 2^31 tiles of 16 slots in all heads and sequences");
+    if (const char *w = bad_workspace(d_ws, ws_bytes, p.total)) return fail(PBD_ERR_WORKSPACE, who, w);
+    uint8_t *ws = static_cast<uint8_t *>(d_ws);
+    DecodeArgs a{};
+    a.kv = v;
+    a.hq = n_q_heads;
+    a.group = n_q_heads / kv->n_kv_heads;
+    a.scale = scale;
+    a.q = static_cast<const uint16_t *>(d_q);
+    a.q_stride = q_stride;
+    a.k_new = static_cast<const uint16_t *>(d_k_new);
+    a.v_new = static_cast<const uint16_t *>(d_v_new);
+    a.new_stride = new_stride;
+    a.new_pos = d_new_positions;
+    a.out = static_cast<uint16_t *>(d_out);
+    a.lse = d_lse_opt;
+    a.accumulate = accumulate != 0;
+    a.fp16 = kv->dtype == PBD_FP16;
+    a.status = reinterpret_cast<int *>(ws);
+    a.part_o = reinterpret_cast<float *>(ws + p.part_o);
+    a.part_ml = reinterpret_cast<float2 *>(ws + p.part_ml);
+    a.row_ml = reinterpret_cast<float2 *>(ws + p.row_ml);
+    a.scores = accumulate ? reinterpret_cast<float *>(ws + p.scores) : nullptr;
+    a.score_pitch = p.score_pitch;
+    const cudaError_t e = launch_decode_attention(a, static_cast<cudaStream_t>(d_stream));
+    return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
+}
+
+size_t pbd_op_evict_workspace_bytes(const pbd_kv_pages *kv, int32_t n_keep) {
+    return bad_sizes(kv) || n_keep < 0 ? 0 : evict_bytes(view(*kv), n_keep);
+}
+
+pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent, int32_t n_sink,
+                        const int32_t *d_next_positions, float *d_out_weights, int32_t *d_out_positions, void *d_ws,
+                        size_t ws_bytes, void *d_stream) {
+    const char *who = "pbd_op_evict";
+    if (const char *w = bad_cache(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
+    if (!kv->d_weights || !kv->d_positions || !d_next_positions || !d_out_weights || !d_out_positions)
+        return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
+    if (n_keep < 0 || n_recent < 0 || n_sink < 0 || (int64_t)n_recent + n_sink > n_keep)
+        return fail(PBD_ERR_INVALID_ARG, who, "n_keep, n_recent and n_sink must not be negative, and the last two fit the first");
+    const KvView v = view(*kv);
+    const long long bytes = (long long)v.B * v.hkv * v.cap * 4;
+    const bool in_place = d_out_weights == kv->d_weights && d_out_positions == kv->d_positions;
+    if (!in_place && (overlap(d_out_weights, bytes, kv->d_weights, bytes) || overlap(d_out_positions, bytes, kv->d_positions, bytes) ||
+                      overlap(d_out_weights, bytes, kv->d_positions, bytes) || overlap(d_out_positions, bytes, kv->d_weights, bytes)))
+        return fail(PBD_ERR_INVALID_ARG, who, "the outputs are the cache's own arrays, both of them, or lie apart from them");
+    if (const char *w = bad_workspace(d_ws, ws_bytes, evict_bytes(v, n_keep))) return fail(PBD_ERR_WORKSPACE, who, w);
+    uint8_t *ws = static_cast<uint8_t *>(d_ws);
+    EvictArgs a{};
+    a.kv = v;
+    a.n_keep = n_keep;
+    a.n_recent = n_recent;
+    a.n_sink = n_sink;
+    a.next_pos = d_next_positions;
+    a.out_weights = d_out_weights;
+    a.out_positions = d_out_positions;
+    a.status = reinterpret_cast<int *>(ws);
+    a.moves = reinterpret_cast<int *>(ws + 1024);
+    a.most = std::max(0ll, std::min((long long)n_keep, v.cap - n_keep));
+    const cudaError_t e = launch_evict(a, static_cast<cudaStream_t>(d_stream));
+    return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
+}
+
+size_t pbd_op_token_logprobs_workspace_bytes(int32_t M, int32_t V, int32_t k) {
+    if (M < 1 || V < 1 || V > (1 << 30) || k < 0 || k > LP_MAX_K || k > V) return 0;
+    const size_t s = logprob_slices(M, V, 4);  // (of any type: 16-bit rows have no more slices)
+    return 1024 + (size_t)M * s * (16 + 8 * (size_t)k);
+}
+
+pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void *d_logits, int64_t ld, float temperature,
+                                 const int32_t *d_tokens_opt, int32_t k, float *d_logprob_opt, float *d_entropy_opt,
+                                 int32_t *d_top_ids, float *d_top_logprobs, void *d_ws, size_t ws_bytes, void *d_stream) {
+    const char *who = "pbd_op_token_logprobs";
+    const size_t need = pbd_op_token_logprobs_workspace_bytes(M, V, k);
+    if (need == 0) return fail(PBD_ERR_INVALID_ARG, who, "unsupported sizes");
+    if (dtype != PBD_FP32 && dtype != PBD_BF16 && dtype != PBD_FP16) return fail(PBD_ERR_INVALID_ARG, who, "unknown type of logits");
+    const int es = dtype == PBD_FP32 ? 4 : 2;
+    if (ld < V) return fail(PBD_ERR_INVALID_ARG, who, "rows lie less than V values apart");
+    if (!(temperature > 0.f) || std::isinf(temperature) || std::isinf(1.f / temperature))
+        return fail(PBD_ERR_INVALID_ARG, who, "temperature must be positive and finite");
+    if (!d_logits || !aligned(d_logits, es)) return fail(PBD_ERR_INVALID_ARG, who, "logits missing or misaligned");
+    if (!d_tokens_opt != !d_logprob_opt) return fail(PBD_ERR_INVALID_ARG, who, "d_tokens_opt and d_logprob_opt come together");
+    if (k > 0 && (!d_top_ids || !d_top_logprobs)) return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
+    if (const char *w = bad_workspace(d_ws, ws_bytes, need)) return fail(PBD_ERR_WORKSPACE, who, w);
+    uint8_t *ws = static_cast<uint8_t *>(d_ws);
+    LogprobArgs a{};
+    a.x = d_logits;
+    a.ld = ld;
+    a.M = M;
+    a.V = V;
+    a.type = dtype;
+    a.inv_t = 1.f / temperature;
+    a.tokens = d_tokens_opt;
+    a.k = k;
+    a.logprob = d_logprob_opt;
+    a.entropy = d_entropy_opt;
+    a.top_ids = d_top_ids;
+    a.top_lp = d_top_logprobs;
+    a.status = reinterpret_cast<int *>(ws);
+    a.slices = logprob_slices(M, V, es);
+    a.stats = reinterpret_cast<float *>(ws + 1024);
+    a.cand = reinterpret_cast<unsigned long long *>(ws + 1024 + (size_t)M * a.slices * 16);
+    const cudaError_t e = launch_logprobs(a, static_cast<cudaStream_t>(d_stream));
+    return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
+}
+
+}  // extern "C"

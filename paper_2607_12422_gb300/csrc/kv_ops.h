@@ -1,0 +1,87 @@
+// kv_ops.h -- the operators on a caller's paged cache and on logits: what their kernels (kv_attn.cu, kv_evict.cu,
+// logprobs.cu) take from their entry points (kv_api.cu).
+#pragma once
+
+#include "common.cuh"
+#include "pbd_internal.h"
+
+namespace pbd {
+
+// A caller's cache as kernels see it (pbd_kv_pages).  Strides in elements of 16 bits.
+struct KvView {
+    const uint16_t *k, *v;
+    long long stride_page, stride_head, stride_slot;
+    const int *table, *lens;
+    float *weights;
+    int *positions;
+    long long cap;  // slots of a sequence: max_pages * page_size
+    int n_pages, page_size, hkv, d, B, max_pages;
+};
+
+constexpr int KV_MAX_WORKERS = 2048;  // warps that share a call's units
+constexpr int KV_MAX_BATCH = 1024;  // sequences of a call: their lengths and first tiles lie in shared memory
+
+// ---- attention of one token (kv_attn.cu)
+struct DecodeArgs {
+    KvView kv;
+    int hq, group;      // query heads; of one KV head
+    float scale;        // of the scores
+    const uint16_t *q;  // [B] rows q_stride apart of [hq][d]
+    long long q_stride;
+    const uint16_t *k_new, *v_new;  // [B] rows new_stride apart of [hkv][d], or null
+    long long new_stride;
+    const int *new_pos;
+    uint16_t *out;  // [B][hq][d]
+    float *lse;     // [B][hq] or null
+    int accumulate;
+    int fp16;
+    int *status;
+    // scratch (decode_plan)
+    float *part_o;    // [workers][2][heads of a chunk][d]
+    float2 *part_ml;  // [workers][2][heads of a chunk]: maximum, sum
+    float2 *row_ml;   // [B][hq]: maximum, 1 / sum
+    float *scores;    // [B][hq][score_pitch] when accumulating
+    long long score_pitch;
+    int workers;
+};
+struct DecodePlan {
+    size_t part_o, part_ml, row_ml, scores, total;  // offsets in the workspace
+    long long score_pitch;
+};
+bool decode_plan(const KvView &kv, int hq, bool accumulate, DecodePlan *p);
+cudaError_t launch_decode_attention(DecodeArgs &a, cudaStream_t st);
+
+// ---- eviction (kv_evict.cu)
+struct EvictArgs {
+    KvView kv;
+    int n_keep, n_recent, n_sink;
+    const int *next_pos;
+    float *out_weights;
+    int *out_positions;
+    int *moves;           // [B * hkv][2][most]: holes in front, kept slots behind
+    long long most;
+    int *status;
+};
+cudaError_t launch_evict(const EvictArgs &a, cudaStream_t st);
+
+// ---- log probabilities (logprobs.cu)
+struct LogprobArgs {
+    const void *x;  // [M] rows ld apart of [V]
+    long long ld;
+    int M, V, type;  // type: pbd_dtype
+    float inv_t;     // 1 / temperature
+    const int *tokens;
+    int k;
+    float *logprob, *entropy, *top_lp;
+    int *top_ids;
+    int *status;
+    // scratch
+    float *stats;              // [M][slices][4]: maximum, sum, sum of weighted distances
+    unsigned long long *cand;  // [M][slices][k]
+    int slices, slice_vecs;
+};
+constexpr int LP_MAX_K = 32;
+int logprob_slices(int M, int V, int es);
+cudaError_t launch_logprobs(LogprobArgs &a, cudaStream_t st);
+
+}  // namespace pbd

@@ -220,6 +220,7 @@ const char *device_code_name(int code) {
         case DEV_BAD_TOKEN: return "token id outside the vocabulary";
         case DEV_BAD_POSITION: return "position beyond the reserved KV pages";
         case DEV_TIMEOUT_DEP: return "a work item's inputs never completed";
+        case DEV_BAD_PAGE: return "page index outside the cache";
         default: return "unknown device code";
     }
 }

@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import re
-from typing import Dict, List, Optional, Sequence
+from typing import Dict, List, NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -47,6 +47,17 @@ class pbd_base_weights(C.Structure):
 
 class pbd_adapter_weights(C.Structure):
     _fields_ = [("lora_a", C.c_void_p * 7), ("lora_b", C.c_void_p * 7), ("mask_embed", C.c_void_p)]
+
+
+PBD_BF16, PBD_FP16, PBD_FP32 = 0, 1, 2  # pbd_dtype
+
+
+class pbd_kv_pages(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("dtype", C.c_int32), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("batch", C.c_int32),
+                ("max_pages", C.c_int32), ("stride_page", C.c_int64), ("stride_head", C.c_int64),
+                ("stride_slot", C.c_int64), ("d_page_table", C.c_void_p), ("d_lens", C.c_void_p),
+                ("d_weights", C.c_void_p), ("d_positions", C.c_void_p)]
 
 
 class pbd_stats(C.Structure):
@@ -116,6 +127,16 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     L.pbd_op_status.restype = C.c_int
     L.pbd_op_linear_static_status.argtypes = [P, P]
     L.pbd_op_linear_static_status.restype = C.c_int
+    I64, F, Z, KV = C.c_int64, C.c_float, C.c_size_t, C.POINTER(pbd_kv_pages)
+    L.pbd_op_decode_attention_workspace_bytes.argtypes = [KV, I32, I32]
+    L.pbd_op_decode_attention.argtypes = [KV, I32, F, P, I64, P, P, I64, P, I32, P, P, P, Z, P]
+    L.pbd_op_evict_workspace_bytes.argtypes = [KV, I32]
+    L.pbd_op_evict.argtypes = [KV, I32, I32, I32, P, P, P, P, Z, P]
+    L.pbd_op_token_logprobs_workspace_bytes.argtypes = [I32, I32, I32]
+    L.pbd_op_token_logprobs.argtypes = [I32, I32, I32, P, I64, F, P, I32, P, P, P, P, P, Z, P]
+    for name in ("decode_attention", "evict", "token_logprobs"):
+        getattr(L, "pbd_op_" + name).restype = C.c_int
+        getattr(L, "pbd_op_%s_workspace_bytes" % name).restype = C.c_size_t
     for name in ("pbd_create", "pbd_destroy", "pbd_prefill", "pbd_draft_block", "pbd_verify_block",
                  "pbd_accept_commit", "pbd_decode_step", "pbd_generate", "pbd_get_state", "pbd_get_tokens",
                  "pbd_read_kv", "pbd_sync", "pbd_op_linear", "pbd_op_lm_head_argmax"):
@@ -213,6 +234,256 @@ def pbd_op_lm_head_argmax(x, E, want_logits: bool = False):
         _raise_if(L, L.pbd_op_status(ws, st, None))
     del buf
     return ids, lg
+
+
+# ------------------------------------------------------------------ a caller's paged cache, and logits
+
+
+def _bad(who, what):
+    raise PbdError(1, "%s: %s" % (who, what))
+
+
+def _dtype(t, who):
+    name = str(t.dtype)
+    code = {"torch.bfloat16": PBD_BF16, "torch.float16": PBD_FP16, "torch.float32": PBD_FP32}.get(name)
+    if code is None:
+        _bad(who, "unsupported type %s" % name)
+    return code
+
+
+def _check(who, name, t, like, shape, dtype=None, rows=False):
+    """t lies on like's device, has this shape and type, and is contiguous (rows: each t[i] is)."""
+    if t.device != like.device:
+        _bad(who, "%s is not on the cache's device" % name)
+    if tuple(t.shape) != tuple(shape):
+        _bad(who, "%s has shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+    if t.dtype != (dtype or like.dtype):
+        _bad(who, "%s has type %s" % (name, t.dtype))
+    if not (t.is_contiguous() or (rows and t.shape[0] and t[0].is_contiguous() and t.stride(0) >= t[0].numel())):
+        _bad(who, "%s is not contiguous" % name)
+
+
+class _OnDevice:
+    """The library runs on the current device: makes `device` current where it is not."""
+
+    def __init__(self, torch, device):
+        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+
+    def __enter__(self):
+        if self.guard:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard:
+            self.guard.__exit__(*exc)
+
+
+class OpWorkspace:
+    """Scratch for the calls that take one (op_workspace): calls that may overlap in time need one each."""
+
+    def __init__(self, nbytes, device):
+        import torch
+        if nbytes <= 0:
+            raise PbdError(1, "op_workspace: unsupported sizes")
+        self.buf = torch.empty(nbytes + 1024, dtype=torch.uint8, device=device)
+        self.device, self.nbytes = self.buf.device, nbytes
+        self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 1024
+
+
+def op_workspace(nbytes: int, device="cuda") -> OpWorkspace:
+    return OpWorkspace(nbytes, device)
+
+
+def _scratch(L, who, workspace, need, device):
+    """(workspace, its pointer, its bytes) for a call that needs `need`."""
+    if need == 0:
+        _bad(who, "unsupported sizes")
+    if workspace is None:
+        workspace = OpWorkspace(need, device)
+    elif workspace.device != device:
+        _bad(who, "the workspace is on another device")
+    return workspace
+
+
+class PagedKV:
+    """A paged key-value cache of one layer (pbd_kv_pages): a handle that keeps the tensors it was given.
+
+    k, v [n_pages, n_kv_heads, page_size, head_dim] bf16 or fp16, with the same strides, the last one 1 (token-major
+    pages: a transposed view); page_table [batch, max_pages] int32, lens [batch] int32; weights and positions
+    [batch, n_kv_heads, max_pages * page_size], fp32 and int32, where they are wanted.  The calls read the tensors' present
+    contents; what lens and positions say is up to the program."""
+
+    def __init__(self, k, v, page_table, lens, weights=None, positions=None):
+        import torch
+        who = "PagedKV"
+        if k.dim() != 4 or page_table.dim() != 2:
+            _bad(who, "k is [n_pages, n_kv_heads, page_size, head_dim] and page_table [batch, max_pages]")
+        if not k.is_cuda or _dtype(k, who) == PBD_FP32:
+            _bad(who, "the cache is bf16 or fp16 on a GPU")
+        if v.shape != k.shape or v.dtype != k.dtype or v.device != k.device or v.stride() != k.stride():
+            _bad(who, "k and v differ in shape, type, device or strides")
+        if k.stride(3) != 1:
+            _bad(who, "the values of a head are not contiguous")
+        B, max_pages = page_table.shape
+        n_pages, hkv, ps, D = k.shape
+        _check(who, "page_table", page_table, k, (B, max_pages), torch.int32)
+        _check(who, "lens", lens, k, (B,), torch.int32)
+        for name, t, dt in (("weights", weights, torch.float32), ("positions", positions, torch.int32)):
+            if t is not None:
+                _check(who, name, t, k, (B, hkv, max_pages * ps), dt)
+        self.k, self.v, self.page_table, self.lens = k, v, page_table, lens
+        self.weights, self.positions = weights, positions
+        self.batch, self.n_kv_heads, self.head_dim, self.device, self.dtype = B, hkv, D, k.device, k.dtype
+        self.c = pbd_kv_pages(k.data_ptr(), v.data_ptr(), _dtype(k, who), n_pages, ps, hkv, D, B, max_pages, k.stride(0),
+                              k.stride(1), k.stride(2), page_table.data_ptr(), lens.data_ptr(), _ptr(weights),
+                              _ptr(positions))
+        self.ref = C.byref(self.c)
+        self._need = {}
+
+
+def decode_attention_workspace_bytes(kv: PagedKV, n_q_heads: int, accumulate: bool = False) -> int:
+    return load().pbd_op_decode_attention_workspace_bytes(kv.ref, n_q_heads, int(accumulate))
+
+
+def pbd_op_decode_attention(q, kv: PagedKV, k_new=None, v_new=None, new_positions=None, scale: Optional[float] = None,
+                            accumulate: bool = False, out=None, want_lse: bool = False, workspace=None,
+                            sync: bool = True):
+    """(out [batch, n_q_heads, head_dim], lse [batch, n_q_heads] fp32 or None): attention of one new token a sequence over
+    a paged cache; see include/pbd_ops.h.  q [batch, n_q_heads, head_dim]; k_new, v_new [batch, n_kv_heads, head_dim]: the
+    token's own K and V, stored into the cache first, with new_positions [batch] int32 into its positions; scale is
+    1/sqrt(head_dim) when not given; accumulate adds the attention weights to the cache's.  With sync, waits and raises
+    PbdError(PBD_ERR_DEVICE) for a length or page outside the cache; without, ask pbd_op_status(workspace)."""
+    import torch
+    who = "pbd_op_decode_attention"
+    L = load()
+    B, D, hkv = kv.batch, kv.head_dim, kv.n_kv_heads
+    if q.dim() != 3:
+        _bad(who, "q is [batch, n_q_heads, head_dim]")
+    hq = q.shape[1]
+    _check(who, "q", q, kv, (B, hq, D), rows=True)
+    if (k_new is None) != (v_new is None):
+        _bad(who, "k_new and v_new come together")
+    new_stride = 0
+    if k_new is not None:
+        _check(who, "k_new", k_new, kv, (B, hkv, D), rows=True)
+        _check(who, "v_new", v_new, kv, (B, hkv, D), rows=True)
+        new_stride = k_new.stride(0) if B > 1 else hkv * D
+        if B > 1 and v_new.stride(0) != new_stride:
+            _bad(who, "rows of k_new and v_new lie differently far apart")
+        if new_positions is not None:
+            _check(who, "new_positions", new_positions, kv, (B,), torch.int32)
+    elif new_positions is not None:
+        _bad(who, "new_positions without k_new and v_new")
+    if out is not None:
+        _check(who, "out", out, kv, (B, hq, D))
+    key = (hq, accumulate)
+    need = kv._need.get(key)
+    if need is None:  # (sizes of a handle do not change)
+        need = kv._need[key] = decode_attention_workspace_bytes(kv, hq, accumulate)
+    with _OnDevice(torch, kv.device):
+        ws = _scratch(L, who, workspace, need, kv.device)
+        if out is None:
+            out = torch.empty(B, hq, D, dtype=kv.dtype, device=kv.device)
+        lse = torch.empty(B, hq, dtype=torch.float32, device=kv.device) if want_lse else None
+        st = torch.cuda.current_stream(kv.device).cuda_stream
+        s = L.pbd_op_decode_attention(kv.ref, hq, scale if scale is not None else D ** -0.5, q.data_ptr(),
+                                      q.stride(0) if B > 1 else hq * D, _ptr(k_new), _ptr(v_new), new_stride,
+                                      _ptr(new_positions), int(accumulate), out.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes,
+                                      st)
+        _raise_if(L, s)
+        if sync:
+            _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    return out, lse
+
+
+def evict_workspace_bytes(kv: PagedKV, n_keep: int) -> int:
+    return load().pbd_op_evict_workspace_bytes(kv.ref, n_keep)
+
+
+def pbd_op_evict(kv: PagedKV, n_keep: int, next_positions, n_recent: int = 0, n_sink: int = 0, out_weights=None,
+                 out_positions=None, workspace=None, sync: bool = True):
+    """(weights, positions) of the kept slots: of each sequence and KV head the n_keep slots of largest accumulated weight
+    stay, the tokens at positions below n_sink and from next_positions [batch] int32 - n_recent on among them; see
+    include/pbd_ops.h.  K and V move in place; weights and positions go to out_weights and out_positions, the cache's own
+    where they are not given.  The program lowers kv.lens to at most n_keep once all layers that share it are through."""
+    import torch
+    who = "pbd_op_evict"
+    L = load()
+    if kv.weights is None or kv.positions is None:
+        _bad(who, "the cache has no weights or positions")
+    if (out_weights is None) != (out_positions is None):
+        _bad(who, "out_weights and out_positions come together")
+    if out_weights is None:
+        out_weights, out_positions = kv.weights, kv.positions
+    else:
+        _check(who, "out_weights", out_weights, kv, kv.weights.shape, torch.float32)
+        _check(who, "out_positions", out_positions, kv, kv.weights.shape, torch.int32)
+    _check(who, "next_positions", next_positions, kv, (kv.batch,), torch.int32)
+    need = kv._need.get(n_keep)
+    if need is None:
+        need = kv._need[n_keep] = evict_workspace_bytes(kv, n_keep) if n_keep >= 0 else 0
+    with _OnDevice(torch, kv.device):
+        ws = _scratch(L, who, workspace, need, kv.device)
+        st = torch.cuda.current_stream(kv.device).cuda_stream
+        s = L.pbd_op_evict(kv.ref, n_keep, n_recent, n_sink, next_positions.data_ptr(), out_weights.data_ptr(),
+                           out_positions.data_ptr(), ws.ptr, ws.nbytes, st)
+        _raise_if(L, s)
+        if sync:
+            _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    return out_weights, out_positions
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: object       # [M] fp32, or None without tokens
+    entropy: object       # [M] fp32
+    top_ids: object       # [M, k] int32, or None for k = 0
+    top_logprobs: object  # [M, k] fp32, or None for k = 0
+
+
+def token_logprobs_workspace_bytes(M: int, V: int, k: int = 0) -> int:
+    return load().pbd_op_token_logprobs_workspace_bytes(M, V, k)
+
+
+def pbd_op_token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, workspace=None, sync: bool = True):
+    """TokenLogprobs of logits [M, V] (fp32, bf16 or fp16; rows may lie apart): log probability of tokens [M] int32 (a
+    negative one: none), entropy, and the k likeliest ids with theirs; see include/pbd_ops.h.  With sync, waits and raises
+    PbdError(PBD_ERR_DEVICE) for a token at or above V; without, ask pbd_op_status(workspace)."""
+    import torch
+    who = "pbd_op_token_logprobs"
+    L = load()
+    if logits.dim() != 2 or not logits.is_cuda:
+        _bad(who, "logits are [M, V] on a GPU")
+    M, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        _bad(who, "the values of a row are not contiguous")
+    dt = _dtype(logits, who)
+    dev = logits.device
+    if tokens is not None:
+        _check(who, "tokens", tokens, logits, (M,), torch.int32)
+    need = L.pbd_op_token_logprobs_workspace_bytes(M, V, k)
+    with _OnDevice(torch, dev):
+        ws = _scratch(L, who, workspace, need, dev)
+        stats = torch.empty(2, M, dtype=torch.float32, device=dev)
+        ids = torch.empty(M, k, dtype=torch.int32, device=dev) if k else None
+        top = torch.empty(M, k, dtype=torch.float32, device=dev) if k else None
+        logprob, entropy = (stats[0], stats[1]) if tokens is not None else (None, stats[1])
+        st = torch.cuda.current_stream(dev).cuda_stream
+        s = L.pbd_op_token_logprobs(M, V, dt, logits.data_ptr(), logits.stride(0) if M > 1 else V, temperature,
+                                    _ptr(tokens), k, _ptr(logprob), entropy.data_ptr(), _ptr(ids), _ptr(top), ws.ptr,
+                                    ws.nbytes, st)
+        _raise_if(L, s)
+        if sync:
+            _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    return TokenLogprobs(logprob, entropy, ids, top)
+
+
+def pbd_op_status(workspace: OpWorkspace) -> None:
+    """Waits for the current stream and raises PbdError(PBD_ERR_DEVICE) if the last call that used the workspace latched an
+    error."""
+    import torch
+    L = load()
+    with _OnDevice(torch, workspace.device):
+        _raise_if(L, L.pbd_op_status(workspace.ptr, torch.cuda.current_stream(workspace.device).cuda_stream, None))
 
 
 def make_config(shape, block_D: int, max_batch: int, max_seq_len: int, draft_layers: int = 0,
