@@ -182,8 +182,7 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
 
 size_t pbd_op_token_logprobs_workspace_bytes(int32_t M, int32_t V, int32_t k) {
     if (M < 1 || V < 1 || V > (1 << 30) || k < 0 || k > LP_MAX_K || k > V) return 0;
-    const size_t s = logprob_slices(M, V, 4);  // (of any type: 16-bit rows have no more slices)
-    return 1024 + (size_t)M * s * (16 + 8 * (size_t)k);
+    return 1024;  // the status word
 }
 
 pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void *d_logits, int64_t ld, float temperature,
@@ -201,7 +200,6 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
     if (!d_tokens_opt != !d_logprob_opt) return fail(PBD_ERR_INVALID_ARG, who, "d_tokens_opt and d_logprob_opt come together");
     if (k > 0 && (!d_top_ids || !d_top_logprobs)) return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
     if (const char *w = bad_workspace(d_ws, ws_bytes, need)) return fail(PBD_ERR_WORKSPACE, who, w);
-    uint8_t *ws = static_cast<uint8_t *>(d_ws);
     LogprobArgs a{};
     a.x = d_logits;
     a.ld = ld;
@@ -215,10 +213,7 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
     a.entropy = d_entropy_opt;
     a.top_ids = d_top_ids;
     a.top_lp = d_top_logprobs;
-    a.status = reinterpret_cast<int *>(ws);
-    a.slices = logprob_slices(M, V, es);
-    a.stats = reinterpret_cast<float *>(ws + 1024);
-    a.cand = reinterpret_cast<unsigned long long *>(ws + 1024 + (size_t)M * a.slices * 16);
+    a.status = static_cast<int *>(d_ws);
     const cudaError_t e = launch_logprobs(a, static_cast<cudaStream_t>(d_stream));
     return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
 }

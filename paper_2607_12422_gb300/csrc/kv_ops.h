@@ -75,13 +75,9 @@ struct LogprobArgs {
     float *logprob, *entropy, *top_lp;
     int *top_ids;
     int *status;
-    // scratch
-    float *stats;              // [M][slices][4]: maximum, sum, sum of weighted distances
-    unsigned long long *cand;  // [M][slices][k]
-    int slices, slice_vecs;
+    int slices, slice_vecs;  // (launch_logprobs)
 };
 constexpr int LP_MAX_K = 32;
-int logprob_slices(int M, int V, int es);
 cudaError_t launch_logprobs(LogprobArgs &a, cudaStream_t st);
 
 }  // namespace pbd

@@ -5,13 +5,12 @@
 //     entropy    = ln S + sum (m - x) / T exp((x - m) / T) / S      (both terms >= 0: nothing cancels)
 //     top k      by value, then by the lower index
 // in one pass over the logits, which bounds it: running maximum and sums in fp32 per thread, joined at the end.  Few
-// rows are cut into slices, one CTA each, and k_logprobs_join joins them.
+// rows are cut into slices: a cluster of CTAs a row, whose parts are joined through distributed shared memory.
 //
-// The alternatives come from the same pass.  The first tile of a slice (16 KB) gives a threshold: the k-th largest of the
-// threads' own maxima, which at least k values reach.  Only k threads can hold values that reach it, so
-// few do; they go to a list in shared memory.  Of later tiles only what is above the threshold is added, some k / i of the i-th
-// tile when the order is random.  If an unlucky order fills the list, it is cut to its k best, which raise the
-// threshold.
+// The alternatives come from the same pass at the price of one store for 64 bytes of logits: the maximum of each group of
+// 64 bytes stays in shared memory.  The k best values lie in the k groups of largest maxima (k values, those maxima,
+// already reach the k-th of them), so at the end k groups are picked and read again.  Groups are contiguous, so that among
+// equal maxima the lower group holds the lower ids.  However the values are ordered, the work is the same.
 #include <algorithm>
 #include <cuda_fp16.h>
 
@@ -25,7 +24,11 @@ namespace {
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
 constexpr int LP_VECS = 4;                        // 16-byte loads of a thread and tile
 constexpr int LP_TILE = LP_THREADS * LP_VECS;     // vectors of a tile
-constexpr int LP_LIST = 2048;                     // more than k of the list and a tile's k threads' 32 values each
+constexpr int LP_TILE_MAX = 4 * 72;               // floats that hold their maxima: four rows of 64, padded for the banks
+constexpr int LP_SEGMENT = 40;                    // tiles whose maxima are kept at a time: 46 KB
+constexpr int LP_CLUSTER = 16;                    // slices of a row at most
+constexpr int LP_BINS = 64;                       // of the selections below
+constexpr int LP_LIST = 2048;                     // keys of a list; 32 groups of 32 values need 1024
 constexpr float LP_FLOOR = -1000.f;               // 2^-1000 is 0 in fp32
 
 typedef unsigned long long u64;
@@ -55,7 +58,7 @@ __device__ __forceinline__ float key_value(u64 k) {
 __device__ __forceinline__ int key_index(u64 k) { return (int)~(uint32_t)k; }
 
 template <int TYPE>
-struct Elem;  // values of a 16-byte vector
+struct Elem;  // values of a 16-byte vector, and what stands for a masked one in it
 template <>
 struct Elem<PBD_FP32> {
     static constexpr int N = 4, SIZE = 4;
@@ -63,10 +66,20 @@ struct Elem<PBD_FP32> {
         x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
     }
     static __device__ __forceinline__ float one(const void *p, long long i) { return static_cast<const float *>(p)[i]; }
+    static __device__ __forceinline__ void put(uint32_t *u, int i, const void *p, long long at, bool real) {
+        u[i] = real ? static_cast<const uint32_t *>(p)[at] : 0xff800000u;
+    }
+};
+template <uint32_t LOWEST>
+struct Elem16 {
+    static constexpr int N = 8, SIZE = 2;
+    static __device__ __forceinline__ void put(uint32_t *u, int i, const void *p, long long at, bool real) {
+        const uint32_t x = real ? static_cast<const uint16_t *>(p)[at] : LOWEST;
+        u[i / 2] = i & 1 ? u[i / 2] | x << 16 : x;
+    }
 };
 template <>
-struct Elem<PBD_BF16> {
-    static constexpr int N = 8, SIZE = 2;
+struct Elem<PBD_BF16> : Elem16<0xff80u> {
     static __device__ __forceinline__ void open(const uint4 &v, float *x) {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -78,8 +91,7 @@ struct Elem<PBD_BF16> {
     static __device__ __forceinline__ float one(const void *p, long long i) { return bf2f(static_cast<const bf16 *>(p)[i]); }
 };
 template <>
-struct Elem<PBD_FP16> {
-    static constexpr int N = 8, SIZE = 2;
+struct Elem<PBD_FP16> : Elem16<0xfc00u> {
     static __device__ __forceinline__ void open(const uint4 &v, float *x) {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -105,34 +117,87 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c) {
     return Stat{m, a.s * fa + b.s * fb, (a.h + a.s * da) * fa + (b.h + b.s * db) * fb};
 }
 
-// The k best of n keys of a list in shared memory, sorted, to its front (and the k-th returned; 0 if there are
-// fewer).  Keys differ, so a key's place is the number of larger ones.  Whole CTA; `tmp` holds k keys.
-__device__ __forceinline__ u64 keep_best(u64 *list, int n, int k, u64 *tmp) {
+// What the selections share (one CTA).
+struct Shared {
+    u64 list[LP_LIST], best[LP_MAX_K], pool[LP_THREADS], bar;
+    int count;
+};
+
+// A lower bound of the k-th largest of all keys, from each thread's largest (0: none): the k-th largest of the maxima of 64
+// bins of threads, which k keys reach; 0 if fewer bins have one.  With keys in any order some k ln(64 / (64 - k)) / (k / 64)
+// of them reach it: 44 for k = 32.  Whole CTA.
+__device__ __forceinline__ u64 bin_bound(u64 mine, int k, Shared &s) {
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += LP_THREADS) {
-        const u64 mine = list[i];
-        int r = 0;
-        for (int j = 0; j < n; ++j) r += list[j] > mine;
-        if (r < k) tmp[r] = mine;
+    s.pool[threadIdx.x] = mine;
+    if (threadIdx.x == 0) s.bar = 0, s.count = 0;
+    __syncthreads();
+    if (threadIdx.x < LP_BINS) {
+#pragma unroll
+        for (int i = 1; i < LP_THREADS / LP_BINS; ++i) mine = max(mine, s.pool[threadIdx.x + i * LP_BINS]);
+        s.pool[threadIdx.x] = mine;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < min(n, k); i += LP_THREADS) list[i] = tmp[i];
-    const u64 last = n >= k ? tmp[k - 1] : 0;
+    if (threadIdx.x < LP_BINS && mine) {
+        int r = 0;
+#pragma unroll 16
+        for (int i = 0; i < LP_BINS; ++i) r += s.pool[i] > mine;
+        if (r == k - 1) s.bar = mine;
+    }
     __syncthreads();
-    return last;
+    return s.bar;
 }
 
-// The k-th largest of one key a thread (0: none); 0 if fewer than k threads have one.  Whole CTA.
-__device__ __forceinline__ u64 kth_of_threads(u64 mine, int k, u64 *all, u64 *out) {
+// Of the n keys key(0 .. n - 1), all different (0: none), the k largest, sorted, into s.best, zeros behind them.  Whole CTA.
+// Their largest: k of n.  `key` gives the same at every call.
+template <typename Key>
+__device__ __forceinline__ void select_best(Key &&key, int n, int k, Shared &s) {
+    u64 mine = 0;
+    for (int i = threadIdx.x; i < n; i += LP_THREADS) mine = max(mine, key(i));
+    u64 bar = bin_bound(mine, k, s);
+    auto collect = [&]() {
+        if (mine && mine >= bar)
+            for (int i = threadIdx.x; i < n; i += LP_THREADS) {
+                const u64 x = key(i);
+                if (x && x >= bar) {
+                    const int p = atomicAdd(&s.count, 1);
+                    if (p < LP_LIST) s.list[p] = x;
+                }
+            }
+        __syncthreads();
+    };
+    collect();
+    if (s.count > LP_LIST) {
+        // few bins hold nearly all of the largest: the k-th key bit by bit
+        u64 at = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+            const u64 tried = at | 1ull << bit;
+            __syncthreads();
+            if (threadIdx.x == 0) s.count = 0;
+            __syncthreads();
+            int c = 0;
+            if (mine >= tried)
+                for (int i = threadIdx.x; i < n; i += LP_THREADS) c += key(i) >= tried;
+            if (c) atomicAdd(&s.count, c);
+            __syncthreads();
+            if (s.count >= k) at = tried;
+        }
+        bar = at;
+        __syncthreads();
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+        collect();
+    }
+    const int have = s.count;
+    if (threadIdx.x < k) s.best[threadIdx.x] = 0;
     __syncthreads();
-    all[threadIdx.x] = mine;
-    if (threadIdx.x == 0) *out = 0;
+    for (int i = threadIdx.x; i < have; i += LP_THREADS) {
+        const u64 x = s.list[i];
+        int r = 0;
+#pragma unroll 4
+        for (int j = 0; j < have; ++j) r += s.list[j] > x;
+        if (r < k) s.best[r] = x;
+    }
     __syncthreads();
-    int r = 0;
-    for (int j = 0; j < LP_THREADS; ++j) r += all[j] > mine;
-    if (mine && r == k - 1) *out = mine;
-    __syncthreads();
-    return *out;
 }
 
 struct Finish {  // a row's results
@@ -156,136 +221,163 @@ struct Finish {  // a row's results
     }
 };
 
-template <int TYPE>
-__device__ __forceinline__ float token_logit(const LogprobArgs &a, int row, bool *has) {
-    *has = false;
-    if (!a.logprob || threadIdx.x != 0) return 0.f;
-    const int t = a.tokens[row];
-    *has = t >= 0 && t < a.V;
-    if (t >= a.V) latch_error(a.status, DEV_BAD_TOKEN);
-    return *has ? Elem<TYPE>::one(a.x, row * a.ld + t) : 0.f;
+// One status word for the call: the first CTA of the grid looks at every row's token.
+__device__ __forceinline__ void check_tokens(const LogprobArgs &a) {
+    bool bad = false;
+    if (a.tokens)
+        for (int i = threadIdx.x; i < a.M; i += LP_THREADS) bad |= a.tokens[i] >= a.V;
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) *a.status = bad ? DEV_BAD_TOKEN : DEV_OK;
 }
 
 template <int TYPE, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS) k_logprobs(const LogprobArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LogprobArgs a) {
     using E = Elem<TYPE>;
-    constexpr int PER = LP_VECS * E::N;
-    __shared__ u64 list[TOP ? LP_LIST : 1], tmp[TOP ? LP_THREADS : 1], kth;
-    __shared__ int added[3];
-    __shared__ Stat ws[LP_WARPS];
+    constexpr int GE = 4 * E::N;  // values of a group
+    extern __shared__ __align__(16) float maxima[];
+    __shared__ Shared sh;
+    __shared__ u64 found[TOP ? LP_MAX_K : 1];  // the best of this CTA's values so far
+    __shared__ Stat ws[LP_WARPS], all;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices;
-    if (a.slices > 1) {
-        pdl_launch();
-        if (blockIdx.x == 0 && tid == 0) *a.status = DEV_OK;  // (k_logprobs_join latches)
-    }
+    if (blockIdx.x == 0) check_tokens(a);
     const float c = a.inv_t * 1.4426950408889634f;
     // vectors are counted from the 16-byte boundary at or before the row's first value
     const char *base = static_cast<const char *>(a.x) + row * a.ld * E::SIZE;
     const int skew = (int)(reinterpret_cast<uintptr_t>(base) & 15) / E::SIZE;
     const char *vbase = base - skew * E::SIZE;
     const int vecs = (a.V + skew + E::N - 1) / E::N;
-    const int v0 = slice * a.slice_vecs, v1 = min(vecs, v0 + a.slice_vecs);
+    const int v0 = min(vecs, slice * a.slice_vecs), v1 = min(vecs, v0 + a.slice_vecs);
+    const int whole0 = skew ? 1 : 0, whole1 = (a.V + skew) / E::N;  // vectors without a row's end in them
 
-    Stat st{-INFINITY, 0.f, 0.f};
-    float bar = -INFINITY;  // threshold of later tiles
-    int have = 0, turn = 0;
-    bool first = true;
-    if (TOP && tid < 3) added[tid] = 0;
-    if (TOP) __syncthreads();
-    for (int v = v0; v < v1; v += LP_TILE, first = false) {
-        float x[PER];
-        uint4 raw[LP_VECS];
+    auto load = [&](int v, uint4 (&raw)[LP_VECS]) {
+        if (v >= whole0 && v + LP_TILE <= min(v1, whole1)) {
 #pragma unroll
-        for (int i = 0; i < LP_VECS; ++i) {
-            const int at = v + i * LP_THREADS + tid, e0 = at * E::N - skew;
-            if (at < v1 && e0 >= 0 && e0 + E::N <= a.V)
-                raw[i] = __ldcs(reinterpret_cast<const uint4 *>(vbase) + at);
+            for (int i = 0; i < LP_VECS; ++i) raw[i] = __ldcs(reinterpret_cast<const uint4 *>(vbase) + v + i * LP_THREADS + tid);
+            return;
         }
 #pragma unroll
-        for (int i = 0; i < LP_VECS; ++i) {
-            const int at = v + i * LP_THREADS + tid, e0 = at * E::N - skew;
-            if (at < v1 && e0 >= 0 && e0 + E::N <= a.V) {
-                E::open(raw[i], x + i * E::N);
-            } else {  // a row's ends, value by value; nothing behind the slice
+        for (int i = 0; i < LP_VECS; ++i) {  // value by value at a row's ends; -inf behind the slice
+            const int at = v + i * LP_THREADS + tid;
+            if (at < v1 && at >= whole0 && at < whole1) {
+                raw[i] = __ldcs(reinterpret_cast<const uint4 *>(vbase) + at);
+            } else {
+                uint32_t u[4];
 #pragma unroll
-                for (int j = 0; j < E::N; ++j)
-                    x[i * E::N + j] = at < v1 && e0 + j >= 0 && e0 + j < a.V ? E::one(base, e0 + j) : -INFINITY;
+                for (int j = 0; j < E::N; ++j) {
+                    const int e = at * E::N - skew + j;
+                    E::put(u, j, base, e, at < v1 && e >= 0 && e < a.V);
+                }
+                raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
             }
         }
-        float mx = x[0];
+    };
+    Stat st{-INFINITY, 0.f, 0.f};
+    if (TOP && tid < a.k) found[tid] = 0;
+    for (int seg = v0; seg < v1; seg += LP_SEGMENT * LP_TILE) {
+        const int seg_end = min(v1, seg + LP_SEGMENT * LP_TILE);
+        uint4 raw[LP_VECS], ahead[LP_VECS];
+        load(seg, raw);
+        float *mrow = maxima + (tid & 3) * 72 + (tid >> 2);
+        for (int v = seg; v < seg_end; v += LP_TILE, mrow += LP_TILE_MAX) {
+            if (v + LP_TILE < seg_end) load(v + LP_TILE, ahead);
+            float mx[LP_VECS], lo = INFINITY;
 #pragma unroll
-        for (int i = 1; i < PER; ++i) mx = fmaxf(mx, x[i]);
-        const float mn = fmaxf(st.m, mx);
-        if (mn > st.m) {
-            const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
-            st.h = (st.h + st.s * d) * f;
-            st.s *= f;
-            st.m = mn;
-        }
-        const float mu = st.m == -INFINITY ? 0.f : st.m;
+            for (int i = 0; i < LP_VECS; ++i) {
+                float x[E::N];
+                E::open(raw[i], x);
+                mx[i] = x[0];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            // (-inf would give 0 * -inf)
-            const float t = max_nan((x[i] - mu) * c, LP_FLOOR), e = lp_ex2(t);
-            st.s += e;
-            st.h += e * t;
+                for (int j = 1; j < E::N; ++j) mx[i] = fmaxf(mx[i], x[j]);
+#pragma unroll
+                for (int j = 0; j < E::N; ++j) lo = fminf(lo, x[j]);
+            }
+            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mn = fmaxf(st.m, mt);
+            if (mn > st.m) {
+                const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
+                st.h = (st.h + st.s * d) * f;
+                st.s *= f;
+                st.m = mn;
+            }
+            const float mu = st.m == -INFINITY ? 0.f : st.m;
+            if ((lo - mu) * c > LP_FLOOR) {
+                F2 s2 = f2(0.f, 0.f), h2 = s2;
+                const F2 nm = f2(-mu, -mu), cc = f2(c, c);
+#pragma unroll
+                for (int i = 0; i < LP_VECS; ++i) {
+                    float x[E::N];
+                    E::open(raw[i], x);
+#pragma unroll
+                    for (int j = 0; j < E::N; j += 2) {
+                        const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
+                        const float2 tt = unpack2(t);
+                        const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
+                        s2 = add2(s2, e);
+                        h2 = fma2(e, t, h2);
+                    }
+                }
+                const float2 s = unpack2(s2), h = unpack2(h2);
+                st.s += s.x + s.y;
+                st.h += h.x + h.y;
+            } else {  // masked values, whose -inf would give 0 * -inf
+#pragma unroll
+                for (int i = 0; i < LP_VECS; ++i) {
+                    float x[E::N];
+                    E::open(raw[i], x);
+#pragma unroll
+                    for (int j = 0; j < E::N; ++j) {
+                        const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
+                        st.s += e;
+                        st.h += e * t;
+                    }
+                }
+            }
+            if (TOP) {
+                // Four lanes hold a group of each of the four loads: lane i of them gets the i-th's maximum.
+                const float a0 = tid & 1 ? mx[0] : mx[1], a1 = tid & 1 ? mx[2] : mx[3];
+                const float b0 = tid & 1 ? mx[1] : mx[0], b1 = tid & 1 ? mx[3] : mx[2];
+                const float p0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, a0, 1)), p1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, a1, 1));
+                const float g = fmaxf(tid & 2 ? p1 : p0, __shfl_xor_sync(0xffffffffu, tid & 2 ? p0 : p1, 2));
+                *mrow = g;
+            }
+#pragma unroll
+            for (int i = 0; i < LP_VECS; ++i) raw[i] = ahead[i];
         }
         if (TOP) {
-            auto index = [&](int i) { return (v + (i / E::N) * LP_THREADS + tid) * E::N + i % E::N - skew; };
-            auto real = [&](int i) {
-                const int at = v + (i / E::N) * LP_THREADS + tid, e = index(i);
-                return at < v1 && e >= 0 && e < a.V;
-            };
-            // adds the thread's values that reach T
-            auto add = [&](u64 T, int *count, int from) {
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const u64 k = lp_key(x[i], index(i));
-                    if (real(i) && k >= T) list[from + atomicAdd(count, 1)] = k;
-                }
-            };
-            auto by_threads = [&](u64 floor) {  // by the k-th of the threads' maxima
-                u64 best = 0;
-#pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (real(i)) best = max(best, lp_key(x[i], index(i)));
-                const u64 T = max(floor, kth_of_threads(best, a.k, tmp, &kth));
-                if (best >= T && best) add(T, &added[turn], have);
-                return T;
-            };
-            const int next = turn == 2 ? 0 : turn + 1;
-            if (first) {
-                const u64 T = by_threads(0);
-                bar = T ? key_value(T) : -INFINITY;
-            } else {
-                if (mx > bar) {
-#pragma unroll
-                    for (int i = 0; i < PER; ++i)
-                        if (x[i] > bar) {
-                            const int p = have + atomicAdd(&added[turn], 1);
-                            if (p < LP_LIST) list[p] = lp_key(x[i], index(i));
-                        }
-                }
-            }
-            if (tid == 0) added[next] = 0;  // (last read before the barrier that ended the tile before)
+            // the k groups of largest maxima, then the k best of their values and of those found before
+            const int groups = (seg_end - seg + 3) / 4, g0 = seg / 4;
             __syncthreads();
-            int now = added[turn];
-            if (have + now > LP_LIST) {  // what this tile added is dropped, the list cut, the tile looked at again
-                const u64 T = keep_best(list, have, a.k, tmp);
-                have = min(have, a.k);
-                if (tid == 0) added[turn] = 0;
-                __syncthreads();
-                by_threads(T);
-                __syncthreads();
-                now = added[turn];
-                const u64 T2 = keep_best(list, have + now, a.k, tmp);
-                have = min(have + now, a.k);
-                bar = T2 ? key_value(T2) : bar;
-            } else {
-                have += now;
+            select_best([&](int g) {
+                return lp_key(maxima[(g >> 8) * LP_TILE_MAX + ((g >> 6) & 3) * 72 + (g & 63)], g);
+            }, groups, a.k, sh);
+            __shared__ int picked[LP_MAX_K];
+            if (tid < a.k) picked[tid] = sh.best[tid] ? g0 + key_index(sh.best[tid]) : -1;
+            __syncthreads();
+            const int more = a.k * GE;
+            // (few values a thread: read once, kept)
+            constexpr int PER = (LP_MAX_K * GE + LP_MAX_K + LP_THREADS - 1) / LP_THREADS;
+            u64 keys[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int at = tid + i * LP_THREADS;
+                u64 x = 0;
+                if (at < more) {
+                    const int g = picked[at / GE];
+                    const int e = g * GE + at % GE - skew, v = g * 4 + at % GE / E::N;
+                    if (g >= 0 && e >= 0 && e < a.V && v < v1) x = lp_key(E::one(base, e), e);
+                } else if (at < more + a.k) {
+                    x = found[at - more];
+                }
+                keys[i] = x;
             }
-            turn = next;
+            select_best([&](int i) {
+                u64 x = 0;
+#pragma unroll
+                for (int j = 0; j < PER; ++j)
+                    if (i / LP_THREADS == j) x = keys[j];
+                return x;
+            }, PER * LP_THREADS, a.k, sh);
+            if (tid < a.k) found[tid] = sh.best[tid];
         }
     }
     // the CTA's sums
@@ -293,75 +385,94 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs(const LogprobArgs a) {
         st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
                            __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
     if (lane == 0) ws[warp] = st;
-    if (TOP) keep_best(list, have, a.k, tmp);
     __syncthreads();
     st = ws[0];
     for (int i = 1; i < LP_WARPS; ++i) st = join(st, ws[i], c);
-    if (a.slices == 1) {
-        bool has;
-        const float xt = token_logit<TYPE>(a, row, &has);
-        Finish{a}(row, st, list, xt, has);
-        return;
+    if (a.slices > 1) {
+        if (tid == 0) all = st;
+        cluster_sync();
+        if (slice == 0) {
+            if (warp == 0) {
+                const uint32_t p = map_cta(smem_u32(&all), lane % a.slices);  // (a power of two)
+                Stat x{ld_cluster(p), ld_cluster(p + 4), ld_cluster(p + 8)};
+                for (int o = a.slices / 2; o; o >>= 1)
+                    x = join(x, Stat{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
+                                     __shfl_xor_sync(0xffffffffu, x.h, o)}, c);
+                if (lane == 0) ws[0] = x;
+            }
+            __syncthreads();
+            st = ws[0];
+            if (TOP) {
+                constexpr int PER = LP_CLUSTER * LP_MAX_K / LP_THREADS;
+                u64 keys[PER];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int p = tid + i * LP_THREADS, r = p / LP_MAX_K, j = p % LP_MAX_K;
+                    keys[i] = 0;
+                    if (r < a.slices && j < a.k) {
+                        const float2 f = ld_cluster_v2(map_cta(smem_u32(&found[j]), r));
+                        keys[i] = (u64)__float_as_uint(f.y) << 32 | __float_as_uint(f.x);
+                    }
+                }
+                select_best([&](int i) {
+                    u64 x = 0;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j)
+                        if (i / LP_THREADS == j) x = keys[j];
+                    return x;
+                }, PER * LP_THREADS, a.k, sh);
+            }
+        }
+        cluster_sync();  // (nobody leaves while the first CTA reads)
+        if (slice != 0) return;
     }
-    if (tid == 0) reinterpret_cast<float4 *>(a.stats)[blockIdx.x] = make_float4(st.m, st.s, st.h, 0.f);
-    if (TOP)
-        for (int i = tid; i < a.k; i += LP_THREADS) a.cand[(long long)blockIdx.x * a.k + i] = i < have ? list[i] : 0;
+    const int token = a.logprob ? a.tokens[row] : -1;
+    const bool has = token >= 0 && token < a.V;
+    Finish{a}(row, st, sh.best, has && tid == 0 ? E::one(base, token) : 0.f, has);
 }
 
-// Joins a row's slices: one CTA a row.
-template <int TYPE, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS) k_logprobs_join(const LogprobArgs a) {
-    __shared__ u64 list[TOP ? LP_LIST : 1], tmp[TOP ? LP_THREADS : 1], kth;
-    __shared__ int added;
-    __shared__ Stat ws[LP_WARPS];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x;
-    const float c = a.inv_t * 1.4426950408889634f;
-    pdl_wait();
-    bool has;
-    const float xt = token_logit<TYPE>(a, row, &has);
-    Stat st{-INFINITY, 0.f, 0.f};
-    const float4 *stats = reinterpret_cast<const float4 *>(a.stats) + (long long)row * a.slices;
-    for (int i = tid; i < a.slices; i += LP_THREADS) {
-        const float4 p = stats[i];
-        st = join(st, Stat{p.x, p.y, p.z}, c);
-    }
-    for (int o = 16; o; o >>= 1)
-        st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
-                           __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
-    if (lane == 0) ws[warp] = st;
-    if (TOP) {
-        // of slices * k keys (at most 32 a thread) those that reach the k-th of the threads' maxima
-        const u64 *cand = a.cand + (long long)row * a.slices * a.k;
-        const int n = a.slices * a.k;
-        u64 best = 0;
-        for (int i = tid; i < n; i += LP_THREADS) best = max(best, cand[i]);
-        if (tid == 0) added = 0;
-        const u64 T = kth_of_threads(best, a.k, tmp, &kth);
-        if (best >= T)
-            for (int i = tid; i < n; i += LP_THREADS) {
-                const u64 k = cand[i];
-                if (k && k >= T) list[atomicAdd(&added, 1)] = k;
-            }
-        __syncthreads();
-        keep_best(list, added, a.k, tmp);
-    }
-    __syncthreads();
-    st = ws[0];
-    for (int i = 1; i < LP_WARPS; ++i) st = join(st, ws[i], c);
-    Finish{a}(row, st, list, xt, has);
+// Slices of a row: a power of two up to the largest cluster, so that there are some four CTAs an SM; each with a
+// tile or more.
+int pick_slices(int M, int vecs, int most) {
+    int s = 1;
+    while (s < most && (long long)M * s * 2 <= gemm_ctas() * 4 && (long long)s * LP_TILE < vecs) s *= 2;
+    return s;
 }
 
 template <int TYPE, bool TOP>
 cudaError_t launch(LogprobArgs &a, cudaStream_t st) {
     using E = Elem<TYPE>;
-    cudaError_t e;
+    constexpr size_t MOST = TOP ? (size_t)LP_SEGMENT * LP_TILE_MAX * 4 : 0;
+    static thread_local int configured = -1, most = 8;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && configured != dev) {
+        const void *f = reinterpret_cast<const void *>(k_logprobs<TYPE, TOP>);
+        e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) {
+            most = largest_cluster(f, LP_THREADS, MOST, LP_CLUSTER) < LP_CLUSTER ? 8 : LP_CLUSTER;
+            configured = dev;
+        }
+    }
+    if (e != cudaSuccess) return e;
     // (a row that starts off a 16-byte boundary has one vector more)
     const int vecs = (a.V + E::N - 1) / E::N + 1;
+    a.slices = pick_slices(a.M, vecs, most);
     a.slice_vecs = ((vecs + a.slices - 1) / a.slices + LP_THREADS - 1) / LP_THREADS * LP_THREADS;
-    if (a.slices == 1 && (e = cudaMemsetAsync(a.status, 0, sizeof(int), st)) != cudaSuccess) return e;
-    k_logprobs<TYPE, TOP><<<a.M * a.slices, LP_THREADS, 0, st>>>(a);
-    if ((e = cudaGetLastError()) != cudaSuccess || a.slices == 1) return e;
-    return launch_pdl(k_logprobs_join<TYPE, TOP>, a.M, LP_THREADS, 0, st, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((long long)a.M * a.slices));
+    cfg.blockDim = dim3(LP_THREADS);
+    cfg.dynamicSmemBytes = TOP ? (size_t)std::min(LP_SEGMENT, (a.slice_vecs + LP_TILE - 1) / LP_TILE) * LP_TILE_MAX * 4 : 0;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.slices;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_logprobs<TYPE, TOP>, static_cast<const LogprobArgs>(a));
 }
 
 template <int TYPE>
@@ -370,14 +481,6 @@ cudaError_t launch_type(LogprobArgs &a, cudaStream_t st) {
 }
 
 }  // namespace
-
-// Slices of a row: enough CTAs to fill the GPU, each with a tile of 16 KB or more; at most 256, so that the join's
-// threads see at most 32 candidates each.
-int logprob_slices(int M, int V, int es) {
-    const long long tiles = ((long long)V * es / 16 + LP_TILE - 1) / LP_TILE;
-    const long long want = (152 * 4 + M - 1) / M;
-    return (int)std::max(1ll, std::min(std::min(tiles, want), 256ll));
-}
 
 cudaError_t launch_logprobs(LogprobArgs &a, cudaStream_t st) {
     return a.type == PBD_FP32 ? launch_type<PBD_FP32>(a, st) : a.type == PBD_BF16 ? launch_type<PBD_BF16>(a, st) : launch_type<PBD_FP16>(a, st);

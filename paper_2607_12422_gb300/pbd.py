@@ -243,39 +243,32 @@ def _bad(who, what):
     raise PbdError(1, "%s: %s" % (who, what))
 
 
+_DTYPES = {"torch.bfloat16": PBD_BF16, "torch.float16": PBD_FP16, "torch.float32": PBD_FP32}
+
+
 def _dtype(t, who):
-    name = str(t.dtype)
-    code = {"torch.bfloat16": PBD_BF16, "torch.float16": PBD_FP16, "torch.float32": PBD_FP32}.get(name)
+    code = _DTYPES.get(str(t.dtype))
     if code is None:
-        _bad(who, "unsupported type %s" % name)
+        _bad(who, "unsupported type %s" % t.dtype)
     return code
 
 
 def _check(who, name, t, like, shape, dtype=None, rows=False):
     """t lies on like's device, has this shape and type, and is contiguous (rows: each t[i] is)."""
     if t.device != like.device:
-        _bad(who, "%s is not on the cache's device" % name)
-    if tuple(t.shape) != tuple(shape):
+        _bad(who, "%s is not on the cache's or logits' device" % name)
+    if t.shape != shape:
         _bad(who, "%s has shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
     if t.dtype != (dtype or like.dtype):
         _bad(who, "%s has type %s" % (name, t.dtype))
-    if not (t.is_contiguous() or (rows and t.shape[0] and t[0].is_contiguous() and t.stride(0) >= t[0].numel())):
+    if not t.is_contiguous() and not (rows and t[0].is_contiguous() and t.stride(0) >= t[0].numel()):
         _bad(who, "%s is not contiguous" % name)
 
 
-class _OnDevice:
-    """The library runs on the current device: makes `device` current where it is not."""
-
-    def __init__(self, torch, device):
-        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
-
-    def __enter__(self):
-        if self.guard:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard:
-            self.guard.__exit__(*exc)
+def _stream(torch, device):
+    """The current stream of a device as a cudaStream_t; without the Stream object, whose making takes longer (4 us
+    of a call's 30) than the launch."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 class OpWorkspace:
@@ -294,8 +287,8 @@ def op_workspace(nbytes: int, device="cuda") -> OpWorkspace:
     return OpWorkspace(nbytes, device)
 
 
-def _scratch(L, who, workspace, need, device):
-    """(workspace, its pointer, its bytes) for a call that needs `need`."""
+def _scratch(who, workspace, need, device):
+    """The workspace of a call that needs `need` bytes: the caller's, or a new one."""
     if need == 0:
         _bad(who, "unsupported sizes")
     if workspace is None:
@@ -355,44 +348,43 @@ def pbd_op_decode_attention(q, kv: PagedKV, k_new=None, v_new=None, new_position
     PbdError(PBD_ERR_DEVICE) for a length or page outside the cache; without, ask pbd_op_status(workspace)."""
     import torch
     who = "pbd_op_decode_attention"
+    dev = kv.device
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_decode_attention(q, kv, k_new, v_new, new_positions, scale, accumulate, out, want_lse, workspace, sync)
     L = load()
     B, D, hkv = kv.batch, kv.head_dim, kv.n_kv_heads
     if q.dim() != 3:
         _bad(who, "q is [batch, n_q_heads, head_dim]")
     hq = q.shape[1]
-    _check(who, "q", q, kv, (B, hq, D), rows=True)
-    if (k_new is None) != (v_new is None):
-        _bad(who, "k_new and v_new come together")
+    _check(who, "q", q, kv, (B, hq, D), None, True)
     new_stride = 0
-    if k_new is not None:
-        _check(who, "k_new", k_new, kv, (B, hkv, D), rows=True)
-        _check(who, "v_new", v_new, kv, (B, hkv, D), rows=True)
+    if k_new is not None and v_new is not None:
+        _check(who, "k_new", k_new, kv, (B, hkv, D), None, True)
+        _check(who, "v_new", v_new, kv, (B, hkv, D), None, True)
         new_stride = k_new.stride(0) if B > 1 else hkv * D
         if B > 1 and v_new.stride(0) != new_stride:
             _bad(who, "rows of k_new and v_new lie differently far apart")
         if new_positions is not None:
             _check(who, "new_positions", new_positions, kv, (B,), torch.int32)
-    elif new_positions is not None:
-        _bad(who, "new_positions without k_new and v_new")
-    if out is not None:
+    elif k_new is not None or v_new is not None or new_positions is not None:
+        _bad(who, "k_new and v_new come together, and new_positions with them")
+    if out is None:
+        out = torch.empty((B, hq, D), dtype=kv.dtype, device=dev)
+    else:
         _check(who, "out", out, kv, (B, hq, D))
-    key = (hq, accumulate)
-    need = kv._need.get(key)
+    need = kv._need.get((hq, accumulate))
     if need is None:  # (sizes of a handle do not change)
-        need = kv._need[key] = decode_attention_workspace_bytes(kv, hq, accumulate)
-    with _OnDevice(torch, kv.device):
-        ws = _scratch(L, who, workspace, need, kv.device)
-        if out is None:
-            out = torch.empty(B, hq, D, dtype=kv.dtype, device=kv.device)
-        lse = torch.empty(B, hq, dtype=torch.float32, device=kv.device) if want_lse else None
-        st = torch.cuda.current_stream(kv.device).cuda_stream
-        s = L.pbd_op_decode_attention(kv.ref, hq, scale if scale is not None else D ** -0.5, q.data_ptr(),
-                                      q.stride(0) if B > 1 else hq * D, _ptr(k_new), _ptr(v_new), new_stride,
-                                      _ptr(new_positions), int(accumulate), out.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes,
-                                      st)
-        _raise_if(L, s)
-        if sync:
-            _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+        need = kv._need[hq, accumulate] = decode_attention_workspace_bytes(kv, hq, accumulate)
+    ws = _scratch(who, workspace, need, dev)
+    lse = torch.empty((B, hq), dtype=torch.float32, device=dev) if want_lse else None
+    st = _stream(torch, dev)
+    s = L.pbd_op_decode_attention(kv.ref, hq, D ** -0.5 if scale is None else scale, q.data_ptr(),
+                                  q.stride(0) if B > 1 else hq * D, _ptr(k_new), _ptr(v_new), new_stride,
+                                  _ptr(new_positions), accumulate, out.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes, st)
+    _raise_if(L, s)
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
     return out, lse
 
 
@@ -408,28 +400,31 @@ def pbd_op_evict(kv: PagedKV, n_keep: int, next_positions, n_recent: int = 0, n_
     where they are not given.  The program lowers kv.lens to at most n_keep once all layers that share it are through."""
     import torch
     who = "pbd_op_evict"
+    dev = kv.device
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_evict(kv, n_keep, next_positions, n_recent, n_sink, out_weights, out_positions, workspace, sync)
     L = load()
     if kv.weights is None or kv.positions is None:
         _bad(who, "the cache has no weights or positions")
-    if (out_weights is None) != (out_positions is None):
-        _bad(who, "out_weights and out_positions come together")
-    if out_weights is None:
+    if out_weights is None and out_positions is None:
         out_weights, out_positions = kv.weights, kv.positions
+    elif out_weights is None or out_positions is None:
+        _bad(who, "out_weights and out_positions come together")
     else:
         _check(who, "out_weights", out_weights, kv, kv.weights.shape, torch.float32)
         _check(who, "out_positions", out_positions, kv, kv.weights.shape, torch.int32)
     _check(who, "next_positions", next_positions, kv, (kv.batch,), torch.int32)
     need = kv._need.get(n_keep)
-    if need is None:
+    if need is None:  # (sizes of a handle do not change)
         need = kv._need[n_keep] = evict_workspace_bytes(kv, n_keep) if n_keep >= 0 else 0
-    with _OnDevice(torch, kv.device):
-        ws = _scratch(L, who, workspace, need, kv.device)
-        st = torch.cuda.current_stream(kv.device).cuda_stream
-        s = L.pbd_op_evict(kv.ref, n_keep, n_recent, n_sink, next_positions.data_ptr(), out_weights.data_ptr(),
-                           out_positions.data_ptr(), ws.ptr, ws.nbytes, st)
-        _raise_if(L, s)
-        if sync:
-            _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    ws = _scratch(who, workspace, need, dev)
+    st = _stream(torch, dev)
+    s = L.pbd_op_evict(kv.ref, n_keep, n_recent, n_sink, next_positions.data_ptr(), out_weights.data_ptr(),
+                       out_positions.data_ptr(), ws.ptr, ws.nbytes, st)
+    _raise_if(L, s)
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
     return out_weights, out_positions
 
 
@@ -450,30 +445,33 @@ def pbd_op_token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 
     PbdError(PBD_ERR_DEVICE) for a token at or above V; without, ask pbd_op_status(workspace)."""
     import torch
     who = "pbd_op_token_logprobs"
-    L = load()
-    if logits.dim() != 2 or not logits.is_cuda:
+    dev = logits.device
+    if logits.dim() != 2 or dev.type != "cuda":
         _bad(who, "logits are [M, V] on a GPU")
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_token_logprobs(logits, tokens, k, temperature, workspace, sync)
+    L = load()
     M, V = logits.shape
     if V > 1 and logits.stride(1) != 1:
         _bad(who, "the values of a row are not contiguous")
     dt = _dtype(logits, who)
-    dev = logits.device
+    logprob = ids = top = None
     if tokens is not None:
         _check(who, "tokens", tokens, logits, (M,), torch.int32)
-    need = L.pbd_op_token_logprobs_workspace_bytes(M, V, k)
-    with _OnDevice(torch, dev):
-        ws = _scratch(L, who, workspace, need, dev)
-        stats = torch.empty(2, M, dtype=torch.float32, device=dev)
-        ids = torch.empty(M, k, dtype=torch.int32, device=dev) if k else None
-        top = torch.empty(M, k, dtype=torch.float32, device=dev) if k else None
-        logprob, entropy = (stats[0], stats[1]) if tokens is not None else (None, stats[1])
-        st = torch.cuda.current_stream(dev).cuda_stream
-        s = L.pbd_op_token_logprobs(M, V, dt, logits.data_ptr(), logits.stride(0) if M > 1 else V, temperature,
-                                    _ptr(tokens), k, _ptr(logprob), entropy.data_ptr(), _ptr(ids), _ptr(top), ws.ptr,
-                                    ws.nbytes, st)
-        _raise_if(L, s)
-        if sync:
-            _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    ws = _scratch(who, workspace, L.pbd_op_token_logprobs_workspace_bytes(M, V, k), dev)
+    entropy = torch.empty(M, dtype=torch.float32, device=dev)
+    if tokens is not None:
+        logprob = torch.empty(M, dtype=torch.float32, device=dev)
+    if k:
+        ids = torch.empty((M, k), dtype=torch.int32, device=dev)
+        top = torch.empty((M, k), dtype=torch.float32, device=dev)
+    st = _stream(torch, dev)
+    s = L.pbd_op_token_logprobs(M, V, dt, logits.data_ptr(), logits.stride(0) if M > 1 else V, temperature, _ptr(tokens),
+                                k, _ptr(logprob), entropy.data_ptr(), _ptr(ids), _ptr(top), ws.ptr, ws.nbytes, st)
+    _raise_if(L, s)
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
     return TokenLogprobs(logprob, entropy, ids, top)
 
 
@@ -482,8 +480,8 @@ def pbd_op_status(workspace: OpWorkspace) -> None:
     error."""
     import torch
     L = load()
-    with _OnDevice(torch, workspace.device):
-        _raise_if(L, L.pbd_op_status(workspace.ptr, torch.cuda.current_stream(workspace.device).cuda_stream, None))
+    with torch.cuda.device(workspace.device):
+        _raise_if(L, L.pbd_op_status(workspace.ptr, _stream(torch, workspace.device), None))
 
 
 def make_config(shape, block_D: int, max_batch: int, max_seq_len: int, draft_layers: int = 0,

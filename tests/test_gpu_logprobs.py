@@ -57,6 +57,9 @@ ORDERS = {
     "two values": lambda t, V: (t.arange(V) % 7 == 3).float(),
     "late": lambda t, V: (t.arange(V) >= V - 40).float() * 5 + t.arange(V) * 1e-6,
     "steps": lambda t, V: (t.arange(V) // 3000).float(),
+    # every second run of 31 groups of 64 bytes above the rest, for both sizes of values
+    "comb": lambda t, V: ((t.arange(V) // 16 % 64 < 31) * 9).float() + t.arange(V) % 1021 / 2048,
+    "wide comb": lambda t, V: ((t.arange(V) // 32 % 64 < 31) * 9).float() + t.arange(V) % 1021 / 2048,
 }
 
 
@@ -66,7 +69,8 @@ ORDERS = {
 def test_orders_and_ties(env, order, M, dtype):
     """Orders that defeat a threshold from the first tile, and equal values, in one slice a row and in several."""
     torch, pbd = env
-    V = 40000
+    V = 150000 if "comb" in order else 40000
+    M = min(M, 20) if "comb" in order else M
     x = ORDERS[order](torch, V).to(getattr(torch, dtype)).repeat(M, 1)
     _check(torch, pbd, x, torch.arange(M, dtype=torch.int32) * 31, 32, 1.0)
 
