@@ -6,9 +6,10 @@
 // fewest bytes there are, and no move's source is another's target.
 //
 // One cluster works on one (sequence, KV head), each CTA on a stretch of its slots.  The keep-th largest key is found by radix
-// selection, 8 bits a round, over 32-bit keys in shared memory; a round's histograms are exchanged through
-// distributed shared memory.  Then warps count and place holes and kept slots with ballots, and the CTAs share the
-// moves.
+// selection over 32-bit keys in shared memory, 11, 11 and 10 bits a round (11 put sign, exponent and two bits of the mantissa
+// into the first: weights of few magnitudes still spread over many counters).  After a round every CTA adds its counters that are
+// not zero, which are few, to each CTA's totals in distributed shared memory.  Then warps count and place holes and kept slots with ballots, and the cluster's
+// warps share the moves, 32 at a time: each lane finds the rows of one, then all of them copy.
 #include <algorithm>
 
 #include "kv_ops.h"
@@ -20,11 +21,15 @@ namespace {
 constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_CLUSTER = 8;        // CTAs of a cluster at most
 constexpr int EV_KEYS = 48 * 1024;   // keys of a CTA that fit shared memory
+constexpr int EV_BINS = 2048;
 
-__device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t a) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+__device__ __forceinline__ uint2 ld_cluster_u32x2(uint32_t a) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
     return v;
+}
+__device__ __forceinline__ void red_cluster_add(uint32_t a, uint32_t v) {
+    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
 
 // Order of the slots: kept tokens first (all ones), then by weight, NaN last (0).
@@ -35,124 +40,189 @@ __device__ __forceinline__ uint32_t order_key(float w, int pos, int n_sink, int 
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-template <bool IN_SMEM>
-__global__ void __launch_bounds__(EV_THREADS) k_evict(const EvictArgs a, int C) {
+// Slots of sequence b.  Lengths and pages outside their ranges are read as nothing, and reported once for the call: the
+// grid's last cluster looks at all of them, so that the status word has one writer and needs no clearing before.
+__device__ __forceinline__ int slots_of(const EvictArgs &a, int b) {
+    return (int)max(0ll, min((long long)a.kv.lens[b], a.kv.cap));
+}
+__device__ void check_cache(const EvictArgs &a) {
+    int code = DEV_OK;
+    for (int b = 0; b < a.kv.B; ++b) {
+        const int n = slots_of(a, b);
+        if (a.kv.lens[b] != n) code = DEV_BAD_POSITION;
+        const int pages = n <= a.n_keep ? 0 : (n + a.kv.page_size - 1) / a.kv.page_size;
+        for (int i = threadIdx.x; i < pages; i += EV_THREADS)
+            if ((unsigned)a.kv.table[(long long)b * a.kv.max_pages + i] >= (unsigned)a.kv.n_pages) code = DEV_BAD_PAGE;
+    }
+    const int length = __syncthreads_or(code == DEV_BAD_POSITION), page = __syncthreads_or(code == DEV_BAD_PAGE);
+    if (threadIdx.x == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
+}
+
+template <bool IN_SMEM, bool ALONE>  // ALONE: clusters of one CTA
+__global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int cluster) {
     extern __shared__ __align__(16) uint32_t keys[];
-    __shared__ uint32_t hist[2][256];
-    __shared__ uint32_t total[256];
-    __shared__ uint32_t pick[2];
-    __shared__ uint32_t warp_cnt[EV_WARPS], cta_cnt[3];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rank = blockIdx.x % C, row = blockIdx.x / C, b = row / a.kv.hkv, h = row - b * a.kv.hkv;
-    const long long cap = a.kv.cap, raw = a.kv.lens[b];
-    const int n = (int)max(0ll, min(raw, cap)), keep = min(n, a.n_keep);
-    if (tid == 0 && rank == 0 && raw != n) latch_error(a.status, DEV_BAD_POSITION);
+    __shared__ __align__(16) uint32_t hist[EV_BINS];                 // this CTA's counters of a round
+    __shared__ __align__(16) uint32_t totals[ALONE ? 1 : 3][EV_BINS];  // the cluster's, of each round
+    __shared__ uint32_t pick[3], warp_cnt[2][EV_WARPS];
+    __shared__ __align__(8) uint2 cta_cnt[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = ALONE ? 1 : cluster;
+    const int rank = ALONE ? 0 : blockIdx.x % C, row = ALONE ? blockIdx.x : blockIdx.x / C;
+    if (row == a.kv.B * a.kv.hkv) {
+        if (rank == 0) check_cache(a);
+        return;
+    }
+    auto sync = [&]() {
+        if (ALONE)
+            __syncthreads();
+        else
+            cluster_sync();
+    };
+    const int b = row / a.kv.hkv, h = row - b * a.kv.hkv, n = slots_of(a, b), keep = min(n, a.n_keep);
+    if (keep == 0) return;
+    const long long cap = a.kv.cap;
     const float *w = a.kv.weights + row * cap;
     const int *pos = a.kv.positions + row * cap;
     float *out_w = a.out_weights + row * cap;
     int *out_pos = a.out_positions + row * cap;
-    const bool copy = out_w != w;
-    if (n == keep) {
-        if (copy)
-            for (int i = rank * EV_THREADS + tid; i < n; i += C * EV_THREADS) {
-                out_w[i] = w[i];
-                out_pos[i] = pos[i];
-            }
-        return;
-    }
-    if (keep == 0) return;
-    const long long rf = (long long)a.next_pos[b] - a.n_recent;
-    const int recent_from = (int)max(-2147483647ll - 1, rf);
+    const int copied = out_w != w ? keep : 0;  // slots in front are copied as they are, and holes then filled
+    const int recent_from = (int)max(-2147483647ll - 1, (long long)a.next_pos[b] - a.n_recent);
     // this CTA's slots, and a warp's part of them (whole groups of 32)
     const int per_warp = ((n + C - 1) / C + EV_THREADS - 1) / EV_THREADS * 32, per = per_warp * EV_WARPS;
     const int s0 = (int)min((long long)n, (long long)rank * per), s1 = (int)min((long long)n, (long long)s0 + per);
+    const uint4 zeros = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4 *>(hist + tid * 4) = zeros;
+    if (!ALONE)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4 *>(totals[i] + tid * 4) = zeros;
+    constexpr int AHEAD = 8;
+    for (int i0 = s0 + tid; i0 < s1; i0 += EV_THREADS * AHEAD) {
+        float x[AHEAD];
+        int p[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int i = i0 + j * EV_THREADS;
+            if (i < s1) {
+                x[j] = w[i];
+                p[j] = pos[i];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int i = i0 + j * EV_THREADS;
+            if (i >= s1) continue;
+            if (IN_SMEM) keys[i - s0] = order_key(x[j], p[j], a.n_sink, recent_from);
+            if (i < copied) {
+                out_w[i] = x[j];
+                out_pos[i] = p[j];
+            }
+        }
+    }
+    if (n == keep) return;
     auto key_at = [&](int slot) {
         return IN_SMEM ? keys[slot - s0] : order_key(w[slot], pos[slot], a.n_sink, recent_from);
     };
-    if (IN_SMEM)
-        for (int i = s0 + tid; i < s1; i += EV_THREADS) keys[i - s0] = order_key(w[i], pos[i], a.n_sink, recent_from);
 
+    sync();  // (the cluster's CTAs run, and their totals are zero)
     uint32_t prefix = 0;  // the digits found so far
     int want = keep;      // the want-th largest of the keys that begin with them
-    for (int round = 0; round < 4; ++round) {
-        const int shift = 24 - 8 * round;
-        uint32_t *hs = hist[round & 1];
-        for (int i = tid; i < 256; i += EV_THREADS) hs[i] = 0;
-        __syncthreads();
+    bool all_equal_kept = false;
+#pragma unroll
+    for (int round = 0; round < 3; ++round) {
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, above = round == 1 ? 21 : 10;
+        const uint32_t mask = round == 2 ? 1023u : 2047u;
         for (int i = s0 + tid; i < s1; i += EV_THREADS) {
             const uint32_t k = key_at(i);
-            const bool in = round == 0 || (k >> (shift + 8)) == prefix;
-            if (in) atomicAdd(&hs[(k >> shift) & 255], 1u);
-        }
-        cluster_sync();
-        if (tid < 256) {
-            uint32_t sum = 0;
-            const uint32_t at = smem_u32(&hs[tid]);
-            for (int c = 0; c < C; ++c) sum += ld_cluster_u32(map_cta(at, c));
-            total[tid] = sum;
+            if (round == 0 || (k >> above) == prefix) atomicAdd(&hist[(k >> shift) & mask], 1u);
         }
         __syncthreads();
-        if (warp == 0) {
-            // lane's 8 digits, from the largest down
-            uint32_t mine = 0, d[8];
+        // this thread's four digits, from the largest down
+        const int at = EV_BINS - 4 - tid * 4;
+        uint4 d = *reinterpret_cast<const uint4 *>(hist + at);
+        *reinterpret_cast<uint4 *>(hist + at) = zeros;
+        if (!ALONE) {
+            const uint32_t own[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                d[i] = total[255 - (lane * 8 + i)];
-                mine += d[i];
-            }
-            uint32_t x = mine;
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-                if (lane >= o) x += y;
-            }
-            uint32_t before = x - mine;
+            for (int i = 0; i < 4; ++i)
+                if (own[i])
+                    for (int c = 0; c < C; ++c) red_cluster_add(map_cta(smem_u32(&totals[round][at + i]), c), own[i]);
+            sync();
+            d = *reinterpret_cast<const uint4 *>(totals[round] + at);
+        }
+        const uint32_t mine = d.x + d.y + d.z + d.w;
+        uint32_t x = mine;
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) warp_cnt[0][warp] = x;
+        __syncthreads();
+        uint32_t before = x - mine;
+        for (int i = 0; i < warp; ++i) before += warp_cnt[0][i];
+        const uint32_t ds[4] = {d.w, d.z, d.y, d.x};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (before < (uint32_t)want && before + d[i] >= (uint32_t)want) {
-                    pick[0] = 255 - (lane * 8 + i);
-                    pick[1] = before;
-                }
-                before += d[i];
+        for (int i = 0; i < 4; ++i) {
+            if (before < (uint32_t)want && before + ds[i] >= (uint32_t)want) {
+                pick[0] = at + 3 - i;
+                pick[1] = before;
+                pick[2] = ds[i];
             }
+            before += ds[i];
         }
         __syncthreads();
-        prefix = prefix << 8 | pick[0];
+        prefix = prefix << (round == 2 ? 10 : 11) | pick[0];
         want -= (int)pick[1];
+        all_equal_kept = (int)pick[2] == want;
     }
     const uint32_t T = prefix;  // kept: larger keys, and of the equal ones the first `want`
     const int w0 = min(s1, s0 + warp * per_warp), w1 = min(s1, w0 + per_warp);
 
-    // equal keys before this warp
-    int eq = 0;
-    for (int i = w0; i < w1; i += 32) {
-        const int s = i + lane;
-        eq += __popc(__ballot_sync(0xffffffffu, s < w1 && key_at(s) == T));
-    }
-    // the sum of `mine` over the warps before this one, in the cluster's order of slots
-    auto before_me = [&](int mine, int which) {
-        if (lane == 0) warp_cnt[warp] = mine;
+    // two sums over the warps before this one, in the cluster's order of slots, and over all
+    auto before_me = [&](uint2 mine, int which, uint2 *sum) {
+        if (lane == 0) warp_cnt[0][warp] = mine.x, warp_cnt[1][warp] = mine.y;
         __syncthreads();
-        int b4 = 0, all = 0;
+        uint2 b4 = make_uint2(0, 0), all = b4;
         for (int i = 0; i < EV_WARPS; ++i) {
-            if (i < warp) b4 += warp_cnt[i];
-            all += warp_cnt[i];
+            const uint32_t x = warp_cnt[0][i], y = warp_cnt[1][i];
+            if (i < warp) b4.x += x, b4.y += y;
+            all.x += x, all.y += y;
         }
-        if (tid == 0) cta_cnt[which] = all;
-        cluster_sync();
-        const uint32_t at = smem_u32(&cta_cnt[which]);
-        for (int c = 0; c < rank; ++c) b4 += ld_cluster_u32(map_cta(at, c));
+        if (!ALONE) {
+            if (tid == 0) cta_cnt[which] = all;
+            sync();
+            const uint32_t at = smem_u32(&cta_cnt[which]);
+            all = make_uint2(0, 0);
+            for (int c = 0; c < C; ++c) {
+                const uint2 x = ld_cluster_u32x2(map_cta(at, c));
+                if (c < rank) b4.x += x.x, b4.y += x.y;
+                all.x += x.x, all.y += x.y;
+            }
+        }
+        *sum = all;
         return b4;
     };
-    const int eq0 = before_me(eq, 0);
-    auto walk = [&](auto &&f) {  // f(slot, kept) for the warp's slots, 32 at a time
+    uint2 all;
+    int eq0 = 0;
+    if (!all_equal_kept) {
+        int eq = 0;
+        for (int i = w0; i < w1; i += 32) {
+            const int s = i + lane;
+            eq += __popc(__ballot_sync(0xffffffffu, s < w1 && key_at(s) == T));
+        }
+        eq0 = before_me(make_uint2(eq, 0), 0, &all).x;
+        __syncthreads();  // (warp_cnt has been read)
+    }
+    auto walk = [&](auto &&f) {  // f(slot, whether it is one, kept) for the warp's slots, 32 at a time
         int e = eq0;
         for (int i = w0; i < w1; i += 32) {
             const int s = i + lane;
             const uint32_t k = s < w1 ? key_at(s) : 0u;
-            const bool same = s < w1 && k == T;
-            const uint32_t m = __ballot_sync(0xffffffffu, same);
-            f(s, s < w1, s < w1 && (k > T || (same && e + __popc(m & ((1u << lane) - 1)) < want)));
-            e += __popc(m);
+            bool kept = k >= T;
+            if (!all_equal_kept) {
+                const uint32_t m = __ballot_sync(0xffffffffu, s < w1 && k == T);
+                kept = k > T || (k == T && e + __popc(m & ((1u << lane) - 1)) < want);
+                e += __popc(m);
+            }
+            f(s, s < w1, s < w1 && kept);
         }
     };
     int holes = 0, tails = 0;
@@ -160,7 +230,9 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(const EvictArgs a, int C) 
         holes += __popc(__ballot_sync(0xffffffffu, real && s < keep && !kept));
         tails += __popc(__ballot_sync(0xffffffffu, real && s >= keep && kept));
     });
-    int hole = before_me(holes, 1), tail = before_me(tails, 2);
+    const uint2 b4 = before_me(make_uint2(holes, tails), 1, &all);
+    const int moves = all.x;
+    int hole = b4.x, tail = b4.y;
     int *to = a.moves + (long long)row * 2 * a.most, *of = to + a.most;
     walk([&](int s, bool real, bool kept) {
         const bool is_hole = real && s < keep && !kept, is_tail = real && s >= keep && kept;
@@ -170,63 +242,62 @@ __global__ void __launch_bounds__(EV_THREADS) k_evict(const EvictArgs a, int C) 
         if (is_tail) of[tail + __popc(mt & below)] = s;
         hole += __popc(mh);
         tail += __popc(mt);
-        if (copy && real && s < keep && kept) {
-            out_w[s] = w[s];
-            out_pos[s] = pos[s];
-        }
     });
-    uint32_t moves = 0;
-    for (int c = 0; c < C; ++c) moves += ld_cluster_u32(map_cta(smem_u32(&cta_cnt[1]), c));
-    cluster_sync();  // the lists are whole, and nobody's counts are read any more
-    for (uint32_t i = rank * EV_THREADS + tid; i < moves; i += C * EV_THREADS) {
-        const int d = to[i], s = of[i];
-        out_w[d] = w[s];
-        out_pos[d] = pos[s];
-    }
-    // rows of K and V in 16-byte pieces
+    sync();  // the lists are whole, and nobody's counts are read any more
+
+    // rows of K and V in 16-byte pieces: a warp copies 32 / pieces rows of each at a time
     const int pieces = a.kv.d / 8, lg = 31 - __clz(pieces);
     const int *table = a.kv.table + (long long)b * a.kv.max_pages;
-    uint16_t *kv[2] = {const_cast<uint16_t *>(a.kv.k), const_cast<uint16_t *>(a.kv.v)};
-    auto place = [&](int slot) {
-        const int p = table[slot / a.kv.page_size];
-        if ((unsigned)p >= (unsigned)a.kv.n_pages) {
-            latch_error(a.status, DEV_BAD_PAGE);
-            return -1ll;
-        }
-        return (long long)p * a.kv.stride_page + h * a.kv.stride_head + (long long)(slot % a.kv.page_size) * a.kv.stride_slot;
+    auto place = [&](int slot) {  // -1: no such page
+        const int q = slot / a.kv.page_size, p = table[q];
+        if ((unsigned)p >= (unsigned)a.kv.n_pages) return -1ll;
+        return (long long)p * a.kv.stride_page + h * a.kv.stride_head + (long long)(slot - q * a.kv.page_size) * a.kv.stride_slot;
     };
-    const long long all = (long long)moves << (lg + 1);
-    for (long long i = rank * EV_THREADS + tid; i < all; i += C * EV_THREADS) {
-        const int mv = (int)(i >> (lg + 1)), which = (int)(i >> lg) & 1, piece = (int)i & (pieces - 1);
-        const long long d = place(to[mv]), s = place(of[mv]);
-        if (d >= 0 && s >= 0)
-            *reinterpret_cast<int4 *>(kv[which] + d + piece * 8) = *reinterpret_cast<const int4 *>(kv[which] + s + piece * 8);
+    for (int m0 = (rank * EV_WARPS + warp) * 32; m0 < moves; m0 += C * EV_THREADS) {
+        long long dst = -1, src = -1;
+        if (m0 + lane < moves) {
+            const int d = to[m0 + lane], s = of[m0 + lane];
+            dst = place(d);
+            src = place(s);
+            out_w[d] = w[s];
+            out_pos[d] = pos[s];
+            if (dst < 0 || src < 0) dst = src = -1;
+        }
+        const int units = min(32, moves - m0) << (lg + 1);  // pieces of this batch: move, K or V, piece
+        constexpr int U = 8;
+        for (int u0 = 0; u0 < units; u0 += 32 * U) {
+            uint4 x[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int u = u0 + j * 32 + lane;
+                const long long s = __shfl_sync(0xffffffffu, src, (u >> (lg + 1)) & 31);
+                if (u < units && s >= 0) x[j] = *reinterpret_cast<const uint4 *>((u >> lg & 1 ? a.kv.v : a.kv.k) + s + (u & (pieces - 1)) * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int u = u0 + j * 32 + lane;
+                const long long d = __shfl_sync(0xffffffffu, dst, (u >> (lg + 1)) & 31);
+                if (u < units && d >= 0)
+                    *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(u >> lg & 1 ? a.kv.v : a.kv.k) + d + (u & (pieces - 1)) * 8) = x[j];
+            }
+        }
     }
 }
 
-}  // namespace
-
-cudaError_t launch_evict(const EvictArgs &a, cudaStream_t st) {
-    cudaError_t e = cudaMemsetAsync(a.status, 0, sizeof(int), st);
-    if (e != cudaSuccess) return e;
-    const int rows = a.kv.B * a.kv.hkv;
-    // CTAs of a cluster: enough for two CTAs an SM in all, each with at least 1024 slots; more where keys ask for it
-    int C = 1;
-    while (C < EV_CLUSTER && (long long)C * 1024 < a.kv.cap && (rows * C < 2 * gemm_ctas() || a.kv.cap > (long long)C * EV_KEYS)) C *= 2;
-    const long long per = (((a.kv.cap + C - 1) / C) + EV_THREADS - 1) / EV_THREADS * EV_THREADS;
-    const bool in_smem = per <= EV_KEYS;
+template <bool IN_SMEM, bool ALONE>
+cudaError_t launch(const EvictArgs &a, int C, size_t smem, cudaStream_t st) {
     static thread_local int configured = -1;
     int dev = 0;
-    if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
-    if (configured != dev) {
-        e = cudaFuncSetAttribute(k_evict<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_KEYS * 4);
-        if (e != cudaSuccess) return e;
-        configured = dev;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && configured != dev) {
+        e = cudaFuncSetAttribute(k_evict<IN_SMEM, ALONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_KEYS * 4);
+        if (e == cudaSuccess) configured = dev;
     }
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * C));
+    cfg.gridDim = dim3((unsigned)((a.kv.B * a.kv.hkv + 1) * C));  // (one cluster more: check_cache)
     cfg.blockDim = dim3(EV_THREADS);
-    cfg.dynamicSmemBytes = in_smem ? (size_t)per * 4 : 0;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -235,7 +306,19 @@ cudaError_t launch_evict(const EvictArgs &a, cudaStream_t st) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, in_smem ? k_evict<true> : k_evict<false>, a, C);
+    return cudaLaunchKernelEx(&cfg, k_evict<IN_SMEM, ALONE>, a, C);
+}
+
+}  // namespace
+
+cudaError_t launch_evict(const EvictArgs &a, cudaStream_t st) {
+    const int rows = a.kv.B * a.kv.hkv;
+    // CTAs of a cluster: as many as run at once, two an SM, each with at least 2048 slots; more where keys ask for it
+    int C = 1;
+    while (C < EV_CLUSTER && (long long)C * 2048 < a.kv.cap && (rows * C * 2 <= 2 * gemm_ctas() || a.kv.cap > (long long)C * EV_KEYS)) C *= 2;
+    const long long per = (((a.kv.cap + C - 1) / C) + EV_THREADS - 1) / EV_THREADS * EV_THREADS;
+    if (per > EV_KEYS) return launch<false, false>(a, C, 0, st);  // (C is EV_CLUSTER)
+    return C == 1 ? launch<true, true>(a, C, (size_t)per * 4, st) : launch<true, false>(a, C, (size_t)per * 4, st);
 }
 
 }  // namespace pbd
