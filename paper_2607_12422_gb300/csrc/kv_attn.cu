@@ -5,11 +5,16 @@
 // in one pass over K and V with a running maximum and sum.  Every cached byte is read once and used for the few
 // query heads of its group, so memory bounds it.
 //
-// Work is cut into units of 16 slots of one (sequence, KV head).  All units of the batch form one list,
-// [sequence][KV head][tile], and each warp takes one contiguous stretch of it, all of the same length: how ragged the
-// lengths are does not matter, and the host need not know them.  A warp has its own ring of units in shared memory, filled by
-// 16-byte asynchronous copies, and never waits for another warp.  Where a stretch begins or ends inside a
-// (sequence, KV head) the warp leaves maximum, sum and unnormalised output in scratch, and k_decode_join joins them.
+// Work is cut into tiles of 16 slots of one (sequence, KV head).  A warp attends to a stretch of tiles with a ring of its own
+// in shared memory, filled by 16-byte asynchronous copies, and waits for no other warp until it is done.
+//
+// Two ways to share the tiles out:
+// - Small calls (launch): one cluster a (sequence, KV head), whose warps take a row's tiles in equal parts and join through
+//   distributed shared memory.  One launch.
+// - All others: the tiles of the whole batch form one list, [sequence][KV head][tile], and each warp takes one contiguous
+//   stretch of it, all of about the same cost: how ragged the lengths are does not matter, and the host need not know
+//   them.  Where a stretch begins or ends inside a (sequence, KV head) the warp leaves maximum, sum and unnormalised output in
+//   scratch, and k_decode_join joins them.
 //
 // Tensor cores: scores are taken as S^T = K Q^T, 16 slots by 8 heads a tile, and outputs as O^T = V^T P^T, 16 dims by 8 heads,
 // so groups of up to 8 heads waste no rows of a tile; groups up to 16 take two tiles, larger ones are cut
@@ -24,13 +29,16 @@ namespace pbd {
 namespace {
 
 constexpr int DA_WARPS = 4;
-constexpr int DA_SLOTS = 16;  // slots of a unit
-constexpr int DA_MIN_UNITS = 2;
+constexpr int DA_SLOTS = 16;      // slots of a tile
+constexpr int DA_MIN_TILES = 2;   // of a warp's stretch
+constexpr int DA_ROW_TILES = 2;   // what beginning and ending a (sequence, KV head) costs a warp, in tiles
+constexpr int DA_CLUSTER = 16;    // CTAs of a cluster at most
+constexpr int DA_CLUSTER_TILES = 16;  // tiles of its warps at most
 
 // stages of a warp's ring and CTAs that fit an SM's shared memory: 96 KB (d = 256: 192 KB) a CTA
 template <int D>
 struct DaShape {
-    static constexpr int UNIT = DA_SLOTS * D * 2 * 2;  // bytes: K rows, then V rows
+    static constexpr int UNIT = DA_SLOTS * D * 2 * 2;  // bytes of a tile: K rows, then V rows
     static constexpr int STAGES = D == 64 ? 6 : 3;
     static constexpr int CTAS = D == 256 ? 1 : 2;
     static constexpr int RING = DA_WARPS * STAGES * UNIT;
@@ -104,7 +112,10 @@ __device__ __forceinline__ int attended(const DecodeArgs &a, int b) {
     return (int)max(0ll, min((long long)a.kv.lens[b], most)) + add;
 }
 
-// first[b]: 16-slot tiles of the sequences before b, first[B] all of them; len[b]: slots attended to.  Whole CTA.
+// The list of all tiles.  A (sequence, KV head, chunk of its query heads) is a row; it counts as its tiles and DA_ROW_TILES
+// more in front, so that stretches with many short rows are shorter.  first[b]: the count of one row of each
+// sequence before b; len[b]: slots attended to.  Whole CTA.
+__device__ __forceinline__ int row_count(int n) { return n > 0 ? (n + DA_SLOTS - 1) / DA_SLOTS + DA_ROW_TILES : 0; }
 __device__ __forceinline__ void tile_lists(const DecodeArgs &a, int *first, int *len) {
     __shared__ int warp_sum[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
@@ -113,7 +124,7 @@ __device__ __forceinline__ void tile_lists(const DecodeArgs &a, int *first, int 
         const int b = b0 + threadIdx.x;
         const int n = b < a.kv.B ? attended(a, b) : 0;
         if (b < a.kv.B) len[b] = n;
-        int x = (n + DA_SLOTS - 1) / DA_SLOTS;
+        int x = row_count(n);
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
@@ -133,18 +144,27 @@ __device__ __forceinline__ void tile_lists(const DecodeArgs &a, int *first, int 
     __syncthreads();
 }
 
-// warps that share `units` units, and the first unit of one of them
-__device__ __forceinline__ int workers_of(const DecodeArgs &a, int units) {
-    return max(1, min(a.workers, (units + DA_MIN_UNITS - 1) / DA_MIN_UNITS));
+// warps that share the list, the first place of one of them, and the one that has a place
+__device__ __forceinline__ int workers_of(const DecodeArgs &a, int count) {
+    return max(1, min(a.workers, (count + DA_MIN_TILES - 1) / DA_MIN_TILES));
 }
-__device__ __forceinline__ int first_unit(int w, int units, int workers) {
-    return (int)((long long)w * units / workers);
-}
+__device__ __forceinline__ int first_of(int w, int count, int workers) { return (int)((long long)w * count / workers); }
+__device__ __forceinline__ int worker_at(long long at, int count, int workers) { return (int)(((at + 1) * workers - 1) / count); }
 
-// A place in the list of units.
-struct UnitAt {
-    int b, hc, t, tiles;  // sequence, KV head and chunk of its query heads, tile, tiles of the sequence
-    __device__ __forceinline__ void seek(int u, const int *first, int B, int HC) {
+// Tiles [t, t_end) of one row: what a warp works on before it leaves the row.
+struct Segment {
+    int b, hc, t, t_end, tiles, n;  // sequence, KV head and chunk, the row's tiles and slots
+    int at, end;                    // list place of the row, end of the warp's stretch
+    __device__ __forceinline__ bool clip(const int *len) {
+        n = len[b];
+        tiles = (n + DA_SLOTS - 1) / DA_SLOTS;
+        t_end = min(tiles, end - at - DA_ROW_TILES);
+        return t < t_end;
+    }
+    // The first segment of the stretch [u, end); false if it has none.
+    __device__ __forceinline__ bool seek(int u, int u_end, const int *first, const int *len, int B, int HC) {
+        end = u_end;
+        if (u >= end) return false;
         int lo = 0, hi = B;  // first[lo] * HC <= u < first[hi] * HC
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
@@ -154,62 +174,58 @@ struct UnitAt {
                 hi = mid;
         }
         b = lo;
-        tiles = first[b + 1] - first[b];
-        const int r = u - first[b] * HC;
-        hc = r / tiles;
-        t = r - hc * tiles;
+        const int per = first[b + 1] - first[b];
+        hc = (u - first[b] * HC) / per;
+        at = first[b] * HC + hc * per;
+        t = max(0, u - at - DA_ROW_TILES);
+        return clip(len) || next(first, len, B, HC);
     }
-    __device__ __forceinline__ void next(const int *first, int B, int HC) {
-        if (++t < tiles) return;
+    __device__ __forceinline__ bool next(const int *first, const int *len, int B, int HC) {
+        at += first[b + 1] - first[b];
+        if (++hc == HC) {
+            hc = 0;
+            do ++b;
+            while (b < B && first[b + 1] == first[b]);
+        }
         t = 0;
-        if (++hc < HC) return;
-        hc = 0;
-        do ++b;
-        while (b < B && first[b + 1] == first[b]);
-        if (b < B) tiles = first[b + 1] - first[b];
+        return b < B && at < end && clip(len);  // (where only a row's front is left the stretch is over)
     }
 };
 
-template <bool FP16, int D, int NT>
-__global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs a) {
+// A warp's work on its segments: `next(segment)` makes the following one of it, `leave(segment, t0, m, l, o)` takes the
+// results of tiles [t0, t_end) of a row: maxima and sums (a lane's own part of them) of heads 8 nt + 2 (lane % 4) + e, and outputs
+// o[ks][nt]: dims 16 ks + lane / 4 (+ 8 in elements 2 and 3) of those heads.
+template <bool FP16, int D, int NT, typename Next, typename Leave>
+__device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int chunks, Segment at, Next &&next, Leave &&leave) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, CPR = D / 8;  // heads of a chunk, k steps, 16-byte pieces of a row
-    extern __shared__ __align__(128) uint8_t smem[];
-    const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const uint32_t ring = smem_u32(smem) + warp * S::STAGES * S::UNIT;
-    int *first = reinterpret_cast<int *>(smem + S::RING), *len = first + B + 1;
-    pdl_launch();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = DEV_OK;  // (k_decode_join latches)
-    tile_lists(a, first, len);
-    const int chunks = (a.group + HEADS - 1) / HEADS, HC = a.kv.hkv * chunks;
-    const int units = first[B] * HC, workers = workers_of(a, units);
-    const int w = warp * gridDim.x + blockIdx.x;  // neighbours in the list on different SMs
-    if (units == 0 || w >= workers) return;
-    const int u_end = first_unit(w + 1, units, workers);
-    int u = first_unit(w, units, workers);
-    UnitAt ld, at;
-    ld.seek(u, first, B, HC);
-    at = ld;
+    constexpr bool Q_AHEAD = KS * NT <= 16;                  // a row's queries are asked for a row ahead, if registers allow
+    const int lane = threadIdx.x & 31;
     const bool append = a.k_new != nullptr;
     // P's scale: weights of fp16 lie in 2^-24 .. 2^14, so that what is far below the maximum keeps its bits
     const float shift = FP16 ? 14.f : 0.f, c = a.scale * 1.4426950408889634f;
+    Segment ld = at;
+    bool loading = true;
 
-    // page of slot lane % 16 of the unit at ld; -1: none
+    // page of slot lane % 16 of the tile at ld; -1: none
     auto page_of = [&]() {
         const int slot = ld.t * DA_SLOTS + (lane & 15);
-        if (slot >= len[ld.b]) return -1;
+        if (slot >= ld.n) return -1;
         const int p = a.kv.table[(long long)ld.b * a.kv.max_pages + slot / a.kv.page_size];
         return (unsigned)p < (unsigned)a.kv.n_pages ? p : -1;
     };
-    // Copies the unit at ld into a stage: lanes 0-15 know K's rows, 16-31 V's.  Rows that are none arrive as zeros.
-    auto issue = [&](int page, int stage) {
-        const int slot = ld.t * DA_SLOTS + (lane & 15), h = ld.hc / chunks, n = len[ld.b];
-        const bool is_new = append && slot == n - 1;
+    auto step = [&]() {
+        if (++ld.t == ld.t_end) loading = next(ld);
+    };
+    // Copies the tile at `g` into a stage: lanes 0-15 know K's rows, 16-31 V's.  Rows that are none arrive as zeros.
+    auto issue = [&](const Segment &g, int page, int stage) {
+        const int slot = g.t * DA_SLOTS + (lane & 15), h = g.hc / chunks;
+        const bool is_new = append && slot == g.n - 1;
         const long long off = (long long)page * a.kv.stride_page + h * a.kv.stride_head +
                               (long long)(slot % a.kv.page_size) * a.kv.stride_slot;
         const uint16_t *row = nullptr;
         if (is_new)
-            row = (lane < 16 ? a.k_new : a.v_new) + ld.b * a.new_stride + (long long)h * D;
+            row = (lane < 16 ? a.k_new : a.v_new) + g.b * a.new_stride + (long long)h * D;
         else if (page >= 0)
             row = (lane < 16 ? a.kv.k : a.kv.v) + off;
         const uint32_t st = ring + stage * S::UNIT;
@@ -224,13 +240,13 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
             cp_async16_or_zero(dst, ks ? ks + cc * 8 : a.kv.k, ks != nullptr);
             cp_async16_or_zero(dst + DA_SLOTS * D * 2, vs ? vs + cc * 8 : a.kv.v, vs != nullptr);
         }
-        if (append && ld.t == ld.tiles - 1 && ld.hc % chunks == 0) {
+        if (append && g.t == g.tiles - 1 && g.hc % chunks == 0) {
             // the new token's row joins the cache; nobody reads it there in this call
-            const int r = (n - 1) & 15;
+            const int r = (g.n - 1) & 15;
             const long long o = __shfl_sync(0xffffffffu, off, r);
             const bool ok = __shfl_sync(0xffffffffu, page, r) >= 0;
             if (ok) {
-                const long long src = ld.b * a.new_stride + (long long)h * D;
+                const long long src = g.b * a.new_stride + (long long)h * D;
                 for (int i = lane; i < CPR; i += 32) {
                     *reinterpret_cast<int4 *>(const_cast<uint16_t *>(a.kv.k) + o + i * 8) =
                         *reinterpret_cast<const int4 *>(a.k_new + src + i * 8);
@@ -239,59 +255,88 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
                 }
             }
             if (lane == 0 && a.new_pos && a.kv.positions)
-                a.kv.positions[((long long)ld.b * a.kv.hkv + h) * a.kv.cap + n - 1] = a.new_pos[ld.b];
+                a.kv.positions[((long long)g.b * a.kv.hkv + h) * a.kv.cap + g.n - 1] = a.new_pos[g.b];
         }
     };
-
-    int to_load = u_end - u, page = page_of(), stage_in = 0;
-    auto load_next = [&]() {
-        if (to_load > 0) {
-            issue(page, stage_in);
-            stage_in = stage_in + 1 == S::STAGES ? 0 : stage_in + 1;
-            if (--to_load > 0) {
-                ld.next(first, B, HC);
-                page = page_of();  // one unit ahead: its latency is not waited for here
+    // a row's queries as B operands: head 8 nt + lane / 4, dims 16 ks + 2 (lane % 4) and the next, and 8 further on
+    uint32_t qn[Q_AHEAD ? KS : 1][NT][2], qf[KS][NT][2];
+    auto load_q = [&](const Segment &g, auto &q_to) {
+        const int h = g.hc / chunks, ch = g.hc - h * chunks;
+        const uint16_t *q = a.q + g.b * a.q_stride + (long long)(h * a.group + ch * HEADS) * D;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int j = nt * 8 + (lane >> 2);
+            const bool real = ch * HEADS + j < a.group;
+            const uint32_t *src = reinterpret_cast<const uint32_t *>(q + j * D + (lane & 3) * 2);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                q_to[ks][nt][0] = real ? src[ks * 8] : 0u;
+                q_to[ks][nt][1] = real ? src[ks * 8 + 4] : 0u;
             }
         }
-        cp_async_commit();
     };
-#pragma unroll
-    for (int s = 0; s < S::STAGES - 1; ++s) load_next();
 
-    uint32_t qf[KS][NT][2];
+    // The first tiles' pages are looked up before any tile is asked for: one latency, not one for each.
+    {
+        Segment early[S::STAGES - 1];
+        int pages[S::STAGES - 1];
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; ++s) {
+            early[s] = ld;
+            pages[s] = -2;
+            if (loading) {
+                pages[s] = page_of();
+                step();
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < S::STAGES - 1; ++s) {
+            if (__any_sync(0xffffffffu, pages[s] != -2)) issue(early[s], pages[s], s);
+            cp_async_commit();
+        }
+    }
+    int page = loading ? page_of() : -1, stage_in = S::STAGES - 1, stage = 0;
+    if constexpr (Q_AHEAD) load_q(at, qn);
+
     float o[KS][NT][4], m[NT][2], l[NT][2];
-    int stage = 0;
     bool fresh = true;
-    int t_first = 0;
+    int t0 = 0;
     // lane constants of the fragments' addresses
     const int k_row = (lane & 7) + ((lane >> 3) & 1) * 8, k_c = lane >> 4;
     const int v_row = (lane & 7) + (lane >> 4) * 8, v_c = (lane >> 3) & 1;
-    for (; u < u_end; ++u) {
-        const int n = len[at.b];
+    for (bool going = true; going;) {
         if (fresh) {
             fresh = false;
-            t_first = at.t;
-            const int h = at.hc / chunks, ch = at.hc - h * chunks;
-            const uint16_t *q = a.q + at.b * a.q_stride + (long long)(h * a.group + ch * HEADS) * D;
+            t0 = at.t;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const int j = nt * 8 + (lane >> 2);
-                const bool real = ch * HEADS + j < a.group;
-                const uint32_t *src = reinterpret_cast<const uint32_t *>(q + j * D + (lane & 3) * 2);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    qf[ks][nt][0] = real ? src[ks * 8] : 0u;
-                    qf[ks][nt][1] = real ? src[ks * 8 + 4] : 0u;
-                }
                 m[nt][0] = m[nt][1] = -INFINITY;
                 l[nt][0] = l[nt][1] = 0.f;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) o[ks][nt][0] = o[ks][nt][1] = o[ks][nt][2] = o[ks][nt][3] = 0.f;
+                for (int ks = 0; ks < KS; ++ks) {
+                    o[ks][nt][0] = o[ks][nt][1] = o[ks][nt][2] = o[ks][nt][3] = 0.f;
+                }
+            }
+            if constexpr (Q_AHEAD) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) qf[ks][nt][0] = qn[ks][nt][0], qf[ks][nt][1] = qn[ks][nt][1];
+                Segment after = at;
+                if (next(after)) load_q(after, qn);
+            } else {
+                load_q(at, qf);
             }
         }
         cp_async_wait<S::STAGES - 2>();
         __syncwarp();  // everybody's copies are there, and everybody is done with the stage that is filled next
-        load_next();
+        if (loading) {
+            issue(ld, page, stage_in);
+            stage_in = stage_in + 1 == S::STAGES ? 0 : stage_in + 1;
+            step();
+            if (loading) page = page_of();  // one tile ahead: its latency is not waited for here
+        }
+        cp_async_commit();
         const uint32_t kst = ring + stage * S::UNIT, vst = kst + DA_SLOTS * D * 2;
         stage = stage + 1 == S::STAGES ? 0 : stage + 1;
 
@@ -307,10 +352,10 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
         }
         // s[nt]: slots lane / 4 and lane / 4 + 8, heads 2 (lane % 4) and the next
         const int slot = at.t * DA_SLOTS + (lane >> 2);
-        if (slot >= n)
+        if (slot >= at.n)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = -INFINITY;
-        if (slot + 8 >= n)
+        if (slot + 8 >= at.n)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt][2] = s[nt][3] = -INFINITY;
         if (a.scores) {
@@ -386,26 +431,60 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
                 mma_16816<FP16>(o[ks][nt], f, pl[nt][0], pl[nt][1]);
             }
         }
-
-        if (at.t == at.tiles - 1 || u == u_end - 1) {
+        if (++at.t == at.t_end) {
             fresh = true;
-            const int h = at.hc / chunks, ch = at.hc - h * chunks;
-            const bool whole = t_first == 0 && at.t == at.tiles - 1;
-            const long long part = (long long)w * 2 + (t_first == 0 ? 1 : 0);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float sum = l[nt][e];
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 4);
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+                    l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 4);
+                    l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 8);
+                    l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], 16);
+                }
+            leave(at, t0, m, l, o);
+            going = next(at);
+        }
+    }
+}
+
+// 1 / sum; 0 for a row without anything, NaN for NaN
+__device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }
+// ln of the sum, whose terms carry the factor of P's scale
+template <bool FP16>
+__device__ __forceinline__ float log_sum(float sum) { return logf(FP16 ? sum * 0x1p-14f : sum); }
+
+// The list, a stretch a warp.
+template <bool FP16, int D, int NT>
+__global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs a) {
+    using S = DaShape<D>;
+    constexpr int HEADS = 8 * NT, KS = D / 16;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int *first = reinterpret_cast<int *>(smem + S::RING), *len = first + B + 1;
+    pdl_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = DEV_OK;  // (k_decode_join latches)
+    tile_lists(a, first, len);
+    const int chunks = (a.group + HEADS - 1) / HEADS, HC = a.kv.hkv * chunks;
+    const int count = first[B] * HC, workers = workers_of(a, count);
+    const int w = warp * gridDim.x + blockIdx.x;  // neighbours in the list on different SMs
+    if (count == 0 || w >= workers) return;
+    Segment at;
+    if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, HC)) return;
+    attend<FP16, D, NT>(
+        a, smem_u32(smem) + warp * S::STAGES * S::UNIT, chunks, at, [&](Segment &g) { return g.next(first, len, B, HC); },
+        [&](const Segment &g, int t0, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
+            const int h = g.hc / chunks, ch = g.hc - h * chunks, d0 = lane >> 2;
+            const bool whole = t0 == 0 && g.t_end == g.tiles;
+            const long long part = (long long)w * 2 + (t0 == 0 ? 1 : 0);  // (a stretch has one row begun before it, and one that goes on)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
                     const int j = nt * 8 + (lane & 3) * 2 + e;
                     if (ch * HEADS + j >= a.group) continue;
-                    const int d0 = lane >> 2;
                     if (whole) {
-                        const long long row = (long long)at.b * a.hq + h * a.group + ch * HEADS + j;
-                        const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+                        const long long row = (long long)g.b * a.hq + h * a.group + ch * HEADS + j;
+                        const float inv = inverse(l[nt][e]);
                         uint16_t *dst = a.out + row * D + d0;
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
@@ -414,185 +493,438 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
                         }
                         if (d0 == 0) {
                             a.row_ml[row] = make_float2(m[nt][e], inv);
-                            if (a.lse) a.lse[row] = m[nt][e] * a.scale + logf(FP16 ? sum * 0x1p-14f : sum);
+                            if (a.lse) a.lse[row] = m[nt][e] * a.scale + log_sum<FP16>(l[nt][e]);
                         }
                     } else {
+                        if (d0 == 0) a.part_ml[part * HEADS + j] = make_float2(m[nt][e], l[nt][e]);
                         float *dst = a.part_o + (part * HEADS + j) * D + d0;
 #pragma unroll
                         for (int ks = 0; ks < KS; ++ks) {
                             dst[ks * 16] = o[ks][nt][e];
                             dst[ks * 16 + 8] = o[ks][nt][2 + e];
                         }
-                        if (d0 == 0) a.part_ml[part * HEADS + j] = make_float2(m[nt][e], sum);
                     }
                 }
-        }
-        at.next(first, B, HC);
+        });
+}
+
+// Lengths and pages outside their ranges: a code, or DEV_OK, in one thread or another.
+__device__ __forceinline__ int check_sequence(const DecodeArgs &a, int b, int tid, int threads) {
+    const int raw = a.kv.lens[b], n = attended(a, b);
+    if (n != raw + (a.k_new ? 1 : 0)) return DEV_BAD_POSITION;
+    const int pages = (n + a.kv.page_size - 1) / a.kv.page_size;
+    for (int i = tid; i < pages; i += threads)
+        if ((unsigned)a.kv.table[(long long)b * a.kv.max_pages + i] >= (unsigned)a.kv.n_pages) return DEV_BAD_PAGE;
+    return DEV_OK;
+}
+
+// Small calls: a cluster of C CTAs a (sequence, KV head).  Its warps take the row's tiles in equal parts; each CTA joins its
+// four warps' results in shared memory, then each takes a share of the outputs from all CTAs' results, and adds the
+// weights of its own slots.
+template <bool FP16, int D, int NT>
+__global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeArgs a, int C) {
+    using S = DaShape<D>;
+    constexpr int HEADS = 8 * NT, KS = D / 16, PITCH = D + 4, THREADS = DA_WARPS * 32, D4 = D / 4;
+    static_assert((HEADS * PITCH + HEADS * D) * 4 <= S::STAGES * S::UNIT, "a warp's and a CTA's results lie in a ring");
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float2 warp_ml[DA_WARPS][HEADS], every[DA_CLUSTER][HEADS], row_ml[HEADS];
+    __shared__ __align__(8) float2 cta_ml[HEADS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = blockIdx.x % C, row = blockIdx.x / C;
+    if (row == a.kv.B * a.kv.hkv) {  // one cluster more: the call's status word has one writer
+        if (rank != 0) return;
+        int code = DEV_OK;
+        for (int b = 0; b < a.kv.B; ++b) code = max(code, check_sequence(a, b, tid, THREADS));
+        const int page = __syncthreads_or(code == DEV_BAD_PAGE), length = __syncthreads_or(code == DEV_BAD_POSITION);
+        if (tid == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
+        return;
     }
+    const int b = row / a.kv.hkv, h = row - b * a.kv.hkv, n = attended(a, b), G = a.group;
+    const float c = a.scale * 1.4426950408889634f, shift = FP16 ? 14.f : 0.f;
+    uint8_t *ring = smem + warp * S::STAGES * S::UNIT;
+    float *mine = reinterpret_cast<float *>(ring), *cta_o = reinterpret_cast<float *>(smem) + HEADS * PITCH;
+    Segment at;
+    at.b = b;
+    at.hc = h;
+    at.n = n;
+    at.tiles = (n + DA_SLOTS - 1) / DA_SLOTS;
+    const int w = rank * DA_WARPS + warp, W = C * DA_WARPS;
+    at.t = first_of(w, at.tiles, W);
+    at.t_end = first_of(w + 1, at.tiles, W);
+    const int slot0 = at.t * DA_SLOTS, slot1 = min(n, at.t_end * DA_SLOTS);
+    if (at.t < at.t_end) {
+        attend<FP16, D, NT>(
+            a, smem_u32(ring), 1, at, [&](Segment &) { return false; },
+            [&](const Segment &, int, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
+                cp_async_wait_all();
+                __syncwarp();  // (the ring is free)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int j = nt * 8 + (lane & 3) * 2 + e, d0 = lane >> 2;
+                        if (d0 == 0) warp_ml[warp][j] = make_float2(m[nt][e], l[nt][e]);
+#pragma unroll
+                        for (int ks = 0; ks < KS; ++ks) {
+                            mine[j * PITCH + ks * 16 + d0] = o[ks][nt][e];
+                            mine[j * PITCH + ks * 16 + d0 + 8] = o[ks][nt][2 + e];
+                        }
+                    }
+            });
+    } else if (lane < HEADS) {
+        warp_ml[warp][lane] = make_float2(-INFINITY, 0.f);
+    }
+    __syncthreads();
+    auto add = [](float4 &acc, float f, const float4 &x) {
+        acc.x += f * x.x;
+        acc.y += f * x.y;
+        acc.z += f * x.z;
+        acc.w += f * x.w;
+    };
+    // (a part whose sum is 0 has no outputs, or was never written)
+    for (int p = tid; p < G * D4; p += THREADS) {
+        const int j = p / D4, d4 = p % D4;
+        float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < DA_WARPS; ++i) mx = fmaxf(mx, warp_ml[i][j].x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float mu = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int i = 0; i < DA_WARPS; ++i) {
+            const float2 x = warp_ml[i][j];
+            if (x.y == 0.f) continue;
+            const float f = ex2((x.x - mu) * c);
+            sum += f * x.y;
+            add(acc, f, *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + i * S::STAGES * S::UNIT) + j * PITCH + d4 * 4));
+        }
+        *reinterpret_cast<float4 *>(cta_o + j * D + d4 * 4) = acc;
+        if (d4 == 0) cta_ml[j] = make_float2(mx, sum);
+    }
+    cluster_sync();
+    for (int i = tid; i < C * G; i += THREADS) {
+        const float2 x = ld_cluster_v2(map_cta(smem_u32(&cta_ml[i % G]), i / G));
+        every[i / G][i % G] = x;
+    }
+    __syncthreads();
+    if (tid < G) {
+        float mx = -INFINITY, sum = 0.f;
+        for (int i = 0; i < C; ++i) mx = fmaxf(mx, every[i][tid].x);
+        const float mu = mx == -INFINITY ? 0.f : mx;
+        for (int i = 0; i < C; ++i) {
+            const float f = every[i][tid].y == 0.f ? 0.f : ex2((every[i][tid].x - mu) * c);
+            sum += f * every[i][tid].y;
+            every[i][tid].x = f;
+        }
+        row_ml[tid] = make_float2(mu, inverse(sum));
+        if (rank == 0 && a.lse) a.lse[(long long)b * a.hq + h * G + tid] = mx * a.scale + log_sum<FP16>(sum);
+    }
+    __syncthreads();
+    for (int p = tid * C + rank; p < G * D4; p += THREADS * C) {
+        const int j = p / D4, d4 = p % D4;
+        const uint32_t from = smem_u32(cta_o + j * D + d4 * 4);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i0 = 0; i0 < C; i0 += 8) {
+            float4 x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < C) x[i] = ld_cluster_v4(map_cta(from, i0 + i));
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i0 + i < C) add(acc, every[i0 + i][j].x, x[i]);
+        }
+        const float inv = row_ml[j].y;
+        uint2 r;
+        r.x = pack2<FP16>(acc.x * inv, acc.y * inv);
+        r.y = pack2<FP16>(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2 *>(a.out + ((long long)b * a.hq + h * G + j) * D + d4 * 4) = r;
+    }
+    cluster_arrive();  // (this CTA reads no other's shared memory any more)
+    if (a.accumulate) {
+        float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
+        const float *sc = a.scores + ((long long)b * a.hq + h * G) * a.score_pitch;
+        const int fresh = a.k_new ? n - 1 : -1;
+        for (int slot = slot0 + lane; slot < slot1; slot += 32) {
+            float sum = slot == fresh ? 0.f : wt[slot];
+#pragma unroll 8
+            for (int j = 0; j < G; ++j) sum += ex2((sc[j * a.score_pitch + slot] - row_ml[j].x) * c + shift) * row_ml[j].y;
+            wt[slot] = sum;
+        }
+    }
+    cluster_wait();
 }
 
 constexpr int DJ_THREADS = 256;
+constexpr int DJ_SLOTS = 4;  // of a thread that adds weights
 
-// Joins what several warps left of one (sequence, query head): out = sum_w f_w o_w / sum_w f_w l_w, f_w = exp(scale (m_w - max)).
-// Sequences without a slot get zeros.  Also where the table's pages and the lengths are looked at.
-template <bool FP16, int D, int NT>
-__global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a) {
-    constexpr int HEADS = 8 * NT, L4 = D / 4, G = DJ_THREADS / L4;
+// Joins what several warps left of a row: out = sum_w f_w o_w / sum_w f_w l_w, f_w = exp(scale (m_w - max)).  TEAM threads a
+// query head: the CTA where many warps share a row, a warp where rows are many.  Sequences without a slot get
+// zeros.  The CTAs behind `join_ctas` add the weights, each taking maximum and sum of its heads from the warps' again.
+template <bool FP16, int D, int NT, int TEAM>
+__global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, int join_ctas, int weight_blocks) {
+    constexpr int HEADS = 8 * NT, TEAMS = DJ_THREADS / TEAM, L = D / 4 < TEAM ? D / 4 : TEAM, V = D / 4 / L, G = TEAM / L;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float red[2][DJ_THREADS / 32];
-    __shared__ float4 sum_o[DJ_THREADS];
+    __shared__ float4 sum_o[TEAM > 32 ? DJ_THREADS : 1];
     const int B = a.kv.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int *first = reinterpret_cast<int *>(smem), *len = first + B + 1;
-    float *fac = reinterpret_cast<float *>(len + B);
-    pdl_launch();
+    float *fac = reinterpret_cast<float *>(smem + (8 * B + 4 + 7) / 8 * 8);  // [TEAMS][workers], or maxima and inverse sums of a group
     tile_lists(a, first, len);
-    pdl_wait();
     const int chunks = (a.group + HEADS - 1) / HEADS, HC = a.kv.hkv * chunks;
-    const int units = first[B] * HC, workers = workers_of(a, units);
+    const int count = first[B] * HC, workers = workers_of(a, count);
     const float c = a.scale * 1.4426950408889634f;
-    for (int b = blockIdx.x; b < B; b += gridDim.x) {
-        const int add = a.k_new ? 1 : 0, raw = a.kv.lens[b];
-        if (tid == 0 && (raw < 0 || raw > a.kv.cap - add)) latch_error(a.status, DEV_BAD_POSITION);
-        const int pages = (len[b] + a.kv.page_size - 1) / a.kv.page_size;
-        bool bad = false;
-        for (int i = tid; i < pages; i += DJ_THREADS)
-            bad |= (unsigned)a.kv.table[(long long)b * a.kv.max_pages + i] >= (unsigned)a.kv.n_pages;
-        if (bad) latch_error(a.status, DEV_BAD_PAGE);
+    // the warps that share a row, and where one of them left it
+    auto span = [&](int b, int h, int ch, int *w0) {
+        const int per = first[b + 1] - first[b], tiles = per - DA_ROW_TILES;
+        const long long at = (long long)first[b] * HC + (long long)(h * chunks + ch) * per + DA_ROW_TILES;
+        *w0 = worker_at(at, count, workers);
+        return worker_at(at + tiles - 1, count, workers) - *w0 + 1;
+    };
+    auto part_at = [&](int w0, int i, int j) { return ((long long)(w0 + i) * 2 + (i == 0)) * HEADS + j; };
+
+    if ((int)blockIdx.x >= join_ctas) {
+        // weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0
+        const int item = blockIdx.x - join_ctas, row = item / weight_blocks, block = item - row * weight_blocks;
+        const int h = row % a.kv.hkv, b = row / a.kv.hkv, n = len[b], fresh = a.k_new ? n - 1 : -1;
+        constexpr int STEP = DJ_THREADS * DJ_SLOTS;
+        if (block * STEP >= n) return;
+        float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
+        float have[DJ_SLOTS];
+        auto load_weights = [&](int s0) {
+#pragma unroll
+            for (int i = 0; i < DJ_SLOTS; ++i) {
+                const int slot = s0 + i * DJ_THREADS + tid;
+                have[i] = slot < n && slot != fresh ? wt[slot] : 0.f;
+            }
+        };
+        load_weights(block * STEP);  // (no kernel of this call has written them)
+        float2 *ml = reinterpret_cast<float2 *>(fac);
+        pdl_wait();
+        for (int g = warp; g < a.group; g += DJ_THREADS / 32) {  // a warp a head
+            const int ch = g / HEADS, j = g - ch * HEADS;
+            int w0;
+            const int nw = span(b, h, ch, &w0);
+            if (nw == 1) {
+                if (lane == 0) {
+                    const float2 x = a.row_ml[(long long)b * a.hq + h * a.group + g];
+                    ml[g] = make_float2(x.x == -INFINITY ? 0.f : x.x, x.y);
+                }
+                continue;
+            }
+            float m = -INFINITY, l = 0.f;
+            for (int i = lane; i < nw; i += 32) {
+                const float2 x = a.part_ml[part_at(w0, i, j)];
+                const float mx = fmaxf(m, x.x), mu = mx == -INFINITY ? 0.f : mx;
+                l = l * ex2((m - mu) * c) + x.y * ex2((x.x - mu) * c);
+                m = mx;
+            }
+            float mx = m;
+            for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+            l *= ex2((m - (mx == -INFINITY ? 0.f : mx)) * c);
+            for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+            if (lane == 0) ml[g] = make_float2(mx == -INFINITY ? 0.f : mx, inverse(l));
+        }
+        __syncthreads();
+        const float shift = FP16 ? 14.f : 0.f;
+        const float *sc = a.scores + ((long long)b * a.hq + h * a.group) * a.score_pitch;
+        for (int s0 = block * STEP; s0 < n; s0 += weight_blocks * STEP) {
+            if (s0 != block * STEP) load_weights(s0);
+            float sum[DJ_SLOTS] = {};
+#pragma unroll 2
+            for (int g = 0; g < a.group; ++g) {
+                const float2 x = ml[g];
+#pragma unroll
+                for (int i = 0; i < DJ_SLOTS; ++i) {
+                    const int slot = s0 + i * DJ_THREADS + tid;
+                    if (slot < n) sum[i] += ex2((sc[g * a.score_pitch + slot] - x.x) * c + shift) * x.y;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < DJ_SLOTS; ++i) {
+                const int slot = s0 + i * DJ_THREADS + tid;
+                if (slot < n) wt[slot] = have[i] + sum[i];
+            }
+        }
+        return;
     }
-    for (int row = blockIdx.x; row < B * a.hq; row += gridDim.x) {
+
+    pdl_wait();
+    for (int b = blockIdx.x; b < B; b += join_ctas) {
+        const int code = check_sequence(a, b, tid, DJ_THREADS);
+        if (code != DEV_OK) latch_error(a.status, code);
+    }
+    const int rows = B * a.hq, team = tid / TEAM, me = tid % TEAM;
+    float *f_team = fac + team * a.workers;
+    auto team_sync = [&]() {
+        if (TEAM > 32)
+            __syncthreads();
+        else
+            __syncwarp();
+    };
+    for (int row = blockIdx.x * TEAMS + team; row < rows; row += join_ctas * TEAMS) {
         const int b = row / a.hq, hq = row - b * a.hq, h = hq / a.group, g = hq - h * a.group;
-        const int ch = g / HEADS, j = g - ch * HEADS, tiles = first[b + 1] - first[b];
-        if (tiles == 0) {
-            for (int d = tid; d < D; d += DJ_THREADS) a.out[(long long)row * D + d] = 0;
-            if (tid == 0 && a.lse) a.lse[row] = -INFINITY;
+        const int ch = g / HEADS, j = g - ch * HEADS;
+        if (len[b] == 0) {
+            for (int d = me; d < D; d += TEAM) a.out[(long long)row * D + d] = 0;
+            if (me == 0 && a.lse) a.lse[row] = -INFINITY;
             continue;
         }
-        const long long u0 = (long long)first[b] * HC + (long long)(h * chunks + ch) * tiles, u1 = u0 + tiles;
-        // the worker that holds unit u is the last whose first unit is not behind it
-        const int w0 = (int)(((u0 + 1) * workers - 1) / units), w1 = (int)((u1 * workers - 1) / units);
-        if (w0 == w1) continue;  // one warp did it all
-        const int nw = w1 - w0 + 1;
+        int w0;
+        const int nw = span(b, h, ch, &w0);
+        if (nw == 1) continue;  // one warp did it all
         float mx = -INFINITY;
-        for (int i = tid; i < nw; i += DJ_THREADS) {
-            const long long part = ((long long)(w0 + i) * 2 + (i == 0)) * HEADS + j;
-            mx = fmaxf(mx, a.part_ml[part].x);
-        }
+        for (int i = me; i < nw; i += TEAM) mx = fmaxf(mx, a.part_ml[part_at(w0, i, j)].x);
         for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-        __syncthreads();  // (red, fac and sum_o of the row before have been read)
-        if (lane == 0) red[0][warp] = mx;
-        __syncthreads();
-        mx = red[0][0];
-        for (int i = 1; i < DJ_THREADS / 32; ++i) mx = fmaxf(mx, red[0][i]);
+        team_sync();  // (what the row before left in shared memory has been read)
+        if (TEAM > 32) {
+            if (lane == 0) red[0][warp] = mx;
+            __syncthreads();
+            for (int i = 0; i < DJ_THREADS / 32; ++i) mx = fmaxf(mx, red[0][i]);
+        }
         const float mu = mx == -INFINITY ? 0.f : mx;
         float sum = 0.f;
-        for (int i = tid; i < nw; i += DJ_THREADS) {
-            const long long part = ((long long)(w0 + i) * 2 + (i == 0)) * HEADS + j;
-            const float2 ml = a.part_ml[part];
+        for (int i = me; i < nw; i += TEAM) {
+            const float2 ml = a.part_ml[part_at(w0, i, j)];
             const float f = ex2((ml.x - mu) * c);
-            fac[i] = f;
+            f_team[i] = f;
             sum += f * ml.y;
         }
         for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-        if (lane == 0) red[1][warp] = sum;
-        __syncthreads();
-        sum = 0.f;
-        for (int i = 0; i < DJ_THREADS / 32; ++i) sum += red[1][i];
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int d4 = tid % L4, grp = tid / L4;
-#pragma unroll 4
-        for (int i = grp; i < nw; i += G) {
-            const long long part = ((long long)(w0 + i) * 2 + (i == 0)) * HEADS + j;
-            const float4 x = *reinterpret_cast<const float4 *>(a.part_o + part * D + d4 * 4);
-            const float f = fac[i];
-            acc.x += f * x.x;
-            acc.y += f * x.y;
-            acc.z += f * x.z;
-            acc.w += f * x.w;
+        if (TEAM > 32 && lane == 0) red[1][warp] = sum;
+        team_sync();
+        if (TEAM > 32) {
+            sum = 0.f;
+            for (int i = 0; i < DJ_THREADS / 32; ++i) sum += red[1][i];
         }
-        sum_o[tid] = acc;
-        __syncthreads();
-        const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
-        if (tid < L4) {
-            for (int i = 1; i < G; ++i) {
-                const float4 x = sum_o[i * L4 + tid];
-                acc.x += x.x;
-                acc.y += x.y;
-                acc.z += x.z;
-                acc.w += x.w;
+        float4 acc[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int d4 = me % L, grp = me / L;
+        constexpr int U = V == 1 ? 8 : 4;
+        for (int i0 = grp; i0 < nw; i0 += G * U) {
+            float4 x[U][V];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * G < nw)
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        x[u][v] = *reinterpret_cast<const float4 *>(a.part_o + part_at(w0, i0 + u * G, j) * D + (v * L + d4) * 4);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * G < nw) {
+                    const float f = f_team[i0 + u * G];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        acc[v].x += f * x[u][v].x;
+                        acc[v].y += f * x[u][v].y;
+                        acc[v].z += f * x[u][v].z;
+                        acc[v].w += f * x[u][v].w;
+                    }
+                }
+        }
+        if (TEAM > 32) {
+            sum_o[tid] = acc[0];  // (V is 1)
+            __syncthreads();
+            if (grp == 0)
+                for (int i = 1; i < G; ++i) {
+                    const float4 x = sum_o[i * L + d4];
+                    acc[0].x += x.x;
+                    acc[0].y += x.y;
+                    acc[0].z += x.z;
+                    acc[0].w += x.w;
+                }
+        } else {
+            for (int s = L; s < TEAM; s <<= 1) {
+                acc[0].x += __shfl_xor_sync(0xffffffffu, acc[0].x, s);
+                acc[0].y += __shfl_xor_sync(0xffffffffu, acc[0].y, s);
+                acc[0].z += __shfl_xor_sync(0xffffffffu, acc[0].z, s);
+                acc[0].w += __shfl_xor_sync(0xffffffffu, acc[0].w, s);
             }
-            uint2 r;
-            r.x = pack2<FP16>(acc.x * inv, acc.y * inv);
-            r.y = pack2<FP16>(acc.z * inv, acc.w * inv);
-            *reinterpret_cast<uint2 *>(a.out + (long long)row * D + tid * 4) = r;
         }
-        if (tid == 0) {
-            a.row_ml[row] = make_float2(mx, inv);
-            if (a.lse) a.lse[row] = mx * a.scale + logf(FP16 ? sum * 0x1p-14f : sum);
-        }
+        const float inv = inverse(sum);
+        if (grp == 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                uint2 r;
+                r.x = pack2<FP16>(acc[v].x * inv, acc[v].y * inv);
+                r.y = pack2<FP16>(acc[v].z * inv, acc[v].w * inv);
+                *reinterpret_cast<uint2 *>(a.out + (long long)row * D + (v * L + d4) * 4) = r;
+            }
+        if (me == 0 && a.lse) a.lse[row] = mx * a.scale + log_sum<FP16>(sum);
     }
 }
 
-constexpr int DW_THREADS = 256;
-
-// weights[b][h][slot] += the weights that the heads of h's group give the slot; the new token's slot starts at 0.
-template <bool FP16>
-__global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs a) {
-    extern __shared__ __align__(128) uint8_t smem[];
-    float2 *ml = reinterpret_cast<float2 *>(smem);
-    const int h = blockIdx.x % a.kv.hkv, b = blockIdx.x / a.kv.hkv;
-    const float c = a.scale * 1.4426950408889634f, shift = FP16 ? 14.f : 0.f;
-    pdl_wait();
-    const int n = attended(a, b);
-    const long long row = (long long)b * a.hq + h * a.group;
-    for (int i = threadIdx.x; i < a.group; i += DW_THREADS) ml[i] = a.row_ml[row + i];
-    __syncthreads();
-    float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
-    const int fresh = a.k_new ? n - 1 : -1;
-    for (int slot = blockIdx.y * DW_THREADS + threadIdx.x; slot < n; slot += gridDim.y * DW_THREADS) {
-        const float *s = a.scores + row * a.score_pitch + slot;
-        float sum = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < a.group; ++i) {
-            const float mu = ml[i].x == -INFINITY ? 0.f : ml[i].x;
-            sum += ex2((s[i * a.score_pitch] - mu) * c + shift) * ml[i].y;
-        }
-        wt[slot] = slot == fresh ? sum : wt[slot] + sum;
+// Kernel attributes, set for the current device before any launch there; *done is the device they were last set for.
+template <typename K>
+cudaError_t configure(K *kernel, size_t smem, int *done, int *most_cluster = nullptr) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || *done == dev) return e;
+    const void *f = reinterpret_cast<const void *>(kernel);
+    e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess && most_cluster) {
+        e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) *most_cluster = largest_cluster(f, DA_WARPS * 32, smem, DA_CLUSTER) < DA_CLUSTER ? 8 : DA_CLUSTER;
     }
+    if (e == cudaSuccess) *done = dev;
+    return e;
+}
+
+template <bool FP16, int D, int NT, int TEAM>
+cudaError_t launch_join(DecodeArgs &a, cudaStream_t st) {
+    static thread_local int done = -1;
+    const size_t lists = (2 * (size_t)a.kv.B + 1) * 4, most = (2 * KV_MAX_BATCH + 3) * 4 + std::max((DJ_THREADS / TEAM) * KV_MAX_WORKERS * 4, 4096 * 8);
+    const size_t facs = std::max((size_t)(DJ_THREADS / TEAM) * a.workers * 4, (size_t)a.group * 8);
+    cudaError_t e = configure(k_decode_join<FP16, D, NT, TEAM>, most, &done);
+    if (e != cudaSuccess) return e;
+    const int teams = DJ_THREADS / TEAM, rows = a.kv.B * a.hq, pairs = a.kv.B * a.kv.hkv;
+    const int join = std::min((rows + teams - 1) / teams, gemm_ctas() * 4);
+    const long long blocks = (a.kv.cap + DJ_THREADS * DJ_SLOTS - 1) / (DJ_THREADS * DJ_SLOTS);
+    const int wb = a.accumulate ? (int)std::max(1ll, std::min(blocks, (long long)(gemm_ctas() * 8 + pairs - 1) / pairs)) : 0;
+    return launch_pdl(k_decode_join<FP16, D, NT, TEAM>, join + wb * pairs, DJ_THREADS, (lists + 7) / 8 * 8 + facs, st, a, join, wb);
+}
+
+// CTAs of a (sequence, KV head)'s cluster, or 0 where the list of tiles is the better way: clusters where all of them run at
+// once and no warp has more than DA_CLUSTER_TILES tiles.
+int pick_cluster(const DecodeArgs &a, int ctas, int most) {
+    const long long rows = (long long)a.kv.B * a.kv.hkv, tiles = (a.kv.cap + DA_SLOTS - 1) / DA_SLOTS;
+    if (a.group > 16 || rows > ctas) return 0;
+    int C = 1;
+    while (C < most && rows * C * 2 <= ctas && C * DA_WARPS < tiles) C *= 2;
+    return tiles <= (long long)C * DA_WARPS * DA_CLUSTER_TILES ? C : 0;
 }
 
 template <bool FP16, int D, int NT>
 cudaError_t launch(DecodeArgs &a, cudaStream_t st) {
     using S = DaShape<D>;
-    const size_t lists = (2 * (size_t)a.kv.B + 1) * 4, smem = S::RING + lists;
-    static thread_local int configured = -1;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && configured != dev) {
-        e = cudaFuncSetAttribute(k_decode_split<FP16, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 S::RING + (2 * KV_MAX_BATCH + 1) * 4);
-        if (e == cudaSuccess) configured = dev;
+    static thread_local int done_c = -1, most = 8;
+    cudaError_t e = configure(k_decode_cluster<FP16, D, NT>, S::RING, &done_c, &most);
+    if (e != cudaSuccess) return e;
+    if (const int C = pick_cluster(a, gemm_ctas() * S::CTAS, most)) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)((a.kv.B * a.kv.hkv + 1) * C));
+        cfg.blockDim = dim3(DA_WARPS * 32);
+        cfg.dynamicSmemBytes = S::RING;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)C;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, k_decode_cluster<FP16, D, NT>, static_cast<const DecodeArgs>(a), C);
     }
+    const size_t lists = (2 * (size_t)a.kv.B + 1) * 4;
+    static thread_local int done = -1;
+    e = configure(k_decode_split<FP16, D, NT>, S::RING + (2 * KV_MAX_BATCH + 1) * 4, &done);
     if (e != cudaSuccess) return e;
     const int grid = gemm_ctas() * S::CTAS;
     a.workers = std::min(grid * DA_WARPS, KV_MAX_WORKERS);
-    k_decode_split<FP16, D, NT><<<grid, DA_WARPS * 32, smem, st>>>(a);
+    k_decode_split<FP16, D, NT><<<grid, DA_WARPS * 32, S::RING + lists, st>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    const size_t jsmem = lists + (size_t)a.workers * 4;
-    e = launch_pdl(k_decode_join<FP16, D, NT>, std::min(a.kv.B * a.hq, gemm_ctas() * 4), DJ_THREADS, jsmem, st, a);
-    if (e != cudaSuccess || !a.accumulate) return e;
-    cudaLaunchConfig_t cfg = {};
-    const int rows = a.kv.B * a.kv.hkv;
-    const long long most = (a.kv.cap + DW_THREADS - 1) / DW_THREADS;
-    cfg.gridDim = dim3((unsigned)rows, (unsigned)std::max(1ll, std::min(most, (long long)(gemm_ctas() * 8 + rows - 1) / rows)));
-    cfg.blockDim = dim3(DW_THREADS);
-    cfg.dynamicSmemBytes = (size_t)a.group * sizeof(float2);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_decode_weights<FP16>, static_cast<const DecodeArgs>(a));
+    // where a row is shared by many warps, a CTA joins it
+    const int rows = a.kv.B * a.kv.hkv * ((a.group + 8 * NT - 1) / (8 * NT));
+    return rows * 16 <= a.workers ? launch_join<FP16, D, NT, DJ_THREADS>(a, st) : launch_join<FP16, D, NT, 32>(a, st);
 }
 
 template <bool FP16, int D>
@@ -621,8 +953,8 @@ bool decode_plan(const KvView &kv, int hq, bool accumulate, DecodePlan *p) {
     p->score_pitch = (kv.cap + DA_SLOTS - 1) / DA_SLOTS * DA_SLOTS;
     p->scores = take(accumulate ? (size_t)kv.B * hq * p->score_pitch * sizeof(float) : 0);
     p->total = off;
-    // units are counted in 32 bits
-    return (long long)kv.B * ((kv.cap + DA_SLOTS - 1) / DA_SLOTS) * kv.hkv * ((group + heads - 1) / heads) < (1ll << 31);
+    // places of the list are counted in 32 bits
+    return (long long)kv.B * ((kv.cap + DA_SLOTS - 1) / DA_SLOTS + DA_ROW_TILES) * kv.hkv * ((group + heads - 1) / heads) < (1ll << 31);
 }
 
 cudaError_t launch_decode_attention(DecodeArgs &a, cudaStream_t st) {

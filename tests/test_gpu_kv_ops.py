@@ -70,6 +70,11 @@ SHAPES = [
     ([2500], 1, 4, 256, 16, "tokens"),
     ([20000], 1, 2, 128, 16, "heads"),
     ([37] * 150, 2, 2, 64, 16, "heads"),
+    ([0, 1, 17, 300, 64] * 70, 1, 2, 64, 16, "heads"),  # more rows than CTAs run at once
+    ([33, 0, 5, 150] * 26, 4, 5, 128, 16, "tokens"),
+    ([200, 1, 90] * 60, 1, 12, 256, 16, "heads"),
+    ([30000, 10, 500, 0], 2, 7, 64, 16, "tokens"),      # too long for clusters
+    ([26000, 4000], 1, 3, 256, 32, "heads"),
 ]
 
 
