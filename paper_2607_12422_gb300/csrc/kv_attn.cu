@@ -53,6 +53,9 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src, bool read) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 template <int N>
 __device__ __forceinline__ void cp_async_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -192,11 +195,18 @@ struct Segment {
     }
 };
 
+// Where a new token's row goes in K and V (-1: nowhere), and its position.
+struct FreshRow {
+    long long off;
+    int pos;
+};
+
 // A warp's work on its segments: `next(segment)` makes the following one of it, `leave(segment, t0, m, l, o)` takes the
 // results of tiles [t0, t_end) of a row: maxima and sums (a lane's own part of them) of heads 8 nt + 2 (lane % 4) + e, and outputs
 // o[ks][nt]: dims 16 ks + lane / 4 (+ 8 in elements 2 and 3) of those heads.
 template <bool FP16, int D, int NT, typename Next, typename Leave>
-__device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int chunks, Segment at, Next &&next, Leave &&leave) {
+__device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int (*page_ring)[DA_SLOTS],
+                                       FreshRow *fresh_rows, int chunks, Segment at, Next &&next, Leave &&leave) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, CPR = D / 8;  // heads of a chunk, k steps, 16-byte pieces of a row
     constexpr bool Q_AHEAD = KS * NT <= 16;                  // a row's queries are asked for a row ahead, if registers allow
@@ -204,18 +214,28 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int c
     const bool append = a.k_new != nullptr;
     // P's scale: weights of fp16 lie in 2^-24 .. 2^14, so that what is far below the maximum keeps its bits
     const float shift = FP16 ? 14.f : 0.f, c = a.scale * 1.4426950408889634f;
-    Segment ld = at;
-    bool loading = true;
+    Segment ld = at, pg = at;  // the next tile to be copied, and the next whose pages are looked up: STAGES - 1 further on
+    bool loading = true, looking = true;
+    int page_in = 0, page_out = 0;
 
-    // page of slot lane % 16 of the tile at ld; -1: none
-    auto page_of = [&]() {
-        const int slot = ld.t * DA_SLOTS + (lane & 15);
-        if (slot >= ld.n) return -1;
-        const int p = a.kv.table[(long long)ld.b * a.kv.max_pages + slot / a.kv.page_size];
-        return (unsigned)p < (unsigned)a.kv.n_pages ? p : -1;
+    auto entry = [&](const Segment &g, int slot) { return a.kv.table + (long long)g.b * a.kv.max_pages + slot / a.kv.page_size; };
+    auto valid = [&](int p) { return (unsigned)p < (unsigned)a.kv.n_pages ? p : -1; };
+    auto step = [&](Segment &g, bool &more) {
+        if (++g.t == g.t_end) more = next(g);
     };
-    auto step = [&]() {
-        if (++ld.t == ld.t_end) loading = next(ld);
+    // Fetches the table's entries for the tile at pg; they are there when its turn to be copied comes, and nobody waits
+    // for them before.
+    auto look_up = [&]() {
+        if (!looking) return;
+        const int slot = pg.t * DA_SLOTS + lane;
+        if (lane < DA_SLOTS) {
+            if (slot < pg.n)
+                cp_async4(smem_u32(&page_ring[page_in][lane]), entry(pg, slot));
+            else
+                page_ring[page_in][lane] = -1;
+        }
+        page_in = page_in + 1 == S::STAGES ? 0 : page_in + 1;
+        step(pg, looking);
     };
     // Copies the tile at `g` into a stage: lanes 0-15 know K's rows, 16-31 V's.  Rows that are none arrive as zeros.
     auto issue = [&](const Segment &g, int page, int stage) {
@@ -240,23 +260,24 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int c
             cp_async16_or_zero(dst, ks ? ks + cc * 8 : a.kv.k, ks != nullptr);
             cp_async16_or_zero(dst + DA_SLOTS * D * 2, vs ? vs + cc * 8 : a.kv.v, vs != nullptr);
         }
-        if (append && g.t == g.tiles - 1 && g.hc % chunks == 0) {
-            // the new token's row joins the cache; nobody reads it there in this call
-            const int r = (g.n - 1) & 15;
-            const long long o = __shfl_sync(0xffffffffu, off, r);
-            const bool ok = __shfl_sync(0xffffffffu, page, r) >= 0;
-            if (ok) {
-                const long long src = g.b * a.new_stride + (long long)h * D;
-                for (int i = lane; i < CPR; i += 32) {
-                    *reinterpret_cast<int4 *>(const_cast<uint16_t *>(a.kv.k) + o + i * 8) =
-                        *reinterpret_cast<const int4 *>(a.k_new + src + i * 8);
-                    *reinterpret_cast<int4 *>(const_cast<uint16_t *>(a.kv.v) + o + i * 8) =
-                        *reinterpret_cast<const int4 *>(a.v_new + src + i * 8);
-                }
-            }
-            if (lane == 0 && a.new_pos && a.kv.positions)
-                a.kv.positions[((long long)g.b * a.kv.hkv + h) * a.kv.cap + g.n - 1] = a.new_pos[g.b];
+        if (is_new && lane < DA_SLOTS) {  // what is needed to store the row when it has arrived
+            fresh_rows[stage].off = page >= 0 ? off : -1;
+            if (a.new_pos) cp_async4(smem_u32(&fresh_rows[stage].pos), a.new_pos + g.b);
         }
+    };
+    // The new token's row joins the cache (nobody reads it there in this call), from the stage it was copied to.
+    auto store_new = [&](const Segment &g, int stage) {
+        const long long o = fresh_rows[stage].off;
+        const int r = (g.n - 1) & 15, h = g.hc / chunks;
+        if (o >= 0)
+            for (int i = lane; i < 2 * CPR; i += 32) {
+                const int cc = i % CPR;
+                uint16_t *to = const_cast<uint16_t *>(i < CPR ? a.kv.k : a.kv.v) + o + cc * 8;
+                const uint32_t from = ring + stage * S::UNIT + (i < CPR ? 0 : DA_SLOTS * D * 2) + r * (D * 2) + ((cc ^ (r & 7)) << 4);
+                *reinterpret_cast<float4 *>(to) = ld_shared_v4(from);
+            }
+        if (lane == 0 && a.new_pos && a.kv.positions)
+            a.kv.positions[((long long)g.b * a.kv.hkv + h) * a.kv.cap + g.n - 1] = fresh_rows[stage].pos;
     };
     // a row's queries as B operands: head 8 nt + lane / 4, dims 16 ks + 2 (lane % 4) and the next, and 8 further on
     uint32_t qn[Q_AHEAD ? KS : 1][NT][2], qf[KS][NT][2];
@@ -278,24 +299,27 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int c
 
     // The first tiles' pages are looked up before any tile is asked for: one latency, not one for each.
     {
-        Segment early[S::STAGES - 1];
         int pages[S::STAGES - 1];
 #pragma unroll
         for (int s = 0; s < S::STAGES - 1; ++s) {
-            early[s] = ld;
-            pages[s] = -2;
-            if (loading) {
-                pages[s] = page_of();
-                step();
+            pages[s] = -1;
+            if (looking) {
+                const int slot = pg.t * DA_SLOTS + (lane & 15);
+                if (slot < pg.n) pages[s] = *entry(pg, slot);
+                step(pg, looking);
             }
         }
 #pragma unroll
         for (int s = 0; s < S::STAGES - 1; ++s) {
-            if (__any_sync(0xffffffffu, pages[s] != -2)) issue(early[s], pages[s], s);
+            if (loading) {
+                issue(ld, valid(pages[s]), s);
+                step(ld, loading);
+            }
+            look_up();
             cp_async_commit();
         }
     }
-    int page = loading ? page_of() : -1, stage_in = S::STAGES - 1, stage = 0;
+    int stage_in = S::STAGES - 1, stage = 0;
     if constexpr (Q_AHEAD) load_q(at, qn);
 
     float o[KS][NT][4], m[NT][2], l[NT][2];
@@ -331,12 +355,14 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int c
         cp_async_wait<S::STAGES - 2>();
         __syncwarp();  // everybody's copies are there, and everybody is done with the stage that is filled next
         if (loading) {
-            issue(ld, page, stage_in);
+            issue(ld, valid(page_ring[page_out][lane & 15]), stage_in);
             stage_in = stage_in + 1 == S::STAGES ? 0 : stage_in + 1;
-            step();
-            if (loading) page = page_of();  // one tile ahead: its latency is not waited for here
+            page_out = page_out + 1 == S::STAGES ? 0 : page_out + 1;
+            step(ld, loading);
         }
+        look_up();
         cp_async_commit();
+        if (append && at.t == at.tiles - 1 && at.hc % chunks == 0) store_new(at, stage);
         const uint32_t kst = ring + stage * S::UNIT, vst = kst + DA_SLOTS * D * 2;
         stage = stage + 1 == S::STAGES ? 0 : stage + 1;
 
@@ -459,6 +485,8 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16;
     extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int page_ring[DA_WARPS][S::STAGES][DA_SLOTS];
+    __shared__ FreshRow fresh_rows[DA_WARPS][S::STAGES];
     const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int *first = reinterpret_cast<int *>(smem + S::RING), *len = first + B + 1;
     pdl_launch();
@@ -471,7 +499,8 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
     Segment at;
     if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, HC)) return;
     attend<FP16, D, NT>(
-        a, smem_u32(smem) + warp * S::STAGES * S::UNIT, chunks, at, [&](Segment &g) { return g.next(first, len, B, HC); },
+        a, smem_u32(smem) + warp * S::STAGES * S::UNIT, page_ring[warp], fresh_rows[warp], chunks, at,
+        [&](Segment &g) { return g.next(first, len, B, HC); },
         [&](const Segment &g, int t0, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
             const int h = g.hc / chunks, ch = g.hc - h * chunks, d0 = lane >> 2;
             const bool whole = t0 == 0 && g.t_end == g.tiles;
@@ -519,16 +548,19 @@ __device__ __forceinline__ int check_sequence(const DecodeArgs &a, int b, int ti
 }
 
 // Small calls: a cluster of C CTAs a (sequence, KV head).  Its warps take the row's tiles in equal parts; each CTA joins its
-// four warps' results in shared memory, then each takes a share of the outputs from all CTAs' results, and adds the
-// weights of its own slots.
+// four warps' results in shared memory and hands maxima and sums to every CTA, and each piece of the outputs to the CTA
+// that finishes it (stores into distributed shared memory, which nobody waits for, where loads from it would each take
+// 0.8 us).  Last, warps add the weights of their own slots.
 template <bool FP16, int D, int NT>
 __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeArgs a, int C) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, PITCH = D + 4, THREADS = DA_WARPS * 32, D4 = D / 4;
-    static_assert((HEADS * PITCH + HEADS * D) * 4 <= S::STAGES * S::UNIT, "a warp's and a CTA's results lie in a ring");
+    static_assert(HEADS * PITCH * 4 <= S::STAGES * S::UNIT, "a warp's results lie in its ring");
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float2 warp_ml[DA_WARPS][HEADS], every[DA_CLUSTER][HEADS], row_ml[HEADS];
-    __shared__ __align__(8) float2 cta_ml[HEADS];
+    __shared__ int page_ring[DA_WARPS][S::STAGES][DA_SLOTS];
+    __shared__ FreshRow fresh_rows[DA_WARPS][S::STAGES];
+    __shared__ float2 warp_ml[DA_WARPS][HEADS], row_ml[HEADS];
+    __shared__ __align__(8) float2 every[DA_CLUSTER][HEADS];  // maximum and sum of each CTA
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = blockIdx.x % C, row = blockIdx.x / C;
     if (row == a.kv.B * a.kv.hkv) {  // one cluster more: the call's status word has one writer
@@ -539,10 +571,11 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
         if (tid == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
         return;
     }
+    cluster_arrive();  // (this CTA runs: others may store into its shared memory)
     const int b = row / a.kv.hkv, h = row - b * a.kv.hkv, n = attended(a, b), G = a.group;
     const float c = a.scale * 1.4426950408889634f, shift = FP16 ? 14.f : 0.f;
     uint8_t *ring = smem + warp * S::STAGES * S::UNIT;
-    float *mine = reinterpret_cast<float *>(ring), *cta_o = reinterpret_cast<float *>(smem) + HEADS * PITCH;
+    float *mine = reinterpret_cast<float *>(ring), *got = reinterpret_cast<float *>(smem + S::RING);  // got[C][own pieces][4]
     Segment at;
     at.b = b;
     at.hc = h;
@@ -552,9 +585,11 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     at.t = first_of(w, at.tiles, W);
     at.t_end = first_of(w + 1, at.tiles, W);
     const int slot0 = at.t * DA_SLOTS, slot1 = min(n, at.t_end * DA_SLOTS);
+    float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
+    if (a.accumulate && slot0 + lane * 32 < slot1) prefetch_l2(wt + slot0 + lane * 32);
     if (at.t < at.t_end) {
         attend<FP16, D, NT>(
-            a, smem_u32(ring), 1, at, [&](Segment &) { return false; },
+            a, smem_u32(ring), page_ring[warp], fresh_rows[warp], 1, at, [&](Segment &) { return false; },
             [&](const Segment &, int, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
                 cp_async_wait_all();
                 __syncwarp();  // (the ring is free)
@@ -581,8 +616,11 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
         acc.z += f * x.z;
         acc.w += f * x.w;
     };
+    // Piece p (a head's four dims) is finished by CTA p % C, as its piece p / C of `own`.
+    const int pieces = G * D4, own = (pieces + C - 1) / C;
+    cluster_wait();
     // (a part whose sum is 0 has no outputs, or was never written)
-    for (int p = tid; p < G * D4; p += THREADS) {
+    for (int p = tid; p < pieces; p += THREADS) {
         const int j = p / D4, d4 = p % D4;
         float mx = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -597,15 +635,10 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
             sum += f * x.y;
             add(acc, f, *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + i * S::STAGES * S::UNIT) + j * PITCH + d4 * 4));
         }
-        *reinterpret_cast<float4 *>(cta_o + j * D + d4 * 4) = acc;
-        if (d4 == 0) cta_ml[j] = make_float2(mx, sum);
+        st_cluster_v4(map_cta(smem_u32(got + (rank * own + p / C) * 4), p % C), acc);
+        if (d4 < C) st_cluster_v2(map_cta(smem_u32(&every[rank][j]), d4), mx, sum);
     }
     cluster_sync();
-    for (int i = tid; i < C * G; i += THREADS) {
-        const float2 x = ld_cluster_v2(map_cta(smem_u32(&cta_ml[i % G]), i / G));
-        every[i / G][i % G] = x;
-    }
-    __syncthreads();
     if (tid < G) {
         float mx = -INFINITY, sum = 0.f;
         for (int i = 0; i < C; ++i) mx = fmaxf(mx, every[i][tid].x);
@@ -619,28 +652,17 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
         if (rank == 0 && a.lse) a.lse[(long long)b * a.hq + h * G + tid] = mx * a.scale + log_sum<FP16>(sum);
     }
     __syncthreads();
-    for (int p = tid * C + rank; p < G * D4; p += THREADS * C) {
-        const int j = p / D4, d4 = p % D4;
-        const uint32_t from = smem_u32(cta_o + j * D + d4 * 4);
+    for (int q = tid; q * C + rank < pieces; q += THREADS) {
+        const int p = q * C + rank, j = p / D4, d4 = p % D4;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i0 = 0; i0 < C; i0 += 8) {
-            float4 x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i0 + i < C) x[i] = ld_cluster_v4(map_cta(from, i0 + i));
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i0 + i < C) add(acc, every[i0 + i][j].x, x[i]);
-        }
+        for (int i = 0; i < C; ++i) add(acc, every[i][j].x, *reinterpret_cast<const float4 *>(got + (i * own + q) * 4));
         const float inv = row_ml[j].y;
         uint2 r;
         r.x = pack2<FP16>(acc.x * inv, acc.y * inv);
         r.y = pack2<FP16>(acc.z * inv, acc.w * inv);
         *reinterpret_cast<uint2 *>(a.out + ((long long)b * a.hq + h * G + j) * D + d4 * 4) = r;
     }
-    cluster_arrive();  // (this CTA reads no other's shared memory any more)
     if (a.accumulate) {
-        float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
         const float *sc = a.scores + ((long long)b * a.hq + h * G) * a.score_pitch;
         const int fresh = a.k_new ? n - 1 : -1;
         for (int slot = slot0 + lane; slot < slot1; slot += 32) {
@@ -650,7 +672,6 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
             wt[slot] = sum;
         }
     }
-    cluster_wait();
 }
 
 constexpr int DJ_THREADS = 256;
@@ -889,7 +910,7 @@ int pick_cluster(const DecodeArgs &a, int ctas, int most) {
     const long long rows = (long long)a.kv.B * a.kv.hkv, tiles = (a.kv.cap + DA_SLOTS - 1) / DA_SLOTS;
     if (a.group > 16 || rows > ctas) return 0;
     int C = 1;
-    while (C < most && rows * C * 2 <= ctas && C * DA_WARPS < tiles) C *= 2;
+    while (C < most && rows * C * 2 <= ctas && C * DA_WARPS * 2 <= tiles) C *= 2;
     return tiles <= (long long)C * DA_WARPS * DA_CLUSTER_TILES ? C : 0;
 }
 
@@ -897,13 +918,14 @@ template <bool FP16, int D, int NT>
 cudaError_t launch(DecodeArgs &a, cudaStream_t st) {
     using S = DaShape<D>;
     static thread_local int done_c = -1, most = 8;
-    cudaError_t e = configure(k_decode_cluster<FP16, D, NT>, S::RING, &done_c, &most);
+    constexpr size_t C_SMEM = S::RING + 8 * NT * D * 4 + DA_CLUSTER * 16;  // (rings, pieces of outputs)
+    cudaError_t e = configure(k_decode_cluster<FP16, D, NT>, C_SMEM, &done_c, &most);
     if (e != cudaSuccess) return e;
     if (const int C = pick_cluster(a, gemm_ctas() * S::CTAS, most)) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)((a.kv.B * a.kv.hkv + 1) * C));
         cfg.blockDim = dim3(DA_WARPS * 32);
-        cfg.dynamicSmemBytes = S::RING;
+        cfg.dynamicSmemBytes = C_SMEM;
         cfg.stream = st;
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
