@@ -137,6 +137,7 @@ pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, fl
     a.status = reinterpret_cast<int *>(ws);
     a.part_o = reinterpret_cast<float *>(ws + p.part_o);
     a.part_ml = reinterpret_cast<float2 *>(ws + p.part_ml);
+    a.worker_bad = reinterpret_cast<int *>(ws + p.worker_bad);
     a.row_ml = reinterpret_cast<float2 *>(ws + p.row_ml);
     a.scores = accumulate ? reinterpret_cast<float *>(ws + p.scores) : nullptr;
     a.score_pitch = p.score_pitch;

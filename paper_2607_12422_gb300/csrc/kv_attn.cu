@@ -204,8 +204,9 @@ struct FreshRow {
 // A warp's work on its segments: `next(segment)` makes the following one of it, `leave(segment, t0, m, l, o)` takes the
 // results of tiles [t0, t_end) of a row: maxima and sums (a lane's own part of them) of heads 8 nt + 2 (lane % 4) + e, and outputs
 // o[ks][nt]: dims 16 ks + lane / 4 (+ 8 in elements 2 and 3) of those heads.
+// Returns whether a page was outside the cache.
 template <bool FP16, int D, int NT, typename Next, typename Leave>
-__device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int (*page_ring)[DA_SLOTS],
+__device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (*page_ring)[DA_SLOTS],
                                        FreshRow *fresh_rows, int chunks, Segment at, Next &&next, Leave &&leave) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, CPR = D / 8;  // heads of a chunk, k steps, 16-byte pieces of a row
@@ -219,7 +220,12 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int (
     int page_in = 0, page_out = 0;
 
     auto entry = [&](const Segment &g, int slot) { return a.kv.table + (long long)g.b * a.kv.max_pages + slot / a.kv.page_size; };
-    auto valid = [&](int p) { return (unsigned)p < (unsigned)a.kv.n_pages ? p : -1; };
+    bool bad = false;
+    auto valid = [&](const Segment &g, int p) {
+        const bool ok = (unsigned)p < (unsigned)a.kv.n_pages;
+        bad |= !ok && g.t * DA_SLOTS + (lane & 15) < g.n;
+        return ok ? p : -1;
+    };
     auto step = [&](Segment &g, bool &more) {
         if (++g.t == g.t_end) more = next(g);
     };
@@ -312,7 +318,7 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int (
 #pragma unroll
         for (int s = 0; s < S::STAGES - 1; ++s) {
             if (loading) {
-                issue(ld, valid(pages[s]), s);
+                issue(ld, valid(ld, pages[s]), s);
                 step(ld, loading);
             }
             look_up();
@@ -355,7 +361,7 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int (
         cp_async_wait<S::STAGES - 2>();
         __syncwarp();  // everybody's copies are there, and everybody is done with the stage that is filled next
         if (loading) {
-            issue(ld, valid(page_ring[page_out][lane & 15]), stage_in);
+            issue(ld, valid(ld, page_ring[page_out][lane & 15]), stage_in);
             stage_in = stage_in + 1 == S::STAGES ? 0 : stage_in + 1;
             page_out = page_out + 1 == S::STAGES ? 0 : page_out + 1;
             step(ld, loading);
@@ -471,6 +477,7 @@ __device__ __forceinline__ void attend(const DecodeArgs &a, uint32_t ring, int (
             going = next(at);
         }
     }
+    return __any_sync(0xffffffffu, bad);
 }
 
 // 1 / sum; 0 for a row without anything, NaN for NaN
@@ -490,15 +497,17 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
     const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int *first = reinterpret_cast<int *>(smem + S::RING), *len = first + B + 1;
     pdl_launch();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = DEV_OK;  // (k_decode_join latches)
     tile_lists(a, first, len);
     const int chunks = (a.group + HEADS - 1) / HEADS, HC = a.kv.hkv * chunks;
     const int count = first[B] * HC, workers = workers_of(a, count);
     const int w = warp * gridDim.x + blockIdx.x;  // neighbours in the list on different SMs
     if (count == 0 || w >= workers) return;
     Segment at;
-    if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, HC)) return;
-    attend<FP16, D, NT>(
+    if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, HC)) {
+        if (lane == 0) a.worker_bad[w] = 0;
+        return;
+    }
+    const bool bad = attend<FP16, D, NT>(
         a, smem_u32(smem) + warp * S::STAGES * S::UNIT, page_ring[warp], fresh_rows[warp], chunks, at,
         [&](Segment &g) { return g.next(first, len, B, HC); },
         [&](const Segment &g, int t0, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
@@ -535,16 +544,14 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
                     }
                 }
         });
+    if (lane == 0) a.worker_bad[w] = bad;  // (k_decode_join reports it: the status word has one writer)
 }
 
-// Lengths and pages outside their ranges: a code, or DEV_OK, in one thread or another.
-__device__ __forceinline__ int check_sequence(const DecodeArgs &a, int b, int tid, int threads) {
-    const int raw = a.kv.lens[b], n = attended(a, b);
-    if (n != raw + (a.k_new ? 1 : 0)) return DEV_BAD_POSITION;
-    const int pages = (n + a.kv.page_size - 1) / a.kv.page_size;
-    for (int i = tid; i < pages; i += threads)
-        if ((unsigned)a.kv.table[(long long)b * a.kv.max_pages + i] >= (unsigned)a.kv.n_pages) return DEV_BAD_PAGE;
-    return DEV_OK;
+// Lengths outside the table, over the whole CTA.
+__device__ __forceinline__ bool bad_length(const DecodeArgs &a) {
+    bool bad = false;
+    for (int b = threadIdx.x; b < a.kv.B; b += blockDim.x) bad |= attended(a, b) != a.kv.lens[b] + (a.k_new ? 1 : 0);
+    return __syncthreads_or(bad);
 }
 
 // Small calls: a cluster of C CTAs a (sequence, KV head).  Its warps take the row's tiles in equal parts; each CTA joins its
@@ -565,9 +572,14 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     const int rank = blockIdx.x % C, row = blockIdx.x / C;
     if (row == a.kv.B * a.kv.hkv) {  // one cluster more: the call's status word has one writer
         if (rank != 0) return;
-        int code = DEV_OK;
-        for (int b = 0; b < a.kv.B; ++b) code = max(code, check_sequence(a, b, tid, THREADS));
-        const int page = __syncthreads_or(code == DEV_BAD_PAGE), length = __syncthreads_or(code == DEV_BAD_POSITION);
+        const bool length = bad_length(a);
+        bool page = false;
+#pragma unroll 8
+        for (int i = tid; i < a.kv.B * a.kv.max_pages; i += THREADS) {  // (clusters mean short tables)
+            const int s = i / a.kv.max_pages, at = i - s * a.kv.max_pages;
+            if (at * a.kv.page_size < attended(a, s)) page |= (unsigned)a.kv.table[i] >= (unsigned)a.kv.n_pages;
+        }
+        page = __syncthreads_or(page);
         if (tid == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
         return;
     }
@@ -675,13 +687,15 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
 }
 
 constexpr int DJ_THREADS = 256;
-constexpr int DJ_SLOTS = 4;  // of a thread that adds weights
+constexpr int DJ_SLOTS = 8;  // of a thread that adds weights, at a time
 
 // Joins what several warps left of a row: out = sum_w f_w o_w / sum_w f_w l_w, f_w = exp(scale (m_w - max)).  TEAM threads a
 // query head: the CTA where many warps share a row, a warp where rows are many.  Sequences without a slot get
-// zeros.  The CTAs behind `join_ctas` add the weights, each taking maximum and sum of its heads from the warps' again.
+// zeros.  The CTAs behind `join_ctas` add the weights: each takes a stretch of the list of [sequence][KV head][tile], and maximum
+// and sum of its heads from the warps' again.  One CTA an SM finds room beside k_decode_split's, so all that does
+// not depend on it is done when it ends.
 template <bool FP16, int D, int NT, int TEAM>
-__global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, int join_ctas, int weight_blocks) {
+__global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, int join_ctas) {
     constexpr int HEADS = 8 * NT, TEAMS = DJ_THREADS / TEAM, L = D / 4 < TEAM ? D / 4 : TEAM, V = D / 4 / L, G = TEAM / L;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float red[2][DJ_THREADS / 32];
@@ -704,74 +718,88 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
 
     if ((int)blockIdx.x >= join_ctas) {
         // weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0
-        const int item = blockIdx.x - join_ctas, row = item / weight_blocks, block = item - row * weight_blocks;
-        const int h = row % a.kv.hkv, b = row / a.kv.hkv, n = len[b], fresh = a.k_new ? n - 1 : -1;
+        const int ctas = gridDim.x - join_ctas, me = blockIdx.x - join_ctas, all = first[B] * a.kv.hkv;
+        float2 *ml = reinterpret_cast<float2 *>(fac);
+        const float shift = FP16 ? 14.f : 0.f;
+        Segment at;
+        bool going = all > 0 && at.seek(first_of(me, all, ctas), first_of(me + 1, all, ctas), first, len, B, a.kv.hkv);
         constexpr int STEP = DJ_THREADS * DJ_SLOTS;
-        if (block * STEP >= n) return;
-        float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
         float have[DJ_SLOTS];
-        auto load_weights = [&](int s0) {
+        auto weights_at = [&]() { return a.kv.weights + ((long long)at.b * a.kv.hkv + at.hc) * a.kv.cap; };
+        auto load_weights = [&](int s0, int s1) {
+            const int fresh = a.k_new ? at.n - 1 : -1;
+            const float *wt = weights_at();
 #pragma unroll
             for (int i = 0; i < DJ_SLOTS; ++i) {
                 const int slot = s0 + i * DJ_THREADS + tid;
-                have[i] = slot < n && slot != fresh ? wt[slot] : 0.f;
+                have[i] = slot < s1 && slot != fresh ? wt[slot] : 0.f;
             }
         };
-        load_weights(block * STEP);  // (no kernel of this call has written them)
-        float2 *ml = reinterpret_cast<float2 *>(fac);
+        if (going) load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS));  // (no kernel of this call has written them)
         pdl_wait();
-        for (int g = warp; g < a.group; g += DJ_THREADS / 32) {  // a warp a head
-            const int ch = g / HEADS, j = g - ch * HEADS;
-            int w0;
-            const int nw = span(b, h, ch, &w0);
-            if (nw == 1) {
-                if (lane == 0) {
-                    const float2 x = a.row_ml[(long long)b * a.hq + h * a.group + g];
-                    ml[g] = make_float2(x.x == -INFINITY ? 0.f : x.x, x.y);
+        for (bool begun = true; going; begun = false) {
+            const int s0 = at.t * DA_SLOTS, s1 = min(at.n, at.t_end * DA_SLOTS);
+            __syncthreads();  // (ml of the row before has been read)
+            for (int g = warp; g < a.group; g += DJ_THREADS / 32) {  // a warp a head
+                const int ch = g / HEADS, j = g - ch * HEADS;
+                int w0;
+                const int nw = span(at.b, at.hc, ch, &w0);
+                if (nw == 1) {
+                    if (lane == 0) {
+                        const float2 x = a.row_ml[(long long)at.b * a.hq + at.hc * a.group + g];
+                        ml[g] = make_float2(x.x == -INFINITY ? 0.f : x.x, x.y);
+                    }
+                    continue;
                 }
-                continue;
+                float m = -INFINITY, l = 0.f;
+#pragma unroll 5
+                for (int i = lane; i < nw; i += 32) {
+                    const float2 x = a.part_ml[part_at(w0, i, j)];
+                    const float mx = fmaxf(m, x.x), mu = mx == -INFINITY ? 0.f : mx;
+                    l = l * ex2((m - mu) * c) + x.y * ex2((x.x - mu) * c);
+                    m = mx;
+                }
+                float mx = m;
+                for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+                const float mu = mx == -INFINITY ? 0.f : mx;
+                l *= ex2((m - mu) * c);
+                for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+                if (lane == 0) ml[g] = make_float2(mu, inverse(l));
             }
-            float m = -INFINITY, l = 0.f;
-            for (int i = lane; i < nw; i += 32) {
-                const float2 x = a.part_ml[part_at(w0, i, j)];
-                const float mx = fmaxf(m, x.x), mu = mx == -INFINITY ? 0.f : mx;
-                l = l * ex2((m - mu) * c) + x.y * ex2((x.x - mu) * c);
-                m = mx;
-            }
-            float mx = m;
-            for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-            l *= ex2((m - (mx == -INFINITY ? 0.f : mx)) * c);
-            for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-            if (lane == 0) ml[g] = make_float2(mx == -INFINITY ? 0.f : mx, inverse(l));
-        }
-        __syncthreads();
-        const float shift = FP16 ? 14.f : 0.f;
-        const float *sc = a.scores + ((long long)b * a.hq + h * a.group) * a.score_pitch;
-        for (int s0 = block * STEP; s0 < n; s0 += weight_blocks * STEP) {
-            if (s0 != block * STEP) load_weights(s0);
-            float sum[DJ_SLOTS] = {};
+            __syncthreads();
+            const float *sc = a.scores + ((long long)at.b * a.hq + at.hc * a.group) * a.score_pitch;
+            float *wt = weights_at();
+            for (int s = s0; s < s1; s += STEP) {
+                if (!begun || s != s0) load_weights(s, s1);
+                float sum[DJ_SLOTS] = {};
 #pragma unroll 2
-            for (int g = 0; g < a.group; ++g) {
-                const float2 x = ml[g];
+                for (int g = 0; g < a.group; ++g) {
+                    const float2 x = ml[g];
+#pragma unroll
+                    for (int i = 0; i < DJ_SLOTS; ++i) {
+                        const int slot = s + i * DJ_THREADS + tid;
+                        if (slot < s1) sum[i] += ex2((sc[g * a.score_pitch + slot] - x.x) * c + shift) * x.y;
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < DJ_SLOTS; ++i) {
-                    const int slot = s0 + i * DJ_THREADS + tid;
-                    if (slot < n) sum[i] += ex2((sc[g * a.score_pitch + slot] - x.x) * c + shift) * x.y;
+                    const int slot = s + i * DJ_THREADS + tid;
+                    if (slot < s1) wt[slot] = have[i] + sum[i];
                 }
             }
-#pragma unroll
-            for (int i = 0; i < DJ_SLOTS; ++i) {
-                const int slot = s0 + i * DJ_THREADS + tid;
-                if (slot < n) wt[slot] = have[i] + sum[i];
-            }
+            going = at.next(first, len, B, a.kv.hkv);
         }
         return;
     }
 
+    const bool length = blockIdx.x == 0 && bad_length(a);
     pdl_wait();
-    for (int b = blockIdx.x; b < B; b += join_ctas) {
-        const int code = check_sequence(a, b, tid, DJ_THREADS);
-        if (code != DEV_OK) latch_error(a.status, code);
+    if (blockIdx.x == 0) {
+        bool page = false;
+        if (count > 0)
+            for (int w = tid; w < workers; w += DJ_THREADS) page |= a.worker_bad[w] != 0;
+        page = __syncthreads_or(page);
+        if (tid == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
     }
     const int rows = B * a.hq, team = tid / TEAM, me = tid % TEAM;
     float *f_team = fac + team * a.workers;
@@ -792,8 +820,22 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
         int w0;
         const int nw = span(b, h, ch, &w0);
         if (nw == 1) continue;  // one warp did it all
-        float mx = -INFINITY;
-        for (int i = me; i < nw; i += TEAM) mx = fmaxf(mx, a.part_ml[part_at(w0, i, j)].x);
+        // the first outputs are asked for before their factors are known
+        constexpr int U = V == 1 ? 8 : 4;
+        const int d4 = me % L, grp = me / L;
+        float4 x[U][V];
+        auto load = [&](int i0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * G < nw)
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        x[u][v] = *reinterpret_cast<const float4 *>(a.part_o + part_at(w0, i0 + u * G, j) * D + (v * L + d4) * 4);
+        };
+        load(grp);
+        const float2 own = me < nw ? a.part_ml[part_at(w0, me, j)] : make_float2(-INFINITY, 0.f);
+        float mx = own.x;
+        for (int i = me + TEAM; i < nw; i += TEAM) mx = fmaxf(mx, a.part_ml[part_at(w0, i, j)].x);
         for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
         team_sync();  // (what the row before left in shared memory has been read)
         if (TEAM > 32) {
@@ -804,7 +846,7 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
         const float mu = mx == -INFINITY ? 0.f : mx;
         float sum = 0.f;
         for (int i = me; i < nw; i += TEAM) {
-            const float2 ml = a.part_ml[part_at(w0, i, j)];
+            const float2 ml = i == me ? own : a.part_ml[part_at(w0, i, j)];
             const float f = ex2((ml.x - mu) * c);
             f_team[i] = f;
             sum += f * ml.y;
@@ -819,16 +861,8 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
         float4 acc[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-        const int d4 = me % L, grp = me / L;
-        constexpr int U = V == 1 ? 8 : 4;
         for (int i0 = grp; i0 < nw; i0 += G * U) {
-            float4 x[U][V];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i0 + u * G < nw)
-#pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        x[u][v] = *reinterpret_cast<const float4 *>(a.part_o + part_at(w0, i0 + u * G, j) * D + (v * L + d4) * 4);
+            if (i0 != grp) load(i0);
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (i0 + u * G < nw) {
@@ -847,11 +881,11 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
             __syncthreads();
             if (grp == 0)
                 for (int i = 1; i < G; ++i) {
-                    const float4 x = sum_o[i * L + d4];
-                    acc[0].x += x.x;
-                    acc[0].y += x.y;
-                    acc[0].z += x.z;
-                    acc[0].w += x.w;
+                    const float4 y = sum_o[i * L + d4];
+                    acc[0].x += y.x;
+                    acc[0].y += y.y;
+                    acc[0].z += y.z;
+                    acc[0].w += y.w;
                 }
         } else {
             for (int s = L; s < TEAM; s <<= 1) {
@@ -897,11 +931,9 @@ cudaError_t launch_join(DecodeArgs &a, cudaStream_t st) {
     const size_t facs = std::max((size_t)(DJ_THREADS / TEAM) * a.workers * 4, (size_t)a.group * 8);
     cudaError_t e = configure(k_decode_join<FP16, D, NT, TEAM>, most, &done);
     if (e != cudaSuccess) return e;
-    const int teams = DJ_THREADS / TEAM, rows = a.kv.B * a.hq, pairs = a.kv.B * a.kv.hkv;
-    const int join = std::min((rows + teams - 1) / teams, gemm_ctas() * 4);
-    const long long blocks = (a.kv.cap + DJ_THREADS * DJ_SLOTS - 1) / (DJ_THREADS * DJ_SLOTS);
-    const int wb = a.accumulate ? (int)std::max(1ll, std::min(blocks, (long long)(gemm_ctas() * 8 + pairs - 1) / pairs)) : 0;
-    return launch_pdl(k_decode_join<FP16, D, NT, TEAM>, join + wb * pairs, DJ_THREADS, (lists + 7) / 8 * 8 + facs, st, a, join, wb);
+    const int teams = DJ_THREADS / TEAM, rows = a.kv.B * a.hq, sms = gemm_ctas();
+    const int join = std::min((rows + teams - 1) / teams, a.accumulate ? sms / 2 : sms), grid = a.accumulate ? sms : join;
+    return launch_pdl(k_decode_join<FP16, D, NT, TEAM>, grid, DJ_THREADS, (lists + 7) / 8 * 8 + facs, st, a, join);
 }
 
 // CTAs of a (sequence, KV head)'s cluster, or 0 where the list of tiles is the better way: clusters where all of them run at
@@ -971,6 +1003,7 @@ bool decode_plan(const KvView &kv, int hq, bool accumulate, DecodePlan *p) {
     };
     p->part_o = take((size_t)KV_MAX_WORKERS * 2 * heads * kv.d * sizeof(float));
     p->part_ml = take((size_t)KV_MAX_WORKERS * 2 * heads * sizeof(float2));
+    p->worker_bad = take((size_t)KV_MAX_WORKERS * sizeof(int));
     p->row_ml = take((size_t)kv.B * hq * sizeof(float2));
     p->score_pitch = (kv.cap + DA_SLOTS - 1) / DA_SLOTS * DA_SLOTS;
     p->scores = take(accumulate ? (size_t)kv.B * hq * p->score_pitch * sizeof(float) : 0);

@@ -46,15 +46,15 @@ __device__ __forceinline__ int slots_of(const EvictArgs &a, int b) {
     return (int)max(0ll, min((long long)a.kv.lens[b], a.kv.cap));
 }
 __device__ void check_cache(const EvictArgs &a) {
-    int code = DEV_OK;
-    for (int b = 0; b < a.kv.B; ++b) {
-        const int n = slots_of(a, b);
-        if (a.kv.lens[b] != n) code = DEV_BAD_POSITION;
-        const int pages = n <= a.n_keep ? 0 : (n + a.kv.page_size - 1) / a.kv.page_size;
-        for (int i = threadIdx.x; i < pages; i += EV_THREADS)
-            if ((unsigned)a.kv.table[(long long)b * a.kv.max_pages + i] >= (unsigned)a.kv.n_pages) code = DEV_BAD_PAGE;
+    bool length = false, page = false;
+    for (int b = threadIdx.x; b < a.kv.B; b += EV_THREADS) length |= a.kv.lens[b] != slots_of(a, b);
+#pragma unroll 8
+    for (long long i = threadIdx.x; i < (long long)a.kv.B * a.kv.max_pages; i += EV_THREADS) {
+        const int b = (int)(i / a.kv.max_pages), at = (int)(i - (long long)b * a.kv.max_pages), n = slots_of(a, b);
+        if (n > a.n_keep && (long long)at * a.kv.page_size < n) page |= (unsigned)a.kv.table[i] >= (unsigned)a.kv.n_pages;
     }
-    const int length = __syncthreads_or(code == DEV_BAD_POSITION), page = __syncthreads_or(code == DEV_BAD_PAGE);
+    length = __syncthreads_or(length);
+    page = __syncthreads_or(page);
     if (threadIdx.x == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
 }
 

@@ -39,13 +39,14 @@ struct DecodeArgs {
     // scratch (decode_plan)
     float *part_o;    // [workers][2][heads of a chunk][d]
     float2 *part_ml;  // [workers][2][heads of a chunk]: maximum, sum
+    int *worker_bad;  // [workers]: a page was outside the cache
     float2 *row_ml;   // [B][hq]: maximum, 1 / sum
     float *scores;    // [B][hq][score_pitch] when accumulating
     long long score_pitch;
     int workers;
 };
 struct DecodePlan {
-    size_t part_o, part_ml, row_ml, scores, total;  // offsets in the workspace
+    size_t part_o, part_ml, worker_bad, row_ml, scores, total;  // offsets in the workspace
     long long score_pitch;
 };
 bool decode_plan(const KvView &kv, int hq, bool accumulate, DecodePlan *p);
