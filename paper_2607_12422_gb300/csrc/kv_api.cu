@@ -70,6 +70,10 @@ KvView view(const pbd_kv_pages &kv) {
     v.d = kv.head_dim;
     v.B = kv.batch;
     v.max_pages = kv.max_pages;
+    // 2^shift / page_size rounded up is off by less than 2^(shift - 30) / 2^30 of the quotient of any slot below 2^30
+    v.page_shift = 30;
+    while ((1ll << (v.page_shift - 30)) < kv.page_size) ++v.page_shift;
+    v.page_mul = (uint32_t)(((1ull << v.page_shift) + kv.page_size - 1) / kv.page_size);
     return v;
 }
 

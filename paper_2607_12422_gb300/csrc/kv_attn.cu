@@ -32,6 +32,8 @@ constexpr int DA_WARPS = 4;
 constexpr int DA_SLOTS = 16;      // slots of a tile
 constexpr int DA_MIN_TILES = 2;   // of a warp's stretch
 constexpr int DA_ROW_TILES = 2;   // what beginning and ending a (sequence, KV head) costs a warp, in tiles
+constexpr float DA_FP16_SHIFT = 10.f, DA_SLACK = 4.f;  // log2 of factors: of P in fp16, of P beyond 1 (attend)
+constexpr int DA_LANES = 8;       // lanes that copy a row together: a whole line
 constexpr int DA_CLUSTER = 16;    // CTAs of a cluster at most
 constexpr int DA_CLUSTER_TILES = 16;  // tiles of its warps at most
 
@@ -50,9 +52,8 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-__device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src, bool read) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
-}
+__device__ const uint4 zero_row[32] = {};  // what is copied for rows that are none
+
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -156,7 +157,7 @@ __device__ __forceinline__ int worker_at(long long at, int count, int workers) {
 
 // Tiles [t, t_end) of one row: what a warp works on before it leaves the row.
 struct Segment {
-    int b, hc, t, t_end, tiles, n;  // sequence, KV head and chunk, the row's tiles and slots
+    int b, h, ch, t, t_end, tiles, n;  // sequence, KV head, chunk of its query heads, the row's tiles and slots
     int at, end;                    // list place of the row, end of the warp's stretch
     __device__ __forceinline__ bool clip(const int *len) {
         n = len[b];
@@ -165,7 +166,8 @@ struct Segment {
         return t < t_end;
     }
     // The first segment of the stretch [u, end); false if it has none.
-    __device__ __forceinline__ bool seek(int u, int u_end, const int *first, const int *len, int B, int HC) {
+    __device__ __forceinline__ bool seek(int u, int u_end, const int *first, const int *len, int B, int hkv, int chunks) {
+        const int HC = hkv * chunks;
         end = u_end;
         if (u >= end) return false;
         int lo = 0, hi = B;  // first[lo] * HC <= u < first[hi] * HC
@@ -178,27 +180,37 @@ struct Segment {
         }
         b = lo;
         const int per = first[b + 1] - first[b];
-        hc = (u - first[b] * HC) / per;
+        const int hc = (u - first[b] * HC) / per;
+        h = hc / chunks;
+        ch = hc - h * chunks;
         at = first[b] * HC + hc * per;
         t = max(0, u - at - DA_ROW_TILES);
-        return clip(len) || next(first, len, B, HC);
+        return clip(len) || next(first, len, B, hkv, chunks);
     }
-    __device__ __forceinline__ bool next(const int *first, const int *len, int B, int HC) {
+    __device__ __forceinline__ bool next(const int *first, const int *len, int B, int hkv, int chunks) {
         at += first[b + 1] - first[b];
-        if (++hc == HC) {
-            hc = 0;
-            do ++b;
-            while (b < B && first[b + 1] == first[b]);
+        if (++ch == chunks) {
+            ch = 0;
+            if (++h == hkv) {
+                h = 0;
+                do ++b;
+                while (b < B && first[b + 1] == first[b]);
+            }
         }
         t = 0;
         return b < B && at < end && clip(len);  // (where only a row's front is left the stretch is over)
     }
 };
 
-// Where a new token's row goes in K and V (-1: nowhere), and its position.
-struct FreshRow {
-    long long off;
-    int pos;
+// What a warp keeps in shared memory beside its tiles.
+template <int STAGES>
+struct Rings {
+    ulonglong2 row[2][DA_SLOTS];  // where the rows of a tile's K and V are: of the tile to be copied, and of the next
+    struct {
+        long long off;  // where a new token's row goes in K and V (-1: nowhere), and its position
+        int pos;
+    } fresh[STAGES + 1];
+    int page[STAGES][DA_SLOTS];  // the table's entries
 };
 
 // A warp's work on its segments: `next(segment)` makes the following one of it, `leave(segment, t0, m, l, o)` takes the
@@ -206,75 +218,81 @@ struct FreshRow {
 // o[ks][nt]: dims 16 ks + lane / 4 (+ 8 in elements 2 and 3) of those heads.
 // Returns whether a page was outside the cache.
 template <bool FP16, int D, int NT, typename Next, typename Leave>
-__device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (*page_ring)[DA_SLOTS],
-                                       FreshRow *fresh_rows, int chunks, Segment at, Next &&next, Leave &&leave) {
+__device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings<DaShape<D>::STAGES> &rings, Segment at, Next &&next,
+                                       Leave &&leave) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, CPR = D / 8;  // heads of a chunk, k steps, 16-byte pieces of a row
     constexpr bool Q_AHEAD = KS * NT <= 16;                  // a row's queries are asked for a row ahead, if registers allow
     const int lane = threadIdx.x & 31;
     const bool append = a.k_new != nullptr;
+    const float c = a.scale * 1.4426950408889634f;
     // P's scale: weights of fp16 lie in 2^-24 .. 2^14, so that what is far below the maximum keeps its bits
-    const float shift = FP16 ? 14.f : 0.f, c = a.scale * 1.4426950408889634f;
-    Segment ld = at, pg = at;  // the next tile to be copied, and the next whose pages are looked up: STAGES - 1 further on
-    bool loading = true, looking = true;
-    int page_in = 0, page_out = 0;
-
-    auto entry = [&](const Segment &g, int slot) { return a.kv.table + (long long)g.b * a.kv.max_pages + slot / a.kv.page_size; };
-    bool bad = false;
-    auto valid = [&](const Segment &g, int p) {
-        const bool ok = (unsigned)p < (unsigned)a.kv.n_pages;
-        bad |= !ok && g.t * DA_SLOTS + (lane & 15) < g.n;
-        return ok ? p : -1;
-    };
+    const float shift = FP16 ? DA_FP16_SHIFT : 0.f;
+    const float slack = fminf(DA_SLACK / c, 1e30f);
+    // Tile by tile, in three steps, each so far ahead of the next that nothing is waited for: the table's entries are
+    // fetched, STAGES - 1 tiles before they are used; rows' addresses are made of them, by a lane a row; the rows are copied, STAGES - 1
+    // tiles before they are multiplied.  (Warps are few, so a step's instructions and waits count: with addresses handed
+    // round by shuffles and entries waited for, 64 ragged sequences of d = 64 took 40 us instead of 28.)
+    Segment rs = at, pg = at;  // the next tile whose addresses are made, and whose entries are fetched
+    bool resolving = true, looking = true, bad = false;
+    int page_in = 0, page_out = 0, buf = 0, fresh_in = 0, fresh_out = 0;
+    auto turn = [](int &i, int n) { i = i + 1 == n ? 0 : i + 1; };
     auto step = [&](Segment &g, bool &more) {
         if (++g.t == g.t_end) more = next(g);
     };
-    // Fetches the table's entries for the tile at pg; they are there when its turn to be copied comes, and nobody waits
-    // for them before.
+    auto entry = [&](const Segment &g, int slot) { return a.kv.table + (long long)g.b * a.kv.max_pages + page_index(a.kv, slot); };
     auto look_up = [&]() {
         if (!looking) return;
         const int slot = pg.t * DA_SLOTS + lane;
-        if (lane < DA_SLOTS) {
-            if (slot < pg.n)
-                cp_async4(smem_u32(&page_ring[page_in][lane]), entry(pg, slot));
-            else
-                page_ring[page_in][lane] = -1;
-        }
-        page_in = page_in + 1 == S::STAGES ? 0 : page_in + 1;
+        if (lane < DA_SLOTS && slot < pg.n) cp_async4(smem_u32(&rings.page[page_in][lane]), entry(pg, slot));
+        turn(page_in, S::STAGES);
         step(pg, looking);
     };
-    // Copies the tile at `g` into a stage: lanes 0-15 know K's rows, 16-31 V's.  Rows that are none arrive as zeros.
-    auto issue = [&](const Segment &g, int page, int stage) {
-        const int slot = g.t * DA_SLOTS + (lane & 15), h = g.hc / chunks;
-        const bool is_new = append && slot == g.n - 1;
-        const long long off = (long long)page * a.kv.stride_page + h * a.kv.stride_head +
-                              (long long)(slot % a.kv.page_size) * a.kv.stride_slot;
-        const uint16_t *row = nullptr;
-        if (is_new)
-            row = (lane < 16 ? a.k_new : a.v_new) + g.b * a.new_stride + (long long)h * D;
-        else if (page >= 0)
-            row = (lane < 16 ? a.kv.k : a.kv.v) + off;
+    // Addresses of the tile at rs into row[to]; page: the entry of slot lane.
+    auto resolve = [&](int page, int to) {
+        const int slot = rs.t * DA_SLOTS + lane;
+        const bool real = slot < rs.n, ok = real && (unsigned)page < (unsigned)a.kv.n_pages;
+        if (lane < DA_SLOTS) {
+            bad |= real && !ok;
+            const long long off = page * a.kv.stride_page + rs.h * a.kv.stride_head +
+                                  (slot - page_index(a.kv, slot) * a.kv.page_size) * a.kv.stride_slot;
+            ulonglong2 at_row;
+            at_row.x = reinterpret_cast<unsigned long long>(ok ? a.kv.k + off : reinterpret_cast<const uint16_t *>(zero_row));
+            at_row.y = reinterpret_cast<unsigned long long>(ok ? a.kv.v + off : reinterpret_cast<const uint16_t *>(zero_row));
+            if (append && slot == rs.n - 1) {
+                const long long src = rs.b * a.new_stride + rs.h * D;
+                at_row.x = reinterpret_cast<unsigned long long>(a.k_new + src);
+                at_row.y = reinterpret_cast<unsigned long long>(a.v_new + src);
+                rings.fresh[fresh_in].off = ok ? off : -1;
+                if (a.new_pos) cp_async4(smem_u32(&rings.fresh[fresh_in].pos), a.new_pos + rs.b);
+            }
+            rings.row[to][lane] = at_row;
+        }
+        turn(fresh_in, S::STAGES + 1);
+        step(rs, resolving);
+    };
+    // Copies the tile of row[from] into a stage: a lane takes 16-byte pieces `piece`, `piece` + LPR, ... of rows r0, r0 + 32 / LPR, ...
+    constexpr int LPR = DA_LANES, PIECES = CPR / LPR;
+    const int piece = lane % LPR, r0 = lane / LPR;
+    auto issue = [&](int from, int stage) {
         const uint32_t st = ring + stage * S::UNIT;
 #pragma unroll
-        for (int j = 0; j < CPR / 2; ++j) {
-            const int i = j * 32 + lane, r = i / CPR, cc = i % CPR;
-            const uint32_t dst = st + r * (D * 2) + ((cc ^ (r & 7)) << 4);
-            const uint16_t *ks = reinterpret_cast<const uint16_t *>(
-                __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), r));
-            const uint16_t *vs = reinterpret_cast<const uint16_t *>(
-                __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), r + 16));
-            cp_async16_or_zero(dst, ks ? ks + cc * 8 : a.kv.k, ks != nullptr);
-            cp_async16_or_zero(dst + DA_SLOTS * D * 2, vs ? vs + cc * 8 : a.kv.v, vs != nullptr);
-        }
-        if (is_new && lane < DA_SLOTS) {  // what is needed to store the row when it has arrived
-            fresh_rows[stage].off = page >= 0 ? off : -1;
-            if (a.new_pos) cp_async4(smem_u32(&fresh_rows[stage].pos), a.new_pos + g.b);
+        for (int x = 0; x < DA_SLOTS * LPR / 32; ++x) {
+            const int r = r0 + x * (32 / LPR);
+            const ulonglong2 p = rings.row[from][r];
+            const uint4 *ks = reinterpret_cast<const uint4 *>(p.x) + piece, *vs = reinterpret_cast<const uint4 *>(p.y) + piece;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const uint32_t dst = st + r * (D * 2) + (((i * LPR + piece) ^ (r & 7)) << 4);
+                cp_async16_at(dst, ks + i * LPR);
+                cp_async16_at(dst + DA_SLOTS * D * 2, vs + i * LPR);
+            }
         }
     };
     // The new token's row joins the cache (nobody reads it there in this call), from the stage it was copied to.
     auto store_new = [&](const Segment &g, int stage) {
-        const long long o = fresh_rows[stage].off;
-        const int r = (g.n - 1) & 15, h = g.hc / chunks;
+        const long long o = rings.fresh[fresh_out].off;
+        const int r = (g.n - 1) & 15;
         if (o >= 0)
             for (int i = lane; i < 2 * CPR; i += 32) {
                 const int cc = i % CPR;
@@ -283,17 +301,16 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (
                 *reinterpret_cast<float4 *>(to) = ld_shared_v4(from);
             }
         if (lane == 0 && a.new_pos && a.kv.positions)
-            a.kv.positions[((long long)g.b * a.kv.hkv + h) * a.kv.cap + g.n - 1] = fresh_rows[stage].pos;
+            a.kv.positions[((long long)g.b * a.kv.hkv + g.h) * a.kv.cap + g.n - 1] = rings.fresh[fresh_out].pos;
     };
     // a row's queries as B operands: head 8 nt + lane / 4, dims 16 ks + 2 (lane % 4) and the next, and 8 further on
     uint32_t qn[Q_AHEAD ? KS : 1][NT][2], qf[KS][NT][2];
     auto load_q = [&](const Segment &g, auto &q_to) {
-        const int h = g.hc / chunks, ch = g.hc - h * chunks;
-        const uint16_t *q = a.q + g.b * a.q_stride + (long long)(h * a.group + ch * HEADS) * D;
+        const uint16_t *q = a.q + g.b * a.q_stride + (long long)(g.h * a.group + g.ch * HEADS) * D;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int j = nt * 8 + (lane >> 2);
-            const bool real = ch * HEADS + j < a.group;
+            const bool real = g.ch * HEADS + j < a.group;
             const uint32_t *src = reinterpret_cast<const uint32_t *>(q + j * D + (lane & 3) * 2);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
@@ -303,28 +320,35 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (
         }
     };
 
-    // The first tiles' pages are looked up before any tile is asked for: one latency, not one for each.
+    // The first tiles' entries are fetched together, before any tile is copied.
+    int to_issue = 0;  // tiles with addresses that have not been copied
     {
-        int pages[S::STAGES - 1];
+        int pages[S::STAGES];
 #pragma unroll
-        for (int s = 0; s < S::STAGES - 1; ++s) {
-            pages[s] = -1;
+        for (int s = 0; s < S::STAGES; ++s)
             if (looking) {
-                const int slot = pg.t * DA_SLOTS + (lane & 15);
-                if (slot < pg.n) pages[s] = *entry(pg, slot);
+                const int slot = pg.t * DA_SLOTS + lane;
+                pages[s] = lane < DA_SLOTS && slot < pg.n ? *entry(pg, slot) : -1;
                 step(pg, looking);
             }
-        }
 #pragma unroll
-        for (int s = 0; s < S::STAGES - 1; ++s) {
-            if (loading) {
-                issue(ld, valid(ld, pages[s]), s);
-                step(ld, loading);
+        for (int s = 0; s < S::STAGES; ++s) {
+            if (resolving) {
+                resolve(pages[s], s & 1);
+                ++to_issue;
             }
-            look_up();
-            cp_async_commit();
+            __syncwarp();
+            if (s < S::STAGES - 1) {
+                if (to_issue > 0) {
+                    issue(s & 1, s);
+                    --to_issue;
+                }
+                look_up();
+                cp_async_commit();
+            }
         }
     }
+    buf = (S::STAGES - 1) & 1;
     int stage_in = S::STAGES - 1, stage = 0;
     if constexpr (Q_AHEAD) load_q(at, qn);
 
@@ -360,17 +384,23 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (
         }
         cp_async_wait<S::STAGES - 2>();
         __syncwarp();  // everybody's copies are there, and everybody is done with the stage that is filled next
-        if (loading) {
-            issue(ld, valid(ld, page_ring[page_out][lane & 15]), stage_in);
-            stage_in = stage_in + 1 == S::STAGES ? 0 : stage_in + 1;
-            page_out = page_out + 1 == S::STAGES ? 0 : page_out + 1;
-            step(ld, loading);
+        if (to_issue > 0) {
+            issue(buf, stage_in);
+            turn(stage_in, S::STAGES);
+            buf ^= 1;
+            --to_issue;
+        }
+        if (resolving) {
+            resolve(lane < DA_SLOTS ? rings.page[page_out][lane] : -1, buf);
+            turn(page_out, S::STAGES);
+            ++to_issue;
         }
         look_up();
         cp_async_commit();
-        if (append && at.t == at.tiles - 1 && at.hc % chunks == 0) store_new(at, stage);
+        if (append && at.t == at.tiles - 1 && at.ch == 0) store_new(at, stage);
+        turn(fresh_out, S::STAGES + 1);
         const uint32_t kst = ring + stage * S::UNIT, vst = kst + DA_SLOTS * D * 2;
-        stage = stage + 1 == S::STAGES ? 0 : stage + 1;
+        turn(stage, S::STAGES);
 
         float s[NT][4];
 #pragma unroll
@@ -391,40 +421,38 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) s[nt][2] = s[nt][3] = -INFINITY;
         if (a.scores) {
-            const int h = at.hc / chunks, ch = at.hc - h * chunks;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int j = ch * HEADS + nt * 8 + (lane & 3) * 2 + e;
+                    const int j = at.ch * HEADS + nt * 8 + (lane & 3) * 2 + e;
                     if (j < a.group) {
-                        float *dst = a.scores + ((long long)at.b * a.hq + h * a.group + j) * a.score_pitch + slot;
+                        float *dst = a.scores + ((long long)at.b * a.hq + at.h * a.group + j) * a.score_pitch + slot;
                         dst[0] = s[nt][e];
                         dst[8] = s[nt][2 + e];
                     }
                 }
         }
-        float mn[NT][2];
+        // m follows the maximum only where a score is above it by more than the slack: what p exceeds 1 by (a factor of 16)
+        // fp32 sums and P's halves have room for, and tiles in which nothing has to be done need no exchange.
         bool grew = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float x = fmaxf(s[nt][e], s[nt][2 + e]);
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-                mn[nt][e] = fmaxf(x, m[nt][e]);
-                grew |= mn[nt][e] > m[nt][e];
-            }
+            for (int e = 0; e < 4; ++e) grew |= s[nt][e] > m[nt][e & 1] + slack;
         if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
+                    float x = fmaxf(s[nt][e], s[nt][2 + e]);
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+                    x = fmaxf(x, m[nt][e]);
                     // (a maximum of -inf goes with a sum of 0: any finite factor will do)
-                    const float f = mn[nt][e] > m[nt][e] ? ex2((m[nt][e] - mn[nt][e]) * c) : 1.f;
-                    m[nt][e] = mn[nt][e];
+                    const float f = x > m[nt][e] ? ex2((m[nt][e] - x) * c) : 1.f;
+                    m[nt][e] = x;
                     l[nt][e] *= f;
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
@@ -484,7 +512,7 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, int (
 __device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }
 // ln of the sum, whose terms carry the factor of P's scale
 template <bool FP16>
-__device__ __forceinline__ float log_sum(float sum) { return logf(FP16 ? sum * 0x1p-14f : sum); }
+__device__ __forceinline__ float log_sum(float sum) { return logf(FP16 ? sum * 0x1p-10f : sum); }
 
 // The list, a stretch a warp.
 template <bool FP16, int D, int NT>
@@ -492,8 +520,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int page_ring[DA_WARPS][S::STAGES][DA_SLOTS];
-    __shared__ FreshRow fresh_rows[DA_WARPS][S::STAGES];
+    __shared__ __align__(16) Rings<S::STAGES> rings[DA_WARPS];
     const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int *first = reinterpret_cast<int *>(smem + S::RING), *len = first + B + 1;
     pdl_launch();
@@ -503,15 +530,15 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
     const int w = warp * gridDim.x + blockIdx.x;  // neighbours in the list on different SMs
     if (count == 0 || w >= workers) return;
     Segment at;
-    if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, HC)) {
+    if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, a.kv.hkv, chunks)) {
         if (lane == 0) a.worker_bad[w] = 0;
         return;
     }
     const bool bad = attend<FP16, D, NT>(
-        a, smem_u32(smem) + warp * S::STAGES * S::UNIT, page_ring[warp], fresh_rows[warp], chunks, at,
-        [&](Segment &g) { return g.next(first, len, B, HC); },
+        a, smem_u32(smem) + warp * S::STAGES * S::UNIT, rings[warp], at,
+        [&](Segment &g) { return g.next(first, len, B, a.kv.hkv, chunks); },
         [&](const Segment &g, int t0, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
-            const int h = g.hc / chunks, ch = g.hc - h * chunks, d0 = lane >> 2;
+            const int h = g.h, ch = g.ch, d0 = lane >> 2;
             const bool whole = t0 == 0 && g.t_end == g.tiles;
             const long long part = (long long)w * 2 + (t0 == 0 ? 1 : 0);  // (a stretch has one row begun before it, and one that goes on)
 #pragma unroll
@@ -564,8 +591,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     constexpr int HEADS = 8 * NT, KS = D / 16, PITCH = D + 4, THREADS = DA_WARPS * 32, D4 = D / 4;
     static_assert(HEADS * PITCH * 4 <= S::STAGES * S::UNIT, "a warp's results lie in its ring");
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int page_ring[DA_WARPS][S::STAGES][DA_SLOTS];
-    __shared__ FreshRow fresh_rows[DA_WARPS][S::STAGES];
+    __shared__ __align__(16) Rings<S::STAGES> rings[DA_WARPS];
     __shared__ float2 warp_ml[DA_WARPS][HEADS], row_ml[HEADS];
     __shared__ __align__(8) float2 every[DA_CLUSTER][HEADS];  // maximum and sum of each CTA
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -585,12 +611,13 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     }
     cluster_arrive();  // (this CTA runs: others may store into its shared memory)
     const int b = row / a.kv.hkv, h = row - b * a.kv.hkv, n = attended(a, b), G = a.group;
-    const float c = a.scale * 1.4426950408889634f, shift = FP16 ? 14.f : 0.f;
+    const float c = a.scale * 1.4426950408889634f, shift = FP16 ? DA_FP16_SHIFT : 0.f;
     uint8_t *ring = smem + warp * S::STAGES * S::UNIT;
     float *mine = reinterpret_cast<float *>(ring), *got = reinterpret_cast<float *>(smem + S::RING);  // got[C][own pieces][4]
     Segment at;
     at.b = b;
-    at.hc = h;
+    at.h = h;
+    at.ch = 0;
     at.n = n;
     at.tiles = (n + DA_SLOTS - 1) / DA_SLOTS;
     const int w = rank * DA_WARPS + warp, W = C * DA_WARPS;
@@ -601,7 +628,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     if (a.accumulate && slot0 + lane * 32 < slot1) prefetch_l2(wt + slot0 + lane * 32);
     if (at.t < at.t_end) {
         attend<FP16, D, NT>(
-            a, smem_u32(ring), page_ring[warp], fresh_rows[warp], 1, at, [&](Segment &) { return false; },
+            a, smem_u32(ring), rings[warp], at, [&](Segment &) { return false; },
             [&](const Segment &, int, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
                 cp_async_wait_all();
                 __syncwarp();  // (the ring is free)
@@ -720,12 +747,12 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
         // weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0
         const int ctas = gridDim.x - join_ctas, me = blockIdx.x - join_ctas, all = first[B] * a.kv.hkv;
         float2 *ml = reinterpret_cast<float2 *>(fac);
-        const float shift = FP16 ? 14.f : 0.f;
+        const float shift = FP16 ? DA_FP16_SHIFT : 0.f;
         Segment at;
-        bool going = all > 0 && at.seek(first_of(me, all, ctas), first_of(me + 1, all, ctas), first, len, B, a.kv.hkv);
+        bool going = all > 0 && at.seek(first_of(me, all, ctas), first_of(me + 1, all, ctas), first, len, B, a.kv.hkv, 1);
         constexpr int STEP = DJ_THREADS * DJ_SLOTS;
         float have[DJ_SLOTS];
-        auto weights_at = [&]() { return a.kv.weights + ((long long)at.b * a.kv.hkv + at.hc) * a.kv.cap; };
+        auto weights_at = [&]() { return a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap; };
         auto load_weights = [&](int s0, int s1) {
             const int fresh = a.k_new ? at.n - 1 : -1;
             const float *wt = weights_at();
@@ -743,10 +770,10 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
             for (int g = warp; g < a.group; g += DJ_THREADS / 32) {  // a warp a head
                 const int ch = g / HEADS, j = g - ch * HEADS;
                 int w0;
-                const int nw = span(at.b, at.hc, ch, &w0);
+                const int nw = span(at.b, at.h, ch, &w0);
                 if (nw == 1) {
                     if (lane == 0) {
-                        const float2 x = a.row_ml[(long long)at.b * a.hq + at.hc * a.group + g];
+                        const float2 x = a.row_ml[(long long)at.b * a.hq + at.h * a.group + g];
                         ml[g] = make_float2(x.x == -INFINITY ? 0.f : x.x, x.y);
                     }
                     continue;
@@ -767,7 +794,7 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
                 if (lane == 0) ml[g] = make_float2(mu, inverse(l));
             }
             __syncthreads();
-            const float *sc = a.scores + ((long long)at.b * a.hq + at.hc * a.group) * a.score_pitch;
+            const float *sc = a.scores + ((long long)at.b * a.hq + at.h * a.group) * a.score_pitch;
             float *wt = weights_at();
             for (int s = s0; s < s1; s += STEP) {
                 if (!begun || s != s0) load_weights(s, s1);
@@ -787,7 +814,7 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
                     if (slot < s1) wt[slot] = have[i] + sum[i];
                 }
             }
-            going = at.next(first, len, B, a.kv.hkv);
+            going = at.next(first, len, B, a.kv.hkv, 1);
         }
         return;
     }

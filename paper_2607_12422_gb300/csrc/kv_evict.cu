@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
     const int pieces = a.kv.d / 8, lg = 31 - __clz(pieces);
     const int *table = a.kv.table + (long long)b * a.kv.max_pages;
     auto place = [&](int slot) {  // -1: no such page
-        const int q = slot / a.kv.page_size, p = table[q];
+        const int q = page_index(a.kv, slot), p = table[q];
         if ((unsigned)p >= (unsigned)a.kv.n_pages) return -1ll;
         return (long long)p * a.kv.stride_page + h * a.kv.stride_head + (long long)(slot - q * a.kv.page_size) * a.kv.stride_slot;
     };

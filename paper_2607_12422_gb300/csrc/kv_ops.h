@@ -16,7 +16,14 @@ struct KvView {
     int *positions;
     long long cap;  // slots of a sequence: max_pages * page_size
     int n_pages, page_size, hkv, d, B, max_pages;
+    uint32_t page_mul, page_shift;  // slot / page_size = slot * page_mul >> page_shift for slots below 2^30
 };
+
+#ifdef __CUDACC__
+__device__ __forceinline__ int page_index(const KvView &kv, int slot) {
+    return (int)((unsigned long long)(uint32_t)slot * kv.page_mul >> kv.page_shift);
+}
+#endif
 
 constexpr int KV_MAX_WORKERS = 2048;  // warps that share a call's units
 constexpr int KV_MAX_BATCH = 1024;  // sequences of a call: their lengths and first tiles lie in shared memory
