@@ -116,10 +116,12 @@ __device__ __forceinline__ int attended(const DecodeArgs &a, int b) {
     return (int)max(0ll, min((long long)a.kv.lens[b], most)) + add;
 }
 
-// The list of all tiles.  A (sequence, KV head, chunk of its query heads) is a row; it counts as its tiles and DA_ROW_TILES
-// more in front, so that stretches with many short rows are shorter.  first[b]: the count of one row of each
-// sequence before b; len[b]: slots attended to.  Whole CTA.
-__device__ __forceinline__ int row_count(int n) { return n > 0 ? (n + DA_SLOTS - 1) / DA_SLOTS + DA_ROW_TILES : 0; }
+// The list of all tiles.  A (sequence, KV head, chunk of its query heads) is a row; it counts as its tiles and ROW more in
+// front, so that stretches with many short rows are shorter.  first[b]: the count of one row of each sequence
+// before b; len[b]: slots attended to.  Whole CTA.
+template <int ROW>
+__device__ __forceinline__ int row_count(int n) { return n > 0 ? (n + DA_SLOTS - 1) / DA_SLOTS + ROW : 0; }
+template <int ROW>
 __device__ __forceinline__ void tile_lists(const DecodeArgs &a, int *first, int *len) {
     __shared__ int warp_sum[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
@@ -128,7 +130,7 @@ __device__ __forceinline__ void tile_lists(const DecodeArgs &a, int *first, int 
         const int b = b0 + threadIdx.x;
         const int n = b < a.kv.B ? attended(a, b) : 0;
         if (b < a.kv.B) len[b] = n;
-        int x = row_count(n);
+        int x = row_count<ROW>(n);
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
@@ -156,13 +158,14 @@ __device__ __forceinline__ int first_of(int w, int count, int workers) { return 
 __device__ __forceinline__ int worker_at(long long at, int count, int workers) { return (int)(((at + 1) * workers - 1) / count); }
 
 // Tiles [t, t_end) of one row: what a warp works on before it leaves the row.
+template <int ROW>
 struct Segment {
     int b, h, ch, t, t_end, tiles, n;  // sequence, KV head, chunk of its query heads, the row's tiles and slots
     int at, end;                    // list place of the row, end of the warp's stretch
     __device__ __forceinline__ bool clip(const int *len) {
         n = len[b];
         tiles = (n + DA_SLOTS - 1) / DA_SLOTS;
-        t_end = min(tiles, end - at - DA_ROW_TILES);
+        t_end = min(tiles, end - at - ROW);
         return t < t_end;
     }
     // The first segment of the stretch [u, end); false if it has none.
@@ -184,7 +187,7 @@ struct Segment {
         h = hc / chunks;
         ch = hc - h * chunks;
         at = first[b] * HC + hc * per;
-        t = max(0, u - at - DA_ROW_TILES);
+        t = max(0, u - at - ROW);
         return clip(len) || next(first, len, B, hkv, chunks);
     }
     __device__ __forceinline__ bool next(const int *first, const int *len, int B, int hkv, int chunks) {
@@ -213,12 +216,14 @@ struct Rings {
     int page[STAGES][DA_SLOTS];  // the table's entries
 };
 
+using Tiles = Segment<DA_ROW_TILES>;
+
 // A warp's work on its segments: `next(segment)` makes the following one of it, `leave(segment, t0, m, l, o)` takes the
 // results of tiles [t0, t_end) of a row: maxima and sums (a lane's own part of them) of heads 8 nt + 2 (lane % 4) + e, and outputs
 // o[ks][nt]: dims 16 ks + lane / 4 (+ 8 in elements 2 and 3) of those heads.
 // Returns whether a page was outside the cache.
 template <bool FP16, int D, int NT, typename Next, typename Leave>
-__device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings<DaShape<D>::STAGES> &rings, Segment at, Next &&next,
+__device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings<DaShape<D>::STAGES> &rings, Tiles at, Next &&next,
                                        Leave &&leave) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, CPR = D / 8;  // heads of a chunk, k steps, 16-byte pieces of a row
@@ -233,14 +238,14 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
     // fetched, STAGES - 1 tiles before they are used; rows' addresses are made of them, by a lane a row; the rows are copied, STAGES - 1
     // tiles before they are multiplied.  (Warps are few, so a step's instructions and waits count: with addresses handed
     // round by shuffles and entries waited for, 64 ragged sequences of d = 64 took 40 us instead of 28.)
-    Segment rs = at, pg = at;  // the next tile whose addresses are made, and whose entries are fetched
+    Tiles rs = at, pg = at;  // the next tile whose addresses are made, and whose entries are fetched
     bool resolving = true, looking = true, bad = false;
     int page_in = 0, page_out = 0, buf = 0, fresh_in = 0, fresh_out = 0;
     auto turn = [](int &i, int n) { i = i + 1 == n ? 0 : i + 1; };
-    auto step = [&](Segment &g, bool &more) {
+    auto step = [&](Tiles &g, bool &more) {
         if (++g.t == g.t_end) more = next(g);
     };
-    auto entry = [&](const Segment &g, int slot) { return a.kv.table + (long long)g.b * a.kv.max_pages + page_index(a.kv, slot); };
+    auto entry = [&](const Tiles &g, int slot) { return a.kv.table + (long long)g.b * a.kv.max_pages + page_index(a.kv, slot); };
     auto look_up = [&]() {
         if (!looking) return;
         const int slot = pg.t * DA_SLOTS + lane;
@@ -290,7 +295,7 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
         }
     };
     // The new token's row joins the cache (nobody reads it there in this call), from the stage it was copied to.
-    auto store_new = [&](const Segment &g, int stage) {
+    auto store_new = [&](const Tiles &g, int stage) {
         const long long o = rings.fresh[fresh_out].off;
         const int r = (g.n - 1) & 15;
         if (o >= 0)
@@ -305,7 +310,7 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
     };
     // a row's queries as B operands: head 8 nt + lane / 4, dims 16 ks + 2 (lane % 4) and the next, and 8 further on
     uint32_t qn[Q_AHEAD ? KS : 1][NT][2], qf[KS][NT][2];
-    auto load_q = [&](const Segment &g, auto &q_to) {
+    auto load_q = [&](const Tiles &g, auto &q_to) {
         const uint16_t *q = a.q + g.b * a.q_stride + (long long)(g.h * a.group + g.ch * HEADS) * D;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -376,7 +381,7 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) qf[ks][nt][0] = qn[ks][nt][0], qf[ks][nt][1] = qn[ks][nt][1];
-                Segment after = at;
+                Tiles after = at;
                 if (next(after)) load_q(after, qn);
             } else {
                 load_q(at, qf);
@@ -524,20 +529,20 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
     const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int *first = reinterpret_cast<int *>(smem + S::RING), *len = first + B + 1;
     pdl_launch();
-    tile_lists(a, first, len);
+    tile_lists<DA_ROW_TILES>(a, first, len);
     const int chunks = (a.group + HEADS - 1) / HEADS, HC = a.kv.hkv * chunks;
     const int count = first[B] * HC, workers = workers_of(a, count);
     const int w = warp * gridDim.x + blockIdx.x;  // neighbours in the list on different SMs
     if (count == 0 || w >= workers) return;
-    Segment at;
+    Tiles at;
     if (!at.seek(first_of(w, count, workers), first_of(w + 1, count, workers), first, len, B, a.kv.hkv, chunks)) {
         if (lane == 0) a.worker_bad[w] = 0;
         return;
     }
     const bool bad = attend<FP16, D, NT>(
         a, smem_u32(smem) + warp * S::STAGES * S::UNIT, rings[warp], at,
-        [&](Segment &g) { return g.next(first, len, B, a.kv.hkv, chunks); },
-        [&](const Segment &g, int t0, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
+        [&](Tiles &g) { return g.next(first, len, B, a.kv.hkv, chunks); },
+        [&](const Tiles &g, int t0, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
             const int h = g.h, ch = g.ch, d0 = lane >> 2;
             const bool whole = t0 == 0 && g.t_end == g.tiles;
             const long long part = (long long)w * 2 + (t0 == 0 ? 1 : 0);  // (a stretch has one row begun before it, and one that goes on)
@@ -614,7 +619,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     const float c = a.scale * 1.4426950408889634f, shift = FP16 ? DA_FP16_SHIFT : 0.f;
     uint8_t *ring = smem + warp * S::STAGES * S::UNIT;
     float *mine = reinterpret_cast<float *>(ring), *got = reinterpret_cast<float *>(smem + S::RING);  // got[C][own pieces][4]
-    Segment at;
+    Tiles at;
     at.b = b;
     at.h = h;
     at.ch = 0;
@@ -628,8 +633,8 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     if (a.accumulate && slot0 + lane * 32 < slot1) prefetch_l2(wt + slot0 + lane * 32);
     if (at.t < at.t_end) {
         attend<FP16, D, NT>(
-            a, smem_u32(ring), rings[warp], at, [&](Segment &) { return false; },
-            [&](const Segment &, int, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
+            a, smem_u32(ring), rings[warp], at, [&](Tiles &) { return false; },
+            [&](const Tiles &, int, const float (&m)[NT][2], const float (&l)[NT][2], const float (&o)[KS][NT][4]) {
                 cp_async_wait_all();
                 __syncwarp();  // (the ring is free)
 #pragma unroll
@@ -713,24 +718,29 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     }
 }
 
-constexpr int DJ_THREADS = 256;
-constexpr int DJ_SLOTS = 8;  // of a thread that adds weights, at a time
+constexpr int DJ_THREADS = 256, DJ_CTAS = 2;
+constexpr int DJ_SLOTS = 8;   // of a thread that adds weights, at a time
+constexpr int DJ_HEADS = 32;  // whose maxima and sums a CTA has at hand
 
 // Joins what several warps left of a row: out = sum_w f_w o_w / sum_w f_w l_w, f_w = exp(scale (m_w - max)).  TEAM threads a
 // query head: the CTA where many warps share a row, a warp where rows are many.  Sequences without a slot get
-// zeros.  The CTAs behind `join_ctas` add the weights: each takes a stretch of the list of [sequence][KV head][tile], and maximum
-// and sum of its heads from the warps' again.  One CTA an SM finds room beside k_decode_split's, so all that does
-// not depend on it is done when it ends.
+// zeros.  A CTA an SM finds room beside k_decode_split's, so that all that does not depend on it is done when it ends.
+// With TEAM = DJ_THREADS the CTAs behind `join_ctas` add the weights: each takes a stretch of the list of [sequence][KV head]
+// [tile], and maxima and sums of its heads from the warps' again, so that it need not wait for the join (131071 tokens: 8 us
+// longer than without weights; with k_decode_weights 11.  For 64 ragged sequences it is the other way round: rows
+// cost a whole CTA 3 us each, 112 us and 12.)
 template <bool FP16, int D, int NT, int TEAM>
 __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, int join_ctas) {
     constexpr int HEADS = 8 * NT, TEAMS = DJ_THREADS / TEAM, L = D / 4 < TEAM ? D / 4 : TEAM, V = D / 4 / L, G = TEAM / L;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float red[2][DJ_THREADS / 32];
     __shared__ float4 sum_o[TEAM > 32 ? DJ_THREADS : 1];
+    __shared__ float2 ml[TEAM > 32 ? DJ_HEADS : 1];
     const int B = a.kv.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int *first = reinterpret_cast<int *>(smem), *len = first + B + 1;
-    float *fac = reinterpret_cast<float *>(smem + (8 * B + 4 + 7) / 8 * 8);  // [TEAMS][workers], or maxima and inverse sums of a group
-    tile_lists(a, first, len);
+    float *fac = reinterpret_cast<float *>(len + B);  // [TEAMS][workers]
+    pdl_launch();
+    tile_lists<DA_ROW_TILES>(a, first, len);
     const int chunks = (a.group + HEADS - 1) / HEADS, HC = a.kv.hkv * chunks;
     const int count = first[B] * HC, workers = workers_of(a, count);
     const float c = a.scale * 1.4426950408889634f;
@@ -743,79 +753,76 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
     };
     auto part_at = [&](int w0, int i, int j) { return ((long long)(w0 + i) * 2 + (i == 0)) * HEADS + j; };
 
-    if ((int)blockIdx.x >= join_ctas) {
+    if (TEAM > 32 && (int)blockIdx.x >= join_ctas) {
         // weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0
         const int ctas = gridDim.x - join_ctas, me = blockIdx.x - join_ctas, all = first[B] * a.kv.hkv;
-        float2 *ml = reinterpret_cast<float2 *>(fac);
         const float shift = FP16 ? DA_FP16_SHIFT : 0.f;
-        Segment at;
-        bool going = all > 0 && at.seek(first_of(me, all, ctas), first_of(me + 1, all, ctas), first, len, B, a.kv.hkv, 1);
+        Tiles at;
+        if (all == 0 || !at.seek(first_of(me, all, ctas), first_of(me + 1, all, ctas), first, len, B, a.kv.hkv, 1)) return;
         constexpr int STEP = DJ_THREADS * DJ_SLOTS;
         float have[DJ_SLOTS];
-        auto weights_at = [&]() { return a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap; };
-        auto load_weights = [&](int s0, int s1) {
-            const int fresh = a.k_new ? at.n - 1 : -1;
-            const float *wt = weights_at();
+        auto load_weights = [&](int s0, int s1, int fresh) {
+            const float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
 #pragma unroll
             for (int i = 0; i < DJ_SLOTS; ++i) {
                 const int slot = s0 + i * DJ_THREADS + tid;
                 have[i] = slot < s1 && slot != fresh ? wt[slot] : 0.f;
             }
         };
-        if (going) load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS));  // (no kernel of this call has written them)
+        load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS), a.k_new ? at.n - 1 : -1);  // (no kernel of this call has written them)
         pdl_wait();
-        for (bool begun = true; going; begun = false) {
+        bool begun = true;
+        do {
             const int s0 = at.t * DA_SLOTS, s1 = min(at.n, at.t_end * DA_SLOTS);
-            __syncthreads();  // (ml of the row before has been read)
-            for (int g = warp; g < a.group; g += DJ_THREADS / 32) {  // a warp a head
-                const int ch = g / HEADS, j = g - ch * HEADS;
-                int w0;
-                const int nw = span(at.b, at.h, ch, &w0);
-                if (nw == 1) {
-                    if (lane == 0) {
-                        const float2 x = a.row_ml[(long long)at.b * a.hq + at.h * a.group + g];
-                        ml[g] = make_float2(x.x == -INFINITY ? 0.f : x.x, x.y);
+            float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
+            for (int g0 = 0; g0 < a.group; g0 += DJ_HEADS) {
+                const int heads = min(DJ_HEADS, a.group - g0);
+                __syncthreads();  // (ml of the heads before has been read)
+                for (int g = warp; g < heads; g += DJ_THREADS / 32) {  // a warp a head
+                    const int ch = (g0 + g) / HEADS, j = g0 + g - ch * HEADS;
+                    int w0;
+                    const int nw = span(at.b, at.h, ch, &w0);
+                    float m = -INFINITY, l = 0.f;
+                    if (nw == 1) {
+                        if (lane == 0) ml[g] = a.row_ml[(long long)at.b * a.hq + at.h * a.group + g0 + g];
+                        continue;
                     }
-                    continue;
-                }
-                float m = -INFINITY, l = 0.f;
 #pragma unroll 5
-                for (int i = lane; i < nw; i += 32) {
-                    const float2 x = a.part_ml[part_at(w0, i, j)];
-                    const float mx = fmaxf(m, x.x), mu = mx == -INFINITY ? 0.f : mx;
-                    l = l * ex2((m - mu) * c) + x.y * ex2((x.x - mu) * c);
-                    m = mx;
+                    for (int i = lane; i < nw; i += 32) {
+                        const float2 x = a.part_ml[part_at(w0, i, j)];
+                        const float mx = fmaxf(m, x.x), mu = mx == -INFINITY ? 0.f : mx;
+                        l = l * ex2((m - mu) * c) + x.y * ex2((x.x - mu) * c);
+                        m = mx;
+                    }
+                    float mx = m;
+                    for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
+                    l *= ex2((m - (mx == -INFINITY ? 0.f : mx)) * c);
+                    for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+                    if (lane == 0) ml[g] = make_float2(mx, inverse(l));
                 }
-                float mx = m;
-                for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-                const float mu = mx == -INFINITY ? 0.f : mx;
-                l *= ex2((m - mu) * c);
-                for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-                if (lane == 0) ml[g] = make_float2(mu, inverse(l));
-            }
-            __syncthreads();
-            const float *sc = a.scores + ((long long)at.b * a.hq + at.h * a.group) * a.score_pitch;
-            float *wt = weights_at();
-            for (int s = s0; s < s1; s += STEP) {
-                if (!begun || s != s0) load_weights(s, s1);
-                float sum[DJ_SLOTS] = {};
+                __syncthreads();
+                const float *sc = a.scores + ((long long)at.b * a.hq + at.h * a.group + g0) * a.score_pitch;
+                for (int s = s0; s < s1; s += STEP) {
+                    if (!begun || s != s0 || g0 != 0) load_weights(s, s1, a.k_new && g0 == 0 ? at.n - 1 : -1);
+                    float sum[DJ_SLOTS] = {};
 #pragma unroll 2
-                for (int g = 0; g < a.group; ++g) {
-                    const float2 x = ml[g];
+                    for (int g = 0; g < heads; ++g) {
+                        const float m = ml[g].x == -INFINITY ? 0.f : ml[g].x, inv = ml[g].y;
+#pragma unroll
+                        for (int i = 0; i < DJ_SLOTS; ++i) {
+                            const int slot = s + i * DJ_THREADS + tid;
+                            if (slot < s1) sum[i] += ex2((sc[g * a.score_pitch + slot] - m) * c + shift) * inv;
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < DJ_SLOTS; ++i) {
                         const int slot = s + i * DJ_THREADS + tid;
-                        if (slot < s1) sum[i] += ex2((sc[g * a.score_pitch + slot] - x.x) * c + shift) * x.y;
+                        if (slot < s1) wt[slot] = have[i] + sum[i];
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < DJ_SLOTS; ++i) {
-                    const int slot = s + i * DJ_THREADS + tid;
-                    if (slot < s1) wt[slot] = have[i] + sum[i];
-                }
             }
-            going = at.next(first, len, B, a.kv.hkv, 1);
-        }
+            begun = false;
+        } while (at.next(first, len, B, a.kv.hkv, 1));
         return;
     }
 
@@ -931,8 +938,83 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
                 r.y = pack2<FP16>(acc[v].z * inv, acc[v].w * inv);
                 *reinterpret_cast<uint2 *>(a.out + (long long)row * D + (v * L + d4) * 4) = r;
             }
-        if (me == 0 && a.lse) a.lse[row] = mx * a.scale + log_sum<FP16>(sum);
+        if (me == 0) {
+            a.row_ml[row] = make_float2(mx, inv);
+            if (a.lse) a.lse[row] = mx * a.scale + log_sum<FP16>(sum);
+        }
     }
+}
+
+constexpr int DW_THREADS = 256, DW_CTAS = 4;
+constexpr int DW_ROW_TILES = 16;  // what a row costs a warp here, in tiles
+constexpr int DW_VECS = 2;        // float4 of a lane and head at a time
+
+// weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0.  A warp a stretch of a
+// list of [sequence][KV head][tile].  For many rows; where rows are few and long, CTAs of k_decode_join do it.
+template <bool FP16>
+__global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs a) {
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int B = a.kv.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int *first = reinterpret_cast<int *>(smem), *len = first + B + 1;
+    tile_lists<DW_ROW_TILES>(a, first, len);
+    const int all = first[B] * a.kv.hkv, warps = gridDim.x * (DW_THREADS / 32), w = warp * gridDim.x + blockIdx.x;
+    const float c = a.scale * 1.4426950408889634f, shift = FP16 ? DA_FP16_SHIFT : 0.f;
+    Segment<DW_ROW_TILES> at;
+    if (all == 0 || !at.seek(first_of(w, all, warps), first_of(w + 1, all, warps), first, len, B, a.kv.hkv, 1)) return;
+    constexpr int STEP = 128 * DW_VECS;
+    float have[DW_VECS][4];
+    auto load_weights = [&](int s0, int s1, int fresh) {
+        const float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
+#pragma unroll
+        for (int v = 0; v < DW_VECS; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int slot = s0 + v * 128 + lane * 4 + i;
+                have[v][i] = slot < s1 && slot != fresh ? wt[slot] : 0.f;
+            }
+    };
+    load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS), a.k_new ? at.n - 1 : -1);  // (no kernel of this call has written them)
+    pdl_wait();
+    bool begun = true;
+    do {
+        const int s0 = at.t * DA_SLOTS, s1 = min(at.n, at.t_end * DA_SLOTS);
+        float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
+        for (int g0 = 0; g0 < a.group; g0 += 32) {
+            const int heads = min(32, a.group - g0);
+            const long long row = (long long)at.b * a.hq + at.h * a.group + g0;
+            float2 ml = make_float2(0.f, 0.f);  // maximum and inverse sum of head g0 + lane
+            if (lane < heads) ml = a.row_ml[row + lane];
+            if (ml.x == -INFINITY) ml.x = 0.f;
+            for (int s = s0; s < s1; s += STEP) {
+                if (!begun || s != s0 || g0 != 0) load_weights(s, s1, a.k_new && g0 == 0 ? at.n - 1 : -1);
+                float sum[DW_VECS][4] = {};
+#pragma unroll 4
+                for (int g = 0; g < heads; ++g) {
+                    const float *sc = a.scores + (row + g) * a.score_pitch;  // (16-byte aligned; whole tiles can be read)
+                    const float m = __shfl_sync(0xffffffffu, ml.x, g), inv = __shfl_sync(0xffffffffu, ml.y, g);
+#pragma unroll
+                    for (int v = 0; v < DW_VECS; ++v) {
+                        const int slot = s + v * 128 + lane * 4;
+                        if (slot < s1) {
+                            const float4 x = *reinterpret_cast<const float4 *>(sc + slot);
+                            sum[v][0] += ex2((x.x - m) * c + shift) * inv;
+                            sum[v][1] += ex2((x.y - m) * c + shift) * inv;
+                            sum[v][2] += ex2((x.z - m) * c + shift) * inv;
+                            sum[v][3] += ex2((x.w - m) * c + shift) * inv;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int v = 0; v < DW_VECS; ++v)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int slot = s + v * 128 + lane * 4 + i;
+                        if (slot < s1) wt[slot] = have[v][i] + sum[v][i];
+                    }
+            }
+        }
+        begun = false;
+    } while (at.next(first, len, B, a.kv.hkv, 1));
 }
 
 // Kernel attributes, set for the current device before any launch there; *done is the device they were last set for.
@@ -943,6 +1025,8 @@ cudaError_t configure(K *kernel, size_t smem, int *done, int *most_cluster = nul
     if (e != cudaSuccess || *done == dev) return e;
     const void *f = reinterpret_cast<const void *>(kernel);
     e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (kernels with another division of an SM's memory do not run beside each other)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e == cudaSuccess && most_cluster) {
         e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e == cudaSuccess) *most_cluster = largest_cluster(f, DA_WARPS * 32, smem, DA_CLUSTER) < DA_CLUSTER ? 8 : DA_CLUSTER;
@@ -954,13 +1038,18 @@ cudaError_t configure(K *kernel, size_t smem, int *done, int *most_cluster = nul
 template <bool FP16, int D, int NT, int TEAM>
 cudaError_t launch_join(DecodeArgs &a, cudaStream_t st) {
     static thread_local int done = -1;
-    const size_t lists = (2 * (size_t)a.kv.B + 1) * 4, most = (2 * KV_MAX_BATCH + 3) * 4 + std::max((DJ_THREADS / TEAM) * KV_MAX_WORKERS * 4, 4096 * 8);
-    const size_t facs = std::max((size_t)(DJ_THREADS / TEAM) * a.workers * 4, (size_t)a.group * 8);
+    const size_t lists = (2 * (size_t)a.kv.B + 1) * 4, most = (2 * KV_MAX_BATCH + 1 + (DJ_THREADS / TEAM) * KV_MAX_WORKERS) * 4;
+    const size_t facs = (size_t)(DJ_THREADS / TEAM) * a.workers * 4;
     cudaError_t e = configure(k_decode_join<FP16, D, NT, TEAM>, most, &done);
     if (e != cudaSuccess) return e;
     const int teams = DJ_THREADS / TEAM, rows = a.kv.B * a.hq, sms = gemm_ctas();
-    const int join = std::min((rows + teams - 1) / teams, a.accumulate ? sms / 2 : sms), grid = a.accumulate ? sms : join;
-    return launch_pdl(k_decode_join<FP16, D, NT, TEAM>, grid, DJ_THREADS, (lists + 7) / 8 * 8 + facs, st, a, join);
+    const bool inside = TEAM > 32 && a.accumulate;
+    const int join = std::min((rows + teams - 1) / teams, inside ? sms / 2 : sms * DJ_CTAS);
+    e = launch_pdl(k_decode_join<FP16, D, NT, TEAM>, inside ? sms * DJ_CTAS : join, DJ_THREADS, lists + facs, st, a, join);
+    if (e != cudaSuccess || !a.accumulate || inside) return e;
+    static thread_local int done_w = -1;
+    if ((e = configure(k_decode_weights<FP16>, (2 * KV_MAX_BATCH + 1) * 4, &done_w)) != cudaSuccess) return e;
+    return launch_pdl(k_decode_weights<FP16>, sms * DW_CTAS, DW_THREADS, lists, st, a);
 }
 
 // CTAs of a (sequence, KV head)'s cluster, or 0 where the list of tiles is the better way: clusters where all of them run at
@@ -1036,7 +1125,7 @@ bool decode_plan(const KvView &kv, int hq, bool accumulate, DecodePlan *p) {
     p->scores = take(accumulate ? (size_t)kv.B * hq * p->score_pitch * sizeof(float) : 0);
     p->total = off;
     // places of the list are counted in 32 bits
-    return (long long)kv.B * ((kv.cap + DA_SLOTS - 1) / DA_SLOTS + DA_ROW_TILES) * kv.hkv * ((group + heads - 1) / heads) < (1ll << 31);
+    return (long long)kv.B * ((kv.cap + DA_SLOTS - 1) / DA_SLOTS + DW_ROW_TILES) * kv.hkv * ((group + heads - 1) / heads) < (1ll << 31);
 }
 
 cudaError_t launch_decode_attention(DecodeArgs &a, cudaStream_t st) {
