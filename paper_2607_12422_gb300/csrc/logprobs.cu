@@ -4,11 +4,13 @@
 //     logprob(t) = (x_t - m) / T - ln S
 //     entropy    = ln S + sum (m - x) / T exp((x - m) / T) / S      (both terms >= 0: nothing cancels)
 //     top k      by value, then by the lower index
-// in one pass over the logits, which bounds it: running maximum and sums in fp32 per thread, joined at the end.  Few
-// rows are cut into slices: a cluster of CTAs a row, whose parts are joined through distributed shared memory.
+// in one pass over the logits, which bounds it: running maximum and sums in fp32 per thread, joined at the end.  A CTA
+// streams 16-KB tiles of its rows through a ring in shared memory, filled by bulk copies that run ahead into the next row while
+// it finishes one.  Few rows are cut into slices: a cluster of CTAs a row, whose parts are joined through distributed
+// shared memory.
 //
-// The alternatives come from the same pass at the price of one store for 64 bytes of logits: the maximum of each group of
-// 64 bytes stays in shared memory.  The k best values lie in the k groups of largest maxima (k values, those maxima,
+// The alternatives come from the same pass at the price of one store for 128 bytes of logits: the maximum of each group of
+// 128 bytes stays in shared memory.  The k best values lie in the k groups of largest maxima (k values, those maxima,
 // already reach the k-th of them), so at the end k groups are picked and read again.  Groups are contiguous, so that among
 // equal maxima the lower group holds the lower ids.  However the values are ordered, the work is the same.
 #include <algorithm>
@@ -24,11 +26,13 @@ namespace {
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
 constexpr int LP_VECS = 4;                        // 16-byte loads of a thread and tile
 constexpr int LP_TILE = LP_THREADS * LP_VECS;     // vectors of a tile
-constexpr int LP_TILE_MAX = 4 * 72;               // floats that hold their maxima: four rows of 64, padded for the banks
-constexpr int LP_SEGMENT = 40;                    // tiles whose maxima are kept at a time: 46 KB
+constexpr int LP_STAGES = 2, LP_CTAS = 3;         // tiles of the ring, CTAs of an SM: 96 KB on their way to it
+constexpr int LP_GROUP = 8;                       // vectors of a group
+constexpr int LP_TILE_MAX = 4 * 40;               // floats that hold a tile's maxima: four rows of 32, padded for the banks
+constexpr int LP_SEGMENT = 40;                    // tiles whose maxima are kept at a time: 26 KB
 constexpr int LP_CLUSTER = 16;                    // slices of a row at most
 constexpr int LP_BINS = 64;                       // of the selections below
-constexpr int LP_LIST = 2048;                     // keys of a list; 32 groups of 32 values need 1024
+constexpr int LP_LIST = 512;                      // keys of a list: ten times what an order at random needs (bin_bound)
 constexpr float LP_FLOOR = -1000.f;               // 2^-1000 is 0 in fp32
 
 typedef unsigned long long u64;
@@ -45,15 +49,16 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return r;
 }
 
-// (value, lower index first) as one number; NaN below everything, 0 is nobody's
-__device__ __forceinline__ u64 lp_key(float x, int i) {
+// Order of values as a number: NaN (1) below everything, 0 is nobody's.
+__device__ __forceinline__ uint32_t lp_order(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);  // (-0 counts as 0)
-    const uint32_t v = x != x ? 0u : (u & 0x80000000u ? ~u : u | 0x80000000u);
-    return (u64)v << 32 | (uint32_t)~i;
+    return x != x ? 1u : (u & 0x80000000u ? ~u : u | 0x80000000u);
 }
+// (value, lower index first) as one number
+__device__ __forceinline__ u64 lp_key(uint32_t order, int i) { return (u64)order << 32 | (uint32_t)~i; }
 __device__ __forceinline__ float key_value(u64 k) {
     const uint32_t v = (uint32_t)(k >> 32);
-    return v == 0 ? __uint_as_float(0x7fffffffu) : __uint_as_float(v & 0x80000000u ? v & 0x7fffffffu : ~v);
+    return v <= 1 ? __uint_as_float(0x7fffffffu) : __uint_as_float(v & 0x80000000u ? v & 0x7fffffffu : ~v);
 }
 __device__ __forceinline__ int key_index(u64 k) { return (int)~(uint32_t)k; }
 
@@ -123,23 +128,25 @@ struct Shared {
     int count;
 };
 
-// A lower bound of the k-th largest of all keys, from each thread's largest (0: none): the k-th largest of the maxima of 64
-// bins of threads, which k keys reach; 0 if fewer bins have one.  With keys in any order some k ln(64 / (64 - k)) / (k / 64)
-// of them reach it: 44 for k = 32.  Whole CTA.
-__device__ __forceinline__ u64 bin_bound(u64 mine, int k, Shared &s) {
+// A lower bound of the k-th largest of all keys, from each thread's largest (0: none), threads numbered by `id`: the k-th
+// largest of the maxima of 64 bins of threads, which k keys reach; 0 if fewer bins have one.  Of keys in any order some
+// 64 ln(64 / (64 - k)) reach it: 44 for k = 32.  Whole CTA.
+__device__ __forceinline__ u64 bin_bound(u64 mine, int id, int k, Shared &s) {
     __syncthreads();
-    s.pool[threadIdx.x] = mine;
+    s.pool[id] = mine;
     if (threadIdx.x == 0) s.bar = 0, s.count = 0;
     __syncthreads();
     if (threadIdx.x < LP_BINS) {
+        mine = s.pool[threadIdx.x];
 #pragma unroll
         for (int i = 1; i < LP_THREADS / LP_BINS; ++i) mine = max(mine, s.pool[threadIdx.x + i * LP_BINS]);
-        s.pool[threadIdx.x] = mine;
     }
+    __syncthreads();
+    if (threadIdx.x < LP_BINS) s.pool[threadIdx.x] = mine;
     __syncthreads();
     if (threadIdx.x < LP_BINS && mine) {
         int r = 0;
-#pragma unroll 16
+#pragma unroll
         for (int i = 0; i < LP_BINS; ++i) r += s.pool[i] > mine;
         if (r == k - 1) s.bar = mine;
     }
@@ -147,22 +154,19 @@ __device__ __forceinline__ u64 bin_bound(u64 mine, int k, Shared &s) {
     return s.bar;
 }
 
-// Of the n keys key(0 .. n - 1), all different (0: none), the k largest, sorted, into s.best, zeros behind them.  Whole CTA.
-// Their largest: k of n.  `key` gives the same at every call.
-template <typename Key>
-__device__ __forceinline__ void select_best(Key &&key, int n, int k, Shared &s) {
-    u64 mine = 0;
-    for (int i = threadIdx.x; i < n; i += LP_THREADS) mine = max(mine, key(i));
-    u64 bar = bin_bound(mine, k, s);
+// The k largest of the CTA's keys, which differ, sorted, into s.best, zeros behind them.  mine: the thread's largest (0: none);
+// each(f): f(key) for all of its keys that may matter, the same ones at every call.  Whole CTA.
+template <typename Each>
+__device__ __forceinline__ void select_best(u64 mine, int id, int k, Shared &s, Each &&each) {
+    u64 bar = bin_bound(mine, id, k, s);
     auto collect = [&]() {
         if (mine && mine >= bar)
-            for (int i = threadIdx.x; i < n; i += LP_THREADS) {
-                const u64 x = key(i);
+            each([&](u64 x) {
                 if (x && x >= bar) {
                     const int p = atomicAdd(&s.count, 1);
                     if (p < LP_LIST) s.list[p] = x;
                 }
-            }
+            });
         __syncthreads();
     };
     collect();
@@ -175,8 +179,7 @@ __device__ __forceinline__ void select_best(Key &&key, int n, int k, Shared &s) 
             if (threadIdx.x == 0) s.count = 0;
             __syncthreads();
             int c = 0;
-            if (mine >= tried)
-                for (int i = threadIdx.x; i < n; i += LP_THREADS) c += key(i) >= tried;
+            if (mine >= tried) each([&](u64 x) { c += x >= tried; });
             if (c) atomicAdd(&s.count, c);
             __syncthreads();
             if (s.count >= k) at = tried;
@@ -193,7 +196,7 @@ __device__ __forceinline__ void select_best(Key &&key, int n, int k, Shared &s) 
     for (int i = threadIdx.x; i < have; i += LP_THREADS) {
         const u64 x = s.list[i];
         int r = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (int j = 0; j < have; ++j) r += s.list[j] > x;
         if (r < k) s.best[r] = x;
     }
@@ -214,7 +217,7 @@ struct Finish {  // a row's results
             }
             if (a.entropy) a.entropy[row] = empty ? 0.f : ls - 0.6931471805599453f * (s.h / s.s);
         }
-        for (int i = threadIdx.x; i < a.k; i += LP_THREADS) {
+        for (int i = threadIdx.x; i < a.k; i += LP_THREADS) {  // (k is at most 32: all by the first warp)
             a.top_ids[(long long)row * a.k + i] = key_index(best[i]);
             a.top_lp[(long long)row * a.k + i] = empty ? -INFINITY : (key_value(best[i]) - mu) * t - ls;
         }
@@ -230,219 +233,293 @@ __device__ __forceinline__ void check_tokens(const LogprobArgs &a) {
     if (threadIdx.x == 0) *a.status = bad ? DEV_BAD_TOKEN : DEV_OK;
 }
 
+// A row as its CTAs see it: vectors are counted from the 16-byte boundary at or before its first value.
+template <int TYPE>
+struct Row {
+    const char *base, *vbase;  // first value, first vector
+    int skew;                  // values of the first vector that are not the row's
+    int v0, v1;                // vectors of this slice
+    int whole0, whole1;        // vectors that hold nothing but values of the row
+    __device__ __forceinline__ Row(const LogprobArgs &a, int row, int slice) {
+        using E = Elem<TYPE>;
+        base = static_cast<const char *>(a.x) + row * a.ld * E::SIZE;
+        skew = (int)(reinterpret_cast<uintptr_t>(base) & 15) / E::SIZE;
+        vbase = base - skew * E::SIZE;
+        const int vecs = (a.V + skew + E::N - 1) / E::N;
+        v0 = min(vecs, slice * a.slice_vecs);
+        v1 = min(vecs, v0 + a.slice_vecs);
+        whole0 = skew ? 1 : 0;
+        whole1 = (a.V + skew) / E::N;
+    }
+};
+
 template <int TYPE, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 4) k_logprobs(const LogprobArgs a) {
+__global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobArgs a) {
     using E = Elem<TYPE>;
-    constexpr int GE = 4 * E::N;  // values of a group
-    extern __shared__ __align__(16) float maxima[];
+    constexpr int GE = LP_GROUP * E::N;  // values of a group
+    extern __shared__ __align__(128) uint8_t dyn[];
+    uint4 *ring = reinterpret_cast<uint4 *>(dyn);
+    float *maxima = reinterpret_cast<float *>(dyn + LP_STAGES * LP_TILE * 16);
     __shared__ Shared sh;
     __shared__ u64 found[TOP ? LP_MAX_K : 1];  // the best of this CTA's values so far
+    __shared__ int picked[TOP ? LP_MAX_K : 1];
     __shared__ Stat ws[LP_WARPS], all;
+    __shared__ __align__(8) uint64_t full[LP_STAGES], empty[LP_STAGES];
+    __shared__ int abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int row = blockIdx.x / a.slices, slice = blockIdx.x - row * a.slices;
-    if (blockIdx.x == 0) check_tokens(a);
+    const int slice = blockIdx.x % a.slices, first_row = blockIdx.x / a.slices, rows_apart = gridDim.x / a.slices;
+    if (tid == 0) {
+        abort = 0;
+        for (int i = 0; i < LP_STAGES; ++i) {
+            mbar_init(&full[i], 1);
+            mbar_init(&empty[i], LP_WARPS);
+        }
+        fence_mbarrier_init();
+    }
+    __syncthreads();
     const float c = a.inv_t * 1.4426950408889634f;
-    // vectors are counted from the 16-byte boundary at or before the row's first value
-    const char *base = static_cast<const char *>(a.x) + row * a.ld * E::SIZE;
-    const int skew = (int)(reinterpret_cast<uintptr_t>(base) & 15) / E::SIZE;
-    const char *vbase = base - skew * E::SIZE;
-    const int vecs = (a.V + skew + E::N - 1) / E::N;
-    const int v0 = min(vecs, slice * a.slice_vecs), v1 = min(vecs, v0 + a.slice_vecs);
-    const int whole0 = skew ? 1 : 0, whole1 = (a.V + skew) / E::N;  // vectors without a row's end in them
 
-    auto load = [&](int v, uint4 (&raw)[LP_VECS]) {
-        if (v >= whole0 && v + LP_TILE <= min(v1, whole1)) {
-#pragma unroll
-            for (int i = 0; i < LP_VECS; ++i) raw[i] = __ldcs(reinterpret_cast<const uint4 *>(vbase) + v + i * LP_THREADS + tid);
+    // the first thread sends for tiles: of row `p_row`, from vector `p_v` on; `sent` of them so far
+    int p_row = first_row, p_v = -1, sent = 0;
+    const uint64_t policy = l2_policy_evict_first();
+    auto send = [&]() {  // (the stage is free)
+        while (p_row < a.M) {
+            const Row<TYPE> r(a, p_row, slice);
+            if (p_v < 0) p_v = r.v0;
+            if (p_v >= r.v1) {
+                p_row += rows_apart;
+                p_v = -1;
+                continue;
+            }
+            const int b = max(p_v, r.whole0), e = max(b, min(min(p_v + LP_TILE, r.v1), r.whole1)), st = sent % LP_STAGES;
+            mbar_arrive_expect_tx(&full[st], (e - b) * 16);
+            if (e > b) bulk_g2s(ring + st * LP_TILE + (b - p_v), r.vbase + (long long)b * 16, (e - b) * 16, &full[st], policy);
+            p_v += LP_TILE;
+            ++sent;
             return;
         }
-#pragma unroll
-        for (int i = 0; i < LP_VECS; ++i) {  // value by value at a row's ends; -inf behind the slice
-            const int at = v + i * LP_THREADS + tid;
-            if (at < v1 && at >= whole0 && at < whole1) {
-                raw[i] = __ldcs(reinterpret_cast<const uint4 *>(vbase) + at);
-            } else {
-                uint32_t u[4];
-#pragma unroll
-                for (int j = 0; j < E::N; ++j) {
-                    const int e = at * E::N - skew + j;
-                    E::put(u, j, base, e, at < v1 && e >= 0 && e < a.V);
-                }
-                raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
-            }
-        }
     };
-    Stat st{-INFINITY, 0.f, 0.f};
-    if (TOP && tid < a.k) found[tid] = 0;
-    for (int seg = v0; seg < v1; seg += LP_SEGMENT * LP_TILE) {
-        const int seg_end = min(v1, seg + LP_SEGMENT * LP_TILE);
-        uint4 raw[LP_VECS], ahead[LP_VECS];
-        load(seg, raw);
-        float *mrow = maxima + (tid & 3) * 72 + (tid >> 2);
-        for (int v = seg; v < seg_end; v += LP_TILE, mrow += LP_TILE_MAX) {
-            if (v + LP_TILE < seg_end) load(v + LP_TILE, ahead);
-            float mx[LP_VECS], lo = INFINITY;
+    if (tid == 0)
+        for (int i = 0; i < LP_STAGES; ++i) send();
+    if (blockIdx.x == 0) check_tokens(a);
+
+    int taken = 0;  // tiles
+    for (int row = first_row; row < a.M; row += rows_apart) {
+        const Row<TYPE> r(a, row, slice);
+        Stat st{-INFINITY, 0.f, 0.f};
+        if (TOP && tid < a.k) found[tid] = 0;
+        for (int seg = r.v0; seg < r.v1; seg += LP_SEGMENT * LP_TILE) {
+            const int seg_end = min(r.v1, seg + LP_SEGMENT * LP_TILE);
+            float *const mrow0 = maxima + (tid & 3) * 40 + (tid >> 3), *mrow = mrow0;
+            // the thread's groups: one a tile; the largest so far, its place among its tiles, and the second's order
+            uint32_t top = 0, second = 0;
+            int top_tile = 0;
+            const int group0 = (tid & 3) * (LP_THREADS / LP_GROUP) + (tid >> 3);  // the first one's number
+            for (int v = seg; v < seg_end; v += LP_TILE, mrow += LP_TILE_MAX) {
+                const int stage = taken % LP_STAGES, turn = (taken / LP_STAGES) & 1;
+                mbar_wait(&full[stage], turn, a.status, DEV_TIMEOUT_LOAD, &abort);
+                uint4 raw[LP_VECS];
 #pragma unroll
-            for (int i = 0; i < LP_VECS; ++i) {
-                float x[E::N];
-                E::open(raw[i], x);
-                mx[i] = x[0];
+                for (int i = 0; i < LP_VECS; ++i) raw[i] = ring[stage * LP_TILE + i * LP_THREADS + tid];
+                __syncwarp();
+                if (lane == 0) mbarrier_arrive_one(&empty[stage]);
+                if (v < r.whole0 || v + LP_TILE > min(r.v1, r.whole1)) {
+                    // value by value at a row's ends; -inf behind the slice
 #pragma unroll
-                for (int j = 1; j < E::N; ++j) mx[i] = fmaxf(mx[i], x[j]);
+                    for (int i = 0; i < LP_VECS; ++i) {
+                        const int at = v + i * LP_THREADS + tid;
+                        if (at < r.v1 && at >= r.whole0 && at < r.whole1) continue;
+                        uint32_t u[4];
 #pragma unroll
-                for (int j = 0; j < E::N; ++j) lo = fminf(lo, x[j]);
-            }
-            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mn = fmaxf(st.m, mt);
-            if (mn > st.m) {
-                const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
-                st.h = (st.h + st.s * d) * f;
-                st.s *= f;
-                st.m = mn;
-            }
-            const float mu = st.m == -INFINITY ? 0.f : st.m;
-            if ((lo - mu) * c > LP_FLOOR) {
-                F2 s2 = f2(0.f, 0.f), h2 = s2;
-                const F2 nm = f2(-mu, -mu), cc = f2(c, c);
+                        for (int j = 0; j < E::N; ++j) {
+                            const int e = at * E::N - r.skew + j;
+                            E::put(u, j, r.base, e, at < r.v1 && e >= 0 && e < a.V);
+                        }
+                        raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                }
+                ++taken;
+                float mx[LP_VECS], lo = INFINITY;
 #pragma unroll
                 for (int i = 0; i < LP_VECS; ++i) {
                     float x[E::N];
                     E::open(raw[i], x);
+                    mx[i] = x[0];
 #pragma unroll
-                    for (int j = 0; j < E::N; j += 2) {
-                        const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
-                        const float2 tt = unpack2(t);
-                        const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
-                        s2 = add2(s2, e);
-                        h2 = fma2(e, t, h2);
+                    for (int j = 1; j < E::N; ++j) mx[i] = fmaxf(mx[i], x[j]);
+#pragma unroll
+                    for (int j = 0; j < E::N; ++j) lo = fminf(lo, x[j]);
+                }
+                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mn = fmaxf(st.m, mt);
+                if (mn > st.m) {
+                    const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
+                    st.h = (st.h + st.s * d) * f;
+                    st.s *= f;
+                    st.m = mn;
+                }
+                const float mu = st.m == -INFINITY ? 0.f : st.m;
+                if ((lo - mu) * c > LP_FLOOR) {
+                    F2 s2 = f2(0.f, 0.f), h2 = s2;
+                    const F2 nm = f2(-mu, -mu), cc = f2(c, c);
+#pragma unroll
+                    for (int i = 0; i < LP_VECS; ++i) {
+                        float x[E::N];
+                        E::open(raw[i], x);
+#pragma unroll
+                        for (int j = 0; j < E::N; j += 2) {
+                            const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
+                            const float2 tt = unpack2(t);
+                            const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
+                            s2 = add2(s2, e);
+                            h2 = fma2(e, t, h2);
+                        }
+                    }
+                    const float2 s = unpack2(s2), h = unpack2(h2);
+                    st.s += s.x + s.y;
+                    st.h += h.x + h.y;
+                } else {  // masked values, whose -inf would give 0 * -inf
+#pragma unroll
+                    for (int i = 0; i < LP_VECS; ++i) {
+                        float x[E::N];
+                        E::open(raw[i], x);
+#pragma unroll
+                        for (int j = 0; j < E::N; ++j) {
+                            const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
+                            st.s += e;
+                            st.h += e * t;
+                        }
                     }
                 }
-                const float2 s = unpack2(s2), h = unpack2(h2);
-                st.s += s.x + s.y;
-                st.h += h.x + h.y;
-            } else {  // masked values, whose -inf would give 0 * -inf
-#pragma unroll
-                for (int i = 0; i < LP_VECS; ++i) {
-                    float x[E::N];
-                    E::open(raw[i], x);
-#pragma unroll
-                    for (int j = 0; j < E::N; ++j) {
-                        const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
-                        st.s += e;
-                        st.h += e * t;
+                if (TOP) {
+                    // Eight lanes hold a group of each of the four loads: lane i of them gets the i-th's maximum.
+                    const float a0 = tid & 1 ? mx[0] : mx[1], a1 = tid & 1 ? mx[2] : mx[3];
+                    const float b0 = tid & 1 ? mx[1] : mx[0], b1 = tid & 1 ? mx[3] : mx[2];
+                    const float p0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, a0, 1)), p1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, a1, 1));
+                    float g = fmaxf(tid & 2 ? p1 : p0, __shfl_xor_sync(0xffffffffu, tid & 2 ? p0 : p1, 2));
+                    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
+                    if ((tid & 4) == 0 && v + group0 * LP_GROUP < r.v1) {
+                        *mrow = g;
+                        const uint32_t order = lp_order(g);
+                        if (order > top) {
+                            second = top;
+                            top = order;
+                            top_tile = (v - seg) / LP_TILE;
+                        } else {
+                            second = max(second, order);
+                        }
                     }
+                }
+                if (tid == 0 && p_row < a.M) {  // the stage goes out again
+                    mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort);
+                    send();
                 }
             }
             if (TOP) {
-                // Four lanes hold a group of each of the four loads: lane i of them gets the i-th's maximum.
-                const float a0 = tid & 1 ? mx[0] : mx[1], a1 = tid & 1 ? mx[2] : mx[3];
-                const float b0 = tid & 1 ? mx[1] : mx[0], b1 = tid & 1 ? mx[3] : mx[2];
-                const float p0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, a0, 1)), p1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, a1, 1));
-                const float g = fmaxf(tid & 2 ? p1 : p0, __shfl_xor_sync(0xffffffffu, tid & 2 ? p0 : p1, 2));
-                *mrow = g;
-            }
-#pragma unroll
-            for (int i = 0; i < LP_VECS; ++i) raw[i] = ahead[i];
-        }
-        if (TOP) {
-            // the k groups of largest maxima, then the k best of their values and of those found before
-            const int groups = (seg_end - seg + 3) / 4, g0 = seg / 4;
-            __syncthreads();
-            select_best([&](int g) {
-                return lp_key(maxima[(g >> 8) * LP_TILE_MAX + ((g >> 6) & 3) * 72 + (g & 63)], g);
-            }, groups, a.k, sh);
-            __shared__ int picked[LP_MAX_K];
-            if (tid < a.k) picked[tid] = sh.best[tid] ? g0 + key_index(sh.best[tid]) : -1;
-            __syncthreads();
-            const int more = a.k * GE;
-            // (few values a thread: read once, kept)
-            constexpr int PER = (LP_MAX_K * GE + LP_MAX_K + LP_THREADS - 1) / LP_THREADS;
-            u64 keys[PER];
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int at = tid + i * LP_THREADS;
-                u64 x = 0;
-                if (at < more) {
-                    const int g = picked[at / GE];
-                    const int e = g * GE + at % GE - skew, v = g * 4 + at % GE / E::N;
-                    if (g >= 0 && e >= 0 && e < a.V && v < v1) x = lp_key(E::one(base, e), e);
-                } else if (at < more + a.k) {
-                    x = found[at - more];
-                }
-                keys[i] = x;
-            }
-            select_best([&](int i) {
-                u64 x = 0;
-#pragma unroll
-                for (int j = 0; j < PER; ++j)
-                    if (i / LP_THREADS == j) x = keys[j];
-                return x;
-            }, PER * LP_THREADS, a.k, sh);
-            if (tid < a.k) found[tid] = sh.best[tid];
-        }
-    }
-    // the CTA's sums
-    for (int o = 16; o; o >>= 1)
-        st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
-                           __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
-    if (lane == 0) ws[warp] = st;
-    __syncthreads();
-    st = ws[0];
-    for (int i = 1; i < LP_WARPS; ++i) st = join(st, ws[i], c);
-    if (a.slices > 1) {
-        if (tid == 0) all = st;
-        cluster_sync();
-        if (slice == 0) {
-            if (warp == 0) {
-                const uint32_t p = map_cta(smem_u32(&all), lane % a.slices);  // (a power of two)
-                Stat x{ld_cluster(p), ld_cluster(p + 4), ld_cluster(p + 8)};
-                for (int o = a.slices / 2; o; o >>= 1)
-                    x = join(x, Stat{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
-                                     __shfl_xor_sync(0xffffffffu, x.h, o)}, c);
-                if (lane == 0) ws[0] = x;
-            }
-            __syncthreads();
-            st = ws[0];
-            if (TOP) {
-                constexpr int PER = LP_CLUSTER * LP_MAX_K / LP_THREADS;
-                u64 keys[PER];
+                // the k groups of largest maxima, then the k best of their values and of those found before
+                constexpr int TILE_GROUPS = LP_TILE / LP_GROUP;
+                const int g0 = seg / LP_GROUP;
+                const u64 mine = top ? lp_key(top, top_tile * TILE_GROUPS + group0) : 0;
+                select_best(mine, (tid & 4) == 0 ? (tid >> 3) * 4 + (tid & 3) : LP_THREADS / 2 + (tid >> 3) * 4 + (tid & 3), a.k, sh, [&](auto &&f) {
+                    f(mine);
+                    if (second >= (uint32_t)(sh.bar >> 32))  // (then the others too)
+                        for (int t = 0; seg + t * LP_TILE + group0 * LP_GROUP < seg_end; ++t)
+                            if (t != top_tile) f(lp_key(lp_order(mrow0[t * LP_TILE_MAX]), t * TILE_GROUPS + group0));
+                });
+                if (tid < a.k) picked[tid] = sh.best[tid] ? g0 + key_index(sh.best[tid]) : -1;
+                __syncthreads();
+                // (few values a thread: read once, kept)
+                const int more = a.k * GE;
+                constexpr int PER = (LP_MAX_K * GE + LP_MAX_K + LP_THREADS - 1) / LP_THREADS;
+                float x[PER];
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const int p = tid + i * LP_THREADS, r = p / LP_MAX_K, j = p % LP_MAX_K;
-                    keys[i] = 0;
-                    if (r < a.slices && j < a.k) {
-                        const float2 f = ld_cluster_v2(map_cta(smem_u32(&found[j]), r));
-                        keys[i] = (u64)__float_as_uint(f.y) << 32 | __float_as_uint(f.x);
-                    }
+                    const int at = tid + i * LP_THREADS;
+                    const int g = at < more ? picked[at / GE] : -1, e = g * GE + at % GE - r.skew;
+                    if (g >= 0 && e >= 0 && e < a.V && g * LP_GROUP + at % GE / E::N < r.v1) x[i] = E::one(r.base, e);
                 }
-                select_best([&](int i) {
-                    u64 x = 0;
+                u64 keys[PER], best = 0;
 #pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        if (i / LP_THREADS == j) x = keys[j];
-                    return x;
-                }, PER * LP_THREADS, a.k, sh);
+                for (int i = 0; i < PER; ++i) {
+                    const int at = tid + i * LP_THREADS;
+                    const int g = at < more ? picked[at / GE] : -1, e = g * GE + at % GE - r.skew;
+                    keys[i] = 0;
+                    if (g >= 0 && e >= 0 && e < a.V && g * LP_GROUP + at % GE / E::N < r.v1) keys[i] = lp_key(lp_order(x[i]), e);
+                    if (at >= more && at < more + a.k) keys[i] = found[at - more];
+                    best = max(best, keys[i]);
+                }
+                select_best(best, tid, a.k, sh, [&](auto &&f) {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) f(keys[i]);
+                });
+                if (tid < a.k) found[tid] = sh.best[tid];
             }
         }
-        cluster_sync();  // (nobody leaves while the first CTA reads)
-        if (slice != 0) return;
+        // the CTA's sums
+        for (int o = 16; o; o >>= 1)
+            st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
+                               __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
+        if (lane == 0) ws[warp] = st;
+        __syncthreads();
+        if (warp == 0) {
+            st = ws[lane % LP_WARPS];
+            for (int o = LP_WARPS / 2; o; o >>= 1)
+                st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
+                                   __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
+            if (lane == 0) all = st;
+        }
+        if (a.slices > 1) {
+            cluster_sync();
+            if (slice == 0) {
+                if (warp == 0) {
+                    const uint32_t p = map_cta(smem_u32(&all), lane % a.slices);  // (a power of two)
+                    Stat x{ld_cluster(p), ld_cluster(p + 4), ld_cluster(p + 8)};
+                    for (int o = a.slices / 2; o; o >>= 1)
+                        x = join(x, Stat{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
+                                         __shfl_xor_sync(0xffffffffu, x.h, o)}, c);
+                    st = x;
+                }
+                if (TOP) {
+                    constexpr int PER = LP_CLUSTER * LP_MAX_K / LP_THREADS;
+                    u64 keys[PER], best = 0;
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) {
+                        const int p = tid + i * LP_THREADS, q = p / LP_MAX_K, j = p % LP_MAX_K;
+                        keys[i] = 0;
+                        if (q < a.slices && j < a.k) {
+                            const float2 f = ld_cluster_v2(map_cta(smem_u32(&found[j]), q));
+                            keys[i] = (u64)__float_as_uint(f.y) << 32 | __float_as_uint(f.x);
+                            best = max(best, keys[i]);
+                        }
+                    }
+                    select_best(best, tid, a.k, sh, [&](auto &&f) {
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) f(keys[i]);
+                    });
+                }
+            }
+            cluster_sync();  // (nobody leaves, or goes on to its next row, while the first CTA reads)
+        }
+        if (slice == 0 && warp == 0) {  // (which has the row's sums)
+            const int token = a.logprob ? a.tokens[row] : -1;
+            const bool has = token >= 0 && token < a.V;
+            Finish{a}(row, st, sh.best, has && tid == 0 ? E::one(r.base, token) : 0.f, has);
+        }
+        __syncthreads();  // (found, best, all and ws are the next row's)
     }
-    const int token = a.logprob ? a.tokens[row] : -1;
-    const bool has = token >= 0 && token < a.V;
-    Finish{a}(row, st, sh.best, has && tid == 0 ? E::one(base, token) : 0.f, has);
 }
 
-// Slices of a row: a power of two up to the largest cluster, so that there are some four CTAs an SM; each with a
-// tile or more.
+// Slices of a row: a power of two up to the largest cluster, so that all CTAs of an SM have work; each with a tile or
+// more.
 int pick_slices(int M, int vecs, int most) {
     int s = 1;
-    while (s < most && (long long)M * s * 2 <= gemm_ctas() * 4 && (long long)s * LP_TILE < vecs) s *= 2;
+    while (s < most && (long long)M * s * 2 <= gemm_ctas() * LP_CTAS && (long long)s * LP_TILE < vecs) s *= 2;
     return s;
 }
 
 template <int TYPE, bool TOP>
 cudaError_t launch(LogprobArgs &a, cudaStream_t st) {
     using E = Elem<TYPE>;
-    constexpr size_t MOST = TOP ? (size_t)LP_SEGMENT * LP_TILE_MAX * 4 : 0;
+    constexpr size_t RING = (size_t)LP_STAGES * LP_TILE * 16, MOST = RING + (TOP ? (size_t)LP_SEGMENT * LP_TILE_MAX * 4 : 0);
     static thread_local int configured = -1, most = 8;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -461,9 +538,10 @@ cudaError_t launch(LogprobArgs &a, cudaStream_t st) {
     a.slices = pick_slices(a.M, vecs, most);
     a.slice_vecs = ((vecs + a.slices - 1) / a.slices + LP_THREADS - 1) / LP_THREADS * LP_THREADS;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((long long)a.M * a.slices));
+    // as many clusters as run at once, each with rows in turn
+    cfg.gridDim = dim3((unsigned)(std::min(a.M, std::max(1, gemm_ctas() * LP_CTAS / a.slices)) * a.slices));
     cfg.blockDim = dim3(LP_THREADS);
-    cfg.dynamicSmemBytes = TOP ? (size_t)std::min(LP_SEGMENT, (a.slice_vecs + LP_TILE - 1) / LP_TILE) * LP_TILE_MAX * 4 : 0;
+    cfg.dynamicSmemBytes = RING + (TOP ? (size_t)std::min(LP_SEGMENT, (a.slice_vecs + LP_TILE - 1) / LP_TILE) * LP_TILE_MAX * 4 : 0);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
