@@ -9,10 +9,12 @@
 // it finishes one.  Few rows are cut into slices: a cluster of CTAs a row, whose parts are joined through distributed
 // shared memory.
 //
-// The alternatives come from the same pass at the price of one store for 128 bytes of logits: the maximum of each group of
-// 128 bytes stays in shared memory.  The k best values lie in the k groups of largest maxima (k values, those maxima,
-// already reach the k-th of them), so at the end k groups are picked and read again.  Groups are contiguous, so that among
-// equal maxima the lower group holds the lower ids.  However the values are ordered, the work is the same.
+// The alternatives come from the same pass.  The k best values lie in the k groups of 128 bytes with the largest maxima (k
+// values, those maxima, already reach the k-th of them), so at the end k groups are picked and read again.  Each of a tile's
+// groups has a thread that keeps the six largest of its groups' maxima, and nothing else is stored: should a seventh matter,
+// the thread reads its groups again, which an order at random asks of one CTA in thousands (with four it was one in 200, and
+// 136 rows took 34 us instead of 24).  Groups are contiguous, so that among equal maxima the lower group holds the lower
+// ids.
 #include <algorithm>
 #include <cuda_fp16.h>
 
@@ -26,10 +28,9 @@ namespace {
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
 constexpr int LP_VECS = 4;                        // 16-byte loads of a thread and tile
 constexpr int LP_TILE = LP_THREADS * LP_VECS;     // vectors of a tile
-constexpr int LP_STAGES = 2, LP_CTAS = 3;         // tiles of the ring, CTAs of an SM: 96 KB on their way to it
+constexpr int LP_STAGES = 3, LP_CTAS = 3;         // tiles of the ring, CTAs of an SM: 144 KB on their way to it
 constexpr int LP_GROUP = 8;                       // vectors of a group
-constexpr int LP_TILE_MAX = 4 * 40;               // floats that hold a tile's maxima: four rows of 32, padded for the banks
-constexpr int LP_SEGMENT = 40;                    // tiles whose maxima are kept at a time: 26 KB
+constexpr int LP_TOP = 6;                         // groups that a thread keeps
 constexpr int LP_CLUSTER = 16;                    // slices of a row at most
 constexpr int LP_BINS = 64;                       // of the selections below
 constexpr int LP_LIST = 512;                      // keys of a list: ten times what an order at random needs (bin_bound)
@@ -70,6 +71,10 @@ struct Elem<PBD_FP32> {
     static __device__ __forceinline__ void open(const uint4 &v, float *x) {
         x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
     }
+    // the largest value (NaN only where there is nothing else)
+    static __device__ __forceinline__ float largest(const uint4 &v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
     static __device__ __forceinline__ float one(const void *p, long long i) { return static_cast<const float *>(p)[i]; }
     static __device__ __forceinline__ void put(uint32_t *u, int i, const void *p, long long at, bool real) {
         u[i] = real ? static_cast<const uint32_t *>(p)[at] : 0xff800000u;
@@ -93,6 +98,11 @@ struct Elem<PBD_BF16> : Elem16<0xff80u> {
             x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
         }
     }
+    static __device__ __forceinline__ float largest(const uint4 &v) {  // (two values an operation)
+        const auto *b = reinterpret_cast<const __nv_bfloat162 *>(&v);
+        const float2 f = __bfloat1622float2(__hmax2(__hmax2(b[0], b[1]), __hmax2(b[2], b[3])));
+        return fmaxf(f.x, f.y);
+    }
     static __device__ __forceinline__ float one(const void *p, long long i) { return bf2f(static_cast<const bf16 *>(p)[i]); }
 };
 template <>
@@ -105,6 +115,11 @@ struct Elem<PBD_FP16> : Elem16<0xfc00u> {
             x[2 * i] = f.x;
             x[2 * i + 1] = f.y;
         }
+    }
+    static __device__ __forceinline__ float largest(const uint4 &v) {
+        const auto *b = reinterpret_cast<const __half2 *>(&v);
+        const float2 f = __half22float2(__hmax2(__hmax2(b[0], b[1]), __hmax2(b[2], b[3])));
+        return fmaxf(f.x, f.y);
     }
     static __device__ __forceinline__ float one(const void *p, long long i) { return __half2float(static_cast<const __half *>(p)[i]); }
 };
@@ -132,23 +147,29 @@ struct Shared {
 // largest of the maxima of 64 bins of threads, which k keys reach; 0 if fewer bins have one.  Of keys in any order some
 // 64 ln(64 / (64 - k)) reach it: 44 for k = 32.  Whole CTA.
 __device__ __forceinline__ u64 bin_bound(u64 mine, int id, int k, Shared &s) {
-    __syncthreads();
     s.pool[id] = mine;
-    if (threadIdx.x == 0) s.bar = 0, s.count = 0;
     __syncthreads();
-    if (threadIdx.x < LP_BINS) {
-        mine = s.pool[threadIdx.x];
+    if (threadIdx.x < 32) {
+        u64 a = 0, b = 0;
 #pragma unroll
-        for (int i = 1; i < LP_THREADS / LP_BINS; ++i) mine = max(mine, s.pool[threadIdx.x + i * LP_BINS]);
-    }
-    __syncthreads();
-    if (threadIdx.x < LP_BINS) s.pool[threadIdx.x] = mine;
-    __syncthreads();
-    if (threadIdx.x < LP_BINS && mine) {
-        int r = 0;
+        for (int i = 0; i < LP_THREADS; i += LP_BINS) {
+            a = max(a, s.pool[threadIdx.x + i]);
+            b = max(b, s.pool[threadIdx.x + i + 32]);
+        }
+        if (threadIdx.x == 0) s.bar = 0, s.count = 0;
+        __syncwarp();
+        s.pool[threadIdx.x] = a;
+        s.pool[threadIdx.x + 32] = b;
+        __syncwarp();
+        int ra = 0, rb = 0;
 #pragma unroll
-        for (int i = 0; i < LP_BINS; ++i) r += s.pool[i] > mine;
-        if (r == k - 1) s.bar = mine;
+        for (int i = 0; i < LP_BINS; ++i) {
+            const u64 x = s.pool[i];
+            ra += x > a;
+            rb += x > b;
+        }
+        if (a && ra == k - 1) s.bar = a;
+        if (b && rb == k - 1) s.bar = b;
     }
     __syncthreads();
     return s.bar;
@@ -159,6 +180,7 @@ __device__ __forceinline__ u64 bin_bound(u64 mine, int id, int k, Shared &s) {
 template <typename Each>
 __device__ __forceinline__ void select_best(u64 mine, int id, int k, Shared &s, Each &&each) {
     u64 bar = bin_bound(mine, id, k, s);
+    if (threadIdx.x < k) s.best[threadIdx.x] = 0;
     auto collect = [&]() {
         if (mine && mine >= bar)
             each([&](u64 x) {
@@ -191,8 +213,6 @@ __device__ __forceinline__ void select_best(u64 mine, int id, int k, Shared &s, 
         collect();
     }
     const int have = s.count;
-    if (threadIdx.x < k) s.best[threadIdx.x] = 0;
-    __syncthreads();
     for (int i = threadIdx.x; i < have; i += LP_THREADS) {
         const u64 x = s.list[i];
         int r = 0;
@@ -205,12 +225,11 @@ __device__ __forceinline__ void select_best(u64 mine, int id, int k, Shared &s, 
 
 struct Finish {  // a row's results
     const LogprobArgs &a;
-    __device__ __forceinline__ void operator()(int row, const Stat &s, const u64 *best, float x_t, bool has_token) const {
+    __device__ __forceinline__ void operator()(int row, const Stat &s, const u64 *best, float x_t, bool has_token, int token) const {
         const float ls = logf(s.s), t = a.inv_t, mu = s.m == -INFINITY ? 0.f : s.m;
         const bool empty = s.m == -INFINITY && s.s == 0.f;  // nothing but -inf
         if (threadIdx.x == 0) {
             if (a.logprob) {
-                const int token = a.tokens[row];
                 float lp = token < 0 ? 0.f : __uint_as_float(0x7fffffffu);
                 if (has_token) lp = empty ? -INFINITY : (x_t - mu) * t - ls;
                 a.logprob[row] = lp;
@@ -224,13 +243,12 @@ struct Finish {  // a row's results
     }
 };
 
-// One status word for the call: the first CTA of the grid looks at every row's token.
+// Every row's token, by one CTA.
 __device__ __forceinline__ void check_tokens(const LogprobArgs &a) {
     bool bad = false;
     if (a.tokens)
         for (int i = threadIdx.x; i < a.M; i += LP_THREADS) bad |= a.tokens[i] >= a.V;
-    bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) *a.status = bad ? DEV_BAD_TOKEN : DEV_OK;
+    if (bad) latch_error(a.status, DEV_BAD_TOKEN);
 }
 
 // A row as its CTAs see it: vectors are counted from the 16-byte boundary at or before its first value.
@@ -259,17 +277,17 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     constexpr int GE = LP_GROUP * E::N;  // values of a group
     extern __shared__ __align__(128) uint8_t dyn[];
     uint4 *ring = reinterpret_cast<uint4 *>(dyn);
-    float *maxima = reinterpret_cast<float *>(dyn + LP_STAGES * LP_TILE * 16);
     __shared__ Shared sh;
-    __shared__ u64 found[TOP ? LP_MAX_K : 1];  // the best of this CTA's values so far
+    __shared__ Stat ws[LP_WARPS], slice_stat[LP_CLUSTER];                       // of warps; of slices (the first CTA's)
+    __shared__ __align__(8) u64 slice_best[TOP ? LP_CLUSTER : 1][LP_MAX_K];
     __shared__ int picked[TOP ? LP_MAX_K : 1];
-    __shared__ Stat ws[LP_WARPS], all;
     __shared__ __align__(8) uint64_t full[LP_STAGES], empty[LP_STAGES];
     __shared__ int abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int slice = blockIdx.x % a.slices, first_row = blockIdx.x / a.slices, rows_apart = gridDim.x / a.slices;
     if (tid == 0) {
         abort = 0;
+        if (blockIdx.x == 0) *a.status = DEV_OK;  // (before anything is latched: waits that give up take a second, and tokens come last)
         for (int i = 0; i < LP_STAGES; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], LP_WARPS);
@@ -301,159 +319,117 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     };
     if (tid == 0)
         for (int i = 0; i < LP_STAGES; ++i) send();
-    if (blockIdx.x == 0) check_tokens(a);
+    if (a.slices > 1) cluster_arrive();
 
     int taken = 0;  // tiles
     for (int row = first_row; row < a.M; row += rows_apart) {
         const Row<TYPE> r(a, row, slice);
         Stat st{-INFINITY, 0.f, 0.f};
-        if (TOP && tid < a.k) found[tid] = 0;
-        for (int seg = r.v0; seg < r.v1; seg += LP_SEGMENT * LP_TILE) {
-            const int seg_end = min(r.v1, seg + LP_SEGMENT * LP_TILE);
-            float *const mrow0 = maxima + (tid & 3) * 40 + (tid >> 3), *mrow = mrow0;
-            // the thread's groups: one a tile; the largest so far, its place among its tiles, and the second's order
-            uint32_t top = 0, second = 0;
-            int top_tile = 0;
-            const int group0 = (tid & 3) * (LP_THREADS / LP_GROUP) + (tid >> 3);  // the first one's number
-            for (int v = seg; v < seg_end; v += LP_TILE, mrow += LP_TILE_MAX) {
-                const int stage = taken % LP_STAGES, turn = (taken / LP_STAGES) & 1;
-                mbar_wait(&full[stage], turn, a.status, DEV_TIMEOUT_LOAD, &abort);
-                uint4 raw[LP_VECS];
+        const int token = tid == 0 && slice == 0 && a.logprob ? a.tokens[row] : -1;
+        // the thread's groups, one a tile: the largest by their maxima's order, the largest first, and their tiles
+        const int group0 = r.v0 / LP_GROUP + (tid & 3) * (LP_THREADS / LP_GROUP) + (tid >> 3);  // the first one's number
+        uint32_t top[LP_TOP] = {};
+        int top_tile[LP_TOP] = {}, tile = 0;
+        for (int v = r.v0; v < r.v1; v += LP_TILE, ++tile) {
+            const int stage = taken % LP_STAGES, turn = (taken / LP_STAGES) & 1;
+            mbar_wait(&full[stage], turn, a.status, DEV_TIMEOUT_LOAD, &abort);
+            uint4 raw[LP_VECS];
 #pragma unroll
-                for (int i = 0; i < LP_VECS; ++i) raw[i] = ring[stage * LP_TILE + i * LP_THREADS + tid];
-                __syncwarp();
-                if (lane == 0) mbarrier_arrive_one(&empty[stage]);
-                if (v < r.whole0 || v + LP_TILE > min(r.v1, r.whole1)) {
-                    // value by value at a row's ends; -inf behind the slice
+            for (int i = 0; i < LP_VECS; ++i) raw[i] = ring[stage * LP_TILE + i * LP_THREADS + tid];
+            __syncwarp();
+            if (lane == 0) mbarrier_arrive_one(&empty[stage]);
+            if (v < r.whole0 || v + LP_TILE > min(r.v1, r.whole1)) {
+                // value by value at a row's ends; -inf behind the slice
 #pragma unroll
-                    for (int i = 0; i < LP_VECS; ++i) {
-                        const int at = v + i * LP_THREADS + tid;
-                        if (at < r.v1 && at >= r.whole0 && at < r.whole1) continue;
-                        uint32_t u[4];
+                for (int i = 0; i < LP_VECS; ++i) {
+                    const int at = v + i * LP_THREADS + tid;
+                    if (at < r.v1 && at >= r.whole0 && at < r.whole1) continue;
+                    uint32_t u[4];
 #pragma unroll
-                        for (int j = 0; j < E::N; ++j) {
-                            const int e = at * E::N - r.skew + j;
-                            E::put(u, j, r.base, e, at < r.v1 && e >= 0 && e < a.V);
-                        }
-                        raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
+                    for (int j = 0; j < E::N; ++j) {
+                        const int e = at * E::N - r.skew + j;
+                        E::put(u, j, r.base, e, at < r.v1 && e >= 0 && e < a.V);
                     }
+                    raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
                 }
-                ++taken;
-                float mx[LP_VECS], lo = INFINITY;
+            }
+            ++taken;
+            float mx[LP_VECS];
+#pragma unroll
+            for (int i = 0; i < LP_VECS; ++i) mx[i] = E::largest(raw[i]);
+            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mn = fmaxf(st.m, mt);
+            if (mn > st.m) {
+                const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
+                st.h = (st.h + st.s * d) * f;
+                st.s *= f;
+                st.m = mn;
+            }
+            const float mu = st.m == -INFINITY ? 0.f : st.m;
+            float ds, dh;
+            {
+                F2 s2 = f2(0.f, 0.f), h2 = s2;
+                const F2 nm = f2(-mu, -mu), cc = f2(c, c);
 #pragma unroll
                 for (int i = 0; i < LP_VECS; ++i) {
                     float x[E::N];
                     E::open(raw[i], x);
-                    mx[i] = x[0];
 #pragma unroll
-                    for (int j = 1; j < E::N; ++j) mx[i] = fmaxf(mx[i], x[j]);
-#pragma unroll
-                    for (int j = 0; j < E::N; ++j) lo = fminf(lo, x[j]);
-                }
-                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mn = fmaxf(st.m, mt);
-                if (mn > st.m) {
-                    const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
-                    st.h = (st.h + st.s * d) * f;
-                    st.s *= f;
-                    st.m = mn;
-                }
-                const float mu = st.m == -INFINITY ? 0.f : st.m;
-                if ((lo - mu) * c > LP_FLOOR) {
-                    F2 s2 = f2(0.f, 0.f), h2 = s2;
-                    const F2 nm = f2(-mu, -mu), cc = f2(c, c);
-#pragma unroll
-                    for (int i = 0; i < LP_VECS; ++i) {
-                        float x[E::N];
-                        E::open(raw[i], x);
-#pragma unroll
-                        for (int j = 0; j < E::N; j += 2) {
-                            const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
-                            const float2 tt = unpack2(t);
-                            const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
-                            s2 = add2(s2, e);
-                            h2 = fma2(e, t, h2);
-                        }
-                    }
-                    const float2 s = unpack2(s2), h = unpack2(h2);
-                    st.s += s.x + s.y;
-                    st.h += h.x + h.y;
-                } else {  // masked values, whose -inf would give 0 * -inf
-#pragma unroll
-                    for (int i = 0; i < LP_VECS; ++i) {
-                        float x[E::N];
-                        E::open(raw[i], x);
-#pragma unroll
-                        for (int j = 0; j < E::N; ++j) {
-                            const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
-                            st.s += e;
-                            st.h += e * t;
-                        }
+                    for (int j = 0; j < E::N; j += 2) {
+                        const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
+                        const float2 tt = unpack2(t);
+                        const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
+                        s2 = add2(s2, e);
+                        h2 = fma2(e, t, h2);
                     }
                 }
-                if (TOP) {
-                    // Eight lanes hold a group of each of the four loads: lane i of them gets the i-th's maximum.
-                    const float a0 = tid & 1 ? mx[0] : mx[1], a1 = tid & 1 ? mx[2] : mx[3];
-                    const float b0 = tid & 1 ? mx[1] : mx[0], b1 = tid & 1 ? mx[3] : mx[2];
-                    const float p0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, a0, 1)), p1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, a1, 1));
-                    float g = fmaxf(tid & 2 ? p1 : p0, __shfl_xor_sync(0xffffffffu, tid & 2 ? p0 : p1, 2));
-                    g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
-                    if ((tid & 4) == 0 && v + group0 * LP_GROUP < r.v1) {
-                        *mrow = g;
-                        const uint32_t order = lp_order(g);
-                        if (order > top) {
-                            second = top;
-                            top = order;
-                            top_tile = (v - seg) / LP_TILE;
-                        } else {
-                            second = max(second, order);
-                        }
+                const float2 s = unpack2(s2), h = unpack2(h2);
+                ds = s.x + s.y;
+                dh = h.x + h.y;
+            }
+            if (dh != dh) {  // masked values give 0 * -inf: once more, with a floor under the exponents
+                ds = dh = 0.f;
+#pragma unroll
+                for (int i = 0; i < LP_VECS; ++i) {
+                    float x[E::N];
+                    E::open(raw[i], x);
+#pragma unroll
+                    for (int j = 0; j < E::N; ++j) {
+                        const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
+                        ds += e;
+                        dh += e * t;
                     }
-                }
-                if (tid == 0 && p_row < a.M) {  // the stage goes out again
-                    mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort);
-                    send();
                 }
             }
+            st.s += ds;
+            st.h += dh;
             if (TOP) {
-                // the k groups of largest maxima, then the k best of their values and of those found before
-                constexpr int TILE_GROUPS = LP_TILE / LP_GROUP;
-                const int g0 = seg / LP_GROUP;
-                const u64 mine = top ? lp_key(top, top_tile * TILE_GROUPS + group0) : 0;
-                select_best(mine, (tid & 4) == 0 ? (tid >> 3) * 4 + (tid & 3) : LP_THREADS / 2 + (tid >> 3) * 4 + (tid & 3), a.k, sh, [&](auto &&f) {
-                    f(mine);
-                    if (second >= (uint32_t)(sh.bar >> 32))  // (then the others too)
-                        for (int t = 0; seg + t * LP_TILE + group0 * LP_GROUP < seg_end; ++t)
-                            if (t != top_tile) f(lp_key(lp_order(mrow0[t * LP_TILE_MAX]), t * TILE_GROUPS + group0));
-                });
-                if (tid < a.k) picked[tid] = sh.best[tid] ? g0 + key_index(sh.best[tid]) : -1;
-                __syncthreads();
-                // (few values a thread: read once, kept)
-                const int more = a.k * GE;
-                constexpr int PER = (LP_MAX_K * GE + LP_MAX_K + LP_THREADS - 1) / LP_THREADS;
-                float x[PER];
+                // Eight lanes hold a group of each of the four loads: lane i of them gets the i-th's maximum.
+                const float a0 = tid & 1 ? mx[0] : mx[1], a1 = tid & 1 ? mx[2] : mx[3];
+                const float b0 = tid & 1 ? mx[1] : mx[0], b1 = tid & 1 ? mx[3] : mx[2];
+                const float p0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, a0, 1)), p1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, a1, 1));
+                float g = fmaxf(tid & 2 ? p1 : p0, __shfl_xor_sync(0xffffffffu, tid & 2 ? p0 : p1, 2));
+                g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
+                const uint32_t order = lp_order(g);
+                if (order > top[LP_TOP - 1] && (tid & 4) == 0 && group0 * LP_GROUP + tile * LP_TILE < r.v1) {
+                    int at = tile;
+                    uint32_t o = order;
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int at = tid + i * LP_THREADS;
-                    const int g = at < more ? picked[at / GE] : -1, e = g * GE + at % GE - r.skew;
-                    if (g >= 0 && e >= 0 && e < a.V && g * LP_GROUP + at % GE / E::N < r.v1) x[i] = E::one(r.base, e);
+                    for (int i = 0; i < LP_TOP; ++i)
+                        if (o > top[i]) {
+                            const uint32_t x = top[i];
+                            const int y = top_tile[i];
+                            top[i] = o, top_tile[i] = at;
+                            o = x, at = y;
+                        }
                 }
-                u64 keys[PER], best = 0;
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int at = tid + i * LP_THREADS;
-                    const int g = at < more ? picked[at / GE] : -1, e = g * GE + at % GE - r.skew;
-                    keys[i] = 0;
-                    if (g >= 0 && e >= 0 && e < a.V && g * LP_GROUP + at % GE / E::N < r.v1) keys[i] = lp_key(lp_order(x[i]), e);
-                    if (at >= more && at < more + a.k) keys[i] = found[at - more];
-                    best = max(best, keys[i]);
-                }
-                select_best(best, tid, a.k, sh, [&](auto &&f) {
-#pragma unroll
-                    for (int i = 0; i < PER; ++i) f(keys[i]);
-                });
-                if (tid < a.k) found[tid] = sh.best[tid];
+            }
+            if (tid == 0 && p_row < a.M) {  // the stage goes out again
+                mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort);
+                send();
             }
         }
+        const bool has = token >= 0 && token < a.V;
+        const float x_t = has ? E::one(r.base, token) : 0.f;  // (asked for here: the token has arrived)
         // the CTA's sums
         for (int o = 16; o; o >>= 1)
             st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
@@ -465,31 +441,68 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
             for (int o = LP_WARPS / 2; o; o >>= 1)
                 st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
                                    __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
-            if (lane == 0) all = st;
+        }
+        if (TOP) {
+            // the k groups of largest maxima
+            constexpr int TILE_GROUPS = LP_TILE / LP_GROUP;
+            const u64 mine = top[0] ? lp_key(top[0], group0 + top_tile[0] * TILE_GROUPS) : 0;
+            select_best(mine, (tid & 4) == 0 ? (tid >> 3) * 4 + (tid & 3) : LP_THREADS / 2 + (tid >> 3) * 4 + (tid & 3), a.k, sh, [&](auto &&f) {
+#pragma unroll
+                for (int i = 0; i < LP_TOP; ++i)
+                    if (top[i]) f(lp_key(top[i], group0 + top_tile[i] * TILE_GROUPS));
+                if (top[LP_TOP - 1] && top[LP_TOP - 1] >= (uint32_t)(sh.bar >> 32))
+                    // others may matter: the thread's groups once more
+                    for (int t = 0, g = group0; g * LP_GROUP < r.v1; ++t, g += TILE_GROUPS) {
+                        bool kept = false;
+#pragma unroll
+                        for (int i = 0; i < LP_TOP; ++i) kept |= t == top_tile[i];
+                        if (kept) continue;
+                        uint32_t o = 0;
+#pragma unroll
+                        for (int i = 0; i < LP_GROUP; ++i) {
+                            const int at = g * LP_GROUP + i;
+                            if (at < r.v1 && at >= r.whole0 && at < r.whole1) {
+                                o = max(o, lp_order(E::largest(*(reinterpret_cast<const uint4 *>(r.vbase) + at))));
+                            } else if (at < r.v1) {
+                                for (int e = max(0, at * E::N - r.skew); e < min(a.V, (at + 1) * E::N - r.skew); ++e)
+                                    o = max(o, lp_order(E::one(r.base, e)));
+                            }
+                        }
+                        f(lp_key(o, g));
+                    }
+            });
         }
         if (a.slices > 1) {
+            // the slices' results go to the first CTA (which waits for no answer, as it would if it fetched them)
+            cluster_wait();  // (it has read those of the row before)
+            if (warp == 0) {
+                if (lane == 0) {
+                    const uint32_t to = map_cta(smem_u32(&slice_stat[slice]), 0);
+                    st_cluster(to, st.m);
+                    st_cluster(to + 4, st.s);
+                    st_cluster(to + 8, st.h);
+                }
+                if (TOP && lane < a.k) {
+                    const u64 x = sh.best[lane];
+                    st_cluster_v2(map_cta(smem_u32(&slice_best[slice][lane]), 0), __uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+                }
+            }
             cluster_sync();
             if (slice == 0) {
                 if (warp == 0) {
-                    const uint32_t p = map_cta(smem_u32(&all), lane % a.slices);  // (a power of two)
-                    Stat x{ld_cluster(p), ld_cluster(p + 4), ld_cluster(p + 8)};
-                    for (int o = a.slices / 2; o; o >>= 1)
-                        x = join(x, Stat{__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
-                                         __shfl_xor_sync(0xffffffffu, x.h, o)}, c);
-                    st = x;
+                    st = lane < a.slices ? slice_stat[lane] : Stat{-INFINITY, 0.f, 0.f};
+                    for (int o = 16; o; o >>= 1)
+                        st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
+                                           __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
                 }
                 if (TOP) {
                     constexpr int PER = LP_CLUSTER * LP_MAX_K / LP_THREADS;
                     u64 keys[PER], best = 0;
 #pragma unroll
                     for (int i = 0; i < PER; ++i) {
-                        const int p = tid + i * LP_THREADS, q = p / LP_MAX_K, j = p % LP_MAX_K;
-                        keys[i] = 0;
-                        if (q < a.slices && j < a.k) {
-                            const float2 f = ld_cluster_v2(map_cta(smem_u32(&found[j]), q));
-                            keys[i] = (u64)__float_as_uint(f.y) << 32 | __float_as_uint(f.x);
-                            best = max(best, keys[i]);
-                        }
+                        const int q = (tid + i * LP_THREADS) / LP_MAX_K, j = tid % LP_MAX_K;
+                        keys[i] = q < a.slices && j < a.k ? slice_best[q][j] : 0;
+                        best = max(best, keys[i]);
                     }
                     select_best(best, tid, a.k, sh, [&](auto &&f) {
 #pragma unroll
@@ -497,59 +510,104 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                     });
                 }
             }
-            cluster_sync();  // (nobody leaves, or goes on to its next row, while the first CTA reads)
+            cluster_arrive();
         }
-        if (slice == 0 && warp == 0) {  // (which has the row's sums)
-            const int token = a.logprob ? a.tokens[row] : -1;
-            const bool has = token >= 0 && token < a.V;
-            Finish{a}(row, st, sh.best, has && tid == 0 ? E::one(r.base, token) : 0.f, has);
+        if (slice == 0) {
+            if (TOP) {
+                // the k best of the groups' values (of all slices: groups are counted over the whole row)
+                if (tid < a.k) picked[tid] = sh.best[tid] ? key_index(sh.best[tid]) : -1;
+                __syncthreads();
+                constexpr int PER = LP_MAX_K * GE / LP_THREADS;
+                auto value_at = [&](int i) {  // -1: none
+                    const int at = tid + i * LP_THREADS, g = at < a.k * GE ? picked[at / GE] : -1, e = g * GE + at % GE - r.skew;
+                    return g >= 0 && e >= 0 && e < a.V ? e : -1;
+                };
+                float x[PER];
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int e = value_at(i);
+                    x[i] = e >= 0 ? E::one(r.base, e) : 0.f;
+                }
+                u64 keys[PER], best = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int e = value_at(i);
+                    keys[i] = e >= 0 ? lp_key(lp_order(x[i]), e) : 0;
+                    best = max(best, keys[i]);
+                }
+                select_best(best, tid, a.k, sh, [&](auto &&f) {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i) f(keys[i]);
+                });
+            }
+            if (warp == 0) Finish{a}(row, st, sh.best, x_t, has, token);  // (the warp that has the row's sums)
         }
-        __syncthreads();  // (found, best, all and ws are the next row's)
+        __syncthreads();  // (best and ws are the next row's)
     }
+    if (a.slices > 1) cluster_wait();
+    if (blockIdx.x == a.slices - 1) check_tokens(a);  // (which has nothing else to do by now)
 }
 
-// Slices of a row: a power of two up to the largest cluster, so that all CTAs of an SM have work; each with a tile or
-// more.
-int pick_slices(int M, int vecs, int most) {
-    int s = 1;
-    while (s < most && (long long)M * s * 2 <= gemm_ctas() * LP_CTAS && (long long)s * LP_TILE < vecs) s *= 2;
-    return s;
+// Slices of a row, CTAs of its cluster, by estimated time.  Rows run in rounds of as many as the GPU holds at once.  A full
+// round takes its bytes at the memory's rate; in the last one fewer CTAs share it, up to what one CTA's ring can ask
+// for (48 KB in some 1.3 us).  Each round has a fixed part, longer for clusters, whose CTAs wait for one another.
+// Rows of 151936 fp32 values: 17 in 16 slices, 136 in 3 (18 us; 2: 19), 2048 whole (186 us; in 2: 199).
+int pick_slices(int M, int vecs, const int (&clusters)[LP_CLUSTER + 1], bool top) {
+    const double rate = 6.6e6, cta = 37e3;  // bytes a us
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= LP_CLUSTER && (s == 1 || (long long)(s - 1) * LP_TILE < vecs); ++s) {
+        if (clusters[s] < 1) continue;
+        const double bytes = 16.0 * vecs / s;  // of a CTA and round
+        const int full = M / clusters[s], rest = M % clusters[s];
+        double us = full * (bytes * clusters[s] * s / rate + (s > 1 ? 6.0 : 1.0)) + (top ? (s > 1 ? 4.0 : 2.5) : 0.0);
+        if (rest > 0) us += bytes / std::min(cta, rate / ((double)rest * s)) + (s > 1 ? 2.0 : 1.0);
+        if (s == 1 || us < least) best = s, least = us;
+    }
+    return best;
 }
 
 template <int TYPE, bool TOP>
 cudaError_t launch(LogprobArgs &a, cudaStream_t st) {
     using E = Elem<TYPE>;
-    constexpr size_t RING = (size_t)LP_STAGES * LP_TILE * 16, MOST = RING + (TOP ? (size_t)LP_SEGMENT * LP_TILE_MAX * 4 : 0);
-    static thread_local int configured = -1, most = 8;
+    constexpr size_t MOST = (size_t)LP_STAGES * LP_TILE * 16;
+    static thread_local int configured = -1, clusters[LP_CLUSTER + 1];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && configured != dev) {
-        const void *f = reinterpret_cast<const void *>(k_logprobs<TYPE, TOP>);
-        e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e == cudaSuccess) {
-            most = largest_cluster(f, LP_THREADS, MOST, LP_CLUSTER) < LP_CLUSTER ? 8 : LP_CLUSTER;
-            configured = dev;
-        }
-    }
     if (e != cudaSuccess) return e;
-    // (a row that starts off a 16-byte boundary has one vector more)
-    const int vecs = (a.V + E::N - 1) / E::N + 1;
-    a.slices = pick_slices(a.M, vecs, most);
-    a.slice_vecs = ((vecs + a.slices - 1) / a.slices + LP_THREADS - 1) / LP_THREADS * LP_THREADS;
     cudaLaunchConfig_t cfg = {};
-    // as many clusters as run at once, each with rows in turn
-    cfg.gridDim = dim3((unsigned)(std::min(a.M, std::max(1, gemm_ctas() * LP_CTAS / a.slices)) * a.slices));
     cfg.blockDim = dim3(LP_THREADS);
-    cfg.dynamicSmemBytes = RING + (TOP ? (size_t)std::min(LP_SEGMENT, (a.slice_vecs + LP_TILE - 1) / LP_TILE) * LP_TILE_MAX * 4 : 0);
-    cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)a.slices;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    if (configured != dev) {
+        const void *f = reinterpret_cast<const void *>(k_logprobs<TYPE, TOP>);
+        e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        cfg.dynamicSmemBytes = MOST;
+        clusters[1] = gemm_ctas() * LP_CTAS;
+        for (int s = 2; s <= LP_CLUSTER; ++s) {
+            cfg.gridDim = dim3((unsigned)s);
+            attr[0].val.clusterDim.x = (unsigned)s;
+            if (cudaOccupancyMaxActiveClusters(&clusters[s], f, &cfg) != cudaSuccess) {
+                clusters[s] = 0;
+                cudaGetLastError();  // (the answer is not an error of a later call)
+            }
+        }
+        configured = dev;
+    }
+    // (a row that starts off a 16-byte boundary has one vector more)
+    const int vecs = (a.V + E::N - 1) / E::N + 1;
+    a.slices = pick_slices(a.M, vecs, clusters, TOP);
+    a.slice_vecs = ((vecs + a.slices - 1) / a.slices + LP_THREADS - 1) / LP_THREADS * LP_THREADS;
+    cfg.gridDim = dim3((unsigned)(std::min(a.M, clusters[a.slices]) * a.slices));
+    cfg.dynamicSmemBytes = MOST;
+    cfg.stream = st;
+    attr[0].val.clusterDim.x = (unsigned)a.slices;
     return cudaLaunchKernelEx(&cfg, k_logprobs<TYPE, TOP>, static_cast<const LogprobArgs>(a));
 }
 
