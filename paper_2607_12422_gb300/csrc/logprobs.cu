@@ -32,7 +32,7 @@ constexpr int LP_STAGES = 3, LP_CTAS = 3;         // tiles of the ring, CTAs of 
 constexpr int LP_GROUP = 8;                       // vectors of a group
 constexpr int LP_TOP = 6;                         // groups that a thread keeps
 constexpr int LP_CLUSTER = 16;                    // slices of a row at most
-constexpr int LP_BINS = 64;                       // of the selections below
+constexpr int LP_BINS = LP_THREADS / 4;           // of the selections below
 constexpr int LP_LIST = 512;                      // keys of a list: ten times what an order at random needs (bin_bound)
 constexpr float LP_FLOOR = -1000.f;               // 2^-1000 is 0 in fp32
 
@@ -139,38 +139,32 @@ __device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c) {
 
 // What the selections share (one CTA).
 struct Shared {
-    u64 list[LP_LIST], best[LP_MAX_K], pool[LP_THREADS], bar;
+    u64 list[LP_LIST], best[LP_MAX_K], bins[LP_BINS], bar;
     int count;
 };
 
-// A lower bound of the k-th largest of all keys, from each thread's largest (0: none), threads numbered by `id`: the k-th
-// largest of the maxima of 64 bins of threads, which k keys reach; 0 if fewer bins have one.  Of keys in any order some
-// 64 ln(64 / (64 - k)) reach it: 44 for k = 32.  Whole CTA.
-__device__ __forceinline__ u64 bin_bound(u64 mine, int id, int k, Shared &s) {
-    s.pool[id] = mine;
+// The number of the n keys in shared memory that are larger than x, by four lanes (lane % 4 = part).
+__device__ __forceinline__ int rank_of(u64 x, const u64 *keys, int n, int part) {
+    int r = 0;
+#pragma unroll 4
+    for (int j = part; j < n; j += 4) r += keys[j] > x;
+    r += __shfl_xor_sync(0xffffffffu, r, 1);
+    return r + __shfl_xor_sync(0xffffffffu, r, 2);
+}
+
+// A lower bound of the k-th largest of all keys, from each thread's largest (0: none): the k-th largest of the maxima of 64
+// bins of four threads, which k keys reach; 0 if fewer bins have one.  Of keys in any order some 64 ln(64 / (64 - k))
+// reach it: 44 for k = 32.  Whole CTA.
+__device__ __forceinline__ u64 bin_bound(u64 mine, int k, Shared &s) {
+    // (lanes 4 and 8 apart: where only lanes with bit 2 clear have keys, every bin still has two of them)
+    mine = max(mine, (u64)__shfl_xor_sync(0xffffffffu, mine, 4));
+    mine = max(mine, (u64)__shfl_xor_sync(0xffffffffu, mine, 8));
+    const int lane = threadIdx.x & 31;
+    if ((lane & 12) == 0) s.bins[(threadIdx.x >> 5) * 8 + (lane & 3) + (lane >> 4) * 4] = mine;
+    if (threadIdx.x == 0) s.bar = 0, s.count = 0;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        u64 a = 0, b = 0;
-#pragma unroll
-        for (int i = 0; i < LP_THREADS; i += LP_BINS) {
-            a = max(a, s.pool[threadIdx.x + i]);
-            b = max(b, s.pool[threadIdx.x + i + 32]);
-        }
-        if (threadIdx.x == 0) s.bar = 0, s.count = 0;
-        __syncwarp();
-        s.pool[threadIdx.x] = a;
-        s.pool[threadIdx.x + 32] = b;
-        __syncwarp();
-        int ra = 0, rb = 0;
-#pragma unroll
-        for (int i = 0; i < LP_BINS; ++i) {
-            const u64 x = s.pool[i];
-            ra += x > a;
-            rb += x > b;
-        }
-        if (a && ra == k - 1) s.bar = a;
-        if (b && rb == k - 1) s.bar = b;
-    }
+    const u64 x = s.bins[threadIdx.x >> 2];
+    if (rank_of(x, s.bins, LP_BINS, threadIdx.x & 3) == k - 1 && x) s.bar = x;
     __syncthreads();
     return s.bar;
 }
@@ -178,8 +172,8 @@ __device__ __forceinline__ u64 bin_bound(u64 mine, int id, int k, Shared &s) {
 // The k largest of the CTA's keys, which differ, sorted, into s.best, zeros behind them.  mine: the thread's largest (0: none);
 // each(f): f(key) for all of its keys that may matter, the same ones at every call.  Whole CTA.
 template <typename Each>
-__device__ __forceinline__ void select_best(u64 mine, int id, int k, Shared &s, Each &&each) {
-    u64 bar = bin_bound(mine, id, k, s);
+__device__ __forceinline__ void select_best(u64 mine, int k, Shared &s, Each &&each) {
+    u64 bar = bin_bound(mine, k, s);
     if (threadIdx.x < k) s.best[threadIdx.x] = 0;
     auto collect = [&]() {
         if (mine && mine >= bar)
@@ -213,12 +207,11 @@ __device__ __forceinline__ void select_best(u64 mine, int id, int k, Shared &s, 
         collect();
     }
     const int have = s.count;
-    for (int i = threadIdx.x; i < have; i += LP_THREADS) {
-        const u64 x = s.list[i];
-        int r = 0;
-#pragma unroll 8
-        for (int j = 0; j < have; ++j) r += s.list[j] > x;
-        if (r < k) s.best[r] = x;
+    for (int i0 = 0; i0 < have; i0 += LP_THREADS / 4) {
+        const int i = i0 + (threadIdx.x >> 2);
+        const u64 x = i < have ? s.list[i] : 0;
+        const int r = rank_of(x, s.list, have, threadIdx.x & 3);
+        if (i < have && r < k) s.best[r] = x;
     }
     __syncthreads();
 }
@@ -446,7 +439,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
             // the k groups of largest maxima
             constexpr int TILE_GROUPS = LP_TILE / LP_GROUP;
             const u64 mine = top[0] ? lp_key(top[0], group0 + top_tile[0] * TILE_GROUPS) : 0;
-            select_best(mine, (tid & 4) == 0 ? (tid >> 3) * 4 + (tid & 3) : LP_THREADS / 2 + (tid >> 3) * 4 + (tid & 3), a.k, sh, [&](auto &&f) {
+            select_best(mine, a.k, sh, [&](auto &&f) {
 #pragma unroll
                 for (int i = 0; i < LP_TOP; ++i)
                     if (top[i]) f(lp_key(top[i], group0 + top_tile[i] * TILE_GROUPS));
@@ -504,7 +497,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                         keys[i] = q < a.slices && j < a.k ? slice_best[q][j] : 0;
                         best = max(best, keys[i]);
                     }
-                    select_best(best, tid, a.k, sh, [&](auto &&f) {
+                    select_best(best, a.k, sh, [&](auto &&f) {
 #pragma unroll
                         for (int i = 0; i < PER; ++i) f(keys[i]);
                     });
@@ -518,24 +511,22 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                 if (tid < a.k) picked[tid] = sh.best[tid] ? key_index(sh.best[tid]) : -1;
                 __syncthreads();
                 constexpr int PER = LP_MAX_K * GE / LP_THREADS;
-                auto value_at = [&](int i) {  // -1: none
-                    const int at = tid + i * LP_THREADS, g = at < a.k * GE ? picked[at / GE] : -1, e = g * GE + at % GE - r.skew;
-                    return g >= 0 && e >= 0 && e < a.V ? e : -1;
-                };
                 float x[PER];
+                int e[PER];  // -1: none
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const int e = value_at(i);
-                    x[i] = e >= 0 ? E::one(r.base, e) : 0.f;
+                    const int at = tid + i * LP_THREADS, g = at < a.k * GE ? picked[at / GE] : -1;
+                    e[i] = g * GE + at % GE - r.skew;
+                    if (g < 0 || e[i] < 0 || e[i] >= a.V) e[i] = -1;
+                    x[i] = e[i] >= 0 ? E::one(r.base, e[i]) : 0.f;
                 }
                 u64 keys[PER], best = 0;
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const int e = value_at(i);
-                    keys[i] = e >= 0 ? lp_key(lp_order(x[i]), e) : 0;
+                    keys[i] = e[i] >= 0 ? lp_key(lp_order(x[i]), e[i]) : 0;
                     best = max(best, keys[i]);
                 }
-                select_best(best, tid, a.k, sh, [&](auto &&f) {
+                select_best(best, a.k, sh, [&](auto &&f) {
 #pragma unroll
                     for (int i = 0; i < PER; ++i) f(keys[i]);
                 });
