@@ -88,7 +88,7 @@ const char *bad_workspace(const void *ws, size_t have, size_t need) {
 
 size_t evict_bytes(const KvView &v, int n_keep) {
     const long long most = std::max(0ll, std::min((long long)n_keep, v.cap - n_keep));
-    return 1024 + ((size_t)v.B * v.hkv * 2 * most * sizeof(int) + 1023) / 1024 * 1024;
+    return 1024 + ((size_t)v.B * v.hkv * (2 * most + 1) * sizeof(int) + 1023) / 1024 * 1024;
 }
 
 }  // namespace
@@ -179,8 +179,9 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
     a.out_weights = d_out_weights;
     a.out_positions = d_out_positions;
     a.status = reinterpret_cast<int *>(ws);
-    a.moves = reinterpret_cast<int *>(ws + 1024);
     a.most = std::max(0ll, std::min((long long)n_keep, v.cap - n_keep));
+    a.counts = reinterpret_cast<int *>(ws + 1024);
+    a.moves = a.counts + (long long)v.B * v.hkv;
     const cudaError_t e = launch_evict(a, static_cast<cudaStream_t>(d_stream));
     return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
 }

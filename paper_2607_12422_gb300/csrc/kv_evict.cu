@@ -8,8 +8,9 @@
 // One cluster works on one (sequence, KV head), each CTA on a stretch of its slots.  The keep-th largest key is found by radix
 // selection over 32-bit keys in shared memory, 11, 11 and 10 bits a round (11 put sign, exponent and two bits of the mantissa
 // into the first: weights of few magnitudes still spread over many counters).  After a round every CTA adds its counters that are
-// not zero, which are few, to each CTA's totals in distributed shared memory.  Then warps count and place holes and kept slots with ballots, and the cluster's
-// warps share the moves, 32 at a time: each lane finds the rows of one, then all of them copy.
+// not zero, which are few, to each CTA's totals in distributed shared memory.  Then warps count and place holes and kept slots with ballots.  The moves
+// follow in the same kernel where a CTA does a row alone (the step of a bounded cache: few moves, and a launch saved); after
+// clusters another kernel makes them, spread over the whole GPU.
 #include <algorithm>
 
 #include "kv_ops.h"
@@ -22,6 +23,7 @@ constexpr int EV_THREADS = 512, EV_WARPS = EV_THREADS / 32;
 constexpr int EV_CLUSTER = 8;        // CTAs of a cluster at most
 constexpr int EV_KEYS = 48 * 1024;   // keys of a CTA that fit shared memory
 constexpr int EV_BINS = 2048;
+constexpr int EV_BATCH = 8;          // moves of a warp at a time: with 32, 8 sequences of 4112 took 17.5 us instead of 15.8
 
 __device__ __forceinline__ uint2 ld_cluster_u32x2(uint32_t a) {
     uint2 v;
@@ -58,6 +60,55 @@ __device__ void check_cache(const EvictArgs &a) {
     if (threadIdx.x == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
 }
 
+// The moves of a row that warp `w` of `warps` makes, EV_BATCH at a time: each lane finds the places of one, then all copy, in 16-byte
+// pieces, 32 / pieces rows of K and V at a time.
+__device__ __forceinline__ void move_rows(const EvictArgs &a, int row, int w, int warps, int moves) {
+    const int lane = threadIdx.x & 31, b = row / a.kv.hkv, h = row - b * a.kv.hkv;
+    const float *weights = a.kv.weights + row * a.kv.cap;
+    const int *pos = a.kv.positions + row * a.kv.cap, *to = a.moves + (long long)row * 2 * a.most, *of = to + a.most;
+    float *out_w = a.out_weights + row * a.kv.cap;
+    int *out_pos = a.out_positions + row * a.kv.cap;
+    const int pieces = a.kv.d / 8, lg = 31 - __clz(pieces);
+    const int *table = a.kv.table + (long long)b * a.kv.max_pages;
+    auto place = [&](int slot) {  // -1: no such page
+        const int q = page_index(a.kv, slot), p = table[q];
+        if ((unsigned)p >= (unsigned)a.kv.n_pages) return -1ll;
+        return (long long)p * a.kv.stride_page + h * a.kv.stride_head + (long long)(slot - q * a.kv.page_size) * a.kv.stride_slot;
+    };
+    for (int m0 = w * EV_BATCH; m0 < moves; m0 += warps * EV_BATCH) {
+        long long dst = -1, src = -1;
+        const bool real = lane < EV_BATCH && m0 + lane < moves;
+        const int d = real ? to[m0 + lane] : 0, s = real ? of[m0 + lane] : 0;
+        if (real) {
+            dst = place(d);
+            src = place(s);
+            if (dst < 0 || src < 0) dst = src = -1;
+        }
+        const int units = min(EV_BATCH, moves - m0) << (lg + 1);  // pieces of this batch: move, K or V, piece
+        constexpr int U = 4;
+        for (int u0 = 0; u0 < units; u0 += 32 * U) {
+            uint4 x[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int u = u0 + j * 32 + lane;
+                const long long from = __shfl_sync(0xffffffffu, src, (u >> (lg + 1)) & 31);
+                if (u < units && from >= 0) x[j] = *reinterpret_cast<const uint4 *>((u >> lg & 1 ? a.kv.v : a.kv.k) + from + (u & (pieces - 1)) * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const int u = u0 + j * 32 + lane;
+                const long long at = __shfl_sync(0xffffffffu, dst, (u >> (lg + 1)) & 31);
+                if (u < units && at >= 0)
+                    *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(u >> lg & 1 ? a.kv.v : a.kv.k) + at + (u & (pieces - 1)) * 8) = x[j];
+            }
+        }
+        if (real) {
+            out_w[d] = weights[s];
+            out_pos[d] = pos[s];
+        }
+    }
+}
+
 template <bool IN_SMEM, bool ALONE>  // ALONE: clusters of one CTA
 __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int cluster) {
     extern __shared__ __align__(16) uint32_t keys[];
@@ -67,6 +118,7 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
     __shared__ __align__(8) uint2 cta_cnt[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, C = ALONE ? 1 : cluster;
     const int rank = ALONE ? 0 : blockIdx.x % C, row = ALONE ? blockIdx.x : blockIdx.x / C;
+    if (!ALONE) pdl_launch();
     if (row == a.kv.B * a.kv.hkv) {
         if (rank == 0) check_cache(a);
         return;
@@ -77,7 +129,8 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
         else
             cluster_sync();
     };
-    const int b = row / a.kv.hkv, h = row - b * a.kv.hkv, n = slots_of(a, b), keep = min(n, a.n_keep);
+    const int b = row / a.kv.hkv, n = slots_of(a, b), keep = min(n, a.n_keep);
+    if (!ALONE && rank == 0 && tid == 0) a.counts[row] = 0;  // (if there is nothing to move)
     if (keep == 0) return;
     const long long cap = a.kv.cap;
     const float *w = a.kv.weights + row * cap;
@@ -231,7 +284,6 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
         tails += __popc(__ballot_sync(0xffffffffu, real && s >= keep && kept));
     });
     const uint2 b4 = before_me(make_uint2(holes, tails), 1, &all);
-    const int moves = all.x;
     int hole = b4.x, tail = b4.y;
     int *to = a.moves + (long long)row * 2 * a.most, *of = to + a.most;
     walk([&](int s, bool real, bool kept) {
@@ -245,43 +297,20 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
     });
     sync();  // the lists are whole, and nobody's counts are read any more
 
-    // rows of K and V in 16-byte pieces: a warp copies 32 / pieces rows of each at a time
-    const int pieces = a.kv.d / 8, lg = 31 - __clz(pieces);
-    const int *table = a.kv.table + (long long)b * a.kv.max_pages;
-    auto place = [&](int slot) {  // -1: no such page
-        const int q = page_index(a.kv, slot), p = table[q];
-        if ((unsigned)p >= (unsigned)a.kv.n_pages) return -1ll;
-        return (long long)p * a.kv.stride_page + h * a.kv.stride_head + (long long)(slot - q * a.kv.page_size) * a.kv.stride_slot;
-    };
-    for (int m0 = (rank * EV_WARPS + warp) * 32; m0 < moves; m0 += C * EV_THREADS) {
-        long long dst = -1, src = -1;
-        if (m0 + lane < moves) {
-            const int d = to[m0 + lane], s = of[m0 + lane];
-            dst = place(d);
-            src = place(s);
-            out_w[d] = w[s];
-            out_pos[d] = pos[s];
-            if (dst < 0 || src < 0) dst = src = -1;
-        }
-        const int units = min(32, moves - m0) << (lg + 1);  // pieces of this batch: move, K or V, piece
-        constexpr int U = 8;
-        for (int u0 = 0; u0 < units; u0 += 32 * U) {
-            uint4 x[U];
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int u = u0 + j * 32 + lane;
-                const long long s = __shfl_sync(0xffffffffu, src, (u >> (lg + 1)) & 31);
-                if (u < units && s >= 0) x[j] = *reinterpret_cast<const uint4 *>((u >> lg & 1 ? a.kv.v : a.kv.k) + s + (u & (pieces - 1)) * 8);
-            }
-#pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const int u = u0 + j * 32 + lane;
-                const long long d = __shfl_sync(0xffffffffu, dst, (u >> (lg + 1)) & 31);
-                if (u < units && d >= 0)
-                    *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(u >> lg & 1 ? a.kv.v : a.kv.k) + d + (u & (pieces - 1)) * 8) = x[j];
-            }
-        }
+    if (ALONE) {
+        move_rows(a, row, warp, EV_WARPS, all.x);
+    } else if (rank == 0 && tid == 0) {
+        a.counts[row] = all.x;  // (k_evict_moves)
     }
+}
+
+constexpr int EM_THREADS = 256;
+
+// The moves of all rows, in small batches, so that every SM has its share however the rows differ.
+__global__ void __launch_bounds__(EM_THREADS, 4) k_evict_moves(const EvictArgs a) {
+    pdl_wait();
+    const int row = blockIdx.x, warp = blockIdx.y * (EM_THREADS / 32) + (threadIdx.x >> 5);
+    move_rows(a, row, warp, gridDim.y * (EM_THREADS / 32), a.counts[row]);
 }
 
 template <bool IN_SMEM, bool ALONE>
@@ -306,7 +335,17 @@ cudaError_t launch(const EvictArgs &a, int C, size_t smem, cudaStream_t st) {
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_evict<IN_SMEM, ALONE>, a, C);
+    e = cudaLaunchKernelEx(&cfg, k_evict<IN_SMEM, ALONE>, a, C);
+    if (e != cudaSuccess || ALONE || a.most == 0) return e;
+    // a batch a warp; fewer warps where rows are many
+    const int rows = a.kv.B * a.kv.hkv;
+    const long long blocks = (a.most + EM_THREADS / 32 * EV_BATCH - 1) / (EM_THREADS / 32 * EV_BATCH), most = std::max(1, gemm_ctas() * 32 / rows);
+    cfg.gridDim = dim3((unsigned)rows, (unsigned)std::min(blocks, most));
+    cfg.blockDim = dim3(EM_THREADS);
+    cfg.dynamicSmemBytes = 0;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    return cudaLaunchKernelEx(&cfg, k_evict_moves, a);
 }
 
 }  // namespace

@@ -67,6 +67,7 @@ struct EvictArgs {
     float *out_weights;
     int *out_positions;
     int *moves;           // [B * hkv][2][most]: holes in front, kept slots behind
+    int *counts;          // [B * hkv]: moves
     long long most;
     int *status;
 };

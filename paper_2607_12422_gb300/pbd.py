@@ -255,6 +255,8 @@ def _dtype(t, who):
 
 def _check(who, name, t, like, shape, dtype=None, rows=False):
     """t lies on like's device, has this shape and type, and is contiguous (rows: each t[i] is)."""
+    if t.shape == shape and t.dtype == (dtype or like.dtype) and t.device == like.device and t.is_contiguous():
+        return  # (the usual case, in one line: a call checks up to five tensors)
     if t.device != like.device:
         _bad(who, "%s is not on the cache's or logits' device" % name)
     if t.shape != shape:
