@@ -109,7 +109,7 @@ typedef enum { PBD_BF16 = 0, PBD_FP16 = 1, PBD_FP32 = 2 } pbd_dtype;
  * values, head_dim values in a row.  [page][head][slot][d] and [page][slot][head][d] are both expressed so.
  * Requirements: head_dim 64, 128 or 256; d_k and d_v 16-byte aligned and every stride a multiple of 8; batch <= 1024.
  * Pages of a sequence's slots [0, d_lens[b]) are read; table entries behind them are not.  Sequences may share pages that
- * a call only reads.  Which token a slot holds is up to the caller: attention does not depend on the order. */
+ * a call only reads, and strides may then be 0.  Which token a slot holds is up to the caller: attention does not depend on the order. */
 typedef struct {
     void *d_k, *d_v;
     int32_t dtype;                    /* PBD_BF16 or PBD_FP16 */
@@ -140,7 +140,7 @@ size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n
  * Requirements: n_q_heads a multiple of n_kv_heads; scale > 0; d_q, d_out, d_k_new and d_v_new 16-byte aligned, row strides
  * multiples of 8; d_out lies over nothing that is read.  The workspace (1024-byte aligned) is scratch; its first word
  * is the status word for pbd_op_status: a length outside [0, max_pages * page_size] (with a new token: one less) or a
- * page outside [0, n_pages) is reported there, read as nothing, and makes the outputs invalid. */
+ * page outside [0, n_pages) is reported there and makes the outputs invalid; nothing is read or stored for it. */
 pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, float scale, const void *d_q, int64_t q_stride,
                                    const void *d_k_new, const void *d_v_new, int64_t new_stride,
                                    const int32_t *d_new_positions, int32_t accumulate, void *d_out, float *d_lse_opt,

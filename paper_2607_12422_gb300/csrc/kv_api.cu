@@ -52,6 +52,20 @@ const char *bad_cache(const pbd_kv_pages *kv) {
     return nullptr;
 }
 
+// Calls that write K and V: rows must not lie over one another.
+const char *bad_rows(const pbd_kv_pages *kv) {
+    const int D = kv->head_dim;
+    if ((kv->page_size > 1 && kv->stride_slot < D) || (kv->n_kv_heads > 1 && kv->stride_head < D) || (kv->n_pages > 1 && kv->stride_page < D))
+        return "a cache that is written to has strides of a row or more";
+    return nullptr;
+}
+
+// bytes from the first value of K (or V) to the last
+long long cache_span(const pbd_kv_pages *kv) {
+    return 2 * ((kv->n_pages - 1) * kv->stride_page + (kv->n_kv_heads - 1) * kv->stride_head +
+                (kv->page_size - 1) * kv->stride_slot + kv->head_dim);
+}
+
 KvView view(const pbd_kv_pages &kv) {
     KvView v{};
     v.k = static_cast<const uint16_t *>(kv.d_k);
@@ -116,6 +130,12 @@ pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, fl
     const int D = kv->head_dim;
     if (q_stride < (int64_t)n_q_heads * D || q_stride % 8 || (d_k_new && (new_stride < (int64_t)kv->n_kv_heads * D || new_stride % 8)))
         return fail(PBD_ERR_INVALID_ARG, who, "row strides must be multiples of 8 values and hold a row");
+    if (const char *w = d_k_new ? bad_rows(kv) : nullptr) return fail(PBD_ERR_INVALID_ARG, who, w);
+    const long long B = kv->batch, out_bytes = 2 * B * n_q_heads * D, new_bytes = 2 * ((B - 1) * new_stride + (long long)kv->n_kv_heads * D);
+    if (overlap(d_out, out_bytes, d_q, 2 * ((B - 1) * q_stride + (long long)n_q_heads * D)) ||
+        overlap(d_out, out_bytes, kv->d_k, cache_span(kv)) || overlap(d_out, out_bytes, kv->d_v, cache_span(kv)) ||
+        (d_k_new && (overlap(d_out, out_bytes, d_k_new, new_bytes) || overlap(d_out, out_bytes, d_v_new, new_bytes))))
+        return fail(PBD_ERR_INVALID_ARG, who, "out lies over something that is read");
     if (accumulate && !kv->d_weights) return fail(PBD_ERR_INVALID_ARG, who, "accumulate needs the cache's d_weights");
     DecodePlan p;
     const KvView v = view(*kv);
@@ -158,6 +178,7 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
                         size_t ws_bytes, void *d_stream) {
     const char *who = "pbd_op_evict";
     if (const char *w = bad_cache(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
+    if (const char *w = bad_rows(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
     if (!kv->d_weights || !kv->d_positions || !d_next_positions || !d_out_weights || !d_out_positions)
         return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
     if (n_keep < 0 || n_recent < 0 || n_sink < 0 || (int64_t)n_recent + n_sink > n_keep)

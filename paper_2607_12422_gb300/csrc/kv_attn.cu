@@ -109,11 +109,12 @@ __device__ __forceinline__ uint16_t round16(float x) {
     return __bfloat16_as_ushort(f2bf(x));
 }
 
-// Slots that the call attends to in sequence b.  Lengths outside the table (which k_decode_join reports) are cut.
+// Slots that the call attends to in sequence b: none where the length, which is reported, lies outside the table (nothing
+// is stored there either).
+__device__ __forceinline__ bool length_ok(const DecodeArgs &a, int n) { return n >= 0 && n <= a.kv.cap - (a.k_new ? 1 : 0); }
 __device__ __forceinline__ int attended(const DecodeArgs &a, int b) {
-    const int add = a.k_new ? 1 : 0;
-    const long long most = a.kv.cap - add;
-    return (int)max(0ll, min((long long)a.kv.lens[b], most)) + add;
+    const int n = a.kv.lens[b];
+    return length_ok(a, n) ? n + (a.k_new ? 1 : 0) : 0;
 }
 
 // The list of all tiles.  A (sequence, KV head, chunk of its query heads) is a row; it counts as its tiles and ROW more in
@@ -582,7 +583,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_split(const DecodeArgs
 // Lengths outside the table, over the whole CTA.
 __device__ __forceinline__ bool bad_length(const DecodeArgs &a) {
     bool bad = false;
-    for (int b = threadIdx.x; b < a.kv.B; b += blockDim.x) bad |= attended(a, b) != a.kv.lens[b] + (a.k_new ? 1 : 0);
+    for (int b = threadIdx.x; b < a.kv.B; b += blockDim.x) bad |= !length_ok(a, a.kv.lens[b]);
     return __syncthreads_or(bad);
 }
 

@@ -42,10 +42,11 @@ __device__ __forceinline__ uint32_t order_key(float w, int pos, int n_sink, int 
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Slots of sequence b.  Lengths and pages outside their ranges are read as nothing, and reported once for the call: the
+// Slots of sequence b; none where the length is outside its range.  Such lengths and pages are reported once for the call: the
 // grid's last cluster looks at all of them, so that the status word has one writer and needs no clearing before.
 __device__ __forceinline__ int slots_of(const EvictArgs &a, int b) {
-    return (int)max(0ll, min((long long)a.kv.lens[b], a.kv.cap));
+    const int n = a.kv.lens[b];
+    return n >= 0 && n <= a.kv.cap ? n : 0;
 }
 __device__ void check_cache(const EvictArgs &a) {
     bool length = false, page = false;

@@ -306,7 +306,15 @@ class PagedKV:
     k, v [n_pages, n_kv_heads, page_size, head_dim] bf16 or fp16, with the same strides, the last one 1 (token-major
     pages: a transposed view); page_table [batch, max_pages] int32, lens [batch] int32; weights and positions
     [batch, n_kv_heads, max_pages * page_size], fp32 and int32, where they are wanted.  The calls read the tensors' present
-    contents; what lens and positions say is up to the program."""
+    contents; what lens and positions say is up to the program, which changes them in place (kv.lens += 1): the handle
+    takes no other tensors."""
+
+    _TENSORS = ("k", "v", "page_table", "lens", "weights", "positions")
+
+    def __setattr__(self, name, value):
+        if name in self._TENSORS and getattr(self, name, value) is not value:
+            _bad("PagedKV", "%s is another tensor than the handle was made for" % name)
+        object.__setattr__(self, name, value)
 
     def __init__(self, k, v, page_table, lens, weights=None, positions=None):
         import torch
@@ -347,7 +355,8 @@ def pbd_op_decode_attention(q, kv: PagedKV, k_new=None, v_new=None, new_position
     a paged cache; see include/pbd_ops.h.  q [batch, n_q_heads, head_dim]; k_new, v_new [batch, n_kv_heads, head_dim]: the
     token's own K and V, stored into the cache first, with new_positions [batch] int32 into its positions; scale is
     1/sqrt(head_dim) when not given; accumulate adds the attention weights to the cache's.  With sync, waits and raises
-    PbdError(PBD_ERR_DEVICE) for a length or page outside the cache; without, ask pbd_op_status(workspace)."""
+    PbdError(PBD_ERR_DEVICE) for a length or page outside the cache; without (as in a graph's capture), ask
+    pbd_op_status(workspace)."""
     import torch
     who = "pbd_op_decode_attention"
     dev = kv.device

@@ -404,6 +404,9 @@ def test_bad_pages_and_lengths_are_reported(env, what):
     with pytest.raises(pbd.PbdError) as e:
         pbd.pbd_op_decode_attention(*args)
     assert e.value.status == 6 and ("page" in str(e.value) or "position" in str(e.value))
+    # nothing was stored for the sequence
+    page = int(c["table"][1, 2])
+    assert torch.equal(g["k"].cpu()[page], c["k"][page]) and torch.equal(g["v"].cpu()[page], c["v"][page])
     if what == "full":
         pbd.pbd_op_decode_attention(q, kv)  # (a full sequence can be read)
         return
@@ -460,6 +463,8 @@ def test_refusals_of_the_binding(env):
         lambda: pbd.pbd_op_decode_attention(q, kv, scale=math.inf),
         lambda: pbd.pbd_op_decode_attention(q, kv, accumulate=True),  # no weights
         lambda: pbd.pbd_op_decode_attention(q, kv, out=torch.empty(2, 4, 64, device="cuda")),
+        lambda: pbd.pbd_op_decode_attention(q, kv, out=q),
+        lambda: setattr(kv, "lens", g["lens"] + 1),
         lambda: pbd.pbd_op_decode_attention(q, kv, workspace=pbd.op_workspace(4096)),
         lambda: pbd.pbd_op_evict(kv, 8, nxt),
         lambda: pbd.pbd_op_evict(_handle(pbd, g, weights=g["weights"], positions=g["positions"]), 8, nxt, n_recent=6, n_sink=3),

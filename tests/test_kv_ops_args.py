@@ -60,14 +60,23 @@ def test_attention_arguments(lib):
                dict(scale=float("inf")), dict(q=None), dict(out=None), dict(q=A + 8), dict(out=A + 4), dict(kn=A), dict(vn=A),
                dict(kn=A, vn=A + 8), dict(qs=511), dict(qs=516), dict(kn=A, vn=A, ns=128), dict(kn=A, vn=A, ns=260)):
         assert attention(lib, kv, **kw) == 1, kw
-    assert attention(lib, cache(d_weights=None), acc=1) == 1 and b"d_weights" in lib.pbd_op_last_error()
+    # the output over q, the cache or the new rows
+    for kw in (dict(out=A), dict(q=A + (1 << 30), qs=1 << 20, out=A + (1 << 30) + (2 << 20)), dict(out=A + 2 * 10 * 4096 - 16),
+               dict(kn=A + (1 << 24), vn=A + (1 << 25), out=A + (1 << 25) + 1520)):
+        kw = dict(dict(q=A + (1 << 28)), **kw)
+        assert attention(lib, kv, **kw) == 1 and b"lies over" in lib.pbd_op_last_error(), kw
+    # new rows into a cache whose rows lie over one another
+    for bad in (dict(stride_slot=0), dict(stride_head=64), dict(stride_page=0)):
+        assert attention(lib, cache(**bad), kn=A, vn=A, q=A + (1 << 28), out=A + (1 << 29)) == 1, bad
+    kv = cache(d_k=A + (1 << 26), d_v=A + (1 << 27))
+    assert attention(lib, cache(d_weights=None, d_k=A + (1 << 26), d_v=A + (1 << 27)), acc=1, out=A + (1 << 29)) == 1 and b"d_weights" in lib.pbd_op_last_error()
     need = lib.pbd_op_decode_attention_workspace_bytes(C.byref(kv), 4, 0)
     assert need and lib.pbd_op_decode_attention_workspace_bytes(C.byref(kv), 4, 1) > need
     for kw in (dict(ws=None), dict(ws=A + 16), dict(n=need - 1), dict(n=need, acc=1)):
-        assert attention(lib, kv, **kw) == 2, kw
+        assert attention(lib, kv, out=A + (1 << 29), **kw) == 2, kw
     # more 16-slot tiles than 32 bits count
     big = cache(batch=1024, page_size=1 << 15, max_pages=1 << 15)
-    assert attention(lib, big) == 3 and lib.pbd_op_decode_attention_workspace_bytes(C.byref(big), 4, 0) == 0
+    assert attention(lib, big, out=A + (1 << 50)) == 3 and lib.pbd_op_decode_attention_workspace_bytes(C.byref(big), 4, 0) == 0
 
 
 def test_evict_arguments(lib):
@@ -78,6 +87,8 @@ def test_evict_arguments(lib):
                dict(ow=A, op=A + 4096),       # one of them the cache's own
                dict(ow=A + 64, op=A + 64)):   # over a part of them
         assert evict(lib, kv, **kw) == 1, kw
+    for bad in (dict(stride_slot=0), dict(stride_head=64), dict(stride_page=0)):
+        assert evict(lib, cache(**bad), ow=A + (1 << 20), op=A + (1 << 21)) == 1 and b"strides" in lib.pbd_op_last_error(), bad
     assert evict(lib, cache(d_weights=None)) == 1 and evict(lib, cache(d_positions=None)) == 1
     need = lib.pbd_op_evict_workspace_bytes(C.byref(kv), 16)
     for kw in (dict(ws=None), dict(ws=A + 16), dict(n=need - 1)):
