@@ -79,6 +79,9 @@ struct Elem<PBD_FP32> {
     static __device__ __forceinline__ void put(uint32_t *u, int i, const void *p, long long at, bool real) {
         u[i] = real ? static_cast<const uint32_t *>(p)[at] : 0xff800000u;
     }
+    static __device__ __forceinline__ float round(float x) { return x; }
+    static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x); }
+    static __device__ __forceinline__ void set(uint32_t *u, int i, uint32_t b) { u[i] = b; }
 };
 template <uint32_t LOWEST>
 struct Elem16 {
@@ -87,9 +90,14 @@ struct Elem16 {
         const uint32_t x = real ? static_cast<const uint16_t *>(p)[at] : LOWEST;
         u[i / 2] = i & 1 ? u[i / 2] | x << 16 : x;
     }
+    static __device__ __forceinline__ void set(uint32_t *u, int i, uint32_t b) {
+        u[i / 2] = i & 1 ? (u[i / 2] & 0xffffu) | b << 16 : (u[i / 2] & 0xffff0000u) | b;
+    }
 };
 template <>
 struct Elem<PBD_BF16> : Elem16<0xff80u> {
+    static __device__ __forceinline__ float round(float x) { return rbf(x); }
+    static __device__ __forceinline__ uint32_t bits(float x) { return __bfloat16_as_ushort(f2bf(x)); }
     static __device__ __forceinline__ void open(const uint4 &v, float *x) {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -107,6 +115,8 @@ struct Elem<PBD_BF16> : Elem16<0xff80u> {
 };
 template <>
 struct Elem<PBD_FP16> : Elem16<0xfc00u> {
+    static __device__ __forceinline__ float round(float x) { return __half2float(__float2half_rn(x)); }
+    static __device__ __forceinline__ uint32_t bits(float x) { return __half_as_ushort(__float2half_rn(x)); }
     static __device__ __forceinline__ void open(const uint4 &v, float *x) {
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -124,17 +134,26 @@ struct Elem<PBD_FP16> : Elem16<0xfc00u> {
     static __device__ __forceinline__ float one(const void *p, long long i) { return __half2float(static_cast<const __half *>(p)[i]); }
 };
 
-// maximum, sum of e = exp((x - m) / T), sum of e * log2(e)
+// Maximum m, sum of e = exp((x - m) / T) without one value that is m (if m is not -inf), sum of e * log2(e).  The 1 that is
+// left out stays apart to the end: a sum of 1 and what is small beside it would lose the small part, which is all that the
+// log probability of an almost certain token and the entropy then consist of.
 struct Stat {
     float m, s, h;
 };
-// b's sums at a's maximum, and the other way round
-__device__ __forceinline__ Stat join(const Stat &a, const Stat &b, float c) {
-    const float m = fmaxf(a.m, b.m), mu = m == -INFINITY ? 0.f : m;
-    // e 2^d has the logarithm log2 e + d; a part without anything (m = -inf, s = 0) stays 0
-    const float da = max_nan((a.m - mu) * c, LP_FLOOR), db = max_nan((b.m - mu) * c, LP_FLOOR);
-    const float fa = lp_ex2(da), fb = lp_ex2(db);
-    return Stat{m, a.s * fa + b.s * fb, (a.h + a.s * da) * fa + (b.h + b.s * db) * fb};
+// `low`, whose maximum is not above m, at the maximum m, with the value that was left out if it is its own to add: e 2^d has the
+// logarithm log2 e + d
+__device__ __forceinline__ void lower(Stat &low, float m, float c, bool own) {
+    const float d = max_nan((low.m - (m == -INFINITY ? 0.f : m)) * c, LP_FLOOR), f = lp_ex2(d);
+    const float all = own && low.m > -INFINITY ? low.s + 1.f : low.s;
+    low.h = (low.h + all * d) * f;
+    low.s = all * f;
+}
+__device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
+    const bool first = a.m >= b.m;
+    Stat &low = first ? b : a;
+    const float m = first ? a.m : b.m;
+    lower(low, m, c, true);
+    return Stat{m, a.s + b.s, a.h + b.h};
 }
 
 // What the selections share (one CTA).
@@ -219,15 +238,16 @@ __device__ __forceinline__ void select_best(u64 mine, int k, Shared &s, Each &&e
 struct Finish {  // a row's results
     const LogprobArgs &a;
     __device__ __forceinline__ void operator()(int row, const Stat &s, const u64 *best, float x_t, bool has_token, int token) const {
-        const float ls = logf(s.s), t = a.inv_t, mu = s.m == -INFINITY ? 0.f : s.m;
+        const float none = __uint_as_float(0x7fffffffu), t = a.inv_t, mu = s.m == -INFINITY ? 0.f : s.m;
+        const float ls = s.m == INFINITY ? none : log1pf(s.s);  // ln of the sum
         const bool empty = s.m == -INFINITY && s.s == 0.f;  // nothing but -inf
         if (threadIdx.x == 0) {
             if (a.logprob) {
-                float lp = token < 0 ? 0.f : __uint_as_float(0x7fffffffu);
+                float lp = token < 0 ? 0.f : none;
                 if (has_token) lp = empty ? -INFINITY : (x_t - mu) * t - ls;
                 a.logprob[row] = lp;
             }
-            if (a.entropy) a.entropy[row] = empty ? 0.f : ls - 0.6931471805599453f * (s.h / s.s);
+            if (a.entropy) a.entropy[row] = empty ? 0.f : ls - 0.6931471805599453f * (s.h / (1.f + s.s));
         }
         for (int i = threadIdx.x; i < a.k; i += LP_THREADS) {  // (k is at most 32: all by the first warp)
             a.top_ids[(long long)row * a.k + i] = key_index(best[i]);
@@ -350,12 +370,34 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
             float mx[LP_VECS];
 #pragma unroll
             for (int i = 0; i < LP_VECS; ++i) mx[i] = E::largest(raw[i]);
-            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mn = fmaxf(st.m, mt);
-            if (mn > st.m) {
-                const float d = max_nan((st.m - mn) * c, LP_FLOOR), f = lp_ex2(d);
-                st.h = (st.h + st.s * d) * f;
-                st.s *= f;
-                st.m = mn;
+            // the warp's maximum; if it is a new one, the lane that leaves one value of it out of its sum
+            int owner;
+            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mw = warp_max(mt, &owner);
+            const bool grew = mw > st.m;
+            if (grew) {
+                lower(st, mw, c, lane == 0);  // (the value left out was the warp's)
+                st.m = mw;
+                if (lane == owner) {
+                    // The value becomes one whose term is 0: 150 below in the exponent to base 2, and far enough for 16 bits; a
+                    // masked one where there is no such value.
+                    float low = E::round(mw - fmaxf(150.f / c, fabsf(mw) * 0x1p-6f));
+                    if (!((low - mw) * c < -140.f)) low = -INFINITY;
+                    const uint32_t gone = E::bits(low);
+                    bool found = false;
+#pragma unroll
+                    for (int i = 0; i < LP_VECS; ++i) {
+                        float x[E::N];
+                        uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                        E::open(raw[i], x);
+#pragma unroll
+                        for (int j = 0; j < E::N; ++j)
+                            if (!found && x[j] == mw) {
+                                E::set(u, j, gone);
+                                found = true;
+                            }
+                        raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
+                }
             }
             const float mu = st.m == -INFINITY ? 0.f : st.m;
             float ds, dh;
@@ -379,7 +421,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                 ds = s.x + s.y;
                 dh = h.x + h.y;
             }
-            if (dh != dh) {  // masked values give 0 * -inf: once more, with a floor under the exponents
+            if (dh != dh) {  // masked values gave 0 * -inf: once more, with a floor under the exponents
                 ds = dh = 0.f;
 #pragma unroll
                 for (int i = 0; i < LP_VECS; ++i) {
@@ -424,9 +466,10 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
         const bool has = token >= 0 && token < a.V;
         const float x_t = has ? E::one(r.base, token) : 0.f;  // (asked for here: the token has arrived)
         // the CTA's sums
-        for (int o = 16; o; o >>= 1)
-            st = join(st, Stat{__shfl_xor_sync(0xffffffffu, st.m, o), __shfl_xor_sync(0xffffffffu, st.s, o),
-                               __shfl_xor_sync(0xffffffffu, st.h, o)}, c);
+        for (int o = 16; o; o >>= 1) {  // (lanes share the maximum)
+            st.s += __shfl_xor_sync(0xffffffffu, st.s, o);
+            st.h += __shfl_xor_sync(0xffffffffu, st.h, o);
+        }
         if (lane == 0) ws[warp] = st;
         __syncthreads();
         if (warp == 0) {
@@ -506,6 +549,8 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
             cluster_arrive();
         }
         if (slice == 0) {
+            // (one lane's sums for all: joined the other way round they may differ by a rounding)
+            st = Stat{__shfl_sync(0xffffffffu, st.m, 0), __shfl_sync(0xffffffffu, st.s, 0), __shfl_sync(0xffffffffu, st.h, 0)};
             if (TOP) {
                 // the k best of the groups' values (of all slices: groups are counted over the whole row)
                 if (tid < a.k) picked[tid] = sh.best[tid] ? key_index(sh.best[tid]) : -1;

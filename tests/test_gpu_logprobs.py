@@ -97,7 +97,7 @@ def test_masked_logits(env, dtype):
 
 
 def test_certain_tokens_keep_their_precision(env):
-    """A token of probability almost 1: its log probability and the entropy are small numbers, off by roundings of 1."""
+    """A token of probability almost 1: its log probability and the entropy are small numbers, right to their own size."""
     torch, pbd = env
     x = torch.zeros(3, 1000)
     x[:, 123] = torch.tensor([12.0, 14.0, 40.0])
@@ -109,6 +109,47 @@ def test_certain_tokens_keep_their_precision(env):
     off = 28 * 2.0 ** -24
     assert (got.logprob.cpu().double() - lp).abs().max() < off
     assert ((got.entropy.cpu().double() - ent).abs() <= off + ent * 2.0 ** -18).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("M,V", [(1, 1000), (1, 151936), (3, 50000), (460, 20000)])
+def test_almost_certain_tokens_to_their_own_size(env, M, V, dtype):
+    """One value far above the rest, in any place, after smaller ones: what is left beside its 1 keeps its relative precision.
+    The rest is a sum of V terms (V / 256 a thread and some 30 more, 2^-24 each), whose exponents of up to 20 carry two
+    roundings (20 * 2^-23), exp2 2^-22; ln(1 + r) and the division two more."""
+    torch, pbd = env
+    g = torch.Generator().manual_seed(V)
+    x = (torch.randn(M, V, generator=g) * 0.5).to(getattr(torch, dtype))
+    at = torch.randint(0, V, (M,), generator=g)
+    x[torch.arange(M), at] = 24.0
+    x[:, V // 3] = torch.maximum(x[:, V // 3], torch.tensor(6.0, dtype=x.dtype))  # an earlier maximum
+    got = pbd.pbd_op_token_logprobs(x.cuda(), at.int().cuda(), k=1)
+    lp, ent, ids, _ = ref.logprobs(torch, x, at.int(), 1, 1.0)
+    z = x.double() - 24.0
+    z[torch.arange(M), at] = -math.inf
+    rest = z.exp().sum(-1)  # 64 bits, the 1 left out
+    rel = (V / 256 + 40) * 2.0 ** -24 + 24 * 2.0 ** -23 + 2.0 ** -21
+    assert ((got.logprob.cpu().double() + torch.log1p(rest)).abs() <= torch.log1p(rest) * rel).all()
+    want = torch.log1p(rest) + (torch.where(z == -math.inf, torch.zeros_like(z), -z) * z.exp()).sum(-1) / (1 + rest)
+    assert ((got.entropy.cpu().double() - want).abs() <= want * 2 * rel).all()
+    assert torch.equal(got.top_ids.cpu()[:, 0].long(), at)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("T", [1e-12, 1e-3, 1e4])
+def test_extreme_temperatures(env, T, dtype):
+    """Near 0 only the maxima count (ties share the probability), far above 1 all values alike; a maximum of 0 and a large one."""
+    torch, pbd = env
+    x = torch.randn(4, 3000, generator=torch.Generator().manual_seed(4)).to(getattr(torch, dtype))
+    x[0] = -x[0].abs()
+    x[0, 77], x[1, 5], x[1, 2999], x[2, 1500] = 0.0, 1000.0, 1000.0, -0.0
+    got = pbd.pbd_op_token_logprobs(x.cuda(), torch.tensor([77, 2999, 8, 9], dtype=torch.int32).cuda(), k=3, temperature=T)
+    # the temperature's inverse in 32 bits, as the kernel has it
+    lp, ent, ids, top = ref.logprobs(torch, x, torch.tensor([77, 2999, 8, 9]), 3, 1.0 / float(torch.tensor(1.0) / torch.tensor(T)))
+    assert torch.equal(got.top_ids.cpu().long(), ids)
+    # (sums as elsewhere; an exponent of n carries n 2^-23, which counts where its term does, below 20 or so)
+    for a, b in ((got.logprob, lp), (got.entropy, ent), (got.top_logprobs, top)):
+        assert ((a.cpu().double() - b).abs() <= 2.0 ** -17 + b.abs() * 2.0 ** -20).all()
 
 
 def test_nan_and_infinity(env):
