@@ -310,31 +310,43 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     __syncthreads();
     const float c = a.inv_t * 1.4426950408889634f;
 
-    // the first thread sends for tiles: of row `p_row`, from vector `p_v` on; `sent` of them so far
-    int p_row = first_row, p_v = -1, sent = 0;
+    // The next tile to be sent for, in all threads: of row `p_row`, vectors [p_v, p_v1) of which are left.  Warps take turns in
+    // sending: it holds a thread up for 600 cycles, and one warp that always did so would hold up all (a third of the time
+    // of 16-bit rows).
+    int p_row = first_row, p_v = 0, p_v1 = 0, sender = 0;
     const uint64_t policy = l2_policy_evict_first();
-    auto send = [&]() {  // (the stage is free)
-        while (p_row < a.M) {
+    auto enter_row = [&]() {  // the first row from p_row on that has a tile
+        for (; p_row < a.M; p_row += rows_apart) {
             const Row<TYPE> r(a, p_row, slice);
-            if (p_v < 0) p_v = r.v0;
-            if (p_v >= r.v1) {
-                p_row += rows_apart;
-                p_v = -1;
-                continue;
-            }
-            const int b = max(p_v, r.whole0), e = max(b, min(min(p_v + LP_TILE, r.v1), r.whole1)), st = sent % LP_STAGES;
-            mbar_arrive_expect_tx(&full[st], (e - b) * 16);
-            if (e > b) bulk_g2s(ring + st * LP_TILE + (b - p_v), r.vbase + (long long)b * 16, (e - b) * 16, &full[st], policy);
-            p_v += LP_TILE;
-            ++sent;
-            return;
+            p_v = r.v0;
+            p_v1 = r.v1;
+            if (p_v < p_v1) return;
         }
     };
-    if (tid == 0)
-        for (int i = 0; i < LP_STAGES; ++i) send();
+    auto send = [&](int st) {  // (one thread; the stage is free)
+        const Row<TYPE> r(a, p_row, slice);
+        const int b = max(p_v, r.whole0), e = max(b, min(min(p_v + LP_TILE, r.v1), r.whole1));
+        mbar_arrive_expect_tx(&full[st], (e - b) * 16);
+        if (e > b) bulk_g2s(ring + st * LP_TILE + (b - p_v), r.vbase + (long long)b * 16, (e - b) * 16, &full[st], policy);
+    };
+    auto advance = [&]() {
+        p_v += LP_TILE;
+        if (p_v >= p_v1) {
+            p_row += rows_apart;
+            enter_row();
+        }
+        sender = sender + 1 == LP_WARPS ? 0 : sender + 1;
+    };
+    enter_row();
+#pragma unroll
+    for (int i = 0; i < LP_STAGES; ++i)
+        if (p_row < a.M) {
+            if (tid == 0) send(i);
+            advance();
+        }
     if (a.slices > 1) cluster_arrive();
 
-    int taken = 0;  // tiles
+    int stage = 0, turn = 0;
     for (int row = first_row; row < a.M; row += rows_apart) {
         const Row<TYPE> r(a, row, slice);
         Stat st{-INFINITY, 0.f, 0.f};
@@ -344,7 +356,6 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
         uint32_t top[LP_TOP] = {};
         int top_tile[LP_TOP] = {}, tile = 0;
         for (int v = r.v0; v < r.v1; v += LP_TILE, ++tile) {
-            const int stage = taken % LP_STAGES, turn = (taken / LP_STAGES) & 1;
             mbar_wait(&full[stage], turn, a.status, DEV_TIMEOUT_LOAD, &abort);
             uint4 raw[LP_VECS];
 #pragma unroll
@@ -366,7 +377,6 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                     raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             }
-            ++taken;
             float mx[LP_VECS];
 #pragma unroll
             for (int i = 0; i < LP_VECS; ++i) mx[i] = E::largest(raw[i]);
@@ -458,10 +468,15 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                         }
                 }
             }
-            if (tid == 0 && p_row < a.M) {  // the stage goes out again
-                mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort);
-                send();
+            if (p_row < a.M) {  // the stage goes out again
+                if (warp == sender && lane == 0) {
+                    mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort);
+                    send(stage);
+                }
+                __syncwarp();
+                advance();
             }
+            if (++stage == LP_STAGES) stage = 0, turn ^= 1;
         }
         const bool has = token >= 0 && token < a.V;
         const float x_t = has ? E::one(r.base, token) : 0.f;  // (asked for here: the token has arrived)
