@@ -33,7 +33,6 @@ constexpr int DA_SLOTS = 16;      // slots of a tile
 constexpr int DA_MIN_TILES = 2;   // of a warp's stretch
 constexpr int DA_ROW_TILES = 2;   // what beginning and ending a (sequence, KV head) costs a warp, in tiles
 constexpr float DA_FP16_SHIFT = 10.f, DA_SLACK = 4.f;  // log2 of factors: of P in fp16, of P beyond 1 (attend)
-constexpr int DA_LANES = 8;       // lanes that copy a row together: a whole line
 constexpr int DA_CLUSTER = 16;    // CTAs of a cluster at most
 constexpr int DA_CLUSTER_TILES = 16;  // tiles of its warps at most
 
@@ -278,7 +277,9 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
         step(rs, resolving);
     };
     // Copies the tile of row[from] into a stage: a lane takes 16-byte pieces `piece`, `piece` + LPR, ... of rows r0, r0 + 32 / LPR, ...
-    constexpr int LPR = DA_LANES, PIECES = CPR / LPR;
+    // Eight lanes take a whole line together; rows of d = 64 have one, and four lanes spare instructions (64 ragged
+    // sequences 31.9 us instead of 33.0; at d = 128 they make 128 x 1024 slower, 123 us instead of 93).
+    constexpr int LPR = D == 64 ? 4 : 8, PIECES = CPR / LPR;
     const int piece = lane % LPR, r0 = lane / LPR;
     auto issue = [&](int from, int stage) {
         const uint32_t st = ring + stage * S::UNIT;

@@ -8,7 +8,8 @@
 // One cluster works on one (sequence, KV head), each CTA on a stretch of its slots.  The keep-th largest key is found by radix
 // selection over 32-bit keys in shared memory, 11, 11 and 10 bits a round (11 put sign, exponent and two bits of the mantissa
 // into the first: weights of few magnitudes still spread over many counters).  After a round every CTA adds its counters that are
-// not zero, which are few, to each CTA's totals in distributed shared memory.  Then warps count and place holes and kept slots with ballots.  The moves
+// not zero, which are few, to totals in distributed shared memory: the first CTA's, which all then read, or each CTA's own in
+// the last round, where a handful is left (with each CTA's own in all rounds 131072 slots take 33 us instead of 31).  Then warps count and place holes and kept slots with ballots.  The moves
 // follow in the same kernel where a CTA does a row alone (the step of a bounded cache: few moves, and a launch saved); after
 // clusters another kernel makes them, spread over the whole GPU.
 #include <algorithm>
@@ -28,6 +29,11 @@ constexpr int EV_BATCH = 8;          // moves of a warp at a time: with 32, 8 se
 __device__ __forceinline__ uint2 ld_cluster_u32x2(uint32_t a) {
     uint2 v;
     asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 ld_cluster_u32x4(uint32_t a) {
+    uint4 v;
+    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
 }
 __device__ __forceinline__ void red_cluster_add(uint32_t a, uint32_t v) {
@@ -148,6 +154,7 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
     if (!ALONE)
 #pragma unroll
         for (int i = 0; i < 3; ++i) *reinterpret_cast<uint4 *>(totals[i] + tid * 4) = zeros;
+    if (!ALONE) cluster_arrive();  // (this CTA runs, and its totals are zero)
     constexpr int AHEAD = 8;
     for (int i0 = s0 + tid; i0 < s1; i0 += EV_THREADS * AHEAD) {
         float x[AHEAD];
@@ -176,7 +183,10 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
         return IN_SMEM ? keys[slot - s0] : order_key(w[slot], pos[slot], a.n_sink, recent_from);
     };
 
-    sync();  // (the cluster's CTAs run, and their totals are zero)
+    if (ALONE)
+        __syncthreads();
+    else
+        cluster_wait();  // (all of the cluster's CTAs)
     uint32_t prefix = 0;  // the digits found so far
     int want = keep;      // the want-th largest of the keys that begin with them
     bool all_equal_kept = false;
@@ -198,9 +208,9 @@ __global__ void __launch_bounds__(EV_THREADS, 2) k_evict(const EvictArgs a, int 
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (own[i])
-                    for (int c = 0; c < C; ++c) red_cluster_add(map_cta(smem_u32(&totals[round][at + i]), c), own[i]);
+                    for (int c = 0; c < (round == 2 ? C : 1); ++c) red_cluster_add(map_cta(smem_u32(&totals[round][at + i]), c), own[i]);
             sync();
-            d = *reinterpret_cast<const uint4 *>(totals[round] + at);
+            d = round == 2 ? *reinterpret_cast<const uint4 *>(totals[round] + at) : ld_cluster_u32x4(map_cta(smem_u32(&totals[round][at]), 0));
         }
         const uint32_t mine = d.x + d.y + d.z + d.w;
         uint32_t x = mine;
