@@ -155,7 +155,7 @@ size_t pbd_op_evict_workspace_bytes(const pbd_kv_pages *kv, int32_t n_keep);
  * position) into the places in front that came free, the i-th into the i-th; all others stay where they are, so the
  * kept ones are slots [0, n_keep) afterwards, in no order of their tokens.  Sequences of at most n_keep slots keep all.
  * K and V move in place.  Weights and positions of the kept slots go to d_out_weights and d_out_positions, shaped like
- * d_weights and d_positions: those arrays themselves, or others apart from them; slots behind the kept ones are not
+ * d_weights and d_positions: those arrays themselves, or others apart from them and from one another; slots behind the kept ones are not
  * written.  d_lens is not changed: the caller lowers it to at most n_keep once all layers are through.
  * Requirements: n_recent + n_sink <= n_keep; no two sequences share a page.  The workspace (1024-byte aligned) is scratch;
  * its first word is the status word for pbd_op_status, as for pbd_op_decode_attention. */
@@ -175,7 +175,7 @@ size_t pbd_op_token_logprobs_workspace_bytes(int32_t M, int32_t V, int32_t k);
  * pbd_op_status (DEV_BAD_TOKEN) and gives NaN.  d_entropy_opt [M] fp32 or NULL.  d_top_ids [M, k] int32 and
  * d_top_logprobs [M, k] fp32, not read for k = 0.  Logits of -inf are masked; a row with nothing else has log
  * probabilities of -inf and entropy 0.  A row that holds NaN or +inf gives NaN (and ids that say nothing).
- * Requirements: 1 <= V <= 2^30, ld >= V, 0 <= k <= min(32, V); temperature > 0.  Sums are fp32.  The workspace (1024-byte
+ * Requirements: 1 <= M <= 2^30, 1 <= V <= 2^30, ld >= V, 0 <= k <= min(32, V); temperature > 0.  Sums are fp32.  The workspace (1024-byte
  * aligned) is scratch; its first word is the status word for pbd_op_status. */
 pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void *d_logits, int64_t ld, float temperature,
                                  const int32_t *d_tokens_opt, int32_t k, float *d_logprob_opt, float *d_entropy_opt,

@@ -22,6 +22,9 @@ pbd_status fail(pbd_status s, const char *who, const char *what, cudaError_t e =
 
 bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// The exponents' factor, which kernels hold with log2 e in it, is finite too.
+bool usable_factor(float f) { return f > 0.f && !std::isinf(f * 1.4426950408889634f); }
+
 bool overlap(const void *a, long long na, const void *b, long long nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
@@ -84,7 +87,7 @@ KvView view(const pbd_kv_pages &kv) {
     v.d = kv.head_dim;
     v.B = kv.batch;
     v.max_pages = kv.max_pages;
-    // 2^shift / page_size rounded up is off by less than 2^(shift - 30) / 2^30 of the quotient of any slot below 2^30
+    // slot * mul / 2^shift is above slot / page_size by less than slot / 2^shift < 2^30 / (2^30 page_size): never in the next page
     v.page_shift = 30;
     while ((1ll << (v.page_shift - 30)) < kv.page_size) ++v.page_shift;
     v.page_mul = (uint32_t)(((1ull << v.page_shift) + kv.page_size - 1) / kv.page_size);
@@ -122,11 +125,12 @@ pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, fl
     const char *who = "pbd_op_decode_attention";
     if (const char *w = bad_cache(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
     if (const char *w = bad_heads(kv, n_q_heads)) return fail(PBD_ERR_INVALID_ARG, who, w);
-    if (!(scale > 0.f) || std::isinf(scale)) return fail(PBD_ERR_INVALID_ARG, who, "scale must be positive and finite");
+    if (!usable_factor(scale)) return fail(PBD_ERR_INVALID_ARG, who, "scale must be positive and finite");
     if (!d_q || !d_out) return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
     if (!d_k_new != !d_v_new) return fail(PBD_ERR_INVALID_ARG, who, "d_k_new and d_v_new come together");
     if (!aligned(d_q, 16) || !aligned(d_out, 16) || !aligned(d_k_new, 16) || !aligned(d_v_new, 16))
         return fail(PBD_ERR_INVALID_ARG, who, "q, out, k_new and v_new must be 16-byte aligned");
+    if (!aligned(d_new_positions, 4) || !aligned(d_lse_opt, 4)) return fail(PBD_ERR_INVALID_ARG, who, "32-bit arrays must be 4-byte aligned");
     const int D = kv->head_dim;
     if (q_stride < (int64_t)n_q_heads * D || q_stride % 8 || (d_k_new && (new_stride < (int64_t)kv->n_kv_heads * D || new_stride % 8)))
         return fail(PBD_ERR_INVALID_ARG, who, "row strides must be multiples of 8 values and hold a row");
@@ -183,12 +187,15 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
         return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
     if (n_keep < 0 || n_recent < 0 || n_sink < 0 || (int64_t)n_recent + n_sink > n_keep)
         return fail(PBD_ERR_INVALID_ARG, who, "n_keep, n_recent and n_sink must not be negative, and the last two fit the first");
+    if (!aligned(d_next_positions, 4) || !aligned(d_out_weights, 4) || !aligned(d_out_positions, 4))
+        return fail(PBD_ERR_INVALID_ARG, who, "32-bit arrays must be 4-byte aligned");
     const KvView v = view(*kv);
     const long long bytes = (long long)v.B * v.hkv * v.cap * 4;
     const bool in_place = d_out_weights == kv->d_weights && d_out_positions == kv->d_positions;
     if (!in_place && (overlap(d_out_weights, bytes, kv->d_weights, bytes) || overlap(d_out_positions, bytes, kv->d_positions, bytes) ||
-                      overlap(d_out_weights, bytes, kv->d_positions, bytes) || overlap(d_out_positions, bytes, kv->d_weights, bytes)))
-        return fail(PBD_ERR_INVALID_ARG, who, "the outputs are the cache's own arrays, both of them, or lie apart from them");
+                      overlap(d_out_weights, bytes, kv->d_positions, bytes) || overlap(d_out_positions, bytes, kv->d_weights, bytes) ||
+                      overlap(d_out_weights, bytes, d_out_positions, bytes)))
+        return fail(PBD_ERR_INVALID_ARG, who, "the outputs are the cache's own arrays, both of them, or lie apart from them and from one another");
     if (const char *w = bad_workspace(d_ws, ws_bytes, evict_bytes(v, n_keep))) return fail(PBD_ERR_WORKSPACE, who, w);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     EvictArgs a{};
@@ -208,7 +215,7 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
 }
 
 size_t pbd_op_token_logprobs_workspace_bytes(int32_t M, int32_t V, int32_t k) {
-    if (M < 1 || V < 1 || V > (1 << 30) || k < 0 || k > LP_MAX_K || k > V) return 0;
+    if (M < 1 || M > (1 << 30) || V < 1 || V > (1 << 30) || k < 0 || k > LP_MAX_K || k > V) return 0;
     return 1024;  // the status word
 }
 
@@ -221,11 +228,14 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
     if (dtype != PBD_FP32 && dtype != PBD_BF16 && dtype != PBD_FP16) return fail(PBD_ERR_INVALID_ARG, who, "unknown type of logits");
     const int es = dtype == PBD_FP32 ? 4 : 2;
     if (ld < V) return fail(PBD_ERR_INVALID_ARG, who, "rows lie less than V values apart");
-    if (!(temperature > 0.f) || std::isinf(temperature) || std::isinf(1.f / temperature))
-        return fail(PBD_ERR_INVALID_ARG, who, "temperature must be positive and finite");
+    if (!(temperature > 0.f) || std::isinf(temperature) || !usable_factor(1.f / temperature))
+        return fail(PBD_ERR_INVALID_ARG, who, "temperature and its inverse must be positive and finite");
     if (!d_logits || !aligned(d_logits, es)) return fail(PBD_ERR_INVALID_ARG, who, "logits missing or misaligned");
     if (!d_tokens_opt != !d_logprob_opt) return fail(PBD_ERR_INVALID_ARG, who, "d_tokens_opt and d_logprob_opt come together");
     if (k > 0 && (!d_top_ids || !d_top_logprobs)) return fail(PBD_ERR_INVALID_ARG, who, "null pointer");
+    if (!aligned(d_tokens_opt, 4) || !aligned(d_logprob_opt, 4) || !aligned(d_entropy_opt, 4) ||
+        (k > 0 && (!aligned(d_top_ids, 4) || !aligned(d_top_logprobs, 4))))
+        return fail(PBD_ERR_INVALID_ARG, who, "32-bit arrays must be 4-byte aligned");
     if (const char *w = bad_workspace(d_ws, ws_bytes, need)) return fail(PBD_ERR_WORKSPACE, who, w);
     LogprobArgs a{};
     a.x = d_logits;

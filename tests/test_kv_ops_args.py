@@ -108,3 +108,25 @@ def test_logprob_arguments(lib):
     for kw in (dict(ws=None), dict(ws=A + 512), dict(n=need - 1)):
         assert call(**kw) == 2, kw
     assert lib.pbd_op_token_logprobs_workspace_bytes(1, 100, 33) == 0
+
+
+def test_calls_that_would_address_or_scale_out_of_range(lib):
+    kv = cache(d_k=A + (1 << 26), d_v=A + (1 << 27))
+    far = dict(out=A + (1 << 29))
+    # a 32-bit array off its boundary
+    for kw in (dict(lse=A + 2), dict(pos=A + 1)):
+        assert attention(lib, kv, **far, **kw) == 1 and b"4-byte" in lib.pbd_op_last_error(), kw
+    for kw in (dict(nxt=A + 2), dict(ow=A + (1 << 20) + 1, op=A + (1 << 21)), dict(ow=A + (1 << 20), op=A + (1 << 21) + 3)):
+        assert evict(lib, kv, **kw) == 1 and b"4-byte" in lib.pbd_op_last_error(), kw
+    # two outputs over one another
+    assert evict(lib, kv, ow=A + (1 << 20), op=A + (1 << 20) + 64) == 1 and b"one another" in lib.pbd_op_last_error()
+
+    def logprobs(M=2, T=1.0, tok=A, lp=A, ent=A, ids=A, top=A):
+        return lib.pbd_op_token_logprobs(M, 100, pbd.PBD_FP32, A, 100, T, tok, 4, lp, ent, ids, top, A, 1 << 40, None)
+    for name in ("tok", "lp", "ent", "ids", "top"):
+        assert logprobs(**{name: A + 2}) == 1 and b"4-byte" in lib.pbd_op_last_error(), name
+    # rows that 32 bits cannot count on from
+    assert logprobs(M=2**31 - 1) == 1 and lib.pbd_op_token_logprobs_workspace_bytes((1 << 30) + 1, 100, 4) == 0
+    # factors that log2 e takes over the largest number: 2.36e38 * 1.4427 = 3.405e38 > 3.4028e38
+    assert logprobs(T=1 / 2.5e38) == 1
+    assert attention(lib, kv, scale=2.5e38, **far) == 1
