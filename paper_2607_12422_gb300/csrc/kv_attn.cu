@@ -31,7 +31,7 @@ namespace {
 constexpr int DA_WARPS = 4;
 constexpr int DA_SLOTS = 16;      // slots of a tile
 constexpr int DA_MIN_TILES = 2;   // of a warp's stretch
-constexpr int DA_ROW_TILES = 2;   // what beginning and ending a (sequence, KV head) costs a warp, in tiles
+constexpr int DA_ROW_TILES = 2;   // what beginning and ending a (sequence, KV head) costs a warp, in tiles (64 ragged: 31.8 us, 35.0 with 1, 32.2 with 4)
 constexpr float DA_FP16_SHIFT = 10.f, DA_SLACK = 4.f;  // log2 of factors: of P in fp16, of P beyond 1 (attend)
 constexpr int DA_CLUSTER = 16;    // CTAs of a cluster at most
 constexpr int DA_CLUSTER_TILES = 16;  // tiles of its warps at most
@@ -237,7 +237,7 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
     // Tile by tile, in three steps, each so far ahead of the next that nothing is waited for: the table's entries are
     // fetched, STAGES - 1 tiles before they are used; rows' addresses are made of them, by a lane a row; the rows are copied, STAGES - 1
     // tiles before they are multiplied.  (Warps are few, so a step's instructions and waits count: with addresses handed
-    // round by shuffles and entries waited for, 64 ragged sequences of d = 64 took 40 us instead of 28.)
+    // round by shuffles and entries waited for, 64 ragged sequences of d = 64 took 40 us instead of 33.)
     Tiles rs = at, pg = at;  // the next tile whose addresses are made, and whose entries are fetched
     bool resolving = true, looking = true, bad = false;
     int page_in = 0, page_out = 0, buf = 0, fresh_in = 0, fresh_out = 0;
@@ -721,23 +721,16 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
 }
 
 constexpr int DJ_THREADS = 256, DJ_CTAS = 2;
-constexpr int DJ_SLOTS = 8;   // of a thread that adds weights, at a time
-constexpr int DJ_HEADS = 32;  // whose maxima and sums a CTA has at hand
 
 // Joins what several warps left of a row: out = sum_w f_w o_w / sum_w f_w l_w, f_w = exp(scale (m_w - max)).  TEAM threads a
 // query head: the CTA where many warps share a row, a warp where rows are many.  Sequences without a slot get
 // zeros.  A CTA an SM finds room beside k_decode_split's, so that all that does not depend on it is done when it ends.
-// With TEAM = DJ_THREADS the CTAs behind `join_ctas` add the weights: each takes a stretch of the list of [sequence][KV head]
-// [tile], and maxima and sums of its heads from the warps' again, so that it need not wait for the join (131071 tokens: 8 us
-// longer than without weights; with k_decode_weights 11.  For 64 ragged sequences it is the other way round: rows
-// cost a whole CTA 3 us each, 112 us and 12.)
 template <bool FP16, int D, int NT, int TEAM>
-__global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, int join_ctas) {
+__global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a) {
     constexpr int HEADS = 8 * NT, TEAMS = DJ_THREADS / TEAM, L = D / 4 < TEAM ? D / 4 : TEAM, V = D / 4 / L, G = TEAM / L;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ float red[2][DJ_THREADS / 32];
     __shared__ float4 sum_o[TEAM > 32 ? DJ_THREADS : 1];
-    __shared__ float2 ml[TEAM > 32 ? DJ_HEADS : 1];
     const int B = a.kv.B, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int *first = reinterpret_cast<int *>(smem), *len = first + B + 1;
     float *fac = reinterpret_cast<float *>(len + B);  // [TEAMS][workers]
@@ -754,79 +747,6 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
         return worker_at(at + tiles - 1, count, workers) - *w0 + 1;
     };
     auto part_at = [&](int w0, int i, int j) { return ((long long)(w0 + i) * 2 + (i == 0)) * HEADS + j; };
-
-    if (TEAM > 32 && (int)blockIdx.x >= join_ctas) {
-        // weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0
-        const int ctas = gridDim.x - join_ctas, me = blockIdx.x - join_ctas, all = first[B] * a.kv.hkv;
-        const float shift = FP16 ? DA_FP16_SHIFT : 0.f;
-        Tiles at;
-        if (all == 0 || !at.seek(first_of(me, all, ctas), first_of(me + 1, all, ctas), first, len, B, a.kv.hkv, 1)) return;
-        constexpr int STEP = DJ_THREADS * DJ_SLOTS;
-        float have[DJ_SLOTS];
-        auto load_weights = [&](int s0, int s1, int fresh) {
-            const float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
-#pragma unroll
-            for (int i = 0; i < DJ_SLOTS; ++i) {
-                const int slot = s0 + i * DJ_THREADS + tid;
-                have[i] = slot < s1 && slot != fresh ? wt[slot] : 0.f;
-            }
-        };
-        load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS), a.k_new ? at.n - 1 : -1);  // (no kernel of this call has written them)
-        pdl_wait();
-        bool begun = true;
-        do {
-            const int s0 = at.t * DA_SLOTS, s1 = min(at.n, at.t_end * DA_SLOTS);
-            float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
-            for (int g0 = 0; g0 < a.group; g0 += DJ_HEADS) {
-                const int heads = min(DJ_HEADS, a.group - g0);
-                __syncthreads();  // (ml of the heads before has been read)
-                for (int g = warp; g < heads; g += DJ_THREADS / 32) {  // a warp a head
-                    const int ch = (g0 + g) / HEADS, j = g0 + g - ch * HEADS;
-                    int w0;
-                    const int nw = span(at.b, at.h, ch, &w0);
-                    float m = -INFINITY, l = 0.f;
-                    if (nw == 1) {
-                        if (lane == 0) ml[g] = a.row_ml[(long long)at.b * a.hq + at.h * a.group + g0 + g];
-                        continue;
-                    }
-#pragma unroll 5
-                    for (int i = lane; i < nw; i += 32) {
-                        const float2 x = a.part_ml[part_at(w0, i, j)];
-                        const float mx = fmaxf(m, x.x), mu = mx == -INFINITY ? 0.f : mx;
-                        l = l * ex2((m - mu) * c) + x.y * ex2((x.x - mu) * c);
-                        m = mx;
-                    }
-                    float mx = m;
-                    for (int s = 16; s; s >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, s));
-                    l *= ex2((m - (mx == -INFINITY ? 0.f : mx)) * c);
-                    for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
-                    if (lane == 0) ml[g] = make_float2(mx, inverse(l));
-                }
-                __syncthreads();
-                const float *sc = a.scores + ((long long)at.b * a.hq + at.h * a.group + g0) * a.score_pitch;
-                for (int s = s0; s < s1; s += STEP) {
-                    if (!begun || s != s0 || g0 != 0) load_weights(s, s1, a.k_new && g0 == 0 ? at.n - 1 : -1);
-                    float sum[DJ_SLOTS] = {};
-#pragma unroll 2
-                    for (int g = 0; g < heads; ++g) {
-                        const float m = ml[g].x == -INFINITY ? 0.f : ml[g].x, inv = ml[g].y;
-#pragma unroll
-                        for (int i = 0; i < DJ_SLOTS; ++i) {
-                            const int slot = s + i * DJ_THREADS + tid;
-                            if (slot < s1) sum[i] += ex2((sc[g * a.score_pitch + slot] - m) * c + shift) * inv;
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < DJ_SLOTS; ++i) {
-                        const int slot = s + i * DJ_THREADS + tid;
-                        if (slot < s1) wt[slot] = have[i] + sum[i];
-                    }
-                }
-            }
-            begun = false;
-        } while (at.next(first, len, B, a.kv.hkv, 1));
-        return;
-    }
 
     const bool length = blockIdx.x == 0 && bad_length(a);
     pdl_wait();
@@ -845,7 +765,7 @@ __global__ void __launch_bounds__(DJ_THREADS) k_decode_join(const DecodeArgs a, 
         else
             __syncwarp();
     };
-    for (int row = blockIdx.x * TEAMS + team; row < rows; row += join_ctas * TEAMS) {
+    for (int row = blockIdx.x * TEAMS + team; row < rows; row += gridDim.x * TEAMS) {
         const int b = row / a.hq, hq = row - b * a.hq, h = hq / a.group, g = hq - h * a.group;
         const int ch = g / HEADS, j = g - ch * HEADS;
         if (len[b] == 0) {
@@ -952,7 +872,9 @@ constexpr int DW_ROW_TILES = 16;  // what a row costs a warp here, in tiles
 constexpr int DW_VECS = 2;        // float4 of a lane and head at a time
 
 // weights[b][h][slot] += what the heads of h's group give the slot; the new token's slot starts at 0.  A warp a stretch of a
-// list of [sequence][KV head][tile].  For many rows; where rows are few and long, CTAs of k_decode_join do it.
+// list of [sequence][KV head][tile].  (CTAs of the join that took stretches and joined the maxima and sums themselves did
+// not have to wait for it, which saved 1.7 us of 101 on 131072 tokens; but each row cost a whole CTA 3 us: four sequences of 100
+// to 60000 took 83 us instead of 69, eight 128 instead of 107.)
 template <bool FP16>
 __global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs a) {
     extern __shared__ __align__(128) uint8_t smem[];
@@ -962,7 +884,10 @@ __global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs 
     const int all = first[B] * a.kv.hkv, warps = gridDim.x * (DW_THREADS / 32), w = warp * gridDim.x + blockIdx.x;
     const float c = a.scale * 1.4426950408889634f, shift = FP16 ? DA_FP16_SHIFT : 0.f;
     Segment<DW_ROW_TILES> at;
-    if (all == 0 || !at.seek(first_of(w, all, warps), first_of(w + 1, all, warps), first, len, B, a.kv.hkv, 1)) return;
+    if (all == 0 || !at.seek(first_of(w, all, warps), first_of(w + 1, all, warps), first, len, B, a.kv.hkv, 1)) {
+        pdl_wait();  // (a kernel behind this one counts on the join's end as well)
+        return;
+    }
     constexpr int STEP = 128 * DW_VECS;
     float have[DW_VECS][4];
     auto load_weights = [&](int s0, int s1, int fresh) {
@@ -1045,17 +970,17 @@ cudaError_t launch_join(DecodeArgs &a, cudaStream_t st) {
     cudaError_t e = configure(k_decode_join<FP16, D, NT, TEAM>, most, &done);
     if (e != cudaSuccess) return e;
     const int teams = DJ_THREADS / TEAM, rows = a.kv.B * a.hq, sms = gemm_ctas();
-    const bool inside = TEAM > 32 && a.accumulate;
-    const int join = std::min((rows + teams - 1) / teams, inside ? sms / 2 : sms * DJ_CTAS);
-    e = launch_pdl(k_decode_join<FP16, D, NT, TEAM>, inside ? sms * DJ_CTAS : join, DJ_THREADS, lists + facs, st, a, join);
-    if (e != cudaSuccess || !a.accumulate || inside) return e;
+    e = launch_pdl(k_decode_join<FP16, D, NT, TEAM>, std::min((rows + teams - 1) / teams, sms * DJ_CTAS), DJ_THREADS, lists + facs, st, a);
+    if (e != cudaSuccess || !a.accumulate) return e;
     static thread_local int done_w = -1;
     if ((e = configure(k_decode_weights<FP16>, (2 * KV_MAX_BATCH + 1) * 4, &done_w)) != cudaSuccess) return e;
     return launch_pdl(k_decode_weights<FP16>, sms * DW_CTAS, DW_THREADS, lists, st, a);
 }
 
 // CTAs of a (sequence, KV head)'s cluster, or 0 where the list of tiles is the better way: clusters where all of them run at
-// once and no warp has more than DA_CLUSTER_TILES tiles.
+// once and no warp has more than DA_CLUSTER_TILES tiles. (Clusters and list, 8 KV heads of d = 128: 1 x 2048 8.0 us and 10.0,
+// 1 x 8192 13.6 and 14.7, 8 x 1757 14.3 and 18.1; a ragged batch of 8, where the longest row sets the time, 12.5 and 13.7, with
+// weights 15.8 and 14.6: the host does not know the lengths. Longer rows than the bound's spread better over the list.)
 int pick_cluster(const DecodeArgs &a, int ctas, int most) {
     const long long rows = (long long)a.kv.B * a.kv.hkv, tiles = (a.kv.cap + DA_SLOTS - 1) / DA_SLOTS;
     if (a.group > 16 || rows > ctas) return 0;
@@ -1094,7 +1019,8 @@ cudaError_t launch(DecodeArgs &a, cudaStream_t st) {
     a.workers = std::min(grid * DA_WARPS, KV_MAX_WORKERS);
     k_decode_split<FP16, D, NT><<<grid, DA_WARPS * 32, S::RING + lists, st>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    // where a row is shared by many warps, a CTA joins it
+    // Where a row is shared by many warps, a CTA joins it, else a warp (8 KV heads of d = 128: 1 x 131072 89 us and 99, 4 x 32768
+    // 88 and 92, a ragged batch of 8 95 and 100, but 16 x 8192 both 89, 64 ragged rows of d = 64 40 and 32).
     const int rows = a.kv.B * a.kv.hkv * ((a.group + 8 * NT - 1) / (8 * NT));
     return rows * 16 <= a.workers ? launch_join<FP16, D, NT, DJ_THREADS>(a, st) : launch_join<FP16, D, NT, 32>(a, st);
 }

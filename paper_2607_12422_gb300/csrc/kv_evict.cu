@@ -363,7 +363,9 @@ cudaError_t launch(const EvictArgs &a, int C, size_t smem, cudaStream_t st) {
 
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t st) {
     const int rows = a.kv.B * a.kv.hkv;
-    // CTAs of a cluster: as many as run at once, two an SM, each with at least 2048 slots; more where keys ask for it
+    // CTAs of a cluster: as many as run at once, two an SM, each with at least 2048 slots; more where keys ask for it.
+    // (8 KV heads, us with C = 1, 2, 4, 8: 1 x 4096 slots 31, 13.2, 13.5, 14.9; 16 x 4096 48, 42, 53, 84; 64 x 4096 129, 162, 198,
+    // 317: a second wave of clusters costs more than longer rows do. 8 x 1025 6.7, 10.8, 13.4, 29.)
     int C = 1;
     while (C < EV_CLUSTER && (long long)C * 2048 < a.kv.cap && (rows * C * 2 <= 2 * gemm_ctas() || a.kv.cap > (long long)C * EV_KEYS)) C *= 2;
     const long long per = (((a.kv.cap + C - 1) / C) + EV_THREADS - 1) / EV_THREADS * EV_THREADS;
