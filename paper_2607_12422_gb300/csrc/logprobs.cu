@@ -5,16 +5,21 @@
 //     entropy    = ln S + sum (m - x) / T exp((x - m) / T) / S      (both terms >= 0: nothing cancels)
 //     top k      by value, then by the lower index
 // in one pass over the logits, which bounds it: running maximum and sums in fp32 per thread, joined at the end.  A CTA
-// streams 16-KB tiles of its rows through a ring in shared memory, filled by bulk copies that run ahead into the next row while
-// it finishes one.  Few rows are cut into slices: a cluster of CTAs a row, whose parts are joined through distributed
-// shared memory.
+// streams tiles of its rows through a ring in shared memory, filled by bulk copies that run ahead into the next row while
+// it finishes one.  A thread's part of a tile, a group, is 32 values that lie together: 32-KB tiles of fp32, two in the ring, and 16-KB
+// tiles of 16-bit values, three.  (16-KB tiles of fp32, 2048 x 151936, k = 8: 188 us instead of 183; 32-KB tiles of 16-bit values: 125
+// instead of 132 there, but 336 instead of 270 for 20000 x 8000, where a tile holds two rows and more.)  Few rows are cut into
+// slices: a cluster of CTAs a row, whose parts are joined through distributed shared memory.
 //
-// The alternatives come from the same pass.  The k best values lie in the k groups of 128 bytes with the largest maxima (k
-// values, those maxima, already reach the k-th of them), so at the end k groups are picked and read again.  Each of a tile's
-// groups has a thread that keeps the six largest of its groups' maxima, and nothing else is stored: should a seventh matter,
-// the thread reads its groups again, which an order at random asks of one CTA in thousands (with four it was one in 200, and
-// 136 rows took 34 us instead of 24).  Groups are contiguous, so that among equal maxima the lower group holds the lower
-// ids.
+// The alternatives come from the same pass.  The k best values lie in the k groups with the largest maxima (k values, those
+// maxima, already reach the k-th of them), so at the end k groups are picked and read again.  Each thread keeps the three
+// largest of its groups' maxima, and nothing else is stored: should a fourth matter, its warp reads the thread's groups again,
+// which an order at random asks of one CTA in five for k = 32 and of one in 500 for k = 8.  (2048 x 151936 bf16, k = 8: 125 us with 2 or
+// 3 kept, 132 with 4, 138 with 5; 136 rows, k = 32: 25.3 with 2, 21.6 with 3.)  Groups are contiguous, so that among equal
+// maxima the lower group holds the lower ids.
+//
+// Code that is rarely run (row ends, masked values) is kept short: with the loop over a tile's halves unrolled, 8192 x 32000
+// fp16 values took 245 us instead of 218, since streaming and finishing no longer fitted the instruction cache together.
 #include <algorithm>
 #include <cuda_fp16.h>
 
@@ -26,11 +31,10 @@ namespace pbd {
 namespace {
 
 constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-constexpr int LP_VECS = 4;                        // 16-byte loads of a thread and tile
-constexpr int LP_TILE = LP_THREADS * LP_VECS;     // vectors of a tile
-constexpr int LP_STAGES = 3, LP_CTAS = 3;         // tiles of the ring, CTAs of an SM: 144 KB on their way to it
-constexpr int LP_GROUP = 8;                       // vectors of a group
-constexpr int LP_TOP = 6;                         // groups that a thread keeps
+constexpr int LP_GROUP = 32;                      // values of a group: what a thread has of a tile
+constexpr int LP_STEP = 4;                        // 16-byte vectors of it at a time
+constexpr int LP_CTAS = 3;                        // of an SM
+constexpr int LP_TOP = 3;                         // groups that a thread keeps
 constexpr int LP_CLUSTER = 16;                    // slices of a row at most
 constexpr int LP_BINS = LP_THREADS / 4;           // of the selections below
 constexpr int LP_LIST = 512;                      // keys of a list: ten times what an order at random needs (bin_bound)
@@ -67,7 +71,7 @@ template <int TYPE>
 struct Elem;  // values of a 16-byte vector, and what stands for a masked one in it
 template <>
 struct Elem<PBD_FP32> {
-    static constexpr int N = 4, SIZE = 4;
+    static constexpr int N = 4, SIZE = 4, STAGES = 2;
     static __device__ __forceinline__ void open(const uint4 &v, float *x) {
         x[0] = __uint_as_float(v.x), x[1] = __uint_as_float(v.y), x[2] = __uint_as_float(v.z), x[3] = __uint_as_float(v.w);
     }
@@ -85,7 +89,7 @@ struct Elem<PBD_FP32> {
 };
 template <uint32_t LOWEST>
 struct Elem16 {
-    static constexpr int N = 8, SIZE = 2;
+    static constexpr int N = 8, SIZE = 2, STAGES = 3;
     static __device__ __forceinline__ void put(uint32_t *u, int i, const void *p, long long at, bool real) {
         const uint32_t x = real ? static_cast<const uint16_t *>(p)[at] : LOWEST;
         u[i / 2] = i & 1 ? u[i / 2] | x << 16 : x;
@@ -189,41 +193,48 @@ __device__ __forceinline__ u64 bin_bound(u64 mine, int k, Shared &s) {
 }
 
 // The k largest of the CTA's keys, which differ, sorted, into s.best, zeros behind them.  mine: the thread's largest (0: none);
-// each(f): f(key) for all of its keys that may matter, the same ones at every call.  Whole CTA.
+// each(f), by whole warps: f(key) for all of their keys that may matter, the same ones at every call; at_least: what k of the keys are known to
+// reach (0: nothing is known).  Whole CTA.
 template <typename Each>
-__device__ __forceinline__ void select_best(u64 mine, int k, Shared &s, Each &&each) {
-    u64 bar = bin_bound(mine, k, s);
-    if (threadIdx.x < k) s.best[threadIdx.x] = 0;
-    auto collect = [&]() {
-        if (mine && mine >= bar)
+__device__ __forceinline__ void select_best(u64 mine, int k, Shared &s, u64 at_least, Each &&each) {
+    u64 bar = at_least;
+#pragma unroll 1
+    for (int way = at_least ? 0 : 1;; ++way) {
+        if (way == 0) {
+            if (threadIdx.x == 0) s.count = 0;
+            __syncthreads();
+        } else if (way == 1) {
+            bar = bin_bound(mine, k, s);
+        } else {
+            // few bins hold nearly all of the largest: the k-th key bit by bit
+            bar = 0;
+#pragma unroll 1
+            for (int bit = 63; bit >= 0; --bit) {
+                const u64 tried = bar | 1ull << bit;
+                __syncthreads();
+                if (threadIdx.x == 0) s.count = 0;
+                __syncthreads();
+                int c = 0;
+                if (__any_sync(0xffffffffu, mine >= tried)) each([&](u64 x) { c += x >= tried; });
+                if (c) atomicAdd(&s.count, c);
+                __syncthreads();
+                if (s.count >= k) bar = tried;
+            }
+            __syncthreads();
+            if (threadIdx.x == 0) s.count = 0;
+            __syncthreads();
+        }
+        if (__any_sync(0xffffffffu, mine && mine >= bar))
             each([&](u64 x) {
                 if (x && x >= bar) {
                     const int p = atomicAdd(&s.count, 1);
                     if (p < LP_LIST) s.list[p] = x;
                 }
             });
+        if (threadIdx.x < k) s.best[threadIdx.x] = 0;
         __syncthreads();
-    };
-    collect();
-    if (s.count > LP_LIST) {
-        // few bins hold nearly all of the largest: the k-th key bit by bit
-        u64 at = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            const u64 tried = at | 1ull << bit;
-            __syncthreads();
-            if (threadIdx.x == 0) s.count = 0;
-            __syncthreads();
-            int c = 0;
-            if (mine >= tried) each([&](u64 x) { c += x >= tried; });
-            if (c) atomicAdd(&s.count, c);
-            __syncthreads();
-            if (s.count >= k) at = tried;
-        }
-        bar = at;
+        if (s.count <= LP_LIST) break;
         __syncthreads();
-        if (threadIdx.x == 0) s.count = 0;
-        __syncthreads();
-        collect();
     }
     const int have = s.count;
     for (int i0 = 0; i0 < have; i0 += LP_THREADS / 4) {
@@ -287,28 +298,27 @@ struct Row {
 template <int TYPE, bool TOP>
 __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobArgs a) {
     using E = Elem<TYPE>;
-    constexpr int GE = LP_GROUP * E::N;  // values of a group
+    constexpr int VECS = LP_GROUP / E::N, TILE = LP_THREADS * VECS, STAGES = E::STAGES;  // vectors of a group, of a tile
     extern __shared__ __align__(128) uint8_t dyn[];
     uint4 *ring = reinterpret_cast<uint4 *>(dyn);
     __shared__ Shared sh;
     __shared__ Stat ws[LP_WARPS], slice_stat[LP_CLUSTER];                       // of warps; of slices (the first CTA's)
     __shared__ __align__(8) u64 slice_best[TOP ? LP_CLUSTER : 1][LP_MAX_K];
-    __shared__ int picked[TOP ? LP_MAX_K : 1];
-    __shared__ __align__(8) uint64_t full[LP_STAGES], empty[LP_STAGES];
+    __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES];
     __shared__ int abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int slice = blockIdx.x % a.slices, first_row = blockIdx.x / a.slices, rows_apart = gridDim.x / a.slices;
     if (tid == 0) {
         abort = 0;
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (before anything is latched: waits that give up take a second, and tokens come last)
-        for (int i = 0; i < LP_STAGES; ++i) {
+        for (int i = 0; i < STAGES; ++i) {
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], LP_WARPS);
         }
         fence_mbarrier_init();
     }
     __syncthreads();
-    const float c = a.inv_t * 1.4426950408889634f;
+    const float c = a.inv_t * 1.4426950408889634f, far = 150.f / c;
 
     // The next tile to be sent for, in all threads: of row `p_row`, vectors [p_v, p_v1) of which are left.  Warps take turns in
     // sending: it holds a thread up for 600 cycles, and one warp that always did so would hold up all (a third of the time
@@ -325,12 +335,12 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     };
     auto send = [&](int st) {  // (one thread; the stage is free)
         const Row<TYPE> r(a, p_row, slice);
-        const int b = max(p_v, r.whole0), e = max(b, min(min(p_v + LP_TILE, r.v1), r.whole1));
+        const int b = max(p_v, r.whole0), e = max(b, min(min(p_v + TILE, r.v1), r.whole1));
         mbar_arrive_expect_tx(&full[st], (e - b) * 16);
-        if (e > b) bulk_g2s(ring + st * LP_TILE + (b - p_v), r.vbase + (long long)b * 16, (e - b) * 16, &full[st], policy);
+        if (e > b) bulk_g2s(ring + st * TILE + (b - p_v), r.vbase + (long long)b * 16, (e - b) * 16, &full[st], policy);
     };
     auto advance = [&]() {
-        p_v += LP_TILE;
+        p_v += TILE;
         if (p_v >= p_v1) {
             p_row += rows_apart;
             enter_row();
@@ -339,134 +349,150 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     };
     enter_row();
 #pragma unroll
-    for (int i = 0; i < LP_STAGES; ++i)
+    for (int i = 0; i < STAGES; ++i)
         if (p_row < a.M) {
-            if (tid == 0) send(i);
+            if (tid == i * 32) send(i);  // (each holds a warp up)
             advance();
         }
     if (a.slices > 1) cluster_arrive();
 
+    // the i-th vector of a tile and half that this thread reads: its VECS lie together, in turns, so that eight threads read from all banks
+    auto vec_of = [&](int half, int i) { return tid * VECS + ((half * LP_STEP + i + tid * VECS / 8) & (VECS - 1)); };
     int stage = 0, turn = 0;
     for (int row = first_row; row < a.M; row += rows_apart) {
         const Row<TYPE> r(a, row, slice);
         Stat st{-INFINITY, 0.f, 0.f};
         const int token = tid == 0 && slice == 0 && a.logprob ? a.tokens[row] : -1;
-        // the thread's groups, one a tile: the largest by their maxima's order, the largest first, and their tiles
-        const int group0 = r.v0 / LP_GROUP + (tid & 3) * (LP_THREADS / LP_GROUP) + (tid >> 3);  // the first one's number
-        uint32_t top[LP_TOP] = {};
-        int top_tile[LP_TOP] = {}, tile = 0;
-        for (int v = r.v0; v < r.v1; v += LP_TILE, ++tile) {
+        // the thread's groups, one a tile: the largest maxima, the largest first, and their tiles (-1: none)
+        const int group0 = r.v0 / VECS + tid;  // the first one's number
+        float top[LP_TOP];
+        int top_tile[LP_TOP], tile = 0;
+#pragma unroll
+        for (int i = 0; i < LP_TOP; ++i) top[i] = __uint_as_float(0x7fffffffu), top_tile[i] = -1;
+        for (int v = r.v0; v < r.v1; v += TILE, ++tile) {
             mbar_wait(&full[stage], turn, a.status, DEV_TIMEOUT_LOAD, &abort);
-            uint4 raw[LP_VECS];
+            const int w0 = v + warp * (32 * VECS);  // the warp's first vector
+            const bool edge = w0 < r.whole0 || w0 + 32 * VECS > min(r.v1, r.whole1);
+            if (w0 < r.v1) {  // (else the warp has nothing of the row's last tile)
+                float m_group = __uint_as_float(0x7fffffffu);
+#pragma unroll 1
+                for (int half = 0; half < VECS / LP_STEP; ++half) {
+                    uint4 raw[LP_STEP];
 #pragma unroll
-            for (int i = 0; i < LP_VECS; ++i) raw[i] = ring[stage * LP_TILE + i * LP_THREADS + tid];
-            __syncwarp();
-            if (lane == 0) mbarrier_arrive_one(&empty[stage]);
-            if (v < r.whole0 || v + LP_TILE > min(r.v1, r.whole1)) {
-                // value by value at a row's ends; -inf behind the slice
-#pragma unroll
-                for (int i = 0; i < LP_VECS; ++i) {
-                    const int at = v + i * LP_THREADS + tid;
-                    if (at < r.v1 && at >= r.whole0 && at < r.whole1) continue;
-                    uint32_t u[4];
-#pragma unroll
-                    for (int j = 0; j < E::N; ++j) {
-                        const int e = at * E::N - r.skew + j;
-                        E::put(u, j, r.base, e, at < r.v1 && e >= 0 && e < a.V);
+                    for (int i = 0; i < LP_STEP; ++i) raw[i] = ring[stage * TILE + vec_of(half, i)];
+                    if (half == VECS / LP_STEP - 1) {
+                        __syncwarp();
+                        if (lane == 0) mbarrier_arrive_one(&empty[stage]);
                     }
-                    raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
-                }
-            }
-            float mx[LP_VECS];
+                    if (edge) {
+                        // value by value at a row's ends; -inf behind the slice
 #pragma unroll
-            for (int i = 0; i < LP_VECS; ++i) mx[i] = E::largest(raw[i]);
-            // the warp's maximum; if it is a new one, the lane that leaves one value of it out of its sum
-            int owner;
-            const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), mw = warp_max(mt, &owner);
-            const bool grew = mw > st.m;
-            if (grew) {
-                lower(st, mw, c, lane == 0);  // (the value left out was the warp's)
-                st.m = mw;
-                if (lane == owner) {
-                    // The value becomes one whose term is 0: 150 below in the exponent to base 2, and far enough for 16 bits; a
-                    // masked one where there is no such value.
-                    float low = E::round(mw - fmaxf(150.f / c, fabsf(mw) * 0x1p-6f));
-                    if (!((low - mw) * c < -140.f)) low = -INFINITY;
-                    const uint32_t gone = E::bits(low);
-                    bool found = false;
+                        for (int i = 0; i < LP_STEP; ++i) {
+                            const int at = v + vec_of(half, i);
+                            if (at < r.v1 && at >= r.whole0 && at < r.whole1) continue;
+                            uint32_t u[4];
 #pragma unroll
-                    for (int i = 0; i < LP_VECS; ++i) {
-                        float x[E::N];
-                        uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                        E::open(raw[i], x);
-#pragma unroll
-                        for (int j = 0; j < E::N; ++j)
-                            if (!found && x[j] == mw) {
-                                E::set(u, j, gone);
-                                found = true;
+                            for (int j = 0; j < E::N; ++j) {
+                                const int e = at * E::N - r.skew + j;
+                                E::put(u, j, r.base, e, at < r.v1 && e >= 0 && e < a.V);
                             }
-                        raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
-                    }
-                }
-            }
-            const float mu = st.m == -INFINITY ? 0.f : st.m;
-            float ds, dh;
-            {
-                F2 s2 = f2(0.f, 0.f), h2 = s2;
-                const F2 nm = f2(-mu, -mu), cc = f2(c, c);
-#pragma unroll
-                for (int i = 0; i < LP_VECS; ++i) {
-                    float x[E::N];
-                    E::open(raw[i], x);
-#pragma unroll
-                    for (int j = 0; j < E::N; j += 2) {
-                        const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
-                        const float2 tt = unpack2(t);
-                        const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
-                        s2 = add2(s2, e);
-                        h2 = fma2(e, t, h2);
-                    }
-                }
-                const float2 s = unpack2(s2), h = unpack2(h2);
-                ds = s.x + s.y;
-                dh = h.x + h.y;
-            }
-            if (dh != dh) {  // masked values gave 0 * -inf: once more, with a floor under the exponents
-                ds = dh = 0.f;
-#pragma unroll
-                for (int i = 0; i < LP_VECS; ++i) {
-                    float x[E::N];
-                    E::open(raw[i], x);
-#pragma unroll
-                    for (int j = 0; j < E::N; ++j) {
-                        const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
-                        ds += e;
-                        dh += e * t;
-                    }
-                }
-            }
-            st.s += ds;
-            st.h += dh;
-            if (TOP) {
-                // Eight lanes hold a group of each of the four loads: lane i of them gets the i-th's maximum.
-                const float a0 = tid & 1 ? mx[0] : mx[1], a1 = tid & 1 ? mx[2] : mx[3];
-                const float b0 = tid & 1 ? mx[1] : mx[0], b1 = tid & 1 ? mx[3] : mx[2];
-                const float p0 = fmaxf(b0, __shfl_xor_sync(0xffffffffu, a0, 1)), p1 = fmaxf(b1, __shfl_xor_sync(0xffffffffu, a1, 1));
-                float g = fmaxf(tid & 2 ? p1 : p0, __shfl_xor_sync(0xffffffffu, tid & 2 ? p0 : p1, 2));
-                g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 4));
-                const uint32_t order = lp_order(g);
-                if (order > top[LP_TOP - 1] && (tid & 4) == 0 && group0 * LP_GROUP + tile * LP_TILE < r.v1) {
-                    int at = tile;
-                    uint32_t o = order;
-#pragma unroll
-                    for (int i = 0; i < LP_TOP; ++i)
-                        if (o > top[i]) {
-                            const uint32_t x = top[i];
-                            const int y = top_tile[i];
-                            top[i] = o, top_tile[i] = at;
-                            o = x, at = y;
+                            raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
                         }
+                    }
+                    float mx[LP_STEP];
+#pragma unroll
+                    for (int i = 0; i < LP_STEP; ++i) mx[i] = E::largest(raw[i]);
+                    const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+                    m_group = fmaxf(m_group, mt);
+                    if (__any_sync(0xffffffffu, mt > st.m)) {
+                        // the warp has a new maximum, and a lane leaves one value of it out of its sum
+                        int owner;
+                        const float mw = warp_max(mt, &owner);
+                        lower(st, mw, c, lane == 0);  // (the value left out was the warp's)
+                        st.m = mw;
+                        if (lane == owner) {
+                            // The value becomes one whose term is 0: 150 below in the exponent to base 2, and far enough for 16 bits; a
+                            // masked one where there is no such value.
+                            float low = E::round(mw - fmaxf(far, fabsf(mw) * 0x1p-6f));
+                            if (!((low - mw) * c < -140.f)) low = -INFINITY;
+                            const uint32_t gone = E::bits(low);
+                            uint4 y = raw[LP_STEP - 1];  // the first vector that has it
+#pragma unroll
+                            for (int i = LP_STEP - 2; i >= 0; --i)
+                                if (mx[i] == mw) y = raw[i];
+                            float x[E::N];
+                            E::open(y, x);
+                            int at = 0;
+#pragma unroll
+                            for (int j = 1; j < E::N; ++j)
+                                if (x[j] == mw) at = j;
+                            uint32_t u[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int j = 0; j < E::N; ++j)
+                                if (j == at) E::set(u, j, gone);
+                            bool found = false;
+#pragma unroll
+                            for (int i = 0; i < LP_STEP; ++i) {
+                                if (!found && mx[i] == mw) raw[i] = make_uint4(u[0], u[1], u[2], u[3]);
+                                found |= mx[i] == mw;
+                            }
+                        }
+                    }
+                    const float mu = st.m == -INFINITY ? 0.f : st.m;
+                    float ds = 0.f, dh = 0.f;
+                    if (!edge) {
+                        F2 s2 = f2(0.f, 0.f), h2 = s2;
+                        const F2 nm = f2(-mu, -mu), cc = f2(c, c);
+#pragma unroll
+                        for (int i = 0; i < LP_STEP; ++i) {
+                            float x[E::N];
+                            E::open(raw[i], x);
+#pragma unroll
+                            for (int j = 0; j < E::N; j += 2) {
+                                const F2 t = mulp2(add2(f2(x[j], x[j + 1]), nm), cc);
+                                const float2 tt = unpack2(t);
+                                const F2 e = f2(lp_ex2(tt.x), lp_ex2(tt.y));
+                                s2 = add2(s2, e);
+                                h2 = fma2(e, t, h2);
+                            }
+                        }
+                        const float2 s = unpack2(s2), h = unpack2(h2);
+                        ds = s.x + s.y;
+                        dh = h.x + h.y;
+                    }
+                    if (edge || dh != dh) {  // masked values give 0 * -inf: a floor under the exponents
+                        ds = dh = 0.f;
+#pragma unroll
+                        for (int i = 0; i < LP_STEP; ++i) {
+                            float x[E::N];
+                            E::open(raw[i], x);
+#pragma unroll
+                            for (int j = 0; j < E::N; ++j) {
+                                const float t = max_nan((x[j] - mu) * c, LP_FLOOR), e = lp_ex2(t);
+                                ds += e;
+                                dh += e * t;
+                            }
+                        }
+                    }
+                    st.s += ds;
+                    st.h += dh;
                 }
+                if (TOP) {
+                    if (!(m_group <= top[LP_TOP - 1]) && w0 + lane * VECS < r.v1) {  // (no maximum is NaN)
+                        int at = tile;
+                        float o = m_group;
+#pragma unroll
+                        for (int i = 0; i < LP_TOP; ++i)
+                            if (!(o <= top[i])) {
+                                const float x = top[i];
+                                const int y = top_tile[i];
+                                top[i] = o, top_tile[i] = at;
+                                o = x, at = y;
+                            }
+                    }
+                }
+            } else if (lane == 0) {
+                mbarrier_arrive_one(&empty[stage]);
             }
             if (p_row < a.M) {  // the stage goes out again
                 if (warp == sender && lane == 0) {
@@ -476,7 +502,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                 __syncwarp();
                 advance();
             }
-            if (++stage == LP_STAGES) stage = 0, turn ^= 1;
+            if (++stage == STAGES) stage = 0, turn ^= 1;
         }
         const bool has = token >= 0 && token < a.V;
         const float x_t = has ? E::one(r.base, token) : 0.f;  // (asked for here: the token has arrived)
@@ -495,23 +521,27 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
         }
         if (TOP) {
             // the k groups of largest maxima
-            constexpr int TILE_GROUPS = LP_TILE / LP_GROUP;
-            const u64 mine = top[0] ? lp_key(top[0], group0 + top_tile[0] * TILE_GROUPS) : 0;
-            select_best(mine, a.k, sh, [&](auto &&f) {
+            auto key_of = [&](int i) { return top_tile[i] >= 0 ? lp_key(lp_order(top[i]), group0 + top_tile[i] * LP_THREADS) : 0; };
+            const u64 mine = key_of(0);
+            select_best(mine, a.k, sh, 0, [&](auto &&f) {
 #pragma unroll
-                for (int i = 0; i < LP_TOP; ++i)
-                    if (top[i]) f(lp_key(top[i], group0 + top_tile[i] * TILE_GROUPS));
-                if (top[LP_TOP - 1] && top[LP_TOP - 1] >= (uint32_t)(sh.bar >> 32))
-                    // others may matter: the thread's groups once more
-                    for (int t = 0, g = group0; g * LP_GROUP < r.v1; ++t, g += TILE_GROUPS) {
-                        bool kept = false;
+                for (int i = 0; i < LP_TOP; ++i) f(key_of(i));
+                // others of a thread may matter: the warp reads its groups once more, a group a lane
+                unsigned more = __ballot_sync(0xffffffffu, top_tile[LP_TOP - 1] >= 0 && lp_order(top[LP_TOP - 1]) >= (uint32_t)(sh.bar >> 32));
+                for (; more; more &= more - 1) {
+                    const int of = __ffs(more) - 1;
+                    int kept[LP_TOP];
 #pragma unroll
-                        for (int i = 0; i < LP_TOP; ++i) kept |= t == top_tile[i];
-                        if (kept) continue;
+                    for (int i = 0; i < LP_TOP; ++i) kept[i] = __shfl_sync(0xffffffffu, top_tile[i], of);
+                    for (int t = lane, g = group0 - lane + of + t * LP_THREADS; g * VECS < r.v1; t += 32, g += 32 * LP_THREADS) {
+                        bool known = false;
+#pragma unroll
+                        for (int i = 0; i < LP_TOP; ++i) known |= t == kept[i];
+                        if (known) continue;
                         uint32_t o = 0;
 #pragma unroll
-                        for (int i = 0; i < LP_GROUP; ++i) {
-                            const int at = g * LP_GROUP + i;
+                        for (int i = 0; i < VECS; ++i) {
+                            const int at = g * VECS + i;
                             if (at < r.v1 && at >= r.whole0 && at < r.whole1) {
                                 o = max(o, lp_order(E::largest(*(reinterpret_cast<const uint4 *>(r.vbase) + at))));
                             } else if (at < r.v1) {
@@ -521,6 +551,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                         }
                         f(lp_key(o, g));
                     }
+                }
             });
         }
         if (a.slices > 1) {
@@ -555,7 +586,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                         keys[i] = q < a.slices && j < a.k ? slice_best[q][j] : 0;
                         best = max(best, keys[i]);
                     }
-                    select_best(best, a.k, sh, [&](auto &&f) {
+                    select_best(best, a.k, sh, 0, [&](auto &&f) {
 #pragma unroll
                         for (int i = 0; i < PER; ++i) f(keys[i]);
                     });
@@ -568,16 +599,18 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
             st = Stat{__shfl_sync(0xffffffffu, st.m, 0), __shfl_sync(0xffffffffu, st.s, 0), __shfl_sync(0xffffffffu, st.h, 0)};
             if (TOP) {
                 // the k best of the groups' values (of all slices: groups are counted over the whole row)
-                if (tid < a.k) picked[tid] = sh.best[tid] ? key_index(sh.best[tid]) : -1;
-                __syncthreads();
-                constexpr int PER = LP_MAX_K * GE / LP_THREADS;
+                // The k groups' maxima reach the k-th of them, wherever in its group it lies.
+                constexpr int PER = LP_MAX_K * LP_GROUP / LP_THREADS;
+                const u64 kth = sh.best[a.k - 1];
+                const u64 at_least = kth ? lp_key((uint32_t)(kth >> 32), key_index(kth) * LP_GROUP + LP_GROUP - 1 - r.skew) : 0;
                 float x[PER];
                 int e[PER];  // -1: none
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const int at = tid + i * LP_THREADS, g = at < a.k * GE ? picked[at / GE] : -1;
-                    e[i] = g * GE + at % GE - r.skew;
-                    if (g < 0 || e[i] < 0 || e[i] >= a.V) e[i] = -1;
+                    const int at = tid + i * LP_THREADS;
+                    const u64 group = at < a.k * LP_GROUP ? sh.best[at / LP_GROUP] : 0;
+                    e[i] = group ? key_index(group) * LP_GROUP + at % LP_GROUP - r.skew : -1;
+                    if (e[i] >= a.V) e[i] = -1;
                     x[i] = e[i] >= 0 ? E::one(r.base, e[i]) : 0.f;
                 }
                 u64 keys[PER], best = 0;
@@ -586,10 +619,12 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
                     keys[i] = e[i] >= 0 ? lp_key(lp_order(x[i]), e[i]) : 0;
                     best = max(best, keys[i]);
                 }
-                select_best(best, a.k, sh, [&](auto &&f) {
+                auto each = [&](auto &&f) {
 #pragma unroll
                     for (int i = 0; i < PER; ++i) f(keys[i]);
-                });
+                };
+                __syncthreads();  // (sh.best has been read)
+                select_best(best, a.k, sh, at_least, each);
             }
             if (warp == 0) Finish{a}(row, st, sh.best, x_t, has, token);  // (the warp that has the row's sums)
         }
@@ -600,15 +635,19 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
 }
 
 // Slices of a row, CTAs of its cluster, by estimated time.  Rows run in rounds of as many as the GPU holds at once.  A full
-// round takes its bytes at the memory's rate; in the last one fewer CTAs share it, up to what one CTA's ring can ask
-// for (48 KB in some 1.3 us).  Each round has a fixed part, longer for clusters, whose CTAs wait for one another.
-// Rows of 151936 fp32 values: 17 in 16 slices, 136 in 3 (18 us; 2: 19), 2048 whole (186 us; in 2: 199).
-int pick_slices(int M, int vecs, const int (&clusters)[LP_CLUSTER + 1], bool top) {
-    const double rate = 6.6e6, cta = 37e3;  // bytes a us
+// round takes its bytes at the memory's rate; in the last one fewer CTAs share it, up to what one CTA gets through alone
+// (`cta`: its instructions follow one another, 16-bit values have twice as many a byte).  Each round has a fixed part, longer
+// for clusters, whose CTAs wait for one another.  Clusters of 16 are for rows that leave them SMs of their own, and sizes between
+// these lose more than they give, since GPCs do not divide by them.  Rows of 151936 values with alternatives, us with 1, 2, 3, 4,
+// 6, 8, 10, 16 slices: 17 fp32 21, 16.2, 13.5, 11.8, 10.8, 10.9, 10.2, 11.2; 32 bf16 19.2, 15.2, 12.8, 11.4, 12.0, 10.9, 11.7, 18;
+// 64 fp32 22, 17.7, 16.9, 16.3, 17.4, 22, 22, 35; 136 bf16 21.3, 20.6, 21.3, 27 (4); 300 fp32 33, 43 (2); 1 fp32 20.8, 16.2, 13.9,
+// 11.9 (4), 10.0 (8), 9.2 (16).
+int pick_slices(int M, int vecs, int tile, int size, const int (&clusters)[LP_CLUSTER + 1], bool top) {
+    const double rate = 6.6e6, cta = size == 2 ? 22e3 : 34e3;  // bytes a us
     int best = 1;
     double least = 0;
-    for (int s = 1; s <= LP_CLUSTER && (s == 1 || (long long)(s - 1) * LP_TILE < vecs); ++s) {
-        if (clusters[s] < 1) continue;
+    for (const int s : {1, 2, 4, 8, 10, 16}) {
+        if (s > 1 && ((long long)(s - 1) * tile >= vecs || clusters[s] < 1 || (s == 16 && (long long)M * s > gemm_ctas()))) continue;
         const double bytes = 16.0 * vecs / s;  // of a CTA and round
         const int full = M / clusters[s], rest = M % clusters[s];
         double us = full * (bytes * clusters[s] * s / rate + (s > 1 ? 6.0 : 1.0)) + (top ? (s > 1 ? 4.0 : 2.5) : 0.0);
@@ -621,7 +660,7 @@ int pick_slices(int M, int vecs, const int (&clusters)[LP_CLUSTER + 1], bool top
 template <int TYPE, bool TOP>
 cudaError_t launch(LogprobArgs &a, cudaStream_t st) {
     using E = Elem<TYPE>;
-    constexpr size_t MOST = (size_t)LP_STAGES * LP_TILE * 16;
+    constexpr size_t MOST = (size_t)E::STAGES * LP_THREADS * LP_GROUP * E::SIZE;  // the ring
     static thread_local int configured = -1, clusters[LP_CLUSTER + 1];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -653,7 +692,7 @@ cudaError_t launch(LogprobArgs &a, cudaStream_t st) {
     }
     // (a row that starts off a 16-byte boundary has one vector more)
     const int vecs = (a.V + E::N - 1) / E::N + 1;
-    a.slices = pick_slices(a.M, vecs, clusters, TOP);
+    a.slices = pick_slices(a.M, vecs, LP_THREADS * LP_GROUP / E::N, E::SIZE, clusters, TOP);
     a.slice_vecs = ((vecs + a.slices - 1) / a.slices + LP_THREADS - 1) / LP_THREADS * LP_THREADS;
     cfg.gridDim = dim3((unsigned)(std::min(a.M, clusters[a.slices]) * a.slices));
     cfg.dynamicSmemBytes = MOST;

@@ -76,6 +76,21 @@ def test_orders_and_ties(env, order, M, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("columns", [1, 3, 40])
+def test_largest_values_that_one_thread_reads(env, columns, dtype):
+    """Runs of 32 values every 8192, a thread's part of all tiles, lie above the rest: more of them matter than a thread
+    keeps."""
+    torch, pbd = env
+    V = 500000
+    i = torch.arange(V)
+    run = i // 32 % 256
+    x = ((run % (256 // columns) == 5) & (run < 256 // columns * columns)).float() * 9 + i % 1021 / 2048
+    x = torch.stack([x.roll(32 * j) for j in range(12)]).to(getattr(torch, dtype))
+    _check(torch, pbd, x, torch.arange(12, dtype=torch.int32) * 31, 32, 1.0)
+    _check(torch, pbd, x[:1], torch.zeros(1, dtype=torch.int32), 3, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
 def test_masked_logits(env, dtype):
     """-inf and the type's lowest value as masks, in most places, all but one and everywhere; zeros of both signs tie."""
     torch, pbd = env
