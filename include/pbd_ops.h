@@ -158,7 +158,9 @@ size_t pbd_op_evict_workspace_bytes(const pbd_kv_pages *kv, int32_t n_keep);
  * d_weights and d_positions: those arrays themselves, or others apart from them and from one another; slots behind the kept ones are not
  * written.  d_lens is not changed: the caller lowers it to at most n_keep once all layers are through.
  * Requirements: n_recent + n_sink <= n_keep; no two sequences share a page.  The workspace (1024-byte aligned) is scratch;
- * its first word is the status word for pbd_op_status, as for pbd_op_decode_attention. */
+ * its first word is the status word for pbd_op_status: a length outside [0, max_pages * page_size], whose sequence is left as it
+ * is, or a page outside [0, n_pages) among those of a sequence that evicts.  A move from or to a slot of such a page is left
+ * out whole: row, weight and position. */
 pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent, int32_t n_sink,
                         const int32_t *d_next_positions, float *d_out_weights, int32_t *d_out_positions, void *d_ws,
                         size_t ws_bytes, void *d_stream);

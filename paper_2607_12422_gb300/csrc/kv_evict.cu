@@ -109,7 +109,7 @@ __device__ __forceinline__ void move_rows(const EvictArgs &a, int row, int w, in
                     *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(u >> lg & 1 ? a.kv.v : a.kv.k) + at + (u & (pieces - 1)) * 8) = x[j];
             }
         }
-        if (real) {
+        if (dst >= 0) {  // (a move that a bad page leaves out keeps its weight and position as well)
             out_w[d] = weights[s];
             out_pos[d] = pos[s];
         }

@@ -1,0 +1,57 @@
+"""Tables that name pages outside the cache: what is reported leaves the cache's slots as they were."""
+import math
+
+import pytest
+
+import _kv_oracle as ref
+from test_gpu_kv_ops import _handle, _to_gpu, env  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def _bits(x):
+    import torch
+    return x.cpu().contiguous().view({2: torch.int16, 4: torch.int32}[x.element_size()])
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("lens,n_keep", [([100, 70], 40), ([5000, 300], 200)])  # a CTA a row; clusters and the moves' kernel
+def test_evict_moves_nothing_from_or_to_a_bad_page(env, lens, n_keep, in_place):  # noqa: F811
+    """Every other page of the first sequence is outside the cache, in front of the kept slots' end and behind it: rows,
+    weights and positions move together or not at all.  The second sequence is evicted as ever."""
+    torch, pbd = env
+    hkv, D, page = 2, 64, 8
+    c = ref.make_cache(torch, lens, hkv, D, page, torch.bfloat16, extra=0, poison=False, seed=4)
+    gen = torch.Generator().manual_seed(9)
+    for b, n in enumerate(lens):
+        for h in range(hkv):
+            c["positions"][b, h, :n] = torch.randperm(n, generator=gen).int()
+    bad = torch.arange(c["table"].shape[1]) % 2 == 1
+    table = c["table"].clone()
+    table[0, bad] = torch.where(torch.arange(int(bad.sum())) % 4 < 2, torch.tensor(c["k"].shape[0]), torch.tensor(-1)).int()
+    g = _to_gpu(torch, dict(c, table=table))
+    kv = _handle(pbd, g, weights=g["weights"], positions=g["positions"])
+    new_w, new_p = torch.full_like(g["weights"], 7.0), torch.full_like(g["positions"], 7)
+    outs = {} if in_place else dict(out_weights=new_w, out_positions=new_p)
+    with pytest.raises(pbd.PbdError) as e:
+        pbd.pbd_op_evict(kv, n_keep, g["lens"].clone(), n_recent=5, n_sink=3, **outs)
+    assert e.value.status == 6 and "page" in str(e.value)
+    want_w, want_p = (c["weights"].clone(), c["positions"].clone()) if in_place else (new_w.cpu() * 0 + 7, new_p.cpu() * 0 + 7)
+    want_k, want_v = c["k"].clone(), c["v"].clone()
+    left_out = 0
+    for b, n in enumerate(lens):
+        for h in range(hkv):
+            src = ref.evict_row(c["weights"][b, h].tolist(), c["positions"][b, h].tolist(), n, n_keep, n, 5, 3)
+            for i, j in enumerate(src):
+                if b == 0 and i != j and (bad[i // page] or bad[j // page]):
+                    left_out += 1
+                    j = i
+                want_w[b, h, i], want_p[b, h, i] = c["weights"][b, h, j], c["positions"][b, h, j]
+                if i != j:
+                    a, d = (int(c["table"][b, z // page]) for z in (i, j))
+                    want_k[a, h, i % page] = c["k"][d, h, j % page]
+                    want_v[a, h, i % page] = c["v"][d, h, j % page]
+    assert left_out > 0
+    got_w, got_p = (g["weights"], g["positions"]) if in_place else (new_w, new_p)
+    assert torch.equal(_bits(got_w), _bits(want_w)) and torch.equal(got_p.cpu(), want_p)
+    assert torch.equal(_bits(g["k"]), _bits(want_k)) and torch.equal(_bits(g["v"]), _bits(want_v))
