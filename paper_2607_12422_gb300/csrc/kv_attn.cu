@@ -307,7 +307,7 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
                 const uint32_t from = ring + stage * S::UNIT + (i < CPR ? 0 : DA_SLOTS * D * 2) + r * (D * 2) + ((cc ^ (r & 7)) << 4);
                 *reinterpret_cast<float4 *>(to) = ld_shared_v4(from);
             }
-        if (lane == 0 && a.new_pos && a.kv.positions)
+        if (o >= 0 && lane == 0 && a.new_pos && a.kv.positions)
             a.kv.positions[((long long)g.b * a.kv.hkv + g.h) * a.kv.cap + g.n - 1] = rings.fresh[fresh_out].pos;
     };
     // a row's queries as B operands: head 8 nt + lane / 4, dims 16 ks + 2 (lane % 4) and the next, and 8 further on

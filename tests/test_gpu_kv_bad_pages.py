@@ -55,3 +55,52 @@ def test_evict_moves_nothing_from_or_to_a_bad_page(env, lens, n_keep, in_place):
     got_w, got_p = (g["weights"], g["positions"]) if in_place else (new_w, new_p)
     assert torch.equal(_bits(got_w), _bits(want_w)) and torch.equal(got_p.cpu(), want_p)
     assert torch.equal(_bits(g["k"]), _bits(want_k)) and torch.equal(_bits(g["v"]), _bits(want_v))
+
+
+# (small calls; the list of tiles with rows joined by CTAs, by warps, and with chunks of a group)
+WAYS = [([40, 70, 33, 50], 2, 2, 64, 16), ([20000, 70, 33, 4000], 1, 3, 128, 16), ([40, 70, 33, 50] * 40, 2, 4, 64, 8),
+        ([77, 130, 41, 300], 1, 40, 128, 24)]
+
+
+def _with_bad_pages(torch, shape, dtype, seed=1):
+    """A cache whose sequences of each four have a bad page in their middle, for the new token's slot, everywhere and
+    nowhere."""
+    lens, hkv, group, D, page = shape
+    c = ref.make_cache(torch, lens, hkv, D, page, dtype, extra=1, seed=seed)
+    table = c["table"].clone()
+    far = c["k"].shape[0]
+    for b, n in enumerate(lens):
+        if b % 4 == 0:
+            table[b, n // page // 2] = far
+        elif b % 4 == 1:
+            table[b, n // page] = -5
+        elif b % 4 == 2:
+            table[b] = far + 7
+    gen = torch.Generator().manual_seed(seed)
+    B = len(lens)
+    q = (torch.randn(B, hkv * group, D, generator=gen) * 1.5).to(dtype)
+    kn, vn = (torch.randn(B, hkv, D, generator=gen).to(dtype) for _ in range(2))
+    ok = [[0 <= int(table[b, j // page]) < far for j in range(n + 1)] for b, n in enumerate(lens)]
+    return c, table, q, kn, vn, ok
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("shape", WAYS, ids=lambda s: "%dx%d-g%d" % (len(s[0]), max(s[0]), s[2]))
+def test_a_new_token_without_a_page_leaves_its_position_alone(env, shape, dtype):  # noqa: F811
+    torch, pbd = env
+    lens, hkv, page = shape[0], shape[1], shape[4]
+    c, table, q, kn, vn, ok = _with_bad_pages(torch, shape, getattr(torch, dtype))
+    g = _to_gpu(torch, dict(c, table=table))
+    kv = _handle(pbd, g, positions=g["positions"])
+    pos = (torch.arange(len(lens), dtype=torch.int32) + 100000).cuda()
+    with pytest.raises(pbd.PbdError) as e:
+        pbd.pbd_op_decode_attention(q.cuda(), kv, kn.cuda(), vn.cuda(), pos)
+    assert e.value.status == 6 and "page" in str(e.value)
+    want = c["positions"].clone()
+    for b, n in enumerate(lens):
+        if ok[b][n]:
+            want[b, :, n] = 100000 + b
+            p, o = int(table[b, n // page]), n % page
+            c["k"][p, :, o], c["v"][p, :, o] = kn[b], vn[b]
+    assert torch.equal(g["positions"].cpu(), want)
+    assert torch.equal(_bits(g["k"]), _bits(c["k"])) and torch.equal(_bits(g["v"]), _bits(c["v"]))
