@@ -116,6 +116,11 @@ __device__ __forceinline__ int attended(const DecodeArgs &a, int b) {
     return length_ok(a, n) ? n + (a.k_new ? 1 : 0) : 0;
 }
 
+// The table's entry for a slot.
+__device__ __forceinline__ int page_of(const DecodeArgs &a, int b, int slot) {
+    return a.kv.table[(long long)b * a.kv.max_pages + page_index(a.kv, slot)];
+}
+
 // The list of all tiles.  A (sequence, KV head, chunk of its query heads) is a row; it counts as its tiles and ROW more in
 // front, so that stretches with many short rows are shorter.  first[b]: the count of one row of each sequence
 // before b; len[b]: slots attended to.  Whole CTA.
@@ -310,6 +315,22 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
         if (o >= 0 && lane == 0 && a.new_pos && a.kv.positions)
             a.kv.positions[((long long)g.b * a.kv.hkv + g.h) * a.kv.cap + g.n - 1] = rings.fresh[fresh_out].pos;
     };
+    // Slots of pages outside the cache take no part (looked up again: an error path).
+    auto mask_bad = [&](const Tiles &g, float (&s)[NT][4]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int slot = g.t * DA_SLOTS + (lane >> 2) + half * 8;
+            if (slot >= g.n || (unsigned)page_of(a, g.b, slot) < (unsigned)a.kv.n_pages) continue;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) s[nt][2 * half] = s[nt][2 * half + 1] = -INFINITY;
+            if (!a.scores) continue;
+            const int j = g.ch * HEADS + (lane & 3) * 2;
+            float *dst = a.scores + ((long long)g.b * a.hq + g.h * a.group + j) * a.score_pitch + slot;
+#pragma unroll 1
+            for (int i = 0; i < 2 * NT; ++i)  // (heads 8 nt + e of the chunk)
+                if (j + (i >> 1) * 8 + (i & 1) < a.group) dst[((i >> 1) * 8 + (i & 1)) * a.score_pitch] = -INFINITY;
+        }
+    };
     // a row's queries as B operands: head 8 nt + lane / 4, dims 16 ks + 2 (lane % 4) and the next, and 8 further on
     uint32_t qn[Q_AHEAD ? KS : 1][NT][2], qf[KS][NT][2];
     auto load_q = [&](const Tiles &g, auto &q_to) {
@@ -442,12 +463,13 @@ __device__ __forceinline__ bool attend(const DecodeArgs &a, uint32_t ring, Rings
         }
         // m follows the maximum only where a score is above it by more than the slack: what p exceeds 1 by (a factor of 16)
         // fp32 sums and P's halves have room for, and tiles in which nothing has to be done need no exchange.
-        bool grew = false;
+        bool grew = bad;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 4; ++e) grew |= s[nt][e] > m[nt][e & 1] + slack;
         if (__any_sync(0xffffffffu, grew)) {
+            if (__any_sync(0xffffffffu, bad)) mask_bad(at, s);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -591,9 +613,10 @@ __device__ __forceinline__ bool bad_length(const DecodeArgs &a) {
 // Small calls: a cluster of C CTAs a (sequence, KV head).  Its warps take the row's tiles in equal parts; each CTA joins its
 // four warps' results in shared memory and hands maxima and sums to every CTA, and each piece of the outputs to the CTA
 // that finishes it (stores into distributed shared memory, which nobody waits for, where loads from it would each take
-// 0.8 us).  Last, warps add the weights of their own slots.
+// 0.8 us).  Last, warps add the weights of their own slots.  (Bound to the CTAs an SM that shared memory allows: left to itself ptxas takes
+// 72 to 128 registers for d = 64 and 128, and 4 x 900 tokens of d = 64 take 7.6 us instead of 7.1, the ragged batch of 8 with weights 15.4 instead of 14.6.)
 template <bool FP16, int D, int NT>
-__global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeArgs a, int C) {
+__global__ void __launch_bounds__(DA_WARPS * 32, DaShape<D>::CTAS) k_decode_cluster(const DecodeArgs a, int C) {
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, PITCH = D + 4, THREADS = DA_WARPS * 32, D4 = D / 4;
     static_assert(HEADS * PITCH * 4 <= S::STAGES * S::UNIT, "a warp's results lie in its ring");
@@ -633,6 +656,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     const int slot0 = at.t * DA_SLOTS, slot1 = min(n, at.t_end * DA_SLOTS);
     float *wt = a.kv.weights + ((long long)b * a.kv.hkv + h) * a.kv.cap;
     if (a.accumulate && slot0 + lane * 32 < slot1) prefetch_l2(wt + slot0 + lane * 32);
+    const int page_new = a.accumulate && a.k_new && n > 0 ? page_of(a, b, n - 1) : -1;  // (a new token's; used at the end)
     if (at.t < at.t_end) {
         attend<FP16, D, NT>(
             a, smem_u32(ring), rings[warp], at, [&](Tiles &) { return false; },
@@ -710,7 +734,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32) k_decode_cluster(const DecodeAr
     }
     if (a.accumulate) {
         const float *sc = a.scores + ((long long)b * a.hq + h * G) * a.score_pitch;
-        const int fresh = a.k_new ? n - 1 : -1;
+        const int fresh = (unsigned)page_new < (unsigned)a.kv.n_pages ? n - 1 : -1;
         for (int slot = slot0 + lane; slot < slot1; slot += 32) {
             float sum = slot == fresh ? 0.f : wt[slot];
 #pragma unroll 8
@@ -890,22 +914,23 @@ __global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs 
     }
     constexpr int STEP = 128 * DW_VECS;
     float have[DW_VECS][4];
-    auto load_weights = [&](int s0, int s1, int fresh) {
+    auto load_weights = [&](int s0, int s1) {
         const float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
 #pragma unroll
         for (int v = 0; v < DW_VECS; ++v)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int slot = s0 + v * 128 + lane * 4 + i;
-                have[v][i] = slot < s1 && slot != fresh ? wt[slot] : 0.f;
+                have[v][i] = slot < s1 ? wt[slot] : 0.f;
             }
     };
-    load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS), a.k_new ? at.n - 1 : -1);  // (no kernel of this call has written them)
+    load_weights(at.t * DA_SLOTS, min(at.n, at.t_end * DA_SLOTS));  // (no kernel of this call has written them)
     pdl_wait();
     bool begun = true;
     do {
         const int s0 = at.t * DA_SLOTS, s1 = min(at.n, at.t_end * DA_SLOTS);
         float *wt = a.kv.weights + ((long long)at.b * a.kv.hkv + at.h) * a.kv.cap;
+        const int page_new = a.k_new && s1 == at.n ? page_of(a, at.b, at.n - 1) : -1;  // (used when the sums are there)
         for (int g0 = 0; g0 < a.group; g0 += 32) {
             const int heads = min(32, a.group - g0);
             const long long row = (long long)at.b * a.hq + at.h * a.group + g0;
@@ -913,7 +938,7 @@ __global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs 
             if (lane < heads) ml = a.row_ml[row + lane];
             if (ml.x == -INFINITY) ml.x = 0.f;
             for (int s = s0; s < s1; s += STEP) {
-                if (!begun || s != s0 || g0 != 0) load_weights(s, s1, a.k_new && g0 == 0 ? at.n - 1 : -1);
+                if (!begun || s != s0 || g0 != 0) load_weights(s, s1);
                 float sum[DW_VECS][4] = {};
 #pragma unroll 4
                 for (int g = 0; g < heads; ++g) {
@@ -931,12 +956,13 @@ __global__ void __launch_bounds__(DW_THREADS) k_decode_weights(const DecodeArgs 
                         }
                     }
                 }
+                const int fresh = g0 == 0 && (unsigned)page_new < (unsigned)a.kv.n_pages ? at.n - 1 : -1;
 #pragma unroll
                 for (int v = 0; v < DW_VECS; ++v)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int slot = s + v * 128 + lane * 4 + i;
-                        if (slot < s1) wt[slot] = have[v][i] + sum[v][i];
+                        if (slot < s1) wt[slot] = (slot == fresh ? 0.f : have[v][i]) + sum[v][i];
                     }
             }
         }

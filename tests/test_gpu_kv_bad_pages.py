@@ -104,3 +104,55 @@ def test_a_new_token_without_a_page_leaves_its_position_alone(env, shape, dtype)
             c["k"][p, :, o], c["v"][p, :, o] = kn[b], vn[b]
     assert torch.equal(g["positions"].cpu(), want)
     assert torch.equal(_bits(g["k"]), _bits(c["k"])) and torch.equal(_bits(g["v"]), _bits(c["v"]))
+
+
+@pytest.mark.parametrize("append", [False, True])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("shape", WAYS, ids=lambda s: "%dx%d-g%d" % (len(s[0]), max(s[0]), s[2]))
+def test_slots_of_bad_pages_take_no_part(env, shape, dtype, append):  # noqa: F811
+    """A softmax over the slots whose pages exist; the weights of all others keep their bits."""
+    from test_gpu_kv_ops import HALF, _check_attention
+    torch, pbd = env
+    lens, hkv, group, D, page = shape
+    c, table, q, kn, vn, ok = _with_bad_pages(torch, shape, getattr(torch, dtype))
+    g = _to_gpu(torch, dict(c, table=table))
+    kv = _handle(pbd, g, weights=g["weights"], positions=g["positions"])
+    new = (kn.cuda(), vn.cuda()) if append else ()
+    with pytest.raises(pbd.PbdError) as e:
+        pbd.pbd_op_decode_attention(q.cuda(), kv, *new, accumulate=True)
+    assert e.value.status == 6 and "page" in str(e.value)
+    g2 = _to_gpu(torch, dict(c, table=table))
+    kv2 = _handle(pbd, g2, weights=g2["weights"], positions=g2["positions"])
+    ws = pbd.op_workspace(pbd.decode_attention_workspace_bytes(kv2, hkv * group, True))
+    out, lse = pbd.pbd_op_decode_attention(q.cuda(), kv2, *new, accumulate=True, want_lse=True, workspace=ws, sync=False)
+    torch.cuda.synchronize()
+    for b, n in enumerate(lens):
+        m = n + append
+        live = torch.tensor(ok[b][:m], dtype=torch.bool)
+        idx = live.nonzero()[:, 0]
+        one = dict(c, table=c["table"][b:b + 1])  # (the table as it would be without the fault)
+        k, v = ref.rows_of(one, c["k"], 0, n), ref.rows_of(one, c["v"], 0, n)
+        if append:
+            k, v = torch.cat([k, kn[b].double()[:, None]], 1), torch.cat([v, vn[b].double()[:, None]], 1)
+        k, v = (x[:, idx].repeat_interleave(group, 0) for x in (k, v))
+        w = c["weights"][b].double().clone()
+        if append and live[n]:
+            w[:, n] = 0
+        tol = w * (group + 1) * 2.0 ** -23 + 1e-30
+        if len(idx) == 0:
+            assert (out[b] == 0).all() and (lse[b] == -math.inf).all()
+        else:
+            s = torch.einsum("hd,hnd->hn", q[b].double(), k) * D ** -0.5
+            l64 = torch.logsumexp(s, -1)
+            p = torch.exp(s - l64[:, None])
+            mag = torch.einsum("hd,hnd->hn", q[b].double().abs(), k.abs()).amax(-1) * D ** -0.5
+            want = dict(out=torch.einsum("hn,hnd->hd", p, v), lse=l64, p=p, pv=torch.einsum("hn,hnd->hd", p, v.abs()), mag=mag)
+            rel = _check_attention(torch, want, out[b], lse[b], m, HALF["bf16" if dtype == "bfloat16" else "fp16"])
+            pw = p.view(hkv, group, -1)
+            w[:, idx] += pw.sum(1)
+            tol[:, idx] = w[:, idx] * (group + 1) * 2.0 ** -23 + 1e-30 + (pw * rel.view(hkv, group, 1)).sum(1)
+        got = g["weights"][b].cpu()
+        assert ((got.double() - w).abs() <= tol).all()
+        dead = torch.ones(c["cap"], dtype=torch.bool)
+        dead[idx] = False
+        assert torch.equal(_bits(got[:, dead]), _bits(c["weights"][b][:, dead]))
