@@ -107,7 +107,8 @@ typedef enum { PBD_BF16 = 0, PBD_FP16 = 1, PBD_FP32 = 2 } pbd_dtype;
  * Slot j of sequence b is slot j % page_size of page d_page_table[b * max_pages + j / page_size]; its K (and likewise V)
  * of one head starts at d_k + page * stride_page + head * stride_head + (j % page_size) * stride_slot, strides in
  * values, head_dim values in a row.  [page][head][slot][d] and [page][slot][head][d] are both expressed so.
- * Requirements: head_dim 64, 128 or 256; d_k and d_v 16-byte aligned and every stride a multiple of 8; batch <= 1024.
+ * Requirements: head_dim 64, 128 or 256; d_k and d_v 16-byte aligned and every stride a multiple of 8; batch <= 1024;
+ * no stride times its number of pages, heads or slots (in all calls: of rows) beyond 2^60 values.
  * Pages of a sequence's slots [0, d_lens[b]) are read; table entries behind them are not.  Sequences may share pages that
  * a call only reads, and strides may then be 0.  Which token a slot holds is up to the caller: attention does not depend on the order. */
 typedef struct {

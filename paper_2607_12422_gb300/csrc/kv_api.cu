@@ -30,6 +30,9 @@ bool overlap(const void *a, long long na, const void *b, long long nb) {
     return x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
 
+// Whether `n` rows `stride` values apart can be addressed: byte offsets and spans stay below 2^63.
+bool addressable(long long n, long long stride) { return n <= 1 || stride <= (1ll << 60) / (n - 1); }
+
 // What is wrong with a cache's sizes and strides, or null.  Pointers are looked at by the entry points: workspace sizes
 // are asked for before there are any.
 const char *bad_sizes(const pbd_kv_pages *kv) {
@@ -43,6 +46,8 @@ const char *bad_sizes(const pbd_kv_pages *kv) {
     if (kv->stride_page < 0 || kv->stride_head < 0 || kv->stride_slot < 0 || kv->stride_page % 8 || kv->stride_head % 8 ||
         kv->stride_slot % 8)
         return "strides must be multiples of 8 values and not negative";
+    if (!addressable(kv->n_pages, kv->stride_page) || !addressable(kv->n_kv_heads, kv->stride_head) || !addressable(kv->page_size, kv->stride_slot))
+        return "strides reach further than 2^60 values";
     return nullptr;
 }
 
@@ -134,6 +139,8 @@ pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, fl
     const int D = kv->head_dim;
     if (q_stride < (int64_t)n_q_heads * D || q_stride % 8 || (d_k_new && (new_stride < (int64_t)kv->n_kv_heads * D || new_stride % 8)))
         return fail(PBD_ERR_INVALID_ARG, who, "row strides must be multiples of 8 values and hold a row");
+    if (!addressable(kv->batch, q_stride) || (d_k_new && !addressable(kv->batch, new_stride)))
+        return fail(PBD_ERR_INVALID_ARG, who, "row strides reach further than 2^60 values");
     if (const char *w = d_k_new ? bad_rows(kv) : nullptr) return fail(PBD_ERR_INVALID_ARG, who, w);
     const long long B = kv->batch, out_bytes = 2 * B * n_q_heads * D, new_bytes = 2 * ((B - 1) * new_stride + (long long)kv->n_kv_heads * D);
     if (overlap(d_out, out_bytes, d_q, 2 * ((B - 1) * q_stride + (long long)n_q_heads * D)) ||
@@ -228,6 +235,7 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
     if (dtype != PBD_FP32 && dtype != PBD_BF16 && dtype != PBD_FP16) return fail(PBD_ERR_INVALID_ARG, who, "unknown type of logits");
     const int es = dtype == PBD_FP32 ? 4 : 2;
     if (ld < V) return fail(PBD_ERR_INVALID_ARG, who, "rows lie less than V values apart");
+    if (!addressable(M, ld)) return fail(PBD_ERR_INVALID_ARG, who, "rows reach further than 2^60 values");
     if (!(temperature > 0.f) || std::isinf(temperature) || !usable_factor(1.f / temperature))
         return fail(PBD_ERR_INVALID_ARG, who, "temperature and its inverse must be positive and finite");
     if (!d_logits || !aligned(d_logits, es)) return fail(PBD_ERR_INVALID_ARG, who, "logits missing or misaligned");
