@@ -109,6 +109,8 @@ typedef enum { PBD_BF16 = 0, PBD_FP16 = 1, PBD_FP32 = 2 } pbd_dtype;
  * values, head_dim values in a row.  [page][head][slot][d] and [page][slot][head][d] are both expressed so.
  * Requirements: head_dim 64, 128 or 256; d_k and d_v 16-byte aligned and every stride a multiple of 8; batch <= 1024;
  * no stride times its number of pages, heads or slots (in all calls: of rows) beyond 2^60 values.
+ * Calls that write rows (a new token's, eviction's moves): each stride is at least what the dimensions of smaller strides span,
+ * and no row of K lies over one of V; they may lie in turns in one buffer.
  * Pages of a sequence's slots [0, d_lens[b]) are read; table entries behind them are not.  Sequences may share pages that
  * a call only reads, and strides may then be 0.  Which token a slot holds is up to the caller: attention does not depend on the order. */
 typedef struct {

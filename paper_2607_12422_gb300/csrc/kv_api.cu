@@ -60,12 +60,52 @@ const char *bad_cache(const pbd_kv_pages *kv) {
     return nullptr;
 }
 
-// Calls that write K and V: rows must not lie over one another.
+// The dimensions of K or V with more than one place, the smallest stride first; below[i]: what a place of it spans.
+struct Places {
+    int n = 0;
+    long long extent[3], stride[3], below[4];
+    explicit Places(const pbd_kv_pages *kv) {
+        const long long all[3][2] = {{kv->n_pages, kv->stride_page}, {kv->n_kv_heads, kv->stride_head}, {kv->page_size, kv->stride_slot}};
+        for (const auto &x : all) {
+            if (x[0] < 2) continue;
+            int i = n++;
+            for (; i > 0 && stride[i - 1] > x[1]; --i) extent[i] = extent[i - 1], stride[i] = stride[i - 1];
+            extent[i] = x[0];
+            stride[i] = x[1];
+        }
+        below[0] = kv->head_dim;
+        for (int i = 0; i < n; ++i) below[i + 1] = below[i] + (extent[i] - 1) * stride[i];
+    }
+    // whether rows lie apart by strides alone: each stride is at least what the dimensions below it span
+    bool apart() const {
+        for (int i = 0; i < n; ++i)
+            if (stride[i] < below[i]) return false;
+        return true;
+    }
+    // whether a row and one of the same rows moved by `off` values meet (rows lie apart): only the two multiples of a stride
+    // next to `off` can bring it within what lies below
+    bool meet(long long off, int dims) const {
+        if (dims == 0) return off > -below[0] && off < below[0];
+        const long long s = stride[dims - 1], q = off / s, most = extent[dims - 1] - 1;
+        for (long long a = q - 1; a <= q + 1; ++a)
+            if (a >= -most && a <= most && meet(off - a * s, dims - 1)) return true;
+        return false;
+    }
+};
+
+// Calls that write K and V: rows must not lie over one another, nor K's over V's.
 const char *bad_rows(const pbd_kv_pages *kv) {
     const int D = kv->head_dim;
     if ((kv->page_size > 1 && kv->stride_slot < D) || (kv->n_kv_heads > 1 && kv->stride_head < D) || (kv->n_pages > 1 && kv->stride_page < D))
         return "a cache that is written to has strides of a row or more";
+    const Places p(kv);
+    if (!p.apart()) return "the rows of a cache that is written to lie over one another";
     return nullptr;
+}
+const char *k_over_v(const pbd_kv_pages *kv) {
+    const Places p(kv);
+    const long long off = (long long)(reinterpret_cast<uintptr_t>(kv->d_v) - reinterpret_cast<uintptr_t>(kv->d_k)) / 2;
+    return p.meet(off, p.n) ? "K and V of a cache that is written to lie over one another" : nullptr;
 }
 
 // bytes from the first value of K (or V) to the last
@@ -153,6 +193,7 @@ pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, fl
     if (!decode_plan(v, n_q_heads, accumulate != 0, &p))
         return fail(PBD_ERR_CAPACITY, who, "more than 2^31 tiles of 16 slots in all heads and sequences");
     if (const char *w = bad_workspace(d_ws, ws_bytes, p.total)) return fail(PBD_ERR_WORKSPACE, who, w);
+    if (const char *w = d_k_new ? k_over_v(kv) : nullptr) return fail(PBD_ERR_INVALID_ARG, who, w);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     DecodeArgs a{};
     a.kv = v;
@@ -204,6 +245,7 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
                       overlap(d_out_weights, bytes, d_out_positions, bytes)))
         return fail(PBD_ERR_INVALID_ARG, who, "the outputs are the cache's own arrays, both of them, or lie apart from them and from one another");
     if (const char *w = bad_workspace(d_ws, ws_bytes, evict_bytes(v, n_keep))) return fail(PBD_ERR_WORKSPACE, who, w);
+    if (const char *w = k_over_v(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     EvictArgs a{};
     a.kv = v;

@@ -44,3 +44,95 @@ def test_row_strides_that_wrap_are_refused(lib):  # noqa: F811
         assert attend(lib, **kw) == 1 and b"2^60" in lib.pbd_op_last_error(), kw
     for kw in (dict(M=3, ld=1 << 60), dict(M=1 << 30, ld=1 << 31)):
         assert score(lib, **kw) == 1 and b"2^60" in lib.pbd_op_last_error(), kw
+
+
+def accepted(status):
+    """No argument was found wrong: the call got as far as the (absent) GPU."""
+    return status not in (1, 2, 3)
+
+
+def gpu():
+    import torch
+    return torch.cuda.is_available()
+
+
+no_gpu = pytest.mark.skipif("gpu()", reason="addresses that are no memory must not reach a GPU")
+
+PS, H, D = 16, 2, 128  # slots of a page, heads, their size in `cache`
+# strides of pages, heads and slots whose rows lie over one another although each is a row or more
+OVER = [(H * PS * D, D, D),               # head 1 of a slot is head 0 of the next
+        (D, 9 * D, 20 * D),               # ten pages over the next head
+        (PS * D, PS * D, D),              # a page's heads over the next page's
+        (H * PS * D, PS * D - 8, D),      # the last slot's row over the next head's first
+        (H * PS * D - 8, PS * D, D), (H * D, D, H * D),
+        (10 * H * D, 7 * D, D + 8)]       # 16 slots reach over the next head's
+# any order of the dimensions that keeps rows apart
+APART = [(H * PS * D, PS * D, D), (H * PS * D, D, H * D), (D, 10 * PS * D, 10 * D), (H * D, D, 10 * H * D), (2 * H * PS * D, PS * D, D),
+         (H * PS * (D + 8) + 64, PS * (D + 8), D + 8)]
+
+
+@pytest.mark.parametrize("strides", OVER, ids=str)
+def test_written_rows_that_lie_over_one_another_are_refused(lib, strides):  # noqa: F811
+    kv = apart(**dict(zip(("stride_page", "stride_head", "stride_slot"), strides)))
+    assert attend(lib, kv) == 1 and b"rows" in lib.pbd_op_last_error()
+    assert drop(lib, kv) == 1 and b"rows" in lib.pbd_op_last_error()
+
+
+@no_gpu
+def test_other_strides_are_not(lib):  # noqa: F811
+    for strides in APART:
+        kv = apart(**dict(zip(("stride_page", "stride_head", "stride_slot"), strides)))
+        assert accepted(attend(lib, kv)) and accepted(drop(lib, kv)), strides
+    for strides in OVER:  # a cache that is only read
+        kv = apart(**dict(zip(("stride_page", "stride_head", "stride_slot"), strides)))
+        assert accepted(attend(lib, kv, kn=None, vn=None, pos=None)), strides
+    # one page, one head or one slot: that stride does not matter
+    assert accepted(drop(lib, apart(n_pages=1, stride_page=0)))
+    assert accepted(drop(lib, apart(n_kv_heads=1, stride_head=0, stride_page=PS * D)))
+    assert accepted(drop(lib, apart(page_size=1, stride_slot=0, stride_head=D, stride_page=H * D)))
+
+
+def test_written_k_and_v_over_one_another_are_refused(lib):  # noqa: F811
+    page = 2 * H * PS * D  # [page][K or V][head][slot][d]
+    for off in (0, 1, PS, H * PS - 1, 2 * H * PS * 9 + 1, -1, -2 * H * PS):  # rows of V behind K
+        kv = apart(stride_page=page, stride_head=PS * D, stride_slot=D, d_v=A + G + 2 * D * off)
+        assert attend(lib, kv) == 1 and b"K and V" in lib.pbd_op_last_error(), off
+        assert drop(lib, kv) == 1 and b"K and V" in lib.pbd_op_last_error(), off
+    kv = apart(stride_page=page, stride_head=2 * PS * D, stride_slot=2 * D, d_v=A + G + 2 * (D - 8))  # the end of K's row
+    assert attend(lib, kv) == 1 and drop(lib, kv) == 1
+
+
+@no_gpu
+def test_k_and_v_in_turns_are_not(lib):  # noqa: F811
+    # [page][K or V][head][slot][d], [page][head][slot][K or V][d], [page][head][K or V][slot][d]; and a cache that is only read
+    for strides, off in (((2 * H * PS * D, PS * D, D), H * PS), ((2 * H * PS * D, 2 * PS * D, 2 * D), 1),
+                         ((2 * H * PS * D, 2 * PS * D, D), PS), ((2 * H * PS * D, PS * D, D), -H * PS),
+                         ((2 * H * PS * D, PS * D, D), 2 * 10 * H * PS)):
+        kv = apart(**dict(zip(("stride_page", "stride_head", "stride_slot"), strides), d_v=A + G + 2 * D * off))
+        assert accepted(attend(lib, kv)) and accepted(drop(lib, kv)), (strides, off)
+    assert accepted(attend(lib, apart(d_v=A + G), kn=None, vn=None, pos=None))
+
+
+@no_gpu
+def test_rows_over_one_another_by_counting(lib):  # noqa: F811
+    """Random small caches: rows counted out one by one.  Strides that keep rows apart in no order of the dimensions may be
+    refused as well."""
+    import random
+    r = random.Random(3)
+    seen = [0, 0]
+    for _ in range(3000):
+        n, h, s = (r.randint(1, 3) for _ in range(3))
+        st = [64 * r.choice([1, 2, 3, 4, 6, 8, 12]) + 8 * r.choice([0, 0, 1, -1]) for _ in range(3)]
+        off = r.choice([0, 8, 64, 120, 128, 192, 256, 384, 512, 1024, 4096, -64, -128, -512]) + 8 * r.choice([0, 0, 1, -1])
+        kv = apart(n_pages=n, n_kv_heads=h, page_size=s, head_dim=64, stride_page=st[0], stride_head=st[1], stride_slot=st[2], d_v=A + G + 2 * off)
+        rows = sorted(p * st[0] + i * st[1] + j * st[2] for p in range(n) for i in range(h) for j in range(s))
+        over = any(b - a < 64 for a, b in zip(rows, rows[1:]))
+        meet = any(abs(a - b - off) < 64 for a in rows for b in rows)
+        ok = accepted(drop(lib, kv))
+        assert accepted(attention(lib, kv, hq=h, q=A, kn=A + 7 * G, vn=A + 8 * G, ns=h * 64, out=A + 10 * G, ws=A + 12 * G)) == ok
+        seen[ok] += 1
+        if over or meet:
+            assert not ok, (n, h, s, st, off)
+        else:
+            assert ok or b"strides of a row" in lib.pbd_op_last_error() or b"the rows" in lib.pbd_op_last_error(), (n, h, s, st, off)
+    assert min(seen) > 300
