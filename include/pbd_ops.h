@@ -141,7 +141,8 @@ size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n
  * Score, softmax and output sums are fp32; p is split into two 16-bit parts for the tensor cores, so that the output's
  * error is that of its one rounding.
  * Requirements: n_q_heads a multiple of n_kv_heads; scale > 0; d_q, d_out, d_k_new and d_v_new 16-byte aligned, row strides
- * multiples of 8; d_out lies over nothing that is read.  The workspace (1024-byte aligned) is scratch; its first word
+ * multiples of 8; nothing that the call writes (d_out, d_lse_opt, the workspace; with a new token K, V and positions; with accumulate
+ * the weights) lies over anything else that it reads or writes.  The workspace (1024-byte aligned) is scratch; its first word
  * is the status word for pbd_op_status: a length outside [0, max_pages * page_size] (with a new token: one less) or a
  * page outside [0, n_pages) is reported there.  The call then means nothing for that sequence, but does no harm: one with such
  * a length counts as empty, and slots of such a page, a new token's too, are left out: they take no part in the softmax,
@@ -162,7 +163,8 @@ size_t pbd_op_evict_workspace_bytes(const pbd_kv_pages *kv, int32_t n_keep);
  * K and V move in place.  Weights and positions of the kept slots go to d_out_weights and d_out_positions, shaped like
  * d_weights and d_positions: those arrays themselves, or others apart from them and from one another; slots behind the kept ones are not
  * written.  d_lens is not changed: the caller lowers it to at most n_keep once all layers are through.
- * Requirements: n_recent + n_sink <= n_keep; no two sequences share a page.  The workspace (1024-byte aligned) is scratch;
+ * Requirements: n_recent + n_sink <= n_keep; no two sequences share a page; nothing that the call writes (K, V, the outputs, the
+ * workspace) lies over anything else that it reads or writes, weights and positions as their own outputs apart.  The workspace (1024-byte aligned) is scratch;
  * its first word is the status word for pbd_op_status: a length outside [0, max_pages * page_size], whose sequence is left as it
  * is, or a page outside [0, n_pages) among those of a sequence that evicts.  A move from or to a slot of such a page is left
  * out whole: row, weight and position. */

@@ -114,6 +114,39 @@ long long cache_span(const pbd_kv_pages *kv) {
                 (kv->page_size - 1) * kv->stride_slot + kv->head_dim);
 }
 
+// What a call reads and writes: nothing that it writes lies over anything else of it.  (K over V is k_over_v's.)
+class Ranges {
+    struct Range {
+        const void *p;
+        long long bytes;
+        const char *name;
+        bool written;
+    } r[16];
+    int n = 0;
+    char text[96];
+
+public:
+    void add(const char *name, const void *p, long long bytes, bool written) {
+        if (p && n < 16) r[n++] = Range{p, bytes, name, written};
+    }
+    void cache(const pbd_kv_pages *kv, bool written) {
+        add("K", kv->d_k, cache_span(kv), written);
+        add("V", kv->d_v, cache_span(kv), written);
+        add("the page table", kv->d_page_table, 4ll * kv->batch * kv->max_pages, false);
+        add("the lengths", kv->d_lens, 4ll * kv->batch, false);
+    }
+    const char *clash() {
+        for (int i = 0; i < n; ++i)
+            for (int j = 0; j < n; ++j) {
+                if (i == j || !r[i].written || !overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes)) continue;
+                if (i < 2 && j < 2) continue;  // (K and V: `cache` comes first)
+                snprintf(text, sizeof text, "%s, which the call writes, lies over %s", r[i].name, r[j].name);
+                return text;
+            }
+        return nullptr;
+    }
+};
+
 KvView view(const pbd_kv_pages &kv) {
     KvView v{};
     v.k = static_cast<const uint16_t *>(kv.d_k);
@@ -194,6 +227,21 @@ pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, fl
         return fail(PBD_ERR_CAPACITY, who, "more than 2^31 tiles of 16 slots in all heads and sequences");
     if (const char *w = bad_workspace(d_ws, ws_bytes, p.total)) return fail(PBD_ERR_WORKSPACE, who, w);
     if (const char *w = d_k_new ? k_over_v(kv) : nullptr) return fail(PBD_ERR_INVALID_ARG, who, w);
+    Ranges mem;
+    mem.cache(kv, d_k_new != nullptr);
+    mem.add("q", d_q, 2 * ((B - 1) * q_stride + (long long)n_q_heads * D), false);
+    mem.add("k_new", d_k_new, new_bytes, false);
+    mem.add("v_new", d_v_new, new_bytes, false);
+    mem.add("out", d_out, out_bytes, true);
+    mem.add("lse", d_lse_opt, 4 * B * n_q_heads, true);
+    mem.add("the workspace", d_ws, (long long)p.total, true);
+    const long long slots = 4 * B * v.hkv * v.cap;
+    if (accumulate) mem.add("the weights", kv->d_weights, slots, true);
+    if (d_k_new && d_new_positions) {
+        mem.add("new_positions", d_new_positions, 4 * B, false);
+        mem.add("the positions", kv->d_positions, slots, true);
+    }
+    if (const char *w = mem.clash()) return fail(PBD_ERR_INVALID_ARG, who, w);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     DecodeArgs a{};
     a.kv = v;
@@ -246,6 +294,17 @@ pbd_status pbd_op_evict(const pbd_kv_pages *kv, int32_t n_keep, int32_t n_recent
         return fail(PBD_ERR_INVALID_ARG, who, "the outputs are the cache's own arrays, both of them, or lie apart from them and from one another");
     if (const char *w = bad_workspace(d_ws, ws_bytes, evict_bytes(v, n_keep))) return fail(PBD_ERR_WORKSPACE, who, w);
     if (const char *w = k_over_v(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
+    Ranges mem;
+    mem.cache(kv, true);
+    mem.add("the weights", kv->d_weights, bytes, in_place);
+    mem.add("the positions", kv->d_positions, bytes, in_place);
+    mem.add("the next positions", d_next_positions, 4ll * v.B, false);
+    if (!in_place) {
+        mem.add("the weights' output", d_out_weights, bytes, true);
+        mem.add("the positions' output", d_out_positions, bytes, true);
+    }
+    mem.add("the workspace", d_ws, (long long)evict_bytes(v, n_keep), true);
+    if (const char *w = mem.clash()) return fail(PBD_ERR_INVALID_ARG, who, w);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     EvictArgs a{};
     a.kv = v;

@@ -136,3 +136,63 @@ def test_rows_over_one_another_by_counting(lib):  # noqa: F811
         else:
             assert ok or b"strides of a row" in lib.pbd_op_last_error() or b"the rows" in lib.pbd_op_last_error(), (n, h, s, st, off)
     assert min(seen) > 300
+
+
+def overlays(at, written, read, sizes):
+    """Every written array over the beginning and the end of every other one."""
+    for w in written:
+        for other in written + read:
+            if other == w or {w, other} == {"d_k", "d_v"}:
+                continue
+            for to in (at[other], at[other] + (sizes[other] - 16) // 16 * 16):
+                if w == "ws":
+                    to = to // 1024 * 1024
+                yield w, other, to
+
+
+@no_gpu
+def test_what_attention_writes_lies_over_nothing_else(lib):  # noqa: F811
+    at = dict(q=A, d_k=A + G, d_v=A + 2 * G, d_page_table=A + 3 * G, d_lens=A + 4 * G, d_weights=A + 5 * G, d_positions=A + 6 * G, kn=A + 7 * G,
+              vn=A + 8 * G, pos=A + 9 * G, out=A + 10 * G, lse=A + 11 * G, ws=A + 12 * G)
+    B, hq, cap, table = 3, 4, 64, 4
+    kv_bytes = 2 * 10 * H * PS * D
+    sizes = dict(q=2 * B * hq * D, d_k=kv_bytes, d_v=kv_bytes, d_page_table=4 * B * table, d_lens=4 * B, d_weights=4 * B * H * cap,
+                 d_positions=4 * B * H * cap, kn=2 * B * H * D, vn=2 * B * H * D, pos=4 * B, out=2 * B * hq * D, lse=4 * B * hq, ws=1024)
+
+    def call(**moved):
+        x = {**at, **moved}
+        kv = cache(**{n: a for n, a in x.items() if n.startswith("d_")})
+        return attention(lib, kv, acc=1, **{n: a for n, a in x.items() if not n.startswith("d_")})
+
+    assert accepted(call())
+    for w, other, to in overlays(at, ("out", "lse", "ws", "d_k", "d_v", "d_weights", "d_positions"), ("q", "kn", "vn", "pos", "d_page_table", "d_lens"), sizes):
+        assert call(**{w: to}) == 1, (w, other)
+        assert b"lies over" in lib.pbd_op_last_error() or b"lie over" in lib.pbd_op_last_error(), (w, other)
+    # what is only read may lie anywhere, and without a new row or weights so may K, V, weights and positions
+    assert accepted(call(kn=at["q"], vn=at["q"])) and accepted(call(pos=at["d_lens"]))
+    kv = cache(d_k=A + G, d_v=A + G, d_weights=A + G, d_positions=A + G, d_page_table=A + 3 * G, d_lens=A + 3 * G)
+    assert accepted(attention(lib, kv, q=A + G, out=at["out"], ws=at["ws"]))
+
+
+@no_gpu
+def test_what_eviction_writes_lies_over_nothing_else(lib):  # noqa: F811
+    at = dict(d_k=A + G, d_v=A + 2 * G, d_page_table=A + 3 * G, d_lens=A + 4 * G, d_weights=A + 5 * G, d_positions=A + 6 * G, nxt=A + 9 * G,
+              ow=A + 10 * G, op=A + 11 * G, ws=A + 12 * G)
+    B, cap, table = 3, 64, 4
+    kv_bytes = 2 * 10 * H * PS * D
+    sizes = dict(d_k=kv_bytes, d_v=kv_bytes, d_page_table=4 * B * table, d_lens=4 * B, d_weights=4 * B * H * cap, d_positions=4 * B * H * cap,
+                 nxt=4 * B, ow=4 * B * H * cap, op=4 * B * H * cap, ws=1024)
+
+    def call(**moved):
+        x = {**at, **moved}
+        kv = cache(**{n: a for n, a in x.items() if n.startswith("d_")})
+        return evict(lib, kv, **{n: a for n, a in x.items() if not n.startswith("d_")})
+
+    assert accepted(call()) and accepted(call(ow=at["d_weights"], op=at["d_positions"]))
+    written, read = ("d_k", "d_v", "ow", "op", "ws"), ("d_page_table", "d_lens", "d_weights", "d_positions", "nxt")
+    for w, other, to in overlays(at, written, read, sizes):
+        assert call(**{w: to}) == 1, (w, other)
+    # in place, weights and positions are written
+    for moved in (dict(d_weights=at["d_positions"], ow=at["d_positions"], op=at["d_positions"]), dict(d_weights=at["d_k"], ow=at["d_k"], op=at["d_positions"]),
+                  dict(d_positions=at["nxt"], op=at["nxt"], ow=at["d_weights"]), dict(d_weights=at["d_lens"], ow=at["d_lens"], op=at["d_positions"])):
+        assert call(**moved) == 1, moved
