@@ -184,8 +184,9 @@ size_t pbd_op_token_logprobs_workspace_bytes(int32_t M, int32_t V, int32_t k);
  * pbd_op_status (DEV_BAD_TOKEN) and gives NaN.  d_entropy_opt [M] fp32 or NULL.  d_top_ids [M, k] int32 and
  * d_top_logprobs [M, k] fp32, not read for k = 0.  Logits of -inf are masked; a row with nothing else has log
  * probabilities of -inf and entropy 0.  A row that holds NaN or +inf gives NaN (and ids that say nothing).
- * Requirements: 1 <= M <= 2^30, 1 <= V <= 2^30, ld >= V, 0 <= k <= min(32, V); temperature > 0.  Sums are fp32.  The workspace (1024-byte
- * aligned) is scratch; its first word is the status word for pbd_op_status. */
+ * Requirements: 1 <= M <= 2^30, 1 <= V <= 2^30, ld >= V, 0 <= k <= min(32, V); temperature > 0; no output lies over the logits, the
+ * tokens, the workspace or another output.  Sums are fp32.  The workspace (1024-byte aligned) is scratch; its first word is
+ * the status word for pbd_op_status. */
 pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void *d_logits, int64_t ld, float temperature,
                                  const int32_t *d_tokens_opt, int32_t k, float *d_logprob_opt, float *d_entropy_opt,
                                  int32_t *d_top_ids, float *d_top_logprobs, void *d_ws, size_t ws_bytes, void *d_stream);

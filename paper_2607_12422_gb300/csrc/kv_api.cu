@@ -123,6 +123,7 @@ class Ranges {
         bool written;
     } r[16];
     int n = 0;
+    bool has_cache = false;  // (its K and V come first)
     char text[96];
 
 public:
@@ -130,6 +131,7 @@ public:
         if (p && n < 16) r[n++] = Range{p, bytes, name, written};
     }
     void cache(const pbd_kv_pages *kv, bool written) {
+        has_cache = true;
         add("K", kv->d_k, cache_span(kv), written);
         add("V", kv->d_v, cache_span(kv), written);
         add("the page table", kv->d_page_table, 4ll * kv->batch * kv->max_pages, false);
@@ -139,7 +141,7 @@ public:
         for (int i = 0; i < n; ++i)
             for (int j = 0; j < n; ++j) {
                 if (i == j || !r[i].written || !overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes)) continue;
-                if (i < 2 && j < 2) continue;  // (K and V: `cache` comes first)
+                if (has_cache && i < 2 && j < 2) continue;
                 snprintf(text, sizeof text, "%s, which the call writes, lies over %s", r[i].name, r[j].name);
                 return text;
             }
@@ -346,6 +348,17 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
         (k > 0 && (!aligned(d_top_ids, 4) || !aligned(d_top_logprobs, 4))))
         return fail(PBD_ERR_INVALID_ARG, who, "32-bit arrays must be 4-byte aligned");
     if (const char *w = bad_workspace(d_ws, ws_bytes, need)) return fail(PBD_ERR_WORKSPACE, who, w);
+    Ranges mem;
+    mem.add("the logits", d_logits, es * ((M - 1) * ld + V), false);
+    mem.add("the tokens", d_tokens_opt, 4ll * M, false);
+    mem.add("the log probabilities", d_logprob_opt, 4ll * M, true);
+    mem.add("the entropy", d_entropy_opt, 4ll * M, true);
+    if (k > 0) {
+        mem.add("the top ids", d_top_ids, 4ll * M * k, true);
+        mem.add("their log probabilities", d_top_logprobs, 4ll * M * k, true);
+    }
+    mem.add("the workspace", d_ws, (long long)need, true);
+    if (const char *w = mem.clash()) return fail(PBD_ERR_INVALID_ARG, who, w);
     LogprobArgs a{};
     a.x = d_logits;
     a.ld = ld;

@@ -196,3 +196,20 @@ def test_what_eviction_writes_lies_over_nothing_else(lib):  # noqa: F811
     for moved in (dict(d_weights=at["d_positions"], ow=at["d_positions"], op=at["d_positions"]), dict(d_weights=at["d_k"], ow=at["d_k"], op=at["d_positions"]),
                   dict(d_positions=at["nxt"], op=at["nxt"], ow=at["d_weights"]), dict(d_weights=at["d_lens"], ow=at["d_lens"], op=at["d_positions"])):
         assert call(**moved) == 1, moved
+
+
+@no_gpu
+def test_what_log_probabilities_write_lies_over_nothing_else(lib):  # noqa: F811
+    at = dict(x=A, tok=A + G, lp=A + 2 * G, ent=A + 3 * G, ids=A + 4 * G, top=A + 5 * G, ws=A + 6 * G)
+    M, V, ld, k = 40, 100, 120, 4
+    sizes = dict(x=4 * ((M - 1) * ld + V), tok=4 * M, lp=4 * M, ent=4 * M, ids=4 * M * k, top=4 * M * k, ws=1024)
+
+    def call(**moved):
+        return score(lib, M=M, V=V, ld=ld, k=k, **{**at, **moved})
+
+    assert accepted(call())
+    for w, other, to in overlays(at, ("lp", "ent", "ids", "top", "ws"), ("x", "tok"), sizes):
+        assert call(**{w: to}) == 1 and b"lies over" in lib.pbd_op_last_error(), (w, other)
+    # what is read may lie anywhere, behind the last row is free, and what is not asked for is not looked at
+    assert accepted(call(tok=at["x"])) and accepted(call(lp=at["x"] + sizes["x"])) and accepted(call(ent=None))
+    assert accepted(score(lib, M=M, V=V, ld=ld, k=0, **{**at, "ids": at["x"], "top": at["lp"]}))
