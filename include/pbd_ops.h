@@ -195,7 +195,7 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
  * pointer that call was given): waits for d_stream, then reads the status word at the start of d_ws.  PBD_OK when no
  * kernel latched an error; PBD_ERR_DEVICE with the latched code in *h_device_code (may be NULL) otherwise, and that
  * call's outputs are invalid; PBD_ERR_INVALID_ARG for a null or misaligned d_ws; PBD_ERR_CUDA if the stream failed.
- * What kernels latch: a device wait bounded at one second that runs out (linear, lm_head), and lengths, pages (7) and
+ * What kernels latch: a device wait bounded at one second that runs out (linear, lm_head, token_logprobs), and lengths, pages (7) and
  * tokens (4) in device memory that lie outside their range (5: a length), which the host cannot check. */
 pbd_status pbd_op_status(const void *d_ws, void *d_stream, int32_t *h_device_code);
 

@@ -305,13 +305,14 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     __shared__ Stat ws[LP_WARPS], slice_stat[LP_CLUSTER];                       // of warps; of slices (the first CTA's)
     __shared__ __align__(8) u64 slice_best[TOP ? LP_CLUSTER : 1][LP_MAX_K];
     __shared__ __align__(8) uint64_t full[STAGES], empty[STAGES];
-    __shared__ int abort;
+    __shared__ int abort, sent[STAGES];  // (sent: tiles sent for into each stage)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int slice = blockIdx.x % a.slices, first_row = blockIdx.x / a.slices, rows_apart = gridDim.x / a.slices;
     if (tid == 0) {
         abort = 0;
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (before anything is latched: waits that give up take a second, and tokens come last)
         for (int i = 0; i < STAGES; ++i) {
+            sent[i] = 0;
             mbar_init(&full[i], 1);
             mbar_init(&empty[i], LP_WARPS);
         }
@@ -336,6 +337,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
     auto send = [&](int st) {  // (one thread; the stage is free)
         const Row<TYPE> r(a, p_row, slice);
         const int b = max(p_v, r.whole0), e = max(b, min(min(p_v + TILE, r.v1), r.whole1));
+        ++sent[st];
         mbar_arrive_expect_tx(&full[st], (e - b) * 16);
         if (e > b) bulk_g2s(ring + st * TILE + (b - p_v), r.vbase + (long long)b * 16, (e - b) * 16, &full[st], policy);
     };
@@ -369,7 +371,9 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
         int top_tile[LP_TOP], tile = 0;
 #pragma unroll
         for (int i = 0; i < LP_TOP; ++i) top[i] = __uint_as_float(0x7fffffffu), top_tile[i] = -1;
-        for (int v = r.v0; v < r.v1; v += TILE, ++tile) {
+        const bool given_up = __any_sync(0xffffffffu, *(volatile int *)&abort);  // (further rows have no tiles then)
+        for (int v = given_up ? r.v1 : r.v0; v < r.v1; v += TILE, ++tile) {
+            // (after a wait that ran out the row goes on with whatever the ring holds, and no thread waits for long again)
             mbar_wait(&full[stage], turn, a.status, DEV_TIMEOUT_LOAD, &abort);
             const int w0 = v + warp * (32 * VECS);  // the warp's first vector
             const bool edge = w0 < r.whole0 || w0 + 32 * VECS > min(r.v1, r.whole1);
@@ -496,8 +500,7 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
             }
             if (p_row < a.M) {  // the stage goes out again
                 if (warp == sender && lane == 0) {
-                    mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort);
-                    send(stage);
+                    if (mbar_wait(&empty[stage], turn, a.status, DEV_TIMEOUT_SLOT, &abort) && !*(volatile int *)&abort) send(stage);
                 }
                 __syncwarp();
                 advance();
@@ -631,6 +634,9 @@ __global__ void __launch_bounds__(LP_THREADS, LP_CTAS) k_logprobs(const LogprobA
         __syncthreads();  // (best and ws are the next row's)
     }
     if (a.slices > 1) cluster_wait();
+    if (tid == 0 && *(volatile int *)&abort)  // error path: the copies in flight get a bounded chance to land
+        for (int i = 0; i < STAGES; ++i)
+            if (sent[i] > 0 && !mbar_wait(&full[i], (sent[i] - 1) & 1, nullptr, 0, nullptr)) break;  // (all had this second)
     if (blockIdx.x == a.slices - 1) check_tokens(a);  // (which has nothing else to do by now)
 }
 
