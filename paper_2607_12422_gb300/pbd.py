@@ -243,6 +243,11 @@ def _bad(who, what):
     raise PbdError(1, "%s: %s" % (who, what))
 
 
+def _int32(*values):
+    """Whether 32 bits hold the numbers (ctypes hands on the low ones of any)."""
+    return all(-1 << 31 <= x < 1 << 31 for x in values)
+
+
 _DTYPES = {"torch.bfloat16": PBD_BF16, "torch.float16": PBD_FP16, "torch.float32": PBD_FP32}
 
 
@@ -329,6 +334,8 @@ class PagedKV:
             _bad(who, "the values of a head are not contiguous")
         B, max_pages = page_table.shape
         n_pages, hkv, ps, D = k.shape
+        if not _int32(B, max_pages, n_pages, hkv, ps, D):
+            _bad(who, "a size does not fit 32 bits")
         _check(who, "page_table", page_table, k, (B, max_pages), torch.int32)
         _check(who, "lens", lens, k, (B,), torch.int32)
         for name, t, dt in (("weights", weights, torch.float32), ("positions", positions, torch.int32)):
@@ -345,7 +352,7 @@ class PagedKV:
 
 
 def decode_attention_workspace_bytes(kv: PagedKV, n_q_heads: int, accumulate: bool = False) -> int:
-    return load().pbd_op_decode_attention_workspace_bytes(kv.ref, n_q_heads, int(accumulate))
+    return load().pbd_op_decode_attention_workspace_bytes(kv.ref, n_q_heads, int(accumulate)) if _int32(n_q_heads) else 0
 
 
 def pbd_op_decode_attention(q, kv: PagedKV, k_new=None, v_new=None, new_positions=None, scale: Optional[float] = None,
@@ -400,7 +407,7 @@ def pbd_op_decode_attention(q, kv: PagedKV, k_new=None, v_new=None, new_position
 
 
 def evict_workspace_bytes(kv: PagedKV, n_keep: int) -> int:
-    return load().pbd_op_evict_workspace_bytes(kv.ref, n_keep)
+    return load().pbd_op_evict_workspace_bytes(kv.ref, n_keep) if _int32(n_keep) else 0
 
 
 def pbd_op_evict(kv: PagedKV, n_keep: int, next_positions, n_recent: int = 0, n_sink: int = 0, out_weights=None,
@@ -425,6 +432,8 @@ def pbd_op_evict(kv: PagedKV, n_keep: int, next_positions, n_recent: int = 0, n_
     else:
         _check(who, "out_weights", out_weights, kv, kv.weights.shape, torch.float32)
         _check(who, "out_positions", out_positions, kv, kv.weights.shape, torch.int32)
+    if not _int32(n_recent, n_sink):
+        _bad(who, "n_recent or n_sink does not fit 32 bits")
     _check(who, "next_positions", next_positions, kv, (kv.batch,), torch.int32)
     need = kv._need.get(n_keep)
     if need is None:  # (sizes of a handle do not change)
@@ -447,7 +456,7 @@ class TokenLogprobs(NamedTuple):
 
 
 def token_logprobs_workspace_bytes(M: int, V: int, k: int = 0) -> int:
-    return load().pbd_op_token_logprobs_workspace_bytes(M, V, k)
+    return load().pbd_op_token_logprobs_workspace_bytes(M, V, k) if _int32(M, V, k) else 0
 
 
 def pbd_op_token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 1.0, workspace=None, sync: bool = True):
@@ -470,7 +479,7 @@ def pbd_op_token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 
     logprob = ids = top = None
     if tokens is not None:
         _check(who, "tokens", tokens, logits, (M,), torch.int32)
-    ws = _scratch(who, workspace, L.pbd_op_token_logprobs_workspace_bytes(M, V, k), dev)
+    ws = _scratch(who, workspace, token_logprobs_workspace_bytes(M, V, k), dev)
     entropy = torch.empty(M, dtype=torch.float32, device=dev)
     if tokens is not None:
         logprob = torch.empty(M, dtype=torch.float32, device=dev)
