@@ -620,6 +620,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32, DaShape<D>::CTAS) k_decode_clus
     using S = DaShape<D>;
     constexpr int HEADS = 8 * NT, KS = D / 16, PITCH = D + 4, THREADS = DA_WARPS * 32, D4 = D / 4;
     static_assert(HEADS * PITCH * 4 <= S::STAGES * S::UNIT, "a warp's results lie in its ring");
+    static_assert(KV_MAX_BATCH * 4 <= S::RING, "the status word's CTA keeps a number a sequence in the rings' place");
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) Rings<S::STAGES> rings[DA_WARPS];
     __shared__ float2 warp_ml[DA_WARPS][HEADS], row_ml[HEADS];
@@ -629,13 +630,7 @@ __global__ void __launch_bounds__(DA_WARPS * 32, DaShape<D>::CTAS) k_decode_clus
     if (row == a.kv.B * a.kv.hkv) {  // one cluster more: the call's status word has one writer
         if (rank != 0) return;
         const bool length = bad_length(a);
-        bool page = false;
-#pragma unroll 8
-        for (int i = tid; i < a.kv.B * a.kv.max_pages; i += THREADS) {  // (clusters mean short tables)
-            const int s = i / a.kv.max_pages, at = i - s * a.kv.max_pages;
-            if (at * a.kv.page_size < attended(a, s)) page |= (unsigned)a.kv.table[i] >= (unsigned)a.kv.n_pages;
-        }
-        page = __syncthreads_or(page);
+        const bool page = any_bad_page<THREADS>(a.kv, reinterpret_cast<int *>(smem), [&](int s) { return attended(a, s); });
         if (tid == 0) *a.status = length ? DEV_BAD_POSITION : page ? DEV_BAD_PAGE : DEV_OK;
         return;
     }
