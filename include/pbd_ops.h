@@ -140,6 +140,8 @@ size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n
  * from 0.  The sums run in an order fixed by the sizes and lengths: repeated calls give the same bits.
  * Score, softmax and output sums are fp32; p is split into two 16-bit parts for the tensor cores, so that the output's
  * error is that of its one rounding.
+ * Attended values of V are finite, in bf16 at most 2^123 / slots (fp32 sums of p v, p up to 16, must not overflow): an infinite one
+ * makes its dimension of the head's outputs NaN or infinite, and no other.
  * Requirements: n_q_heads a multiple of n_kv_heads; scale > 0; d_q, d_out, d_k_new and d_v_new 16-byte aligned, row strides
  * multiples of 8; nothing that the call writes (d_out, d_lse_opt, the workspace; with a new token K, V and positions; with accumulate
  * the weights) lies over anything else that it reads or writes.  The workspace (1024-byte aligned) is scratch; its first word
