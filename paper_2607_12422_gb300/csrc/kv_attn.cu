@@ -999,9 +999,9 @@ cudaError_t launch_join(DecodeArgs &a, cudaStream_t st) {
 }
 
 // CTAs of a (sequence, KV head)'s cluster, or 0 where the list of tiles is the better way: clusters where all of them run at
-// once and no warp has more than DA_CLUSTER_TILES tiles. (Clusters and list, 8 KV heads of d = 128: 1 x 2048 8.0 us and 10.0,
-// 1 x 8192 13.6 and 14.7, 8 x 1757 14.3 and 18.1; a ragged batch of 8, where the longest row sets the time, 12.5 and 13.7, with
-// weights 15.8 and 14.6: the host does not know the lengths. Longer rows than the bound's spread better over the list.)
+// once and no warp has more than DA_CLUSTER_TILES tiles. (Clusters and list, 8 KV heads of d = 128: 1 x 2048 6.3 us and 9.0,
+// 1 x 8192 11.8 and 14.0, 8 x 1757 13.9 and 16.8; a ragged batch of 8, where the longest row sets the time, 10.7 and 11.9, with
+// weights 14.2 and 16.6; 4 x 900 of d = 64 with weights 7.1 and 13.3. Longer rows than the bound's spread better over the list.)
 int pick_cluster(const DecodeArgs &a, int ctas, int most) {
     const long long rows = (long long)a.kv.B * a.kv.hkv, tiles = (a.kv.cap + DA_SLOTS - 1) / DA_SLOTS;
     if (a.group > 16 || rows > ctas) return 0;

@@ -50,7 +50,7 @@ __device__ __forceinline__ uint32_t order_key(float w, int pos, int n_sink, int 
 }
 
 // Slots of sequence b; none where the length is outside its range.  Such lengths and pages are reported once for the call: the
-// grid's last cluster looks at all of them, so that the status word has one writer and needs no clearing before.
+// grid's last cluster looks at all of them that are in use, so that the status word has one writer and needs no clearing before.
 __device__ __forceinline__ int slots_of(const EvictArgs &a, int b) {
     const int n = a.kv.lens[b];
     return n >= 0 && n <= a.kv.cap ? n : 0;
@@ -362,7 +362,7 @@ cudaError_t launch(const EvictArgs &a, int C, size_t smem, cudaStream_t st) {
 
 cudaError_t launch_evict(const EvictArgs &a, cudaStream_t st) {
     const int rows = a.kv.B * a.kv.hkv;
-    // CTAs of a cluster: as many as run at once, two an SM, each with at least 2048 slots; more where keys ask for it.
+    // CTAs of a cluster: as many as run at once, two an SM, each with more than 1024 slots; more where keys ask for it.
     // (8 KV heads, us with C = 1, 2, 4, 8: 1 x 4096 slots 31, 13.2, 13.5, 14.9; 16 x 4096 48, 42, 53, 84; 64 x 4096 129, 162, 198,
     // 317: a second wave of clusters costs more than longer rows do. 8 x 1025 6.7, 10.8, 13.4, 29.)
     int C = 1;

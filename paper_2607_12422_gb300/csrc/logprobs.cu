@@ -7,16 +7,17 @@
 // in one pass over the logits, which bounds it: running maximum and sums in fp32 per thread, joined at the end.  A CTA
 // streams tiles of its rows through a ring in shared memory, filled by bulk copies that run ahead into the next row while
 // it finishes one.  A thread's part of a tile, a group, is 32 values that lie together: 32-KB tiles of fp32, two in the ring, and 16-KB
-// tiles of 16-bit values, three.  (16-KB tiles of fp32, 2048 x 151936, k = 8: 188 us instead of 183; 32-KB tiles of 16-bit values: 125
-// instead of 132 there, but 336 instead of 270 for 20000 x 8000, where a tile holds two rows and more.)  Few rows are cut into
+// tiles of 16-bit values, three.  (16-KB tiles of fp32, groups of 16, 2048 x 151936, k = 8: 191 us instead of 185; 32-KB tiles of 16-bit
+// values, groups of 64: 125 instead of 132 there, but 346 instead of 278 for 20000 x 8000, where a tile holds two rows and more, and
+// 22.9 instead of 21.7 for 136 x 151936, k = 32.)  Few rows are cut into
 // slices: a cluster of CTAs a row, whose parts are joined through distributed shared memory.
 //
 // The alternatives come from the same pass.  The k best values lie in the k groups with the largest maxima (k values, those
 // maxima, already reach the k-th of them), so at the end k groups are picked and read again.  Each thread keeps the three
 // largest of its groups' maxima, and nothing else is stored: should a fourth matter, its warp reads the thread's groups again,
-// which an order at random asks of one CTA in five for k = 32 and of one in 500 for k = 8.  (2048 x 151936 bf16, k = 8: 125 us with 2 or
-// 3 kept, 132 with 4, 138 with 5; 136 rows, k = 32: 25.3 with 2, 21.6 with 3.)  Groups are contiguous, so that among equal
-// maxima the lower group holds the lower ids.
+// which an order at random asks of one CTA in five for k = 32 and of one in 500 for k = 8.  (2048 x 151936 bf16, k = 8: 128 us with 2
+// kept, 132 with 3, 138 with 4, 145 with 5; 136 rows, k = 32: 23.7 with 2, 21.7 with 3 and 21.6 with 4.)  Groups are contiguous, so
+// that among equal maxima the lower group holds the lower ids.
 //
 // Code that is rarely run (row ends, masked values) is kept short: with the loop over a tile's halves unrolled, 8192 x 32000
 // fp16 values took 245 us instead of 218, since streaming and finishing no longer fitted the instruction cache together.
