@@ -148,7 +148,7 @@ size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n
  * is the status word for pbd_op_status: a length outside [0, max_pages * page_size] (with a new token: one less) or a
  * page outside [0, n_pages) is reported there.  The call then means nothing for that sequence, but does no harm: one with such
  * a length counts as empty, and slots of such a page, a new token's too, are left out: they take no part in the softmax,
- * and their K, V, weights and positions stay as they are. */
+ * and their K, V, weights and positions stay as they are (in a KV head one of whose scores is NaN all weights become NaN). */
 pbd_status pbd_op_decode_attention(const pbd_kv_pages *kv, int32_t n_q_heads, float scale, const void *d_q, int64_t q_stride,
                                    const void *d_k_new, const void *d_v_new, int64_t new_stride,
                                    const int32_t *d_new_positions, int32_t accumulate, void *d_out, float *d_lse_opt,
