@@ -432,7 +432,7 @@ def pbd_op_evict(kv: PagedKV, n_keep: int, next_positions, n_recent: int = 0, n_
     else:
         _check(who, "out_weights", out_weights, kv, kv.weights.shape, torch.float32)
         _check(who, "out_positions", out_positions, kv, kv.weights.shape, torch.int32)
-    if not _int32(n_recent, n_sink):
+    if not (-1 << 31 <= n_recent < 1 << 31 and -1 << 31 <= n_sink < 1 << 31):
         _bad(who, "n_recent or n_sink does not fit 32 bits")
     _check(who, "next_positions", next_positions, kv, (kv.batch,), torch.int32)
     need = kv._need.get(n_keep)
@@ -479,7 +479,9 @@ def pbd_op_token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 
     logprob = ids = top = None
     if tokens is not None:
         _check(who, "tokens", tokens, logits, (M,), torch.int32)
-    ws = _scratch(who, workspace, token_logprobs_workspace_bytes(M, V, k), dev)
+    if M >> 31 or V >> 31 or not -1 << 31 <= k < 1 << 31:  # (_int32, without its call)
+        _bad(who, "a size does not fit 32 bits")
+    ws = _scratch(who, workspace, L.pbd_op_token_logprobs_workspace_bytes(M, V, k), dev)
     entropy = torch.empty(M, dtype=torch.float32, device=dev)
     if tokens is not None:
         logprob = torch.empty(M, dtype=torch.float32, device=dev)
