@@ -165,7 +165,7 @@ size_t pbd_op_evict_workspace_bytes(const pbd_kv_pages *kv, int32_t n_keep);
  * K and V move in place.  Weights and positions of the kept slots go to d_out_weights and d_out_positions, shaped like
  * d_weights and d_positions: those arrays themselves, or others apart from them and from one another; slots behind the kept ones are not
  * written.  d_lens is not changed: the caller lowers it to at most n_keep once all layers are through.
- * Requirements: n_recent + n_sink <= n_keep; no two sequences share a page; nothing that the call writes (K, V, the outputs, the
+ * Requirements: n_recent + n_sink <= n_keep; no page in use is named twice, by one sequence or two; nothing that the call writes (K, V, the outputs, the
  * workspace) lies over anything else that it reads or writes, weights and positions as their own outputs apart.  The workspace (1024-byte aligned) is scratch;
  * its first word is the status word for pbd_op_status: a length outside [0, max_pages * page_size], whose sequence is left as it
  * is, or a page outside [0, n_pages) among those of a sequence that evicts.  A move from or to a slot of such a page is left
