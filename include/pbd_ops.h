@@ -124,7 +124,8 @@ typedef struct {
     int32_t *d_positions;             /* the same shape: position of the token in each slot, or NULL */
 } pbd_kv_pages;
 
-/* Workspace bytes pbd_op_decode_attention needs (0 if unsupported); only the cache's sizes, strides and type are read. */
+/* Workspace bytes pbd_op_decode_attention needs (0 if unsupported); only the cache's sizes, strides and type are read.  With
+ * accumulate it has a score for every query head and slot of the tables, 4 * batch * n_q_heads * max_pages * page_size bytes of it. */
 size_t pbd_op_decode_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t n_q_heads, int32_t accumulate);
 
 /* Attention of one new token per sequence over a paged cache (the attention step of a plain decoding pass, on the
