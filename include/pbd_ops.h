@@ -194,12 +194,103 @@ pbd_status pbd_op_token_logprobs(int32_t M, int32_t V, int32_t dtype, const void
                                  const int32_t *d_tokens_opt, int32_t k, float *d_logprob_opt, float *d_entropy_opt,
                                  int32_t *d_top_ids, float *d_top_logprobs, void *d_ws, size_t ws_bytes, void *d_stream);
 
+/* Workspace bytes pbd_op_assign_pages needs (0 if unsupported). */
+size_t pbd_op_assign_pages_workspace_bytes(int32_t batch);
+
+/* Pages for the next tokens of every sequence, and the packed rows' slots, from lengths in device memory: what a step does
+ * before its layers.  Sequence b has d_lens[b] cached tokens and gets d_n_new[b] more; afterwards it holds exactly the
+ * ceil((d_lens[b] + d_n_new[b]) / page_size) pages at the front of its table row, so that a sequence that has ended
+ * (both 0) gives all of its pages back, and one that was cut back those behind its end.
+ * Held pages: d_held[b] entries of d_page_table [batch, max_pages].  Free ones: a stack, d_free [n_pages], of *d_n_free
+ * entries, the last on top.  First the sequences give back, in their order and each its entries in theirs, then they take from the top,
+ * in the same order.  Entries of a table row behind those held, and of d_free at or behind the new *d_n_free, stay as they were.
+ * Outputs: d_starts [batch + 1], the packed rows of sequence b being [d_starts[b], d_starts[b + 1]); for each packed row its
+ * slot page * page_size + place in the page in d_slots [max_new], and its position d_lens[b] + i in d_positions_opt
+ * [max_new] or NULL.  Rows behind the last sequence's get -1 and 0: max_new may be a captured step's largest size.
+ * d_lens is not changed: the caller raises it once all layers are through.
+ * The workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 a length below 0 or
+ * beyond max_pages * page_size, or more than max_new new tokens; 7 a page outside [0, n_pages) among those given or taken, or held and
+ * free ones of more than n_pages in all; 8 not enough free pages.  Nothing is assigned then: table, held and free pages
+ * stay as they were, the starts are 0 and all slots -1.  (7 with starts: a page held before lies outside; its rows' slots are -1.)
+ * Requirements: batch <= 1024; max_pages * page_size <= 2^30; max_new <= 2^30; no page is held or free twice; nothing that the call
+ * writes lies over anything else that it reads or writes. */
+pbd_status pbd_op_assign_pages(int32_t batch, int32_t max_pages, int32_t page_size, int32_t n_pages, const int32_t *d_lens,
+                               const int32_t *d_n_new, int32_t *d_page_table, int32_t *d_held, int32_t *d_free,
+                               int32_t *d_n_free, int32_t max_new, int32_t *d_starts, int64_t *d_slots,
+                               int32_t *d_positions_opt, void *d_ws, size_t ws_bytes, void *d_stream);
+
+/* Workspace bytes pbd_op_prompt_attention needs (0 if unsupported). */
+size_t pbd_op_prompt_attention_workspace_bytes(int32_t T, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                               int32_t head_dim);
+
+/* Attention over whole prompts, causal: T packed rows of `batch` sequences, sequence b the rows [d_starts[b], d_starts[b + 1]);
+ * row i of a sequence sees its rows 0 to i.  Query head h reads KV head h / (n_q_heads / n_kv_heads),
+ *     s_j = q . k_j,  p = softmax(scale * s),  out = sum_j p_j v_j,  lse = ln sum_j exp(scale * s_j).
+ * d_q: T rows q_stride values apart of [n_q_heads, head_dim]; d_k, d_v: T rows kv_stride values apart of [n_kv_heads, head_dim], so that the
+ * three may be parts of one projection's rows; d_out [T, n_q_heads, head_dim]; all of type dtype, PBD_BF16 or PBD_FP16.
+ * d_lse_opt [T, n_q_heads] fp32 or NULL.  Rows of no sequence are neither read nor written.
+ * kv_opt with d_slots_opt [T] (both or neither): K and V of each sequence's row t are stored into slot d_slots_opt[t] of the cache (its page's
+ * number times page_size plus the place there, as pbd_op_assign_pages gives it); negative: not stored.  Of the cache K, V, sizes and strides
+ * count, not table and lengths.
+ * Score, softmax and output sums are fp32; p is rounded to the type for the tensor cores (relative to the row's largest weight, so the
+ * error is a rounding's share of each p_j v_j), and out once more.
+ * A value of V that is infinite or NaN makes its dimension NaN or infinite in the outputs of the rows and heads that see it, and
+ * no other; K and V of rows that a row does not see do not touch it, whatever they hold.  Finite values of V: in bf16 at most 2^123 / T.
+ * Requirements: head_dim 64, 128 or 256; n_q_heads a multiple of n_kv_heads; batch <= 1024; scale > 0; d_q, d_k, d_v and d_out 16-byte
+ * aligned, row strides multiples of 8 below 2^38; no slot twice; nothing that the call writes lies over anything else that it reads or writes.
+ * The workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 bounds of a sequence that
+ * descend or lie outside [0, T], whose rows are left out; 7 a slot outside the cache, whose row is not stored. */
+pbd_status pbd_op_prompt_attention(int32_t T, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                   int32_t dtype, float scale, const void *d_q, int64_t q_stride, const void *d_k,
+                                   const void *d_v, int64_t kv_stride, const int32_t *d_starts, const pbd_kv_pages *kv_opt,
+                                   const int64_t *d_slots_opt, void *d_out, float *d_lse_opt, void *d_ws, size_t ws_bytes,
+                                   void *d_stream);
+
+/* Workspace bytes pbd_op_tree_attention needs (0 if unsupported); only the cache's sizes, strides and type are read. */
+size_t pbd_op_tree_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t T, int32_t n_q_heads);
+
+/* Attention of up to 64 drafted tokens a sequence over a paged cache (the attention step of a verify pass, on the caller's own
+ * cache): T packed rows, sequence b the rows [d_starts[b], d_starts[b + 1]), its nodes in order.  d_parents_opt [T]: the node of the
+ * same sequence that a node follows, before it, or -1 for one that follows the cached tokens; NULL: each node follows the one before it (a
+ * verify block).  Node i sees the d_lens[b] cached slots, its ancestors and itself; formulas, heads, d_q and d_out as
+ * pbd_op_prompt_attention.  A row that sees nothing gets zeros and -inf.
+ * d_k_new, d_v_new: the nodes' own K and V, T rows new_stride values apart of [n_kv_heads, head_dim].  They are stored into slots
+ * d_lens[b] + i (whose pages the table must name), and node i's position goes to d_positions from d_new_positions_opt [T]
+ * when both are there.  d_lens and d_weights are not changed.  pbd_op_commit_path then makes an accepted path contiguous.
+ * Rounding, infinite and NaN values of V as pbd_op_prompt_attention; a node does not touch those that do not descend from it.
+ * Requirements: T <= 2^30; scale > 0; d_q, d_k_new, d_v_new and d_out 16-byte aligned, row strides multiples of 8 below 2^38; no page
+ * in use is named twice among those that new rows go to; nothing that the call writes lies over anything else that it reads or writes.  The
+ * workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 bounds that descend, lie outside [0, T]
+ * or span more than 64 rows, or a length outside [0, max_pages * page_size - nodes]: the sequence is left out; 7 a page
+ * outside [0, n_pages): its slots, new nodes' among them, take no part and are not stored; 9 a parent that is not before
+ * its node: it counts as -1. */
+pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_heads, float scale, const void *d_q,
+                                 int64_t q_stride, const void *d_k_new, const void *d_v_new, int64_t new_stride,
+                                 const int32_t *d_starts, const int32_t *d_parents_opt, const int32_t *d_new_positions_opt,
+                                 void *d_out, float *d_lse_opt, void *d_ws, size_t ws_bytes, void *d_stream);
+
+/* Workspace bytes pbd_op_commit_path needs (0 if unsupported); only the cache's sizes, strides and type are read. */
+size_t pbd_op_commit_path_workspace_bytes(const pbd_kv_pages *kv, int32_t max_path);
+
+/* Makes the accepted path of each sequence's drafted tree contiguous behind its cached tokens: K, V and, where the cache has them,
+ * weight and position of slot d_lens[b] + d_path[b * max_path + i] go to slot d_lens[b] + i, for i < d_n_accepted[b].  A path names nodes in
+ * ascending order (a node comes after its parent), the first of them 0 or above; entries behind d_n_accepted[b] are not read.  Other slots stay
+ * as they are.  d_lens is not changed: a layer's call leaves it to the caller, who adds the accepted numbers once all layers are through.
+ * Requirements: 1 <= max_path <= 64; no page in use is named twice; nothing that the call writes (K, V, weights, positions, the workspace)
+ * lies over anything else that it reads or writes.  The workspace (1024-byte aligned) is scratch; its first word is the status word for
+ * pbd_op_status: 5 a number outside [0, max_path] or a length outside [0, max_pages * page_size], 9 a path that does not
+ * ascend or leaves the tree's 64 nodes or the table: that sequence is left as it is; 7 a page outside [0, n_pages): moves
+ * from and to its slots are left out. */
+pbd_status pbd_op_commit_path(const pbd_kv_pages *kv, const int32_t *d_path, int32_t max_path, const int32_t *d_n_accepted,
+                              void *d_ws, size_t ws_bytes, void *d_stream);
+
 /* Device status of the last call of an entry point above that used the workspace d_ws (the 1024-byte-aligned
  * pointer that call was given): waits for d_stream, then reads the status word at the start of d_ws.  PBD_OK when no
  * kernel latched an error; PBD_ERR_DEVICE with the latched code in *h_device_code (may be NULL) otherwise, and that
  * call's outputs are invalid; PBD_ERR_INVALID_ARG for a null or misaligned d_ws; PBD_ERR_CUDA if the stream failed.
- * What kernels latch: a device wait bounded at one second that runs out (linear, lm_head, token_logprobs), and lengths, pages (7) and
- * tokens (4) in device memory that lie outside their range (5: a length), which the host cannot check. */
+ * What kernels latch: a device wait bounded at one second that runs out (1, 2, 3 or 6: linear, lm_head, token_logprobs, prompt and tree
+ * attention), and lengths, pages (7; 8: none left), trees (9) and tokens (4) in device memory that lie outside their range (5: a
+ * length), which the host cannot check. */
 pbd_status pbd_op_status(const void *d_ws, void *d_stream, int32_t *h_device_code);
 
 /* Message of the last failed pbd_op_* call on this thread ("" if none). */

@@ -25,6 +25,8 @@ enum : int {
     DEV_BAD_POSITION = 5,   // position beyond the reserved pages
     DEV_TIMEOUT_DEP = 6,    // a work item's inputs never completed
     DEV_BAD_PAGE = 7,       // page index outside the cache
+    DEV_NO_PAGES = 8,       // fewer free pages than sequences need
+    DEV_BAD_TREE = 9,       // parent or path of a drafted tree out of order
 };
 
 constexpr unsigned long long WAIT_LIMIT_NS = 1000000000ull;  // 1 s

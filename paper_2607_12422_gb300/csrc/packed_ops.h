@@ -1,0 +1,53 @@
+// packed_ops.h -- operators on packed rows of several sequences and the pages behind them: what their kernels (page_ops.cu,
+// packed_attn.cu) take from their entry points (packed_api.cu).
+#pragma once
+
+#include "kv_ops.h"
+
+namespace pbd {
+
+constexpr int TREE_NODES = 64;  // drafted tokens of a sequence at most: a node's ancestors are the bits of one word
+
+// ---- pages from lengths (page_ops.cu)
+struct AssignArgs {
+    const int *lens, *n_new;  // [B]
+    int *table;               // [B][max_pages]
+    int *held, *free_list, *n_free;
+    int B, max_pages, page_size, n_pages, max_new;
+    long long cap;      // slots of a sequence
+    int *starts;        // [B + 1]
+    long long *slots;   // [max_new]
+    int *positions;     // [max_new] or null
+    int *status;
+};
+cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st);
+
+// ---- accepted paths (page_ops.cu)
+struct CommitArgs {
+    KvView kv;
+    const int *path;  // [B][max_path]
+    const int *n_accepted;
+    int max_path;
+    int *status;
+};
+cudaError_t launch_commit_path(const CommitArgs &a, cudaStream_t st);
+
+// ---- attention of packed rows (packed_attn.cu)
+struct PackedArgs {
+    KvView kv;       // tree: the cache; prompt: where K and V are stored (k null: nowhere)
+    int T, B, hq, hkv, group, d, fp16;
+    float scale;
+    const uint16_t *q, *k, *v;  // rows q_stride and kv_stride apart of [heads][d]
+    long long q_stride, kv_stride;
+    const int *starts;       // [B + 1]
+    const long long *slots;  // prompt: [T] or null
+    const int *parents;      // tree: [T] or null (a chain)
+    const int *new_pos;      // tree: [T] or null
+    uint16_t *out;           // [T][hq][d]
+    float *lse;              // [T][hq] or null
+    int *status;
+};
+cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st);
+cudaError_t launch_tree_attention(const PackedArgs &a, cudaStream_t st);
+
+}  // namespace pbd

@@ -1,0 +1,273 @@
+// page_ops.cu -- pages and slot maps from request lengths (pbd_op_assign_pages) and the move of an accepted path's rows
+// (pbd_op_commit_path).
+#include <algorithm>
+
+#include "packed_ops.h"
+
+namespace pbd {
+
+namespace {
+
+// ------------------------------------------------------------------ pages from lengths
+//
+// need_b = ceil((len_b + new_b) / page_size).  Sequences with more pages than that give the rest back, those with fewer
+// take what they lack.  With exclusive prefix sums G_b of what is given, T_b of what is taken and N_b of the new tokens:
+//     the stack's place n_free + G_b + i holds the i-th page that b gives,
+//     the i-th page that b takes is at place n_free + G - 1 - (T_b + i),          G, T: the totals,
+//     token N_b + i of the packed rows is at slot len_b + i of b.
+// Sequences either give or take, places at or above n_free are only written and those below only read, so nothing has to be
+// kept aside and the result does not depend on any order of threads.
+//
+// One CTA, a thread a sequence, does the sums (a chain of latencies: lengths, scans, pages), and checks all that it will use
+// before it writes anything.  A few packed rows are expanded to slots by the same CTA; more by a second kernel.
+constexpr int AP_THREADS = 1024;
+static_assert(KV_MAX_BATCH <= AP_THREADS, "a thread a sequence");
+constexpr int AP_ALONE = 8192;  // packed rows that the first CTA expands itself
+
+struct AssignSums {
+    int fresh[KV_MAX_BATCH + 1], give[KV_MAX_BATCH + 1], take[KV_MAX_BATCH + 1];  // exclusive, totals behind
+    int len[KV_MAX_BATCH], held[KV_MAX_BATCH], need[KV_MAX_BATCH];
+    long long warp[4][32];
+};
+
+// the sequence that place i of a prefix sum belongs to
+__device__ __forceinline__ int owner(const int *sum, int n, int i) {
+    int lo = 0, hi = n;  // sum[lo] <= i < sum[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (sum[mid] <= i)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+// Packed row t; total: rows of all sequences.
+__device__ __forceinline__ bool expand(const AssignArgs &a, const int *starts, const int *lens, int total, int t) {
+    long long slot = -1;
+    int pos = 0;
+    bool bad = false;
+    if (t < total) {
+        const int b = owner(starts, a.B, t);
+        pos = lens[b] + (t - starts[b]);
+        const int i = pos / a.page_size;
+        const int page = a.table[(long long)b * a.max_pages + i];
+        bad = (unsigned)page >= (unsigned)a.n_pages;
+        if (!bad) slot = (long long)page * a.page_size + (pos - i * a.page_size);
+    }
+    a.slots[t] = slot;
+    if (a.positions) a.positions[t] = pos;
+    return bad;
+}
+
+__global__ void __launch_bounds__(AP_THREADS) k_assign_pages(const __grid_constant__ AssignArgs a) {
+    __shared__ AssignSums S;
+    const int b = threadIdx.x, lane = b & 31, warp = b >> 5;
+    pdl_launch();
+    const int n_free = *a.n_free;
+    int len = 0, fresh = 0, held = 0;
+    if (b < a.B) len = a.lens[b], fresh = a.n_new[b], held = a.held[b];
+    const bool bad_len = len < 0 || fresh < 0 || (long long)len + fresh > a.cap;
+    bool bad_page = held < 0 || held > a.max_pages || n_free < 0 || n_free > a.n_pages;
+    if (bad_len) fresh = 0;
+    if (bad_page) held = 0;
+    const int need = bad_len ? 0 : (int)(((long long)len + fresh + a.page_size - 1) / a.page_size);
+    // inclusive sums over the warp, then over the warps (64 bits: nothing is known to be sound yet)
+    const long long own[4] = {fresh, max(held - need, 0), max(need - held, 0), held};
+    long long sum[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        sum[j] = own[j];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, sum[j], o);
+            if (lane >= o) sum[j] += y;
+        }
+        if (lane == 31) S.warp[j][warp] = sum[j];
+    }
+    __syncthreads();
+    long long total[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        long long w = S.warp[j][lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, w, o);
+            if (lane >= o) w += y;
+        }
+        total[j] = __shfl_sync(0xffffffffu, w, 31);
+        const long long before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
+        sum[j] += (warp ? before : 0) - own[j];
+    }
+    // (sums beyond 32 bits come with one of the totals below out of range, and are not used then)
+    if (b < a.B) {
+        S.fresh[b] = (int)sum[0], S.give[b] = (int)sum[1], S.take[b] = (int)sum[2];
+        S.len[b] = len, S.held[b] = held, S.need[b] = need;
+    }
+    if (b == 0) S.fresh[a.B] = (int)total[0], S.give[a.B] = (int)total[1], S.take[a.B] = (int)total[2];
+    int code = __syncthreads_or(bad_len) || total[0] > a.max_new ? DEV_BAD_POSITION : DEV_OK;
+    // (a page that is held and free at once would be given to two sequences)
+    if (__syncthreads_or(bad_page) || total[3] + n_free > a.n_pages) code = code ? code : DEV_BAD_PAGE;
+    if (code == DEV_OK && total[2] > n_free + total[1]) code = DEV_NO_PAGES;
+    const int give = (int)total[1], take = (int)total[2], top = n_free + give;
+    auto given = [&](int i) {
+        const int s = owner(S.give, a.B, i);
+        return a.table[(long long)s * a.max_pages + S.need[s] + (i - S.give[s])];
+    };
+    auto taken = [&](int i) {
+        const int at = top - 1 - i;
+        return at < n_free ? a.free_list[at] : given(at - n_free);
+    };
+    auto valid = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+    if (code == DEV_OK) {
+        bad_page = false;
+        for (int i = b; i < give; i += AP_THREADS) bad_page |= !valid(given(i));
+        for (int i = b; i < min(take, take - give); i += AP_THREADS) bad_page |= !valid(a.free_list[n_free - 1 - i]);
+        if (__syncthreads_or(bad_page)) code = DEV_BAD_PAGE;
+    }
+    if (code == DEV_OK) {
+        for (int i = b; i < take; i += AP_THREADS) {
+            const int s = owner(S.take, a.B, i);
+            a.table[(long long)s * a.max_pages + S.held[s] + (i - S.take[s])] = taken(i);
+        }
+        for (int i = b; i < give - take; i += AP_THREADS) a.free_list[n_free + i] = given(i);
+        if (b < a.B) a.held[b] = need;
+        if (b == 0) *a.n_free = top - take;
+    }
+    if (b < a.B) a.starts[b] = code == DEV_OK ? S.fresh[b] : 0;
+    if (b == 0) a.starts[a.B] = code == DEV_OK ? S.fresh[a.B] : 0, *a.status = code;
+    if (a.max_new > AP_ALONE) return;
+    __syncthreads();
+    const int rows = code == DEV_OK ? S.fresh[a.B] : 0;
+    bool bad = false;
+    for (int t = b; t < a.max_new; t += AP_THREADS) bad |= expand(a, S.fresh, S.len, rows, t);
+    if (__syncthreads_or(bad) && b == 0 && code == DEV_OK) *a.status = DEV_BAD_PAGE;
+}
+
+constexpr int AP_EXPAND = 256;
+__global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constant__ AssignArgs a) {
+    __shared__ int starts[KV_MAX_BATCH + 1], lens[KV_MAX_BATCH];
+    for (int b = threadIdx.x; b < a.B; b += AP_EXPAND) lens[b] = a.lens[b];
+    pdl_wait();
+    for (int b = threadIdx.x; b <= a.B; b += AP_EXPAND) starts[b] = a.starts[b];
+    __syncthreads();
+    const int total = starts[a.B];
+    bool bad = false;
+    for (long long t = blockIdx.x * AP_EXPAND + threadIdx.x; t < a.max_new; t += (long long)gridDim.x * AP_EXPAND)
+        bad |= expand(a, starts, lens, total, (int)t);
+    if (bad) latch_error(a.status, DEV_BAD_PAGE);
+}
+
+// ------------------------------------------------------------------ accepted paths
+//
+// Row len + path[i] of a sequence goes to len + i, i < n_accepted.  path ascends, so path[i] >= i; a row's target may be
+// another one's source.  One CTA takes all rows of one (sequence, KV head): it holds them in registers before it writes any.
+// Bound by a chain of loads (length, path, table, row), and by random rows of 2 d bytes where there are many.
+constexpr int CP_THREADS = 256;
+
+// whether the path of sequence b can be walked
+__device__ __forceinline__ bool path_ok(const CommitArgs &a, int b, int n, int len) {
+    return n >= 0 && n <= a.max_path && len >= 0 && len <= a.kv.cap;
+}
+
+template <int D>
+__global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constant__ CommitArgs a) {
+    constexpr int CPR = D / 8, MOST = 2 * TREE_NODES * CPR / CP_THREADS;  // 16-byte pieces of a row, of a thread
+    __shared__ long long of[TREE_NODES], to[TREE_NODES];  // value offsets of the rows, -1: does not move
+    __shared__ int slot_of[TREE_NODES];
+    if (blockIdx.x == (unsigned)(a.kv.B * a.kv.hkv)) {  // the last CTA looks at everything for the call's status
+        int code = DEV_OK;
+        for (long long i = threadIdx.x; i < (long long)a.kv.B * (a.max_path + 1); i += CP_THREADS) {
+            const int b = (int)(i / (a.max_path + 1)), at = (int)(i - (long long)b * (a.max_path + 1)) - 1;
+            const int n = a.n_accepted[b], len = a.kv.lens[b];
+            if (!path_ok(a, b, n, len)) {
+                code = max(code, (int)DEV_BAD_POSITION);
+                continue;
+            }
+            if (at < 0 || at >= n) continue;
+            const int p = a.path[(long long)b * a.max_path + at], before = at ? a.path[(long long)b * a.max_path + at - 1] : -1;
+            if (p <= before || p >= TREE_NODES || (long long)len + p >= a.kv.cap) {
+                code = max(code, (int)DEV_BAD_TREE);
+                continue;
+            }
+            if (p == at) continue;
+            const int *table = a.kv.table + (long long)b * a.kv.max_pages;
+            if ((unsigned)table[page_index(a.kv, len + p)] >= (unsigned)a.kv.n_pages ||
+                (unsigned)table[page_index(a.kv, len + at)] >= (unsigned)a.kv.n_pages)
+                code = max(code, (int)DEV_BAD_PAGE);
+        }
+        code = __syncthreads_or(code == DEV_BAD_TREE) ? DEV_BAD_TREE
+               : __syncthreads_or(code == DEV_BAD_PAGE) ? DEV_BAD_PAGE
+               : __syncthreads_or(code != DEV_OK) ? DEV_BAD_POSITION
+                                                  : DEV_OK;
+        if (threadIdx.x == 0) *a.status = code;
+        return;
+    }
+    const int b = blockIdx.x / a.kv.hkv, h = blockIdx.x - b * a.kv.hkv;
+    const int n = a.n_accepted[b], len = a.kv.lens[b];
+    if (!path_ok(a, b, n, len) || n == 0) return;
+    const int i = threadIdx.x;
+    bool bad = false;
+    if (i < n) {
+        const int p = a.path[(long long)b * a.max_path + i], before = i ? a.path[(long long)b * a.max_path + i - 1] : -1;
+        bad = p <= before || p >= TREE_NODES || (long long)len + p >= a.kv.cap;
+        long long from = -1, dest = -1;
+        if (!bad && p != i) {
+            const int *table = a.kv.table + (long long)b * a.kv.max_pages;
+            const int si = page_index(a.kv, len + p), di = page_index(a.kv, len + i);
+            const int sp = table[si], dp = table[di];
+            if ((unsigned)sp < (unsigned)a.kv.n_pages && (unsigned)dp < (unsigned)a.kv.n_pages) {
+                from = sp * a.kv.stride_page + h * a.kv.stride_head + (len + p - si * a.kv.page_size) * a.kv.stride_slot;
+                dest = dp * a.kv.stride_page + h * a.kv.stride_head + (len + i - di * a.kv.page_size) * a.kv.stride_slot;
+            }
+        }
+        of[i] = from, to[i] = dest, slot_of[i] = len + p;
+    }
+    if (__syncthreads_or(bad)) return;  // the sequence stays as it is
+    uint4 piece[MOST];
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+        const int x = threadIdx.x + j * CP_THREADS, r = x / (2 * CPR), c = x % (2 * CPR);
+        if (r < n && of[r] >= 0) piece[j] = *reinterpret_cast<const uint4 *>((c < CPR ? a.kv.k : a.kv.v) + of[r] + (c % CPR) * 8);
+    }
+    const long long row = ((long long)b * a.kv.hkv + h) * a.kv.cap;
+    float w = 0.f;
+    int pos = 0;
+    const bool moves = i < n && of[i] >= 0;
+    if (moves && a.kv.weights) w = a.kv.weights[row + slot_of[i]];
+    if (moves && a.kv.positions) pos = a.kv.positions[row + slot_of[i]];
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+        const int x = threadIdx.x + j * CP_THREADS, r = x / (2 * CPR), c = x % (2 * CPR);
+        if (r < n && of[r] >= 0)
+            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(c < CPR ? a.kv.k : a.kv.v) + to[r] + (c % CPR) * 8) = piece[j];
+    }
+    if (moves && a.kv.weights) a.kv.weights[row + len + i] = w;
+    if (moves && a.kv.positions) a.kv.positions[row + len + i] = pos;
+}
+
+}  // namespace
+
+cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st) {
+    k_assign_pages<<<1, AP_THREADS, 0, st>>>(a);
+    if (a.max_new > AP_ALONE) {
+        const int grid = std::min((a.max_new + AP_EXPAND - 1) / AP_EXPAND, 8 * gemm_ctas());
+        const cudaError_t e = launch_pdl(k_expand_slots, grid, AP_EXPAND, 0, st, a);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_commit_path(const CommitArgs &a, cudaStream_t st) {
+    const int grid = a.kv.B * a.kv.hkv + 1;
+    switch (a.kv.d) {
+        case 64: k_commit_path<64><<<grid, CP_THREADS, 0, st>>>(a); break;
+        case 128: k_commit_path<128><<<grid, CP_THREADS, 0, st>>>(a); break;
+        default: k_commit_path<256><<<grid, CP_THREADS, 0, st>>>(a); break;
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace pbd

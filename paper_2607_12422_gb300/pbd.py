@@ -134,7 +134,15 @@ def load(path: str = LIB_PATH) -> C.CDLL:
     L.pbd_op_evict.argtypes = [KV, I32, I32, I32, P, P, P, P, Z, P]
     L.pbd_op_token_logprobs_workspace_bytes.argtypes = [I32, I32, I32]
     L.pbd_op_token_logprobs.argtypes = [I32, I32, I32, P, I64, F, P, I32, P, P, P, P, P, Z, P]
-    for name in ("decode_attention", "evict", "token_logprobs"):
+    L.pbd_op_assign_pages_workspace_bytes.argtypes = [I32]
+    L.pbd_op_assign_pages.argtypes = [I32, I32, I32, I32, P, P, P, P, P, P, I32, P, P, P, P, Z, P]
+    L.pbd_op_prompt_attention_workspace_bytes.argtypes = [I32, I32, I32, I32, I32]
+    L.pbd_op_prompt_attention.argtypes = [I32, I32, I32, I32, I32, I32, F, P, I64, P, P, I64, P, KV, P, P, P, P, Z, P]
+    L.pbd_op_tree_attention_workspace_bytes.argtypes = [KV, I32, I32]
+    L.pbd_op_tree_attention.argtypes = [KV, I32, I32, F, P, I64, P, P, I64, P, P, P, P, P, P, Z, P]
+    L.pbd_op_commit_path_workspace_bytes.argtypes = [KV, I32]
+    L.pbd_op_commit_path.argtypes = [KV, P, I32, P, P, Z, P]
+    for name in ("decode_attention", "evict", "token_logprobs", "assign_pages", "prompt_attention", "tree_attention", "commit_path"):
         getattr(L, "pbd_op_" + name).restype = C.c_int
         getattr(L, "pbd_op_%s_workspace_bytes" % name).restype = C.c_size_t
     for name in ("pbd_create", "pbd_destroy", "pbd_prefill", "pbd_draft_block", "pbd_verify_block",
@@ -344,6 +352,7 @@ class PagedKV:
         self.k, self.v, self.page_table, self.lens = k, v, page_table, lens
         self.weights, self.positions = weights, positions
         self.batch, self.n_kv_heads, self.head_dim, self.device, self.dtype = B, hkv, D, k.device, k.dtype
+        self.page_size = ps
         self.c = pbd_kv_pages(k.data_ptr(), v.data_ptr(), _dtype(k, who), n_pages, ps, hkv, D, B, max_pages, k.stride(0),
                               k.stride(1), k.stride(2), page_table.data_ptr(), lens.data_ptr(), _ptr(weights),
                               _ptr(positions))
@@ -495,6 +504,232 @@ def pbd_op_token_logprobs(logits, tokens=None, k: int = 0, temperature: float = 
     if sync:
         _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
     return TokenLogprobs(logprob, entropy, ids, top)
+
+
+class PagePool:
+    """The pages of a paged cache and who holds them (one for all layers): a handle that keeps the tensors it was given.
+
+    page_table [batch, max_pages] int32, whose row b names in its first held[b] entries the pages of sequence b; held [batch],
+    free [n_pages] and n_free [1] int32: a stack of the free pages.  Without the last three all pages are free."""
+
+    def __init__(self, page_table, page_size: int, n_pages: int, held=None, free=None, n_free=None):
+        import torch
+        who = "PagePool"
+        if page_table.dim() != 2 or not page_table.is_cuda:
+            _bad(who, "page_table is [batch, max_pages] on a GPU")
+        B, max_pages = page_table.shape
+        if not _int32(B, max_pages, page_size, n_pages) or n_pages < 1:
+            _bad(who, "a size does not fit 32 bits, or there is no page")
+        dev = page_table.device
+        if held is None and free is None and n_free is None:
+            held = torch.zeros(B, dtype=torch.int32, device=dev)
+            free = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=dev)
+            n_free = torch.full((1,), n_pages, dtype=torch.int32, device=dev)
+        elif held is None or free is None or n_free is None:
+            _bad(who, "held, free and n_free come together")
+        for name, t, shape in (("page_table", page_table, (B, max_pages)), ("held", held, (B,)), ("free", free, (n_pages,)),
+                               ("n_free", n_free, (1,))):
+            _check(who, name, t, page_table, shape, torch.int32)
+        self.page_table, self.held, self.free, self.n_free = page_table, held, free, n_free
+        self.batch, self.max_pages, self.page_size, self.n_pages, self.device = B, max_pages, page_size, n_pages, dev
+
+
+class AssignedPages(NamedTuple):
+    starts: object     # [batch + 1] int32: sequence b has the packed rows [starts[b], starts[b + 1])
+    slots: object      # [max_new] int64: a row's slot in the cache, -1 behind the last sequence's
+    positions: object  # [max_new] int32: its position, 0 there
+
+
+def assign_pages_workspace_bytes(batch: int) -> int:
+    return load().pbd_op_assign_pages_workspace_bytes(batch) if _int32(batch) else 0
+
+
+def pbd_op_assign_pages(pool: PagePool, lens, n_new, max_new: int, out: Optional[AssignedPages] = None, workspace=None,
+                        sync: bool = True):
+    """AssignedPages of the next n_new [batch] int32 tokens behind lens [batch] int32 cached ones: each sequence gets the pages
+    that it lacks from the pool and gives back those behind its end (all, if it has ended: both 0); see include/pbd_ops.h.
+    max_new: packed rows to make room for; out: an earlier call's result to write to.  With sync, waits and raises
+    PbdError(PBD_ERR_DEVICE) where lengths, pages or the pool's size do not allow it, and nothing is assigned; without, ask
+    pbd_op_status(workspace)."""
+    import torch
+    who = "pbd_op_assign_pages"
+    dev = pool.device
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_assign_pages(pool, lens, n_new, max_new, out, workspace, sync)
+    L = load()
+    B, i32 = pool.batch, torch.int32
+    _check(who, "lens", lens, pool, (B,), i32)
+    _check(who, "n_new", n_new, pool, (B,), i32)
+    if not 0 <= max_new < 1 << 31:
+        _bad(who, "max_new is negative or does not fit 32 bits")
+    if out is None:
+        out = AssignedPages(torch.empty(B + 1, dtype=i32, device=dev), torch.empty(max_new, dtype=torch.int64, device=dev),
+                            torch.empty(max_new, dtype=i32, device=dev))
+    else:
+        _check(who, "starts", out.starts, pool, (B + 1,), i32)
+        _check(who, "slots", out.slots, pool, (max_new,), torch.int64)
+        _check(who, "positions", out.positions, pool, (max_new,), i32)
+    ws = _scratch(who, workspace, L.pbd_op_assign_pages_workspace_bytes(B), dev)
+    st = _stream(torch, dev)
+    s = L.pbd_op_assign_pages(B, pool.max_pages, pool.page_size, pool.n_pages, lens.data_ptr(), n_new.data_ptr(),
+                              pool.page_table.data_ptr(), pool.held.data_ptr(), pool.free.data_ptr(), pool.n_free.data_ptr(),
+                              max_new, out.starts.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(), ws.ptr, ws.nbytes, st)
+    _raise_if(L, s)
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    return out
+
+
+def _packed_rows(who, q, k, v, names):
+    """(T, hq, hkv, D, row strides of q, of k and v) of packed rows: q [T, n_q_heads, head_dim], k and v [T, n_kv_heads,
+    head_dim], rows may lie apart."""
+    if q.dim() != 3 or k.dim() != 3:
+        _bad(who, "q is [T, n_q_heads, head_dim] and %s [T, n_kv_heads, head_dim]" % names[0])
+    T, hq, D = q.shape
+    hkv = k.shape[1]
+    if T < 1:
+        _bad(who, "there is no row")
+    if not _int32(T, hq, hkv, D):
+        _bad(who, "a size does not fit 32 bits")
+    _check(who, "q", q, q, (T, hq, D), None, True)
+    _check(who, names[0], k, q, (T, hkv, D), None, True)
+    _check(who, names[1], v, q, (T, hkv, D), None, True)
+    qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (hq * D, hkv * D)
+    if T > 1 and v.stride(0) != ks:
+        _bad(who, "rows of %s and %s lie differently far apart" % names)
+    return T, hq, hkv, D, qs, ks
+
+
+def _packed_outputs(torch, who, q, out, lse, want_lse):
+    T, hq, D = q.shape
+    if out is None:
+        out = torch.empty((T, hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _check(who, "out", out, q, (T, hq, D))
+    if lse is not None:
+        _check(who, "lse", lse, q, (T, hq), torch.float32)
+    elif want_lse:
+        lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+    return out, lse
+
+
+def prompt_attention_workspace_bytes(T: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    sizes = (T, batch, n_q_heads, n_kv_heads, head_dim)
+    return load().pbd_op_prompt_attention_workspace_bytes(*sizes) if _int32(*sizes) else 0
+
+
+def pbd_op_prompt_attention(q, k, v, starts, kv: Optional[PagedKV] = None, slots=None, scale: Optional[float] = None, out=None,
+                            lse=None, want_lse: bool = False, workspace=None, sync: bool = True):
+    """(out [T, n_q_heads, head_dim], lse [T, n_q_heads] fp32 or None): causal attention over whole prompts, packed rows of several
+    sequences; see include/pbd_ops.h.  q [T, n_q_heads, head_dim]; k, v [T, n_kv_heads, head_dim], bf16 or fp16, rows may
+    lie apart; starts [batch + 1] int32: sequence b has rows [starts[b], starts[b + 1]).  kv with slots [T] int64 (of
+    pbd_op_assign_pages): K and V are stored into the cache as well.  scale is 1/sqrt(head_dim) when not given; out and lse
+    may be handed in, whose rows of no sequence stay as they are.  With sync, waits and raises PbdError(PBD_ERR_DEVICE) for bounds or
+    slots out of range; without (as in a graph's capture), ask pbd_op_status(workspace)."""
+    import torch
+    who = "pbd_op_prompt_attention"
+    dev = q.device
+    if dev.type != "cuda":
+        _bad(who, "q is on a GPU")
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_prompt_attention(q, k, v, starts, kv, slots, scale, out, lse, want_lse, workspace, sync)
+    L = load()
+    T, hq, hkv, D, qs, ks = _packed_rows(who, q, k, v, ("k", "v"))
+    if starts.dim() != 1 or starts.shape[0] < 2:
+        _bad(who, "starts is [batch + 1]")
+    B = starts.shape[0] - 1
+    _check(who, "starts", starts, q, (B + 1,), torch.int32)
+    if (kv is None) != (slots is None):
+        _bad(who, "kv and slots come together")
+    if kv is not None:
+        if kv.device != dev:
+            _bad(who, "the cache is on another device")
+        _check(who, "slots", slots, q, (T,), torch.int64)
+    dt = _dtype(q, who)
+    ws = _scratch(who, workspace, prompt_attention_workspace_bytes(T, B, hq, hkv, D), dev)
+    out, lse = _packed_outputs(torch, who, q, out, lse, want_lse)
+    st = _stream(torch, dev)
+    s = L.pbd_op_prompt_attention(T, B, hq, hkv, D, dt, D ** -0.5 if scale is None else scale, q.data_ptr(), qs, k.data_ptr(),
+                                  v.data_ptr(), ks, starts.data_ptr(), kv.ref if kv is not None else None, _ptr(slots),
+                                  out.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes, st)
+    _raise_if(L, s)
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    return out, lse
+
+
+def tree_attention_workspace_bytes(kv: PagedKV, T: int, n_q_heads: int) -> int:
+    return load().pbd_op_tree_attention_workspace_bytes(kv.ref, T, n_q_heads) if _int32(T, n_q_heads) else 0
+
+
+def pbd_op_tree_attention(q, kv: PagedKV, k_new, v_new, starts, parents=None, new_positions=None, scale: Optional[float] = None,
+                          out=None, lse=None, want_lse: bool = False, workspace=None, sync: bool = True):
+    """(out [T, n_q_heads, head_dim], lse [T, n_q_heads] fp32 or None): attention of drafted tokens, up to 64 a sequence, over a
+    paged cache, whose slots behind kv.lens get their K and V; see include/pbd_ops.h.  q, k_new, v_new: packed rows as
+    pbd_op_prompt_attention's; starts [batch + 1] int32; parents [T] int32: the node of the sequence that a node follows, -1 for the
+    cached tokens (None: a chain, as in a verify block); new_positions [T] int32 go into the cache's.  scale, out, lse and sync as
+    there.  pbd_op_commit_path makes an accepted path contiguous."""
+    import torch
+    who = "pbd_op_tree_attention"
+    dev = kv.device
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_tree_attention(q, kv, k_new, v_new, starts, parents, new_positions, scale, out, lse, want_lse, workspace, sync)
+    L = load()
+    T, hq, hkv, D, qs, ks = _packed_rows(who, q, k_new, v_new, ("k_new", "v_new"))
+    if q.device != dev or q.dtype != kv.dtype or hkv != kv.n_kv_heads or D != kv.head_dim:
+        _bad(who, "device, type, n_kv_heads or head_dim are not the cache's")
+    _check(who, "starts", starts, q, (kv.batch + 1,), torch.int32)
+    if parents is not None:
+        _check(who, "parents", parents, q, (T,), torch.int32)
+    if new_positions is not None:
+        _check(who, "new_positions", new_positions, q, (T,), torch.int32)
+    key = ("tree", T, hq)
+    need = kv._need.get(key)
+    if need is None:  # (sizes of a handle do not change)
+        need = kv._need[key] = tree_attention_workspace_bytes(kv, T, hq)
+    ws = _scratch(who, workspace, need, dev)
+    out, lse = _packed_outputs(torch, who, q, out, lse, want_lse)
+    st = _stream(torch, dev)
+    s = L.pbd_op_tree_attention(kv.ref, T, hq, D ** -0.5 if scale is None else scale, q.data_ptr(), qs, k_new.data_ptr(), v_new.data_ptr(),
+                                ks, starts.data_ptr(), _ptr(parents), _ptr(new_positions), out.data_ptr(), _ptr(lse), ws.ptr, ws.nbytes, st)
+    _raise_if(L, s)
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
+    return out, lse
+
+
+def commit_path_workspace_bytes(kv: PagedKV, max_path: int) -> int:
+    return load().pbd_op_commit_path_workspace_bytes(kv.ref, max_path) if _int32(max_path) else 0
+
+
+def pbd_op_commit_path(kv: PagedKV, path, n_accepted, workspace=None, sync: bool = True) -> None:
+    """Moves the rows (and weights and positions) of each sequence's accepted path, nodes path[b, :n_accepted[b]] of its
+    drafted tree in ascending order, into the slots from kv.lens[b] on; see include/pbd_ops.h.  path [batch, max_path] and n_accepted
+    [batch] int32.  The program adds n_accepted to kv.lens once all layers that share it are through."""
+    import torch
+    who = "pbd_op_commit_path"
+    dev = kv.device
+    if torch.cuda.current_device() != dev.index:  # the library runs on the current device
+        with torch.cuda.device(dev):
+            return pbd_op_commit_path(kv, path, n_accepted, workspace, sync)
+    L = load()
+    if path.dim() != 2 or not _int32(path.shape[1]):
+        _bad(who, "path is [batch, max_path]")
+    most = path.shape[1]
+    _check(who, "path", path, kv, (kv.batch, most), torch.int32)
+    _check(who, "n_accepted", n_accepted, kv, (kv.batch,), torch.int32)
+    key = ("commit", most)
+    need = kv._need.get(key)
+    if need is None:  # (sizes of a handle do not change)
+        need = kv._need[key] = commit_path_workspace_bytes(kv, most)
+    ws = _scratch(who, workspace, need, dev)
+    st = _stream(torch, dev)
+    _raise_if(L, L.pbd_op_commit_path(kv.ref, path.data_ptr(), most, n_accepted.data_ptr(), ws.ptr, ws.nbytes, st))
+    if sync:
+        _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
 
 
 def pbd_op_status(workspace: OpWorkspace) -> None:
