@@ -18,9 +18,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
-// 2-D bf16 row-major [rows, cols] tensor map with box {64, box_rows}, 128-byte swizzle; rows lie ld values apart
-// (0: cols).
-bool encode_bf16_map(CUtensorMap *map, const void *base, int rows, int cols, int box_rows, int ld) {
+static EncodeTiledFn encode_tiled() {
     static EncodeTiledFn enc = nullptr;
     if (!enc) {
         void *fn = nullptr;
@@ -28,16 +26,33 @@ bool encode_bf16_map(CUtensorMap *map, const void *base, int rows, int cols, int
         if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
                 cudaSuccess ||
             fn == nullptr || q != cudaDriverEntryPointSuccess)
-            return false;
+            return nullptr;
         enc = reinterpret_cast<EncodeTiledFn>(fn);
     }
+    return enc;
+}
+
+// 2-D bf16 row-major [rows, cols] tensor map with box {64, box_rows}, 128-byte swizzle; rows lie ld values apart
+// (0: cols).
+bool encode_bf16_map(CUtensorMap *map, const void *base, int rows, int cols, int box_rows, int ld) {
     if (ld == 0) ld = cols;
-    if ((reinterpret_cast<uintptr_t>(base) & 15) || (ld * 2) % 16) return false;
-    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-    cuuint32_t box[2] = {(cuuint32_t)KT, (cuuint32_t)box_rows};
-    cuuint32_t es[2] = {1, 1};
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, es,
+    const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows}, strides[1] = {(uint64_t)ld * 2};
+    const uint32_t box[2] = {(uint32_t)KT, (uint32_t)box_rows};
+    return encode_map_16(map, base, 2, dims, strides, box);
+}
+
+// The same of any rank, for 16-bit values of any kind; strides in bytes, of the dimensions behind the first.
+bool encode_map_16(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides, const uint32_t *box) {
+    const EncodeTiledFn enc = encode_tiled();
+    if (!enc || rank < 2 || rank > 5 || (reinterpret_cast<uintptr_t>(base) & 15)) return false;
+    cuuint64_t d[5], st[4];
+    cuuint32_t bx[5], es[5];
+    for (int i = 0; i < rank; ++i) d[i] = dims[i], bx[i] = box[i], es[i] = 1;
+    for (int i = 0; i < rank - 1; ++i) {
+        if (strides[i] % 16) return false;
+        st[i] = strides[i];
+    }
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), d, st, bx, es,
                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

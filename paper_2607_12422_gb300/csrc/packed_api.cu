@@ -23,6 +23,7 @@ const char *bad_rows_of(int T, int batch, int hq, int hkv, int D, int64_t q_stri
         return "row strides must be multiples of 8 values and hold a row";
     // (tensor maps hold strides below 2^40 bytes)
     if (q_stride >= (1ll << 38) || kv_stride >= (1ll << 38)) return "row strides must be below 2^38 values";
+    if (!addressable(T, q_stride) || !addressable(T, kv_stride)) return "rows reach further than 2^60 values";
     return nullptr;
 }
 

@@ -150,7 +150,6 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st) { return launch<false>(a, st); }
 cudaError_t launch_tree_attention(const PackedArgs &a, cudaStream_t st) { return launch<true>(a, st); }
 
 }  // namespace pbd

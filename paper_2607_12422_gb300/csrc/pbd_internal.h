@@ -332,6 +332,7 @@ cudaError_t launch_pack_b(const void *b, int N, int r, void *out, cudaStream_t s
 
 // 2-D bf16 row-major [rows, cols] tensor map, rows ld values apart (0: cols), box {64, box_rows}, 128-byte swizzle.
 bool encode_bf16_map(CUtensorMap *map, const void *base, int rows, int cols, int box_rows, int ld = 0);
+bool encode_map_16(CUtensorMap *map, const void *base, int rank, const uint64_t *dims, const uint64_t *strides, const uint32_t *box);
 
 // Per-instantiation kernel attributes (dynamic shared memory), set once before any capture.
 cudaError_t configure_linear_kernels();
