@@ -18,7 +18,7 @@ LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libpbd.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 SOURCES = ["lm_head.cu", "gemm.cu", "linear_op.cu", "rows.cu", "steps.cu", "pass_kernel.cu", "ops.cu", "ops_api.cu", "op_linear_static.cu",
-           "kv_api.cu", "kv_attn.cu", "kv_evict.cu", "logprobs.cu", "packed_api.cu", "packed_attn.cu", "page_ops.cu", "prompt_attn.cu", "pbd.cu"]
+           "kv_api.cu", "kv_attn.cu", "kv_evict.cu", "logprobs.cu", "packed_api.cu", "page_ops.cu", "prompt_attn.cu", "tree_attn.cu", "pbd.cu"]
 HEADERS = ["attn.cuh", "common.cuh", "flash.cuh", "kv_checks.h", "kv_ops.h", "packed_ops.h", "pbd_internal.h"]
 
 

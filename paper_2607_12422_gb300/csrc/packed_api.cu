@@ -150,8 +150,9 @@ pbd_status pbd_op_prompt_attention(int32_t T, int32_t batch, int32_t n_q_heads, 
 }
 
 size_t pbd_op_tree_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t T, int32_t n_q_heads) {
-    if (bad_sizes(kv) || bad_heads(kv, n_q_heads) || T < 1 || T > (1 << 30)) return 0;
-    return 1024;
+    TreePlan p;
+    if (bad_sizes(kv) || bad_heads(kv, n_q_heads) || T < 1 || T > (1 << 30) || !tree_plan(view(*kv), T, n_q_heads, &p)) return 0;
+    return p.total;
 }
 
 pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_heads, float scale, const void *d_q,
@@ -169,10 +170,12 @@ pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_
         return fail(PBD_ERR_INVALID_ARG, who, "q, k_new, v_new and out must be 16-byte aligned");
     if (!aligned(d_starts, 4) || !aligned(d_parents_opt, 4) || !aligned(d_new_positions_opt, 4) || !aligned(d_lse_opt, 4))
         return fail(PBD_ERR_INVALID_ARG, who, "32-bit arrays must be 4-byte aligned");
-    const size_t need = pbd_op_tree_attention_workspace_bytes(kv, T, n_q_heads);
+    TreePlan p;
+    const KvView v = view(*kv);
+    if (!tree_plan(v, T, n_q_heads, &p)) return fail(PBD_ERR_CAPACITY, who, "more than 2^31 blocks of 128 slots in all heads and sequences");
+    const size_t need = p.total;
     if (const char *w = bad_workspace(d_ws, ws_bytes, need)) return fail(PBD_ERR_WORKSPACE, who, w);
     if (const char *w = k_over_v(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);
-    const KvView v = view(*kv);
     Ranges mem;
     mem.cache(kv, true);
     mem.add("q", d_q, rows_span(T, q_stride, n_q_heads, D), false);
@@ -208,7 +211,12 @@ pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_
     a.new_pos = d_new_positions_opt;
     a.out = static_cast<uint16_t *>(d_out);
     a.lse = d_lse_opt;
-    a.status = static_cast<int *>(d_ws);
+    uint8_t *ws = static_cast<uint8_t *>(d_ws);
+    a.status = reinterpret_cast<int *>(ws);
+    a.part_rows = p.rows;
+    a.worker_code = reinterpret_cast<int *>(ws + p.codes);
+    a.part_ml = reinterpret_cast<float2 *>(ws + p.part_ml);
+    a.part_o = reinterpret_cast<float *>(ws + p.part_o);
     const cudaError_t e = launch_tree_attention(a, static_cast<cudaStream_t>(d_stream));
     return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
 }

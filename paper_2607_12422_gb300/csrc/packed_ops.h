@@ -1,5 +1,5 @@
 // packed_ops.h -- operators on packed rows of several sequences and the pages behind them: what their kernels (page_ops.cu,
-// packed_attn.cu) take from their entry points (packed_api.cu).
+// prompt_attn.cu, tree_attn.cu) take from their entry points (packed_api.cu).
 #pragma once
 
 #include "kv_ops.h"
@@ -32,7 +32,7 @@ struct CommitArgs {
 };
 cudaError_t launch_commit_path(const CommitArgs &a, cudaStream_t st);
 
-// ---- attention of packed rows (packed_attn.cu)
+// ---- attention of packed rows (prompt_attn.cu, tree_attn.cu)
 struct PackedArgs {
     KvView kv;       // tree: the cache; prompt: where K and V are stored (k null: nowhere)
     int T, B, hq, hkv, group, d, fp16;
@@ -46,8 +46,20 @@ struct PackedArgs {
     uint16_t *out;           // [T][hq][d]
     float *lse;              // [T][hq] or null
     int *status;
+    // tree: scratch (tree_plan)
+    int workers, part_rows;  // CTAs; rows of one's part of a unit
+    int *worker_code;        // [workers]
+    float2 *part_ml;         // [workers][2][part_rows]: maximum, sum
+    float *part_o;           // [workers][2][part_rows][d]
 };
 cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st);
-cudaError_t launch_tree_attention(const PackedArgs &a, cudaStream_t st);
+
+constexpr int TREE_MAX_WORKERS = 160;
+struct TreePlan {
+    size_t codes, part_ml, part_o, total;  // offsets in the workspace
+    int rows;
+};
+bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p);
+cudaError_t launch_tree_attention(PackedArgs &a, cudaStream_t st);
 
 }  // namespace pbd
