@@ -18,16 +18,20 @@ namespace {
 // Sequences either give or take, places at or above n_free are only written and those below only read, so nothing has to be
 // kept aside and the result does not depend on any order of threads.
 //
-// One CTA, a thread a sequence, does the sums (a chain of latencies: lengths, scans, pages), and checks all that it will use
-// before it writes anything.  A few packed rows are expanded to slots by the same CTA; more by a second kernel.
+// One cluster: each of its CTAs makes the sums for itself, a thread a sequence (a chain of latencies: lengths, scans, pages), and they share
+// the pages out.  All that will be used is checked before anything is written.  A few packed rows are expanded to slots by
+// the same kernel; more by a second one.
 constexpr int AP_THREADS = 1024;
 static_assert(KV_MAX_BATCH <= AP_THREADS, "a thread a sequence");
-constexpr int AP_ALONE = 8192;  // packed rows that the first CTA expands itself
+constexpr int AP_CLUSTER = 8;   // CTAs where pages or rows are many
+constexpr int AP_FEW = 4096;    // pages and packed rows that one CTA deals with
+constexpr int AP_ROWS = 32768;  // packed rows that a cluster expands itself
 
 struct AssignSums {
     int fresh[KV_MAX_BATCH + 1], give[KV_MAX_BATCH + 1], take[KV_MAX_BATCH + 1];  // exclusive, totals behind
     int len[KV_MAX_BATCH], held[KV_MAX_BATCH], need[KV_MAX_BATCH];
     long long warp[4][32];
+    int bad[AP_CLUSTER];  // what each CTA of the cluster found
 };
 
 // the sequence that place i of a prefix sum belongs to
@@ -64,7 +68,9 @@ __device__ __forceinline__ bool expand(const AssignArgs &a, const int *starts, c
 __global__ void __launch_bounds__(AP_THREADS) k_assign_pages(const __grid_constant__ AssignArgs a) {
     __shared__ AssignSums S;
     const int b = threadIdx.x, lane = b & 31, warp = b >> 5;
+    const int rank = blockIdx.x, ctas = gridDim.x, me = rank * AP_THREADS + b, all = ctas * AP_THREADS;  // (one cluster)
     pdl_launch();
+    cluster_arrive();
     const int n_free = *a.n_free;
     int len = 0, fresh = 0, held = 0;
     if (b < a.B) len = a.lens[b], fresh = a.n_new[b], held = a.held[b];
@@ -122,28 +128,39 @@ __global__ void __launch_bounds__(AP_THREADS) k_assign_pages(const __grid_consta
     auto valid = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
     if (code == DEV_OK) {
         bad_page = false;
-        for (int i = b; i < give; i += AP_THREADS) bad_page |= !valid(given(i));
-        for (int i = b; i < min(take, take - give); i += AP_THREADS) bad_page |= !valid(a.free_list[n_free - 1 - i]);
-        if (__syncthreads_or(bad_page)) code = DEV_BAD_PAGE;
+#pragma unroll 4
+        for (int i = me; i < give; i += all) bad_page |= !valid(given(i));
+#pragma unroll 4
+        for (int i = me; i < take - give; i += all) bad_page |= !valid(a.free_list[n_free - 1 - i]);
     }
+    // (code so far is the same in all CTAs; what all of them found also says that all have read what is written below)
+    const int bad_here = __syncthreads_or(code == DEV_OK && bad_page);
+    cluster_wait();
+    if (b < ctas) st_cluster_u32(map_cta(smem_u32(&S.bad[rank]), b), bad_here);
+    cluster_sync();
+    for (int i = 0; i < ctas; ++i)
+        if (S.bad[i]) code = DEV_BAD_PAGE;
     if (code == DEV_OK) {
-        for (int i = b; i < take; i += AP_THREADS) {
+#pragma unroll 2
+        for (int i = me; i < take; i += all) {
             const int s = owner(S.take, a.B, i);
             a.table[(long long)s * a.max_pages + S.held[s] + (i - S.take[s])] = taken(i);
         }
-        for (int i = b; i < give - take; i += AP_THREADS) a.free_list[n_free + i] = given(i);
-        if (b < a.B) a.held[b] = need;
-        if (b == 0) *a.n_free = top - take;
+#pragma unroll 2
+        for (int i = me; i < give - take; i += all) a.free_list[n_free + i] = given(i);
+        if (rank == 0 && b < a.B) a.held[b] = need;
+        if (me == 0) *a.n_free = top - take;
     }
-    if (b < a.B) a.starts[b] = code == DEV_OK ? S.fresh[b] : 0;
-    if (b == 0) a.starts[a.B] = code == DEV_OK ? S.fresh[a.B] : 0, *a.status = code;
-    if (a.max_new > AP_ALONE) return;
-    __syncthreads();
+    if (rank == 0 && b < a.B) a.starts[b] = code == DEV_OK ? S.fresh[b] : 0;
+    if (me == 0) a.starts[a.B] = code == DEV_OK ? S.fresh[a.B] : 0, *a.status = code;
+    if (a.max_new > AP_ROWS) return;
+    cluster_sync();  // (the table's new entries)
     const int rows = code == DEV_OK ? S.fresh[a.B] : 0;
     bool bad = false;
-    for (int t = b; t < a.max_new; t += AP_THREADS) bad |= expand(a, S.fresh, S.len, rows, t);
-    if (__syncthreads_or(bad) && b == 0 && code == DEV_OK) *a.status = DEV_BAD_PAGE;
+    for (int t = me; t < a.max_new; t += all) bad |= expand(a, S.fresh, S.len, rows, t);
+    if (bad) latch_error(a.status, DEV_BAD_PAGE);
 }
+
 
 constexpr int AP_EXPAND = 256;
 __global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constant__ AssignArgs a) {
@@ -163,7 +180,8 @@ __global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constan
 //
 // Row len + path[i] of a sequence goes to len + i, i < n_accepted.  path ascends, so path[i] >= i; a row's target may be
 // another one's source.  One CTA takes all rows of one (sequence, KV head): it holds them in registers before it writes any.
-// Bound by a chain of loads (length, path, table, row), and by random rows of 2 d bytes where there are many.
+// Bound by a chain of loads (length, path, table, row), and by random rows of 2 d bytes where there are many.  k_clear_status, which
+// overlaps it, makes room for what any CTA finds wrong (one CTA that looks at all paths takes 50 us for 512 of them).
 constexpr int CP_THREADS = 256;
 
 // whether the path of sequence b can be walked
@@ -171,44 +189,29 @@ __device__ __forceinline__ bool path_ok(const CommitArgs &a, int b, int n, int l
     return n >= 0 && n <= a.max_path && len >= 0 && len <= a.kv.cap;
 }
 
+__global__ void k_clear_status(int *status) {
+    pdl_launch();
+    *status = DEV_OK;
+}
+__device__ __noinline__ void report(const CommitArgs &a, int code) {
+    pdl_wait();  // (the status has been cleared)
+    latch_error(a.status, code);
+}
+
 template <int D>
 __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constant__ CommitArgs a) {
     constexpr int CPR = D / 8, MOST = 2 * TREE_NODES * CPR / CP_THREADS;  // 16-byte pieces of a row, of a thread
     __shared__ long long of[TREE_NODES], to[TREE_NODES];  // value offsets of the rows, -1: does not move
     __shared__ int slot_of[TREE_NODES];
-    if (blockIdx.x == (unsigned)(a.kv.B * a.kv.hkv)) {  // the last CTA looks at everything for the call's status
-        int code = DEV_OK;
-        for (long long i = threadIdx.x; i < (long long)a.kv.B * (a.max_path + 1); i += CP_THREADS) {
-            const int b = (int)(i / (a.max_path + 1)), at = (int)(i - (long long)b * (a.max_path + 1)) - 1;
-            const int n = a.n_accepted[b], len = a.kv.lens[b];
-            if (!path_ok(a, b, n, len)) {
-                code = max(code, (int)DEV_BAD_POSITION);
-                continue;
-            }
-            if (at < 0 || at >= n) continue;
-            const int p = a.path[(long long)b * a.max_path + at], before = at ? a.path[(long long)b * a.max_path + at - 1] : -1;
-            if (p <= before || p >= TREE_NODES || (long long)len + p >= a.kv.cap) {
-                code = max(code, (int)DEV_BAD_TREE);
-                continue;
-            }
-            if (p == at) continue;
-            const int *table = a.kv.table + (long long)b * a.kv.max_pages;
-            if ((unsigned)table[page_index(a.kv, len + p)] >= (unsigned)a.kv.n_pages ||
-                (unsigned)table[page_index(a.kv, len + at)] >= (unsigned)a.kv.n_pages)
-                code = max(code, (int)DEV_BAD_PAGE);
-        }
-        code = __syncthreads_or(code == DEV_BAD_TREE) ? DEV_BAD_TREE
-               : __syncthreads_or(code == DEV_BAD_PAGE) ? DEV_BAD_PAGE
-               : __syncthreads_or(code != DEV_OK) ? DEV_BAD_POSITION
-                                                  : DEV_OK;
-        if (threadIdx.x == 0) *a.status = code;
-        return;
-    }
     const int b = blockIdx.x / a.kv.hkv, h = blockIdx.x - b * a.kv.hkv;
     const int n = a.n_accepted[b], len = a.kv.lens[b];
-    if (!path_ok(a, b, n, len) || n == 0) return;
+    if (!path_ok(a, b, n, len)) {
+        if (h == 0 && threadIdx.x == 0) report(a, DEV_BAD_POSITION);
+        return pdl_wait();
+    }
+    if (n == 0) return pdl_wait();
     const int i = threadIdx.x;
-    bool bad = false;
+    bool bad = false, bad_page = false;
     if (i < n) {
         const int p = a.path[(long long)b * a.max_path + i], before = i ? a.path[(long long)b * a.max_path + i - 1] : -1;
         bad = p <= before || p >= TREE_NODES || (long long)len + p >= a.kv.cap;
@@ -217,14 +220,16 @@ __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constan
             const int *table = a.kv.table + (long long)b * a.kv.max_pages;
             const int si = page_index(a.kv, len + p), di = page_index(a.kv, len + i);
             const int sp = table[si], dp = table[di];
-            if ((unsigned)sp < (unsigned)a.kv.n_pages && (unsigned)dp < (unsigned)a.kv.n_pages) {
+            bad_page = (unsigned)sp >= (unsigned)a.kv.n_pages || (unsigned)dp >= (unsigned)a.kv.n_pages;
+            if (!bad_page) {
                 from = sp * a.kv.stride_page + h * a.kv.stride_head + (len + p - si * a.kv.page_size) * a.kv.stride_slot;
                 dest = dp * a.kv.stride_page + h * a.kv.stride_head + (len + i - di * a.kv.page_size) * a.kv.stride_slot;
             }
         }
         of[i] = from, to[i] = dest, slot_of[i] = len + p;
     }
-    if (__syncthreads_or(bad)) return;  // the sequence stays as it is
+    if (h == 0 && (bad || bad_page)) report(a, bad ? DEV_BAD_TREE : DEV_BAD_PAGE);
+    if (__syncthreads_or(bad)) return pdl_wait();  // the sequence stays as it is
     uint4 piece[MOST];
 #pragma unroll
     for (int j = 0; j < MOST; ++j) {
@@ -246,13 +251,18 @@ __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constan
     }
     if (moves && a.kv.weights) a.kv.weights[row + len + i] = w;
     if (moves && a.kv.positions) a.kv.positions[row + len + i] = pos;
+    pdl_wait();
 }
 
 }  // namespace
 
 cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st) {
-    k_assign_pages<<<1, AP_THREADS, 0, st>>>(a);
-    if (a.max_new > AP_ALONE) {
+    // (512 sequences, 10000 pages taken, as many given back by the next call, 220000 rows: 196 us the two with one CTA, XX with eight;
+    // 8 sequences: YY and ZZ)
+    const bool many = a.max_new > AP_FEW || std::min<long long>(a.n_pages, (long long)a.B * a.max_pages) > AP_FEW;
+    const cudaError_t e = launch_cluster(k_assign_pages, many ? AP_CLUSTER : 1, AP_THREADS, st, a);
+    if (e != cudaSuccess) return e;
+    if (a.max_new > AP_ROWS) {
         const int grid = std::min((a.max_new + AP_EXPAND - 1) / AP_EXPAND, 8 * gemm_ctas());
         const cudaError_t e = launch_pdl(k_expand_slots, grid, AP_EXPAND, 0, st, a);
         if (e != cudaSuccess) return e;
@@ -261,13 +271,13 @@ cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st) {
 }
 
 cudaError_t launch_commit_path(const CommitArgs &a, cudaStream_t st) {
-    const int grid = a.kv.B * a.kv.hkv + 1;
+    const int grid = a.kv.B * a.kv.hkv;
+    k_clear_status<<<1, 1, 0, st>>>(a.status);
     switch (a.kv.d) {
-        case 64: k_commit_path<64><<<grid, CP_THREADS, 0, st>>>(a); break;
-        case 128: k_commit_path<128><<<grid, CP_THREADS, 0, st>>>(a); break;
-        default: k_commit_path<256><<<grid, CP_THREADS, 0, st>>>(a); break;
+        case 64: return launch_pdl(k_commit_path<64>, grid, CP_THREADS, 0, st, a);
+        case 128: return launch_pdl(k_commit_path<128>, grid, CP_THREADS, 0, st, a);
+        default: return launch_pdl(k_commit_path<256>, grid, CP_THREADS, 0, st, a);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace pbd
