@@ -161,6 +161,25 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, int *s
     return ok;
 }
 
+// The same in fewer instructions, for kernels whose warps run different code: one that runs little beside others that run much
+// fetches its instructions anew each time.
+__device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, int *status, int code, volatile int *abort) {
+    const uint32_t a = smem_u32(bar);
+    uint64_t t0 = 0;
+#pragma unroll 1
+    for (uint32_t n = 1; !mbar_try_wait(a, parity); ++n) {
+        if (n & 127) continue;
+        const uint64_t t = globaltimer_ns();
+        t0 = t0 ? t0 : t;
+        if (t - t0 > WAIT_LIMIT_NS) {
+            latch_error(status, code);
+            if (abort) *abort = 1;
+        }
+        if (t - t0 > WAIT_LIMIT_NS || (abort && *abort)) return false;
+    }
+    return true;
+}
+
 // ------------------------------------------------------------------ TMA
 
 __device__ __forceinline__ uint64_t l2_policy_evict_first() {

@@ -270,9 +270,15 @@ cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st) {
     return cudaGetLastError();
 }
 
+cudaError_t launch_clear_status(int *status, cudaStream_t st) {
+    k_clear_status<<<1, 1, 0, st>>>(status);
+    return cudaGetLastError();
+}
+
 cudaError_t launch_commit_path(const CommitArgs &a, cudaStream_t st) {
     const int grid = a.kv.B * a.kv.hkv;
-    k_clear_status<<<1, 1, 0, st>>>(a.status);
+    const cudaError_t e = launch_clear_status(a.status, st);
+    if (e != cudaSuccess) return e;
     switch (a.kv.d) {
         case 64: return launch_pdl(k_commit_path<64>, grid, CP_THREADS, 0, st, a);
         case 128: return launch_pdl(k_commit_path<128>, grid, CP_THREADS, 0, st, a);

@@ -6,12 +6,18 @@
 //
 // A tile's 128 rows are 128 / P tokens of P heads of one KV head, P the power of two in the group (16 at most), so that
 // tiles waste no rows and a block of K and V serves the whole group.  A CTA takes two tiles, of consecutive tokens (heads of 256: one), over
-// blocks of 128 keys up to its last token.  While the threads of one tile turn scores into P, the tensor core works on the other's.
+// blocks of 128 keys up to its last token.
 //
-// Warps 0-7: the tiles' rows, a thread each.  Warp 8: TMA.  Warp 9: MMAs.  Warps 10 and 11 look after values of V that not all rows
-// of the CTA see (those of its last one or two blocks): 0 x NaN would be NaN in rows that do not.  Rows behind the sequence's end become zero;
-// of the others, infinite and NaN values do, and the first row that sees one is noted for each dimension: from that row on the
-// result is NaN there.
+// Each CTA works on a list of such items, with its tensor core on the next one's first blocks while the rows of one leave.
+//
+// 0 x NaN is NaN: an infinite or NaN value of V among the keys that a row's mask hides would reach it (and so would the rows of
+// the packed neighbour in a sequence's last block).  Looking for such values first costs 4000 cycles an item.  Instead the rows look at
+// their results, and an item with one that is not finite is done again, carefully: in the one or two blocks that not all of its rows see,
+// rows of V behind the sequence's end become zero, infinite and NaN values too, and the first row that sees one is noted for each dimension; from
+// that row on the result is NaN there.
+//
+// Warps 0-15: the tiles' rows.  Warp 16: TMA.  Warps 17 and 18: the tiles' MMAs (one thread for both spent more on issuing and waiting
+// than the tensor core on multiplying: 16384 tokens 916 us).  Warp 19: the list, and V of items done again.
 #include <algorithm>
 
 #include "flash.cuh"
@@ -23,124 +29,130 @@ using namespace flash;
 
 namespace {
 
-constexpr int PA_THREADS = 384;
 constexpr int PA_MASKED = 2;  // blocks that not all rows of a CTA see, at most
 
 template <int D>
 struct PromptShape : Shape<D> {
     using S = Shape<D>;
     static constexpr int STAGES = D == 64 ? 8 : 4;
+    static constexpr int AHEAD = D == 64 ? 8 : 4;  // items that are told of, and notes of their values of V: more than the ring can be ahead of the rows
     static constexpr int SMEM = S::TILES * S::QT + STAGES * S::UNIT + 1024;
+};
+
+// What a CTA works on: tokens from q0 of a sequence of `len`, heads ch * P .. of the group of KV head h.  len 0: nothing more.
+struct PromptItem {
+    int start, len, q0, h, ch;
+    int nb[2], masked;  // the tiles' blocks; those that all rows of both see
+    int careful;        // done again
 };
 
 template <int D>
 struct PromptState {
-    uint64_t full[PromptShape<D>::STAGES], empty[PromptShape<D>::STAGES], q_full, s_full[2], p_full[2], o_full[2], drain;
-    uint64_t v_full[PA_MASKED], v_fixed[PA_MASKED];
+    using L = PromptShape<D>;
+    uint64_t full[L::STAGES], empty[L::STAGES], q_full, q_free, s_full[2], p_full[2][2], o_done[2], o_free[2], turn[2], drain[2];
+    uint64_t v_full[L::AHEAD][PA_MASKED], v_fixed[L::AHEAD][PA_MASKED], item_full[L::AHEAD], item_free[L::AHEAD];
     uint32_t tmem;
-    int abort, odd;
-    int first_odd[D];  // the first row that sees an infinite or NaN value in this dimension
+    int abort, bad;  // bad: bounds of a sequence
+    PromptItem item[L::AHEAD];
+    float top[2][2][ROWS];    // what the two threads of a row tell each other
+    int odd[L::AHEAD];  // whether a result is not finite
+    int first_odd[L::AHEAD][D];  // done again: the first row that sees an infinite or NaN value in this dimension
     int start[KV_MAX_BATCH], tiles[KV_MAX_BATCH];
 };
 
-// What a CTA works on: tokens from q0 of a sequence, heads ch * P .. of the group of KV head h.
-struct PromptItem {
-    int b, start, len, q0, h, ch;
-};
-
-// Items with the most keys come first: by token tile, the last ones before, then by sequence; the heads of one innermost.  A warp.
-__device__ __forceinline__ bool find_item(const PackedArgs &a, const int *start, const int *tiles, int heads, int chunks, int tokens, PromptItem &it) {
+// Item o of all.  Those with the most keys come first: by token tile, the last ones before, then by sequence; the heads of one
+// innermost.  A warp; `most`: the largest number of token tiles.
+__device__ __forceinline__ bool find_item(const PackedArgs &a, const int *start, const int *tiles, long long x, int total, int most, int heads, int chunks,
+                                          int tokens, int tile_tokens, bool two, PromptItem &it) {
     const int lane = threadIdx.x & 31;
-    const int o = blockIdx.x / heads, hc = blockIdx.x - o * heads;
+    if (x >= (long long)total * heads) return false;
+    const int o = (int)(x / heads), hc = (int)(x - (long long)o * heads);
     // items of token tiles t and above
     auto count = [&](int t) {
         int n = 0;
         for (int b = lane; b < a.B; b += 32) n += max(tiles[b] - t, 0);
         return __reduce_add_sync(0xffffffffu, n);
     };
-    int most = 0;
-    for (int b = lane; b < a.B; b += 32) most = max(most, tiles[b]);
-    int lo = 0, hi = __reduce_max_sync(0xffffffffu, most);  // count(hi) <= o < count(lo)
-    if (o >= count(0)) return false;
+    int lo = 0, hi = most, above = 0;  // count(hi) = above <= o < count(lo)
     while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (count(mid) <= o)
-            hi = mid;
+        const int mid = (lo + hi) >> 1, n = count(mid);
+        if (n <= o)
+            hi = mid, above = n;
         else
             lo = mid;
     }
-    int r = o - count(lo + 1);  // which of the sequences with a token tile lo
+    int r = o - above, b = 0;  // which of the sequences with a token tile lo
     for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int b = b0 + lane;
-        const unsigned m = __ballot_sync(0xffffffffu, b < a.B && tiles[b] > lo);
+        const bool in = b0 + lane < a.B && tiles[b0 + lane] > lo;
+        const unsigned m = __ballot_sync(0xffffffffu, in);
         const int n = __popc(m);
         if (r < n) {
-            it.b = b0 + (int)__fns(m, 0, r + 1);
+            const int before = __popc(m & ((1u << lane) - 1));
+            b = b0 + __ffs(__ballot_sync(0xffffffffu, in && before == r)) - 1;
             break;
         }
         r -= n;
     }
-    it.start = start[it.b];
-    it.len = a.starts[it.b + 1] - it.start;
+    it.start = start[b];
+    it.len = a.starts[b + 1] - it.start;
     it.q0 = lo * tokens;
     it.h = hc / chunks;
     it.ch = hc - it.h * chunks;
+    for (int i = 0; i < 2; ++i) {
+        const int first = it.q0 + i * tile_tokens;
+        it.nb[i] = first >= it.len || (i && !two) ? 0 : min(first + tile_tokens - 1, it.len - 1) / KEYS + 1;
+    }
+    it.masked = (it.q0 + 1) / KEYS;
+    it.careful = 0;
     return true;
 }
 
-// The call's status, by two warps: bounds and slots.
-__device__ __forceinline__ void check_call(const PackedArgs &a, int t) {
-    int code = DEV_OK;
-    for (int b = t; b < a.B; b += 64) {
+// Clears the status and stores K and V into the cache, beside k_prompt: a warp a row.  Its CTAs fit an SM together with k_prompt's, whose
+// registers leave 4096.  (By k_prompt's own threads, before an item's first scores, it costs them registers that they lack.)
+constexpr int PS_WARPS = 4;
+__global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid_constant__ PackedArgs a) {
+    __shared__ int start[KV_MAX_BATCH], end[KV_MAX_BATCH];
+    pdl_launch();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = DEV_OK;
+    if (!a.kv.k) return;
+    for (int b = threadIdx.x; b < a.B; b += 32 * PS_WARPS) {
         const int s = a.starts[b], e = a.starts[b + 1];
-        if (s < 0 || e < s || e > a.T) code = DEV_BAD_POSITION;
+        start[b] = s;
+        end[b] = s < 0 || e > a.T ? s : e;
     }
-    if (a.kv.k) {
-        const long long slots = (long long)a.kv.n_pages * a.kv.page_size;
-#pragma unroll 8
-        for (int i = t; i < a.T; i += 64)
-            if (a.slots[i] >= slots) code = code ? code : DEV_BAD_PAGE;
-    }
-    // (one of the two codes where both occur)
-    if (code != DEV_OK) latch_error(a.status, code);
-}
-
-// K and V of `n` tokens from t0 on (of the packed rows) into the cache: 128 threads.
-template <int D>
-__device__ __forceinline__ void store_rows(const PackedArgs &a, int t0, int n, int h, int t) {
-    constexpr int CPR = D / 8, U = 8;  // 16-byte pieces of a row; loads on their way together
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
     const long long slots = (long long)a.kv.n_pages * a.kv.page_size;
-    for (int i0 = t; i0 < n * CPR; i0 += U * 128) {
-        uint4 k[U], v[U];
-        long long slot[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * 128, r = i / CPR, c = i % CPR;
-            slot[u] = -1;
-            if (i >= n * CPR) continue;
-            slot[u] = a.slots[t0 + r];
-            const long long src = (long long)(t0 + r) * a.kv_stride + h * D + c * 8;
-            k[u] = *reinterpret_cast<const uint4 *>(a.k + src);
-            v[u] = *reinterpret_cast<const uint4 *>(a.v + src);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (slot[u] < 0 || slot[u] >= slots) continue;
-            const int c = (i0 + u * 128) % CPR;
-            const long long page = slot[u] >> 32 ? slot[u] / a.kv.page_size : (long long)((uint32_t)slot[u] / (uint32_t)a.kv.page_size);
-            const long long dst = page * a.kv.stride_page + h * a.kv.stride_head + (slot[u] - page * a.kv.page_size) * a.kv.stride_slot + c * 8;
-            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.k) + dst) = k[u];
-            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.v) + dst) = v[u];
+    bool bad = false;
+    for (int t = blockIdx.x * PS_WARPS + (threadIdx.x >> 5); t < a.T; t += gridDim.x * PS_WARPS) {
+        bool mine = false;
+        for (int b = lane; b < a.B; b += 32) mine |= start[b] <= t && t < end[b];
+        if (!__any_sync(0xffffffffu, mine)) continue;
+        const long long slot = a.slots[t];
+        bad |= slot >= slots;
+        if (slot < 0 || slot >= slots) continue;
+        const long long page = slot >> 32 ? slot / a.kv.page_size : (long long)((uint32_t)slot / (uint32_t)a.kv.page_size);
+        const long long dst = page * a.kv.stride_page + (slot - page * a.kv.page_size) * a.kv.stride_slot, src = (long long)t * a.kv_stride;
+        const int per = a.d / 8;
+#pragma unroll 2
+        for (int i = lane; i < a.hkv * per; i += 32) {
+            const long long to = dst + (i / per) * a.kv.stride_head + (i % per) * 8;
+            const uint4 k = *reinterpret_cast<const uint4 *>(a.k + src + i * 8), v = *reinterpret_cast<const uint4 *>(a.v + src + i * 8);
+            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.k) + to) = k;
+            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.v) + to) = v;
         }
     }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) a.worker_code[blockIdx.x] = bad ? DEV_BAD_PAGE : DEV_OK;
 }
 
 template <int D, bool FP16>
-__global__ void __launch_bounds__(PA_THREADS, 1)
+__global__ void __launch_bounds__(THREADS, 1)
     k_prompt(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
              const __grid_constant__ PackedArgs a, int log_p) {
     using L = PromptShape<D>;
-    constexpr int TILES = L::TILES, UNITS = L::UNITS, STAGES = L::STAGES;
+    constexpr int TILES = L::TILES, UNITS = L::UNITS, STAGES = L::STAGES, AHEAD = L::AHEAD;
+    constexpr bool TWO = TILES == 2;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sq = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *ring = sq + TILES * L::QT;
@@ -148,264 +160,388 @@ __global__ void __launch_bounds__(PA_THREADS, 1)
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int P = 1 << log_p, tile_tokens = ROWS >> log_p, tokens = TILES * tile_tokens;
     const int chunks = a.group >> log_p, heads = a.hkv * chunks;
+    if (warp == 16) tmem_alloc(&S.tmem, TM_COLS);
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(&S.full[i], 1);
-            mbar_init(&S.empty[i], 1);
+            mbar_init(&S.empty[i], TILES);
         }
         mbar_init(&S.q_full, 1);
-        mbar_init(&S.drain, 1);
+        mbar_init(&S.q_free, TILES);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&S.s_full[i], 1);
-            mbar_init(&S.p_full[i], 4);
-            mbar_init(&S.o_full[i], 1);
+            mbar_init(&S.p_full[i][0], 8);
+            mbar_init(&S.p_full[i][1], 8);
+            mbar_init(&S.o_done[i], 1);
+            mbar_init(&S.o_free[i], 8);
+            mbar_init(&S.turn[i], 1);
+            mbar_init(&S.drain[i], 1);
         }
-        for (int i = 0; i < PA_MASKED; ++i) {
-            mbar_init(&S.v_full[i], 1);
-            mbar_init(&S.v_fixed[i], 2);
+        for (int i = 0; i < AHEAD; ++i) {
+            for (int k = 0; k < PA_MASKED; ++k) {
+                mbar_init(&S.v_full[i][k], 1);
+                mbar_init(&S.v_fixed[i][k], 1);
+            }
+            mbar_init(&S.item_full[i], 1);
+            mbar_init(&S.item_free[i], ROW_WARPS + 1 + TILES);
         }
-        S.abort = S.odd = 0;
+        S.abort = S.bad = 0;
         fence_mbarrier_init();
+    }
+    __syncthreads();
+    if (threadIdx.x == 32) {
         prefetch_tensormap(&qmap);
         prefetch_tensormap(&kmap);
         prefetch_tensormap(&vmap);
-        if (blockIdx.x == 0) *a.status = DEV_OK;  // (before any thread of this CTA reports; a wait runs out a second later)
     }
-    for (int i = threadIdx.x; i < D; i += PA_THREADS) S.first_odd[i] = 0x7fffffff;
-    for (int b = threadIdx.x; b < a.B; b += PA_THREADS) {
+    for (int b = threadIdx.x; b < a.B; b += THREADS) {
         const int s = a.starts[b], e = a.starts[b + 1];
         S.start[b] = s;
-        S.tiles[b] = s < 0 || e < s || e > a.T ? 0 : (e - s + tokens - 1) / tokens;
+        const bool bad = s < 0 || e < s || e > a.T;
+        S.tiles[b] = bad ? 0 : (e - s + tokens - 1) / tokens;
+        if (bad && blockIdx.x == 0) S.bad = 1;
     }
-    if (warp == 8) tmem_alloc(&S.tmem, TM_COLS);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = S.tmem;
-    PromptItem it = {};
-    const bool has = find_item(a, S.start, S.tiles, heads, chunks, tokens, it);  // (the same in every warp)
-    // a tile's blocks, and those that all rows see
-    auto blocks = [&](int tile) {
-        const int first = it.q0 + tile * tile_tokens;
-        return !has || first >= it.len ? 0 : min(first + tile_tokens - 1, it.len - 1) / KEYS + 1;
+    // Whether there is an n-th item: S.item[n % AHEAD].
+    auto item_there = [&](int n) {
+        return mbar_wait_short(&S.item_full[n % AHEAD], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort) && *(volatile int *)&S.item[n % AHEAD].len > 0;
     };
-    const int nb0 = blocks(0), nb1 = TILES == 2 ? blocks(1) : 0, nmax = max(nb0, nb1), masked = has ? (it.q0 + 1) / KEYS : 0;
 
-    // registers: of the launch's 3 x 128 x 168 the last warpgroup keeps 128 x 72, the others take 128 x 216 each
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 8) {
-            if (has && elect_one()) {
-                // ---- TMA: the queries, then K 0, V 0, K 1, V 1, ...
-                int issued = 0;
-                mbar_arrive_expect_tx(&S.q_full, (uint32_t)(TILES * L::QT));
-                for (int i = 0; i < TILES; ++i)
-                    for (int c = 0; c < D / 64; ++c)
-                        tma_load_4d(sq + i * L::QT + c * SUB, &qmap, c * 64, 0, it.h * chunks + it.ch, it.start + it.q0 + i * tile_tokens, &S.q_full);
+    if (warp >= ROW_WARPS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+        if (warp == 16) {
+            if (elect_one()) {
+                // ---- TMA: an item's queries, then K and V in the ring's order
+                int issued = 0, n = 0;
                 bool ok = true;
-                for (int j = 0; ok && j < 2 * nmax; ++j)
-                    for (int u = 0; u < UNITS; ++u) {
-                        const int slot = issued % STAGES;
-                        if (!mbar_wait(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort)) {
-                            ok = false;
-                            break;
+                for (; ok; ++n) {
+                    if (!item_there(n)) break;
+                    const int s = n % AHEAD;
+                    const PromptItem it = S.item[s];
+                    mbarrier_arrive_one(&S.item_free[s]);
+                    const int nmax = max(it.nb[0], it.nb[1]);
+                    if (n > 0 && !mbar_wait_short(&S.q_free, (n - 1) & 1, a.status, DEV_TIMEOUT_SLOT, &S.abort)) break;
+                    mbar_arrive_expect_tx(&S.q_full, (uint32_t)(TILES * L::QT));
+                    for (int i = 0; i < TILES; ++i)
+                        for (int c = 0; c < D / 64; ++c)
+                            tma_load_4d(sq + i * L::QT + c * SUB, &qmap, c * 64, 0, it.h * chunks + it.ch, it.start + it.q0 + i * tile_tokens, &S.q_full);
+                    for (int k = it.careful ? nmax - it.masked : 0; k < PA_MASKED; ++k) mbarrier_arrive_one(&S.v_full[s][k]);
+                    for (int x = 0; ok && x < 2 * nmax; ++x) {
+                        const int y = at_place(x, nmax, TWO), kb = y < 0 ? ~y : y;
+                        for (int u = 0; u < UNITS; ++u) {
+                            const int slot = issued % STAGES;
+                            if (!mbar_wait_short(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort)) {
+                                ok = false;
+                                break;
+                            }
+                            ++issued;
+                            uint64_t *bar = &S.full[slot];
+                            if (y < 0 && it.careful && kb >= it.masked) {  // V that is looked at first
+                                mbarrier_arrive_one(bar);
+                                bar = &S.v_full[s][kb - it.masked];
+                                if (u == 0) mbar_arrive_expect_tx(bar, (uint32_t)(UNITS * L::UNIT));
+                            } else {
+                                mbar_arrive_expect_tx(bar, (uint32_t)L::UNIT);
+                            }
+                            for (int c = 0; c < L::DU / 64; ++c)
+                                tma_load_3d(ring + slot * L::UNIT + c * SUB, y < 0 ? &vmap : &kmap, u * L::DU + c * 64, it.h, it.start + kb * KEYS, bar);
                         }
-                        ++issued;
-                        const int kb = j >> 1;
-                        uint64_t *bar = &S.full[slot];
-                        if ((j & 1) && kb >= masked) {  // V that is looked at first
-                            mbarrier_arrive_one(bar);
-                            bar = &S.v_full[kb - masked];
-                            if (u == 0) mbar_arrive_expect_tx(bar, (uint32_t)(UNITS * L::UNIT));
-                        } else {
-                            mbar_arrive_expect_tx(bar, (uint32_t)L::UNIT);
-                        }
-                        for (int c = 0; c < L::DU / 64; ++c)
-                            tma_load_3d(ring + slot * L::UNIT + c * SUB, (j & 1) ? &vmap : &kmap, u * L::DU + c * 64, it.h, it.start + kb * KEYS, bar);
                     }
+                }
                 if (*(volatile int *)&S.abort) {  // error path: the copies in flight get a bounded chance to land
-                    bool landed = mbar_wait(&S.q_full, 0, nullptr, 0, nullptr);
-                    for (int h = issued > STAGES ? issued - STAGES : 0; landed && h < issued; ++h)
-                        landed = mbar_wait(&S.full[h % STAGES], (h / STAGES) & 1, nullptr, 0, nullptr);
-                    for (int k = 0; landed && k < PA_MASKED; ++k)
-                        if (issued > ((masked + k) * 2 + 2) * UNITS - 1) landed = mbar_wait(&S.v_full[k], 0, nullptr, 0, nullptr);
+                    const uint64_t t0 = globaltimer_ns();
+                    while (globaltimer_ns() - t0 < WAIT_LIMIT_NS / 100) __nanosleep(1000);
                 }
             }
-        } else if (warp == 9) {
-            if (has && elect_one()) {
-                // ---- MMAs: for every block, tile after tile, O += P V of the block before, then S
-                int pos = 0;
-                bool ok = mbar_wait(&S.q_full, 0, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-                auto landed = [&](int at) {
-                    ok = ok && mbar_wait(&S.full[at % STAGES], (at / STAGES) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+        } else if (warp < 17 + TILES) {
+            if (elect_one()) {
+                // ---- MMAs of tile i
+                const int i = warp - 17;
+                const uint8_t *q = sq + i * L::QT;
+                const uint32_t o = tmem + TM_O + i * D;
+                bool ok = true;
+                int pos = 0, step = 0, used = 0, used_o = 0;  // blocks' K and V, sections, blocks and items of the tile so far
+                auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.abort); };
+                auto landed = [&](int place) {
+                    for (int u = 0; u < UNITS; ++u) wait(&S.full[(place * UNITS + u) % STAGES], (place * UNITS + u) / STAGES, DEV_TIMEOUT_LOAD);
                 };
-                for (int j = 0; ok && j <= nmax; ++j) {
-                    const int vp = pos, kp = pos + (j ? UNITS : 0);
-                    pos = kp + UNITS;
-                    for (int i = 0; ok && i < TILES; ++i) {
-                        const int nb = i ? nb1 : nb0;
-                        if (j > 0 && j <= nb) {
-                            ok = mbar_wait(&S.p_full[i], (j - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-                            // (the last block's keys behind the sequence's end are not multiplied, to 16)
-                            const int steps = min(KEYS, it.len - (j - 1) * KEYS + 15) / 16;
-                            for (int u = 0; ok && u < UNITS; ++u) {
-                                landed(vp + u);
-                                if (j - 1 >= masked) ok = ok && mbar_wait(&S.v_fixed[j - 1 - masked], 0, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-                                if (!ok) break;
-                                tc_fence_after();
-                                mma_values<D, FP16>(tmem + TM_O + i * D, tmem + i * KEYS, ring + ((vp + u) % STAGES) * L::UNIT, u, steps, j == 1);
-                            }
-                            if (ok && j == nb) mma_commit(&S.o_full[i]);
+                auto unit = [&](int place, int u) { return ring + ((place * UNITS + u) % STAGES) * L::UNIT; };
+                auto scores = [&](int buf, int place) {
+                    for (int u = 0; u < UNITS; ++u) mma_scores<D, FP16>(tmem + buf * KEYS, q, unit(place, u), u);
+                    mma_commit(&S.s_full[buf]);
+                };
+                // (K and V that a tile has seen are given back by its rows, when they see S and O: each commit here costs 200 cycles)
+                auto skip = [&](int place) {
+                    for (int u = 0; u < UNITS; ++u) mbarrier_arrive_one(&S.empty[(place * UNITS + u) % STAGES]);
+                };
+                for (int n = 0; ok; ++n) {
+                    if (!item_there(n)) break;
+                    const PromptItem *it = &S.item[n % AHEAD];
+                    const int nb = it->nb[i], nmax = max(it->nb[0], it->nb[1]), len = it->len, masked = it->careful ? it->masked : nmax;
+                    mbarrier_arrive_one(&S.item_free[n % AHEAD]);
+                    // P V of block j from the first part of P on
+                    auto values = [&](int buf, int j, int place, int phase) {
+                        // (the last block's keys behind the sequence's end are not multiplied, to 16)
+                        const int steps = min(KEYS, len - j * KEYS + 15) / 16;
+                        for (int u = 0; u < UNITS; ++u) mma_values<D, FP16>(o, tmem + buf * KEYS, unit(place, u), u, 0, steps, j == 0);
+                        wait(&S.p_full[buf][1], phase, DEV_TIMEOUT_MMA);
+                        if (!ok) return;
+                        tc_fence_after();
+                        for (int u = 0; u < UNITS; ++u) mma_values<D, FP16>(o, tmem + buf * KEYS, unit(place, u), u, 1, steps, j == 0);
+                    };
+                    auto values_ready = [&](int j, int place) {
+                        landed(place);
+                        if (j >= masked) wait(&S.v_fixed[n % AHEAD][j - masked], n / AHEAD, DEV_TIMEOUT_LOAD);
+                        if (j == 0 && used_o > 0 && nb > 0) wait(&S.o_free[i], used_o - 1, DEV_TIMEOUT_MMA);
+                    };
+                    wait(&S.q_full, n, DEV_TIMEOUT_LOAD);
+                    if (TWO) {  // for every block O += P V of the one before, then S; the tiles in turns
+#pragma unroll 1
+                        for (int j = 0; ok && j <= nmax; ++j, ++step) {
+                            const int vp = pos + v_place(j - 1, nmax, true), kp = pos + k_place(j, true);
+                            if (j > 0) values_ready(j - 1, vp);
+                            if (j < nmax) landed(kp);
+                            if (i + step > 0) wait(&S.turn[i], step + i - 1, DEV_TIMEOUT_MMA);
+                            if (j > 0 && j <= nb) wait(&S.p_full[i][0], used + j - 1, DEV_TIMEOUT_MMA);
+                            if (!ok) break;
+                            tc_fence_after();
+                            if (j > 0 && j <= nb) values(i, j - 1, vp, used + j - 1);
+                            if (ok && j < nb) scores(i, kp);
+                            mbarrier_arrive_one(&S.turn[i ^ 1]);
+                            if (j > 0 && j == nb) mma_commit(&S.o_done[i]);
+                            if (j == max(nb, 1) - 1) mma_commit(&S.q_free);
+                            if (j > nb) skip(vp);  // (blocks that only the other tile sees)
+                            if (j >= nb && j < nmax) skip(kp);
                         }
-                        if (ok && j > 0 && i == TILES - 1)
-                            for (int u = 0; u < UNITS; ++u) {
-                                landed(vp + u);
-                                mma_commit(&S.empty[(vp + u) % STAGES]);
-                            }
-                        if (ok && j < nb) {
-                            for (int u = 0; ok && u < UNITS; ++u) {
-                                landed(kp + u);
+                    } else {  // S of the next block, then O += P V of this one
+                        landed(pos);
+                        if (ok) {
+                            tc_fence_after();
+                            scores(used & 1, pos);
+                            if (nmax == 1) mma_commit(&S.q_free);
+                        }
+#pragma unroll 1
+                        for (int j = 0; ok && j < nmax; ++j) {
+                            const int vp = pos + v_place(j, nmax, false), kp = pos + k_place(j + 1, false), x = used + j;
+                            if (j + 1 < nmax) {
+                                landed(kp);
                                 if (!ok) break;
                                 tc_fence_after();
-                                mma_scores<D, FP16>(tmem + i * KEYS, sq + i * L::QT, ring + ((kp + u) % STAGES) * L::UNIT, u);
+                                scores((x + 1) & 1, kp);
+                                if (j + 2 == nmax) mma_commit(&S.q_free);
                             }
-                            if (ok) mma_commit(&S.s_full[i]);
+                            values_ready(j, vp);
+                            wait(&S.p_full[x & 1][0], x >> 1, DEV_TIMEOUT_MMA);
+                            if (!ok) break;
+                            tc_fence_after();
+                            values(x & 1, j, vp, x >> 1);
+                            mma_commit(&S.o_done[0]);
                         }
                     }
-                    if (ok && j < nmax)
-                        for (int u = 0; u < UNITS; ++u) mma_commit(&S.empty[(kp + u) % STAGES]);
+                    pos += 2 * nmax;
+                    used += nb;
+                    used_o += nb > 0;
                 }
-                if (!ok) {  // every MMA issued completes before TMEM is released
-                    mma_commit(&S.drain);
-                    mbar_wait(&S.drain, 0, nullptr, 0, nullptr);
-                }
+                mma_commit(&S.drain[i]);  // every MMA issued completes before TMEM is released
+                mbar_wait_short(&S.drain[i], 0, nullptr, 0, nullptr);
             }
-        } else {
-            const int t = (warp - 10) * 32 + lane;
-            // ---- V of the blocks that not all rows see
+        } else if (warp == 19) {
+            // ---- the list, one item ahead; V of items done again
+            int total = 0, most = 0, pos = 0, given = 0;  // given: items of the CTA's share so far
+            for (int b = lane; b < a.B; b += 32) total += S.tiles[b], most = max(most, S.tiles[b]);
+            total = __reduce_add_sync(0xffffffffu, total);
+            most = __reduce_max_sync(0xffffffffu, most);
             bool ok = true;
-            for (int j = masked; ok && j < nmax; ++j) {
-                ok = mbar_wait(&S.v_full[j - masked], 0, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-                if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                for (int u = 0; u < UNITS; ++u) {
-                    const int slot = ((2 * j + 1) * UNITS + u) % STAGES;
-                    const uint32_t at = smem_u32(ring + slot * L::UNIT);
-#pragma unroll 4
-                    for (int i = t; i < L::UNIT / 16; i += 64) {
-                        const int r = (i >> 3) & 127, key = j * KEYS + r;
-                        uint4 x = ld_shared_u4(at + i * 16);
-                        if (key >= it.len) {
-                            if (key < ((it.len + 15) & ~15)) st_shared_u4(at + i * 16, make_uint4(0, 0, 0, 0));
-                            continue;
-                        }
-                        uint32_t w[4] = {x.x, x.y, x.z, x.w};
-                        if (!(odd_halves<FP16>(w[0]) | odd_halves<FP16>(w[1]) | odd_halves<FP16>(w[2]) | odd_halves<FP16>(w[3]))) continue;
-                        const int d0 = u * L::DU + (i >> 10) * 64 + (((i & 7) ^ (r & 7)) << 3);
+            auto next_item = [&]() {  // there and back over the CTAs: each gets long and short ones
+                PromptItem it{};
+                const long long x = (long long)given * gridDim.x + (given & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+                ++given;
+                if (!find_item(a, S.start, S.tiles, x, total, most, heads, chunks, tokens, tile_tokens, TWO, it)) it.len = 0;
+                return it;
+            };
+            auto publish = [&](int n, const PromptItem &it) {
+                const int s = n % AHEAD;
+                if (it.careful)
+                    for (int d = lane; d < D; d += 32) S.first_odd[s][d] = 0x7fffffff;
+                __syncwarp();
+                if (lane == 0) {
+                    S.item[s] = it;
+                    S.odd[s] = 0;
+                    mbarrier_arrive_one(&S.item_full[s]);
+                }
+                __syncwarp();
+                return it.len > 0;
+            };
+            int told = 0;  // items that the others have been told of, one ahead where there is one
+            if (publish(told++, next_item())) {
+                const PromptItem next = next_item();
+                if (next.len > 0) publish(told++, next);
+            }
+            for (int n = 0; ok && S.item[n % AHEAD].len > 0; ++n) {
+                const int s = n % AHEAD;
+                const PromptItem it = S.item[s];
+                const int nmax = max(it.nb[0], it.nb[1]);
+                for (int k = 0; ok && k < PA_MASKED; ++k) {
+                    const int j = it.masked + k;
+                    if (it.careful) ok = mbar_wait_short(&S.v_full[s][k], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                    for (int u = 0; it.careful && j < nmax && u < UNITS; ++u) {
+                        const int slot = ((pos + v_place(j, nmax, TWO)) * UNITS + u) % STAGES;
+                        const uint32_t at = smem_u32(ring + slot * L::UNIT);
+                        const int all = it.len - j * KEYS;  // keys of the block
+                        for (int r = all + (lane >> 3); r < KEYS; r += 4)
+                            for (int c = 0; c < L::DU / 64; ++c) st_shared_u4(at + c * SUB + r * 128 + (lane & 7) * 16, make_uint4(0, 0, 0, 0));
+                        __syncwarp();
+                        // (loads of many rows on their way together: one after the other they took 8000 cycles)
+                        constexpr int U = 8;
+#pragma unroll 1
+                        for (int x0 = lane; x0 < L::UNIT / 16; x0 += 32 * U) {
+                            uint4 v[U];
+                            uint32_t any = 0;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const uint32_t half = 0xffffu << (16 * (e & 1));
-                            if (odd_halves<FP16>(w[e >> 1]) & half) {
-                                w[e >> 1] &= ~half;
-                                atomicMin(&S.first_odd[d0 + e], key);
+                            for (int y = 0; y < U; ++y) v[y] = ld_shared_u4(at + (x0 + 32 * y) * 16);
+#pragma unroll
+                            for (int y = 0; y < U; ++y)
+                                any |= odd_halves<FP16>(v[y].x) | odd_halves<FP16>(v[y].y) | odd_halves<FP16>(v[y].z) | odd_halves<FP16>(v[y].w);
+                            if (any == 0) continue;
+#pragma unroll 1
+                            for (int e = 0; e < 8 * U; ++e) {  // (value by value: this is rare)
+                                const int x = x0 + 32 * (e >> 3), r = (x >> 3) & 127;
+                                const uint32_t to = at + x * 16 + 2 * (e & 7);
+                                uint16_t y;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(to) : "memory");
+                                if (!odd_halves<FP16>(y)) continue;
+                                asm volatile("st.shared.u16 [%0], %1;" ::"r"(to), "h"((uint16_t)0) : "memory");
+                                atomicMin(&S.first_odd[s][u * L::DU + (x >> 10) * 64 + (((x & 7) ^ (r & 7)) << 3) + (e & 7)], j * KEYS + r);
                             }
                         }
-                        st_shared_u4(at + i * 16, make_uint4(w[0], w[1], w[2], w[3]));
-                        S.odd = 1;
                     }
+                    fence_proxy_async_shared();
+                    __syncwarp();
+                    if (lane == 0) mbarrier_arrive_one(&S.v_fixed[s][k]);
                 }
-                fence_proxy_async_shared();
-                __syncwarp();
-                if (lane == 0) mbarrier_arrive_one(&S.v_fixed[j - masked]);
+                pos += 2 * nmax;
+                // when everybody is through with it: the next one, or this one again
+                ok = ok && mbar_wait_short(&S.item_free[s], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                PromptItem next = it;
+                next.careful = 1;
+                if (it.careful || !*(volatile int *)&S.odd[s]) next = next_item();
+                if (next.len > 0 || told == n + 1) publish(told++, next);
             }
-            if (blockIdx.x == 0) check_call(a, t);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        // ---- softmax: thread r of tile i the row of token first + r / P, head r % P
-        const int i = warp >> 2, w = warp & 3, nb = i ? nb1 : nb0, row = w * 32 + lane;
-        const int first = it.q0 + i * tile_tokens, token = first + (row >> log_p);
-        if (nb > 0) {
-            if (a.kv.k && it.ch == 0) store_rows<D>(a, it.start + first, min(tile_tokens, it.len - first), it.h, row);
-            const uint32_t lanes = (uint32_t)(w * 32) << 16, ts = tmem + lanes + i * KEYS, to = tmem + lanes + TM_O + i * D;
-            const float c = a.scale * 1.4426950408889634f;
-            Row r;
-            bool ok = true;
-            for (int j = 0; j < nb; ++j) {
-                ok = mbar_wait(&S.s_full[i], j & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ROW_REGS));
+        // ---- rows: row r of tile i is token first + r / P, head r % P
+        const int i = warp >> 3, half = (warp >> 2) & 1, w = warp & 3, row = w * 32 + lane, id = 1 + i * 4 + w;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16, ts = tmem + lanes + 64 * half, to = tmem + lanes + TM_O + i * D + half * (D / 2);
+        const float c = a.scale * 1.4426950408889634f;
+        const bool wide = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;
+        float *top = S.top[i][0];
+        Row r{0.f, 0.f};
+        bool ok = true;
+        int used = 0, used_o = 0, pos = 0;  // blocks and items of the tile so far, blocks' K and V of the CTA
+        auto release = [&](int place) {
+            if (w == 0 && half == 0 && lane == 0)
+                for (int u = 0; u < UNITS; ++u) mbarrier_arrive_one(&S.empty[(place * UNITS + u) % STAGES]);
+        };
+        for (int n = 0; ok; ++n) {
+            const int s = n % AHEAD;
+            const volatile PromptItem &it = S.item[s];  // (read again at the end, to spare registers)
+            if (pair_any(id, !mbar_wait_short(&S.item_full[s], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort))) break;
+            const int nb = it.nb[i], first = it.q0 + i * tile_tokens;
+            if (it.len == 0) break;
+            const int nmax = max(it.nb[0], it.nb[1]);
+            if (nb == 0) {
+                pos += 2 * nmax;
+                if (lane == 0) mbarrier_arrive_one(&S.item_free[s]);
+                continue;
+            }
+            for (int j = 0; ok && j < nb; ++j, ++used) {
+                const int buf = TWO ? i : used & 1;
+                bool there = mbar_wait_short(&S.s_full[buf], (TWO ? used : used >> 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort), o_waited = TWO || j == 0;
+                there = __all_sync(0xffffffffu, there);
+                release(pos + k_place(j, TWO));
+                if (TWO && j > 0) release(pos + v_place(j - 1, nmax, TWO));
                 tc_fence_after();
-                uint32_t s[KEYS];
+                uint32_t s[64];
 #pragma unroll
-                for (int x = 0; x < KEYS; x += 32) tmem_ld_32cols(ts + x, *reinterpret_cast<uint32_t(*)[32]>(&s[x]));
+                for (int x = 0; x < 64; x += 32) tmem_ld_32cols(ts + buf * KEYS + x, *reinterpret_cast<uint32_t(*)[32]>(&s[x]));
                 tmem_ld_wait();
                 if (j * KEYS + KEYS - 1 > first) {
-                    const int last = token - j * KEYS;
+                    const int last = first + (row >> log_p) - j * KEYS - 64 * half;
 #pragma unroll
-                    for (int x = 0; x < KEYS; ++x)
+                    for (int x = 0; x < 64; ++x)
                         if (x > last) s[x] = __float_as_uint(-INFINITY);
                 }
-                softmax_block<D, FP16>(r, s, c, j == 0, ts, to);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbarrier_arrive_one(&S.p_full[i]);
-            }
-            if (ok) ok = mbar_wait(&S.o_full[i], 0, a.status, DEV_TIMEOUT_MMA, &S.abort);
-            for (int k = 0; ok && masked + k < nmax; ++k) ok = mbar_wait(&S.v_fixed[k], 0, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-            if (__all_sync(0xffffffffu, ok)) {
-                // rows go out through the queries' place (all scores of the tile are there), a row's pieces by neighbouring lanes
-                tc_fence_after();
-                const float f = row_factor(r);
-                const bool odd = *(volatile int *)&S.odd;
-                const uint32_t stage = smem_u32(sq + i * L::QT) + w * 32 * (D * 2);
-#pragma unroll 1
-                for (int x = 0; x < D; x += 32) {
-                    uint32_t o[32];
-                    tmem_ld_32cols(to + x, o);
-                    tmem_ld_wait();
-                    if (odd)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (S.first_odd[x + e] <= token) o[e] = 0x7fffffffu;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y)
-                            v[y] = pack16<FP16>(__uint_as_float(o[e + 2 * y]) * f, __uint_as_float(o[e + 2 * y + 1]) * f);
-                        st_shared_u4(stage + lane * (D * 2) + ((((x + e) >> 3) ^ (lane & 7)) << 4), make_uint4(v[0], v[1], v[2], v[3]));
+                auto o_ready = [&]() {  // (with two tiles S of this block has come after O of the one before)
+                    bool o = true;
+                    if (!o_waited) {
+                        o = mbar_wait_short(&S.o_done[0], (used - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+                        release(pos + v_place(j - 1, nmax, TWO));
                     }
-                }
-                __syncwarp();
-                constexpr int CPR = D / 8, RPI = 32 / CPR;  // pieces of a row, rows of a step
-                const int piece = lane % CPR, head = it.h * a.group + it.ch * P;
-#pragma unroll 4
-                for (int x = 0; x < 32; x += RPI) {
-                    const int rr = x + lane / CPR, tk = first + ((w * 32 + rr) >> log_p);
-                    if (tk >= it.len) continue;
-                    const uint4 v = ld_shared_u4(stage + rr * (D * 2) + ((piece ^ (rr & 7)) << 4));
-                    *reinterpret_cast<uint4 *>(a.out + ((long long)(it.start + tk) * a.hq + head + ((w * 32 + rr) & (P - 1))) * D + piece * 8) = v;
-                }
-                if (a.lse && token < it.len)
-                    a.lse[(long long)(it.start + token) * a.hq + head + (row & (P - 1))] = row_lse<FP16>(r, a.scale);
+                    o_waited = true;
+                    return __all_sync(0xffffffffu, o) != 0;
+                };
+                ok = softmax_half<D, FP16>(r, s, there, c, j == 0, ts + buf * KEYS, to, id, top, half, row, o_ready, [&](int part) {
+                    if (!TWO && part == 1) o_ready();  // (every phase is waited for)
+                    if (lane == 0) mbarrier_arrive_one(&S.p_full[buf][part]);
+                });
             }
+            bool there = mbar_wait_short(&S.o_done[i], (TWO ? used_o : used - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+            ++used_o;
+            release(pos + v_place(nb - 1, nmax, TWO));
+            pos += 2 * nmax;
+            const bool careful = it.careful != 0;
+            for (int k = 0; careful && there && k < PA_MASKED; ++k) there = mbar_wait_short(&S.v_fixed[s][k], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+            if (!ok || pair_any(id, !there)) break;
+            top[half * ROWS + row] = r.l;
+            pair_sync(id);
+            r.l += top[(half ^ 1) * ROWS + row];
+            tc_fence_after();
+            const int head = it.h * a.group + it.ch * P + (row & (P - 1)), token = first + (row >> log_p);
+            const bool real = token < it.len;
+            const long long out_row = (long long)(it.start + token) * a.hq + head;
+            const bool odd = store_half<D, FP16>(to, row_factor(r), a.out + out_row * D + half * (D / 2), real, wide, careful,
+                                                 [&](int d) { return S.first_odd[s][half * (D / 2) + d] <= token; });
+            tc_fence_before();
+            if (__any_sync(0xffffffffu, odd) && lane == 0) *(volatile int *)&S.odd[s] = 1;
+            __syncwarp();
+            if (lane == 0) {
+                mbarrier_arrive_one(&S.o_free[i]);
+                mbarrier_arrive_one(&S.item_free[s]);
+            }
+            if (a.lse && half == 0 && real) a.lse[out_row] = row_lse<FP16>(r, a.scale);
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 8) tmem_dealloc(tmem, TM_COLS);
+    if (warp == 16) tmem_dealloc(tmem, TM_COLS);
+    pdl_wait();  // (k_prompt_store: nothing else is waited for, since it began after all before it)
+    if (blockIdx.x == 0 && warp == 19) {
+        int code = S.bad ? DEV_BAD_POSITION : DEV_OK;
+        for (int i = lane; a.kv.k && i < a.workers; i += 32) code = code ? code : *(volatile int *)&a.worker_code[i];
+        if (code != DEV_OK) latch_error(a.status, code);
+    }
 }
 
 template <int D, bool FP16>
-cudaError_t launch(const PackedArgs &a, cudaStream_t st) {
+cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     using L = PromptShape<D>;
     static_assert(L::SMEM + sizeof(PromptState<D>) <= 227 * 1024, "shared memory");
-    const cudaError_t e = cudaFuncSetAttribute(k_prompt<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(k_prompt<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
+    // (an SM divides its memory into cache and shared one kernel's way at a time: without this the two do not share an SM)
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_prompt_store, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
     int log_p = 0;
     while (log_p < 4 && a.group % (2 << log_p) == 0) ++log_p;
     const int P = 1 << log_p, tokens = L::TILES * (ROWS / P), heads = a.hq / P;
-    const long long tiles = std::min<long long>(a.T / tokens + a.B, a.T), grid = tiles * heads;
-    if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+    const long long items = std::min<long long>(a.T / tokens + a.B, a.T) * heads;
+    const int grid = (int)std::min<long long>(items, gemm_ctas());
+    if (grid < 1) return cudaErrorInvalidDevice;
     CUtensorMap qm, km, vm;
     const uint64_t qs = (uint64_t)a.q_stride * 2, ks = (uint64_t)a.kv_stride * 2;
     const uint64_t qd[4] = {(uint64_t)D, (uint64_t)P, (uint64_t)heads, (uint64_t)a.T}, qst[3] = {D * 2, (uint64_t)P * D * 2, qs};
@@ -414,13 +550,15 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t st) {
     const uint32_t kb[3] = {64, 1, KEYS};
     if (!encode_map_16(&qm, a.q, 4, qd, qst, qb) || !encode_map_16(&km, a.k, 3, kd, kst, kb) || !encode_map_16(&vm, a.v, 3, kd, kst, kb))
         return cudaErrorInvalidValue;
-    k_prompt<D, FP16><<<(unsigned)grid, PA_THREADS, L::SMEM, st>>>(qm, km, vm, a, log_p);
-    return cudaGetLastError();
+    a.workers = a.kv.k ? std::min({(a.T + PS_WARPS - 1) / PS_WARPS, gemm_ctas(), PROMPT_MAX_WORKERS}) : 1;
+    k_prompt_store<<<a.workers, 32 * PS_WARPS, 0, st>>>(a);
+    const cudaError_t c = cudaGetLastError();
+    return c != cudaSuccess ? c : launch_pdl(k_prompt<D, FP16>, grid, THREADS, L::SMEM, st, qm, km, vm, a, log_p);
 }
 
 }  // namespace
 
-cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st) {
+cudaError_t launch_prompt_attention(PackedArgs &a, cudaStream_t st) {
     if (a.fp16) return a.d == 64 ? launch<64, true>(a, st) : a.d == 128 ? launch<128, true>(a, st) : launch<256, true>(a, st);
     return a.d == 64 ? launch<64, false>(a, st) : a.d == 128 ? launch<128, false>(a, st) : launch<256, false>(a, st);
 }

@@ -10,11 +10,11 @@
 // of about the same cost: how ragged the lengths are does not matter, and the host need not know them.  Where a stretch begins or ends
 // inside a (sequence, KV head) the CTA leaves maximum, sum and unnormalised output in scratch, and k_tree_join joins them.
 //
-// Warps 0-7: rows, a thread each (queries, softmax, outputs).  Warps 8-11 copy K and V, row by row, since pages may have any length:
-// 16 bytes a lane, asynchronously.  Warp 12: MMAs.  The blocks with nodes among their keys, a (sequence, KV head)'s last one or
-// two, are waited for by the warps that copy them: they store the nodes' rows into the cache, and look for infinite and NaN values
-// of V, which would be NaN in rows that do not see them (0 x NaN): such values become zero, and who sees them is noted for each
-// dimension.
+// Warps 0-15: rows (queries, softmax, outputs).  Warps 16 and 17 see to K and V: tiled copies of the rows that a page has in a piece where
+// pages hold a multiple of 8, row by row else, 16 bytes a lane.  Warps 18 and 19: the tiles' MMAs.
+// The blocks with nodes among their keys, a (sequence, KV head)'s last one or two, are copied row by row and waited for by those
+// who copy: they store the nodes' rows into the cache, and look for infinite and NaN values of V, which would be NaN in rows that do not
+// see them (0 x NaN): such values become zero, and who sees them is noted for each dimension.
 #include <algorithm>
 
 #include "flash.cuh"
@@ -26,7 +26,6 @@ using namespace flash;
 
 namespace {
 
-constexpr int TA_THREADS = 512;
 constexpr int TA_ROW = 2;        // what beginning and ending a (sequence, KV head) costs a CTA, in blocks
 constexpr int TA_MIN = 3;        // places of a CTA's stretch at least
 constexpr int TA_MASKS = 8;      // blocks whose masks are kept
@@ -43,7 +42,7 @@ struct TreeShape : Shape<D> {
 // Counts of the list: a (sequence, KV head, chunk of rows) is a unit; it has its blocks and TA_ROW places more in front.
 struct TreeList {
     int first[KV_MAX_BATCH + 1];  // places before sequence b
-    int start[KV_MAX_BATCH], len[KV_MAX_BATCH], nodes[KV_MAX_BATCH];
+    int len[KV_MAX_BATCH], nodes[KV_MAX_BATCH];
 };
 
 __device__ __forceinline__ bool tree_ok(const PackedArgs &a, int b) {
@@ -66,7 +65,7 @@ __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
         if (b < a.B) {
             const bool ok = tree_ok(a, b);
             const int n = ok ? a.starts[b + 1] - a.starts[b] : 0, len = ok ? a.kv.lens[b] : 0;
-            T.start[b] = a.starts[b], T.len[b] = len, T.nodes[b] = n;
+            T.len[b] = len, T.nodes[b] = n;
             if (n > 0) x = a.hkv * chunks_of<D>(n * a.group) * (blocks_of(len, n) + TA_ROW);
         }
         for (int o = 1; o < 32; o <<= 1) {
@@ -144,14 +143,19 @@ struct Segment {
     }
 };
 
+constexpr int TA_COPY_WARPS = 2, TA_COPY_ROWS = KEYS / TA_COPY_WARPS;  // rows of a block of one
+
 template <int D>
 struct TreeState {
     using L = TreeShape<D>;
-    uint64_t full[L::STAGES], empty[L::STAGES], q_full[2], s_full[2], p_full[2], o_full[2], o_free[2], tail[L::RING_SEGS], cleared, drain;
+    // s_full, p_full: S and P of the first tile's place, of the second tile, and of the second place where one tile uses both.  (Each has one
+    // party that arrives and one that waits, and they see all of its phases: who skips one takes an older one for it.)
+    uint64_t full[L::STAGES], empty[L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], tail[L::RING_SEGS], cleared, drain[2];
     uint32_t tmem;
     int abort, bad_page, bad_tree;
+    float top[2][2][ROWS];              // what the two threads of a row tell each other
     uint32_t valid[TA_MASKS][4];        // keys of a block whose pages are in the cache
-    ulonglong2 rows[4][32];             // a copying warp's rows: where K and V come from
+    ulonglong2 rows[TA_COPY_WARPS][2][TA_COPY_ROWS];  // a copying warp's rows of two blocks: where K and V come from
     // of a segment: who sees infinite or NaN values, in each dimension: the nodes' bits, or everybody (a cached slot)
     int odd[L::RING_SEGS];
     unsigned long long odd_nodes[L::RING_SEGS][D];
@@ -166,9 +170,14 @@ __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src
 __device__ __forceinline__ void cp_async_arrive(uint64_t *bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+__device__ __forceinline__ void mbarrier_arrive_many(uint64_t *bar, uint32_t n) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
+}
 
+// box: rows of a page that one tiled copy brings (0: none do).
 template <int D, bool FP16>
-__global__ void __launch_bounds__(TA_THREADS, 1) k_tree(const __grid_constant__ PackedArgs a) {
+__global__ void __launch_bounds__(THREADS, 1)
+    k_tree(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PackedArgs a, int box) {
     using L = TreeShape<D>;
     constexpr int TILES = L::TILES, UNITS = L::UNITS, STAGES = L::STAGES;
     extern __shared__ uint8_t smem_raw[];
@@ -178,239 +187,342 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_tree(const __grid_constant__ 
     __shared__ TreeList T;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     pdl_launch();
+    if (warp == 18) tmem_alloc(&S.tmem, TM_COLS);
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
-            mbar_init(&S.full[i], 128);
-            mbar_init(&S.empty[i], 1);
+            mbar_init(&S.full[i], 32 * TA_COPY_WARPS);
+            mbar_init(&S.empty[i], 2);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&S.q_full[i], 4);
-            mbar_init(&S.s_full[i], 1);
-            mbar_init(&S.p_full[i], 4);
-            mbar_init(&S.o_full[i], 1);
-            mbar_init(&S.o_free[i], 4);
+            mbar_init(&S.q_full[i], 8);
+            mbar_init(&S.o_done[i], 1);
+            mbar_init(&S.o_free[i], 8);
+            mbar_init(&S.turn[i], 1);
+            mbar_init(&S.drain[i], 1);
         }
-        for (int i = 0; i < L::RING_SEGS; ++i) mbar_init(&S.tail[i], 128);
-        mbar_init(&S.cleared, 128);
-        mbar_init(&S.drain, 1);
+        for (int i = 0; i < 3; ++i) {
+            mbar_init(&S.s_full[i], 1);
+            mbar_init(&S.p_full[i][0], 8);
+            mbar_init(&S.p_full[i][1], 8);
+        }
+        for (int i = 0; i < L::RING_SEGS; ++i) mbar_init(&S.tail[i], 32 * TA_COPY_WARPS);
+        mbar_init(&S.cleared, 32 * TA_COPY_WARPS);
         S.abort = S.bad_page = S.bad_tree = 0;
         fence_mbarrier_init();
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (k_tree_join reports; a wait runs out a second later)
     }
-    const int count = tree_list<D>(a, T);
-    const int workers = workers_of(a, count), me = blockIdx.x;
-    Segment seg;
-    const bool has = me < workers && seg.seek<D>(first_of(me, count, workers), first_of(me + 1, count, workers), a, T);
-    if (!has) {
-        if (threadIdx.x == 0) a.worker_code[me] = DEV_OK;
-        return;
+    if (threadIdx.x == 32 && box) {
+        prefetch_tensormap(&kmap);
+        prefetch_tensormap(&vmap);
     }
-    if (warp == 12) tmem_alloc(&S.tmem, TM_COLS);
     tc_fence_before();
-    __syncthreads();
+    const int count = tree_list<D>(a, T);  // (its barriers order what is above, too)
+    const int workers = workers_of(a, count), me = blockIdx.x;
     tc_fence_after();
     const uint32_t tmem = S.tmem;
-    bool more = true;
+    Segment seg{};
+    bool more = me < workers && seg.seek<D>(first_of(me, count, workers), first_of(me + 1, count, workers), a, T);
+    // rows of the segment's unit from its chunk's first on
+    auto rows_of = [&]() { return T.nodes[seg.b] * a.group - (seg.unit % seg.chunks) * L::ROWS_ALL; };
 
-    // registers: of the launch's 4 x 128 x 128 the rows' warpgroups take 128 x 200 each, the others keep 128 x 56
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-        if (warp < 12) {
-            // ---- copies: K 0, V 0, K 1, V 1, ... of each segment; warp w rows 32 w .. of each block
-            const int w = warp - 8, key0 = 32 * w + lane;
-            ulonglong2 *rows = S.rows[w];
-            constexpr int CPR = L::DU / 8, RPI = 32 / CPR;  // 16-byte pieces of a unit's row, rows of a step
+    if (warp >= ROW_WARPS) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+        if (warp < 16 + TA_COPY_WARPS) {
+            // ---- copies, in the ring's order; warp w rows 64 w .. of each block
+            const int w = warp - 16, t_copy = w * 32 + lane;
+            constexpr int CPR = L::DU / 8, RPI = 32 / CPR, STEPS = TA_COPY_ROWS / RPI;  // 16-byte pieces of a unit's row, rows of a step, steps
             const int piece = lane % CPR, r_lane = lane / CPR;
             // where piece `piece` of the warp's row r lies in a unit
-            auto place = [&](int r) { return (uint32_t)((piece >> 3) * SUB + (32 * w + r) * 128 + (((piece & 7) ^ (r & 7)) << 4)); };
-            auto entry = [&](const Segment &g, int t) {
-                const int key = t * KEYS + key0;
+            auto place = [&](int r) { return (uint32_t)((piece >> 3) * SUB + (TA_COPY_ROWS * w + r) * 128 + (((piece & 7) ^ (r & 7)) << 4)); };
+            auto entry = [&](const Segment &g, int t, int e) {
+                const int key = t * KEYS + TA_COPY_ROWS * w + 32 * e + lane;
                 return key < T.len[g.b] + T.nodes[g.b] ? a.kv.table[(long long)g.b * a.kv.max_pages + page_index(a.kv, key)] : 0;
             };
             int issued = 0, block = 0, sn = 0, clears = 0;
             bool ok = true;
-            int page = entry(seg, seg.t);
+            int page[2] = {0, 0}, pend_unit = -1, pend_t = 0, pend_kv = 0, pend_u = 0;  // what the last copy of rows has still to be looked at
+            if (more)
+                for (int e = 0; e < 2; ++e) page[e] = entry(seg, seg.t, e);
             for (; ok && more; ++sn) {
-                const int b = seg.b, len = T.len[b], nodes = T.nodes[b], h = seg.unit / seg.chunks;
-                const bool store = seg.unit % seg.chunks == 0;
-                const int tail0 = len / KEYS;  // the first block with nodes or places behind them
+                const int b = seg.b, len = T.len[b], nodes = T.nodes[b], h = seg.unit / seg.chunks, start = a.starts[b];
+                const bool store = seg.unit % seg.chunks == 0, two = TILES == 2 && rows_of() > ROWS;
+                const int tail0 = len / KEYS, nb = seg.t_end - seg.t;  // (the first block with nodes or places behind them)
                 const int si = sn % L::RING_SEGS;
                 Segment nxt = seg;
                 const bool nxt_more = nxt.next<D>(a, T);
-                for (int t = seg.t; ok && t < seg.t_end; ++t, ++block) {
-                    const int key = t * KEYS + key0;
-                    const bool cached = key < len, node = !cached && key < len + nodes;
-                    const bool real = (cached || node) && (unsigned)page < (unsigned)a.kv.n_pages;
-                    const int pi = page_index(a.kv, key);
-                    const long long off = real ? page * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot : -1;
-                    if ((cached || node) && !real) *(volatile int *)&S.bad_page = 1;
-                    ulonglong2 at = make_ulonglong2(0, 0);
-                    if (real) {
-                        const long long src = cached ? off : (long long)(T.start[b] + key - len) * a.kv_stride + h * D;
-                        at.x = reinterpret_cast<unsigned long long>((cached ? a.kv.k : a.k) + src);
-                        at.y = reinterpret_cast<unsigned long long>((cached ? a.kv.v : a.v) + src);
-                    }
-                    const unsigned valid = __ballot_sync(0xffffffffu, real);
-                    __syncwarp();
-                    rows[lane] = at;
-                    if (lane == 0) *(volatile uint32_t *)&S.valid[block % TA_MASKS][w] = valid;
-                    if (node && store && a.new_pos && a.kv.positions && real)
-                        a.kv.positions[((long long)b * a.hkv + h) * a.kv.cap + key] = a.new_pos[T.start[b] + key - len];
-                    __syncwarp();
-                    // the next block's pages are asked for now
-                    const bool last = t + 1 == seg.t_end;
-                    const int next_page = !last ? entry(seg, t + 1) : nxt_more ? entry(nxt, nxt.t) : 0;
-                    const bool tail = t >= tail0;
-                    if (tail && t == max(seg.t, tail0)) {  // nobody looks at this segment's notes yet
-                        for (int d = threadIdx.x - 256; d < D; d += 128) S.odd_nodes[si][d] = 0, S.odd_all[si][d] = 0;
-                        if (threadIdx.x == 256) S.odd[si] = 0;
-                        mbarrier_arrive_one(&S.cleared);
-                        ok = mbar_wait(&S.cleared, clears++ & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-                        ok = __all_sync(0xffffffffu, ok);
-                    }
-                    for (int kv = 0; ok && kv < 2; ++kv)
-                        for (int u = 0; u < UNITS; ++u) {
-                            const int slot = issued % STAGES;
-                            ok = mbar_wait(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort);
-                            if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                            ++issued;
-                            const uint32_t to = smem_u32(ring + slot * L::UNIT);
-#pragma unroll 8
-                            for (int x = 0; x < 32; x += RPI) {
-                                const int r = x + r_lane;
-                                const unsigned long long *p = &rows[r].x + kv;
-                                const uint16_t *src = reinterpret_cast<const uint16_t *>(*p);
-                                cp_async16_or_zero(to + place(r), src ? src + u * L::DU + piece * 8 : a.q, src != nullptr);
-                            }
-                            if (!tail) {
-                                cp_async_arrive(&S.full[slot]);
-                                continue;
-                            }
-                            cp_async_commit();
-                            cp_async_wait_all();
-#pragma unroll 4
-                            for (int x = 0; x < 32; x += RPI) {  // (each lane its own pieces)
-                                const int r = x + r_lane, k = t * KEYS + 32 * w + r, i = k - len;
-                                if (!(valid >> r & 1)) continue;
-                                const uint4 v = ld_shared_u4(to + place(r));
-                                const int d0 = u * L::DU + piece * 8;
-                                if (store && i >= 0) {
-                                    const int pg = a.kv.table[(long long)b * a.kv.max_pages + page_index(a.kv, k)];
-                                    const long long dst = pg * a.kv.stride_page + h * a.kv.stride_head +
-                                                          (k - page_index(a.kv, k) * a.kv.page_size) * a.kv.stride_slot + d0;
-                                    *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(kv ? a.kv.v : a.kv.k) + dst) = v;
-                                }
-                                uint32_t wd[4] = {v.x, v.y, v.z, v.w};
-                                if (kv == 0 || !(odd_halves<FP16>(wd[0]) | odd_halves<FP16>(wd[1]) | odd_halves<FP16>(wd[2]) | odd_halves<FP16>(wd[3])))
-                                    continue;
+                // Rows of the last block with nodes that were copied: K's go to the cache, V's too and are looked at.
+                auto finish = [&]() {
+                    const uint32_t to = smem_u32(ring + pend_unit * L::UNIT);
+                    const uint32_t *valid = S.valid[(block + pend_t - seg.t) % TA_MASKS] + 2 * w;
+                    const int k0 = pend_t * KEYS + TA_COPY_ROWS * w, d0 = pend_u * L::DU + piece * 8;
+#pragma unroll 1
+                    for (int x0 = 0; x0 < STEPS; x0 += 4) {
+                        uint4 v[4];
+                        uint32_t any = 0;
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    const uint32_t half = 0xffffu << (16 * (e & 1));
-                                    if (!(odd_halves<FP16>(wd[e >> 1]) & half)) continue;
-                                    wd[e >> 1] &= ~half;
-                                    if (i < 0)
-                                        S.odd_all[si][d0 + e] = 1;
-                                    else
-                                        atomicOr(&S.odd_nodes[si][d0 + e], 1ull << i);
-                                }
-                                st_shared_u4(to + place(r), make_uint4(wd[0], wd[1], wd[2], wd[3]));
-                                S.odd[si] = 1;
-                            }
-                            fence_proxy_async_shared();
-                            mbarrier_arrive_one(&S.full[slot]);
+                        for (int y = 0; y < 4; ++y) {
+                            v[y] = ld_shared_u4(to + place((x0 + y) * RPI + r_lane));
+                            any |= odd_halves<FP16>(v[y].x) | odd_halves<FP16>(v[y].y) | odd_halves<FP16>(v[y].z) | odd_halves<FP16>(v[y].w);
                         }
-                    page = next_page;
+                        if (store && k0 + (x0 + 4) * RPI > len) {
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const int r = (x0 + y) * RPI + r_lane, key = k0 + r;
+                                if (key < len || !(valid[r >> 5] >> (r & 31) & 1)) continue;
+                                const int pi = page_index(a.kv, key);
+                                const long long dst = a.kv.table[(long long)b * a.kv.max_pages + pi] * a.kv.stride_page + h * a.kv.stride_head +
+                                                      (key - pi * a.kv.page_size) * a.kv.stride_slot + d0;
+                                *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(pend_kv ? a.kv.v : a.kv.k) + dst) = v[y];
+                            }
+                        }
+                        if (any == 0 || pend_kv == 0) continue;
+#pragma unroll 1
+                        for (int e = 0; e < 32; ++e) {  // (value by value: this is rare)
+                            const int r = (x0 + (e >> 3)) * RPI + r_lane, i = k0 + r - len;
+                            const uint32_t at = to + place(r) + 2 * (e & 7);
+                            uint16_t y;
+                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at) : "memory");
+                            if (!odd_halves<FP16>(y)) continue;
+                            asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((uint16_t)0) : "memory");
+                            if (i < 0)
+                                S.odd_all[si][d0 + (e & 7)] = 1;
+                            else
+                                atomicOr(&S.odd_nodes[si][d0 + (e & 7)], 1ull << i);
+                            S.odd[si] = 1;
+                        }
+                    }
+                    fence_proxy_async_shared();
+                    mbarrier_arrive_one(&S.full[pend_unit]);
+                    pend_unit = -1;
+                };
+                for (int n = 0; ok && n < 2 * nb; ++n) {
+                    const int x = at_place(n, nb, two), kv = x < 0, t = seg.t + (kv ? ~x : x);
+                    const bool tail = t >= tail0;
+                    if (!kv) {  // the block's rows
+                        const int key0 = t * KEYS + TA_COPY_ROWS * w + lane;
+                        __syncwarp();
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int key = key0 + 32 * e;
+                            const bool cached = key < len, node = !cached && key < len + nodes;
+                            const bool real = (cached || node) && (unsigned)page[e] < (unsigned)a.kv.n_pages;
+                            const int pi = page_index(a.kv, key);
+                            if ((cached || node) && !real) *(volatile int *)&S.bad_page = 1;
+                            ulonglong2 at = make_ulonglong2(0, 0);
+                            if (real && box && !tail) {
+                                at.x = (unsigned)page[e] + 1ull;
+                            } else if (real) {
+                                const long long src = cached ? page[e] * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot
+                                                             : (long long)(start + key - len) * a.kv_stride + h * D;
+                                at.x = reinterpret_cast<unsigned long long>((cached ? a.kv.k : a.k) + src);
+                                at.y = reinterpret_cast<unsigned long long>((cached ? a.kv.v : a.v) + src);
+                            }
+                            const unsigned valid = __ballot_sync(0xffffffffu, real);
+                            S.rows[w][t & 1][32 * e + lane] = at;
+                            if (lane == 0) *(volatile uint32_t *)&S.valid[(block + t - seg.t) % TA_MASKS][2 * w + e] = valid;
+                            if (node && store && a.new_pos && a.kv.positions && real)
+                                a.kv.positions[((long long)b * a.hkv + h) * a.kv.cap + key] = a.new_pos[start + key - len];
+                            // the next block's pages are asked for now
+                            page[e] = t + 1 < seg.t_end ? entry(seg, t + 1, e) : nxt_more ? entry(nxt, nxt.t, e) : 0;
+                        }
+                        __syncwarp();
+                        if (tail && t == max(seg.t, tail0)) {  // nobody looks at this segment's notes yet
+                            for (int d = t_copy; d < D; d += 32 * TA_COPY_WARPS) S.odd_nodes[si][d] = 0, S.odd_all[si][d] = 0;
+                            if (t_copy == 0) S.odd[si] = 0;
+                            mbarrier_arrive_one(&S.cleared);
+                            ok = mbar_wait_short(&S.cleared, clears++ & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+                            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                        }
+                    }
+                    const ulonglong2 *rows = S.rows[w][t & 1];
+                    for (int u = 0; ok && u < UNITS; ++u) {
+                        const int slot = issued % STAGES;
+                        ok = mbar_wait_short(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort);
+                        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                        ++issued;
+                        uint64_t *bar = &S.full[slot];
+                        uint8_t *unit = ring + slot * L::UNIT;
+                        if (box && !tail) {  // a lane a piece of a page
+                            const int pieces = TA_COPY_ROWS / box, r = lane * box;
+                            const bool mine = lane < pieces;
+                            const int pg = mine ? (int)rows[mine ? r : 0].x - 1 : -1;
+                            const int there = __popc(__ballot_sync(0xffffffffu, pg >= 0));
+                            if (lane == 0) mbar_expect_tx(bar, (uint32_t)(there * box * L::DU * 2));
+                            __syncwarp();
+                            const int key = t * KEYS + TA_COPY_ROWS * w + r;
+                            if (pg >= 0) {
+                                for (int c = 0; c < L::DU / 64; ++c)
+                                    tma_load_4d(unit + c * SUB + (TA_COPY_ROWS * w + r) * 128, kv ? &vmap : &kmap, u * L::DU + c * 64,
+                                                key - page_index(a.kv, key) * a.kv.page_size, h, pg, bar);
+                            } else if (mine) {  // (slots of a page outside the cache: zeros, which no weight makes NaN)
+                                for (int i = 0; i < box * L::DU / 8; ++i)
+                                    st_shared_u4(smem_u32(unit) + (i / (8 * box)) * SUB + (TA_COPY_ROWS * w + r + (i / 8) % box) * 128 + (i & 7) * 16,
+                                                 make_uint4(0, 0, 0, 0));
+                                fence_proxy_async_shared();
+                            }
+                            __syncwarp();
+                            mbarrier_arrive_one(bar);
+                        } else {
+                            const uint32_t to = smem_u32(unit);
+#pragma unroll 1
+                            for (int x0 = 0; x0 < STEPS; x0 += 8) {
+                                unsigned long long src[8];
+#pragma unroll
+                                for (int y = 0; y < 8; ++y) src[y] = (&rows[(x0 + y) * RPI + r_lane].x)[kv];
+#pragma unroll
+                                for (int y = 0; y < 8; ++y)
+                                    cp_async16_or_zero(to + place((x0 + y) * RPI + r_lane),
+                                                       src[y] ? reinterpret_cast<const uint16_t *>(src[y]) + u * L::DU + piece * 8 : a.q, src[y] != 0);
+                            }
+                            if (!tail) cp_async_arrive(bar);
+                        }
+                        if (tail) cp_async_commit();
+                        if (pend_unit >= 0) {
+                            if (tail)
+                                cp_async_wait_1();
+                            else
+                                cp_async_wait_all();
+                            finish();
+                        }
+                        if (tail) pend_unit = slot, pend_t = t, pend_kv = kv, pend_u = u;
+                    }
                 }
+                cp_async_wait_all();
+                if (ok && pend_unit >= 0) finish();
                 if (ok && seg.t_end > tail0) mbarrier_arrive_one(&S.tail[si]);  // (only a stretch's last segment has no such block)
+                block += nb;
                 seg = nxt;
                 more = nxt_more;
             }
             cp_async_commit();
             cp_async_wait_all();  // also on the error path: nothing is in flight when the CTA ends
-        } else if (warp == 12 && elect_one()) {
-            // ---- MMAs: for every block, tile after tile, O += P V of the block before, then S
-            int pos = 0, used_p[2] = {0, 0}, used[2] = {0, 0};  // ring units; blocks and segments of a tile so far
+            if (*(volatile int *)&S.abort) {  // (and tiled copies get a bounded chance to land)
+                const uint64_t t0 = globaltimer_ns();
+                while (globaltimer_ns() - t0 < WAIT_LIMIT_NS / 100) __nanosleep(1000);
+            }
+        } else if (warp < 18 + TILES && elect_one()) {
+            // ---- MMAs of tile i
+            const int i = warp - 18;
+            const uint8_t *q = sq + i * L::QT;
+            const uint32_t o = tmem + TM_O + i * D;
+            int pos = 0, step = 0, used_o = 0, cnt0 = 0, cnt1 = 0, cnt2 = 0, twos = 0;  // blocks' K and V, sections, segments of the tile, phases of s_full, segments of two tiles
             bool ok = true;
-            auto landed = [&](int at) { ok = ok && mbar_wait(&S.full[at % STAGES], (at / STAGES) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort); };
+            auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.abort); };
+            auto landed = [&](int place) {
+                for (int u = 0; u < UNITS; ++u) wait(&S.full[(place * UNITS + u) % STAGES], (place * UNITS + u) / STAGES, DEV_TIMEOUT_LOAD);
+                if (!box) fence_proxy_async_shared();  // (cp.async's copies land in the generic proxy)
+            };
+            auto unit = [&](int place, int u) { return ring + ((place * UNITS + u) % STAGES) * L::UNIT; };
+            auto scores = [&](int buf, int bar, int place) {
+                for (int u = 0; u < UNITS; ++u) mma_scores<D, FP16>(tmem + buf * KEYS, q, unit(place, u), u);
+                mma_commit(&S.s_full[bar]);
+            };
             while (ok && more) {
-                const int nb = seg.t_end - seg.t, all = T.len[seg.b] + T.nodes[seg.b];
-                const int n_rows = T.nodes[seg.b] * a.group - (seg.unit % seg.chunks) * L::ROWS_ALL;
-                const int tiles = TILES == 2 && n_rows > ROWS ? 2 : 1;
-                for (int j = 0; ok && j <= nb; ++j) {
-                    const int vp = pos, kp = pos + (j ? UNITS : 0);
-                    if (j) pos += UNITS;
-                    if (j < nb) pos += UNITS;
-                    for (int i = 0; ok && i < tiles; ++i) {
-                        if (j > 0) {
-                            ok = mbar_wait(&S.p_full[i], used_p[i] & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-                            ++used_p[i];
-                            if (j == 1 && used[i] > 0) ok = ok && mbar_wait(&S.o_free[i], (used[i] - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-                            const int steps = min(KEYS, all - (seg.t + j - 1) * KEYS + 15) / 16;
-                            for (int u = 0; ok && u < UNITS; ++u) {
-                                landed(vp + u);
-                                if (!ok) break;
-                                fence_proxy_async_shared();  // (copies by cp.async land in the generic proxy)
-                                tc_fence_after();
-                                mma_values<D, FP16>(tmem + TM_O + i * D, tmem + i * KEYS, ring + ((vp + u) % STAGES) * L::UNIT, u, steps, j == 1);
-                            }
-                            if (ok && j == nb) mma_commit(&S.o_full[i]);
-                        }
-                        if (ok && j > 0 && i == tiles - 1)
-                            for (int u = 0; u < UNITS; ++u) mma_commit(&S.empty[(vp + u) % STAGES]);
-                        if (ok && j < nb) {
-                            if (j == 0) ok = mbar_wait(&S.q_full[i], used[i] & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-                            for (int u = 0; ok && u < UNITS; ++u) {
-                                landed(kp + u);
-                                if (!ok) break;
-                                fence_proxy_async_shared();
-                                tc_fence_after();
-                                mma_scores<D, FP16>(tmem + i * KEYS, sq + i * L::QT, ring + ((kp + u) % STAGES) * L::UNIT, u);
-                            }
-                            if (ok) mma_commit(&S.s_full[i]);
-                        }
+                const int nb = seg.t_end - seg.t, keys = T.len[seg.b] + T.nodes[seg.b] - seg.t * KEYS;
+                const bool two = TILES == 2 && rows_of() > ROWS;
+                auto values = [&](int buf, int bar, int j, int place, int phase) {
+                    const int steps = min(KEYS, keys - j * KEYS + 15) / 16;  // (keys behind the last are not multiplied, to 16)
+                    for (int u = 0; u < UNITS; ++u) mma_values<D, FP16>(o, tmem + buf * KEYS, unit(place, u), u, 0, steps, j == 0);
+                    wait(&S.p_full[bar][1], phase, DEV_TIMEOUT_MMA);
+                    if (!ok) return;
+                    tc_fence_after();
+                    for (int u = 0; u < UNITS; ++u) mma_values<D, FP16>(o, tmem + buf * KEYS, unit(place, u), u, 1, steps, j == 0);
+                };
+                auto values_ready = [&](int j, int place) {
+                    landed(place);
+                    if (j == 0 && used_o > 0) wait(&S.o_free[i], used_o - 1, DEV_TIMEOUT_MMA);
+                };
+                if (two) {  // for every block O += P V of the one before, then S; the tiles in turns
+                    const int cnt = i ? cnt1 : cnt0;
+                    wait(&S.q_full[i], used_o, DEV_TIMEOUT_LOAD);
+#pragma unroll 1
+                    for (int j = 0; ok && j <= nb; ++j, ++step) {
+                        const int vp = pos + v_place(j - 1, nb, true), kp = pos + k_place(j, true);
+                        if (i + step > 0) wait(&S.turn[i], step + i - 1, DEV_TIMEOUT_MMA);
+                        if (j > 0) values_ready(j - 1, vp);
+                        if (j < nb) landed(kp);
+                        if (j > 0) wait(&S.p_full[i][0], cnt + j - 1, DEV_TIMEOUT_MMA);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (j > 0) values(i, i, j - 1, vp, cnt + j - 1);
+                        if (ok && j < nb) scores(i, i, kp);
+                        mbarrier_arrive_one(&S.turn[i ^ 1]);
+                        if (j == nb) mma_commit(&S.o_done[i]);
                     }
-                    if (ok && j < nb)
-                        for (int u = 0; u < UNITS; ++u) mma_commit(&S.empty[(kp + u) % STAGES]);
+                    cnt0 += nb, cnt1 += nb;
+                    ++used_o, ++twos;
+                } else {  // S of the next block, then O += P V of this one
+                    if (i == 0) {
+                        wait(&S.q_full[0], used_o, DEV_TIMEOUT_LOAD);
+                        landed(pos);
+                        if (ok) {
+                            tc_fence_after();
+                            scores(0, 0, pos);
+                        }
+                        if (twos > 0) wait(&S.o_done[1], twos - 1, DEV_TIMEOUT_MMA);  // (the second tile has left the second place)
+#pragma unroll 1
+                        for (int j = 0; ok && j < nb; ++j) {
+                            const int vp = pos + v_place(j, nb, false), kp = pos + k_place(j + 1, false), buf = j & 1;
+                            if (j + 1 < nb) {
+                                landed(kp);
+                                if (!ok) break;
+                                tc_fence_after();
+                                scores(buf ^ 1, buf ? 0 : 2, kp);
+                            }
+                            const int phase = (buf ? cnt2 : cnt0) + (j >> 1), bar = 2 * buf;
+                            values_ready(j, vp);
+                            wait(&S.p_full[bar][0], phase, DEV_TIMEOUT_MMA);
+                            if (!ok) break;
+                            tc_fence_after();
+                            values(buf, bar, j, vp, phase);
+                            mma_commit(&S.o_done[0]);
+                        }
+                        ++used_o;
+                    }
+                    cnt0 += (nb + 1) / 2, cnt2 += nb / 2;
                 }
-                for (int i = 0; i < tiles; ++i) ++used[i];
+                pos += 2 * nb;
                 more = seg.next<D>(a, T);
             }
-            mma_commit(&S.drain);  // also on the error path: every MMA issued completes before TMEM is released
-            mbar_wait(&S.drain, 0, nullptr, 0, nullptr);
+            mma_commit(&S.drain[i]);  // every MMA issued completes before TMEM is released
+            mbar_wait_short(&S.drain[i], 0, nullptr, 0, nullptr);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
-        // ---- rows: thread r of tile i the row r of the unit's 128 i ..: node row / group, head row % group
-        const int i = warp >> 2, w = warp & 3;
-        const uint32_t lanes = (uint32_t)(w * 32) << 16, ts = tmem + lanes + i * KEYS, to = tmem + lanes + TM_O + i * D;
-        const uint32_t mine = smem_u32(sq + i * L::QT);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(ROW_REGS));
+        // ---- rows: row r of tile i is the unit's row 128 i + r: node row / group, head row % group
+        const int i = warp >> 3, half = (warp >> 2) & 1, w = warp & 3, id = 1 + i * 4 + w, place_row = i * ROWS + w * 32 + lane;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16, ts = tmem + lanes + 64 * half, to = tmem + lanes + TM_O + i * D + half * (D / 2);
         const float c = a.scale * 1.4426950408889634f;
-        constexpr int CPR = D / 8, RPI = 32 / CPR;
-        const int piece = lane % CPR;
-        // where piece `piece` of the warp's row r lies in the tile
-        auto place = [&](int r, int p) { return mine + (uint32_t)((p >> 3) * SUB + (w * 32 + r) * 128 + (((p & 7) ^ (r & 7)) << 4)); };
-        int used = 0, used_s = 0, block = 0, sn = 0;  // segments and blocks of the tile; blocks and segments of the CTA
+        float *top = S.top[i][0];
+        Row r{0.f, 0.f};
+        int o_phase = 0, cnt = 0, cnt2 = 0, block = 0, pos = 0, sn = 0;  // phases of o_done, of the tile's s_full, of the second place's; blocks, K and V, segments
         bool ok = true;
         for (; ok && more; ++sn, more = seg.next<D>(a, T)) {
-            const int b = seg.b, nb = seg.t_end - seg.t, len = T.len[b], nodes = T.nodes[b], h = seg.unit / seg.chunks;
-            const int row = (seg.unit % seg.chunks) * L::ROWS_ALL + i * ROWS + w * 32 + lane, n_rows = nodes * a.group;
-            const bool whole = nb == seg.blocks, ends = seg.t_end > len / KEYS;  // (with nodes, or places behind them, among its keys)
-            const int part = seg.t == 0;  // of units a stretch has at most two parts: an end and a beginning
-            if (i >= TILES || i * ROWS + (seg.unit % seg.chunks) * L::ROWS_ALL >= n_rows) {  // (uniform over the tile)
-                block += nb;
-                continue;
-            }
-            const bool real = row < n_rows;
-            const int node = real ? row / a.group : 0, head = h * a.group + (real ? row - node * a.group : 0);
-            const long long q_off = real ? (long long)(T.start[b] + node) * a.q_stride + head * D : -1;
-            // the queries (the tile's last MMAs are done, and its outputs have left)
+            const int b = seg.b, nb = seg.t_end - seg.t, len = T.len[b], n_rows = rows_of();
+            const bool two = TILES == 2 && n_rows > ROWS, whole = nb == seg.blocks, ends = seg.t_end > len / KEYS;  // (ends: nodes among its keys)
+            const int pos0 = pos;
+            pos += 2 * nb, block += nb;
+            if (i && !two) continue;  // (nothing for the second tile)
+            auto release = [&](int place) {  // K or V of a block is not needed any more
+                if (w == 0 && half == 0 && lane == 0)
+                    for (int u = 0; u < UNITS; ++u) mbarrier_arrive_many(&S.empty[((pos0 + place) * UNITS + u) % STAGES], two ? 1 : 2);
+            };
+            const bool real = place_row < n_rows;
+            const int row = place_row + (seg.unit % seg.chunks) * L::ROWS_ALL, node = real ? row / a.group : 0;
+            const int head = (seg.unit / seg.chunks) * a.group + (real ? row - node * a.group : 0);
+            {  // the queries (the tile's last MMAs are done); a row's two warps share its pieces
+                constexpr int CPH = D / 16, RPI = 32 / CPH;
+                const int piece = half * CPH + lane % CPH;
+                const uint32_t mine = smem_u32(sq + i * L::QT) + (piece >> 3) * SUB + w * 32 * 128;
+                const long long q_off = real ? (long long)(a.starts[b] + node) * a.q_stride + head * D : -1;
 #pragma unroll 4
-            for (int x = 0; x < 32; x += RPI) {
-                const int r = x + lane / CPR;
-                const long long o = __shfl_sync(0xffffffffu, q_off, r);
-                cp_async16_or_zero(place(r, piece), o >= 0 ? a.q + o + piece * 8 : a.q, o >= 0);
+                for (int x = 0; x < 32; x += RPI) {
+                    const int rr = x + lane / CPH;
+                    const long long off = __shfl_sync(0xffffffffu, q_off, rr);
+                    cp_async16_or_zero(mine + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), off >= 0 ? a.q + off + piece * 8 : a.q, off >= 0);
+                }
+                cp_async_commit();
             }
-            cp_async_commit();
             // ancestors: lane x holds nodes x and x + 32
             uint64_t anc = 0;
             if (ends) {
@@ -421,13 +533,14 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_tree(const __grid_constant__ 
                 for (int e = 0; e < 2; ++e) {
                     const int x = lane + 32 * e;
                     p[e] = -1;
-                    if (x < nodes) {
-                        p[e] = a.parents ? a.parents[T.start[b] + x] : x - 1;
+                    if (x < T.nodes[b]) {
+                        p[e] = a.parents ? a.parents[a.starts[b] + x] : x - 1;
                         if (p[e] < -1 || p[e] >= x) bad = true, p[e] = -1;
                     }
                     m[e] = 1ull << x;
                 }
                 if (__any_sync(0xffffffffu, bad) && lane == 0) *(volatile int *)&S.bad_tree = 1;
+#pragma unroll 1
                 for (int step = 0; step < 6; ++step) {  // whole paths twice as long each time
                     uint64_t up[2];
                     int pp[2];
@@ -448,102 +561,109 @@ __global__ void __launch_bounds__(TA_THREADS, 1) k_tree(const __grid_constant__ 
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbarrier_arrive_one(&S.q_full[i]);
-            Row r;
-            for (int j = 0; j < nb; ++j, ++block, ++used_s) {
-                ok = mbar_wait(&S.s_full[i], used_s & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            for (int j = 0; ok && j < nb; ++j) {
+                const int buf = two ? i : j & 1, bar = two ? i : 2 * buf, phase = two ? cnt + j : (buf ? cnt2 : cnt) + (j >> 1);
+                bool there = mbar_wait_short(&S.s_full[bar], phase & 1, a.status, DEV_TIMEOUT_MMA, &S.abort), o_waited = two || j == 0;
+                there = __all_sync(0xffffffffu, there);
+                release(k_place(j, two));
+                if (two && j > 0) release(v_place(j - 1, nb, true));
                 tc_fence_after();
-                uint32_t s[KEYS];
+                uint32_t s[64];
 #pragma unroll
-                for (int x = 0; x < KEYS; x += 32) tmem_ld_32cols(ts + x, *reinterpret_cast<uint32_t(*)[32]>(&s[x]));
+                for (int x = 0; x < 64; x += 32) tmem_ld_32cols(ts + buf * KEYS + x, *reinterpret_cast<uint32_t(*)[32]>(&s[x]));
                 tmem_ld_wait();
-                const int k0 = (seg.t + j) * KEYS;
+                const int k0 = (seg.t + j) * KEYS + 64 * half;
                 const bool bad = *(volatile int *)&S.bad_page != 0;
-                if (bad || k0 + KEYS > len) {
+                if (bad || k0 + 64 > len) {
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
+                    for (int x = 0; x < 2; ++x) {
                         const int from = k0 + 32 * x - len;  // of the word's first key: its node
                         uint32_t see = from >= 0 ? (from < 64 ? (uint32_t)(anc >> from) : 0u)
                                                  : from <= -32 ? 0xffffffffu : (uint32_t)(anc << -from) | ((1u << -from) - 1);
-                        if (bad) see &= *(volatile uint32_t *)&S.valid[block % TA_MASKS][x];
+                        if (bad) see &= *(volatile uint32_t *)&S.valid[(block - nb + j) % TA_MASKS][2 * half + x];
 #pragma unroll
                         for (int y = 0; y < 32; ++y)
                             if (!(see >> y & 1)) s[32 * x + y] = __float_as_uint(-INFINITY);
                     }
                 }
-                softmax_block<D, FP16>(r, s, c, j == 0, ts, to);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbarrier_arrive_one(&S.p_full[i]);
-            }
-            const int si = sn % L::RING_SEGS;
-            if (ok) ok = mbar_wait(&S.o_full[i], used & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-            if (ok && ends) ok = mbar_wait(&S.tail[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-            if (!(ok = __all_sync(0xffffffffu, ok))) break;
-            tc_fence_after();
-            ++used;
-            const bool odd = ends && *(volatile int *)&S.odd[si];
-            const float f = whole ? row_factor(r) : 1.f;
-            const int place_row = i * ROWS + w * 32 + lane;
-            float *po = a.part_o + (((long long)me * 2 + part) * a.part_rows + place_row) * D;
-#pragma unroll 1
-            for (int x = 0; x < D; x += 32) {
-                uint32_t o[32];
-                tmem_ld_32cols(to + x, o);
-                tmem_ld_wait();
-                if (odd)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (S.odd_all[si][x + e] || (S.odd_nodes[si][x + e] & anc)) o[e] = 0x7fffffffu;
-                if (whole) {  // through the queries' place, so that neighbouring lanes store a row's pieces
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) v[y] = pack16<FP16>(__uint_as_float(o[e + 2 * y]) * f, __uint_as_float(o[e + 2 * y + 1]) * f);
-                        st_shared_u4(place(lane, (x + e) >> 3), make_uint4(v[0], v[1], v[2], v[3]));
+                auto o_ready = [&]() {  // (with two tiles S of this block has come after O of the one before)
+                    bool o = true;
+                    if (!o_waited) {
+                        o = mbar_wait_short(&S.o_done[0], (o_phase + j - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+                        release(v_place(j - 1, nb, false));
                     }
-                } else if (real) {
+                    o_waited = true;
+                    return __all_sync(0xffffffffu, o) != 0;
+                };
+                ok = softmax_half<D, FP16>(r, s, there, c, j == 0, ts + buf * KEYS, to, id, top, half, w * 32 + lane, o_ready, [&](int part) {
+                    if (!two && part == 1) o_ready();  // (every phase is waited for)
+                    if (lane == 0) mbarrier_arrive_one(&S.p_full[bar][part]);
+                });
+            }
+            cnt += two ? nb : (nb + 1) / 2;
+            if (!two) cnt2 += nb / 2;
+            const int si = sn % L::RING_SEGS;
+            o_phase += two ? 1 : nb;
+            bool there = mbar_wait_short(&S.o_done[i], (o_phase - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+            if (there && ends) there = mbar_wait_short(&S.tail[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+            release(v_place(nb - 1, nb, two));
+            if (!ok || pair_any(id, !there)) break;
+            top[half * ROWS + w * 32 + lane] = r.l;
+            pair_sync(id);
+            r.l += top[(half ^ 1) * ROWS + w * 32 + lane];
+            tc_fence_after();
+            const bool odd = ends && *(volatile int *)&S.odd[si];
+            auto drop = [&](int d) { return S.odd_all[si][half * (D / 2) + d] != 0 || (S.odd_nodes[si][half * (D / 2) + d] & anc) != 0; };
+            const long long out_row = (long long)(a.starts[b] + node) * a.hq + head;
+            if (whole) {
+                store_half<D, FP16>(to, row_factor(r), a.out + out_row * D + half * (D / 2), real, (reinterpret_cast<uintptr_t>(a.out) & 31) == 0, odd, drop);
+                if (a.lse && half == 0 && real) a.lse[out_row] = row_lse<FP16>(r, a.scale);
+            } else {  // a row's four values beside those of its neighbours
+                const long long part = (long long)me * 2 + (seg.t == 0);  // of units a stretch has at most two parts: an end and a beginning
+                float4 *po = reinterpret_cast<float4 *>(a.part_o) + (part * (D / 4) + half * (D / 8)) * a.part_rows + place_row;
+#pragma unroll 1
+                for (int x = 0; x < D / 2; x += 32) {
+                    uint32_t v[32];
+                    tmem_ld_32cols(to + x, v);
+                    tmem_ld_wait();
+                    if (odd)
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        *reinterpret_cast<uint4 *>(po + x + e) = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        for (int e = 0; e < 32; ++e)
+                            if (drop(x + e)) v[e] = 0x7fffffffu;
+                    if (real)
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            po[(long long)((x + e) / 4) * a.part_rows] =
+                                make_float4(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
                 }
+                if (real && half == 0) a.part_ml[part * a.part_rows + place_row] = make_float2(r.m, r.l);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbarrier_arrive_one(&S.o_free[i]);
-            const long long out_row = real ? (long long)(T.start[b] + node) * a.hq + head : -1;
-            if (!whole) {
-                if (real) a.part_ml[((long long)me * 2 + part) * a.part_rows + place_row] = make_float2(r.m, r.l);
-                continue;
-            }
-            if (a.lse && real) a.lse[out_row] = row_lse<FP16>(r, a.scale);
-#pragma unroll 4
-            for (int x = 0; x < 32; x += RPI) {
-                const int rr = x + lane / CPR;
-                const long long o = __shfl_sync(0xffffffffu, out_row, rr);
-                const uint4 v = ld_shared_u4(place(rr, piece));
-                if (o >= 0) *reinterpret_cast<uint4 *>(a.out + o * D + piece * 8) = v;
-            }
-            __syncwarp();
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) tmem_dealloc(tmem, TM_COLS);
+    if (warp == 18) tmem_dealloc(tmem, TM_COLS);
     if (threadIdx.x == 0) a.worker_code[me] = S.bad_page ? DEV_BAD_PAGE : S.bad_tree ? DEV_BAD_TREE : DEV_OK;
 }
 
-// Joins the parts of units that several CTAs worked on: a warp a row.  The first CTA reports.
-constexpr int TJ_WARPS = 8;
+// Joins the parts of units that several CTAs worked on: a warp four rows of a unit (node by node, the heads of its group
+// innermost), eight lanes a row.  The first CTA reports.
+constexpr int TJ_WARPS = 8, TJ_ROWS = 4;
 template <int D, bool FP16>
 __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_constant__ PackedArgs a) {
     using L = TreeShape<D>;
-    constexpr int PER = D / 32;
     __shared__ TreeList T;
+    __shared__ int most_nodes;
+    if (threadIdx.x == 0) most_nodes = 0;
     const int count = tree_list<D>(a, T), workers = workers_of(a, count);
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, lr = lane >> 3, ld = lane & 7;
     const float c = a.scale * 1.4426950408889634f;
+    for (int b = threadIdx.x; b < a.B; b += 32 * TJ_WARPS) atomicMax(&most_nodes, T.nodes[b]);
+    __syncthreads();
+    const int per_unit = (most_nodes * a.group + TJ_ROWS - 1) / TJ_ROWS;  // groups of rows of a (sequence, KV head)
     pdl_wait();
     if (blockIdx.x == 0) {
         int code = DEV_OK;
@@ -555,50 +675,64 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
         const int c7 = __syncthreads_or(code == DEV_BAD_PAGE), c9 = __syncthreads_or(code == DEV_BAD_TREE);
         if (threadIdx.x == 0 && (c5 | c7 | c9)) latch_error(a.status, c5 ? DEV_BAD_POSITION : c7 ? DEV_BAD_PAGE : DEV_BAD_TREE);
     }
-    // (packed rows behind the last sequence's may be many)
-    __shared__ int rows_end;
-    if (threadIdx.x == 0) rows_end = 0;
-    __syncthreads();
-    for (int b = threadIdx.x; b < a.B; b += 32 * TJ_WARPS)
-        if (T.nodes[b] > 0) atomicMax(&rows_end, T.start[b] + T.nodes[b]);
-    __syncthreads();
-    for (long long x = (long long)blockIdx.x * TJ_WARPS + (threadIdx.x >> 5); x < (long long)rows_end * a.hq; x += (long long)gridDim.x * TJ_WARPS) {
-        const int t = (int)(x / a.hq), head = (int)(x - (long long)t * a.hq);
-        int b = -1;
-        for (int b0 = 0; b < 0 && b0 < a.B; b0 += 32) {
-            const int y = b0 + lane;
-            const unsigned m = __ballot_sync(0xffffffffu, y < a.B && T.nodes[y] > 0 && T.start[y] <= t && t < T.start[y] + T.nodes[y]);
-            if (m) b = b0 + __ffs(m) - 1;
-        }
-        if (b < 0) continue;
-        const int h = head / a.group, row = (t - T.start[b]) * a.group + head - h * a.group, chunk = row / L::ROWS_ALL, pr = row - chunk * L::ROWS_ALL;
-        const int blocks = blocks_of(T.len[b], T.nodes[b]), per = blocks + TA_ROW;
-        const int at = T.first[b] + (h * chunks_of<D>(T.nodes[b] * a.group) + chunk) * per;
+    const long long all = (long long)a.B * a.hkv * per_unit;
+    for (long long x = (long long)blockIdx.x * TJ_WARPS + (threadIdx.x >> 5); x < all; x += (long long)gridDim.x * TJ_WARPS) {
+        const int bh = (int)(x / per_unit), b = bh / a.hkv, h = bh - b * a.hkv, row = (int)(x - (long long)bh * per_unit) * TJ_ROWS + lr;
+        const int n_rows = T.nodes[b] * a.group;
+        if (row - lr >= n_rows) continue;
+        const int chunk = (row - lr) / L::ROWS_ALL, pr = row - chunk * L::ROWS_ALL;  // (a chunk is a multiple of four rows)
+        const int per = blocks_of(T.len[b], T.nodes[b]) + TA_ROW;
+        const int at = T.first[b] + (h * chunks_of<D>(n_rows) + chunk) * per;
         const int w0 = worker_at(at + TA_ROW, count, workers), w1 = worker_at(at + per - 1, count, workers);
         if (w0 == w1) continue;  // one CTA had all blocks
-        auto part = [&](int w) { return ((long long)w * 2 + (w == w0)) * a.part_rows + pr; };
+        const bool real = row < n_rows;
+        auto part = [&](int w) { return (long long)w * 2 + (w == w0); };
         float m = -INFINITY;
-        for (int w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[part(w)].x);
-        float l = 0.f, o[PER];
-        for (int j = 0; j < PER; ++j) o[j] = 0.f;
-        for (int w = w0; w <= w1; ++w) {
-            const long long p = part(w);
-            const float2 ml = a.part_ml[p];
+        for (int w = w0; real && w <= w1; ++w) m = fmaxf(m, a.part_ml[part(w) * a.part_rows + pr].x);
+        float l = 0.f;
+        float4 o[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int w = w0; real && w <= w1; ++w) {
+            const float2 ml = a.part_ml[part(w) * a.part_rows + pr];
+            const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + part(w) * (D / 4) * a.part_rows + pr;
             const float f = ml.x == m ? 1.f : ex2((ml.x - m) * c);
             l += ml.y * f;
-            for (int j = 0; j < PER; ++j) o[j] += a.part_o[p * D + lane + 32 * j] * f;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                const float4 v = po[(long long)(ld + 8 * j) * a.part_rows];
+                o[j].x += v.x * f, o[j].y += v.y * f, o[j].z += v.z * f, o[j].w += v.w * f;
+            }
         }
+        if (!real) continue;
         const Row r{m, l};
         const float inv = row_factor(r);
-        for (int j = 0; j < PER; ++j) {
-            const float y = o[j] * inv;
-            a.out[((long long)t * a.hq + head) * D + lane + 32 * j] = (uint16_t)pack16<FP16>(y, y);
-        }
-        if (a.lse && lane == 0) a.lse[(long long)t * a.hq + head] = row_lse<FP16>(r, a.scale);
+        const int node = row / a.group;
+        const long long out_row = (long long)(a.starts[b] + node) * a.hq + h * a.group + row - node * a.group;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+            *reinterpret_cast<uint2 *>(a.out + out_row * D + (ld + 8 * j) * 4) =
+                make_uint2(pack16<FP16>(o[j].x * inv, o[j].y * inv), pack16<FP16>(o[j].z * inv, o[j].w * inv));
+        if (a.lse && ld == 0) a.lse[out_row] = row_lse<FP16>(r, a.scale);
     }
 }
 
 int rows_all(int d) { return (d == 256 ? 1 : 2) * ROWS; }
+
+// Rows of a page that one tiled copy can bring: a power of two that divides its length, 8 (a swizzle's rows) to 32, and 0 where
+// there is none or a tensor map cannot express the cache.
+int tree_box(const KvView &kv, CUtensorMap *kmap, CUtensorMap *vmap) {
+    int box = 1;
+    while (box < 32 && kv.page_size % (2 * box) == 0) box *= 2;
+    const long long most = 1ll << 38;  // (tensor maps hold strides below 2^40 bytes)
+    if (box < 8 || kv.stride_page >= most || kv.stride_head >= most || kv.stride_slot >= most) return 0;
+    const uint64_t dims[4] = {(uint64_t)kv.d, (uint64_t)kv.page_size, (uint64_t)kv.hkv, (uint64_t)kv.n_pages};
+    auto bytes = [&](long long s) { return (uint64_t)std::max(s, (long long)kv.d) * 2; };  // (one place has any stride)
+    const uint64_t st[3] = {bytes(kv.stride_slot), bytes(kv.stride_head), bytes(kv.stride_page)};
+    const uint32_t bx[4] = {64, (uint32_t)box, 1, 1};
+    return encode_map_16(kmap, kv.k, 4, dims, st, bx) && encode_map_16(vmap, kv.v, 4, dims, st, bx) ? box : 0;
+}
 
 template <int D, bool FP16>
 cudaError_t launch(PackedArgs &a, cudaStream_t st) {
@@ -608,9 +742,13 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     a.workers = std::min(gemm_ctas(), TREE_MAX_WORKERS);
     if (a.workers < 1) return cudaErrorInvalidDevice;
-    k_tree<D, FP16><<<a.workers, TA_THREADS, L::SMEM, st>>>(a);
-    const long long rows = std::min<long long>(a.T, (long long)a.B * TREE_NODES) * a.hq;
-    const int grid = (int)std::min<long long>((rows + TJ_WARPS - 1) / TJ_WARPS, 8ll * gemm_ctas());
+    CUtensorMap kmap{}, vmap{};
+    const int box = tree_box(a.kv, &kmap, &vmap);
+    k_tree<D, FP16><<<a.workers, THREADS, L::SMEM, st>>>(kmap, vmap, a, box);
+    const cudaError_t c = cudaGetLastError();
+    if (c != cudaSuccess) return c;
+    const long long warps = ((long long)std::min<long long>(a.T, (long long)a.B * TREE_NODES) * a.hq + TJ_ROWS - 1) / TJ_ROWS;
+    const int grid = (int)std::min<long long>((warps + TJ_WARPS - 1) / TJ_WARPS, 8ll * gemm_ctas());
     return launch_pdl(k_tree_join<D, FP16>, grid, 32 * TJ_WARPS, 0, st, a);
 }
 

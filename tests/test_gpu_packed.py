@@ -204,6 +204,10 @@ TREES = [
     ([0, 1, 17, 300, 64] * 40, [5, 0, 1, 16, 2] * 40, 1, 2, 64, 16, "heads"),
     ([30000, 10, 500, 0], [4, 64, 1, 2], 2, 7, 64, 5, "tokens"),
     ([127, 128, 129, 63, 64, 191], [1, 1, 64, 65 - 1, 64, 2], 1, 4, 128, 16, "heads"),
+    # units of one and of two tiles of rows in turns, many to a CTA
+    ([300, 20, 0, 700] * 24, [1, 26, 64, 3] * 24, 2, 7, 64, 32, "tokens"),
+    ([130, 0, 500, 40, 260] * 30, [64, 2, 1, 33, 40] * 30, 2, 4, 128, 16, "heads"),
+    ([1000, 90] * 40, [17, 64] * 40, 1, 16, 128, 8, "heads"),
 ]
 
 
