@@ -77,27 +77,38 @@ __host__ __device__ constexpr uint32_t idesc(int N) {
     return FP16 ? idesc_bf16_f32(128, N) & ~((1u << 7) | (1u << 10)) : idesc_bf16_f32(128, N);
 }
 
+// Where the 64-dim halves of a ring unit lie: SUB apart, each with its 128 rows, or beside one another, eight rows at a time (pages'
+// rows come so in half as many copies).
+template <int D, bool BESIDE>
+struct Layout {
+    static constexpr int HALF = BESIDE ? 1024 : SUB;                            // bytes to the next 64 dims
+    static constexpr int EIGHT = BESIDE ? Shape<D>::DU / 64 * 1024 : 1024;      // to the next eight rows
+    // row r, 16-byte piece p of it
+    static __device__ __forceinline__ uint32_t at(int r, int p) { return (uint32_t)((p >> 3) * HALF + (r >> 3) * EIGHT + (r & 7) * 128 + (((p & 7) ^ (r & 7)) << 4)); }
+};
+
 // S of one tile from one ring unit of K (dims u * DU of them); issued by one thread.
-template <int D, bool FP16>
+template <int D, bool FP16, bool BESIDE = false>
 __device__ __forceinline__ void mma_scores(uint32_t s, const uint8_t *q, const uint8_t *k, int u) {
     using L = Shape<D>;
-    const uint64_t qd = sw128_kmajor_desc(q + u * L::UNIT), kd = sw128_kmajor_desc(k);
+    using Y = Layout<D, BESIDE>;
+    const uint64_t qd = sw128_kmajor_desc(q + u * L::UNIT), kd = sw128_desc(k, 16, Y::EIGHT);
 #pragma unroll
-    for (int ks = 0; ks < L::DU / 16; ++ks) {
-        const uint64_t off = (uint64_t)((ks >> 2) * (SUB / 16) + 2 * (ks & 3));
-        mma_bf16_ss(s, qd + off, kd + off, idesc<FP16>(KEYS), (u | ks) != 0);
-    }
+    for (int ks = 0; ks < L::DU / 16; ++ks)
+        mma_bf16_ss(s, qd + (uint64_t)((ks >> 2) * (SUB / 16) + 2 * (ks & 3)), kd + (uint64_t)((ks >> 2) * (Y::HALF / 16) + 2 * (ks & 3)), idesc<FP16>(KEYS),
+                    (u | ks) != 0);
 }
 // O of one tile += P V of one ring unit of V, one part of P (keys 0-31 and 64-95, or 32-63 and 96-127), of the first `steps` 16 keys.
-template <int D, bool FP16>
+template <int D, bool FP16, bool BESIDE = false>
 __device__ __forceinline__ void mma_values(uint32_t o, uint32_t p, const uint8_t *v, int u, int part, int steps, bool first) {
     using L = Shape<D>;
-    const uint64_t vd = sw128_mnmajor_desc(v, SUB);
+    using Y = Layout<D, BESIDE>;
+    const uint64_t vd = sw128_desc(v, Y::HALF, Y::EIGHT);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
         const int ks = (x >> 1) * 4 + part * 2 + (x & 1);
         if (ks < steps)
-            mma_bf16_ts(o + u * L::DU, p + (ks >> 2) * 64 + (ks & 3) * 8, vd + (uint64_t)(ks * (16 * 128 / 16)), idesc<FP16>(L::DU) | IDESC_B_MN,
+            mma_bf16_ts(o + u * L::DU, p + (ks >> 2) * 64 + (ks & 3) * 8, vd + (uint64_t)(ks * (2 * Y::EIGHT / 16)), idesc<FP16>(L::DU) | IDESC_B_MN,
                         !first || part != 0 || x != 0);
     }
 }

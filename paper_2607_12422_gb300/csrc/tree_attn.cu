@@ -10,11 +10,11 @@
 // of about the same cost: how ragged the lengths are does not matter, and the host need not know them.  Where a stretch begins or ends
 // inside a (sequence, KV head) the CTA leaves maximum, sum and unnormalised output in scratch, and k_tree_join joins them.
 //
-// Warps 0-15: rows (queries, softmax, outputs).  Warps 16 and 17 see to K and V: tiled copies of the rows that a page has in a piece where
+// Warps 0-15: rows (queries, softmax, outputs).  Warp 16 copies K, warp 17 V: tiled copies of the rows that a page has in a piece where
 // pages hold a multiple of 8, row by row else, 16 bytes a lane.  Warps 18 and 19: the tiles' MMAs.
 // The blocks with nodes among their keys, a (sequence, KV head)'s last one or two, are copied row by row and waited for by those
 // who copy: they store the nodes' rows into the cache, and look for infinite and NaN values of V, which would be NaN in rows that do not
-// see them (0 x NaN): such values become zero, and who sees them is noted for each dimension.
+// see them (0 x NaN): such values of nodes become zero, and who they were is noted for each dimension.  (Cached rows are seen by all.)
 #include <algorithm>
 
 #include "flash.cuh"
@@ -33,10 +33,10 @@ constexpr int TA_MASKS = 8;      // blocks whose masks are kept
 template <int D>
 struct TreeShape : Shape<D> {
     using S = Shape<D>;
-    static constexpr int STAGES = D == 64 ? 8 : 4;
+    static constexpr int STAGES = D == 64 ? 4 : 2;  // units of the ring of K, and of V's
     static constexpr int RING_SEGS = D == 64 ? 8 : 4;  // segments that copies can be ahead, and one more
     static constexpr int ROWS_ALL = S::TILES * ROWS;
-    static constexpr int SMEM = S::TILES * S::QT + STAGES * S::UNIT + 1024;
+    static constexpr int SMEM = S::TILES * S::QT + 2 * STAGES * S::UNIT + 1024;
 };
 
 // Counts of the list: a (sequence, KV head, chunk of rows) is a unit; it has its blocks and TA_ROW places more in front.
@@ -53,44 +53,65 @@ __device__ __forceinline__ int blocks_of(int len, int nodes) { return (len + nod
 template <int D>
 __device__ __forceinline__ int chunks_of(int rows) { return (rows + TreeShape<D>::ROWS_ALL - 1) / TreeShape<D>::ROWS_ALL; }
 
-// Whole CTA; returns the list's length.
+// Whole CTA; returns the list's length.  (Up to 32 sequences are one warp's: what comes before the first copy is what a small call waits for.)
 template <int D>
 __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
-    __shared__ int warp_sum[32];
+    __shared__ int warp_sum[32], total;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-    int carry = 0;
-    for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
-        const int b = b0 + threadIdx.x;
-        int x = 0;
-        if (b < a.B) {
-            const bool ok = tree_ok(a, b);
-            const int n = ok ? a.starts[b + 1] - a.starts[b] : 0, len = ok ? a.kv.lens[b] : 0;
-            T.len[b] = len, T.nodes[b] = n;
-            if (n > 0) x = a.hkv * chunks_of<D>(n * a.group) * (blocks_of(len, n) + TA_ROW);
-        }
+    auto places = [&](int b) {
+        const int s = a.starts[b], e = a.starts[b + 1], l = a.kv.lens[b];
+        const bool ok = s >= 0 && e >= s && e <= a.T && e - s <= TREE_NODES && l >= 0 && l + (long long)(e - s) <= a.kv.cap;
+        const int n = ok ? e - s : 0, len = ok ? l : 0;
+        T.len[b] = len, T.nodes[b] = n;
+        return n > 0 ? a.hkv * chunks_of<D>(n * a.group) * (blocks_of(len, n) + TA_ROW) : 0;
+    };
+    auto scan = [&](int x) {
+#pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
+        return x;
+    };
+    if (threadIdx.x == 0) T.first[0] = 0;
+    if (a.B <= 32) {
+        if (warp == 0) {
+            const int x = scan(lane < a.B ? places(lane) : 0);
+            if (lane < a.B) T.first[lane + 1] = x;
+            if (lane == 31) total = x;
+        }
+        __syncthreads();
+        return total;
+    }
+    int carry = 0;
+    for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
+        const int b = b0 + threadIdx.x;
+        const int x = scan(b < a.B ? places(b) : 0);
         if (lane == 31) warp_sum[warp] = x;
         __syncthreads();
-        int before = carry, all = 0;
-        for (int w = 0; w < n_warps; ++w) {
-            if (w < warp) before += warp_sum[w];
-            all += warp_sum[w];
-        }
+        const int sums = scan(lane < n_warps ? warp_sum[lane] : 0);
+        const int before = carry + (warp ? __shfl_sync(0xffffffffu, sums, warp - 1) : 0);
         if (b < a.B) T.first[b + 1] = before + x;
-        carry += all;
+        carry += __shfl_sync(0xffffffffu, sums, 31);
         __syncthreads();
     }
-    if (threadIdx.x == 0) T.first[0] = 0;
-    __syncthreads();
     return carry;
 }
 
-__device__ __forceinline__ int workers_of(const PackedArgs &a, int count) { return max(1, min(a.workers, (count + TA_MIN - 1) / TA_MIN)); }
-__device__ __forceinline__ int first_of(int w, int count, int workers) { return (int)((long long)w * count / workers); }
-__device__ __forceinline__ int worker_at(long long at, int count, int workers) { return (int)(((at + 1) * workers - 1) / count); }
+// CTAs that share the list, the first place of one of them, and the one that has a place.
+struct Shares {
+    int workers, each, more;  // places of a CTA; CTAs with one more
+    __device__ __forceinline__ Shares(const PackedArgs &a, int count) {
+        workers = max(1, min(a.workers, (count + TA_MIN - 1) / TA_MIN));
+        each = count / workers;
+        more = count - each * workers;
+    }
+    __device__ __forceinline__ int first(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int owner(int at) const {
+        const int big = more * (each + 1);
+        return at < big ? at / (each + 1) : more + (at - big) / each;
+    }
+};
 
 // Blocks [t, t_end) of one unit: what a CTA works on before it leaves the unit.
 struct Segment {
@@ -143,23 +164,20 @@ struct Segment {
     }
 };
 
-constexpr int TA_COPY_WARPS = 2, TA_COPY_ROWS = KEYS / TA_COPY_WARPS;  // rows of a block of one
-
 template <int D>
 struct TreeState {
     using L = TreeShape<D>;
     // s_full, p_full: S and P of the first tile's place, of the second tile, and of the second place where one tile uses both.  (Each has one
     // party that arrives and one that waits, and they see all of its phases: who skips one takes an older one for it.)
-    uint64_t full[L::STAGES], empty[L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], tail[L::RING_SEGS], cleared, drain[2];
+    uint64_t full[2][L::STAGES], empty[2][L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], tail[L::RING_SEGS], drain[2];
     uint32_t tmem;
     int abort, bad_page, bad_tree;
     float top[2][2][ROWS];              // what the two threads of a row tell each other
-    uint32_t valid[TA_MASKS][4];        // keys of a block whose pages are in the cache
-    ulonglong2 rows[TA_COPY_WARPS][2][TA_COPY_ROWS];  // a copying warp's rows of two blocks: where K and V come from
-    // of a segment: who sees infinite or NaN values, in each dimension: the nodes' bits, or everybody (a cached slot)
+    alignas(8) uint32_t valid[TA_MASKS][4];  // keys of a block whose pages are in the cache
+    unsigned long long rows[2][KEYS];  // where a block's rows of K, and of V, come from; of pieces: the map's coordinates
+    // of a segment: nodes with infinite or NaN values, in each dimension
     int odd[L::RING_SEGS];
     unsigned long long odd_nodes[L::RING_SEGS][D];
-    int odd_all[L::RING_SEGS][D];
 };
 
 __device__ __forceinline__ void cp_async16_or_zero(uint32_t dst, const void *src, bool real) {
@@ -174,10 +192,10 @@ __device__ __forceinline__ void mbarrier_arrive_many(uint64_t *bar, uint32_t n) 
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
 }
 
-// box: rows of a page that one tiled copy brings (0: none do).
+// box: rows of a page that one tiled copy brings (0: none do); page_step: a page's stride in heads.
 template <int D, bool FP16>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_tree(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PackedArgs a, int box) {
+    k_tree(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, const __grid_constant__ PackedArgs a, int box, int page_step) {
     using L = TreeShape<D>;
     constexpr int TILES = L::TILES, UNITS = L::UNITS, STAGES = L::STAGES;
     extern __shared__ uint8_t smem_raw[];
@@ -190,8 +208,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (warp == 18) tmem_alloc(&S.tmem, TM_COLS);
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
-            mbar_init(&S.full[i], 32 * TA_COPY_WARPS);
-            mbar_init(&S.empty[i], 2);
+            for (int kv = 0; kv < 2; ++kv) {
+                mbar_init(&S.full[kv][i], box ? 1 : 32);
+                mbar_init(&S.empty[kv][i], 2);
+            }
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&S.q_full[i], 8);
@@ -205,8 +225,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&S.p_full[i][0], 8);
             mbar_init(&S.p_full[i][1], 8);
         }
-        for (int i = 0; i < L::RING_SEGS; ++i) mbar_init(&S.tail[i], 32 * TA_COPY_WARPS);
-        mbar_init(&S.cleared, 32 * TA_COPY_WARPS);
+        for (int i = 0; i < L::RING_SEGS; ++i) mbar_init(&S.tail[i], 1);
         S.abort = S.bad_page = S.bad_tree = 0;
         fence_mbarrier_init();
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (k_tree_join reports; a wait runs out a second later)
@@ -217,182 +236,207 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     tc_fence_before();
     const int count = tree_list<D>(a, T);  // (its barriers order what is above, too)
-    const int workers = workers_of(a, count), me = blockIdx.x;
+    const Shares shares(a, count);
+    const int me = blockIdx.x;
     tc_fence_after();
     const uint32_t tmem = S.tmem;
     Segment seg{};
-    bool more = me < workers && seg.seek<D>(first_of(me, count, workers), first_of(me + 1, count, workers), a, T);
+    bool more = me < shares.workers && seg.seek<D>(shares.first(me), shares.first(me + 1), a, T);
     // rows of the segment's unit from its chunk's first on
     auto rows_of = [&]() { return T.nodes[seg.b] * a.group - (seg.unit % seg.chunks) * L::ROWS_ALL; };
 
     if (warp >= ROW_WARPS) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-        if (warp < 16 + TA_COPY_WARPS) {
-            // ---- copies, in the ring's order; warp w rows 64 w .. of each block
-            const int w = warp - 16, t_copy = w * 32 + lane;
-            constexpr int CPR = L::DU / 8, RPI = 32 / CPR, STEPS = TA_COPY_ROWS / RPI;  // 16-byte pieces of a unit's row, rows of a step, steps
-            const int piece = lane % CPR, r_lane = lane / CPR;
-            // where piece `piece` of the warp's row r lies in a unit
-            auto place = [&](int r) { return (uint32_t)((piece >> 3) * SUB + (TA_COPY_ROWS * w + r) * 128 + (((piece & 7) ^ (r & 7)) << 4)); };
-            auto entry = [&](const Segment &g, int t, int e) {
-                const int key = t * KEYS + TA_COPY_ROWS * w + 32 * e + lane;
-                return key < T.len[g.b] + T.nodes[g.b] ? a.kv.table[(long long)g.b * a.kv.max_pages + page_index(a.kv, key)] : 0;
-            };
-            int issued = 0, block = 0, sn = 0, clears = 0;
+        if (warp < 18) {
+            // ---- copies: warp 16 K, warp 17 V.  (Warps that run little beside others that run much fetch their code anew each time, at about 6
+            // cycles an instruction: whole blocks of cached slots have a short path of their own.)
+            const int kv = warp - 16;
+            constexpr int CPR = L::DU / 8, RPI = 32 / CPR;  // 16-byte pieces of a unit's row, rows of a step
+            using Y = Layout<D, true>;
+            const int piece = lane % CPR, r_lane = lane / CPR, pieces = box ? KEYS / box : 0;
+            unsigned long long *rows = S.rows[kv];
+            const CUtensorMap *map = kv ? &vmap : &kmap;
+            uint8_t *units = ring + kv * STAGES * L::UNIT;
+            int issued = 0, block = 0, sn = 0;
             bool ok = true;
-            int page[2] = {0, 0}, pend_unit = -1, pend_t = 0, pend_kv = 0, pend_u = 0;  // what the last copy of rows has still to be looked at
-            if (more)
-                for (int e = 0; e < 2; ++e) page[e] = entry(seg, seg.t, e);
+            int pend = -1, pend_u = 0, pend_t = 0;  // the unit of rows that has still to be looked at
+            // What a lane says of a unit that it has copied: with tiled copies one lane for its warp.
+            auto arrive = [&](uint64_t *bar) {
+                if (box) __syncwarp();
+                if (!box || lane == 0) mbarrier_arrive_one(bar);
+            };
+            auto next_slot = [&]() {
+                const int slot = issued % STAGES;
+                ok = __all_sync(0xffffffffu, mbar_wait_short(&S.empty[kv][slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort));
+                ++issued;
+                return slot;
+            };
+            // A piece's place in the map, packed: page and head in one (outside the map for a page outside the cache: the copy brings
+            // zeros, which no weight makes NaN), and eights of the page.
+            auto packed = [&](int page, int h, int key) {
+                const bool bad = (unsigned)page >= (unsigned)a.kv.n_pages;
+                return (unsigned long long)(unsigned)(bad ? -1 : page * page_step + h) << 32 | (unsigned)(key - page_index(a.kv, key) * a.kv.page_size) / 8;
+            };
+            auto copy_piece = [&](uint8_t *unit, int r, int u, uint64_t *bar) {
+                const unsigned long long at = rows[r];
+                tma_load_5d(unit + r / 8 * Y::EIGHT, map, 0, 0, u * (L::DU / 64), (int)(unsigned)at, (int)(at >> 32), bar);
+            };
             for (; ok && more; ++sn) {
-                const int b = seg.b, len = T.len[b], nodes = T.nodes[b], h = seg.unit / seg.chunks, start = a.starts[b];
-                const bool store = seg.unit % seg.chunks == 0, two = TILES == 2 && rows_of() > ROWS;
-                const int tail0 = len / KEYS, nb = seg.t_end - seg.t;  // (the first block with nodes or places behind them)
-                const int si = sn % L::RING_SEGS;
-                Segment nxt = seg;
-                const bool nxt_more = nxt.next<D>(a, T);
-                // Rows of the last block with nodes that were copied: K's go to the cache, V's too and are looked at.
-                auto finish = [&]() {
-                    const uint32_t to = smem_u32(ring + pend_unit * L::UNIT);
-                    const uint32_t *valid = S.valid[(block + pend_t - seg.t) % TA_MASKS] + 2 * w;
-                    const int k0 = pend_t * KEYS + TA_COPY_ROWS * w, d0 = pend_u * L::DU + piece * 8;
+                const int b = seg.b, len = T.len[b], nodes = T.nodes[b], h = seg.unit / seg.chunks;
+                const int tail0 = len / KEYS, si = sn % L::RING_SEGS;  // (the first block with nodes or places behind them)
+                const int *table = a.kv.table + (long long)b * a.kv.max_pages;
+                int t = seg.t;
+                if (box && t < min(tail0, seg.t_end)) {
+                    int page = lane < pieces ? table[page_index(a.kv, t * KEYS + lane * box)] : 0;
 #pragma unroll 1
-                    for (int x0 = 0; x0 < STEPS; x0 += 4) {
-                        uint4 v[4];
-                        uint32_t any = 0;
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            v[y] = ld_shared_u4(to + place((x0 + y) * RPI + r_lane));
-                            any |= odd_halves<FP16>(v[y].x) | odd_halves<FP16>(v[y].y) | odd_halves<FP16>(v[y].z) | odd_halves<FP16>(v[y].w);
+                    for (; ok && t < min(tail0, seg.t_end); ++t) {
+                        const int key = t * KEYS + lane * box;
+                        __syncwarp();
+                        if (lane < pieces) rows[lane * box] = packed(page, h, key);
+                        const unsigned lost = __ballot_sync(0xffffffffu, lane < pieces && (unsigned)page >= (unsigned)a.kv.n_pages);
+                        if (lost) *(volatile int *)&S.bad_page = 1;
+                        if (kv == 0 && lane < 4) {
+                            uint32_t valid = 0xffffffffu;
+                            if (lost)
+                                for (int r = 0; r < 32; ++r)
+                                    if (lost >> ((32 * lane + r) / box) & 1) valid &= ~(1u << r);
+                            *(volatile uint32_t *)&S.valid[(block + t - seg.t) % TA_MASKS][lane] = valid;
                         }
-                        if (store && k0 + (x0 + 4) * RPI > len) {
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) {
-                                const int r = (x0 + y) * RPI + r_lane, key = k0 + r;
-                                if (key < len || !(valid[r >> 5] >> (r & 31) & 1)) continue;
-                                const int pi = page_index(a.kv, key);
-                                const long long dst = a.kv.table[(long long)b * a.kv.max_pages + pi] * a.kv.stride_page + h * a.kv.stride_head +
-                                                      (key - pi * a.kv.page_size) * a.kv.stride_slot + d0;
-                                *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(pend_kv ? a.kv.v : a.kv.k) + dst) = v[y];
+                        if (lane < pieces && t + 1 < min(tail0, seg.t_end)) page = table[page_index(a.kv, key + KEYS)];
+                        __syncwarp();
+#pragma unroll 1
+                        for (int u = 0; u < UNITS; ++u) {
+                            const int slot = next_slot();
+                            if (!ok) break;
+                            if (elect_one()) {
+                                uint64_t *bar = &S.full[kv][slot];
+                                mbar_arrive_expect_tx(bar, (uint32_t)L::UNIT);
+#pragma unroll 1
+                                for (int r = 0; r < KEYS; r += box) copy_piece(units + slot * L::UNIT, r, u, bar);
                             }
+                            __syncwarp();
                         }
-                        if (any == 0 || pend_kv == 0) continue;
+                    }
+                }
+                // Blocks with nodes, and all where pages hold no multiple of 8.  Rows behind `hi` are not multiplied.
+                const bool store = seg.unit % seg.chunks == 0;
+                const int start = a.starts[b];
+                auto row_hi = [&](int t) { return min(((len + nodes + 15) & ~15) - t * KEYS, KEYS); };
+                // Nodes' rows of the last unit that was copied: they go to the cache, and V's are looked at.
+                auto finish = [&]() {
+                    const uint32_t to = smem_u32(units + pend * L::UNIT);
+                    const int k0 = pend_t * KEYS, d0 = pend_u * L::DU + piece * 8, hi = row_hi(pend_t);
 #pragma unroll 1
-                        for (int e = 0; e < 32; ++e) {  // (value by value: this is rare)
-                            const int r = (x0 + (e >> 3)) * RPI + r_lane, i = k0 + r - len;
-                            const uint32_t at = to + place(r) + 2 * (e & 7);
+                    for (int r = max(len - k0, 0) / RPI * RPI + r_lane; r < hi; r += RPI) {  // (each lane its own pieces)
+                        const int key = k0 + r, i = key - len;
+                        if (i < 0 || rows[r] == 0) continue;
+                        const uint4 v = ld_shared_u4(to + Y::at(r, piece));
+                        if (store) {
+                            const int pi = page_index(a.kv, key);
+                            const long long dst = table[pi] * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot + d0;
+                            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(kv ? a.kv.v : a.kv.k) + dst) = v;
+                        }
+                        if (kv == 0 || !(odd_halves<FP16>(v.x) | odd_halves<FP16>(v.y) | odd_halves<FP16>(v.z) | odd_halves<FP16>(v.w))) continue;
+#pragma unroll 1
+                        for (int e = 0; e < 8; ++e) {  // (value by value: this is rare)
+                            const uint32_t at = to + Y::at(r, piece) + 2 * e;
                             uint16_t y;
                             asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at) : "memory");
                             if (!odd_halves<FP16>(y)) continue;
                             asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((uint16_t)0) : "memory");
-                            if (i < 0)
-                                S.odd_all[si][d0 + (e & 7)] = 1;
-                            else
-                                atomicOr(&S.odd_nodes[si][d0 + (e & 7)], 1ull << i);
+                            atomicOr(&S.odd_nodes[si][d0 + e], 1ull << i);
                             S.odd[si] = 1;
                         }
                     }
                     fence_proxy_async_shared();
-                    mbarrier_arrive_one(&S.full[pend_unit]);
-                    pend_unit = -1;
+                    arrive(&S.full[kv][pend]);
+                    pend = -1;
                 };
-                for (int n = 0; ok && n < 2 * nb; ++n) {
-                    const int x = at_place(n, nb, two), kv = x < 0, t = seg.t + (kv ? ~x : x);
-                    const bool tail = t >= tail0;
-                    if (!kv) {  // the block's rows
-                        const int key0 = t * KEYS + TA_COPY_ROWS * w + lane;
-                        __syncwarp();
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int key = key0 + 32 * e;
-                            const bool cached = key < len, node = !cached && key < len + nodes;
-                            const bool real = (cached || node) && (unsigned)page[e] < (unsigned)a.kv.n_pages;
-                            const int pi = page_index(a.kv, key);
-                            if ((cached || node) && !real) *(volatile int *)&S.bad_page = 1;
-                            ulonglong2 at = make_ulonglong2(0, 0);
-                            if (real && box && !tail) {
-                                at.x = (unsigned)page[e] + 1ull;
-                            } else if (real) {
-                                const long long src = cached ? page[e] * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot
-                                                             : (long long)(start + key - len) * a.kv_stride + h * D;
-                                at.x = reinterpret_cast<unsigned long long>((cached ? a.kv.k : a.k) + src);
-                                at.y = reinterpret_cast<unsigned long long>((cached ? a.kv.v : a.v) + src);
-                            }
-                            const unsigned valid = __ballot_sync(0xffffffffu, real);
-                            S.rows[w][t & 1][32 * e + lane] = at;
-                            if (lane == 0) *(volatile uint32_t *)&S.valid[(block + t - seg.t) % TA_MASKS][2 * w + e] = valid;
-                            if (node && store && a.new_pos && a.kv.positions && real)
-                                a.kv.positions[((long long)b * a.hkv + h) * a.kv.cap + key] = a.new_pos[start + key - len];
-                            // the next block's pages are asked for now
-                            page[e] = t + 1 < seg.t_end ? entry(seg, t + 1, e) : nxt_more ? entry(nxt, nxt.t, e) : 0;
-                        }
-                        __syncwarp();
-                        if (tail && t == max(seg.t, tail0)) {  // nobody looks at this segment's notes yet
-                            for (int d = t_copy; d < D; d += 32 * TA_COPY_WARPS) S.odd_nodes[si][d] = 0, S.odd_all[si][d] = 0;
-                            if (t_copy == 0) S.odd[si] = 0;
-                            mbarrier_arrive_one(&S.cleared);
-                            ok = mbar_wait_short(&S.cleared, clears++ & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-                            if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                        }
-                    }
-                    const ulonglong2 *rows = S.rows[w][t & 1];
-                    for (int u = 0; ok && u < UNITS; ++u) {
-                        const int slot = issued % STAGES;
-                        ok = mbar_wait_short(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort);
-                        if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                        ++issued;
-                        uint64_t *bar = &S.full[slot];
-                        uint8_t *unit = ring + slot * L::UNIT;
-                        if (box && !tail) {  // a lane a piece of a page
-                            const int pieces = TA_COPY_ROWS / box, r = lane * box;
-                            const bool mine = lane < pieces;
-                            const int pg = mine ? (int)rows[mine ? r : 0].x - 1 : -1;
-                            const int there = __popc(__ballot_sync(0xffffffffu, pg >= 0));
-                            if (lane == 0) mbar_expect_tx(bar, (uint32_t)(there * box * L::DU * 2));
-                            __syncwarp();
-                            const int key = t * KEYS + TA_COPY_ROWS * w + r;
-                            if (pg >= 0) {
-                                for (int c = 0; c < L::DU / 64; ++c)
-                                    tma_load_4d(unit + c * SUB + (TA_COPY_ROWS * w + r) * 128, kv ? &vmap : &kmap, u * L::DU + c * 64,
-                                                key - page_index(a.kv, key) * a.kv.page_size, h, pg, bar);
-                            } else if (mine) {  // (slots of a page outside the cache: zeros, which no weight makes NaN)
-                                for (int i = 0; i < box * L::DU / 8; ++i)
-                                    st_shared_u4(smem_u32(unit) + (i / (8 * box)) * SUB + (TA_COPY_ROWS * w + r + (i / 8) % box) * 128 + (i & 7) * 16,
-                                                 make_uint4(0, 0, 0, 0));
-                                fence_proxy_async_shared();
-                            }
-                            __syncwarp();
-                            mbarrier_arrive_one(bar);
-                        } else {
-                            const uint32_t to = smem_u32(unit);
+                if (kv && seg.t_end > tail0) {  // nobody looks at this segment's notes yet
+                    for (int d = lane; d < D; d += 32) S.odd_nodes[si][d] = 0;
+                    if (lane == 0) S.odd[si] = 0;
+                }
 #pragma unroll 1
-                            for (int x0 = 0; x0 < STEPS; x0 += 8) {
-                                unsigned long long src[8];
-#pragma unroll
-                                for (int y = 0; y < 8; ++y) src[y] = (&rows[(x0 + y) * RPI + r_lane].x)[kv];
-#pragma unroll
-                                for (int y = 0; y < 8; ++y)
-                                    cp_async16_or_zero(to + place((x0 + y) * RPI + r_lane),
-                                                       src[y] ? reinterpret_cast<const uint16_t *>(src[y]) + u * L::DU + piece * 8 : a.q, src[y] != 0);
-                            }
-                            if (!tail) cp_async_arrive(bar);
+                for (; ok && t < seg.t_end; ++t) {
+                    const bool tail = t >= tail0;
+                    const int lo = box ? max(min((len - t * KEYS) / box * box, KEYS), 0) : 0, hi = row_hi(t);  // (rows below lo come in pieces)
+                    if (pend >= 0) {  // (its rows are looked up below)
+                        cp_async_wait_all();
+                        finish();
+                    }
+                    __syncwarp();
+#pragma unroll 1
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 32 * e + lane, key = t * KEYS + r, pi = page_index(a.kv, key);
+                        const bool cached = key < len, node = !cached && key < len + nodes;
+                        const int page = cached || node ? table[pi] : -1;
+                        const bool real = (unsigned)page < (unsigned)a.kv.n_pages;
+                        if ((cached || node) && !real) *(volatile int *)&S.bad_page = 1;
+                        unsigned long long at = 0;
+                        if (r < lo) {
+                            at = packed(page, h, key);
+                        } else if (real) {
+                            const uint16_t *from = cached ? (kv ? a.kv.v : a.kv.k) + page * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot
+                                                          : (kv ? a.v : a.k) + (long long)(start + key - len) * a.kv_stride + h * D;
+                            at = reinterpret_cast<unsigned long long>(from);
                         }
-                        if (tail) cp_async_commit();
-                        if (pend_unit >= 0) {
-                            if (tail)
-                                cp_async_wait_1();
-                            else
-                                cp_async_wait_all();
+                        rows[r] = at;
+                        const unsigned valid = __ballot_sync(0xffffffffu, real);
+                        if (kv == 0 && lane == 0) *(volatile uint32_t *)&S.valid[(block + t - seg.t) % TA_MASKS][e] = valid;
+                        if (kv == 0 && node && a.new_pos && a.kv.positions && real && store)
+                            a.kv.positions[((long long)b * a.hkv + h) * a.kv.cap + key] = a.new_pos[start + key - len];
+                    }
+                    __syncwarp();
+#pragma unroll 1
+                    for (int u = 0; ok && u < UNITS; ++u) {
+                        const int slot = next_slot();
+                        if (!ok) break;
+                        uint64_t *bar = &S.full[kv][slot];
+                        uint8_t *unit = units + slot * L::UNIT;
+                        if (lo > 0 && elect_one()) {
+                            mbar_expect_tx(bar, (uint32_t)(lo * L::DU * 2));
+#pragma unroll 1
+                            for (int r = 0; r < lo; r += box) copy_piece(unit, r, u, bar);
+                        }
+                        __syncwarp();
+                        if (hi <= lo) {
+                            arrive(bar);
+                            continue;
+                        }
+                        const uint32_t to = smem_u32(unit);
+#pragma unroll 1
+                        for (int x0 = lo; x0 < hi; x0 += 8 * RPI) {
+                            unsigned long long src[8];
+#pragma unroll
+                            for (int y = 0; y < 8; ++y) src[y] = rows[min(x0 + y * RPI, KEYS - RPI) + r_lane];
+#pragma unroll
+                            for (int y = 0; y < 8; ++y)
+                                if (x0 + y * RPI < hi)
+                                    cp_async16_or_zero(to + Y::at(x0 + y * RPI + r_lane, piece),
+                                                       src[y] ? reinterpret_cast<const uint16_t *>(src[y]) + u * L::DU + piece * 8 : a.q, src[y] != 0);
+                        }
+                        if (!tail) {
+                            cp_async_arrive(bar);
+                            continue;
+                        }
+                        cp_async_commit();
+                        if (pend >= 0) {
+                            cp_async_wait_1();
                             finish();
                         }
-                        if (tail) pend_unit = slot, pend_t = t, pend_kv = kv, pend_u = u;
+                        pend = slot, pend_t = t, pend_u = u;
                     }
                 }
-                cp_async_wait_all();
-                if (ok && pend_unit >= 0) finish();
-                if (ok && seg.t_end > tail0) mbarrier_arrive_one(&S.tail[si]);  // (only a stretch's last segment has no such block)
-                block += nb;
-                seg = nxt;
-                more = nxt_more;
+                if (ok && pend >= 0) {
+                    cp_async_wait_all();
+                    finish();
+                }
+                if (kv && seg.t_end > tail0) {  // (only a stretch's last segment has no such block)
+                    __syncwarp();
+                    if (ok && lane == 0) mbarrier_arrive_one(&S.tail[si]);
+                }
+                block += seg.t_end - seg.t;
+                more = seg.next<D>(a, T);
             }
             cp_async_commit();
             cp_async_wait_all();  // also on the error path: nothing is in flight when the CTA ends
@@ -405,31 +449,31 @@ __global__ void __launch_bounds__(THREADS, 1)
             const int i = warp - 18;
             const uint8_t *q = sq + i * L::QT;
             const uint32_t o = tmem + TM_O + i * D;
-            int pos = 0, step = 0, used_o = 0, cnt0 = 0, cnt1 = 0, cnt2 = 0, twos = 0;  // blocks' K and V, sections, segments of the tile, phases of s_full, segments of two tiles
+            int pos = 0, step = 0, used_o = 0, cnt0 = 0, cnt1 = 0, cnt2 = 0, twos = 0;  // blocks, sections, segments of the tile, phases of s_full, segments of two tiles
             bool ok = true;
             auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.abort); };
-            auto landed = [&](int place) {
-                for (int u = 0; u < UNITS; ++u) wait(&S.full[(place * UNITS + u) % STAGES], (place * UNITS + u) / STAGES, DEV_TIMEOUT_LOAD);
+            auto landed = [&](int kv, int j) {  // K or V of the CTA's block j
+                for (int u = 0; u < UNITS; ++u) wait(&S.full[kv][(j * UNITS + u) % STAGES], (j * UNITS + u) / STAGES, DEV_TIMEOUT_LOAD);
                 if (!box) fence_proxy_async_shared();  // (cp.async's copies land in the generic proxy)
             };
-            auto unit = [&](int place, int u) { return ring + ((place * UNITS + u) % STAGES) * L::UNIT; };
-            auto scores = [&](int buf, int bar, int place) {
-                for (int u = 0; u < UNITS; ++u) mma_scores<D, FP16>(tmem + buf * KEYS, q, unit(place, u), u);
+            auto unit = [&](int kv, int j, int u) { return ring + (kv * STAGES + (j * UNITS + u) % STAGES) * L::UNIT; };
+            auto scores = [&](int buf, int bar, int j) {
+                for (int u = 0; u < UNITS; ++u) mma_scores<D, FP16, true>(tmem + buf * KEYS, q, unit(0, pos + j, u), u);
                 mma_commit(&S.s_full[bar]);
             };
             while (ok && more) {
                 const int nb = seg.t_end - seg.t, keys = T.len[seg.b] + T.nodes[seg.b] - seg.t * KEYS;
                 const bool two = TILES == 2 && rows_of() > ROWS;
-                auto values = [&](int buf, int bar, int j, int place, int phase) {
+                auto values = [&](int buf, int bar, int j, int phase) {
                     const int steps = min(KEYS, keys - j * KEYS + 15) / 16;  // (keys behind the last are not multiplied, to 16)
-                    for (int u = 0; u < UNITS; ++u) mma_values<D, FP16>(o, tmem + buf * KEYS, unit(place, u), u, 0, steps, j == 0);
+                    for (int u = 0; u < UNITS; ++u) mma_values<D, FP16, true>(o, tmem + buf * KEYS, unit(1, pos + j, u), u, 0, steps, j == 0);
                     wait(&S.p_full[bar][1], phase, DEV_TIMEOUT_MMA);
                     if (!ok) return;
                     tc_fence_after();
-                    for (int u = 0; u < UNITS; ++u) mma_values<D, FP16>(o, tmem + buf * KEYS, unit(place, u), u, 1, steps, j == 0);
+                    for (int u = 0; u < UNITS; ++u) mma_values<D, FP16, true>(o, tmem + buf * KEYS, unit(1, pos + j, u), u, 1, steps, j == 0);
                 };
-                auto values_ready = [&](int j, int place) {
-                    landed(place);
+                auto values_ready = [&](int j) {
+                    landed(1, pos + j);
                     if (j == 0 && used_o > 0) wait(&S.o_free[i], used_o - 1, DEV_TIMEOUT_MMA);
                 };
                 if (two) {  // for every block O += P V of the one before, then S; the tiles in turns
@@ -437,15 +481,14 @@ __global__ void __launch_bounds__(THREADS, 1)
                     wait(&S.q_full[i], used_o, DEV_TIMEOUT_LOAD);
 #pragma unroll 1
                     for (int j = 0; ok && j <= nb; ++j, ++step) {
-                        const int vp = pos + v_place(j - 1, nb, true), kp = pos + k_place(j, true);
                         if (i + step > 0) wait(&S.turn[i], step + i - 1, DEV_TIMEOUT_MMA);
-                        if (j > 0) values_ready(j - 1, vp);
-                        if (j < nb) landed(kp);
+                        if (j > 0) values_ready(j - 1);
+                        if (j < nb) landed(0, pos + j);
                         if (j > 0) wait(&S.p_full[i][0], cnt + j - 1, DEV_TIMEOUT_MMA);
                         if (!ok) break;
                         tc_fence_after();
-                        if (j > 0) values(i, i, j - 1, vp, cnt + j - 1);
-                        if (ok && j < nb) scores(i, i, kp);
+                        if (j > 0) values(i, i, j - 1, cnt + j - 1);
+                        if (ok && j < nb) scores(i, i, j);
                         mbarrier_arrive_one(&S.turn[i ^ 1]);
                         if (j == nb) mma_commit(&S.o_done[i]);
                     }
@@ -454,34 +497,34 @@ __global__ void __launch_bounds__(THREADS, 1)
                 } else {  // S of the next block, then O += P V of this one
                     if (i == 0) {
                         wait(&S.q_full[0], used_o, DEV_TIMEOUT_LOAD);
-                        landed(pos);
+                        landed(0, pos);
                         if (ok) {
                             tc_fence_after();
-                            scores(0, 0, pos);
+                            scores(0, 0, 0);
                         }
                         if (twos > 0) wait(&S.o_done[1], twos - 1, DEV_TIMEOUT_MMA);  // (the second tile has left the second place)
 #pragma unroll 1
                         for (int j = 0; ok && j < nb; ++j) {
-                            const int vp = pos + v_place(j, nb, false), kp = pos + k_place(j + 1, false), buf = j & 1;
+                            const int buf = j & 1;
                             if (j + 1 < nb) {
-                                landed(kp);
+                                landed(0, pos + j + 1);
                                 if (!ok) break;
                                 tc_fence_after();
-                                scores(buf ^ 1, buf ? 0 : 2, kp);
+                                scores(buf ^ 1, buf ? 0 : 2, j + 1);
                             }
                             const int phase = (buf ? cnt2 : cnt0) + (j >> 1), bar = 2 * buf;
-                            values_ready(j, vp);
+                            values_ready(j);
                             wait(&S.p_full[bar][0], phase, DEV_TIMEOUT_MMA);
                             if (!ok) break;
                             tc_fence_after();
-                            values(buf, bar, j, vp, phase);
+                            values(buf, bar, j, phase);
                             mma_commit(&S.o_done[0]);
                         }
                         ++used_o;
                     }
                     cnt0 += (nb + 1) / 2, cnt2 += nb / 2;
                 }
-                pos += 2 * nb;
+                pos += nb;
                 more = seg.next<D>(a, T);
             }
             mma_commit(&S.drain[i]);  // every MMA issued completes before TMEM is released
@@ -495,17 +538,17 @@ __global__ void __launch_bounds__(THREADS, 1)
         const float c = a.scale * 1.4426950408889634f;
         float *top = S.top[i][0];
         Row r{0.f, 0.f};
-        int o_phase = 0, cnt = 0, cnt2 = 0, block = 0, pos = 0, sn = 0;  // phases of o_done, of the tile's s_full, of the second place's; blocks, K and V, segments
+        int o_phase = 0, cnt = 0, cnt2 = 0, block = 0, sn = 0;  // phases of o_done, of the tile's s_full, of the second place's; blocks, segments
         bool ok = true;
         for (; ok && more; ++sn, more = seg.next<D>(a, T)) {
             const int b = seg.b, nb = seg.t_end - seg.t, len = T.len[b], n_rows = rows_of();
             const bool two = TILES == 2 && n_rows > ROWS, whole = nb == seg.blocks, ends = seg.t_end > len / KEYS;  // (ends: nodes among its keys)
-            const int pos0 = pos;
-            pos += 2 * nb, block += nb;
+            const int pos = block;
+            block += nb;
             if (i && !two) continue;  // (nothing for the second tile)
-            auto release = [&](int place) {  // K or V of a block is not needed any more
+            auto release = [&](int kv, int j) {  // K or V of a block is not needed any more
                 if (w == 0 && half == 0 && lane == 0)
-                    for (int u = 0; u < UNITS; ++u) mbarrier_arrive_many(&S.empty[((pos0 + place) * UNITS + u) % STAGES], two ? 1 : 2);
+                    for (int u = 0; u < UNITS; ++u) mbarrier_arrive_many(&S.empty[kv][((pos + j) * UNITS + u) % STAGES], two ? 1 : 2);
             };
             const bool real = place_row < n_rows;
             const int row = place_row + (seg.unit % seg.chunks) * L::ROWS_ALL, node = real ? row / a.group : 0;
@@ -565,8 +608,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const int buf = two ? i : j & 1, bar = two ? i : 2 * buf, phase = two ? cnt + j : (buf ? cnt2 : cnt) + (j >> 1);
                 bool there = mbar_wait_short(&S.s_full[bar], phase & 1, a.status, DEV_TIMEOUT_MMA, &S.abort), o_waited = two || j == 0;
                 there = __all_sync(0xffffffffu, there);
-                release(k_place(j, two));
-                if (two && j > 0) release(v_place(j - 1, nb, true));
+                release(0, j);
+                if (two && j > 0) release(1, j - 1);
                 tc_fence_after();
                 uint32_t s[64];
 #pragma unroll
@@ -580,7 +623,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         const int from = k0 + 32 * x - len;  // of the word's first key: its node
                         uint32_t see = from >= 0 ? (from < 64 ? (uint32_t)(anc >> from) : 0u)
                                                  : from <= -32 ? 0xffffffffu : (uint32_t)(anc << -from) | ((1u << -from) - 1);
-                        if (bad) see &= *(volatile uint32_t *)&S.valid[(block - nb + j) % TA_MASKS][2 * half + x];
+                        if (bad) see &= *(volatile uint32_t *)&S.valid[(pos + j) % TA_MASKS][2 * half + x];
 #pragma unroll
                         for (int y = 0; y < 32; ++y)
                             if (!(see >> y & 1)) s[32 * x + y] = __float_as_uint(-INFINITY);
@@ -590,7 +633,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     bool o = true;
                     if (!o_waited) {
                         o = mbar_wait_short(&S.o_done[0], (o_phase + j - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-                        release(v_place(j - 1, nb, false));
+                        release(1, j - 1);
                     }
                     o_waited = true;
                     return __all_sync(0xffffffffu, o) != 0;
@@ -606,14 +649,14 @@ __global__ void __launch_bounds__(THREADS, 1)
             o_phase += two ? 1 : nb;
             bool there = mbar_wait_short(&S.o_done[i], (o_phase - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
             if (there && ends) there = mbar_wait_short(&S.tail[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
-            release(v_place(nb - 1, nb, two));
+            release(1, nb - 1);
             if (!ok || pair_any(id, !there)) break;
             top[half * ROWS + w * 32 + lane] = r.l;
             pair_sync(id);
             r.l += top[(half ^ 1) * ROWS + w * 32 + lane];
             tc_fence_after();
             const bool odd = ends && *(volatile int *)&S.odd[si];
-            auto drop = [&](int d) { return S.odd_all[si][half * (D / 2) + d] != 0 || (S.odd_nodes[si][half * (D / 2) + d] & anc) != 0; };
+            auto drop = [&](int d) { return (S.odd_nodes[si][half * (D / 2) + d] & anc) != 0; };
             const long long out_row = (long long)(a.starts[b] + node) * a.hq + head;
             if (whole) {
                 store_half<D, FP16>(to, row_factor(r), a.out + out_row * D + half * (D / 2), real, (reinterpret_cast<uintptr_t>(a.out) & 31) == 0, odd, drop);
@@ -658,7 +701,8 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
     __shared__ TreeList T;
     __shared__ int most_nodes;
     if (threadIdx.x == 0) most_nodes = 0;
-    const int count = tree_list<D>(a, T), workers = workers_of(a, count);
+    const int count = tree_list<D>(a, T);
+    const Shares shares(a, count);
     const int lane = threadIdx.x & 31, lr = lane >> 3, ld = lane & 7;
     const float c = a.scale * 1.4426950408889634f;
     for (int b = threadIdx.x; b < a.B; b += 32 * TJ_WARPS) atomicMax(&most_nodes, T.nodes[b]);
@@ -683,7 +727,7 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
         const int chunk = (row - lr) / L::ROWS_ALL, pr = row - chunk * L::ROWS_ALL;  // (a chunk is a multiple of four rows)
         const int per = blocks_of(T.len[b], T.nodes[b]) + TA_ROW;
         const int at = T.first[b] + (h * chunks_of<D>(n_rows) + chunk) * per;
-        const int w0 = worker_at(at + TA_ROW, count, workers), w1 = worker_at(at + per - 1, count, workers);
+        const int w0 = shares.owner(at + TA_ROW), w1 = shares.owner(at + per - 1);
         if (w0 == w1) continue;  // one CTA had all blocks
         const bool real = row < n_rows;
         auto part = [&](int w) { return (long long)w * 2 + (w == w0); };
@@ -721,17 +765,21 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
 int rows_all(int d) { return (d == 256 ? 1 : 2) * ROWS; }
 
 // Rows of a page that one tiled copy can bring: a power of two that divides its length, 8 (a swizzle's rows) to 32, and 0 where
-// there is none or a tensor map cannot express the cache.
-int tree_box(const KvView &kv, CUtensorMap *kmap, CUtensorMap *vmap) {
+// there is none or a tensor map cannot express the cache.  Its dimensions: 64 of a row, eight rows, the row's other 64s,
+// the other eights, and page and head in one (a page's stride is one of whole heads in both of the usual orders).
+int tree_box(const KvView &kv, CUtensorMap *kmap, CUtensorMap *vmap, int *page_step) {
     int box = 1;
     while (box < 32 && kv.page_size % (2 * box) == 0) box *= 2;
-    const long long most = 1ll << 38;  // (tensor maps hold strides below 2^40 bytes)
-    if (box < 8 || kv.stride_page >= most || kv.stride_head >= most || kv.stride_slot >= most) return 0;
-    const uint64_t dims[4] = {(uint64_t)kv.d, (uint64_t)kv.page_size, (uint64_t)kv.hkv, (uint64_t)kv.n_pages};
-    auto bytes = [&](long long s) { return (uint64_t)std::max(s, (long long)kv.d) * 2; };  // (one place has any stride)
-    const uint64_t st[3] = {bytes(kv.stride_slot), bytes(kv.stride_head), bytes(kv.stride_page)};
-    const uint32_t bx[4] = {64, (uint32_t)box, 1, 1};
-    return encode_map_16(kmap, kv.k, 4, dims, st, bx) && encode_map_16(vmap, kv.v, 4, dims, st, bx) ? box : 0;
+    auto some = [&](long long s, long long n) { return n > 1 ? s : std::max(s, (long long)kv.d); };  // (one place has any stride)
+    const long long head = kv.hkv > 1 ? kv.stride_head : some(kv.stride_page, kv.n_pages), slot = some(kv.stride_slot, kv.page_size);
+    const long long most = 1ll << 35;  // (tensor maps hold strides below 2^40 bytes)
+    long long step = kv.n_pages > 1 ? kv.stride_page / head : kv.hkv;
+    if (box < 8 || head >= most || slot >= most || (kv.n_pages > 1 && kv.stride_page % head) || step < 1 || step * kv.n_pages + kv.hkv > 0x7fffffffll) return 0;
+    *page_step = (int)step;
+    const uint64_t dims[5] = {64, 8, (uint64_t)kv.d / 64, (uint64_t)kv.page_size / 8, (uint64_t)(step * (kv.n_pages - 1) + kv.hkv)};
+    const uint64_t st[4] = {(uint64_t)slot * 2, 128, (uint64_t)slot * 16, (uint64_t)head * 2};
+    const uint32_t bx[5] = {64, 8, (uint32_t)std::min(kv.d, 128) / 64, (uint32_t)box / 8, 1};
+    return encode_map_16(kmap, kv.k, 5, dims, st, bx) && encode_map_16(vmap, kv.v, 5, dims, st, bx) ? box : 0;
 }
 
 template <int D, bool FP16>
@@ -743,8 +791,9 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     a.workers = std::min(gemm_ctas(), TREE_MAX_WORKERS);
     if (a.workers < 1) return cudaErrorInvalidDevice;
     CUtensorMap kmap{}, vmap{};
-    const int box = tree_box(a.kv, &kmap, &vmap);
-    k_tree<D, FP16><<<a.workers, THREADS, L::SMEM, st>>>(kmap, vmap, a, box);
+    int step = 0;
+    const int box = tree_box(a.kv, &kmap, &vmap, &step);
+    k_tree<D, FP16><<<a.workers, THREADS, L::SMEM, st>>>(kmap, vmap, a, box, step);
     const cudaError_t c = cudaGetLastError();
     if (c != cudaSuccess) return c;
     const long long warps = ((long long)std::min<long long>(a.T, (long long)a.B * TREE_NODES) * a.hq + TJ_ROWS - 1) / TJ_ROWS;
