@@ -149,29 +149,25 @@ template <int D, bool FP16, typename Drop>
 __device__ __forceinline__ bool store_half(uint32_t o_at, float f, uint16_t *out, bool real, bool wide, bool careful, Drop &&drop) {
     uint32_t odd = 0;
 #pragma unroll 1
-    for (int x = 0; x < D / 2; x += 32) {
-        uint32_t o[32];
-        tmem_ld_32cols(o_at + x, o);
+    for (int x = 0; x < D / 2; x += 16) {
+        uint32_t o[16], v[8];
+        tmem_ld_16cols(o_at + x, o);
         tmem_ld_wait();
         if (careful)
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
+            for (int e = 0; e < 16; ++e)
                 if (drop(x + e)) o[e] = 0x7fffffffu;
         if (!real) continue;
 #pragma unroll
-        for (int e = 0; e < 32; e += 16) {
-            uint32_t v[8];
-#pragma unroll
-            for (int y = 0; y < 8; ++y) {
-                v[y] = pack16<FP16>(__uint_as_float(o[e + 2 * y]) * f, __uint_as_float(o[e + 2 * y + 1]) * f);
-                odd |= odd_halves<FP16>(v[y]);
-            }
-            if (wide) {
-                st_global_32(out + x + e, v);
-            } else {
-                *reinterpret_cast<uint4 *>(out + x + e) = make_uint4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<uint4 *>(out + x + e + 8) = make_uint4(v[4], v[5], v[6], v[7]);
-            }
+        for (int y = 0; y < 8; ++y) {
+            v[y] = pack16<FP16>(__uint_as_float(o[2 * y]) * f, __uint_as_float(o[2 * y + 1]) * f);
+            odd |= odd_halves<FP16>(v[y]);
+        }
+        if (wide) {
+            st_global_32(out + x, v);
+        } else {
+            *reinterpret_cast<uint4 *>(out + x) = make_uint4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<uint4 *>(out + x + 8) = make_uint4(v[4], v[5], v[6], v[7]);
         }
     }
     return odd != 0;

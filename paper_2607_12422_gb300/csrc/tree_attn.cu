@@ -173,6 +173,7 @@ struct TreeState {
     uint32_t tmem;
     int abort, bad_page, bad_tree;
     float top[2][2][ROWS];              // what the two threads of a row tell each other
+    Segment row_seg[ROW_WARPS];         // where each of the rows' warps is (to spare registers)
     alignas(8) uint32_t valid[TA_MASKS][4];  // keys of a block whose pages are in the cache
     unsigned long long rows[2][KEYS];  // where a block's rows of K, and of V, come from; of pieces: the map's coordinates
     // of a segment: nodes with infinite or NaN values, in each dimension
@@ -540,9 +541,21 @@ __global__ void __launch_bounds__(THREADS, 1)
         Row r{0.f, 0.f};
         int o_phase = 0, cnt = 0, cnt2 = 0, block = 0, sn = 0;  // phases of o_done, of the tile's s_full, of the second place's; blocks, segments
         bool ok = true;
-        for (; ok && more; ++sn, more = seg.next<D>(a, T)) {
-            const int b = seg.b, nb = seg.t_end - seg.t, len = T.len[b], n_rows = rows_of();
-            const bool two = TILES == 2 && n_rows > ROWS, whole = nb == seg.blocks, ends = seg.t_end > len / KEYS;  // (ends: nodes among its keys)
+        S.row_seg[warp] = seg;
+        auto advance = [&]() {
+            __syncwarp();
+            Segment g = S.row_seg[warp];
+            const bool any = g.next<D>(a, T);
+            __syncwarp();
+            S.row_seg[warp] = g;
+            return any;
+        };
+        for (; ok && more; ++sn, more = advance()) {
+            __syncwarp();
+            const Segment *g = &S.row_seg[warp];
+            const int b = g->b, nb = g->t_end - g->t, first_row = g->unit % g->chunks * L::ROWS_ALL, n_rows = T.nodes[b] * a.group - first_row;
+            const int from0 = g->t * KEYS + 64 * half - T.len[b];  // the node of this thread's first key, cached ones below 0
+            const bool two = TILES == 2 && n_rows > ROWS, whole = nb == g->blocks, ends = g->t_end > T.len[b] / KEYS;  // (ends: nodes among its keys)
             const int pos = block;
             block += nb;
             if (i && !two) continue;  // (nothing for the second tile)
@@ -551,12 +564,12 @@ __global__ void __launch_bounds__(THREADS, 1)
                     for (int u = 0; u < UNITS; ++u) mbarrier_arrive_many(&S.empty[kv][((pos + j) * UNITS + u) % STAGES], two ? 1 : 2);
             };
             const bool real = place_row < n_rows;
-            const int row = place_row + (seg.unit % seg.chunks) * L::ROWS_ALL, node = real ? row / a.group : 0;
-            const int head = (seg.unit / seg.chunks) * a.group + (real ? row - node * a.group : 0);
+            const int node = real ? (place_row + first_row) / a.group : 0;
             {  // the queries (the tile's last MMAs are done); a row's two warps share its pieces
                 constexpr int CPH = D / 16, RPI = 32 / CPH;
                 const int piece = half * CPH + lane % CPH;
                 const uint32_t mine = smem_u32(sq + i * L::QT) + (piece >> 3) * SUB + w * 32 * 128;
+                const int head = g->unit / g->chunks * a.group + place_row + first_row - node * a.group;
                 const long long q_off = real ? (long long)(a.starts[b] + node) * a.q_stride + head * D : -1;
 #pragma unroll 4
                 for (int x = 0; x < 32; x += RPI) {
@@ -615,12 +628,11 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
                 for (int x = 0; x < 64; x += 32) tmem_ld_32cols(ts + buf * KEYS + x, *reinterpret_cast<uint32_t(*)[32]>(&s[x]));
                 tmem_ld_wait();
-                const int k0 = (seg.t + j) * KEYS + 64 * half;
                 const bool bad = *(volatile int *)&S.bad_page != 0;
-                if (bad || k0 + 64 > len) {
+                if (bad || from0 + j * KEYS + 64 > 0) {
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const int from = k0 + 32 * x - len;  // of the word's first key: its node
+                        const int from = from0 + j * KEYS + 32 * x;  // of the word's first key
                         uint32_t see = from >= 0 ? (from < 64 ? (uint32_t)(anc >> from) : 0u)
                                                  : from <= -32 ? 0xffffffffu : (uint32_t)(anc << -from) | ((1u << -from) - 1);
                         if (bad) see &= *(volatile uint32_t *)&S.valid[(pos + j) % TA_MASKS][2 * half + x];
@@ -657,25 +669,27 @@ __global__ void __launch_bounds__(THREADS, 1)
             tc_fence_after();
             const bool odd = ends && *(volatile int *)&S.odd[si];
             auto drop = [&](int d) { return (S.odd_nodes[si][half * (D / 2) + d] & anc) != 0; };
-            const long long out_row = (long long)(a.starts[b] + node) * a.hq + head;
+            const Segment *e = &S.row_seg[warp];  // (read again)
+            const int row = place_row + e->unit % e->chunks * L::ROWS_ALL, head = e->unit / e->chunks * a.group + row % a.group;
+            const long long out_row = (long long)(a.starts[e->b] + row / a.group) * a.hq + head;
             if (whole) {
                 store_half<D, FP16>(to, row_factor(r), a.out + out_row * D + half * (D / 2), real, (reinterpret_cast<uintptr_t>(a.out) & 31) == 0, odd, drop);
                 if (a.lse && half == 0 && real) a.lse[out_row] = row_lse<FP16>(r, a.scale);
             } else {  // a row's four values beside those of its neighbours
-                const long long part = (long long)me * 2 + (seg.t == 0);  // of units a stretch has at most two parts: an end and a beginning
+                const long long part = (long long)me * 2 + (e->t == 0);  // of units a stretch has at most two parts: an end and a beginning
                 float4 *po = reinterpret_cast<float4 *>(a.part_o) + (part * (D / 4) + half * (D / 8)) * a.part_rows + place_row;
 #pragma unroll 1
-                for (int x = 0; x < D / 2; x += 32) {
-                    uint32_t v[32];
-                    tmem_ld_32cols(to + x, v);
+                for (int x = 0; x < D / 2; x += 16) {
+                    uint32_t v[16];
+                    tmem_ld_16cols(to + x, v);
                     tmem_ld_wait();
                     if (odd)
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
+                        for (int e = 0; e < 16; ++e)
                             if (drop(x + e)) v[e] = 0x7fffffffu;
                     if (real)
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
+                        for (int e = 0; e < 16; e += 4)
                             po[(long long)((x + e) / 4) * a.part_rows] =
                                 make_float4(__uint_as_float(v[e]), __uint_as_float(v[e + 1]), __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
                 }
@@ -692,8 +706,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (threadIdx.x == 0) a.worker_code[me] = S.bad_page ? DEV_BAD_PAGE : S.bad_tree ? DEV_BAD_TREE : DEV_OK;
 }
 
-// Joins the parts of units that several CTAs worked on: a warp four rows of a unit (node by node, the heads of its group
-// innermost), eight lanes a row.  The first CTA reports.
+// Joins the parts of units that several CTAs worked on: a warp 32 dimensions of four rows of a unit (node by node, the heads of its
+// group innermost), eight lanes a row.  Parts are taken eight at a time, whose loads go out together (one after the other, 64 nodes
+// behind 131071 slots, whose units have 20 parts, took 50 us here).  The first CTA reports.
 constexpr int TJ_WARPS = 8, TJ_ROWS = 4;
 template <int D, bool FP16>
 __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_constant__ PackedArgs a) {
@@ -707,7 +722,7 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
     const float c = a.scale * 1.4426950408889634f;
     for (int b = threadIdx.x; b < a.B; b += 32 * TJ_WARPS) atomicMax(&most_nodes, T.nodes[b]);
     __syncthreads();
-    const int per_unit = (most_nodes * a.group + TJ_ROWS - 1) / TJ_ROWS;  // groups of rows of a (sequence, KV head)
+    const int per_unit = (most_nodes * a.group + TJ_ROWS - 1) / TJ_ROWS * (D / 32);  // of a (sequence, KV head)
     pdl_wait();
     if (blockIdx.x == 0) {
         int code = DEV_OK;
@@ -721,44 +736,46 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
     }
     const long long all = (long long)a.B * a.hkv * per_unit;
     for (long long x = (long long)blockIdx.x * TJ_WARPS + (threadIdx.x >> 5); x < all; x += (long long)gridDim.x * TJ_WARPS) {
-        const int bh = (int)(x / per_unit), b = bh / a.hkv, h = bh - b * a.hkv, row = (int)(x - (long long)bh * per_unit) * TJ_ROWS + lr;
-        const int n_rows = T.nodes[b] * a.group;
-        if (row - lr >= n_rows) continue;
-        const int chunk = (row - lr) / L::ROWS_ALL, pr = row - chunk * L::ROWS_ALL;  // (a chunk is a multiple of four rows)
+        const int bh = (int)(x / per_unit), b = bh / a.hkv, h = bh - b * a.hkv, y = (int)(x - (long long)bh * per_unit);
+        const int row0 = y / (D / 32) * TJ_ROWS, d4 = y % (D / 32) * 8 + ld, n_rows = T.nodes[b] * a.group;
+        if (row0 >= n_rows) continue;
+        const int chunk = row0 / L::ROWS_ALL, pr = min(row0 + lr, n_rows - 1) - chunk * L::ROWS_ALL;  // (a chunk is a multiple of four rows)
         const int per = blocks_of(T.len[b], T.nodes[b]) + TA_ROW;
         const int at = T.first[b] + (h * chunks_of<D>(n_rows) + chunk) * per;
         const int w0 = shares.owner(at + TA_ROW), w1 = shares.owner(at + per - 1);
         if (w0 == w1) continue;  // one CTA had all blocks
-        const bool real = row < n_rows;
         auto part = [&](int w) { return (long long)w * 2 + (w == w0); };
+        auto max_sum = [&](int w) { return w <= w1 ? a.part_ml[part(w) * a.part_rows + pr] : make_float2(-INFINITY, 0.f); };
         float m = -INFINITY;
-        for (int w = w0; real && w <= w1; ++w) m = fmaxf(m, a.part_ml[part(w) * a.part_rows + pr].x);
+#pragma unroll 4
+        for (int w = w0 + ld; w <= w1; w += 8) m = fmaxf(m, max_sum(w).x);
+#pragma unroll
+        for (int o = 4; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         float l = 0.f;
-        float4 o[D / 32];
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int w = w0; real && w <= w1; ++w) {
-            const float2 ml = a.part_ml[part(w) * a.part_rows + pr];
-            const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + part(w) * (D / 4) * a.part_rows + pr;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 *po = reinterpret_cast<const float4 *>(a.part_o) + (long long)d4 * a.part_rows + pr;
+        for (int w8 = w0; w8 <= w1; w8 += 8) {
+            const float2 ml = max_sum(w8 + ld);
             const float f = ml.x == m ? 1.f : ex2((ml.x - m) * c);
-            l += ml.y * f;
+            l += ml.y * f;  // (NaN where ml is: a part that nobody has adds 0)
+            float4 v[8];
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) {
-                const float4 v = po[(long long)(ld + 8 * j) * a.part_rows];
-                o[j].x += v.x * f, o[j].y += v.y * f, o[j].z += v.z * f, o[j].w += v.w * f;
+            for (int k = 0; k < 8; ++k) v[k] = w8 + k <= w1 ? po[part(w8 + k) * (D / 4) * a.part_rows] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float g = __shfl_sync(0xffffffffu, f, (lane & 24) + k);
+                if (w8 + k <= w1) o.x += v[k].x * g, o.y += v[k].y * g, o.z += v[k].z * g, o.w += v[k].w * g;
             }
         }
-        if (!real) continue;
+#pragma unroll
+        for (int e = 4; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
+        if (row0 + lr >= n_rows) continue;
         const Row r{m, l};
         const float inv = row_factor(r);
-        const int node = row / a.group;
+        const int row = row0 + lr, node = row / a.group;
         const long long out_row = (long long)(a.starts[b] + node) * a.hq + h * a.group + row - node * a.group;
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j)
-            *reinterpret_cast<uint2 *>(a.out + out_row * D + (ld + 8 * j) * 4) =
-                make_uint2(pack16<FP16>(o[j].x * inv, o[j].y * inv), pack16<FP16>(o[j].z * inv, o[j].w * inv));
-        if (a.lse && ld == 0) a.lse[out_row] = row_lse<FP16>(r, a.scale);
+        *reinterpret_cast<uint2 *>(a.out + out_row * D + d4 * 4) = make_uint2(pack16<FP16>(o.x * inv, o.y * inv), pack16<FP16>(o.z * inv, o.w * inv));
+        if (a.lse && d4 == 0) a.lse[out_row] = row_lse<FP16>(r, a.scale);
     }
 }
 
@@ -796,7 +813,7 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     k_tree<D, FP16><<<a.workers, THREADS, L::SMEM, st>>>(kmap, vmap, a, box, step);
     const cudaError_t c = cudaGetLastError();
     if (c != cudaSuccess) return c;
-    const long long warps = ((long long)std::min<long long>(a.T, (long long)a.B * TREE_NODES) * a.hq + TJ_ROWS - 1) / TJ_ROWS;
+    const long long warps = ((long long)std::min<long long>(a.T, (long long)a.B * TREE_NODES) * a.hq + TJ_ROWS - 1) / TJ_ROWS * (D / 32);
     const int grid = (int)std::min<long long>((warps + TJ_WARPS - 1) / TJ_WARPS, 8ll * gemm_ctas());
     return launch_pdl(k_tree_join<D, FP16>, grid, 32 * TJ_WARPS, 0, st, a);
 }
