@@ -11,6 +11,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace pbd {
 
 typedef __nv_bfloat16 bf16;
@@ -563,6 +565,20 @@ cudaError_t launch_pdl(void (*kernel)(P...), int grid, int threads, size_t smem,
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
+// Calls `f`, which sets kernels' attributes, the first time on each device.  `done`: a bit a device (from 64 devices on f is called
+// each time).
+template <typename F>
+cudaError_t once_per_device(std::atomic<uint64_t> &done, F &&f) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = f();
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 // One cluster of `ctas` CTAs.
 template <typename... P, typename... A>
 cudaError_t launch_cluster(void (*kernel)(P...), int ctas, int threads, cudaStream_t st, A &&...args) {
@@ -575,7 +591,7 @@ cudaError_t launch_cluster(void (*kernel)(P...), int ctas, int threads, cudaStre
     attr[0].val.clusterDim.x = (unsigned)ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = ctas > 1;  // (one CTA is a cluster by itself)
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 

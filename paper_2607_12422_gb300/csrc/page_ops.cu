@@ -126,28 +126,40 @@ __global__ void __launch_bounds__(AP_THREADS) k_assign_pages(const __grid_consta
         return at < n_free ? a.free_list[at] : given(at - n_free);
     };
     auto valid = [&](int page) { return (unsigned)page < (unsigned)a.n_pages; };
+    // Every page that moves, first those that are taken, then those that stay on the stack: where from, where to.
+    const int moves = max(take, give);
+    auto source = [&](int i) { return i < take ? taken(i) : given(i - take); };
+    auto put = [&](int i, int page) {
+        if (i < take) {
+            const int s = owner(S.take, a.B, i);
+            a.table[(long long)s * a.max_pages + S.held[s] + (i - S.take[s])] = page;
+        } else {
+            a.free_list[n_free + i - take] = page;
+        }
+    };
+    constexpr int KEPT = 4;  // a thread's first moves stay in registers between the check and the writing
+    int page[KEPT];
+    bad_page = false;
     if (code == DEV_OK) {
-        bad_page = false;
-#pragma unroll 4
-        for (int i = me; i < give; i += all) bad_page |= !valid(given(i));
-#pragma unroll 4
-        for (int i = me; i < take - give; i += all) bad_page |= !valid(a.free_list[n_free - 1 - i]);
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k) {
+            page[k] = me + k * all < moves ? source(me + k * all) : 0;
+            bad_page |= !valid(page[k]);
+        }
+        for (int i = me + KEPT * all; i < moves; i += all) bad_page |= !valid(source(i));
     }
     // (code so far is the same in all CTAs; what all of them found also says that all have read what is written below)
-    const int bad_here = __syncthreads_or(code == DEV_OK && bad_page);
+    const int bad_here = __syncthreads_or(bad_page);
     cluster_wait();
     if (b < ctas) st_cluster_u32(map_cta(smem_u32(&S.bad[rank]), b), bad_here);
     cluster_sync();
     for (int i = 0; i < ctas; ++i)
         if (S.bad[i]) code = DEV_BAD_PAGE;
     if (code == DEV_OK) {
-#pragma unroll 2
-        for (int i = me; i < take; i += all) {
-            const int s = owner(S.take, a.B, i);
-            a.table[(long long)s * a.max_pages + S.held[s] + (i - S.take[s])] = taken(i);
-        }
-#pragma unroll 2
-        for (int i = me; i < give - take; i += all) a.free_list[n_free + i] = given(i);
+#pragma unroll
+        for (int k = 0; k < KEPT; ++k)
+            if (me + k * all < moves) put(me + k * all, page[k]);
+        for (int i = me + KEPT * all; i < moves; i += all) put(i, source(i));
         if (rank == 0 && b < a.B) a.held[b] = need;
         if (me == 0) *a.n_free = top - take;
     }
@@ -160,7 +172,6 @@ __global__ void __launch_bounds__(AP_THREADS) k_assign_pages(const __grid_consta
     for (int t = me; t < a.max_new; t += all) bad |= expand(a, S.fresh, S.len, rows, t);
     if (bad) latch_error(a.status, DEV_BAD_PAGE);
 }
-
 
 constexpr int AP_EXPAND = 256;
 __global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constant__ AssignArgs a) {
@@ -178,11 +189,12 @@ __global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constan
 
 // ------------------------------------------------------------------ accepted paths
 //
-// Row len + path[i] of a sequence goes to len + i, i < n_accepted.  path ascends, so path[i] >= i; a row's target may be
-// another one's source.  One CTA takes all rows of one (sequence, KV head): it holds them in registers before it writes any.
-// Bound by a chain of loads (length, path, table, row), and by random rows of 2 d bytes where there are many.  k_clear_status, which
-// overlaps it, makes room for what any CTA finds wrong (one CTA that looks at all paths takes 50 us for 512 of them).
-constexpr int CP_THREADS = 256;
+// Row len + path[i] of a sequence goes to len + i, i < n_accepted.  path ascends, so path[i] >= i: a row's target may be an earlier
+// row's source, and never a later one's.  So rows are taken in their order, some at a time, which are read before any of them is written.
+// One small CTA takes one (sequence, KV head): each is a chain of loads (length, path, table, rows), so that many at once count.
+// (512 sequences of 8 KV heads, 12 rows to move in each on average, 26 MB read and as much written: 9.2 us, 5.7 TB/s; with 256 threads 16.2, and 17.7 when
+// each takes four heads.  8 sequences: 3.2 us, launches and that chain.)  k_clear_status, which overlaps it, makes room for what any CTA finds wrong (one CTA that looks at all paths takes 50 us for 512 of them).
+constexpr int CP_THREADS = 128;
 
 // whether the path of sequence b can be walked
 __device__ __forceinline__ bool path_ok(const CommitArgs &a, int b, int n, int len) {
@@ -200,17 +212,16 @@ __device__ __noinline__ void report(const CommitArgs &a, int code) {
 
 template <int D>
 __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constant__ CommitArgs a) {
-    constexpr int CPR = D / 8, MOST = 2 * TREE_NODES * CPR / CP_THREADS;  // 16-byte pieces of a row, of a thread
+    constexpr int CPR = D / 8, U = 4;  // 16-byte pieces of a row, of a thread at a time
     __shared__ long long of[TREE_NODES], to[TREE_NODES];  // value offsets of the rows, -1: does not move
     __shared__ int slot_of[TREE_NODES];
     const int b = blockIdx.x / a.kv.hkv, h = blockIdx.x - b * a.kv.hkv;
-    const int n = a.n_accepted[b], len = a.kv.lens[b];
+    const int n = a.n_accepted[b], len = a.kv.lens[b], i = threadIdx.x;
     if (!path_ok(a, b, n, len)) {
-        if (h == 0 && threadIdx.x == 0) report(a, DEV_BAD_POSITION);
+        if (h == 0 && i == 0) report(a, DEV_BAD_POSITION);
         return pdl_wait();
     }
     if (n == 0) return pdl_wait();
-    const int i = threadIdx.x;
     bool bad = false, bad_page = false;
     if (i < n) {
         const int p = a.path[(long long)b * a.max_path + i], before = i ? a.path[(long long)b * a.max_path + i - 1] : -1;
@@ -230,35 +241,37 @@ __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constan
     }
     if (h == 0 && (bad || bad_page)) report(a, bad ? DEV_BAD_TREE : DEV_BAD_PAGE);
     if (__syncthreads_or(bad)) return pdl_wait();  // the sequence stays as it is
-    uint4 piece[MOST];
+    for (int x0 = i; x0 < n * 2 * CPR + i; x0 += U * CP_THREADS) {
+        uint4 piece[U];
 #pragma unroll
-    for (int j = 0; j < MOST; ++j) {
-        const int x = threadIdx.x + j * CP_THREADS, r = x / (2 * CPR), c = x % (2 * CPR);
-        if (r < n && of[r] >= 0) piece[j] = *reinterpret_cast<const uint4 *>((c < CPR ? a.kv.k : a.kv.v) + of[r] + (c % CPR) * 8);
+        for (int j = 0; j < U; ++j) {
+            const int x = x0 + j * CP_THREADS, r = x / (2 * CPR), c = x % (2 * CPR);
+            if (r < n && of[r] >= 0) piece[j] = *reinterpret_cast<const uint4 *>((c < CPR ? a.kv.k : a.kv.v) + of[r] + (c % CPR) * 8);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int x = x0 + j * CP_THREADS, r = x / (2 * CPR), c = x % (2 * CPR);
+            if (r < n && of[r] >= 0) *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(c < CPR ? a.kv.k : a.kv.v) + to[r] + (c % CPR) * 8) = piece[j];
+        }
     }
-    const long long row = ((long long)b * a.kv.hkv + h) * a.kv.cap;
+    const long long at = ((long long)b * a.kv.hkv + h) * a.kv.cap;
     float w = 0.f;
     int pos = 0;
     const bool moves = i < n && of[i] >= 0;
-    if (moves && a.kv.weights) w = a.kv.weights[row + slot_of[i]];
-    if (moves && a.kv.positions) pos = a.kv.positions[row + slot_of[i]];
+    if (moves && a.kv.weights) w = a.kv.weights[at + slot_of[i]];
+    if (moves && a.kv.positions) pos = a.kv.positions[at + slot_of[i]];
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < MOST; ++j) {
-        const int x = threadIdx.x + j * CP_THREADS, r = x / (2 * CPR), c = x % (2 * CPR);
-        if (r < n && of[r] >= 0)
-            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(c < CPR ? a.kv.k : a.kv.v) + to[r] + (c % CPR) * 8) = piece[j];
-    }
-    if (moves && a.kv.weights) a.kv.weights[row + len + i] = w;
-    if (moves && a.kv.positions) a.kv.positions[row + len + i] = pos;
+    if (moves && a.kv.weights) a.kv.weights[at + len + i] = w;
+    if (moves && a.kv.positions) a.kv.positions[at + len + i] = pos;
     pdl_wait();
 }
 
 }  // namespace
 
 cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st) {
-    // (512 sequences, 10000 pages taken, as many given back by the next call, 220000 rows: 196 us the two with one CTA, XX with eight;
-    // 8 sequences: YY and ZZ)
+    // (512 sequences, 10000 pages taken, as many given back by the next call, 220000 rows: 200 us the two calls with one CTA, 36 with eight;
+    // 8 sequences, few pages: 10.2 us the two with one CTA; 12.7 when that one is launched as a cluster)
     const bool many = a.max_new > AP_FEW || std::min<long long>(a.n_pages, (long long)a.B * a.max_pages) > AP_FEW;
     const cudaError_t e = launch_cluster(k_assign_pages, many ? AP_CLUSTER : 1, AP_THREADS, st, a);
     if (e != cudaSuccess) return e;

@@ -532,9 +532,12 @@ template <int D, bool FP16>
 cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     using L = PromptShape<D>;
     static_assert(L::SMEM + sizeof(PromptState<D>) <= 227 * 1024, "shared memory");
-    cudaError_t e = cudaFuncSetAttribute(k_prompt<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
-    // (an SM divides its memory into cache and shared one kernel's way at a time: without this the two do not share an SM)
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_prompt_store, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    static std::atomic<uint64_t> set{0};
+    const cudaError_t e = once_per_device(set, [] {
+        const cudaError_t x = cudaFuncSetAttribute(k_prompt<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
+        // (an SM divides its memory into cache and shared one kernel's way at a time: without this the two do not share an SM)
+        return x != cudaSuccess ? x : cudaFuncSetAttribute(k_prompt_store, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    });
     if (e != cudaSuccess) return e;
     int log_p = 0;
     while (log_p < 4 && a.group % (2 << log_p) == 0) ++log_p;

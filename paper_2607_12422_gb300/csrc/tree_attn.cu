@@ -287,6 +287,8 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const int tail0 = len / KEYS, si = sn % L::RING_SEGS;  // (the first block with nodes or places behind them)
                 const int *table = a.kv.table + (long long)b * a.kv.max_pages;
                 int t = seg.t;
+                if (tail0 * KEYS + lane < len + nodes)  // (a load each in turn later)
+                    asm volatile("prefetch.global.L1 [%0];" ::"l"(table + page_index(a.kv, min(tail0 * KEYS + 4 * lane, len + nodes - 1))));
                 if (box && t < min(tail0, seg.t_end)) {
                     int page = lane < pieces ? table[page_index(a.kv, t * KEYS + lane * box)] : 0;
 #pragma unroll 1
@@ -367,10 +369,9 @@ __global__ void __launch_bounds__(THREADS, 1)
                     }
                     __syncwarp();
 #pragma unroll 1
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 32 * e + lane, key = t * KEYS + r, pi = page_index(a.kv, key);
+                    for (int e = 0; 32 * e < hi; ++e) {
+                        const int r = 32 * e + lane, key = t * KEYS + r, pi = page_index(a.kv, key), page = key < len + nodes ? table[pi] : -1;
                         const bool cached = key < len, node = !cached && key < len + nodes;
-                        const int page = cached || node ? table[pi] : -1;
                         const bool real = (unsigned)page < (unsigned)a.kv.n_pages;
                         if ((cached || node) && !real) *(volatile int *)&S.bad_page = 1;
                         unsigned long long at = 0;
@@ -803,7 +804,8 @@ template <int D, bool FP16>
 cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     using L = TreeShape<D>;
     static_assert(L::SMEM + sizeof(TreeState<D>) + sizeof(TreeList) + 128 <= 227 * 1024, "shared memory");
-    const cudaError_t e = cudaFuncSetAttribute(k_tree<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM);
+    static std::atomic<uint64_t> set{0};
+    const cudaError_t e = once_per_device(set, [] { return cudaFuncSetAttribute(k_tree<D, FP16>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::SMEM); });
     if (e != cudaSuccess) return e;
     a.workers = std::min(gemm_ctas(), TREE_MAX_WORKERS);
     if (a.workers < 1) return cudaErrorInvalidDevice;

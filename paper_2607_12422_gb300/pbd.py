@@ -7,6 +7,7 @@ library is missing this module raises; there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import re
 from typing import Dict, List, NamedTuple, Optional, Sequence
@@ -512,6 +513,13 @@ class PagePool:
     page_table [batch, max_pages] int32, whose row b names in its first held[b] entries the pages of sequence b; held [batch],
     free [n_pages] and n_free [1] int32: a stack of the free pages.  Without the last three all pages are free."""
 
+    _TENSORS = ("page_table", "held", "free", "n_free")
+
+    def __setattr__(self, name, value):
+        if name in self._TENSORS and getattr(self, name, value) is not value:
+            _bad("PagePool", "%s is another tensor than the handle was made for" % name)
+        object.__setattr__(self, name, value)
+
     def __init__(self, page_table, page_size: int, n_pages: int, held=None, free=None, n_free=None):
         import torch
         who = "PagePool"
@@ -532,6 +540,8 @@ class PagePool:
             _check(who, name, t, page_table, shape, torch.int32)
         self.page_table, self.held, self.free, self.n_free = page_table, held, free, n_free
         self.batch, self.max_pages, self.page_size, self.n_pages, self.device = B, max_pages, page_size, n_pages, dev
+        self._sizes = (B, max_pages, page_size, n_pages)
+        self._pool = tuple(t.data_ptr() for t in (page_table, held, free, n_free))
 
 
 class AssignedPages(NamedTuple):
@@ -540,6 +550,7 @@ class AssignedPages(NamedTuple):
     positions: object  # [max_new] int32: its position, 0 there
 
 
+@functools.lru_cache(maxsize=None)
 def assign_pages_workspace_bytes(batch: int) -> int:
     return load().pbd_op_assign_pages_workspace_bytes(batch) if _int32(batch) else 0
 
@@ -570,11 +581,10 @@ def pbd_op_assign_pages(pool: PagePool, lens, n_new, max_new: int, out: Optional
         _check(who, "starts", out.starts, pool, (B + 1,), i32)
         _check(who, "slots", out.slots, pool, (max_new,), torch.int64)
         _check(who, "positions", out.positions, pool, (max_new,), i32)
-    ws = _scratch(who, workspace, L.pbd_op_assign_pages_workspace_bytes(B), dev)
+    ws = _scratch(who, workspace, assign_pages_workspace_bytes(B), dev)
     st = _stream(torch, dev)
-    s = L.pbd_op_assign_pages(B, pool.max_pages, pool.page_size, pool.n_pages, lens.data_ptr(), n_new.data_ptr(),
-                              pool.page_table.data_ptr(), pool.held.data_ptr(), pool.free.data_ptr(), pool.n_free.data_ptr(),
-                              max_new, out.starts.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(), ws.ptr, ws.nbytes, st)
+    s = L.pbd_op_assign_pages(*pool._sizes, lens.data_ptr(), n_new.data_ptr(), *pool._pool, max_new, out.starts.data_ptr(),
+                              out.slots.data_ptr(), out.positions.data_ptr(), ws.ptr, ws.nbytes, st)
     _raise_if(L, s)
     if sync:
         _raise_if(L, L.pbd_op_status(ws.ptr, st, None))
@@ -592,11 +602,15 @@ def _packed_rows(who, q, k, v, names):
         _bad(who, "there is no row")
     if not _int32(T, hq, hkv, D):
         _bad(who, "a size does not fit 32 bits")
-    _check(who, "q", q, q, (T, hq, D), None, True)
-    _check(who, names[0], k, q, (T, hkv, D), None, True)
-    _check(who, names[1], v, q, (T, hkv, D), None, True)
-    qs, ks = (q.stride(0), k.stride(0)) if T > 1 else (hq * D, hkv * D)
-    if T > 1 and v.stride(0) != ks:
+    q_at, k_at, v_at = q.stride(), k.stride(), v.stride()
+    shape = (T, hkv, D)
+    if not (k.shape == shape == v.shape and k.dtype == q.dtype == v.dtype and k.device == q.device == v.device and k_at[1:] == v_at[1:] == (D, 1) == q_at[1:]
+            and k_at[0] >= hkv * D <= v_at[0] and q_at[0] >= hq * D):  # (the usual case in one line)
+        _check(who, "q", q, q, (T, hq, D), None, True)
+        _check(who, names[0], k, q, shape, None, True)
+        _check(who, names[1], v, q, shape, None, True)
+    qs, ks = (q_at[0], k_at[0]) if T > 1 else (hq * D, hkv * D)
+    if T > 1 and v_at[0] != ks:
         _bad(who, "rows of %s and %s lie differently far apart" % names)
     return T, hq, hkv, D, qs, ks
 
@@ -614,6 +628,7 @@ def _packed_outputs(torch, who, q, out, lse, want_lse):
     return out, lse
 
 
+@functools.lru_cache(maxsize=4096)
 def prompt_attention_workspace_bytes(T: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
     sizes = (T, batch, n_q_heads, n_kv_heads, head_dim)
     return load().pbd_op_prompt_attention_workspace_bytes(*sizes) if _int32(*sizes) else 0
