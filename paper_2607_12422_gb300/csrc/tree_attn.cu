@@ -169,7 +169,7 @@ struct TreeState {
     using L = TreeShape<D>;
     // s_full, p_full: S and P of the first tile's place, of the second tile, and of the second place where one tile uses both.  (Each has one
     // party that arrives and one that waits, and they see all of its phases: who skips one takes an older one for it.)
-    uint64_t full[2][L::STAGES], empty[2][L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], tail[L::RING_SEGS], drain[2];
+    uint64_t full[2][L::STAGES], empty[2][L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], tail[L::RING_SEGS], notes_free[L::RING_SEGS], drain[2];
     uint32_t tmem;
     int abort, bad_page, bad_tree;
     float top[2][2][ROWS];              // what the two threads of a row tell each other
@@ -226,7 +226,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&S.p_full[i][0], 8);
             mbar_init(&S.p_full[i][1], 8);
         }
-        for (int i = 0; i < L::RING_SEGS; ++i) mbar_init(&S.tail[i], 1);
+        for (int i = 0; i < L::RING_SEGS; ++i) {
+            mbar_init(&S.tail[i], 1);
+            mbar_init(&S.notes_free[i], ROW_WARPS);
+        }
         S.abort = S.bad_page = S.bad_tree = 0;
         fence_mbarrier_init();
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (k_tree_join reports; a wait runs out a second later)
@@ -355,7 +358,10 @@ __global__ void __launch_bounds__(THREADS, 1)
                     arrive(&S.full[kv][pend]);
                     pend = -1;
                 };
-                if (kv && seg.t_end > tail0) {  // nobody looks at this segment's notes yet
+                if (kv && seg.t_end > tail0) {
+                    // all rows are through with the notes that were here (with units of one tile the second tile's may be far behind)
+                    if (sn >= L::RING_SEGS)
+                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_free[si], (sn / L::RING_SEGS - 1) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
                     for (int d = lane; d < D; d += 32) S.odd_nodes[si][d] = 0;
                     if (lane == 0) S.odd[si] = 0;
                 }
@@ -698,7 +704,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbarrier_arrive_one(&S.o_free[i]);
+            if (lane == 0) {
+                mbarrier_arrive_one(&S.o_free[i]);
+                mbarrier_arrive_many(&S.notes_free[si], two ? 1 : 2);
+            }
         }
     }
     tc_fence_before();
