@@ -12,9 +12,10 @@
 //
 // Warps 0-15: rows (queries, softmax, outputs).  Warp 16 copies K, warp 17 V: tiled copies of the rows that a page has in a piece where
 // pages hold a multiple of 8, row by row else, 16 bytes a lane.  Warps 18 and 19: the tiles' MMAs.
-// The blocks with nodes among their keys, a (sequence, KV head)'s last one or two, are copied row by row and waited for by those
-// who copy: they store the nodes' rows into the cache, and look for infinite and NaN values of V, which would be NaN in rows that do not
-// see them (0 x NaN): such values of nodes become zero, and who they were is noted for each dimension.  (Cached rows are seen by all.)
+// The blocks with nodes among their keys, a (sequence, KV head)'s last one or two, are copied row by row.  The rows' warps, of the second tile
+// where a unit has one, store the nodes' rows into the cache and look for infinite and NaN values of V, which would be NaN in rows that
+// do not see them (0 x NaN): who has one is noted for each dimension, and the warp that copies V makes such values zero before they are
+// multiplied.  (Cached rows are seen by all.)  When the two warps that copy did all of this, eight trees of up to 64 nodes took 31.8 us, now 24.8.
 #include <algorithm>
 
 #include "flash.cuh"
@@ -26,8 +27,14 @@ using namespace flash;
 
 namespace {
 
-constexpr int TA_ROW = 2;        // what beginning and ending a (sequence, KV head) costs a CTA, in blocks
-constexpr int TA_MIN = 3;        // places of a CTA's stretch at least
+// Costs in places: of a block of a unit of one tile, of two, and of a unit besides.  Heads of 64: by the rows' work (1.0 and 1.5 us; 5 us); else
+// memory bounds both (1.5 us; 6 us).  (64 sequences of 1 to 26 nodes, seven heads a KV head, us: 92 with two blocks for a unit and one cost
+// for both, 83 with 8 places for a unit, 76 with 10, 79 with 18.  Eight of up to 64 nodes, heads of 128: 26.5 with 2, 24.9 with 4, 25.2 with 6.)
+template <int D>
+struct Cost {
+    static constexpr int ONE = D == 64 ? 2 : 1, TWO = D == 64 ? 3 : 1, ROW = D == 64 ? 10 : 4;
+};
+constexpr int TA_MIN = 3;        // places of a CTA's stretch at least (17 nodes behind 512 slots: 15.8 us, with 6 18.1)
 constexpr int TA_MASKS = 8;      // blocks whose masks are kept
 
 template <int D>
@@ -39,7 +46,7 @@ struct TreeShape : Shape<D> {
     static constexpr int SMEM = S::TILES * S::QT + 2 * STAGES * S::UNIT + 1024;
 };
 
-// Counts of the list: a (sequence, KV head, chunk of rows) is a unit; it has its blocks and TA_ROW places more in front.
+// Counts of the list: a (sequence, KV head, chunk of rows) is a unit; it has places in front, and some for each block.
 struct TreeList {
     int first[KV_MAX_BATCH + 1];  // places before sequence b
     int len[KV_MAX_BATCH], nodes[KV_MAX_BATCH];
@@ -52,6 +59,9 @@ __device__ __forceinline__ bool tree_ok(const PackedArgs &a, int b) {
 __device__ __forceinline__ int blocks_of(int len, int nodes) { return (len + nodes + KEYS - 1) / KEYS; }
 template <int D>
 __device__ __forceinline__ int chunks_of(int rows) { return (rows + TreeShape<D>::ROWS_ALL - 1) / TreeShape<D>::ROWS_ALL; }
+// of a block of such a sequence's units (the last of several may be of one tile)
+template <int D>
+__device__ __forceinline__ int cost_of(int rows) { return TreeShape<D>::TILES == 2 && rows > ROWS ? Cost<D>::TWO : Cost<D>::ONE; }
 
 // Whole CTA; returns the list's length.  (Up to 32 sequences are one warp's: what comes before the first copy is what a small call waits for.)
 template <int D>
@@ -63,7 +73,7 @@ __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
         const bool ok = s >= 0 && e >= s && e <= a.T && e - s <= TREE_NODES && l >= 0 && l + (long long)(e - s) <= a.kv.cap;
         const int n = ok ? e - s : 0, len = ok ? l : 0;
         T.len[b] = len, T.nodes[b] = n;
-        return n > 0 ? a.hkv * chunks_of<D>(n * a.group) * (blocks_of(len, n) + TA_ROW) : 0;
+        return n > 0 ? a.hkv * chunks_of<D>(n * a.group) * (blocks_of(len, n) * cost_of<D>(n * a.group) + Cost<D>::ROW) : 0;
     };
     auto scan = [&](int x) {
 #pragma unroll
@@ -102,7 +112,7 @@ __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
 struct Shares {
     int workers, each, more;  // places of a CTA; CTAs with one more
     __device__ __forceinline__ Shares(const PackedArgs &a, int count) {
-        workers = max(1, min(a.workers, (count + TA_MIN - 1) / TA_MIN));
+        workers = max(1, min(a.workers, count / TA_MIN));  // (so that one in the middle of a unit has a block)
         each = count / workers;
         more = count - each * workers;
     }
@@ -115,17 +125,22 @@ struct Shares {
 
 // Blocks [t, t_end) of one unit: what a CTA works on before it leaves the unit.
 struct Segment {
-    int b, unit, units, t, t_end, blocks;  // sequence, unit of it, its units, blocks, the unit's blocks
+    int b, unit, units, t, t_end, blocks, cost;  // sequence, unit of it, its units, blocks, the unit's blocks, places of one
     int at, end;                           // list place of the unit, end of the stretch
     int chunks;
     template <int D>
     __device__ __forceinline__ void enter(const PackedArgs &a, const TreeList &T) {
         blocks = blocks_of(T.len[b], T.nodes[b]);
         chunks = chunks_of<D>(T.nodes[b] * a.group);
+        cost = cost_of<D>(T.nodes[b] * a.group);
         units = a.hkv * chunks;
     }
+    // the block that has place x of the unit or is the first behind it: a block belongs to whom its first place does
+    template <int D>
+    __device__ __forceinline__ int block_at(int x) const { return max(x - Cost<D>::ROW + cost - 1, 0) / cost; }
+    template <int D>
     __device__ __forceinline__ bool clip() {
-        t_end = min(blocks, end - at - TA_ROW);
+        t_end = min(blocks, block_at<D>(end - at));
         return t < t_end;
     }
     // The first segment of the stretch [u, u_end); false if it has none.
@@ -143,15 +158,15 @@ struct Segment {
         }
         b = lo;
         enter<D>(a, T);
-        const int per = blocks + TA_ROW;
+        const int per = blocks * cost + Cost<D>::ROW;
         unit = (u - T.first[b]) / per;
         at = T.first[b] + unit * per;
-        t = max(0, u - at - TA_ROW);
-        return clip() || next<D>(a, T);
+        t = block_at<D>(u - at);
+        return clip<D>() || next<D>(a, T);
     }
     template <int D>
     __device__ __forceinline__ bool next(const PackedArgs &a, const TreeList &T) {
-        at += blocks + TA_ROW;
+        at += blocks * cost + Cost<D>::ROW;
         t = 0;
         if (++unit == units) {
             unit = 0;
@@ -160,7 +175,7 @@ struct Segment {
             if (b >= a.B || at >= end) return false;
             enter<D>(a, T);
         }
-        return at < end && clip();  // (where only a unit's front is left the stretch is over)
+        return at < end && clip<D>();  // (where only a unit's front is left the stretch is over)
     }
 };
 
@@ -169,14 +184,15 @@ struct TreeState {
     using L = TreeShape<D>;
     // s_full, p_full: S and P of the first tile's place, of the second tile, and of the second place where one tile uses both.  (Each has one
     // party that arrives and one that waits, and they see all of its phases: who skips one takes an older one for it.)
-    uint64_t full[2][L::STAGES], empty[2][L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], tail[L::RING_SEGS], notes_free[L::RING_SEGS], drain[2];
+    uint64_t full[2][L::STAGES], empty[2][L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], drain[2];
+    uint64_t notes_ready[L::RING_SEGS], notes_made[L::RING_SEGS], notes_free[L::RING_SEGS];
     uint32_t tmem;
     int abort, bad_page, bad_tree;
     float top[2][2][ROWS];              // what the two threads of a row tell each other
     Segment row_seg[ROW_WARPS];         // where each of the rows' warps is (to spare registers)
     alignas(8) uint32_t valid[TA_MASKS][4];  // keys of a block whose pages are in the cache
     unsigned long long rows[2][KEYS];  // where a block's rows of K, and of V, come from; of pieces: the map's coordinates
-    // of a segment: nodes with infinite or NaN values, in each dimension
+    // of a segment: whether there are, and which nodes have infinite or NaN values, in each dimension
     int odd[L::RING_SEGS];
     unsigned long long odd_nodes[L::RING_SEGS][D];
 };
@@ -227,13 +243,16 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&S.p_full[i][1], 8);
         }
         for (int i = 0; i < L::RING_SEGS; ++i) {
-            mbar_init(&S.tail[i], 1);
+            mbar_init(&S.notes_ready[i], 1);
+            mbar_init(&S.notes_made[i], ROW_WARPS);
             mbar_init(&S.notes_free[i], ROW_WARPS);
+            S.odd[i] = 0;
         }
         S.abort = S.bad_page = S.bad_tree = 0;
         fence_mbarrier_init();
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (k_tree_join reports; a wait runs out a second later)
     }
+    for (int x = threadIdx.x; x < L::RING_SEGS * D; x += THREADS) (&S.odd_nodes[0][0])[x] = 0;
     if (threadIdx.x == 32 && box) {
         prefetch_tensormap(&kmap);
         prefetch_tensormap(&vmap);
@@ -292,6 +311,18 @@ __global__ void __launch_bounds__(THREADS, 1)
                 int t = seg.t;
                 if (tail0 * KEYS + lane < len + nodes)  // (a load each in turn later)
                     asm volatile("prefetch.global.L1 [%0];" ::"l"(table + page_index(a.kv, min(tail0 * KEYS + 4 * lane, len + nodes - 1))));
+                if (kv && seg.t_end > tail0) {
+                    // room for this segment's notes: all rows are through with those that were there.  (Said before the first copy: rows wait for it.)
+                    if (sn >= L::RING_SEGS)
+                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_free[si], (sn / L::RING_SEGS - 1) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
+                    if (ok && S.odd[si]) {
+                        __syncwarp();
+                        for (int d = lane; d < D; d += 32) S.odd_nodes[si][d] = 0;
+                        if (lane == 0) S.odd[si] = 0;
+                    }
+                    __syncwarp();
+                    if (ok && lane == 0) mbarrier_arrive_one(&S.notes_ready[si]);
+                }
                 if (box && t < min(tail0, seg.t_end)) {
                     int page = lane < pieces ? table[page_index(a.kv, t * KEYS + lane * box)] : 0;
 #pragma unroll 1
@@ -325,46 +356,32 @@ __global__ void __launch_bounds__(THREADS, 1)
                     }
                 }
                 // Blocks with nodes, and all where pages hold no multiple of 8.  Rows behind `hi` are not multiplied.
-                const bool store = seg.unit % seg.chunks == 0;
                 const int start = a.starts[b];
                 auto row_hi = [&](int t) { return min(((len + nodes + 15) & ~15) - t * KEYS, KEYS); };
-                // Nodes' rows of the last unit that was copied: they go to the cache, and V's are looked at.
+                // The last unit that was copied.  V: once the rows have looked at the nodes' values, of which some become zero.
                 auto finish = [&]() {
-                    const uint32_t to = smem_u32(units + pend * L::UNIT);
-                    const int k0 = pend_t * KEYS, d0 = pend_u * L::DU + piece * 8, hi = row_hi(pend_t);
+                    if (kv) {
+                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_made[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
+                        if (*(volatile int *)&S.odd[si]) {
+                            const uint32_t to = smem_u32(units + pend * L::UNIT);
+                            const int k0 = pend_t * KEYS;
 #pragma unroll 1
-                    for (int r = max(len - k0, 0) / RPI * RPI + r_lane; r < hi; r += RPI) {  // (each lane its own pieces)
-                        const int key = k0 + r, i = key - len;
-                        if (i < 0 || rows[r] == 0) continue;
-                        const uint4 v = ld_shared_u4(to + Y::at(r, piece));
-                        if (store) {
-                            const int pi = page_index(a.kv, key);
-                            const long long dst = table[pi] * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot + d0;
-                            *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(kv ? a.kv.v : a.kv.k) + dst) = v;
-                        }
-                        if (kv == 0 || !(odd_halves<FP16>(v.x) | odd_halves<FP16>(v.y) | odd_halves<FP16>(v.z) | odd_halves<FP16>(v.w))) continue;
+                            for (int r = max(len - k0, 0) / RPI * RPI + r_lane; r < row_hi(pend_t); r += RPI) {  // (each lane its own pieces)
+                                if (k0 + r < len) continue;
 #pragma unroll 1
-                        for (int e = 0; e < 8; ++e) {  // (value by value: this is rare)
-                            const uint32_t at = to + Y::at(r, piece) + 2 * e;
-                            uint16_t y;
-                            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at) : "memory");
-                            if (!odd_halves<FP16>(y)) continue;
-                            asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((uint16_t)0) : "memory");
-                            atomicOr(&S.odd_nodes[si][d0 + e], 1ull << i);
-                            S.odd[si] = 1;
+                                for (int e = 0; e < 8; ++e) {  // (value by value: this is rare)
+                                    const uint32_t at = to + Y::at(r, piece) + 2 * e;
+                                    uint16_t y;
+                                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at) : "memory");
+                                    if (odd_halves<FP16>(y)) asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((uint16_t)0) : "memory");
+                                }
+                            }
                         }
                     }
                     fence_proxy_async_shared();
                     arrive(&S.full[kv][pend]);
                     pend = -1;
                 };
-                if (kv && seg.t_end > tail0) {
-                    // all rows are through with the notes that were here (with units of one tile the second tile's may be far behind)
-                    if (sn >= L::RING_SEGS)
-                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_free[si], (sn / L::RING_SEGS - 1) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
-                    for (int d = lane; d < D; d += 32) S.odd_nodes[si][d] = 0;
-                    if (lane == 0) S.odd[si] = 0;
-                }
 #pragma unroll 1
                 for (; ok && t < seg.t_end; ++t) {
                     const bool tail = t >= tail0;
@@ -374,9 +391,12 @@ __global__ void __launch_bounds__(THREADS, 1)
                         finish();
                     }
                     __syncwarp();
+                    auto page_of = [&](int key) { return key < len + nodes ? table[page_index(a.kv, key)] : -1; };
+                    int next_page = page_of(t * KEYS + lane);
 #pragma unroll 1
                     for (int e = 0; 32 * e < hi; ++e) {
-                        const int r = 32 * e + lane, key = t * KEYS + r, pi = page_index(a.kv, key), page = key < len + nodes ? table[pi] : -1;
+                        const int r = 32 * e + lane, key = t * KEYS + r, pi = page_index(a.kv, key), page = next_page;
+                        next_page = page_of(key + 32);
                         const bool cached = key < len, node = !cached && key < len + nodes;
                         const bool real = (unsigned)page < (unsigned)a.kv.n_pages;
                         if ((cached || node) && !real) *(volatile int *)&S.bad_page = 1;
@@ -384,15 +404,13 @@ __global__ void __launch_bounds__(THREADS, 1)
                         if (r < lo) {
                             at = packed(page, h, key);
                         } else if (real) {
-                            const uint16_t *from = cached ? (kv ? a.kv.v : a.kv.k) + page * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot
-                                                          : (kv ? a.v : a.k) + (long long)(start + key - len) * a.kv_stride + h * D;
+                            const long long slot = page * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot;
+                            const uint16_t *from = cached ? (kv ? a.kv.v : a.kv.k) + slot : (kv ? a.v : a.k) + (long long)(start + key - len) * a.kv_stride + h * D;
                             at = reinterpret_cast<unsigned long long>(from);
                         }
                         rows[r] = at;
                         const unsigned valid = __ballot_sync(0xffffffffu, real);
                         if (kv == 0 && lane == 0) *(volatile uint32_t *)&S.valid[(block + t - seg.t) % TA_MASKS][e] = valid;
-                        if (kv == 0 && node && a.new_pos && a.kv.positions && real && store)
-                            a.kv.positions[((long long)b * a.hkv + h) * a.kv.cap + key] = a.new_pos[start + key - len];
                     }
                     __syncwarp();
 #pragma unroll 1
@@ -438,10 +456,6 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (ok && pend >= 0) {
                     cp_async_wait_all();
                     finish();
-                }
-                if (kv && seg.t_end > tail0) {  // (only a stretch's last segment has no such block)
-                    __syncwarp();
-                    if (ok && lane == 0) mbarrier_arrive_one(&S.tail[si]);
                 }
                 block += seg.t_end - seg.t;
                 more = seg.next<D>(a, T);
@@ -565,65 +579,96 @@ __global__ void __launch_bounds__(THREADS, 1)
             const bool two = TILES == 2 && n_rows > ROWS, whole = nb == g->blocks, ends = g->t_end > T.len[b] / KEYS;  // (ends: nodes among its keys)
             const int pos = block;
             block += nb;
-            if (i && !two) continue;  // (nothing for the second tile)
+            const bool idle = i && !two;  // the second tile's rows of a unit of one
             auto release = [&](int kv, int j) {  // K or V of a block is not needed any more
                 if (w == 0 && half == 0 && lane == 0)
                     for (int u = 0; u < UNITS; ++u) mbarrier_arrive_many(&S.empty[kv][((pos + j) * UNITS + u) % STAGES], two ? 1 : 2);
             };
             const bool real = place_row < n_rows;
             const int node = real ? (place_row + first_row) / a.group : 0;
-            {  // the queries (the tile's last MMAs are done); a row's two warps share its pieces
-                constexpr int CPH = D / 16, RPI = 32 / CPH;
-                const int piece = half * CPH + lane % CPH;
-                const uint32_t mine = smem_u32(sq + i * L::QT) + (piece >> 3) * SUB + w * 32 * 128;
-                const int head = g->unit / g->chunks * a.group + place_row + first_row - node * a.group;
-                const long long q_off = real ? (long long)(a.starts[b] + node) * a.q_stride + head * D : -1;
-#pragma unroll 4
-                for (int x = 0; x < 32; x += RPI) {
-                    const int rr = x + lane / CPH;
-                    const long long off = __shfl_sync(0xffffffffu, q_off, rr);
-                    cp_async16_or_zero(mine + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), off >= 0 ? a.q + off + piece * 8 : a.q, off >= 0);
-                }
-                cp_async_commit();
-            }
-            // ancestors: lane x holds nodes x and x + 32
             uint64_t anc = 0;
-            if (ends) {
-                int p[2];
-                uint64_t m[2];
-                bool bad = false;
+            if (!idle) {
+                int p[2];  // ancestors: lane x holds nodes x and x + 32
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int x = lane + 32 * e;
-                    p[e] = -1;
-                    if (x < T.nodes[b]) {
-                        p[e] = a.parents ? a.parents[a.starts[b] + x] : x - 1;
-                        if (p[e] < -1 || p[e] >= x) bad = true, p[e] = -1;
-                    }
-                    m[e] = 1ull << x;
+                    p[e] = ends && x < T.nodes[b] ? (a.parents ? a.parents[a.starts[b] + x] : x - 1) : -1;
                 }
-                if (__any_sync(0xffffffffu, bad) && lane == 0) *(volatile int *)&S.bad_tree = 1;
-#pragma unroll 1
-                for (int step = 0; step < 6; ++step) {  // whole paths twice as long each time
-                    uint64_t up[2];
-                    int pp[2];
+                {  // the queries (the tile's last MMAs are done); a row's two warps share its pieces
+                    constexpr int CPH = D / 16, RPI = 32 / CPH;
+                    const int piece = half * CPH + lane % CPH;
+                    const uint32_t mine = smem_u32(sq + i * L::QT) + (piece >> 3) * SUB + w * 32 * 128;
+                    const int head = g->unit / g->chunks * a.group + place_row + first_row - node * a.group;
+                    const long long q_off = real ? (long long)(a.starts[b] + node) * a.q_stride + head * D : -1;
+#pragma unroll 4
+                    for (int x = 0; x < 32; x += RPI) {
+                        const int rr = x + lane / CPH;
+                        const long long off = __shfl_sync(0xffffffffu, q_off, rr);
+                        cp_async16_or_zero(mine + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), off >= 0 ? a.q + off + piece * 8 : a.q, off >= 0);
+                    }
+                    cp_async_commit();
+                }
+                if (ends) {
+                    uint64_t m[2];
+                    bool bad = false;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const uint64_t lo = __shfl_sync(0xffffffffu, m[0], p[e] & 31), hi = __shfl_sync(0xffffffffu, m[1], p[e] & 31);
-                        const int plo = __shfl_sync(0xffffffffu, p[0], p[e] & 31), phi = __shfl_sync(0xffffffffu, p[1], p[e] & 31);
-                        up[e] = p[e] < 0 ? 0 : p[e] < 32 ? lo : hi;
-                        pp[e] = p[e] < 0 ? -1 : p[e] < 32 ? plo : phi;
+                        const int x = lane + 32 * e;
+                        if (p[e] < -1 || p[e] >= x) bad = true, p[e] = -1;
+                        m[e] = 1ull << x;
                     }
+                    if (__any_sync(0xffffffffu, bad) && lane == 0) *(volatile int *)&S.bad_tree = 1;
+#pragma unroll 1
+                    for (int step = 0; step < 6; ++step) {  // whole paths twice as long each time
+                        uint64_t up[2];
+                        int pp[2];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) m[e] |= up[e], p[e] = pp[e];
+                        for (int e = 0; e < 2; ++e) {
+                            const uint64_t lo = __shfl_sync(0xffffffffu, m[0], p[e] & 31), hi = __shfl_sync(0xffffffffu, m[1], p[e] & 31);
+                            const int plo = __shfl_sync(0xffffffffu, p[0], p[e] & 31), phi = __shfl_sync(0xffffffffu, p[1], p[e] & 31);
+                            up[e] = p[e] < 0 ? 0 : p[e] < 32 ? lo : hi;
+                            pp[e] = p[e] < 0 ? -1 : p[e] < 32 ? plo : phi;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) m[e] |= up[e], p[e] = pp[e];
+                    }
+                    const uint64_t lo = __shfl_sync(0xffffffffu, m[0], node & 31), hi = __shfl_sync(0xffffffffu, m[1], node & 31);
+                    anc = node < 32 ? lo : hi;
                 }
-                const uint64_t lo = __shfl_sync(0xffffffffu, m[0], node & 31), hi = __shfl_sync(0xffffffffu, m[1], node & 31);
-                anc = node < 32 ? lo : hi;
+                cp_async_wait_all();
+                fence_proxy_async_shared();
+                __syncwarp();
+                if (lane == 0) mbarrier_arrive_one(&S.q_full[i]);
             }
-            cp_async_wait_all();
-            fence_proxy_async_shared();
-            __syncwarp();
-            if (lane == 0) mbarrier_arrive_one(&S.q_full[i]);
+            if (ends && (two || i)) {  // the nodes' K and V go to the cache, and V is looked at: by rows that have nothing else to do, if there are
+                constexpr int CPR = D / 8;
+                const int si = sn % L::RING_SEGS;
+                const bool room = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_ready[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
+                const int h = g->unit / g->chunks, start = a.starts[b], len = T.len[b], first = two ? 0 : ROW_WARPS * 16;
+                const int from = max(g->t * KEYS - len, 0), to = min(T.nodes[b], g->t_end * KEYS - len);  // (of this stretch's blocks)
+#pragma unroll 1
+                for (int x = threadIdx.x - first; room && x < (to - from) * CPR; x += ROW_WARPS * 32 - first) {
+                    const int n = from + x / CPR, p = x % CPR, key = len + n, pi = page_index(a.kv, key);
+                    const long long src = (long long)(start + n) * a.kv_stride + h * D + p * 8;
+                    const uint4 k = *reinterpret_cast<const uint4 *>(a.k + src), v = *reinterpret_cast<const uint4 *>(a.v + src);
+                    const int page = a.kv.table[(long long)b * a.kv.max_pages + pi];
+                    if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
+                    if (first_row == 0) {
+                        const long long dst = page * a.kv.stride_page + h * a.kv.stride_head + (key - pi * a.kv.page_size) * a.kv.stride_slot + p * 8;
+                        *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.k) + dst) = k;
+                        *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.v) + dst) = v;
+                        if (p == 0 && a.new_pos && a.kv.positions) a.kv.positions[((long long)b * a.hkv + h) * a.kv.cap + key] = a.new_pos[start + n];
+                    }
+                    if (!(odd_halves<FP16>(v.x) | odd_halves<FP16>(v.y) | odd_halves<FP16>(v.z) | odd_halves<FP16>(v.w))) continue;
+#pragma unroll 1
+                    for (int e = 0; e < 8; ++e)  // (value by value: this is rare)
+                        if (odd_halves<FP16>(a.v[src + e])) atomicOr(&S.odd_nodes[si][p * 8 + e], 1ull << n);
+                    *(volatile int *)&S.odd[si] = 1;
+                }
+                __syncwarp();
+                if (room && lane == 0) mbarrier_arrive_many(&S.notes_made[si], two ? 1 : 2);
+            }
+            if (idle) continue;
             for (int j = 0; ok && j < nb; ++j) {
                 const int buf = two ? i : j & 1, bar = two ? i : 2 * buf, phase = two ? cnt + j : (buf ? cnt2 : cnt) + (j >> 1);
                 bool there = mbar_wait_short(&S.s_full[bar], phase & 1, a.status, DEV_TIMEOUT_MMA, &S.abort), o_waited = two || j == 0;
@@ -664,10 +709,10 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             cnt += two ? nb : (nb + 1) / 2;
             if (!two) cnt2 += nb / 2;
-            const int si = sn % L::RING_SEGS;
             o_phase += two ? 1 : nb;
+            const int si = sn % L::RING_SEGS;
             bool there = mbar_wait_short(&S.o_done[i], (o_phase - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-            if (there && ends) there = mbar_wait_short(&S.tail[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+            if (there && ends) there = mbar_wait_short(&S.notes_made[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort);
             release(1, nb - 1);
             if (!ok || pair_any(id, !there)) break;
             top[half * ROWS + w * 32 + lane] = r.l;
@@ -750,9 +795,9 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
         const int row0 = y / (D / 32) * TJ_ROWS, d4 = y % (D / 32) * 8 + ld, n_rows = T.nodes[b] * a.group;
         if (row0 >= n_rows) continue;
         const int chunk = row0 / L::ROWS_ALL, pr = min(row0 + lr, n_rows - 1) - chunk * L::ROWS_ALL;  // (a chunk is a multiple of four rows)
-        const int per = blocks_of(T.len[b], T.nodes[b]) + TA_ROW;
+        const int cost = cost_of<D>(n_rows), blocks = blocks_of(T.len[b], T.nodes[b]), per = blocks * cost + Cost<D>::ROW;
         const int at = T.first[b] + (h * chunks_of<D>(n_rows) + chunk) * per;
-        const int w0 = shares.owner(at + TA_ROW), w1 = shares.owner(at + per - 1);
+        const int w0 = shares.owner(at + Cost<D>::ROW), w1 = shares.owner(at + per - cost);
         if (w0 == w1) continue;  // one CTA had all blocks
         auto part = [&](int w) { return (long long)w * 2 + (w == w0); };
         auto max_sum = [&](int w) { return w <= w1 ? a.part_ml[part(w) * a.part_rows + pr] : make_float2(-INFINITY, 0.f); };
@@ -835,7 +880,8 @@ bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p) {
     // (places of the list are counted in 32 bits)
     const int most = rows_all(kv.d), group = hq / kv.hkv;
     const double units = (double)kv.B * kv.hkv * ((TREE_NODES * group + most - 1) / most);
-    if (units * (double)((kv.cap + KEYS - 1) / KEYS + TA_ROW) >= 2147483647.0) return false;
+    const int cost = kv.d == 64 ? Cost<64>::TWO : Cost<128>::TWO, row = kv.d == 64 ? Cost<64>::ROW : Cost<128>::ROW;
+    if (units * ((double)((kv.cap + KEYS - 1) / KEYS) * cost + row) >= 2147483647.0) return false;
     p->rows = std::min({most, TREE_NODES * group, std::min(T, 1 << 16) * group});
     size_t at = 1024;
     auto take = [&](size_t bytes) {
