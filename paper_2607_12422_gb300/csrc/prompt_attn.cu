@@ -4,9 +4,9 @@
 //     s_ij = q_i . k_j (j <= i),  p_ij = exp(scale (s_ij - max_j s_ij)),  l_i = sum_j p_ij,  out_i = sum_j p_ij v_j / l_i
 // in one pass over the keys (flash.cuh).  The tensor core bounds it: 4 D operations a (row, key).
 //
-// A tile's 128 rows are 128 / P tokens of P heads of one KV head, P the power of two in the group (16 at most), so that
-// tiles waste no rows and a block of K and V serves the whole group.  A CTA takes two tiles, of consecutive tokens (heads of 256: one), over
-// blocks of 128 keys up to its last token.
+// A tile's 128 rows are 128 / P tokens of P heads of one KV head, P a divisor of the group for which few rows are left over, so that
+// a block of K and V serves the whole group and short sequences fill tiles.  A CTA takes two tiles, of consecutive tokens (heads of 256: one),
+// over blocks of 128 keys up to its last token.
 //
 // Each CTA works on a list of such items, with its tensor core on the next one's first blocks while the rows of one leave.
 //
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid
 template <int D, bool FP16>
 __global__ void __launch_bounds__(THREADS, 1)
     k_prompt(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-             const __grid_constant__ PackedArgs a, int log_p) {
+             const __grid_constant__ PackedArgs a, int P, uint32_t inv_p) {
     using L = PromptShape<D>;
     constexpr int TILES = L::TILES, UNITS = L::UNITS, STAGES = L::STAGES, AHEAD = L::AHEAD;
     constexpr bool TWO = TILES == 2;
@@ -158,8 +158,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     uint8_t *ring = sq + TILES * L::QT;
     __shared__ PromptState<D> S;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int P = 1 << log_p, tile_tokens = ROWS >> log_p, tokens = TILES * tile_tokens;
-    const int chunks = a.group >> log_p, heads = a.hkv * chunks;
+    const int tile_tokens = ROWS * inv_p >> 16, tokens = TILES * tile_tokens;  // (inv_p: 1 / P in 16 bits, exact for what it is used for)
+    const int chunks = a.group * inv_p >> 16, heads = a.hkv * chunks;
     if (warp == 16) tmem_alloc(&S.tmem, TM_COLS);
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
@@ -189,6 +189,10 @@ __global__ void __launch_bounds__(THREADS, 1)
         fence_mbarrier_init();
     }
     __syncthreads();
+    // rows of no token stay zero
+    for (int x = tile_tokens * P * 8 + threadIdx.x; x < ROWS * 8; x += THREADS)
+        for (int c = 0; c < TILES * (D / 64); ++c) st_shared_u4(smem_u32(sq) + c * SUB + x * 16, make_uint4(0, 0, 0, 0));
+    fence_proxy_async_shared();
     if (threadIdx.x == 32) {
         prefetch_tensormap(&qmap);
         prefetch_tensormap(&kmap);
@@ -224,7 +228,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     mbarrier_arrive_one(&S.item_free[s]);
                     const int nmax = max(it.nb[0], it.nb[1]);
                     if (n > 0 && !mbar_wait_short(&S.q_free, (n - 1) & 1, a.status, DEV_TIMEOUT_SLOT, &S.abort)) break;
-                    mbar_arrive_expect_tx(&S.q_full, (uint32_t)(TILES * L::QT));
+                    mbar_arrive_expect_tx(&S.q_full, (uint32_t)(TILES * (D / 64) * 128 * tile_tokens * P));
                     for (int i = 0; i < TILES; ++i)
                         for (int c = 0; c < D / 64; ++c)
                             tma_load_4d(sq + i * L::QT + c * SUB, &qmap, c * 64, 0, it.h * chunks + it.ch, it.start + it.q0 + i * tile_tokens, &S.q_full);
@@ -472,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 for (int x = 0; x < 64; x += 32) tmem_ld_32cols(ts + buf * KEYS + x, *reinterpret_cast<uint32_t(*)[32]>(&s[x]));
                 tmem_ld_wait();
                 if (j * KEYS + KEYS - 1 > first) {
-                    const int last = first + (row >> log_p) - j * KEYS - 64 * half;
+                    const int last = first + (int)(row * inv_p >> 16) - j * KEYS - 64 * half;
 #pragma unroll
                     for (int x = 0; x < 64; ++x)
                         if (x > last) s[x] = __float_as_uint(-INFINITY);
@@ -502,8 +506,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             pair_sync(id);
             r.l += top[(half ^ 1) * ROWS + row];
             tc_fence_after();
-            const int head = it.h * a.group + it.ch * P + (row & (P - 1)), token = first + (row >> log_p);
-            const bool real = token < it.len;
+            const int place = row * inv_p >> 16, head = it.h * a.group + it.ch * P + row - place * P, token = first + place;
+            const bool real = token < it.len && place < tile_tokens;
             const long long out_row = (long long)(it.start + token) * a.hq + head;
             const bool odd = store_half<D, FP16>(to, row_factor(r), a.out + out_row * D + half * (D / 2), real, wide, careful,
                                                  [&](int d) { return S.first_odd[s][half * (D / 2) + d] <= token; });
@@ -539,9 +543,12 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
         return x != cudaSuccess ? x : cudaFuncSetAttribute(k_prompt_store, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     });
     if (e != cudaSuccess) return e;
-    int log_p = 0;
-    while (log_p < 4 && a.group % (2 << log_p) == 0) ++log_p;
-    const int P = 1 << log_p, tokens = L::TILES * (ROWS / P), heads = a.hq / P;
+    // the largest divisor of the group up to 16 that leaves at most 8 rows over.  (32 ragged prompts, groups of seven: 95 us with
+    // 7 heads a tile, 107 with one.)
+    int P = std::min(a.group, 16);
+    while (a.group % P || ROWS % P > 8) --P;
+    const uint32_t inv_p = 65536 / P + 1;
+    const int tokens = L::TILES * (ROWS / P), heads = a.hq / P;
     const long long items = std::min<long long>(a.T / tokens + a.B, a.T) * heads;
     const int grid = (int)std::min<long long>(items, gemm_ctas());
     if (grid < 1) return cudaErrorInvalidDevice;
@@ -556,7 +563,7 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     a.workers = a.kv.k ? std::min({(a.T + PS_WARPS - 1) / PS_WARPS, gemm_ctas(), PROMPT_MAX_WORKERS}) : 1;
     k_prompt_store<<<a.workers, 32 * PS_WARPS, 0, st>>>(a);
     const cudaError_t c = cudaGetLastError();
-    return c != cudaSuccess ? c : launch_pdl(k_prompt<D, FP16>, grid, THREADS, L::SMEM, st, qm, km, vm, a, log_p);
+    return c != cudaSuccess ? c : launch_pdl(k_prompt<D, FP16>, grid, THREADS, L::SMEM, st, qm, km, vm, a, P, inv_p);
 }
 
 }  // namespace

@@ -35,6 +35,7 @@ struct Cost {
     static constexpr int ONE = D == 64 ? 2 : 1, TWO = D == 64 ? 3 : 1, ROW = D == 64 ? 10 : 4;
 };
 constexpr int TA_MIN = 3;        // places of a CTA's stretch at least (17 nodes behind 512 slots: 15.8 us, with 6 18.1)
+static_assert(TA_MIN >= Cost<64>::TWO, "who is in the middle of a unit has a block");
 constexpr int TA_MASKS = 8;      // blocks whose masks are kept
 
 template <int D>
