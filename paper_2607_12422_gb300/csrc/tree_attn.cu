@@ -28,8 +28,8 @@ using namespace flash;
 namespace {
 
 // Costs in places: of a block of a unit of one tile, of two, and of a unit besides.  Heads of 64: by the rows' work (1.0 and 1.5 us; 5 us); else
-// memory bounds both (1.5 us; 6 us).  (64 sequences of 1 to 26 nodes, seven heads a KV head, us: 92 with two blocks for a unit and one cost
-// for both, 83 with 8 places for a unit, 76 with 10, 79 with 18.  Eight of up to 64 nodes, heads of 128: 26.5 with 2, 24.9 with 4, 25.2 with 6.)
+// memory bounds both (1.5 us; 6 us).  (64 sequences of 1 to 26 nodes, seven heads a KV head, us, with a slower join: 92 with two blocks for a unit and
+// one cost for both, 83 with 8 places for a unit, 76 with 10, 79 with 18.  Eight of up to 64 nodes, heads of 128: 26.5 with 2, 24.9 with 4, 25.2 with 6.)
 template <int D>
 struct Cost {
     static constexpr int ONE = D == 64 ? 2 : 1, TWO = D == 64 ? 3 : 1, ROW = D == 64 ? 10 : 4;
@@ -144,12 +144,11 @@ struct Segment {
         t_end = min(blocks, block_at<D>(end - at));
         return t < t_end;
     }
-    // The first segment of the stretch [u, u_end); false if it has none.
+    // The unit that has place u; false if there is none.
     template <int D>
-    __device__ __forceinline__ bool seek(int u, int u_end, const PackedArgs &a, const TreeList &T) {
-        end = u_end;
-        if (u >= end) return false;
+    __device__ __forceinline__ bool find(int u, const PackedArgs &a, const TreeList &T) {
         int lo = 0, hi = a.B;  // first[lo] <= u < first[hi]
+        if (u >= T.first[hi]) return false;
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (T.first[mid] <= u)
@@ -162,6 +161,13 @@ struct Segment {
         const int per = blocks * cost + Cost<D>::ROW;
         unit = (u - T.first[b]) / per;
         at = T.first[b] + unit * per;
+        return true;
+    }
+    // The first segment of the stretch [u, u_end); false if it has none.
+    template <int D>
+    __device__ __forceinline__ bool seek(int u, int u_end, const PackedArgs &a, const TreeList &T) {
+        end = u_end;
+        if (u >= end || !find<D>(u, a, T)) return false;
         t = block_at<D>(u - at);
         return clip<D>() || next<D>(a, T);
     }
@@ -764,21 +770,45 @@ __global__ void __launch_bounds__(THREADS, 1)
 
 // Joins the parts of units that several CTAs worked on: a warp 32 dimensions of four rows of a unit (node by node, the heads of its
 // group innermost), eight lanes a row.  Parts are taken eight at a time, whose loads go out together (one after the other, 64 nodes
-// behind 131071 slots, whose units have 20 parts, took 50 us here).  The first CTA reports.
+// behind 131071 slots, whose units have 20 parts, took 50 us here).  Every CTA counts the tasks of such units, so that all warps get as
+// many (going over all rows instead and leaving out most: 64 ragged sequences 75.6 us, now 71.3; 17 nodes behind 512 slots 16, now 14.5).
+// The first CTA reports.
 constexpr int TJ_WARPS = 8, TJ_ROWS = 4;
+static_assert(TREE_MAX_WORKERS <= 32 * TJ_WARPS, "a thread a CTA of k_tree");
+struct JoinUnit {
+    int b, h, last, row0, rows;  // sequence, KV head, its last CTA, first row in the (sequence, KV head), rows
+};
 template <int D, bool FP16>
 __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_constant__ PackedArgs a) {
     using L = TreeShape<D>;
     __shared__ TreeList T;
-    __shared__ int most_nodes;
-    if (threadIdx.x == 0) most_nodes = 0;
+    __shared__ JoinUnit units[TREE_MAX_WORKERS];
+    __shared__ int first[32 * TJ_WARPS + 1], warp_tasks[TJ_WARPS];  // tasks before a unit
     const int count = tree_list<D>(a, T);
     const Shares shares(a, count);
-    const int lane = threadIdx.x & 31, lr = lane >> 3, ld = lane & 7;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lr = lane >> 3, ld = lane & 7;
     const float c = a.scale * 1.4426950408889634f;
-    for (int b = threadIdx.x; b < a.B; b += 32 * TJ_WARPS) atomicMax(&most_nodes, T.nodes[b]);
+    // A thread a CTA of k_tree: the unit that it begins and others continue, if there is one, has the place where the next one's stretch begins.
+    int tasks = 0;
+    Segment seg{};
+    if ((int)threadIdx.x + 1 < shares.workers && seg.find<D>(shares.first(threadIdx.x + 1), a, T)) {
+        const int at = seg.at + Cost<D>::ROW, w0 = threadIdx.x, w1 = shares.owner(at + (seg.blocks - 1) * seg.cost), h = seg.unit / seg.chunks;
+        const int row0 = (seg.unit - h * seg.chunks) * L::ROWS_ALL, n = min(T.nodes[seg.b] * a.group - row0, L::ROWS_ALL);
+        if (shares.owner(at) == w0 && w1 > w0) tasks = (n + TJ_ROWS - 1) / TJ_ROWS * (D / 32);
+        units[w0] = {seg.b, h, w1, row0, n};
+    }
+    int sum = tasks;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += y;
+    }
+    if (lane == 31) warp_tasks[warp] = sum;
     __syncthreads();
-    const int per_unit = (most_nodes * a.group + TJ_ROWS - 1) / TJ_ROWS * (D / 32);  // of a (sequence, KV head)
+    for (int w = 0; w < warp; ++w) sum += warp_tasks[w];
+    first[threadIdx.x + 1] = sum;
+    if (threadIdx.x == 0) first[0] = 0;
+    __syncthreads();
     pdl_wait();
     if (blockIdx.x == 0) {
         int code = DEV_OK;
@@ -790,16 +820,18 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
         const int c7 = __syncthreads_or(code == DEV_BAD_PAGE), c9 = __syncthreads_or(code == DEV_BAD_TREE);
         if (threadIdx.x == 0 && (c5 | c7 | c9)) latch_error(a.status, c5 ? DEV_BAD_POSITION : c7 ? DEV_BAD_PAGE : DEV_BAD_TREE);
     }
-    const long long all = (long long)a.B * a.hkv * per_unit;
-    for (long long x = (long long)blockIdx.x * TJ_WARPS + (threadIdx.x >> 5); x < all; x += (long long)gridDim.x * TJ_WARPS) {
-        const int bh = (int)(x / per_unit), b = bh / a.hkv, h = bh - b * a.hkv, y = (int)(x - (long long)bh * per_unit);
-        const int row0 = y / (D / 32) * TJ_ROWS, d4 = y % (D / 32) * 8 + ld, n_rows = T.nodes[b] * a.group;
-        if (row0 >= n_rows) continue;
-        const int chunk = row0 / L::ROWS_ALL, pr = min(row0 + lr, n_rows - 1) - chunk * L::ROWS_ALL;  // (a chunk is a multiple of four rows)
-        const int cost = cost_of<D>(n_rows), blocks = blocks_of(T.len[b], T.nodes[b]), per = blocks * cost + Cost<D>::ROW;
-        const int at = T.first[b] + (h * chunks_of<D>(n_rows) + chunk) * per;
-        const int w0 = shares.owner(at + Cost<D>::ROW), w1 = shares.owner(at + per - cost);
-        if (w0 == w1) continue;  // one CTA had all blocks
+    for (int x = blockIdx.x * TJ_WARPS + warp; x < first[32 * TJ_WARPS]; x += gridDim.x * TJ_WARPS) {
+        int w0 = 0, hi = 32 * TJ_WARPS;  // first[w0] <= x < first[hi]
+        while (hi - w0 > 1) {
+            const int mid = (w0 + hi) >> 1;
+            if (first[mid] <= x)
+                w0 = mid;
+            else
+                hi = mid;
+        }
+        const JoinUnit u = units[w0];
+        const int b = u.b, h = u.h, w1 = u.last, n = u.rows, y = x - first[w0];
+        const int row0 = y / (D / 32) * TJ_ROWS, d4 = y % (D / 32) * 8 + ld, pr = min(row0 + lr, n - 1);
         auto part = [&](int w) { return (long long)w * 2 + (w == w0); };
         auto max_sum = [&](int w) { return w <= w1 ? a.part_ml[part(w) * a.part_rows + pr] : make_float2(-INFINITY, 0.f); };
         float m = -INFINITY;
@@ -825,13 +857,14 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
         }
 #pragma unroll
         for (int e = 4; e; e >>= 1) l += __shfl_xor_sync(0xffffffffu, l, e);
-        if (row0 + lr >= n_rows) continue;
-        const Row r{m, l};
-        const float inv = row_factor(r);
-        const int row = row0 + lr, node = row / a.group;
-        const long long out_row = (long long)(a.starts[b] + node) * a.hq + h * a.group + row - node * a.group;
-        *reinterpret_cast<uint2 *>(a.out + out_row * D + d4 * 4) = make_uint2(pack16<FP16>(o.x * inv, o.y * inv), pack16<FP16>(o.z * inv, o.w * inv));
-        if (a.lse && d4 == 0) a.lse[out_row] = row_lse<FP16>(r, a.scale);
+        if (row0 + lr < n) {
+            const Row r{m, l};
+            const float inv = row_factor(r);
+            const int row = u.row0 + row0 + lr, node = row / a.group;
+            const long long out_row = (long long)(a.starts[b] + node) * a.hq + h * a.group + row - node * a.group;
+            *reinterpret_cast<uint2 *>(a.out + out_row * D + d4 * 4) = make_uint2(pack16<FP16>(o.x * inv, o.y * inv), pack16<FP16>(o.z * inv, o.w * inv));
+            if (a.lse && d4 == 0) a.lse[out_row] = row_lse<FP16>(r, a.scale);
+        }
     }
 }
 
@@ -870,9 +903,8 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     k_tree<D, FP16><<<a.workers, THREADS, L::SMEM, st>>>(kmap, vmap, a, box, step);
     const cudaError_t c = cudaGetLastError();
     if (c != cudaSuccess) return c;
-    const long long warps = ((long long)std::min<long long>(a.T, (long long)a.B * TREE_NODES) * a.hq + TJ_ROWS - 1) / TJ_ROWS * (D / 32);
-    const int grid = (int)std::min<long long>((warps + TJ_WARPS - 1) / TJ_WARPS, 8ll * gemm_ctas());
-    return launch_pdl(k_tree_join<D, FP16>, grid, 32 * TJ_WARPS, 0, st, a);
+    const int most = (std::min({TREE_NODES * a.group, L::ROWS_ALL, std::min(a.T, 1 << 16) * a.group}) + TJ_ROWS - 1) / TJ_ROWS * (D / 32);  // tasks of a unit
+    return launch_pdl(k_tree_join<D, FP16>, std::min((a.workers * most + TJ_WARPS - 1) / TJ_WARPS, 4 * gemm_ctas()), 32 * TJ_WARPS, 0, st, a);
 }
 
 }  // namespace
