@@ -16,6 +16,10 @@
 // rows of V behind the sequence's end become zero, infinite and NaN values too, and the first row that sees one is noted for each dimension; from
 // that row on the result is NaN there.
 //
+// 16384 tokens, 16 heads of 128 on 8 KV heads, stored: 692-725 us, 1.5 to 1.6 PFLOP/s, the tensor core busy 70 % of the time and waiting for the chain
+// scores, softmax, P V of two tiles (1400 cycles a tile and block, 1050 of them products).  Eight ragged prompts of 420 to 1757: 57 us; 32 ragged
+// ones, groups of seven heads of 64: 91 us, of which 8 are spent before the first scores and half of the rest on items' first and last blocks.
+//
 // Warps 0-15: the tiles' rows.  Warp 16: TMA.  Warps 17 and 18: the tiles' MMAs (one thread for both spent more on issuing and waiting
 // than the tensor core on multiplying: 16384 tokens 916 us).  Warp 19: the list, and V of items done again.
 #include <algorithm>

@@ -10,6 +10,9 @@
 // of about the same cost: how ragged the lengths are does not matter, and the host need not know them.  Where a stretch begins or ends
 // inside a (sequence, KV head) the CTA leaves maximum, sum and unnormalised output in scratch, and k_tree_join joins them.
 //
+// 64 nodes behind 131071 slots, heads of 128: 105 us, between first and last block 6.4 TB/s (1.54 us a block of 64 KB an SM).  Heads of 64: a block takes
+// the rows 1.0 us (memory 0.76), of two tiles 1.5.  17 nodes behind 512: 14.5 us, of which 8 pass before the first scores.
+//
 // Warps 0-15: rows (queries, softmax, outputs).  Warp 16 copies K, warp 17 V: tiled copies of the rows that a page has in a piece where
 // pages hold a multiple of 8, row by row else, 16 bytes a lane.  Warps 18 and 19: the tiles' MMAs.
 // The blocks with nodes among their keys, a (sequence, KV head)'s last one or two, are copied row by row.  The rows' warps, of the second tile

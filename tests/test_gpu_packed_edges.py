@@ -258,3 +258,47 @@ def test_a_pool_keeps_its_tensors(env):  # noqa: F811
         setattr(pool, name, getattr(pool, name))
     pool.held += 0  # (in place)
     assert pool.n_free.tolist() == [8]
+
+
+def test_all_of_them_at_once_on_streams_of_their_own(env):  # noqa: F811
+    """A prompt, trees of two caches and the paths of a third, none waiting for another: what each gives alone."""
+    torch, pbd = env
+    hkv, group, page, dt = 2, 4, 16, torch.bfloat16
+    hq = hkv * group
+    prompts = [x.cuda() for x in ref.rows(torch, 900, hq, hkv, 128, dt, False)]
+    starts = i32(torch, [0, 700, 900])
+    lens, nodes = [400, 90, 1000, 0], [64, 20, 33, 5]
+    T = sum(nodes)
+    trees, fresh = [], []
+    for D in (128, 64):
+        c = ref.tree_case(torch, lens, nodes, hkv, D, page, dt, "heads")
+        trees.append((c, [x.cuda() for x in ref.rows(torch, T, hq, hkv, D, dt, False, seed=D)]))
+        fresh.append([to_gpu(torch, c) for _ in range(2)])
+    node_starts = ref.starts_of(torch, nodes).cuda()
+    third = kvref.make_cache(torch, [n + 64 for n in lens], hkv, 128, page, dt, extra=0)
+    third["lens"] = torch.tensor(lens, dtype=torch.int32)
+    paths, took = i32(torch, [list(range(1, 64, 2))] * 4), i32(torch, [32, 7, 0, 31])
+
+    def calls(turn, where):
+        out = []
+        copies = [f[turn] for f in fresh]
+        moved = to_gpu(torch, third)
+        torch.cuda.synchronize()
+
+        def prompt():
+            out.append(pbd.pbd_op_prompt_attention(*prompts, starts, sync=False)[0])
+
+        def tree(i):
+            g, (q, kn, vn) = copies[i], trees[i][1]
+            out.append(pbd.pbd_op_tree_attention(q, pbd.PagedKV(g["k"], g["v"], g["table"], g["lens"]), kn, vn, node_starts, sync=False)[0])
+
+        def commit():
+            pbd.pbd_op_commit_path(pbd.PagedKV(moved["k"], moved["v"], moved["table"], moved["lens"]), paths, took, sync=False)
+        for f, s in zip((prompt, lambda: tree(0), lambda: tree(1), commit), where):
+            with torch.cuda.stream(s):
+                f()
+        torch.cuda.synchronize()
+        return out + [x[n] for x in copies + [moved] for n in ("k", "v")]
+    alone = calls(0, [torch.cuda.current_stream()] * 4)
+    for x, y in zip(alone, calls(1, [torch.cuda.Stream() for _ in range(4)])):
+        assert torch.equal(x.contiguous().view(torch.int16), y.contiguous().view(torch.int16))
