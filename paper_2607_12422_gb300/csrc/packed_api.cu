@@ -87,7 +87,7 @@ pbd_status pbd_op_assign_pages(int32_t batch, int32_t max_pages, int32_t page_si
 size_t pbd_op_prompt_attention_workspace_bytes(int32_t T, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                                int32_t head_dim) {
     if (bad_rows_of(T, batch, n_q_heads, n_kv_heads, head_dim, (int64_t)n_q_heads * head_dim, (int64_t)n_kv_heads * head_dim)) return 0;
-    return 1024 + PROMPT_MAX_WORKERS * sizeof(int);
+    return 1024;
 }
 
 pbd_status pbd_op_prompt_attention(int32_t T, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -145,7 +145,6 @@ pbd_status pbd_op_prompt_attention(int32_t T, int32_t batch, int32_t n_q_heads, 
     a.out = static_cast<uint16_t *>(d_out);
     a.lse = d_lse_opt;
     a.status = static_cast<int *>(d_ws);
-    a.worker_code = a.status + 256;
     const cudaError_t e = launch_prompt_attention(a, static_cast<cudaStream_t>(d_stream));
     return e == cudaSuccess ? PBD_OK : fail(PBD_ERR_CUDA, who, "launch", e);
 }

@@ -50,13 +50,12 @@ struct PackedArgs {
     uint16_t *out;           // [T][hq][d]
     float *lse;              // [T][hq] or null
     int *status;
-    // scratch (prompt: codes alone; tree_plan)
+    // scratch (tree alone; tree_plan)
     int workers, part_rows;  // CTAs; rows of one's part of a unit
     int *worker_code;        // [workers]
     float2 *part_ml;         // [workers][2][part_rows]: maximum, sum
     float *part_o;           // [workers][2][part_rows][d]
 };
-constexpr int PROMPT_MAX_WORKERS = 256;  // CTAs that store K and V; a code of each in the workspace
 cudaError_t launch_prompt_attention(PackedArgs &a, cudaStream_t st);
 
 constexpr int TREE_MAX_WORKERS = 160;

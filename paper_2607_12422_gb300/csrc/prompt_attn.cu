@@ -16,7 +16,7 @@
 // rows of V behind the sequence's end become zero, infinite and NaN values too, and the first row that sees one is noted for each dimension; from
 // that row on the result is NaN there.
 //
-// 16384 tokens, 16 heads of 128 on 8 KV heads, stored: 692-725 us, 1.5 to 1.6 PFLOP/s, the tensor core busy 70 % of the time and waiting for the chain
+// 16384 tokens, 16 heads of 128 on 8 KV heads, stored: 677-725 us, 1.5 to 1.6 PFLOP/s, the tensor core busy 70 % of the time and waiting for the chain
 // scores, softmax, P V of two tiles (1400 cycles a tile and block, 1050 of them products).  Eight ragged prompts of 420 to 1757: 57 us; 32 ragged
 // ones, groups of seven heads of 64: 91 us, of which 8 are spent before the first scores and half of the rest on items' first and last blocks.
 //
@@ -111,14 +111,11 @@ __device__ __forceinline__ bool find_item(const PackedArgs &a, const int *start,
     return true;
 }
 
-// Clears the status and stores K and V into the cache, beside k_prompt: a warp a row.  Its CTAs fit an SM together with k_prompt's, whose
-// registers leave 4096.  (By k_prompt's own threads, before an item's first scores, it costs them registers that they lack.)
+// Stores K and V into the cache, beside k_prompt: a warp a row.  Its CTAs fit an SM together with k_prompt's, whose registers leave 4096.  (By
+// k_prompt's own threads, before an item's first scores, it costs them registers that they lack.)
 constexpr int PS_WARPS = 4;
 __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid_constant__ PackedArgs a) {
     __shared__ int start[KV_MAX_BATCH], end[KV_MAX_BATCH];
-    pdl_launch();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = DEV_OK;
-    if (!a.kv.k) return;
     for (int b = threadIdx.x; b < a.B; b += 32 * PS_WARPS) {
         const int s = a.starts[b], e = a.starts[b + 1];
         start[b] = s;
@@ -146,8 +143,8 @@ __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid
             *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.v) + to) = v;
         }
     }
-    bad = __syncthreads_or(bad);
-    if (threadIdx.x == 0) a.worker_code[blockIdx.x] = bad ? DEV_BAD_PAGE : DEV_OK;
+    pdl_wait();  // (k_prompt has cleared the status, and said what it found: that goes first)
+    if (__syncthreads_or(bad) && threadIdx.x == 0) latch_error(a.status, DEV_BAD_PAGE);
 }
 
 template <int D, bool FP16>
@@ -164,6 +161,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int tile_tokens = ROWS * inv_p >> 16, tokens = TILES * tile_tokens;  // (inv_p: 1 / P in 16 bits, exact for what it is used for)
     const int chunks = a.group * inv_p >> 16, heads = a.hkv * chunks;
+    pdl_launch();
     if (warp == 16) tmem_alloc(&S.tmem, TM_COLS);
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
@@ -191,6 +189,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         S.abort = S.bad = 0;
         fence_mbarrier_init();
+        if (blockIdx.x == 0) *a.status = DEV_OK;  // (a wait runs out a second later)
     }
     __syncthreads();
     // rows of no token stay zero
@@ -528,12 +527,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     tc_fence_before();
     __syncthreads();
     if (warp == 16) tmem_dealloc(tmem, TM_COLS);
-    pdl_wait();  // (k_prompt_store: nothing else is waited for, since it began after all before it)
-    if (blockIdx.x == 0 && warp == 19) {
-        int code = S.bad ? DEV_BAD_POSITION : DEV_OK;
-        for (int i = lane; a.kv.k && i < a.workers; i += 32) code = code ? code : *(volatile int *)&a.worker_code[i];
-        if (code != DEV_OK) latch_error(a.status, code);
-    }
+    if (blockIdx.x == 0 && threadIdx.x == 0 && S.bad) latch_error(a.status, DEV_BAD_POSITION);
 }
 
 template <int D, bool FP16>
@@ -564,10 +558,10 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     const uint32_t kb[3] = {64, 1, KEYS};
     if (!encode_map_16(&qm, a.q, 4, qd, qst, qb) || !encode_map_16(&km, a.k, 3, kd, kst, kb) || !encode_map_16(&vm, a.v, 3, kd, kst, kb))
         return cudaErrorInvalidValue;
-    a.workers = a.kv.k ? std::min({(a.T + PS_WARPS - 1) / PS_WARPS, gemm_ctas(), PROMPT_MAX_WORKERS}) : 1;
-    k_prompt_store<<<a.workers, 32 * PS_WARPS, 0, st>>>(a);
+    k_prompt<D, FP16><<<grid, THREADS, L::SMEM, st>>>(qm, km, vm, a, P, inv_p);
     const cudaError_t c = cudaGetLastError();
-    return c != cudaSuccess ? c : launch_pdl(k_prompt<D, FP16>, grid, THREADS, L::SMEM, st, qm, km, vm, a, P, inv_p);
+    // (the store as the second of the two, not the first, which k_prompt's CTAs would wait for: 512 tokens 15.5 us instead of 16.2)
+    return c != cudaSuccess || !a.kv.k ? c : launch_pdl(k_prompt_store, std::min((a.T + PS_WARPS - 1) / PS_WARPS, gemm_ctas()), 32 * PS_WARPS, 0, st, a);
 }
 
 }  // namespace

@@ -302,3 +302,22 @@ def test_all_of_them_at_once_on_streams_of_their_own(env):  # noqa: F811
     alone = calls(0, [torch.cuda.current_stream()] * 4)
     for x, y in zip(alone, calls(1, [torch.cuda.Stream() for _ in range(4)])):
         assert torch.equal(x.contiguous().view(torch.int16), y.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("D,group", [(64, 11), (128, 13), (128, 15), (256, 9), (64, 26), (128, 14), (64, 6)])
+def test_prompts_of_groups_that_leave_rows_over(env, D, group):  # noqa: F811
+    """Heads a KV head that do not divide a tile's 128 rows, two KV heads, prompts around a tile's tokens and a block of keys; the
+    rows behind the prompts are NaN."""
+    torch, pbd = env
+    tile = 128 // group
+    lens, hkv, dt = [1, tile, 0, tile + 1, 2 * tile - 1, 129, 2 * tile + 1, 300], 2, torch.bfloat16
+    hq, T = hkv * group, sum(lens) + 3
+    q, k, v = ref.rows(torch, T, hq, hkv, D, dt, True, lens)
+    starts = ref.starts_of(torch, lens)
+    out, lse = torch.full((T, hq, D), 7.0, dtype=dt, device="cuda"), torch.full((T, hq), 7.0, device="cuda")
+    pbd.pbd_op_prompt_attention(*ref.fused_to_gpu(torch, q, k, v), starts.cuda(), out=out, lse=lse)
+    for i, n in enumerate(lens):
+        if n:
+            at = slice(int(starts[i]), int(starts[i + 1]))
+            ref.check(torch, ref.attend(torch, q[at], k[at], v[at], ref.causal(torch, n)), out[at], lse[at], "bf16")
+    assert (out[T - 3:] == 7).all() and (lse[T - 3:] == 7).all()
