@@ -22,10 +22,6 @@ struct AssignArgs {
 };
 cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st);
 
-// Clears a status word (page_ops.cu) beside a kernel launched by launch_pdl next, whose threads call pdl_wait before they report and
-// whose CTAs all do before they end; what it reads otherwise was there before the clearing kernel began.
-cudaError_t launch_clear_status(int *status, cudaStream_t st);
-
 // ---- accepted paths (page_ops.cu)
 struct CommitArgs {
     KvView kv;
@@ -56,7 +52,7 @@ struct PackedArgs {
     float2 *part_ml;         // [workers][2][part_rows]: maximum, sum
     float *part_o;           // [workers][2][part_rows][d]
 };
-cudaError_t launch_prompt_attention(PackedArgs &a, cudaStream_t st);
+cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st);
 
 constexpr int TREE_MAX_WORKERS = 160;
 struct TreePlan {

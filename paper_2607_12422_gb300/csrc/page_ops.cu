@@ -193,7 +193,8 @@ __global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constan
 // row's source, and never a later one's.  So rows are taken in their order, some at a time, which are read before any of them is written.
 // One small CTA takes one (sequence, KV head): each is a chain of loads (length, path, table, rows), so that many at once count.
 // (512 sequences of 8 KV heads, 12 rows to move in each on average, 26 MB read and as much written: 9.2 us, 5.7 TB/s; with 256 threads 16.2, and 17.7 when
-// each takes four heads.  8 sequences: 3.2 us, launches and that chain.)  k_clear_status, which overlaps it, makes room for what any CTA finds wrong (one CTA that looks at all paths takes 50 us for 512 of them).
+// each takes four heads.  8 sequences: 3.2 us, launches and that chain.)  k_clear_status, which overlaps it, makes room for what any CTA
+// finds wrong (one CTA that looks at all paths takes 50 us for 512 of them).
 constexpr int CP_THREADS = 128;
 
 // whether the path of sequence b can be walked
@@ -283,14 +284,10 @@ cudaError_t launch_assign_pages(const AssignArgs &a, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_clear_status(int *status, cudaStream_t st) {
-    k_clear_status<<<1, 1, 0, st>>>(status);
-    return cudaGetLastError();
-}
-
 cudaError_t launch_commit_path(const CommitArgs &a, cudaStream_t st) {
     const int grid = a.kv.B * a.kv.hkv;
-    const cudaError_t e = launch_clear_status(a.status, st);
+    k_clear_status<<<1, 1, 0, st>>>(a.status);
+    const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     switch (a.kv.d) {
         case 64: return launch_pdl(k_commit_path<64>, grid, CP_THREADS, 0, st, a);

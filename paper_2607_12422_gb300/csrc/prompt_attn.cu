@@ -531,7 +531,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 template <int D, bool FP16>
-cudaError_t launch(PackedArgs &a, cudaStream_t st) {
+cudaError_t launch(const PackedArgs &a, cudaStream_t st) {
     using L = PromptShape<D>;
     static_assert(L::SMEM + sizeof(PromptState<D>) <= 227 * 1024, "shared memory");
     static std::atomic<uint64_t> set{0};
@@ -566,7 +566,7 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_prompt_attention(PackedArgs &a, cudaStream_t st) {
+cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st) {
     if (a.fp16) return a.d == 64 ? launch<64, true>(a, st) : a.d == 128 ? launch<128, true>(a, st) : launch<256, true>(a, st);
     return a.d == 64 ? launch<64, false>(a, st) : a.d == 128 ? launch<128, false>(a, st) : launch<256, false>(a, st);
 }
