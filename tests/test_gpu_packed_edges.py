@@ -321,3 +321,69 @@ def test_prompts_of_groups_that_leave_rows_over(env, D, group):  # noqa: F811
             at = slice(int(starts[i]), int(starts[i + 1]))
             ref.check(torch, ref.attend(torch, q[at], k[at], v[at], ref.causal(torch, n)), out[at], lse[at], "bf16")
     assert (out[T - 3:] == 7).all() and (lse[T - 3:] == 7).all()
+
+
+def test_the_most_heads_and_sequences(env):  # noqa: F811
+    """4096 query heads on one KV head; 1024 sequences, many of them empty."""
+    torch, pbd = env
+    dt = torch.bfloat16
+    for lens, nodes, hkv, group, D, page in (([40], [3], 1, 4096, 64, 16), ([i % 37 for i in range(1024)], [i % 3 for i in range(1024)], 1, 2, 128, 8)):
+        hq, T = hkv * group, sum(nodes)
+        q, kn, vn = ref.rows(torch, T, hq, hkv, D, dt, False)
+        starts = ref.starts_of(torch, nodes)
+        gpu = [x.cuda() for x in (q, kn, vn)]
+        out, lse = (x.cpu() for x in pbd.pbd_op_prompt_attention(*gpu, starts.cuda(), want_lse=True))
+        c = ref.tree_case(torch, lens, nodes, hkv, D, page, dt, "heads")
+        g = to_gpu(torch, c)
+        kv = pbd.PagedKV(g["k"], g["v"], g["table"], g["lens"])
+        out2, lse2 = (x.cpu() for x in pbd.pbd_op_tree_attention(gpu[0], kv, *gpu[1:], starts.cuda(), want_lse=True))
+        for b, m in enumerate(nodes):
+            if m:
+                at = slice(int(starts[b]), int(starts[b + 1]))
+                ref.check(torch, ref.attend(torch, q[at], kn[at], vn[at], ref.causal(torch, m)), out[at], lse[at], "bf16")
+                ref.check(torch, ref.tree_attention(torch, c, b, q[at], kn[at], vn[at], None), out2[at], lse2[at], "bf16")
+
+
+def test_a_first_call_within_a_capture(env):  # noqa: F811
+    """In a process of its own, whose first calls of all four are captured as one step."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import sys
+sys.path[:0] = ["tests", "."]
+import torch, _packed_oracle as ref
+from paper_2607_12422_gb300 import pbd
+hkv, group, D, page, n, m = 2, 2, 128, 16, 150, 20
+dt = torch.bfloat16
+q, k, v = (x.cuda() for x in ref.rows(torch, n, hkv * group, hkv, D, dt, False))
+tq, tk, tv = (x.cuda() for x in ref.rows(torch, m, hkv * group, hkv, D, dt, False, seed=2))
+cache = [torch.zeros(20, hkv, page, D, dtype=dt, device="cuda") for _ in range(2)]
+pool = pbd.PagePool(torch.zeros(1, 20, dtype=torch.int32, device="cuda"), page, 20)
+lens, none = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in range(2))
+new, nodes, took = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (n, m, 2))
+path = torch.tensor([[1, 7]], dtype=torch.int32, device="cuda")
+kv = pbd.PagedKV(*cache, pool.page_table, lens)
+ws = pbd.op_workspace(max(pbd.tree_attention_workspace_bytes(kv, m, hkv * group), 4096))
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = pbd.pbd_op_assign_pages(pool, lens, new, n, workspace=ws, sync=False)
+    out1 = pbd.pbd_op_prompt_attention(q, k, v, got.starts, kv=kv, slots=got.slots, workspace=ws, sync=False)[0]
+    lens.add_(new)
+    got = pbd.pbd_op_assign_pages(pool, lens, nodes, m, workspace=ws, sync=False)
+    out2 = pbd.pbd_op_tree_attention(tq, kv, tk, tv, got.starts, workspace=ws, sync=False)[0]
+    pbd.pbd_op_commit_path(kv, path, took, workspace=ws, sync=False)
+graph.replay()
+pbd.pbd_op_status(ws)
+ref.check(torch, ref.attend(torch, q.cpu(), k.cpu(), v.cpu(), ref.causal(torch, n)), out1, None, "bf16")
+sees = torch.cat([torch.ones(m, n, dtype=torch.bool), ref.causal(torch, m)], 1)
+ref.check(torch, ref.attend(torch, tq.cpu(), torch.cat([k, tk]).cpu(), torch.cat([v, tv]).cpu(), sees), out2, None, "bf16")
+table = pool.page_table[0].tolist()
+for i, x in ((n, 1), (n + 1, 7)):
+    assert torch.equal(cache[0][table[i // page], :, i % page], tk[x]) and torch.equal(cache[1][table[i // page], :, i % page], tv[x])
+print("done")
+"""
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300,
+                         cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert got.returncode == 0 and got.stdout.strip().endswith("done"), got.stderr[-2000:]
