@@ -17,8 +17,8 @@
 // that row on the result is NaN there.
 //
 // 16384 tokens, 16 heads of 128 on 8 KV heads, stored: 677-725 us, 1.5 to 1.6 PFLOP/s, the tensor core busy 70 % of the time and waiting for the chain
-// scores, softmax, P V of two tiles (1400 cycles a tile and block, 1050 of them products).  Eight ragged prompts of 420 to 1757: 57 us; 32 ragged
-// ones, groups of seven heads of 64: 91 us, of which 8 are spent before the first scores and half of the rest on items' first and last blocks.
+// scores, softmax, P V of two tiles (1400 cycles a tile and block, 1050 of them products).  Eight ragged prompts of 420 to 1757: 54 us; 32 ragged
+// ones, groups of seven heads of 64: 88 us, of which 8 are spent before the first scores and half of the rest on items' first and last blocks.
 //
 // Warps 0-15: the tiles' rows.  Warp 16: TMA.  Warps 17 and 18: the tiles' MMAs (one thread for both spent more on issuing and waiting
 // than the tensor core on multiplying: 16384 tokens 916 us).  Warp 19: the list, and V of items done again.
@@ -112,7 +112,9 @@ __device__ __forceinline__ bool find_item(const PackedArgs &a, const int *start,
 }
 
 // Stores K and V into the cache, beside k_prompt: a warp a row.  Its CTAs fit an SM together with k_prompt's, whose registers leave 4096.  (By
-// k_prompt's own threads, before an item's first scores, it costs them registers that they lack.)
+// k_prompt's own threads, before an item's first scores, it costs them registers that they lack.)  Beside k_prompt's warps its own fetch their code
+// anew for every row, and that bounds it: a short loop without divisions and unrolling, the next row's slot on its way (1000 prompts of 40
+// tokens, 8 KV heads of 128: 215 us with k_prompt's 192, 295 before; two warps a CTA with all of a row's loads on their way: 857).
 constexpr int PS_WARPS = 4;
 __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid_constant__ PackedArgs a) {
     __shared__ int start[KV_MAX_BATCH], end[KV_MAX_BATCH];
@@ -124,20 +126,23 @@ __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid
     __syncthreads();
     const int lane = threadIdx.x & 31;
     const long long slots = (long long)a.kv.n_pages * a.kv.page_size;
+    const int log_per = 28 - __clz(a.d), pieces = a.hkv << log_per;  // 16-byte pieces of a head, of a row
     bool bad = false;
-    for (int t = blockIdx.x * PS_WARPS + (threadIdx.x >> 5); t < a.T; t += gridDim.x * PS_WARPS) {
+    int t = blockIdx.x * PS_WARPS + (threadIdx.x >> 5);
+    long long next = t < a.T ? a.slots[t] : -1;
+    for (; t < a.T; t += gridDim.x * PS_WARPS) {
+        const long long slot = next;
+        if (a.T - t > gridDim.x * PS_WARPS) next = a.slots[t + gridDim.x * PS_WARPS];
         bool mine = false;
         for (int b = lane; b < a.B; b += 32) mine |= start[b] <= t && t < end[b];
         if (!__any_sync(0xffffffffu, mine)) continue;
-        const long long slot = a.slots[t];
         bad |= slot >= slots;
         if (slot < 0 || slot >= slots) continue;
         const long long page = slot >> 32 ? slot / a.kv.page_size : (long long)((uint32_t)slot / (uint32_t)a.kv.page_size);
         const long long dst = page * a.kv.stride_page + (slot - page * a.kv.page_size) * a.kv.stride_slot, src = (long long)t * a.kv_stride;
-        const int per = a.d / 8;
-#pragma unroll 2
-        for (int i = lane; i < a.hkv * per; i += 32) {
-            const long long to = dst + (i / per) * a.kv.stride_head + (i % per) * 8;
+#pragma unroll 1
+        for (int i = lane; i < pieces; i += 32) {
+            const long long to = dst + (i >> log_per) * a.kv.stride_head + (i & ((1 << log_per) - 1)) * 8;
             const uint4 k = *reinterpret_cast<const uint4 *>(a.k + src + i * 8), v = *reinterpret_cast<const uint4 *>(a.v + src + i * 8);
             *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.k) + to) = k;
             *reinterpret_cast<uint4 *>(const_cast<uint16_t *>(a.kv.v) + to) = v;
