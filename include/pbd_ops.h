@@ -238,8 +238,9 @@ size_t pbd_op_prompt_attention_workspace_bytes(int32_t T, int32_t batch, int32_t
  * no other; K and V of rows that a row does not see do not touch it, whatever they hold.  Finite values of V: in bf16 at most 2^123 / T.
  * Requirements: head_dim 64, 128 or 256; n_q_heads a multiple of n_kv_heads; batch <= 1024; scale > 0; d_q, d_k, d_v and d_out 16-byte
  * aligned, row strides multiples of 8 below 2^38; no slot twice; nothing that the call writes lies over anything else that it reads or writes.
- * The workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 bounds of a sequence that
- * descend or lie outside [0, T], whose rows are left out; 7 a slot outside the cache, whose row is not stored. */
+ * The workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 a sequence whose bounds
+ * descend or lie outside [0, T], or that begins below any bound in front of its own: its rows are left out (so no row is two sequences');
+ * 7 a slot outside the cache, whose row is not stored. */
 pbd_status pbd_op_prompt_attention(int32_t T, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                                    int32_t dtype, float scale, const void *d_q, int64_t q_stride, const void *d_k,
                                    const void *d_v, int64_t kv_stride, const int32_t *d_starts, const pbd_kv_pages *kv_opt,
@@ -261,7 +262,8 @@ size_t pbd_op_tree_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t T, 
  * Requirements: T <= 2^30; scale > 0; d_q, d_k_new, d_v_new and d_out 16-byte aligned, row strides multiples of 8 below 2^38; no page
  * in use is named twice among those that new rows go to; nothing that the call writes lies over anything else that it reads or writes.  The
  * workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 bounds that descend, lie outside [0, T]
- * or span more than 64 rows, or a length outside [0, max_pages * page_size - nodes]: the sequence is left out; 7 a page
+ * or span more than 64 rows, a sequence that begins below any bound in front of its own, or a length outside [0, max_pages * page_size -
+ * nodes]: the sequence is left out; 7 a page
  * outside [0, n_pages): its slots, new nodes' among them, take no part and are not stored; 9 a parent that is not before
  * its node: it counts as -1. */
 pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_heads, float scale, const void *d_q,

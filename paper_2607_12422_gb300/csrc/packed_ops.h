@@ -54,6 +54,19 @@ struct PackedArgs {
 };
 cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st);
 
+#ifdef __CUDACC__
+// Whether a sequence's bounds lie inside the packed rows.  Where all do, no row is two sequences'; where some do not, a sequence takes part
+// only if it also begins at or behind all bounds in front of its own (behind_all): what follows a descent would lie over rows before it.
+__device__ __forceinline__ bool bounds_ok(const PackedArgs &a, int s, int e) { return s >= 0 && e >= s && e <= a.T; }
+__device__ __forceinline__ bool behind_all(const int *starts, int b) {
+    const int s = starts[b];
+#pragma unroll 1
+    for (int i = 0; i < b; ++i)
+        if (starts[i] > s) return false;
+    return true;
+}
+#endif
+
 constexpr int TREE_MAX_WORKERS = 160;
 struct TreePlan {
     size_t codes, part_ml, part_o, total;  // offsets in the workspace

@@ -118,12 +118,18 @@ __device__ __forceinline__ bool find_item(const PackedArgs &a, const int *start,
 constexpr int PS_WARPS = 4;
 __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid_constant__ PackedArgs a) {
     __shared__ int start[KV_MAX_BATCH], end[KV_MAX_BATCH];
+    bool descends = false;
     for (int b = threadIdx.x; b < a.B; b += 32 * PS_WARPS) {
         const int s = a.starts[b], e = a.starts[b + 1];
         start[b] = s;
-        end[b] = s < 0 || e > a.T ? s : e;
+        end[b] = bounds_ok(a, s, e) ? e : s;
+        descends |= e < s;
     }
-    __syncthreads();
+    if (__syncthreads_or(descends)) {
+        for (int b = threadIdx.x; b < a.B; b += 32 * PS_WARPS)
+            if (!behind_all(a.starts, b)) end[b] = start[b];
+        __syncthreads();
+    }
     const int lane = threadIdx.x & 31;
     const long long slots = (long long)a.kv.n_pages * a.kv.page_size;
     const int log_per = 28 - __clz(a.d), pieces = a.hkv << log_per;  // 16-byte pieces of a head, of a row
@@ -209,12 +215,17 @@ __global__ void __launch_bounds__(THREADS, 1)
     for (int b = threadIdx.x; b < a.B; b += THREADS) {
         const int s = a.starts[b], e = a.starts[b + 1];
         S.start[b] = s;
-        const bool bad = s < 0 || e < s || e > a.T;
-        S.tiles[b] = bad ? 0 : (e - s + tokens - 1) / tokens;
-        if (bad && blockIdx.x == 0) S.bad = 1;
+        const bool ok = bounds_ok(a, s, e);
+        S.tiles[b] = ok ? (e - s + tokens - 1) / tokens : 0;
+        if (!ok) S.bad = 1;
     }
     tc_fence_before();
     __syncthreads();
+    if (S.bad) {
+        for (int b = threadIdx.x; b < a.B; b += THREADS)
+            if (!behind_all(a.starts, b)) S.tiles[b] = 0;
+        __syncthreads();
+    }
     tc_fence_after();
     const uint32_t tmem = S.tmem;
     // Whether there is an n-th item: S.item[n % AHEAD].

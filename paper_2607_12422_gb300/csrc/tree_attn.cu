@@ -56,10 +56,6 @@ struct TreeList {
     int len[KV_MAX_BATCH], nodes[KV_MAX_BATCH];
 };
 
-__device__ __forceinline__ bool tree_ok(const PackedArgs &a, int b) {
-    const int s = a.starts[b], e = a.starts[b + 1], len = a.kv.lens[b];
-    return s >= 0 && e >= s && e <= a.T && e - s <= TREE_NODES && len >= 0 && len + (long long)(e - s) <= a.kv.cap;
-}
 __device__ __forceinline__ int blocks_of(int len, int nodes) { return (len + nodes + KEYS - 1) / KEYS; }
 template <int D>
 __device__ __forceinline__ int chunks_of(int rows) { return (rows + TreeShape<D>::ROWS_ALL - 1) / TreeShape<D>::ROWS_ALL; }
@@ -67,15 +63,18 @@ __device__ __forceinline__ int chunks_of(int rows) { return (rows + TreeShape<D>
 template <int D>
 __device__ __forceinline__ int cost_of(int rows) { return TreeShape<D>::TILES == 2 && rows > ROWS ? Cost<D>::TWO : Cost<D>::ONE; }
 
-// Whole CTA; returns the list's length.  (Up to 32 sequences are one warp's: what comes before the first copy is what a small call waits for.)
+// Whole CTA; returns the list's length.  bad: whether this thread has seen a sequence that is left out.  (Up to 32 sequences are one warp's: what comes before the first copy is what a small call waits for.)
 template <int D>
-__device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
+__device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T, bool &bad) {
     __shared__ int warp_sum[32], total;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n_warps = blockDim.x >> 5;
-    auto places = [&](int b) {
+    bool descends = false;
+    auto places = [&](int b, bool out = false) {
         const int s = a.starts[b], e = a.starts[b + 1], l = a.kv.lens[b];
-        const bool ok = s >= 0 && e >= s && e <= a.T && e - s <= TREE_NODES && l >= 0 && l + (long long)(e - s) <= a.kv.cap;
+        const bool ok = !out && bounds_ok(a, s, e) && e - s <= TREE_NODES && l >= 0 && l + (long long)(e - s) <= a.kv.cap;
         const int n = ok ? e - s : 0, len = ok ? l : 0;
+        bad |= !ok;
+        descends |= e < s;
         T.len[b] = len, T.nodes[b] = n;
         return n > 0 ? a.hkv * chunks_of<D>(n * a.group) * (blocks_of(len, n) * cost_of<D>(n * a.group) + Cost<D>::ROW) : 0;
     };
@@ -90,7 +89,9 @@ __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
     if (threadIdx.x == 0) T.first[0] = 0;
     if (a.B <= 32) {
         if (warp == 0) {
-            const int x = scan(lane < a.B ? places(lane) : 0);
+            int x = lane < a.B ? places(lane) : 0;
+            if (__any_sync(0xffffffffu, descends) && lane < a.B) x = places(lane, !behind_all(a.starts, lane));
+            x = scan(x);
             if (lane < a.B) T.first[lane + 1] = x;
             if (lane == 31) total = x;
         }
@@ -100,9 +101,13 @@ __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T) {
     int carry = 0;
     for (int b0 = 0; b0 < a.B; b0 += blockDim.x) {
         const int b = b0 + threadIdx.x;
-        const int x = scan(b < a.B ? places(b) : 0);
+        int x = scan(b < a.B ? places(b) : 0);
         if (lane == 31) warp_sum[warp] = x;
-        __syncthreads();
+        if (__syncthreads_or(descends)) {  // (here or in front)
+            x = scan(b < a.B ? places(b, !behind_all(a.starts, b)) : 0);
+            if (lane == 31) warp_sum[warp] = x;
+            __syncthreads();
+        }
         const int sums = scan(lane < n_warps ? warp_sum[lane] : 0);
         const int before = carry + (warp ? __shfl_sync(0xffffffffu, sums, warp - 1) : 0);
         if (b < a.B) T.first[b + 1] = before + x;
@@ -268,7 +273,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         prefetch_tensormap(&vmap);
     }
     tc_fence_before();
-    const int count = tree_list<D>(a, T);  // (its barriers order what is above, too)
+    bool left_out = false;
+    const int count = tree_list<D>(a, T, left_out);  // (its barriers order what is above, too)
     const Shares shares(a, count);
     const int me = blockIdx.x;
     tc_fence_after();
@@ -787,7 +793,8 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
     __shared__ TreeList T;
     __shared__ JoinUnit units[TREE_MAX_WORKERS];
     __shared__ int first[32 * TJ_WARPS + 1], warp_tasks[TJ_WARPS];  // tasks before a unit
-    const int count = tree_list<D>(a, T);
+    bool left_out = false;
+    const int count = tree_list<D>(a, T, left_out);
     const Shares shares(a, count);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, lr = lane >> 3, ld = lane & 7;
     const float c = a.scale * 1.4426950408889634f;
@@ -814,11 +821,8 @@ __global__ void __launch_bounds__(32 * TJ_WARPS) k_tree_join(const __grid_consta
     __syncthreads();
     pdl_wait();
     if (blockIdx.x == 0) {
+        const int c5 = __syncthreads_or(left_out);
         int code = DEV_OK;
-        for (int b = threadIdx.x; b < a.B; b += 32 * TJ_WARPS)
-            if (!tree_ok(a, b)) code = DEV_BAD_POSITION;
-        const int c5 = __syncthreads_or(code != DEV_OK);
-        code = DEV_OK;
         for (int w = threadIdx.x; w < a.workers; w += 32 * TJ_WARPS) code = max(code, a.worker_code[w]);
         const int c7 = __syncthreads_or(code == DEV_BAD_PAGE), c9 = __syncthreads_or(code == DEV_BAD_TREE);
         if (threadIdx.x == 0 && (c5 | c7 | c9)) latch_error(a.status, c5 ? DEV_BAD_POSITION : c7 ? DEV_BAD_PAGE : DEV_BAD_TREE);
