@@ -2,7 +2,7 @@
 //
 // Inline PTX wrappers for mbarriers, TMA bulk copies (1-D bulk and 2-D tiled), and the
 // 5th-generation tensor core (tcgen05.alloc / mma / commit / ld), plus bounded waits:
-// every spin on an mbarrier gives up after WAIT_LIMIT_NS, latches an error code in the
+// every spin on an mbarrier gives up after WAIT_LIMIT_NS (or its kernel's own limit), latches an error code in the
 // device status word and lets the kernel exit cleanly instead of hanging the GPU.
 #pragma once
 
@@ -163,21 +163,23 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, int *s
     return ok;
 }
 
-// The same in fewer instructions, for kernels whose warps run different code: one that runs little beside others that run much
-// fetches its instructions anew each time.
-__device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, int *status, int code, volatile int *abort) {
+// The same in fewer instructions and registers, for kernels whose warps run different code: one that runs little beside others that run
+// much fetches its instructions anew each time.  patience: what the CTA's waits share, the limit in units of 2^20 ns, 0 once one has run out;
+// null: WAIT_LIMIT_NS.
+constexpr uint32_t WAIT_PATIENCE = (uint32_t)(WAIT_LIMIT_NS >> 20) + 1;
+__device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, int *status, int code, volatile uint32_t *patience) {
     const uint32_t a = smem_u32(bar);
-    uint64_t t0 = 0;
+    uint32_t t0 = 0;
 #pragma unroll 1
     for (uint32_t n = 1; !mbar_try_wait(a, parity); ++n) {
         if (n & 127) continue;
-        const uint64_t t = globaltimer_ns();
+        const uint32_t t = (uint32_t)(globaltimer_ns() >> 20);
         t0 = t0 ? t0 : t;
-        if (t - t0 > WAIT_LIMIT_NS) {
-            latch_error(status, code);
-            if (abort) *abort = 1;
-        }
-        if (t - t0 > WAIT_LIMIT_NS || (abort && *abort)) return false;
+        const uint32_t limit = patience ? (uint32_t)*patience : (uint32_t)WAIT_PATIENCE;
+        if (t - t0 < limit) continue;
+        latch_error(status, code);
+        if (patience) *patience = 0;
+        return false;
     }
     return true;
 }

@@ -46,13 +46,21 @@ struct PackedArgs {
     uint16_t *out;           // [T][hq][d]
     float *lse;              // [T][hq] or null
     int *status;
+    uint32_t patience;       // after which a wait in the kernel gives up, in 2^20 ns
     // scratch (tree alone; tree_plan)
     int workers, part_rows;  // CTAs; rows of one's part of a unit
     int *worker_code;        // [workers]
     float2 *part_ml;         // [workers][2][part_rows]: maximum, sum
     float *part_o;           // [workers][2][part_rows][d]
 };
-cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st);
+cudaError_t launch_prompt_attention(PackedArgs &a, cudaStream_t st);
+
+// Some waits in these kernels last as long as the work between two things that a warp has to do: rows of an item's second tile, when it has
+// none, wait for the whole item; the second tile's MMAs of a CTA's stretch for all units of one tile in front.  So a wait gives up after a second
+// and 32 us for each block of that work (a block takes 1 to 2 us, copied row by row 5 to 10).
+inline uint32_t packed_patience(double blocks) { return (uint32_t)((1e9 + 32e3 * blocks) / (1 << 20)) + 1; }
+inline uint32_t prompt_patience(int T) { return packed_patience(T / 128 + 1); }  // the longest item's blocks
+inline uint32_t tree_patience(double places, int workers) { return packed_patience(places / workers + 1); }  // of the longest list
 
 #ifdef __CUDACC__
 // Whether a sequence's bounds lie inside the packed rows.  Where all do, no row is two sequences'; where some do not, a sequence takes part
@@ -72,6 +80,7 @@ struct TreePlan {
     size_t codes, part_ml, part_o, total;  // offsets in the workspace
     int rows;
 };
+double tree_places(const KvView &kv, int hq);  // of the list at most
 bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p);
 cudaError_t launch_tree_attention(PackedArgs &a, cudaStream_t st);
 

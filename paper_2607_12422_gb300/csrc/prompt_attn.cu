@@ -56,7 +56,8 @@ struct PromptState {
     uint64_t full[L::STAGES], empty[L::STAGES], q_full, q_free, s_full[2], p_full[2][2], o_done[2], o_free[2], turn[2], drain[2];
     uint64_t v_full[L::AHEAD][PA_MASKED], v_fixed[L::AHEAD][PA_MASKED], item_full[L::AHEAD], item_free[L::AHEAD];
     uint32_t tmem;
-    int abort, bad;  // bad: bounds of a sequence
+    uint32_t patience;  // mbar_wait_short
+    int bad;  // bounds of a sequence
     PromptItem item[L::AHEAD];
     float top[2][2][ROWS];    // what the two threads of a row tell each other
     int odd[L::AHEAD];  // whether a result is not finite
@@ -198,7 +199,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&S.item_full[i], 1);
             mbar_init(&S.item_free[i], ROW_WARPS + 1 + TILES);
         }
-        S.abort = S.bad = 0;
+        S.patience = a.patience;
+        S.bad = 0;
         fence_mbarrier_init();
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (a wait runs out a second later)
     }
@@ -230,7 +232,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t tmem = S.tmem;
     // Whether there is an n-th item: S.item[n % AHEAD].
     auto item_there = [&](int n) {
-        return mbar_wait_short(&S.item_full[n % AHEAD], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort) && *(volatile int *)&S.item[n % AHEAD].len > 0;
+        return mbar_wait_short(&S.item_full[n % AHEAD], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience) && *(volatile int *)&S.item[n % AHEAD].len > 0;
     };
 
     if (warp >= ROW_WARPS) {
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                     const PromptItem it = S.item[s];
                     mbarrier_arrive_one(&S.item_free[s]);
                     const int nmax = max(it.nb[0], it.nb[1]);
-                    if (n > 0 && !mbar_wait_short(&S.q_free, (n - 1) & 1, a.status, DEV_TIMEOUT_SLOT, &S.abort)) break;
+                    if (n > 0 && !mbar_wait_short(&S.q_free, (n - 1) & 1, a.status, DEV_TIMEOUT_SLOT, &S.patience)) break;
                     mbar_arrive_expect_tx(&S.q_full, (uint32_t)(TILES * (D / 64) * 128 * tile_tokens * P));
                     for (int i = 0; i < TILES; ++i)
                         for (int c = 0; c < D / 64; ++c)
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         const int y = at_place(x, nmax, TWO), kb = y < 0 ? ~y : y;
                         for (int u = 0; u < UNITS; ++u) {
                             const int slot = issued % STAGES;
-                            if (!mbar_wait_short(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort)) {
+                            if (!mbar_wait_short(&S.empty[slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.patience)) {
                                 ok = false;
                                 break;
                             }
@@ -274,7 +276,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                         }
                     }
                 }
-                if (*(volatile int *)&S.abort) {  // error path: the copies in flight get a bounded chance to land
+                if (*(volatile uint32_t *)&S.patience == 0) {  // error path: the copies in flight get a bounded chance to land
                     const uint64_t t0 = globaltimer_ns();
                     while (globaltimer_ns() - t0 < WAIT_LIMIT_NS / 100) __nanosleep(1000);
                 }
@@ -287,7 +289,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const uint32_t o = tmem + TM_O + i * D;
                 bool ok = true;
                 int pos = 0, step = 0, used = 0, used_o = 0;  // blocks' K and V, sections, blocks and items of the tile so far
-                auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.abort); };
+                auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.patience); };
                 auto landed = [&](int place) {
                     for (int u = 0; u < UNITS; ++u) wait(&S.full[(place * UNITS + u) % STAGES], (place * UNITS + u) / STAGES, DEV_TIMEOUT_LOAD);
                 };
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 const int nmax = max(it.nb[0], it.nb[1]);
                 for (int k = 0; ok && k < PA_MASKED; ++k) {
                     const int j = it.masked + k;
-                    if (it.careful) ok = mbar_wait_short(&S.v_full[s][k], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+                    if (it.careful) ok = mbar_wait_short(&S.v_full[s][k], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_LOAD, &S.patience);
                     if (!(ok = __all_sync(0xffffffffu, ok))) break;
                     for (int u = 0; it.careful && j < nmax && u < UNITS; ++u) {
                         const int slot = ((pos + v_place(j, nmax, TWO)) * UNITS + u) % STAGES;
@@ -448,7 +450,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 }
                 pos += 2 * nmax;
                 // when everybody is through with it: the next one, or this one again
-                ok = ok && mbar_wait_short(&S.item_free[s], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort);
+                ok = ok && mbar_wait_short(&S.item_free[s], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience);
                 if (!(ok = __all_sync(0xffffffffu, ok))) break;
                 PromptItem next = it;
                 next.careful = 1;
@@ -474,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int n = 0; ok; ++n) {
             const int s = n % AHEAD;
             const volatile PromptItem &it = S.item[s];  // (read again at the end, to spare registers)
-            if (pair_any(id, !mbar_wait_short(&S.item_full[s], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort))) break;
+            if (pair_any(id, !mbar_wait_short(&S.item_full[s], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience))) break;
             const int nb = it.nb[i], first = it.q0 + i * tile_tokens;
             if (it.len == 0) break;
             const int nmax = max(it.nb[0], it.nb[1]);
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             for (int j = 0; ok && j < nb; ++j, ++used) {
                 const int buf = TWO ? i : used & 1;
-                bool there = mbar_wait_short(&S.s_full[buf], (TWO ? used : used >> 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort), o_waited = TWO || j == 0;
+                bool there = mbar_wait_short(&S.s_full[buf], (TWO ? used : used >> 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.patience), o_waited = TWO || j == 0;
                 there = __all_sync(0xffffffffu, there);
                 release(pos + k_place(j, TWO));
                 if (TWO && j > 0) release(pos + v_place(j - 1, nmax, TWO));
@@ -503,7 +505,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 auto o_ready = [&]() {  // (with two tiles S of this block has come after O of the one before)
                     bool o = true;
                     if (!o_waited) {
-                        o = mbar_wait_short(&S.o_done[0], (used - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+                        o = mbar_wait_short(&S.o_done[0], (used - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.patience);
                         release(pos + v_place(j - 1, nmax, TWO));
                     }
                     o_waited = true;
@@ -514,12 +516,12 @@ __global__ void __launch_bounds__(THREADS, 1)
                     if (lane == 0) mbarrier_arrive_one(&S.p_full[buf][part]);
                 });
             }
-            bool there = mbar_wait_short(&S.o_done[i], (TWO ? used_o : used - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+            bool there = mbar_wait_short(&S.o_done[i], (TWO ? used_o : used - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.patience);
             ++used_o;
             release(pos + v_place(nb - 1, nmax, TWO));
             pos += 2 * nmax;
             const bool careful = it.careful != 0;
-            for (int k = 0; careful && there && k < PA_MASKED; ++k) there = mbar_wait_short(&S.v_fixed[s][k], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_LOAD, &S.abort);
+            for (int k = 0; careful && there && k < PA_MASKED; ++k) there = mbar_wait_short(&S.v_fixed[s][k], (n / AHEAD) & 1, a.status, DEV_TIMEOUT_LOAD, &S.patience);
             if (!ok || pair_any(id, !there)) break;
             top[half * ROWS + row] = r.l;
             pair_sync(id);
@@ -582,7 +584,8 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_prompt_attention(const PackedArgs &a, cudaStream_t st) {
+cudaError_t launch_prompt_attention(PackedArgs &a, cudaStream_t st) {
+    a.patience = prompt_patience(a.T);
     if (a.fp16) return a.d == 64 ? launch<64, true>(a, st) : a.d == 128 ? launch<128, true>(a, st) : launch<256, true>(a, st);
     return a.d == 64 ? launch<64, false>(a, st) : a.d == 128 ? launch<128, false>(a, st) : launch<256, false>(a, st);
 }

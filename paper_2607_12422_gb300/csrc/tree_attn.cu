@@ -202,7 +202,8 @@ struct TreeState {
     uint64_t full[2][L::STAGES], empty[2][L::STAGES], q_full[2], s_full[3], p_full[3][2], o_done[2], o_free[2], turn[2], drain[2];
     uint64_t notes_ready[L::RING_SEGS], notes_made[L::RING_SEGS], notes_free[L::RING_SEGS];
     uint32_t tmem;
-    int abort, bad_page, bad_tree;
+    uint32_t patience;  // mbar_wait_short
+    int bad_page, bad_tree;
     float top[2][2][ROWS];              // what the two threads of a row tell each other
     Segment row_seg[ROW_WARPS];         // where each of the rows' warps is (to spare registers)
     alignas(8) uint32_t valid[TA_MASKS][4];  // keys of a block whose pages are in the cache
@@ -263,7 +264,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             mbar_init(&S.notes_free[i], ROW_WARPS);
             S.odd[i] = 0;
         }
-        S.abort = S.bad_page = S.bad_tree = 0;
+        S.patience = a.patience;
+        S.bad_page = S.bad_tree = 0;
         fence_mbarrier_init();
         if (blockIdx.x == 0) *a.status = DEV_OK;  // (k_tree_join reports; a wait runs out a second later)
     }
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             };
             auto next_slot = [&]() {
                 const int slot = issued % STAGES;
-                ok = __all_sync(0xffffffffu, mbar_wait_short(&S.empty[kv][slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.abort));
+                ok = __all_sync(0xffffffffu, mbar_wait_short(&S.empty[kv][slot], ((issued / STAGES) & 1) ^ 1, a.status, DEV_TIMEOUT_SLOT, &S.patience));
                 ++issued;
                 return slot;
             };
@@ -330,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 if (kv && seg.t_end > tail0) {
                     // room for this segment's notes: all rows are through with those that were there.  (Said before the first copy: rows wait for it.)
                     if (sn >= L::RING_SEGS)
-                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_free[si], (sn / L::RING_SEGS - 1) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
+                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_free[si], (sn / L::RING_SEGS - 1) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience));
                     if (ok && S.odd[si]) {
                         __syncwarp();
                         for (int d = lane; d < D; d += 32) S.odd_nodes[si][d] = 0;
@@ -377,7 +379,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 // The last unit that was copied.  V: once the rows have looked at the nodes' values, of which some become zero.
                 auto finish = [&]() {
                     if (kv) {
-                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_made[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
+                        ok = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_made[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience));
                         if (*(volatile int *)&S.odd[si]) {
                             const uint32_t to = smem_u32(units + pend * L::UNIT);
                             const int k0 = pend_t * KEYS;
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
             cp_async_commit();
             cp_async_wait_all();  // also on the error path: nothing is in flight when the CTA ends
-            if (*(volatile int *)&S.abort) {  // (and tiled copies get a bounded chance to land)
+            if (*(volatile uint32_t *)&S.patience == 0) {  // (and tiled copies get a bounded chance to land)
                 const uint64_t t0 = globaltimer_ns();
                 while (globaltimer_ns() - t0 < WAIT_LIMIT_NS / 100) __nanosleep(1000);
             }
@@ -489,7 +491,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             const uint32_t o = tmem + TM_O + i * D;
             int pos = 0, step = 0, used_o = 0, cnt0 = 0, cnt1 = 0, cnt2 = 0, twos = 0;  // blocks, sections, segments of the tile, phases of s_full, segments of two tiles
             bool ok = true;
-            auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.abort); };
+            auto wait = [&](uint64_t *bar, int phase, int code) { ok = ok && mbar_wait_short(bar, phase & 1, a.status, code, &S.patience); };
             auto landed = [&](int kv, int j) {  // K or V of the CTA's block j
                 for (int u = 0; u < UNITS; ++u) wait(&S.full[kv][(j * UNITS + u) % STAGES], (j * UNITS + u) / STAGES, DEV_TIMEOUT_LOAD);
                 if (!box) fence_proxy_async_shared();  // (cp.async's copies land in the generic proxy)
@@ -659,7 +661,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (ends && (two || i)) {  // the nodes' K and V go to the cache, and V is looked at: by rows that have nothing else to do, if there are
                 constexpr int CPR = D / 8;
                 const int si = sn % L::RING_SEGS;
-                const bool room = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_ready[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort));
+                const bool room = __all_sync(0xffffffffu, mbar_wait_short(&S.notes_ready[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience));
                 const int h = g->unit / g->chunks, start = a.starts[b], len = T.len[b], first = two ? 0 : ROW_WARPS * 16;
                 const int from = max(g->t * KEYS - len, 0), to = min(T.nodes[b], g->t_end * KEYS - len);  // (of this stretch's blocks)
 #pragma unroll 1
@@ -687,7 +689,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (idle) continue;
             for (int j = 0; ok && j < nb; ++j) {
                 const int buf = two ? i : j & 1, bar = two ? i : 2 * buf, phase = two ? cnt + j : (buf ? cnt2 : cnt) + (j >> 1);
-                bool there = mbar_wait_short(&S.s_full[bar], phase & 1, a.status, DEV_TIMEOUT_MMA, &S.abort), o_waited = two || j == 0;
+                bool there = mbar_wait_short(&S.s_full[bar], phase & 1, a.status, DEV_TIMEOUT_MMA, &S.patience), o_waited = two || j == 0;
                 there = __all_sync(0xffffffffu, there);
                 release(0, j);
                 if (two && j > 0) release(1, j - 1);
@@ -712,7 +714,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                 auto o_ready = [&]() {  // (with two tiles S of this block has come after O of the one before)
                     bool o = true;
                     if (!o_waited) {
-                        o = mbar_wait_short(&S.o_done[0], (o_phase + j - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
+                        o = mbar_wait_short(&S.o_done[0], (o_phase + j - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.patience);
                         release(1, j - 1);
                     }
                     o_waited = true;
@@ -727,8 +729,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (!two) cnt2 += nb / 2;
             o_phase += two ? 1 : nb;
             const int si = sn % L::RING_SEGS;
-            bool there = mbar_wait_short(&S.o_done[i], (o_phase - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.abort);
-            if (there && ends) there = mbar_wait_short(&S.notes_made[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.abort);
+            bool there = mbar_wait_short(&S.o_done[i], (o_phase - 1) & 1, a.status, DEV_TIMEOUT_MMA, &S.patience);
+            if (there && ends) there = mbar_wait_short(&S.notes_made[si], (sn / L::RING_SEGS) & 1, a.status, DEV_TIMEOUT_DEP, &S.patience);
             release(1, nb - 1);
             if (!ok || pair_any(id, !there)) break;
             top[half * ROWS + w * 32 + lane] = r.l;
@@ -904,6 +906,7 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     a.workers = std::min(gemm_ctas(), TREE_MAX_WORKERS);
     if (a.workers < 1) return cudaErrorInvalidDevice;
+    a.patience = tree_patience(tree_places(a.kv, a.hq), a.workers);
     CUtensorMap kmap{}, vmap{};
     int step = 0;
     const int box = tree_box(a.kv, &kmap, &vmap, &step);
@@ -916,12 +919,16 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p) {
-    // (places of the list are counted in 32 bits)
+double tree_places(const KvView &kv, int hq) {
     const int most = rows_all(kv.d), group = hq / kv.hkv;
     const double units = (double)kv.B * kv.hkv * ((TREE_NODES * group + most - 1) / most);
     const int cost = kv.d == 64 ? Cost<64>::TWO : Cost<128>::TWO, row = kv.d == 64 ? Cost<64>::ROW : Cost<128>::ROW;
-    if (units * ((double)((kv.cap + KEYS - 1) / KEYS) * cost + row) >= 2147483647.0) return false;
+    return units * ((double)((kv.cap + KEYS - 1) / KEYS) * cost + row);
+}
+
+bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p) {
+    const int most = rows_all(kv.d), group = hq / kv.hkv;
+    if (tree_places(kv, hq) >= 2147483647.0) return false;  // (counted in 32 bits)
     p->rows = std::min({most, TREE_NODES * group, std::min(T, 1 << 16) * group});
     size_t at = 1024;
     auto take = [&](size_t bytes) {
