@@ -260,12 +260,14 @@ size_t pbd_op_tree_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t T, 
  * when both are there.  d_lens and d_weights are not changed.  pbd_op_commit_path then makes an accepted path contiguous.
  * Rounding, infinite and NaN values of V as pbd_op_prompt_attention; a node does not touch those that do not descend from it.
  * Requirements: T <= 2^30; scale > 0; d_q, d_k_new, d_v_new and d_out 16-byte aligned, row strides multiples of 8 below 2^38; no page
- * in use is named twice among those that new rows go to; nothing that the call writes lies over anything else that it reads or writes.  The
- * workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 bounds that descend, lie outside [0, T]
+ * in use is named twice among those that new rows go to; nothing that the call writes lies over anything else that it reads or writes; the
+ * table has room for no more than 2^31 - 2 places in all (else PBD_ERR_CAPACITY, and 0 workspace bytes): with R = min(64, T) *
+ * (n_q_heads / n_kv_heads), each of min(batch, T) sequences, n_kv_heads heads and ceil(R / 256) chunks (head_dim 256: ceil(R / 128)) counts 4
+ * places and one for every 128 slots of its table row; at head_dim 64 10 and two, three where R > 128.
+ * The workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 bounds that descend, lie outside [0, T]
  * or span more than 64 rows, a sequence that begins below any bound in front of its own, or a length outside [0, max_pages * page_size -
- * nodes]: the sequence is left out; 7 a page
- * outside [0, n_pages): its slots, new nodes' among them, take no part and are not stored; 9 a parent that is not before
- * its node: it counts as -1. */
+ * nodes]: the sequence is left out; 7 a page outside [0, n_pages): its slots, new nodes' among them, take no part and are not stored; 9 a
+ * parent that is not before its node: it counts as -1. */
 pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_heads, float scale, const void *d_q,
                                  int64_t q_stride, const void *d_k_new, const void *d_v_new, int64_t new_stride,
                                  const int32_t *d_starts, const int32_t *d_parents_opt, const int32_t *d_new_positions_opt,

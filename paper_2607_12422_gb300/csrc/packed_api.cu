@@ -172,7 +172,7 @@ pbd_status pbd_op_tree_attention(const pbd_kv_pages *kv, int32_t T, int32_t n_q_
         return fail(PBD_ERR_INVALID_ARG, who, "32-bit arrays must be 4-byte aligned");
     TreePlan p;
     const KvView v = view(*kv);
-    if (!tree_plan(v, T, n_q_heads, &p)) return fail(PBD_ERR_CAPACITY, who, "more than 2^31 blocks of 128 slots in all heads and sequences");
+    if (!tree_plan(v, T, n_q_heads, &p)) return fail(PBD_ERR_CAPACITY, who, "the table has room for more places than the list holds (2^31 - 2; pbd_ops.h)");
     const size_t need = p.total;
     if (const char *w = bad_workspace(d_ws, ws_bytes, need)) return fail(PBD_ERR_WORKSPACE, who, w);
     if (const char *w = k_over_v(kv)) return fail(PBD_ERR_INVALID_ARG, who, w);

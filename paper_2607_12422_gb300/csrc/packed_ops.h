@@ -80,7 +80,7 @@ struct TreePlan {
     size_t codes, part_ml, part_o, total;  // offsets in the workspace
     int rows;
 };
-double tree_places(const KvView &kv, int hq);  // of the list at most
+double tree_places(const KvView &kv, int T, int hq);  // of the list at most
 bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p);
 cudaError_t launch_tree_attention(PackedArgs &a, cudaStream_t st);
 

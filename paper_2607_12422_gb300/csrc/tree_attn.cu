@@ -61,7 +61,7 @@ template <int D>
 __device__ __forceinline__ int chunks_of(int rows) { return (rows + TreeShape<D>::ROWS_ALL - 1) / TreeShape<D>::ROWS_ALL; }
 // of a block of such a sequence's units (the last of several may be of one tile)
 template <int D>
-__device__ __forceinline__ int cost_of(int rows) { return TreeShape<D>::TILES == 2 && rows > ROWS ? Cost<D>::TWO : Cost<D>::ONE; }
+__host__ __device__ __forceinline__ int cost_of(int rows) { return TreeShape<D>::TILES == 2 && rows > ROWS ? Cost<D>::TWO : Cost<D>::ONE; }
 
 // Whole CTA; returns the list's length.  bad: whether this thread has seen a sequence that is left out.  (Up to 32 sequences are one warp's: what comes before the first copy is what a small call waits for.)
 template <int D>
@@ -906,7 +906,7 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     a.workers = std::min(gemm_ctas(), TREE_MAX_WORKERS);
     if (a.workers < 1) return cudaErrorInvalidDevice;
-    a.patience = tree_patience(tree_places(a.kv, a.hq), a.workers);
+    a.patience = tree_patience(tree_places(a.kv, a.T, a.hq), a.workers);
     CUtensorMap kmap{}, vmap{};
     int step = 0;
     const int box = tree_box(a.kv, &kmap, &vmap, &step);
@@ -919,16 +919,18 @@ cudaError_t launch(PackedArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-double tree_places(const KvView &kv, int hq) {
-    const int most = rows_all(kv.d), group = hq / kv.hkv;
-    const double units = (double)kv.B * kv.hkv * ((TREE_NODES * group + most - 1) / most);
-    const int cost = kv.d == 64 ? Cost<64>::TWO : Cost<128>::TWO, row = kv.d == 64 ? Cost<64>::ROW : Cost<128>::ROW;
-    return units * ((double)((kv.cap + KEYS - 1) / KEYS) * cost + row);
+double tree_places(const KvView &kv, int T, int hq) {
+    // (no row is two sequences': T rows are those of T sequences at most, and of a sequence as many)
+    const int most = rows_all(kv.d), rows = std::min(TREE_NODES, T) * (hq / kv.hkv);
+    const double units = (double)std::min(kv.B, T) * kv.hkv * ((rows + most - 1) / most), blocks = (double)((kv.cap + KEYS - 1) / KEYS);
+    const int cost = kv.d == 64 ? cost_of<64>(rows) : kv.d == 128 ? cost_of<128>(rows) : cost_of<256>(rows);
+    const int row = kv.d == 64 ? Cost<64>::ROW : kv.d == 128 ? Cost<128>::ROW : Cost<256>::ROW;
+    return units * (blocks * cost + row);
 }
 
 bool tree_plan(const KvView &kv, int T, int hq, TreePlan *p) {
     const int most = rows_all(kv.d), group = hq / kv.hkv;
-    if (tree_places(kv, hq) >= 2147483647.0) return false;  // (counted in 32 bits)
+    if (tree_places(kv, T, hq) >= 2147483647.0) return false;  // (counted in 32 bits)
     p->rows = std::min({most, TREE_NODES * group, std::min(T, 1 << 16) * group});
     size_t at = 1024;
     auto take = [&](size_t bytes) {
