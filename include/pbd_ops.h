@@ -235,7 +235,8 @@ size_t pbd_op_prompt_attention_workspace_bytes(int32_t T, int32_t batch, int32_t
  * Score, softmax and output sums are fp32; p is rounded to the type for the tensor cores (relative to the row's largest weight, so the
  * error is a rounding's share of each p_j v_j), and out once more.
  * A value of V that is infinite or NaN makes its dimension NaN or infinite in the outputs of the rows and heads that see it, and
- * no other; K and V of rows that a row does not see do not touch it, whatever they hold.  Finite values of V: in bf16 at most 2^123 / T.
+ * no other; K and V of rows that a row does not see do not touch it, whatever they hold.  Finite values of V: in bf16 at most 2^123 / T
+ * (fp32 sums of p v, p up to 16, must not overflow).
  * Requirements: head_dim 64, 128 or 256; n_q_heads a multiple of n_kv_heads; batch <= 1024; scale > 0; d_q, d_k, d_v and d_out 16-byte
  * aligned, row strides multiples of 8 below 2^38; no slot twice; nothing that the call writes lies over anything else that it reads or writes.
  * The workspace (1024-byte aligned) is scratch; its first word is the status word for pbd_op_status: 5 a sequence whose bounds
@@ -258,7 +259,8 @@ size_t pbd_op_tree_attention_workspace_bytes(const pbd_kv_pages *kv, int32_t T, 
  * d_k_new, d_v_new: the nodes' own K and V, T rows new_stride values apart of [n_kv_heads, head_dim].  They are stored into slots
  * d_lens[b] + i (whose pages the table must name), and node i's position goes to d_positions from d_new_positions_opt [T]
  * when both are there.  d_lens and d_weights are not changed.  pbd_op_commit_path then makes an accepted path contiguous.
- * Rounding, infinite and NaN values of V as pbd_op_prompt_attention; a node does not touch those that do not descend from it.
+ * Rounding, infinite and NaN values of V as pbd_op_prompt_attention; a node does not touch those that do not descend from it.  Finite values of
+ * V, cached ones and nodes' own: in bf16 at most 2^123 / (d_lens[b] + nodes), the keys that a row's sums may have (not / T).
  * Requirements: T <= 2^30; scale > 0; d_q, d_k_new, d_v_new and d_out 16-byte aligned, row strides multiples of 8 below 2^38; no page
  * in use is named twice among those that new rows go to; nothing that the call writes lies over anything else that it reads or writes; the
  * table has room for no more than 2^31 - 2 places in all (else PBD_ERR_CAPACITY, and 0 workspace bytes): with R = min(64, T) *
