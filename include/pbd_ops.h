@@ -285,8 +285,8 @@ size_t pbd_op_commit_path_workspace_bytes(const pbd_kv_pages *kv, int32_t max_pa
  * Requirements: 1 <= max_path <= 64; no page in use is named twice; nothing that the call writes (K, V, weights, positions, the workspace)
  * lies over anything else that it reads or writes.  The workspace (1024-byte aligned) is scratch; its first word is the status word for
  * pbd_op_status: 5 a number outside [0, max_path] or a length outside [0, max_pages * page_size], 9 a path that does not
- * ascend or leaves the tree's 64 nodes or the table: that sequence is left as it is; 7 a page outside [0, n_pages): moves
- * from and to its slots are left out. */
+ * ascend or leaves the tree's 64 nodes or the table: that sequence is left as it is, whatever its pages are; 7 a page outside
+ * [0, n_pages): moves from and to its slots are left out.  (Of several sequences' faults one is reported.) */
 pbd_status pbd_op_commit_path(const pbd_kv_pages *kv, const int32_t *d_path, int32_t max_path, const int32_t *d_n_accepted,
                               void *d_ws, size_t ws_bytes, void *d_stream);
 

@@ -240,8 +240,11 @@ __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constan
         }
         of[i] = from, to[i] = dest, slot_of[i] = len + p;
     }
-    if (h == 0 && (bad || bad_page)) report(a, bad ? DEV_BAD_TREE : DEV_BAD_PAGE);
-    if (__syncthreads_or(bad)) return pdl_wait();  // the sequence stays as it is
+    if (__syncthreads_or(bad)) {  // the sequence stays as it is, whatever its pages are
+        if (h == 0 && bad) report(a, DEV_BAD_TREE);
+        return pdl_wait();
+    }
+    if (h == 0 && bad_page) report(a, DEV_BAD_PAGE);
     for (int x0 = i; x0 < n * 2 * CPR + i; x0 += U * CP_THREADS) {
         uint4 piece[U];
 #pragma unroll

@@ -109,6 +109,8 @@ def test_trees(env, code, kw, D):  # noqa: F811
     (BAD_LENGTH, [[2, 5, 9], [1, 2, 3]], [3, 4], [20, 30], None), (BAD_LENGTH, [[2, 5, 9], [1, 2, 3]], [3, -1], [20, 30], None),
     (BAD_LENGTH, [[2, 5, 9], [1, 2, 3]], [3, 3], [20, -1], None), (BAD_LENGTH, [[2, 5, 9], [1, 2, 3]], [3, 3], [20, 57], None),
     (BAD_PAGE, [[2, 5, 9], [1, 5, 12]], [3, 3], [20, 30], 4),
+    # of one sequence: what its path says before its pages
+    (BAD_TREE, [[2, 5, 9], [5, 5, 12]], [3, 3], [20, 30], 4),
 ], ids=str)
 def test_paths(env, code, path, n, lens, page):  # noqa: F811
     torch, pbd = env
