@@ -163,20 +163,20 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, int *s
     return ok;
 }
 
-// The same in fewer instructions and registers, for kernels whose warps run different code: one that runs little beside others that run
-// much fetches its instructions anew each time.  patience: what the CTA's waits share, the limit in units of 2^20 ns, 0 once one has run out;
-// null: WAIT_LIMIT_NS.
+// The same in fewer instructions, for kernels whose warps run different code: one that runs little beside others that run much
+// fetches its instructions anew each time.  patience: what the CTA's waits share, the limit in units of 2^20 ns, 0 once one has run out;
+// null: WAIT_LIMIT_NS.  (With the clock held in 32 bits 32 ragged prompts take 78.6 us instead of 80.5, but 1000 prompts of 40 tokens, whose
+// rows are stored by a kernel beside this one, 228 instead of 214.)
 constexpr uint32_t WAIT_PATIENCE = (uint32_t)(WAIT_LIMIT_NS >> 20) + 1;
 __device__ __forceinline__ bool mbar_wait_short(uint64_t *bar, uint32_t parity, int *status, int code, volatile uint32_t *patience) {
     const uint32_t a = smem_u32(bar);
-    uint32_t t0 = 0;
+    uint64_t t0 = 0;
 #pragma unroll 1
     for (uint32_t n = 1; !mbar_try_wait(a, parity); ++n) {
         if (n & 127) continue;
-        const uint32_t t = (uint32_t)(globaltimer_ns() >> 20);
+        const uint64_t t = globaltimer_ns();
         t0 = t0 ? t0 : t;
-        const uint32_t limit = patience ? (uint32_t)*patience : (uint32_t)WAIT_PATIENCE;
-        if (t - t0 < limit) continue;
+        if ((t - t0) >> 20 < (patience ? (uint32_t)*patience : (uint32_t)WAIT_PATIENCE)) continue;
         latch_error(status, code);
         if (patience) *patience = 0;
         return false;
