@@ -197,8 +197,8 @@ __global__ void __launch_bounds__(AP_EXPAND) k_expand_slots(const __grid_constan
 // finds wrong (one CTA that looks at all paths takes 50 us for 512 of them).
 constexpr int CP_THREADS = 128;
 
-// whether the path of sequence b can be walked
-__device__ __forceinline__ bool path_ok(const CommitArgs &a, int b, int n, int len) {
+// whether a path of n nodes behind len slots can be walked
+__device__ __forceinline__ bool path_ok(const CommitArgs &a, int n, int len) {
     return n >= 0 && n <= a.max_path && len >= 0 && len <= a.kv.cap;
 }
 
@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(CP_THREADS) k_commit_path(const __grid_constan
     __shared__ int slot_of[TREE_NODES];
     const int b = blockIdx.x / a.kv.hkv, h = blockIdx.x - b * a.kv.hkv;
     const int n = a.n_accepted[b], len = a.kv.lens[b], i = threadIdx.x;
-    if (!path_ok(a, b, n, len)) {
+    if (!path_ok(a, n, len)) {
         if (h == 0 && i == 0) report(a, DEV_BAD_POSITION);
         return pdl_wait();
     }

@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             uint8_t *units = ring + kv * STAGES * L::UNIT;
             int issued = 0, block = 0, sn = 0;
             bool ok = true;
-            int pend = -1, pend_u = 0, pend_t = 0;  // the unit of rows that has still to be looked at
+            int pend = -1, pend_t = 0;  // the unit of rows that has still to be looked at
             // What a lane says of a unit that it has copied: with tiled copies one lane for its warp.
             auto arrive = [&](uint64_t *bar) {
                 if (box) __syncwarp();
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                             cp_async_wait_1();
                             finish();
                         }
-                        pend = slot, pend_t = t, pend_u = u;
+                        pend = slot, pend_t = t;
                     }
                 }
                 if (ok && pend >= 0) {
