@@ -121,12 +121,16 @@ class Ranges {
         bool written;
     } r[16];
     int n = 0;
-    bool has_cache = false;  // (its K and V come first)
+    bool has_cache = false, full = false;  // (its K and V come first); whether there was one more than there is room for
     char text[96];
 
 public:
     void add(const char *name, const void *p, long long bytes, bool written) {
-        if (p && n < 16) r[n++] = Range{p, bytes, name, written};
+        if (!p) return;
+        if (n == 16)
+            full = true;
+        else
+            r[n++] = Range{p, bytes, name, written};
     }
     void cache(const pbd_kv_pages *kv, bool written) {
         has_cache = true;
@@ -136,6 +140,7 @@ public:
         add("the lengths", kv->d_lens, 4ll * kv->batch, false);
     }
     const char *clash() {
+        if (full) return "the call has more arrays than are compared";
         for (int i = 0; i < n; ++i)
             for (int j = 0; j < n; ++j) {
                 if (i == j || !r[i].written || !overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes)) continue;
