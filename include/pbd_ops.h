@@ -228,10 +228,11 @@ size_t pbd_op_prompt_attention_workspace_bytes(int32_t T, int32_t batch, int32_t
  *     s_j = q . k_j,  p = softmax(scale * s),  out = sum_j p_j v_j,  lse = ln sum_j exp(scale * s_j).
  * d_q: T rows q_stride values apart of [n_q_heads, head_dim]; d_k, d_v: T rows kv_stride values apart of [n_kv_heads, head_dim], so that the
  * three may be parts of one projection's rows; d_out [T, n_q_heads, head_dim]; all of type dtype, PBD_BF16 or PBD_FP16.
- * d_lse_opt [T, n_q_heads] fp32 or NULL.  Rows of no sequence are neither read nor written.
+ * d_lse_opt [T, n_q_heads] fp32 or NULL.  Rows of no sequence are neither read nor written.  A row sees rows of the call alone, nothing that
+ * is cached already: prompts begin at an empty cache, or come whole.
  * kv_opt with d_slots_opt [T] (both or neither): K and V of each sequence's row t are stored into slot d_slots_opt[t] of the cache (its page's
  * number times page_size plus the place there, as pbd_op_assign_pages gives it); negative: not stored.  Of the cache K, V, sizes and strides
- * count, not table and lengths.
+ * count, not table and lengths (which have to be named all the same).
  * Score, softmax and output sums are fp32; p is rounded to the type for the tensor cores (relative to the row's largest weight, so the
  * error is a rounding's share of each p_j v_j), and out once more.
  * A value of V that is infinite or NaN makes its dimension NaN or infinite in the outputs of the rows and heads that see it, and

@@ -23,6 +23,9 @@ namespace {
 // the same kernel; more by a second one.
 constexpr int AP_THREADS = 1024;
 static_assert(KV_MAX_BATCH <= AP_THREADS, "a thread a sequence");
+// (Two calls of 64 sequences, us, by the packed rows of each: one CTA 13.0 / 14.2 / 17.3 / 23.2 with 500 / 2000 / 4000 / 8000 rows, a cluster 15.2 /
+// 15.4 / 15.3 / 15.4: they meet near 2500.  A cluster alone 15.4 / 17.4 / 20.7 / 26.5 / 59 with 8000 / 16000 / 32000 / 64000 / 220000, with the second
+// kernel 15.4 / 15.9 / 16.3 / 15.9 / 19.4: they meet near 8000.)
 constexpr int AP_CLUSTER = 8;   // CTAs where pages or rows are many
 constexpr int AP_FEW = 4096;    // pages and packed rows that one CTA deals with
 constexpr int AP_ROWS = 32768;  // packed rows that a cluster expands itself

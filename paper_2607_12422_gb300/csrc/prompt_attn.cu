@@ -16,9 +16,10 @@
 // rows of V behind the sequence's end become zero, infinite and NaN values too, and the first row that sees one is noted for each dimension; from
 // that row on the result is NaN there.
 //
-// 16384 tokens, 16 heads of 128 on 8 KV heads, stored: 677-725 us, 1.5 to 1.6 PFLOP/s, the tensor core busy 70 % of the time and waiting for the chain
-// scores, softmax, P V of two tiles (1400 cycles a tile and block, 1050 of them products).  Eight ragged prompts of 420 to 1757: 54 us; 32 ragged
-// ones, groups of seven heads of 64: 88 us, of which 8 are spent before the first scores and half of the rest on items' first and last blocks.
+// 16384 tokens, 16 heads of 128 on 8 KV heads, stored: 680-727 us, 1.5 to 1.6 PFLOP/s, the tensor core busy 70 % of the time and waiting for the chain
+// scores, softmax, P V of two tiles (1400 cycles a tile and block, 1050 of them products).  Eight ragged prompts of 420 to 1757: 54 us, 36 blocks of a tile a
+// CTA on average and 44 in the fullest; 32 ragged ones, groups of seven heads of 64: 81 us.  The first scores are there 4 (512 tokens) to 7 us after a
+// CTA's start.  Heads of 256, one tile a CTA: the eight 106 us, 8192 tokens 380-398 us (1.4 PFLOP/s).
 //
 // Warps 0-15: the tiles' rows.  Warp 16: TMA.  Warps 17 and 18: the tiles' MMAs (one thread for both spent more on issuing and waiting
 // than the tensor core on multiplying: 16384 tokens 916 us).  Warp 19: the list, and V of items done again.
@@ -115,7 +116,7 @@ __device__ __forceinline__ bool find_item(const PackedArgs &a, const int *start,
 // Stores K and V into the cache, beside k_prompt: a warp a row.  Its CTAs fit an SM together with k_prompt's, whose registers leave 4096.  (By
 // k_prompt's own threads, before an item's first scores, it costs them registers that they lack.)  Beside k_prompt's warps its own fetch their code
 // anew for every row, and that bounds it: a short loop without divisions and unrolling, the next row's slot on its way (1000 prompts of 40
-// tokens, 8 KV heads of 128: 215 us with k_prompt's 192, 295 before; two warps a CTA with all of a row's loads on their way: 857).
+// tokens, 8 KV heads of 128: 215 us, 211 alone, k_prompt alone 192; 295 before; two warps a CTA with all of a row's loads on their way: 857).
 constexpr int PS_WARPS = 4;
 __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid_constant__ PackedArgs a) {
     __shared__ int start[KV_MAX_BATCH], end[KV_MAX_BATCH];
@@ -559,8 +560,10 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t st) {
         return x != cudaSuccess ? x : cudaFuncSetAttribute(k_prompt_store, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     });
     if (e != cudaSuccess) return e;
-    // the largest divisor of the group up to 16 that leaves at most 8 rows over.  (32 ragged prompts, groups of seven: 95 us with
-    // 7 heads a tile, 107 with one.)
+    // the largest divisor of the group up to 16 that leaves at most 8 rows over.  (One head a tile instead: 1000 prompts of 40 tokens 392 us instead of
+    // 216, 32 ragged ones in groups of seven 95.5 instead of 81, eight in groups of 16 53.8 instead of 50.3, of 32 98 instead of 90.6.  Up to 8 or 32:
+    // within 1 %.  No row left over: groups of seven have one head a tile then.  Up to 16 rows: a group of 13 has 13 heads a tile, 49.1 us
+    // instead of 48.8: K and V come from the L2 when each head reads them.)
     int P = std::min(a.group, 16);
     while (a.group % P || ROWS % P > 8) --P;
     const uint32_t inv_p = 65536 / P + 1;

@@ -10,8 +10,10 @@
 // of about the same cost: how ragged the lengths are does not matter, and the host need not know them.  Where a stretch begins or ends
 // inside a (sequence, KV head) the CTA leaves maximum, sum and unnormalised output in scratch, and k_tree_join joins them.
 //
-// 64 nodes behind 131071 slots, heads of 128: 105 us, between first and last block 6.4 TB/s (1.54 us a block of 64 KB an SM).  Heads of 64: a block takes
-// the rows 1.0 us (memory 0.76), of two tiles 1.5.  17 nodes behind 512: 14.5 us, of which 8 pass before the first scores.
+// 64 nodes behind 131071 slots, heads of 128: 106 us, between first and last block 6.4 TB/s (1.54 us a block of 64 KB an SM); the first scores are there
+// 7 us after the start, and the join ends 11 us after the last block.  Heads of 64: a block takes the rows 1.0 us (memory 0.76), of two tiles 1.5.
+// 17 nodes behind 512: 15 us, of which 5 pass before the first scores (7 with cold caches) and 3 in the join.  Heads of 256: 64 nodes behind 65535 slots
+// 117 us, 4.6 TB/s in all.  Row by row, 16 bytes a lane (pages of 5 slots, of one): the first case takes 223 and 255 us.
 //
 // Warps 0-15: rows (queries, softmax, outputs).  Warp 16 copies K, warp 17 V: tiled copies of the rows that a page has in a piece where
 // pages hold a multiple of 8, row by row else, 16 bytes a lane.  Warps 18 and 19: the tiles' MMAs.
@@ -31,13 +33,17 @@ using namespace flash;
 namespace {
 
 // Costs in places: of a block of a unit of one tile, of two, and of a unit besides.  Heads of 64: by the rows' work (1.0 and 1.5 us; 5 us); else
-// memory bounds both (1.5 us; 6 us).  (64 sequences of 1 to 26 nodes, seven heads a KV head, us, with a slower join: 92 with two blocks for a unit and
-// one cost for both, 83 with 8 places for a unit, 76 with 10, 79 with 18.  Eight of up to 64 nodes, heads of 128: 26.5 with 2, 24.9 with 4, 25.2 with 6.)
+// memory bounds both (1.5 us; 6 us).  Measured, us, with places for a unit in front of the colon:
+//     64 sequences of 1 to 26 nodes, seven heads of 64 a KV head      2: 110  6: 81  10: 69  14: 72  18: 75; one cost for all blocks and 3: 81
+//     eight of up to 64 nodes, heads of 128                           1: 27.2  2: 27.2  4: 25.6  6: 26.1  8: 26.1  12: 27.4
+//     64 nodes behind 131071 slots, heads of 128                      1: 103.7  2: 107  4: 106  6: 104.5  8: 104.2  12: 103.5
+//     the eight, heads of 256                                         1: 41.2  2: 41.3  4: 40.0  6: 41.6  8: 42.9
+//     the 64, heads of 256                                            1: 245  2: 214  4: 177  6: 174  8: 182
 template <int D>
 struct Cost {
     static constexpr int ONE = D == 64 ? 2 : 1, TWO = D == 64 ? 3 : 1, ROW = D == 64 ? 10 : 4;
 };
-constexpr int TA_MIN = 3;        // places of a CTA's stretch at least (17 nodes behind 512 slots: 15.8 us, with 6 18.1)
+constexpr int TA_MIN = 3;        // places of a CTA's stretch at least (17 nodes behind 512 slots: 14.7 us, with 4 15.5, with 6 16.9)
 static_assert(TA_MIN >= Cost<64>::TWO, "who is in the middle of a unit has a block");
 constexpr int TA_MASKS = 8;      // blocks whose masks are kept
 
@@ -782,7 +788,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 // Joins the parts of units that several CTAs worked on: a warp 32 dimensions of four rows of a unit (node by node, the heads of its
 // group innermost), eight lanes a row.  Parts are taken eight at a time, whose loads go out together (one after the other, 64 nodes
 // behind 131071 slots, whose units have 20 parts, took 50 us here).  Every CTA counts the tasks of such units, so that all warps get as
-// many (going over all rows instead and leaving out most: 64 ragged sequences 75.6 us, now 71.3; 17 nodes behind 512 slots 16, now 14.5).
+// many (going over all rows instead and leaving out most: 64 ragged sequences 75.6 us instead of 71.3; 17 nodes behind 512 slots 16 instead of 14.5).
 // The first CTA reports.
 constexpr int TJ_WARPS = 8, TJ_ROWS = 4;
 static_assert(TREE_MAX_WORKERS <= 32 * TJ_WARPS, "a thread a CTA of k_tree");
