@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(32 * PS_WARPS, 16) k_prompt_store(const __grid
     for (int b = threadIdx.x; b < a.B; b += 32 * PS_WARPS) {
         const int s = a.starts[b], e = a.starts[b + 1];
         start[b] = s;
-        end[b] = bounds_ok(a, s, e) ? e : s;
+        end[b] = s < 0 || e > a.T ? s : e;  // (between bounds that descend there is no row)
         descends |= e < s;
     }
     if (__syncthreads_or(descends)) {
