@@ -296,8 +296,8 @@ pbd_status pbd_op_commit_path(const pbd_kv_pages *kv, const int32_t *d_path, int
  * kernel latched an error; PBD_ERR_DEVICE with the latched code in *h_device_code (may be NULL) otherwise, and that
  * call's outputs are invalid; PBD_ERR_INVALID_ARG for a null or misaligned d_ws; PBD_ERR_CUDA if the stream failed.
  * What kernels latch: a device wait that runs out, after one second (1, 2, 3 or 6: linear, lm_head, token_logprobs, prompt and tree
- * attention; in the last two one and 32 us for each 128 keys of a call's longest possible work between two waits), and lengths, pages (7; 8: none left), trees (9) and tokens (4) in device memory that lie outside their range (5: a
- * length), which the host cannot check. */
+ * attention; in the last two one and 32 us for each 128 keys of a call's longest possible work between two waits), and lengths, pages (7;
+ * 8: none left), trees (9) and tokens (4) in device memory that lie outside their range (5: a length), which the host cannot check. */
 pbd_status pbd_op_status(const void *d_ws, void *d_stream, int32_t *h_device_code);
 
 /* Message of the last failed pbd_op_* call on this thread ("" if none). */

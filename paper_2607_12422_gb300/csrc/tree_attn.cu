@@ -69,7 +69,8 @@ __device__ __forceinline__ int chunks_of(int rows) { return (rows + TreeShape<D>
 template <int D>
 __host__ __device__ __forceinline__ int cost_of(int rows) { return TreeShape<D>::TILES == 2 && rows > ROWS ? Cost<D>::TWO : Cost<D>::ONE; }
 
-// Whole CTA; returns the list's length.  bad: whether this thread has seen a sequence that is left out.  (Up to 32 sequences are one warp's: what comes before the first copy is what a small call waits for.)
+// Whole CTA; returns the list's length.  bad: whether this thread has seen a sequence that is left out.  (Up to 32 sequences are one
+// warp's: what comes before the first copy is what a small call waits for.)
 template <int D>
 __device__ __forceinline__ int tree_list(const PackedArgs &a, TreeList &T, bool &bad) {
     __shared__ int warp_sum[32], total;
